@@ -1,0 +1,1263 @@
+// Products on the tcgen05 tensor cores with both operands as they lie in HBM:
+// two 4-bit tensors with block scales (polyq_fp4_linear, polyq_fp4_ffn), or
+// 16-bit tensors (polyq_ffn_forward, polyq_ffn_backward).
+//
+//   D[m][n] = sum_k A[m][k] B[n][k]
+//
+// Every kind moves 128 bytes of each operand row per stage, four MMAs: 256
+// 4-bit or 64 16-bit elements of K.  Two kernels:
+//   mm_pair  many rows: persistent CTA pairs (cta_group::2), 256 rows of A by NT
+//            rows of B a tile, A the tokens, B the weights.
+//   mm_few   few tokens: the weights are A (128 rows a CTA), the tokens B; the
+//            CTAs of a cluster share the contraction and add their parts through
+//            distributed shared memory, in rank order.
+// GATED kernels hold gate and up side by side in tensor memory, so that one
+// thread has both values of an output and applies the activation and the
+// product in registers.  Every wait is bounded and reports through the
+// workspace status word.
+#include <cuda.h>
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+
+#include <algorithm>
+#include <atomic>
+#include <cmath>
+#include <cstring>
+
+#include "polyq_dev.cuh"
+#include "polyq_fp4_dev.cuh"
+#include "polyq_internal.h"
+#include "polyq_tc.cuh"
+
+namespace {
+
+using namespace polyq;
+using namespace polyq::tc;
+
+constexpr int k16 = 0, kMx = 1, kNv = 2;  // operand kinds
+constexpr int kTileM = 256;               // rows of A of a pair's tile
+constexpr int kHalf = 128;                // of which each CTA holds half
+constexpr int kRowBytes = 128;            // an operand row in a stage
+constexpr int kOpBytes = kHalf * kRowBytes;
+constexpr int kSmemMax = 227 * 1024 - 1024;  // less the static barriers
+constexpr int kMaxDevices = 64;
+
+struct MmParams {
+  CUtensorMap a[2], b[2];  // operand tiles (per segment, problem or matrix, see below)
+  CUtensorMap sa, sb[2];   // scales, rows of one atom
+  int M, N;                // output rows (A) and columns (B), of one problem
+  int kt, k_last;          // stages of a segment, MMAs of its last stage
+  int segs;                // segments of the contraction: a[s] with b[s]
+  int probs;               // problems: a[p] with b[0]
+  int tiles_m, tiles_n, tiles;
+  int a_mn, b_mn;          // operand has M (N) contiguous instead of K
+  int atoms;               // scale atoms of a row group
+  uint32_t idesc;
+  float alpha[2];          // tensor scales of the result (GATED: of gate, of up)
+  // outputs: y[p], of `type`; or 4 bits; and the saved gate and up values
+  void* y[2];
+  const void* res;
+  int64_t y_stride, res_stride;
+  int type, vec;           // vec: rows of y and res start on 16 bytes
+  uint8_t *codes, *scales;
+  int64_t code_stride, out_atoms;
+  int qfmt;                // 0, kMx or kNv
+  float g, inv_g;
+  void* saved[2];
+  int64_t saved_stride;
+  int* status;
+};
+
+__device__ __forceinline__ float silu(float a) { return __fdividef(a, 1.f + __expf(-a)); }
+
+__device__ __forceinline__ uint32_t pack16(float lo, float hi, bool bf16) {
+  if (bf16) {
+    const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&v);
+  }
+  const __half2 v = __floats2half2_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&v);
+}
+__device__ __forceinline__ float load_dense(const void* p, int64_t i, int type) {
+  return type == POLYQ_F32    ? ((const float*)p)[i]
+         : type == POLYQ_BF16 ? __bfloat162float(((const __nv_bfloat16*)p)[i])
+                              : __half2float(((const __half*)p)[i]);
+}
+__device__ __forceinline__ void store_dense(void* p, int64_t i, float v, int type) {
+  if (type == POLYQ_F32) ((float*)p)[i] = v;
+  else if (type == POLYQ_BF16) ((__nv_bfloat16*)p)[i] = __float2bfloat16_rn(v);
+  else ((__half*)p)[i] = __float2half_rn(v);
+}
+// fp16 keeps a saved finite value finite.
+__device__ __forceinline__ float saved_range(float v, bool bf16) {
+  return bf16 || fabsf(v) == INFINITY ? v : v > 65504.f ? 65504.f : v < -65504.f ? -65504.f : v;
+}
+
+// 32 consecutive values of a row, the first n of them inside.
+__device__ __forceinline__ void store_row32(void* y, int64_t off, const float (&v)[32], int n, int type,
+                                            bool vec) {
+  if (vec && n == 32) {
+    if (type == POLYQ_F32) {
+      float4* d = reinterpret_cast<float4*>((float*)y + off);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) d[i] = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+    } else {
+      uint4* d = reinterpret_cast<uint4*>((uint16_t*)y + off);
+      const bool b = type == POLYQ_BF16;
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        d[i] = make_uint4(pack16(v[8 * i], v[8 * i + 1], b), pack16(v[8 * i + 2], v[8 * i + 3], b),
+                          pack16(v[8 * i + 4], v[8 * i + 5], b), pack16(v[8 * i + 6], v[8 * i + 7], b));
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 32; ++i)
+      if (i < n) store_dense(y, off + i, v[i], type);
+  }
+}
+__device__ __forceinline__ void add_row32(const void* r, int64_t off, float (&v)[32], int n, int type,
+                                          bool vec) {
+  if (vec && n == 32) {
+    if (type == POLYQ_F32) {
+      const float4* s = reinterpret_cast<const float4*>((const float*)r + off);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float4 f = s[i];
+        v[4 * i] += f.x;
+        v[4 * i + 1] += f.y;
+        v[4 * i + 2] += f.z;
+        v[4 * i + 3] += f.w;
+      }
+    } else {
+      const uint4* s = reinterpret_cast<const uint4*>((const uint16_t*)r + off);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint4 u = s[i];
+        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          float2 f;
+          if (type == POLYQ_BF16) f = make_float2(bf16_lo(w[j]), bf16_hi(w[j]));
+          else f = __half22float2(*reinterpret_cast<const __half2*>(&w[j]));
+          v[8 * i + 2 * j] += f.x;
+          v[8 * i + 2 * j + 1] += f.y;
+        }
+      }
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 32; ++i)
+      if (i < n) v[i] += load_dense(r, off + i, type);
+  }
+}
+
+// 32 consecutive values of row m from column f0 (a multiple of 32) as one block
+// of 32 or two of 16; values past the row's end are 0.
+template <bool NV>
+__device__ __forceinline__ void store_codes32(const MmParams& P, int64_t m, int64_t f0, float (&v)[32]) {
+  uint32_t c[4];
+  constexpr int BL = NV ? 16 : 32;
+#pragma unroll
+  for (int b = 0; b < 32 / BL; ++b) {
+    uint32_t mx = 0;
+#pragma unroll
+    for (int i = 0; i < BL; ++i) {
+      if (NV) v[BL * b + i] = P.inv_g != 0.f ? v[BL * b + i] * P.inv_g : __fdiv_rn(v[BL * b + i], P.g);
+      mx = max(mx, __float_as_uint(v[BL * b + i]) & 0x7FFFFFFFu);
+    }
+    const fp4::Scale<NV> sc(mx);
+#pragma unroll
+    for (int i = 0; i < BL / 8; ++i) {
+      float q[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) q[j] = sc.div(v[BL * b + 8 * i + j]);
+      c[b * BL / 8 + i] = fp4::codes8(q);
+    }
+    const int64_t blk = f0 / BL + b;
+    if (blk >> 2 < P.out_atoms) P.scales[fp4::scale_off(m, blk, P.out_atoms)] = (uint8_t)sc.byte;
+  }
+  // rows are padded to 16 bytes: a chunk that starts inside the row fits
+  if (f0 < P.N) *reinterpret_cast<uint4*>(P.codes + m * P.code_stride + f0 / 2) = make_uint4(c[0], c[1], c[2], c[3]);
+}
+
+// ---------------------------------------------------------------------------
+// many rows: CTA pairs
+// ---------------------------------------------------------------------------
+template <int KIND_, int NT_, bool GATED_>
+struct Pair {
+  static constexpr int KIND = KIND_, NT = NT_;
+  static constexpr bool GATED = GATED_;
+  static constexpr int ATOMS = KIND == k16 ? 0 : KIND == kNv ? 4 : 2;  // scale atoms of a stage
+  static constexpr int GROUPS = NT / 128;                              // row groups of B's scales
+  static constexpr int kB = NT / 2 * kRowBytes;
+  static constexpr int kSa = ATOMS * 512, kSb = ATOMS * 512 * GROUPS;
+  static constexpr int kStage = kOpBytes + kB + kSa + kSb;
+  static constexpr int STAGES = (kSmemMax - 1024) / kStage;
+  static constexpr int kBOff = STAGES * kOpBytes, kSaOff = kBOff + STAGES * kB;
+  static constexpr int kSbOff = kSaOff + STAGES * kSa;
+  static constexpr size_t kSmem = (size_t)STAGES * kStage + 1024;
+  // Tensor memory: two accumulators of NT columns and two stages' scales.  With
+  // NT = 256 and scales the accumulators share OV columns: the epilogue drains
+  // those first and releases them for the next tile before the rest.
+  static constexpr int kSfStage = ATOMS * 4 * (1 + GROUPS);
+  static constexpr int kSfCols = (2 * kSfStage + 31) / 32 * 32;
+  static constexpr int kSfCol = NT == 256 ? 512 - kSfCols : 2 * NT;
+  static constexpr int kAcc1 = NT == 256 ? kSfCol - 256 : NT;
+  static constexpr int OV = NT - kAcc1;
+  static constexpr int kEpiWarp = 4, EPI = 8;
+  static constexpr int kThreads = 32 * (kEpiWarp + EPI);
+  static_assert(kSfCol + kSfCols <= 512 && OV % 32 == 0 && STAGES >= 4, "");
+};
+
+// The tiles of a pair, in order.  Tiles of eight row tiles are taken together,
+// rows fastest, so that the pairs at work share both operands through L2.
+struct Tiles {
+  int t;
+  __device__ __forceinline__ void init() { t = (int)(blockIdx.x >> 1); }
+  __device__ __forceinline__ bool next(const MmParams& P, int& prob, int& tm, int& tn) {
+    if (t >= P.tiles) return false;
+    const int per = P.tiles_m * P.tiles_n;
+    prob = t / per;
+    const int r = t - prob * per;
+    const int g = r / (8 * P.tiles_n), rows = min(8, P.tiles_m - 8 * g);
+    const int i = r - g * 8 * P.tiles_n;
+    tn = i / rows;
+    tm = 8 * g + (i - tn * rows);
+    t += (int)(gridDim.x >> 1);
+    return true;
+  }
+};
+
+template <class C>
+__global__ void __launch_bounds__(C::kThreads, 1) mm_pair(const __grid_constant__ MmParams P) {
+  extern __shared__ __align__(1024) uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
+                                             ~(uintptr_t)1023);
+  __shared__ uint64_t bar_full[C::STAGES];   // leader: both CTAs' copies of a stage have landed
+  __shared__ uint64_t bar_empty[C::STAGES];  // a stage's MMAs are done
+  __shared__ uint64_t bar_accf[2];           // an accumulator is complete
+  __shared__ uint64_t bar_acce[2];           // leader: both CTAs have drained it (OV: what is shared)
+  __shared__ uint64_t bar_done;              // every MMA is done
+  __shared__ uint32_t tmem_slot;
+  __shared__ volatile int s_abort;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t rank = cluster_ctarank();
+
+  if (threadIdx.x == 0) {
+    s_abort = 0;
+    for (int s = 0; s < C::STAGES; ++s) {
+      mbar_init(smem_u32(&bar_full[s]), 1);
+      mbar_init(smem_u32(&bar_empty[s]), 1);
+    }
+    for (int b = 0; b < 2; ++b) {
+      mbar_init(smem_u32(&bar_accf[b]), 1);
+      mbar_init(smem_u32(&bar_acce[b]), 2 * C::EPI);
+    }
+    mbar_init(smem_u32(&bar_done), 1);
+    mbar_fence_init();
+  }
+  if (warp == 1) {
+    tmem_alloc<2>(smem_u32(&tmem_slot), 512);
+    tmem_relinquish<2>();
+  }
+  tc_fence_before();
+  __syncthreads();
+  cluster_sync();
+  tc_fence_after();
+  const uint32_t tmem = tmem_slot;
+  pdl_trigger();
+
+  // A role gives up: both CTAs stop, and this one stays a thousand times the
+  // time of a copy, so that none lands after its CTA has left.
+  auto fail = [&](int code) {
+    s_abort = 1;
+    const uint32_t peer = mapa(smem_u32((const void*)&s_abort), rank ^ 1u);
+    asm volatile("st.relaxed.cluster.shared::cluster.u32 [%0], %1;" ::"r"(peer), "r"(1) : "memory");
+    atomicExch(P.status, code);
+    for (const long long t0 = clock64(); clock64() - t0 < kStayCycles;) __nanosleep(1000);
+  };
+  Tiles T;
+  T.init();
+  int prob, tm, tn;
+  const int n_it = P.segs * P.kt;
+
+  if (warp == 0) {
+    // ---------------- producer: this CTA's half of A, of B, and the scales ----------------
+    if (elect_one()) {
+      pdl_wait();
+      int s = 0;
+      uint32_t ph = 1;
+      const uint32_t full0 = mapa(smem_u32(&bar_full[0]), 0);
+      while (!s_abort && T.next(P, prob, tm, tn)) {
+        const int m0 = tm * kTileM + (int)rank * kHalf;
+        const int n0 = C::GATED ? tn * (C::NT / 2) : tn * C::NT + (int)rank * (C::NT / 2);
+        for (int i = 0; i < n_it; ++i) {
+          const int w = wait(smem_u32(&bar_empty[s]), ph, &s_abort);
+          if (w != kOk) {
+            if (w == kTimeout) fail(kStatusTimeoutEmpty);
+            break;
+          }
+          const int seg = i >= P.kt, kt = seg ? i - P.kt : i;
+          if (rank == 0) mbar_expect_tx(smem_u32(&bar_full[s]), 2 * C::kStage);
+          const uint32_t bar = full0 + 8 * s;
+          const uint32_t da = smem_u32(smem + s * kOpBytes);
+          const uint32_t db = smem_u32(smem + C::kBOff + s * C::kB);
+          const CUtensorMap* ma = &P.a[C::GATED ? 0 : seg + prob];
+          const CUtensorMap* mb = &P.b[C::GATED ? (int)rank : seg];
+          if (C::KIND == k16) {
+            if (!P.a_mn) {
+              tma_load_2d_pair(da, ma, kt * 64, m0, bar);
+            } else {
+              tma_load_2d_pair(da, ma, m0, kt * 64, bar);
+              tma_load_2d_pair(da + 8192, ma, m0 + 64, kt * 64, bar);
+            }
+            if (!P.b_mn) {
+              tma_load_2d_pair(db, mb, kt * 64, n0, bar);
+            } else {
+              tma_load_2d_pair(db, mb, n0, kt * 64, bar);
+              if (C::NT == 256) tma_load_2d_pair(db + 8192, mb, n0 + 64, kt * 64, bar);
+            }
+          } else {
+            tma_load_2d_pair(da, ma, kt * kRowBytes, m0, bar);
+            tma_load_2d_pair(db, mb, kt * kRowBytes, n0, bar);
+            const uint32_t sa = smem_u32(smem + C::kSaOff + s * C::kSa);
+            const uint32_t sb = smem_u32(smem + C::kSbOff + s * C::kSb);
+            tma_load_2d_pair(sa, &P.sa, 0, (m0 / 128) * P.atoms + kt * C::ATOMS, bar);
+#pragma unroll
+            for (int j = 0; j < C::GROUPS; ++j)
+              tma_load_2d_pair(sb + j * C::ATOMS * 512, &P.sb[C::GATED ? j : 0], 0,
+                               (C::GATED ? tn : tn * C::GROUPS + j) * P.atoms + kt * C::ATOMS, bar);
+          }
+          if (++s == C::STAGES) {
+            s = 0;
+            ph ^= 1u;
+          }
+        }
+      }
+    }
+  } else if (warp == 1 && rank == 0) {
+    // ---------------- MMA issuer (leader CTA) ----------------
+    if (elect_one()) {
+      int s = 0, it = 0, tc = 0;
+      uint32_t ph = 0;
+      const uint64_t a0 = desc_sw128(smem_u32(smem), P.a_mn ? 8192 : 16);
+      const uint64_t b0 = desc_sw128(smem_u32(smem + C::kBOff), P.b_mn ? 8192 : 16);
+      const uint64_t sa0 = desc_scales(smem_u32(smem + C::kSaOff));
+      const uint64_t sb0 = desc_scales(smem_u32(smem + C::kSbOff));
+      // K = 16 of 16-bit elements: 32 bytes on in a K-major row, 16 rows on otherwise
+      const int a_step = P.a_mn ? 2048 >> 4 : 32 >> 4, b_step = P.b_mn ? 2048 >> 4 : 32 >> 4;
+      for (; !s_abort && T.next(P, prob, tm, tn); ++tc) {
+        const int buf = tc & 1;
+        int w = kOk;
+        if (C::OV > 0) {
+          if (tc >= 1) w = wait(smem_u32(&bar_acce[0]), (tc - 1) & 1, &s_abort);
+        } else if (tc >= 2) {
+          w = wait(smem_u32(&bar_acce[buf]), ((tc >> 1) - 1) & 1, &s_abort);
+        }
+        if (w != kOk) {
+          if (w == kTimeout) fail(kStatusTimeoutEmpty);
+          break;
+        }
+        tc_fence_after();
+        const uint32_t acc = tmem + (buf ? C::kAcc1 : 0);
+        for (int i = 0; i < n_it; ++i, ++it) {
+          w = wait(smem_u32(&bar_full[s]), ph, &s_abort);
+          // the scale columns of two stages ago are free once that stage's MMAs are done
+          if (C::KIND != k16 && w == kOk && it >= 2)
+            w = wait(smem_u32(&bar_empty[(it - 2) % C::STAGES]), ((it - 2) / C::STAGES) & 1, &s_abort);
+          if (w != kOk) {
+            if (w == kTimeout) fail(kStatusTimeoutFull);
+            break;
+          }
+          tc_fence_after();
+          const int kt = i >= P.kt ? i - P.kt : i;
+          const int n_mma = kt == P.kt - 1 ? P.k_last : 4;
+          const uint64_t a = a0 + (uint64_t)((s * kOpBytes) >> 4), b = b0 + (uint64_t)((s * C::kB) >> 4);
+          if constexpr (C::KIND == k16) {
+            for (int kk = 0; kk < n_mma; ++kk)
+              mma_16<2>(acc, a + (uint64_t)(kk * a_step), b + (uint64_t)(kk * b_step), P.idesc, (i | kk) > 0);
+          } else {
+            const uint32_t sf = tmem + C::kSfCol + (it & 1) * C::kSfStage;
+            const uint64_t sa = sa0 + (uint64_t)((s * C::kSa) >> 4), sb = sb0 + (uint64_t)((s * C::kSb) >> 4);
+#pragma unroll
+            for (int q = 0; q < C::ATOMS; ++q) {
+              const uint32_t c = sf + q * 4 * (1 + C::GROUPS);
+              copy_scales<2>(c, sa + (uint64_t)(q * 32));
+#pragma unroll
+              for (int j = 0; j < C::GROUPS; ++j)
+                copy_scales<2>(c + 4 + 4 * j, sb + (uint64_t)((j * C::ATOMS + q) * 32));
+            }
+            for (int kk = 0; kk < n_mma; ++kk) {
+              constexpr bool NV = C::KIND == kNv;
+              const uint32_t c = sf + (NV ? kk : kk >> 1) * 4 * (1 + C::GROUPS);
+              const uint32_t id = NV || !(kk & 1) ? P.idesc : P.idesc | idesc_fp4(0, 0, false, 2);
+              mma_fp4<2, NV>(acc, a + (uint64_t)(2 * kk), b + (uint64_t)(2 * kk), id, c, c + 4, (i | kk) > 0);
+            }
+          }
+          commit<2>(smem_u32(&bar_empty[s]));
+          if (++s == C::STAGES) {
+            s = 0;
+            ph ^= 1u;
+          }
+        }
+        commit<2>(smem_u32(&bar_accf[buf]));
+      }
+      // the pair's shared and tensor memory stay in use until the last MMA is done
+      commit<2>(smem_u32(&bar_done));
+      wait_stay(smem_u32(&bar_done), 0);
+    }
+  } else if (warp == 1) {
+    // The leader's commits arrive in this CTA's shared memory too, where no
+    // role waits for those of the last stages: stay for the last of all.
+    if (elect_one()) wait_stay(smem_u32(&bar_done), 0);
+  } else if (warp >= C::kEpiWarp) {
+    // ---------------- epilogue: a lane owns a row of the tile ----------------
+    const int q = warp & 3, half = (warp - C::kEpiWarp) >> 2;
+    const uint32_t acce0 = mapa(smem_u32(&bar_acce[0]), 0);
+    constexpr int kChunks = C::GATED ? C::NT / 64 : C::NT / 32;
+    constexpr int kOvChunks = C::OV / 32;
+    pdl_wait();
+    for (int tc = 0; !s_abort && T.next(P, prob, tm, tn); ++tc) {
+      const int buf = tc & 1;
+      const int64_t m = (int64_t)tm * kTileM + (int)rank * kHalf + 32 * q + lane;
+      const int n0 = C::GATED ? tn * (C::NT / 2) : tn * C::NT;
+      const int w = wait(smem_u32(&bar_accf[buf]), (tc >> 1) & 1, &s_abort);
+      if (w != kOk) {
+        if (w == kTimeout) fail(kStatusTimeoutFull);
+        break;
+      }
+      tc_fence_after();
+      const uint32_t t0 = tmem + ((uint32_t)(32 * q) << 16) + (buf ? C::kAcc1 : 0);
+      bool released = false;
+      auto release = [&]() {
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive_cluster(acce0 + (C::OV > 0 ? 0 : 8 * buf));
+        released = true;
+      };
+#pragma unroll 1
+      for (int i = half; i < kChunks; i += 2) {
+        // the columns that the accumulators share are the first one's last, the second one's first
+        const int c = C::OV > 0 && buf == 0 ? kChunks - 1 - i : i;
+        uint32_t r0[32], r1[C::GATED ? 32 : 1];
+        tc_ld_32x32b_x32(t0 + 32 * c, r0);
+        if constexpr (C::GATED) tc_ld_32x32b_x32(t0 + C::NT / 2 + 32 * c, r1);
+        tc_wait_ld();
+        tc_regs_ready(r0);
+        tc_regs_ready(r1);
+        if (C::OV > 0 && !released && i + 2 >= kOvChunks) release();
+        const int n = n0 + 32 * c, cnt = min(32, P.N - n);
+        if (m >= P.M || (cnt <= 0 && !P.qfmt)) continue;
+        float v[32];
+        if constexpr (C::GATED) {
+          if (P.saved[0] && cnt > 0) {
+            const bool bf = P.type == POLYQ_BF16;
+            float s[32];
+#pragma unroll
+            for (int j = 0; j < 32; ++j) s[j] = saved_range(__uint_as_float(r0[j]), bf);
+            store_row32(P.saved[0], m * P.saved_stride + n, s, cnt, P.type, true);
+#pragma unroll
+            for (int j = 0; j < 32; ++j) s[j] = saved_range(__uint_as_float(r1[j]), bf);
+            store_row32(P.saved[1], m * P.saved_stride + n, s, cnt, P.type, true);
+          }
+#pragma unroll
+          for (int j = 0; j < 32; ++j)
+            v[j] = silu(__uint_as_float(r0[j]) * P.alpha[0]) * (__uint_as_float(r1[j]) * P.alpha[1]);
+          if (P.qfmt) {
+#pragma unroll
+            for (int j = 0; j < 32; ++j) v[j] = j < cnt ? v[j] : 0.f;
+            if (P.qfmt == kNv) store_codes32<true>(P, m, n, v);
+            else store_codes32<false>(P, m, n, v);
+            continue;
+          }
+        } else {
+#pragma unroll
+          for (int j = 0; j < 32; ++j) v[j] = __uint_as_float(r0[j]) * P.alpha[0];
+          if (P.res) add_row32(P.res, m * P.res_stride + n, v, cnt, P.type, P.vec);
+        }
+        store_row32(P.y[C::GATED ? 0 : prob], m * P.y_stride + n, v, cnt, P.type, P.vec);
+      }
+      __syncwarp();
+      if (!released) release();
+    }
+  }
+
+  __syncthreads();
+  cluster_sync();
+  if (warp == 1) {
+    tc_fence_after();
+    tmem_dealloc<2>(tmem, 512);
+  }
+  cluster_sync();
+}
+
+// ---------------------------------------------------------------------------
+// few tokens: weights as the rows of A, the contraction shared by a cluster
+// ---------------------------------------------------------------------------
+constexpr int kMaxSplit = 8;
+
+template <int KIND_, int NT_, bool GATED_>
+struct Few {
+  static constexpr int KIND = KIND_, NT = NT_;  // NT tokens
+  static constexpr bool GATED = GATED_;
+  static constexpr int MATS = GATED ? 2 : 1;
+  static constexpr int ATOMS = KIND == k16 ? 0 : KIND == kNv ? 4 : 2;
+  static constexpr int kB = NT * kRowBytes;
+  static constexpr int kSa = ATOMS * 512 * MATS, kSb = ATOMS * 512;
+  static constexpr int kStage = MATS * kOpBytes + kB + kSa + kSb;
+  static constexpr int kFit = (kSmemMax - 1024) / kStage;
+  static constexpr int STAGES = kFit < 12 ? kFit : 12;
+  static constexpr int kBOff = STAGES * MATS * kOpBytes, kSaOff = kBOff + STAGES * kB;
+  static constexpr int kSbOff = kSaOff + STAGES * kSa;
+  static constexpr size_t kSmem = (size_t)STAGES * kStage + 1024;
+  static constexpr int kSfStage = ATOMS * 4 * (MATS + 1);
+  static constexpr int kSfCol = MATS * NT;
+  static constexpr int kCols = kSfCol + 2 * kSfStage;
+  static constexpr int kTmem = kCols <= 32 ? 32 : kCols <= 64 ? 64 : kCols <= 128 ? 128 : kCols <= 256 ? 256 : 512;
+  static constexpr int kThreads = 256;
+  static_assert(MATS * NT * kHalf * 4 <= STAGES * kStage && STAGES >= 4, "the parts fit where the stages were");
+};
+
+template <class C>
+__global__ void __launch_bounds__(C::kThreads, 1) mm_few(const __grid_constant__ MmParams P, int split) {
+  extern __shared__ __align__(1024) uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
+                                             ~(uintptr_t)1023);
+  __shared__ uint64_t bar_full[C::STAGES];
+  __shared__ uint64_t bar_empty[C::STAGES];
+  __shared__ uint64_t bar_acc;
+  __shared__ uint32_t tmem_slot;
+  __shared__ volatile int s_abort;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int rank = split > 1 ? (int)cluster_ctarank() : 0;
+  const int tile = (int)blockIdx.x / split;
+  const int n0 = tile * kHalf, m0 = (int)blockIdx.y * C::NT;  // weight rows, tokens
+  const int kt0 = (int)((int64_t)rank * P.kt / split), kt1 = (int)((int64_t)(rank + 1) * P.kt / split);
+
+  if (threadIdx.x == 0) {
+    s_abort = 0;
+    for (int s = 0; s < C::STAGES; ++s) {
+      mbar_init(smem_u32(&bar_full[s]), 1);
+      mbar_init(smem_u32(&bar_empty[s]), 1);
+    }
+    mbar_init(smem_u32(&bar_acc), 1);
+    mbar_fence_init();
+  }
+  if (warp == 1) {
+    tmem_alloc<1>(smem_u32(&tmem_slot), C::kTmem);
+    tmem_relinquish<1>();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = tmem_slot;
+  pdl_trigger();
+  auto fail = [&](int code) {
+    s_abort = 1;
+    atomicExch(P.status, code);
+    for (const long long t0 = clock64(); clock64() - t0 < kStayCycles;) __nanosleep(1000);
+  };
+
+  if (warp == 0) {
+    // ---------------- producer ----------------
+    if (elect_one()) {
+      pdl_wait();
+      int s = 0;
+      uint32_t ph = 1;
+      for (int kt = kt0; kt < kt1; ++kt) {
+        const int w = wait(smem_u32(&bar_empty[s]), ph, &s_abort);
+        if (w != kOk) {
+          if (w == kTimeout) fail(kStatusTimeoutEmpty);
+          break;
+        }
+        const uint32_t bar = smem_u32(&bar_full[s]);
+        mbar_expect_tx(bar, C::kStage);
+        const uint32_t da = smem_u32(smem + s * C::MATS * kOpBytes), db = smem_u32(smem + C::kBOff + s * C::kB);
+        const int k = C::KIND == k16 ? kt * 64 : kt * kRowBytes;
+#pragma unroll
+        for (int j = 0; j < C::MATS; ++j) tma_load_2d(da + j * kOpBytes, &P.b[j], k, n0, bar);
+        tma_load_2d(db, &P.a[0], k, m0, bar);
+        if (C::KIND != k16) {
+          const uint32_t sa = smem_u32(smem + C::kSaOff + s * C::kSa);
+          const int row = kt * C::ATOMS;
+#pragma unroll
+          for (int j = 0; j < C::MATS; ++j)
+            tma_load_2d(sa + j * C::ATOMS * 512, &P.sb[j], 0, tile * P.atoms + row, bar);
+          tma_load_2d(smem_u32(smem + C::kSbOff + s * C::kSb), &P.sa, 0, (m0 / 128) * P.atoms + row, bar);
+        }
+        if (++s == C::STAGES) {
+          s = 0;
+          ph ^= 1u;
+        }
+      }
+    }
+  } else if (warp == 1) {
+    // ---------------- MMA issuer ----------------
+    if (elect_one()) {
+      int s = 0;
+      uint32_t ph = 0;
+      const uint64_t a0 = desc_sw128(smem_u32(smem), 16), b0 = desc_sw128(smem_u32(smem + C::kBOff), 16);
+      const uint64_t sa0 = desc_scales(smem_u32(smem + C::kSaOff)), sb0 = desc_scales(smem_u32(smem + C::kSbOff));
+      for (int kt = kt0; kt < kt1; ++kt) {
+        const int it = kt - kt0;
+        int w = wait(smem_u32(&bar_full[s]), ph, &s_abort);
+        if (C::KIND != k16 && w == kOk && it >= 2)
+          w = wait(smem_u32(&bar_empty[(it - 2) % C::STAGES]), ((it - 2) / C::STAGES) & 1, &s_abort);
+        if (w != kOk) {
+          if (w == kTimeout) fail(kStatusTimeoutFull);
+          break;
+        }
+        tc_fence_after();
+        const int n_mma = kt == P.kt - 1 ? P.k_last : 4;
+        const uint64_t a = a0 + (uint64_t)((s * C::MATS * kOpBytes) >> 4), b = b0 + (uint64_t)((s * C::kB) >> 4);
+        const uint32_t sf = tmem + C::kSfCol + (it & 1) * C::kSfStage;
+        if constexpr (C::KIND != k16) {
+          const uint64_t sa = sa0 + (uint64_t)((s * C::kSa) >> 4), sb = sb0 + (uint64_t)((s * C::kSb) >> 4);
+#pragma unroll
+          for (int q = 0; q < C::ATOMS; ++q) {
+            const uint32_t c = sf + q * 4 * (C::MATS + 1);
+#pragma unroll
+            for (int j = 0; j < C::MATS; ++j) copy_scales<1>(c + 4 * j, sa + (uint64_t)((j * C::ATOMS + q) * 32));
+            copy_scales<1>(c + 4 * C::MATS, sb + (uint64_t)(q * 32));
+          }
+        }
+        for (int kk = 0; kk < n_mma; ++kk)
+#pragma unroll
+          for (int j = 0; j < C::MATS; ++j) {
+            const uint64_t aj = a + (uint64_t)((j * kOpBytes) >> 4) + (uint64_t)(2 * kk);
+            if constexpr (C::KIND == k16) {
+              mma_16<1>(tmem + j * C::NT, aj, b + (uint64_t)(2 * kk), P.idesc, (it | kk) > 0);
+            } else {
+              constexpr bool NV = C::KIND == kNv;
+              const uint32_t c = sf + (NV ? kk : kk >> 1) * 4 * (C::MATS + 1);
+              const uint32_t id = NV || !(kk & 1) ? P.idesc : P.idesc | idesc_fp4(0, 0, false, 2);
+              mma_fp4<1, NV>(tmem + j * C::NT, aj, b + (uint64_t)(2 * kk), id, c + 4 * j, c + 4 * C::MATS,
+                             (it | kk) > 0);
+            }
+          }
+        commit<1>(smem_u32(&bar_empty[s]));
+        if (++s == C::STAGES) {
+          s = 0;
+          ph ^= 1u;
+        }
+      }
+      commit<1>(smem_u32(&bar_acc));
+      wait_stay(smem_u32(&bar_acc), 0);
+    }
+  }
+  __syncthreads();  // every copy has landed and every MMA is done (or a role has given up)
+  tc_fence_after();
+
+  // ---------------- epilogue ----------------
+  // The CTA's part into shared memory, [column][weight row]; then CTA r of the
+  // cluster adds the parts of the columns r, r + split, ... in rank order.
+  const int q = warp & 3, half = warp >> 2;
+  float* part = reinterpret_cast<float*>(smem);
+#pragma unroll 1
+  for (int c = half * 16; c < C::MATS * C::NT; c += 32) {
+    uint32_t r[16];
+    tmem_ld16(tmem + ((uint32_t)(32 * q) << 16) + c, r);
+    tc_wait_ld();
+    tc_regs_ready(r);
+#pragma unroll
+    for (int j = 0; j < 16; ++j) part[(c + j) * kHalf + 32 * q + lane] = __uint_as_float(r[j]);
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (split > 1) cluster_sync();
+  pdl_wait();
+  const int n = n0 + 32 * q + lane;
+  const uint32_t mine = smem_u32(part + 32 * q + lane);
+  auto sum = [&](int col) {
+    const uint32_t at = mine + col * (kHalf * 4);
+    if (split == 1) return part[col * kHalf + 32 * q + lane];
+    float v = 0.f;
+    for (int r = 0; r < split; ++r) v += ld_cluster_f32(mapa(at, r));
+    return v;
+  };
+#pragma unroll 2
+  for (int j = rank + split * half; j < C::NT; j += 2 * split) {
+    const int64_t m = m0 + j;
+    if (m >= P.M) break;
+    float v = sum(j) * P.alpha[0];
+    if constexpr (C::GATED) {
+      const float u = sum(C::NT + j) * P.alpha[1];
+      if (P.saved[0] && n < P.N) {
+        store_dense(P.saved[0], m * P.saved_stride + n, saved_range(v, P.type == POLYQ_BF16), P.type);
+        store_dense(P.saved[1], m * P.saved_stride + n, saved_range(u, P.type == POLYQ_BF16), P.type);
+      }
+      v = silu(v) * u;
+      if (P.qfmt) {
+        // a block is the warp (MX) or half of it (NV), a lane an element
+        const bool nv = P.qfmt == kNv;
+        float t = n < P.N ? v : 0.f;
+        if (nv) t = P.inv_g != 0.f ? t * P.inv_g : __fdiv_rn(t, P.g);
+        uint32_t mx = __float_as_uint(t) & 0x7FFFFFFFu;
+#pragma unroll
+        for (int d = 1; d < 16; d *= 2) mx = max(mx, __shfl_xor_sync(0xffffffffu, mx, d));
+        if (!nv) mx = max(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
+        float z[8] = {};
+        uint32_t byte;
+        if (nv) {
+          const fp4::Scale<true> sc(mx);
+          byte = sc.byte;
+          z[0] = sc.div(t);
+        } else {
+          const fp4::Scale<false> sc(mx);
+          byte = sc.byte;
+          z[0] = sc.div(t);
+        }
+        uint32_t w = (fp4::codes8(z) & 15u) << (4 * (lane & 7));  // 8 lanes make a word
+#pragma unroll
+        for (int d = 1; d < 8; d *= 2) w |= __shfl_xor_sync(0xffffffffu, w, d);
+        if ((lane & 7) == 0 && n < P.N) *reinterpret_cast<uint32_t*>(P.codes + m * P.code_stride + n / 2) = w;
+        const int bl = nv ? 16 : 32;
+        const int64_t blk = n / bl;
+        if ((lane & (bl - 1)) == 0 && blk >> 2 < P.out_atoms)
+          P.scales[fp4::scale_off(m, blk, P.out_atoms)] = (uint8_t)byte;
+        continue;
+      }
+    } else if (P.res && n < P.N) {
+      v += load_dense(P.res, m * P.res_stride + n, P.type);
+    }
+    if (n < P.N) store_dense(P.y[0], m * P.y_stride + n, v, P.type);
+  }
+  __syncthreads();
+  if (split > 1) cluster_sync();  // a peer may still read this CTA's part
+  if (warp == 1) {
+    tc_fence_after();
+    tmem_dealloc<1>(tmem, C::kTmem);
+  }
+}
+
+// ---------------------------------------------------------------------------
+// gradients of the activation and the product
+// ---------------------------------------------------------------------------
+// da = dh u s (1 + a (1 - s)), du = dh a s with s = 1 / (1 + exp(-a)); 8
+// elements a thread.  One pass over a, u, dh; bound by HBM.
+struct ActParams {
+  const void *a, *u, *dh;
+  void *da, *du;
+  int64_t T, F, stride, dh_stride, items;  // stride: of a, u, da, du
+  int vec;                                 // rows of dh start on 16 bytes
+};
+template <bool BF16>
+__global__ void __launch_bounds__(256) act_backward(const __grid_constant__ ActParams P) {
+  pdl_trigger();
+  pdl_wait();
+  const int64_t per = P.stride / 8;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < P.items; i += (int64_t)gridDim.x * 256) {
+    const int64_t t = i / per, f = (i - t * per) * 8;
+    if (f >= P.F) continue;
+    uint32_t a[4], u[4], d[4], da[4], du[4];
+    const uint4 av = *reinterpret_cast<const uint4*>((const uint16_t*)P.a + t * P.stride + f);
+    const uint4 uv = *reinterpret_cast<const uint4*>((const uint16_t*)P.u + t * P.stride + f);
+    a[0] = av.x, a[1] = av.y, a[2] = av.z, a[3] = av.w;
+    u[0] = uv.x, u[1] = uv.y, u[2] = uv.z, u[3] = uv.w;
+    const uint16_t* dr = (const uint16_t*)P.dh + t * P.dh_stride + f;
+    const int n = (int)(P.F - f < 8 ? P.F - f : 8);
+    if (P.vec && n == 8) {
+      const uint4 dv = *reinterpret_cast<const uint4*>(dr);
+      d[0] = dv.x, d[1] = dv.y, d[2] = dv.z, d[3] = dv.w;
+    } else {
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        d[j] = (2 * j < n ? dr[2 * j] : 0u) | (uint32_t)(2 * j + 1 < n ? dr[2 * j + 1] : 0u) << 16;
+    }
+    auto get = [](uint32_t w) {
+      if (BF16) return make_float2(bf16_lo(w), bf16_hi(w));
+      return __half22float2(*reinterpret_cast<const __half2*>(&w));
+    };
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float2 x = get(a[j]), y = get(u[j]), g = get(d[j]);
+      auto grad = [](float x, float y, float g, float& ga, float& gu) {
+        const float s = __fdividef(1.f, 1.f + __expf(-x)), xs = x * s;
+        gu = g * xs;
+        ga = g * y * (s + xs * (1.f - s));
+      };
+      float2 ga, gu;
+      grad(x.x, y.x, g.x, ga.x, gu.x);
+      grad(x.y, y.y, g.y, ga.y, gu.y);
+      da[j] = pack16(ga.x, ga.y, BF16);
+      du[j] = pack16(gu.x, gu.y, BF16);
+    }
+    // columns past F of a row's last 8 are padding that nothing reads
+    *reinterpret_cast<uint4*>((uint16_t*)P.da + t * P.stride + f) = make_uint4(da[0], da[1], da[2], da[3]);
+    *reinterpret_cast<uint4*>((uint16_t*)P.du + t * P.stride + f) = make_uint4(du[0], du[1], du[2], du[3]);
+  }
+}
+
+// ---------------------------------------------------------------------------
+// host side
+// ---------------------------------------------------------------------------
+int device_index(int* dev, const char* who) {
+  *dev = 0;
+  cudaGetDevice(dev);
+  if (*dev < 0 || *dev >= kMaxDevices)
+    return polyq_set_error(POLYQ_EUNSUPPORTED, "%s: device %d >= %d", who, *dev, kMaxDevices);
+  return POLYQ_OK;
+}
+
+// Clusters of `size` CTAs of a kernel that fit on the device at once (cached).
+int resident_clusters(const void* f, int threads, size_t smem, int size, std::atomic<int>* cached, int* out,
+                      const char* who) {
+  int n = cached->load(std::memory_order_acquire);
+  if (n == 0) {
+    cudaError_t e = cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = size;
+    at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(size);
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    if (e == cudaSuccess) e = cudaOccupancyMaxActiveClusters(&n, f, &cfg);
+    if (e != cudaSuccess || n < 1)
+      return polyq_set_error(POLYQ_ECUDA, "%s: %d clusters of %d fit: %s", who, n, size, cudaGetErrorString(e));
+    cached->store(n, std::memory_order_release);
+  }
+  *out = n;
+  return POLYQ_OK;
+}
+
+int launch_cluster(const void* f, dim3 grid, int threads, size_t smem, int cluster, void** args, void* stream,
+                   const char* who) {
+  cudaLaunchAttribute at[2];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  at[1].id = cudaLaunchAttributeClusterDimension;
+  at[1].val.clusterDim.x = cluster;
+  at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.stream = (cudaStream_t)stream;
+  cfg.attrs = at;
+  cfg.numAttrs = 2;
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
+  const cudaError_t e = cudaLaunchKernelExC(&cfg, f, args);
+  if (e != cudaSuccess) return polyq_set_error(POLYQ_ECUDA, "%s: launch: %s", who, cudaGetErrorString(e));
+  return POLYQ_OK;
+}
+
+// Tiles of a pair launch: P.M, P.N, P.probs are set.
+template <class C>
+int run_pair(MmParams& P, int dev, void* stream, const char* who) {
+  static std::atomic<int> cached[kMaxDevices];
+  int pairs = 0;
+  const int rc = resident_clusters((const void*)mm_pair<C>, C::kThreads, C::kSmem, 2, &cached[dev], &pairs, who);
+  if (rc) return rc;
+  const int cols = C::GATED ? C::NT / 2 : C::NT;
+  P.tiles_m = (P.M + kTileM - 1) / kTileM;
+  P.tiles_n = (P.N + cols - 1) / cols;
+  const int64_t tiles = (int64_t)P.tiles_m * P.tiles_n * P.probs;
+  if (tiles >= 1ll << 31) return polyq_set_error(POLYQ_EUNSUPPORTED, "%s: %lld tiles", who, (long long)tiles);
+  P.tiles = (int)tiles;
+  void* args[] = {&P};
+  return launch_cluster((const void*)mm_pair<C>, dim3((unsigned)(2 * std::min(P.tiles, pairs))), C::kThreads,
+                        C::kSmem, 2, args, stream, who);
+}
+
+// Few tokens: P.M tokens, P.N weight rows.
+template <class C>
+int run_few(MmParams& P, int dev, void* stream, const char* who) {
+  static std::atomic<int> cached[kMaxDevices][kMaxSplit];
+  const int64_t tiles = (P.N + kHalf - 1) / kHalf, ty = (P.M + C::NT - 1) / C::NT;
+  if (ty > 65535) return polyq_set_error(POLYQ_EUNSUPPORTED, "%s: %d tokens", who, P.M);
+  // the split with the shortest longest CTA: waves of tiles times stages, and
+  // about two stages' time for a cluster's exchange
+  int best = 1;
+  double t_best = 1e30;
+  for (int s = 1; s <= kMaxSplit && s <= P.kt; ++s) {
+    int fit = 0;
+    const int rc = resident_clusters((const void*)mm_few<C>, C::kThreads, C::kSmem, s, &cached[dev][s - 1], &fit, who);
+    if (rc) return rc;
+    const double t = (double)((tiles * ty + fit - 1) / fit) * ((P.kt + s - 1) / s + 4.0 + (s > 1 ? 2.0 : 0.0));
+    if (t < 0.97 * t_best) {
+      t_best = t;
+      best = s;
+    }
+  }
+  void* args[] = {&P, &best};
+  return launch_cluster((const void*)mm_few<C>, dim3((unsigned)(tiles * best), (unsigned)ty), C::kThreads, C::kSmem,
+                        best, args, stream, who);
+}
+
+int check_workspace(const void* ws, size_t bytes, size_t need, const char* who) {
+  if (!ws || bytes < need)
+    return polyq_set_error(POLYQ_ENOMEM, "%s: workspace needs %zu bytes, got %zu", who, need, bytes);
+  if ((uintptr_t)ws % 256) return polyq_set_error(POLYQ_EINVAL, "%s: workspace must be 256-byte aligned", who);
+  return POLYQ_OK;
+}
+
+int elem_bytes(int type) { return type == POLYQ_F32 ? 4 : 2; }
+bool vec_rows(const polyq_dense* d) {
+  return (uintptr_t)d->data % 16 == 0 && d->stride * elem_bytes(d->type) % 16 == 0;
+}
+
+// Tensor maps of a 4-bit operand: its code tiles of `rows` rows, and its scales.
+int map_fp4(CUtensorMap* codes, CUtensorMap* scales, const polyq_fp4* t, int rows, const char* who) {
+  const bool nv = t->format == POLYQ_FP4_NV;
+  const int64_t atom_rows = (t->rows + 127) / 128 * fp4::atoms(t->K, nv);
+  if (atom_rows >= 1ll << 30)
+    return polyq_set_error(POLYQ_EUNSUPPORTED, "%s: [%lld][%lld]", who, (long long)t->rows, (long long)t->K);
+  int rc = polyq_tensor_map_2d(codes, t->codes, 1, (uint64_t)(t->K + 1) / 2, (uint64_t)t->rows,
+                               (uint64_t)t->code_stride, kRowBytes, (uint32_t)rows, 128);
+  if (!rc) rc = polyq_tensor_map_2d(scales, t->scales, 4, 128, (uint64_t)atom_rows, 512, 128, nv ? 4 : 2);
+  return rc;
+}
+// A 16-bit matrix [rows][cols] as an operand: K-major tiles (box of 64 columns)
+// or, with `mn`, tiles of 64 K rows by 64 columns.
+int map_16(CUtensorMap* m, const void* data, int64_t stride, int64_t rows, int64_t cols, bool mn, int box_rows) {
+  return polyq_tensor_map_2d(m, data, 2, (uint64_t)cols, (uint64_t)rows, (uint64_t)stride * 2, 64,
+                             mn ? 64u : (uint32_t)box_rows, 128);
+}
+
+constexpr int kFewTokens = 128;  // at most this many tokens: mm_few
+int few_tile(int64_t M) { return M <= 16 ? 16 : M <= 32 ? 32 : M <= 64 ? 64 : 128; }
+
+template <int KIND, bool GATED>
+int dispatch_few(MmParams& P, int dev, void* stream, const char* who) {
+  switch (few_tile(P.M)) {
+    case 16: return run_few<Few<KIND, 16, GATED>>(P, dev, stream, who);
+    case 32: return run_few<Few<KIND, 32, GATED>>(P, dev, stream, who);
+    case 64: return run_few<Few<KIND, 64, GATED>>(P, dev, stream, who);
+    default: return run_few<Few<KIND, 128, GATED>>(P, dev, stream, who);
+  }
+}
+
+void set_quant_out(MmParams& P, const polyq_fp4* q) {
+  const bool nv = q->format == POLYQ_FP4_NV;
+  P.codes = q->codes;
+  P.scales = q->scales;
+  P.code_stride = q->code_stride;
+  P.out_atoms = fp4::atoms(q->K, nv);
+  P.qfmt = nv ? kNv : kMx;
+  P.g = q->tensor_scale;
+  int e;
+  P.inv_g = std::frexp(P.g, &e) == 0.5f && std::isfinite(1.f / P.g) ? 1.f / P.g : 0.f;
+}
+
+float product_scale(const polyq_fp4* a, const polyq_fp4* b) {
+  return (float)((double)a->tensor_scale * (double)b->tensor_scale);
+}
+
+// Whether the wide tile wins: waves of tiles of 256 columns against waves of
+// half of that, which take a little more than half the time each.
+bool wide_tile(const MmParams& P, int sms, bool gated) {
+  const int64_t tm = (P.M + kTileM - 1) / kTileM * (int64_t)P.probs, pairs = std::max(1, sms / 2);
+  const int c = gated ? 128 : 256;
+  const int64_t w = (tm * ((P.N + c - 1) / c) + pairs - 1) / pairs, h = (tm * ((P.N + c / 2 - 1) / (c / 2)) + pairs - 1) / pairs;
+  return w <= 0.58 * h;
+}
+
+// The product of 4-bit operands: x [M][K] with w0 (and w1) [N][K].
+template <int KIND, bool GATED>
+int run_fp4(MmParams& P, const polyq_fp4* x, const polyq_fp4* w0, const polyq_fp4* w1, void* stream,
+            const char* who) {
+  int dev = 0, sms = 0;
+  int rc = device_index(&dev, who);
+  if (!rc) rc = polyq_sm_count(&sms);
+  if (rc) return rc;
+  const bool nv = KIND == kNv, few = x->rows <= kFewTokens;
+  P.M = (int)x->rows;
+  P.N = (int)w0->rows;
+  P.segs = P.probs = 1;
+  P.kt = (int)((x->K + 255) / 256);
+  P.k_last = (int)((x->K - (int64_t)(P.kt - 1) * 256 + 63) / 64);
+  P.atoms = (int)fp4::atoms(x->K, nv);
+  P.alpha[0] = product_scale(x, w0);
+  P.alpha[1] = GATED ? product_scale(x, w1) : 1.f;
+  if (few) {
+    const int nt = few_tile(P.M);
+    P.idesc = idesc_fp4(kHalf, nt, !nv, 0);
+    rc = map_fp4(&P.a[0], &P.sa, x, nt, who);
+    if (!rc) rc = map_fp4(&P.b[0], &P.sb[0], w0, kHalf, who);
+    if (!rc && GATED) rc = map_fp4(&P.b[1], &P.sb[1], w1, kHalf, who);
+    return rc ? rc : dispatch_few<KIND, GATED>(P, dev, stream, who);
+  }
+  const bool wide = GATED || wide_tile(P, sms, GATED);
+  P.idesc = idesc_fp4(kTileM, wide ? 256 : 128, !nv, 0);
+  rc = map_fp4(&P.a[0], &P.sa, x, kHalf, who);
+  if (!rc) rc = map_fp4(&P.b[0], &P.sb[0], w0, wide ? 128 : 64, who);
+  if (GATED) {
+    if (!rc) rc = map_fp4(&P.b[1], &P.sb[1], w1, 128, who);
+  } else {
+    P.b[1] = P.b[0];
+  }
+  if (rc) return rc;
+  if constexpr (!GATED)
+    if (!wide) return run_pair<Pair<KIND, 128, false>>(P, dev, stream, who);
+  return run_pair<Pair<KIND, 256, GATED>>(P, dev, stream, who);
+}
+
+int check_same(const polyq_fp4* x, const polyq_fp4* w, const char* who, const char* what) {
+  if (w->K != x->K || w->format != x->format)
+    return polyq_set_error(POLYQ_EINVAL, "%s: %s [%lld][%lld] format %d against x [%lld][%lld] format %d", who,
+                           what, (long long)w->rows, (long long)w->K, w->format, (long long)x->rows,
+                           (long long)x->K, x->format);
+  return POLYQ_OK;
+}
+
+// A 16-bit operand of the training block.
+int check_16(const polyq_dense* d, int64_t cols, int type, const char* who, const char* what) {
+  int rc = polyq_check_dense(d, cols, who, what);
+  if (rc) return rc;
+  if (d->type != type || type == POLYQ_F32)
+    return polyq_set_error(POLYQ_EINVAL, "%s: %s: type %d (all bf16 or all f16)", who, what, d->type);
+  return POLYQ_OK;
+}
+int check_operand(const polyq_dense* d, int64_t cols, int type, const char* who, const char* what) {
+  int rc = check_16(d, cols, type, who, what);
+  if (rc) return rc;
+  if (!vec_rows(d))
+    return polyq_set_error(POLYQ_EINVAL, "%s: %s: rows must start on 16 bytes (address and stride)", who, what);
+  return POLYQ_OK;
+}
+int check_sizes(int64_t T, int64_t F, int64_t K, const char* who) {
+  if (T < 1 || F < 1 || K < 1 || T > (1 << 24) || F > (1 << 24) || K > (1 << 24))
+    return polyq_set_error(POLYQ_EINVAL, "%s: T=%lld F=%lld K=%lld", who, (long long)T, (long long)F, (long long)K);
+  return POLYQ_OK;
+}
+
+// A 16-bit product on pairs.
+template <bool GATED>
+int run_16(MmParams& P, bool wide, int dev, void* stream, const char* who) {
+  return wide ? run_pair<Pair<k16, 256, GATED>>(P, dev, stream, who)
+              : run_pair<Pair<k16, 128, GATED>>(P, dev, stream, who);
+}
+
+}  // namespace
+
+extern "C" int polyq_fp4_linear(const polyq_fp4* x, const polyq_fp4* w, const polyq_dense* residual,
+                                const polyq_dense* y, void* workspace, size_t workspace_bytes, void* stream) {
+  polyq_clear_error();
+  const char* who = "polyq_fp4_linear";
+  int rc = polyq_check_fp4(x, who, "x");
+  if (!rc) rc = polyq_check_fp4(w, who, "w");
+  if (!rc) rc = check_same(x, w, who, "w");
+  if (!rc) rc = polyq_check_dense(y, w->rows, who, "y");
+  if (!rc && residual) rc = polyq_check_dense(residual, w->rows, who, "residual");
+  if (!rc) rc = check_workspace(workspace, workspace_bytes, POLYQ_FP4_WORKSPACE_BYTES, who);
+  if (rc) return rc;
+  if (residual && residual->type != y->type)
+    return polyq_set_error(POLYQ_EINVAL, "%s: residual has type %d, y %d", who, residual->type, y->type);
+  if (residual && residual->data == y->data && residual->stride != y->stride)
+    return polyq_set_error(POLYQ_EINVAL, "%s: residual is y with another stride", who);
+  MmParams P;
+  memset(&P, 0, sizeof P);
+  P.y[0] = y->data;
+  P.y_stride = y->stride;
+  P.type = y->type;
+  P.vec = vec_rows(y) && (!residual || vec_rows(residual));
+  P.res = residual ? residual->data : nullptr;
+  P.res_stride = residual ? residual->stride : 0;
+  P.status = (int*)workspace;
+  return x->format == POLYQ_FP4_NV ? run_fp4<kNv, false>(P, x, w, nullptr, stream, who)
+                                   : run_fp4<kMx, false>(P, x, w, nullptr, stream, who);
+}
+
+extern "C" int polyq_fp4_ffn(const polyq_fp4* x, const polyq_fp4* gate, const polyq_fp4* up, const polyq_dense* h,
+                             const polyq_fp4* hq, void* workspace, size_t workspace_bytes, void* stream) {
+  polyq_clear_error();
+  const char* who = "polyq_fp4_ffn";
+  int rc = polyq_check_fp4(x, who, "x");
+  if (!rc) rc = polyq_check_fp4(gate, who, "gate");
+  if (!rc) rc = polyq_check_fp4(up, who, "up");
+  if (!rc) rc = check_same(x, gate, who, "gate");
+  if (!rc) rc = check_same(x, up, who, "up");
+  if (rc) return rc;
+  if (gate->rows != up->rows || !h == !hq)
+    return polyq_set_error(POLYQ_EINVAL, "%s: gate has %lld rows, up %lld; one of h and hq is wanted", who,
+                           (long long)gate->rows, (long long)up->rows);
+  if (h) rc = polyq_check_dense(h, gate->rows, who, "h");
+  else rc = polyq_check_fp4(hq, who, "hq");
+  if (!rc && hq && (hq->rows != x->rows || hq->K != gate->rows))
+    rc = polyq_set_error(POLYQ_EINVAL, "%s: hq is [%lld][%lld]", who, (long long)hq->rows, (long long)hq->K);
+  if (!rc) rc = check_workspace(workspace, workspace_bytes, POLYQ_FP4_WORKSPACE_BYTES, who);
+  if (rc) return rc;
+  MmParams P;
+  memset(&P, 0, sizeof P);
+  if (h) {
+    P.y[0] = h->data;
+    P.y_stride = h->stride;
+    P.type = h->type;
+    P.vec = vec_rows(h);
+  } else {
+    set_quant_out(P, hq);
+  }
+  P.status = (int*)workspace;
+  return x->format == POLYQ_FP4_NV ? run_fp4<kNv, true>(P, x, gate, up, stream, who)
+                                   : run_fp4<kMx, true>(P, x, gate, up, stream, who);
+}
+
+extern "C" int64_t polyq_ffn_saved_stride(int64_t F) { return (F + 7) / 8 * 8; }
+
+extern "C" int polyq_ffn_forward(const polyq_dense* x, const polyq_dense* gate, const polyq_dense* up, int64_t T,
+                                 int64_t F, int64_t K, const polyq_dense* h, void* saved, void* workspace,
+                                 size_t workspace_bytes, void* stream) {
+  polyq_clear_error();
+  const char* who = "polyq_ffn_forward";
+  int rc = check_sizes(T, F, K, who);
+  if (!rc) rc = polyq_check_dense(x, K, who, "x");
+  if (!rc) rc = check_operand(x, K, x->type, who, "x");
+  if (!rc) rc = check_operand(gate, K, x->type, who, "gate");
+  if (!rc) rc = check_operand(up, K, x->type, who, "up");
+  if (!rc) rc = check_16(h, F, x->type, who, "h");
+  if (!rc) rc = check_workspace(workspace, workspace_bytes, POLYQ_FP4_WORKSPACE_BYTES, who);
+  if (rc) return rc;
+  if ((uintptr_t)saved % 16) return polyq_set_error(POLYQ_EINVAL, "%s: saved must be 16-byte aligned", who);
+  int dev = 0, sms = 0;
+  rc = device_index(&dev, who);
+  if (!rc) rc = polyq_sm_count(&sms);
+  if (rc) return rc;
+  MmParams P;
+  memset(&P, 0, sizeof P);
+  P.M = (int)T;
+  P.N = (int)F;
+  P.segs = P.probs = 1;
+  P.kt = (int)((K + 63) / 64);
+  P.k_last = (int)((K - (int64_t)(P.kt - 1) * 64 + 15) / 16);
+  P.alpha[0] = P.alpha[1] = 1.f;
+  P.y[0] = h->data;
+  P.y_stride = h->stride;
+  P.type = h->type;
+  P.vec = vec_rows(h);
+  if (saved) {
+    P.saved_stride = polyq_ffn_saved_stride(F);
+    P.saved[0] = saved;
+    P.saved[1] = (uint16_t*)saved + T * P.saved_stride;
+  }
+  P.status = (int*)workspace;
+  const bool bf16 = x->type == POLYQ_BF16, few = T <= kFewTokens;
+  const bool wide = !few && wide_tile(P, sms, true);
+  const int nt = few_tile(T);
+  P.idesc = few ? idesc_16(kHalf, nt, bf16, false, false) : idesc_16(kTileM, wide ? 256 : 128, bf16, false, false);
+  rc = map_16(&P.a[0], x->data, x->stride, T, K, false, few ? nt : kHalf);
+  const int brows = few || wide ? 128 : 64;
+  if (!rc) rc = map_16(&P.b[0], gate->data, gate->stride, F, K, false, brows);
+  if (!rc) rc = map_16(&P.b[1], up->data, up->stride, F, K, false, brows);
+  if (rc) return rc;
+  return few ? dispatch_few<k16, true>(P, dev, stream, who) : run_16<true>(P, wide, dev, stream, who);
+}
+
+extern "C" int polyq_ffn_backward_workspace_bytes(int64_t T, int64_t F, size_t* bytes) {
+  polyq_clear_error();
+  int rc = check_sizes(T, F, 1, "polyq_ffn_backward_workspace_bytes");
+  if (rc) return rc;
+  if (!bytes) return polyq_set_error(POLYQ_EINVAL, "polyq_ffn_backward_workspace_bytes: bytes is NULL");
+  *bytes = POLYQ_FP4_WORKSPACE_BYTES + (size_t)T * (size_t)polyq_ffn_saved_stride(F) * 4;
+  return POLYQ_OK;
+}
+
+extern "C" int polyq_ffn_backward(const polyq_dense* x, const polyq_dense* gate, const polyq_dense* up, int64_t T,
+                                  int64_t F, int64_t K, const void* saved, const polyq_dense* dh,
+                                  const polyq_dense* dx, const polyq_dense* dgate, const polyq_dense* dup,
+                                  void* workspace, size_t workspace_bytes, void* stream) {
+  polyq_clear_error();
+  const char* who = "polyq_ffn_backward";
+  size_t need = 0;
+  int rc = check_sizes(T, F, K, who);
+  if (!rc) rc = polyq_check_dense(x, K, who, "x");
+  if (!rc) rc = check_operand(x, K, x->type, who, "x");
+  if (!rc) rc = check_operand(gate, K, x->type, who, "gate");
+  if (!rc) rc = check_operand(up, K, x->type, who, "up");
+  if (!rc) rc = check_16(dh, F, x->type, who, "dh");
+  if (!rc) rc = polyq_ffn_backward_workspace_bytes(T, F, &need);
+  if (!rc) rc = check_workspace(workspace, workspace_bytes, need, who);
+  if (rc) return rc;
+  if (!saved || (uintptr_t)saved % 16)
+    return polyq_set_error(POLYQ_EINVAL, "%s: saved must be given, 16-byte aligned", who);
+  if (!dgate != !dup || (!dx && !dgate))
+    return polyq_set_error(POLYQ_EINVAL, "%s: dx, or dgate and dup, or all three are wanted", who);
+  if (dx) rc = polyq_check_dense(dx, K, who, "dx");
+  if (!rc && dgate) rc = polyq_check_dense(dgate, K, who, "dgate");
+  if (!rc && dup) rc = polyq_check_dense(dup, K, who, "dup");
+  if (rc) return rc;
+  for (const polyq_dense* d : {dx, dgate, dup})
+    if (d && d->type != x->type && d->type != POLYQ_F32)
+      return polyq_set_error(POLYQ_EINVAL, "%s: a gradient of type %d", who, d->type);
+  if (dgate && (dgate->type != dup->type || dgate->stride != dup->stride))
+    return polyq_set_error(POLYQ_EINVAL, "%s: dgate and dup must have one type and stride", who);
+  int dev = 0, sms = 0;
+  rc = device_index(&dev, who);
+  if (!rc) rc = polyq_sm_count(&sms);
+  if (rc) return rc;
+
+  const bool bf16 = x->type == POLYQ_BF16;
+  const int64_t fs = polyq_ffn_saved_stride(F);
+  uint16_t* da = (uint16_t*)((uint8_t*)workspace + POLYQ_FP4_WORKSPACE_BYTES);
+  uint16_t* du = da + T * fs;
+  {
+    ActParams A;
+    A.a = saved;
+    A.u = (const uint16_t*)saved + T * fs;
+    A.dh = dh->data;
+    A.da = da;
+    A.du = du;
+    A.T = T;
+    A.F = F;
+    A.stride = fs;
+    A.dh_stride = dh->stride;
+    A.items = T * (fs / 8);
+    A.vec = vec_rows(dh);
+    void* args[] = {&A};
+    rc = launch_cluster(bf16 ? (const void*)act_backward<true> : (const void*)act_backward<false>,
+                        dim3((unsigned)std::min<int64_t>((A.items + 255) / 256, 1 << 30)), 256, 0, 1, args, stream, who);
+    if (rc) return rc;
+  }
+  MmParams P;
+  memset(&P, 0, sizeof P);
+  P.alpha[0] = 1.f;
+  P.status = (int*)workspace;
+  if (dx) {
+    // dx [T][K]: A = da, du [T][F], B = gate, up [F][K] with K contiguous
+    P.M = (int)T;
+    P.N = (int)K;
+    P.segs = 2;
+    P.probs = 1;
+    P.kt = (int)((F + 63) / 64);
+    P.k_last = (int)((F - (int64_t)(P.kt - 1) * 64 + 15) / 16);
+    P.b_mn = 1;
+    P.y[0] = dx->data;
+    P.y_stride = dx->stride;
+    P.type = dx->type;
+    P.vec = vec_rows(dx);
+    const bool wide = wide_tile(P, sms, false);
+    P.idesc = idesc_16(kTileM, wide ? 256 : 128, bf16, false, true);
+    rc = map_16(&P.a[0], da, fs, T, F, false, kHalf);
+    if (!rc) rc = map_16(&P.a[1], du, fs, T, F, false, kHalf);
+    if (!rc) rc = map_16(&P.b[0], gate->data, gate->stride, F, K, true, 0);
+    if (!rc) rc = map_16(&P.b[1], up->data, up->stride, F, K, true, 0);
+    if (!rc) rc = run_16<false>(P, wide, dev, stream, who);
+    if (rc) return rc;
+  }
+  if (dgate) {
+    // dgate, dup [F][K]: A = da, du with F contiguous, B = x with K contiguous, over T
+    P.M = (int)F;
+    P.N = (int)K;
+    P.segs = 1;
+    P.probs = 2;
+    P.kt = (int)((T + 63) / 64);
+    P.k_last = (int)((T - (int64_t)(P.kt - 1) * 64 + 15) / 16);
+    P.a_mn = P.b_mn = 1;
+    P.y[0] = dgate->data;
+    P.y[1] = dup->data;
+    P.y_stride = dgate->stride;
+    P.type = dgate->type;
+    P.vec = vec_rows(dgate) && vec_rows(dup);
+    const bool wide = wide_tile(P, sms, false);
+    P.idesc = idesc_16(kTileM, wide ? 256 : 128, bf16, true, true);
+    rc = map_16(&P.a[0], da, fs, T, F, true, 0);
+    if (!rc) rc = map_16(&P.a[1], du, fs, T, F, true, 0);
+    if (!rc) rc = map_16(&P.b[0], x->data, x->stride, T, K, true, 0);
+    P.b[1] = P.b[0];
+    if (!rc) rc = run_16<false>(P, wide, dev, stream, who);
+  }
+  return rc;
+}

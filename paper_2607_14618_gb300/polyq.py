@@ -98,7 +98,23 @@ class GemvPhase(C.Structure):
                 ("ys", C.c_void_p * MAX_GROUP), ("residuals", C.c_void_p * MAX_GROUP)]
 
 
+FP4_MX, FP4_NV = 0, 1
+FP4_WORKSPACE_BYTES = 256
+T_F32, T_BF16, T_F16 = 0, 1, 2
+
+
+class Fp4Desc(C.Structure):
+    _fields_ = [("codes", C.c_void_p), ("scales", C.c_void_p), ("rows", C.c_int64),
+                ("K", C.c_int64), ("code_stride", C.c_int64), ("format", C.c_int32),
+                ("tensor_scale", C.c_float)]
+
+
+class Dense(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("stride", C.c_int64), ("type", C.c_int32)]
+
+
 _P = C.c_void_p
+_FP4, _DENSE = C.POINTER(Fp4Desc), C.POINTER(Dense)
 _SIGS = {
     "polyq_last_error": (C.c_char_p, []),
     "polyq_pack_opts_default": (None, [C.POINTER(PackOpts)]),
@@ -141,6 +157,20 @@ _SIGS = {
     "polyq_linear_gemm": (C.c_int, [C.POINTER(DevLayer), _P, C.c_int64, _P, _P, C.c_size_t, _P]),
     "polyq_unpack_codes": (C.c_int, [C.POINTER(DevLayer), _P, _P]),
     "polyq_f64_to_f16": (C.c_uint16, [C.c_double]),
+    # include/polyq_fp4.h
+    "polyq_fp4_bytes": (C.c_int, [C.c_int64, C.c_int64, C.c_int32, C.POINTER(C.c_int64),
+                                  C.POINTER(C.c_int64)]),
+    "polyq_fp4_quantize": (C.c_int, [_DENSE, _FP4, _P]),
+    "polyq_fp4_dequantize": (C.c_int, [_FP4, _DENSE, _P]),
+    "polyq_fp4_linear": (C.c_int, [_FP4, _FP4, _DENSE, _DENSE, _P, C.c_size_t, _P]),
+    "polyq_fp4_ffn": (C.c_int, [_FP4, _FP4, _FP4, _DENSE, _FP4, _P, C.c_size_t, _P]),
+    "polyq_ffn_saved_stride": (C.c_int64, [C.c_int64]),
+    "polyq_ffn_forward": (C.c_int, [_DENSE, _DENSE, _DENSE, C.c_int64, C.c_int64, C.c_int64,
+                                    _DENSE, _P, _P, C.c_size_t, _P]),
+    "polyq_ffn_backward_workspace_bytes": (C.c_int, [C.c_int64, C.c_int64,
+                                                     C.POINTER(C.c_size_t)]),
+    "polyq_ffn_backward": (C.c_int, [_DENSE, _DENSE, _DENSE, C.c_int64, C.c_int64, C.c_int64, _P,
+                                     _DENSE, _DENSE, _DENSE, _DENSE, _P, C.c_size_t, _P]),
 }
 for _name, (_res, _args) in _SIGS.items():
     _fn = getattr(_lib, _name)
@@ -703,3 +733,261 @@ def workspace_status(workspace, stream=None):
     v = C.c_int()
     _check(_lib.polyq_workspace_status(workspace.data_ptr(), C.byref(v), _stream_ptr(stream)))
     return v.value
+
+
+# ---- 4-bit floating point and the gated feed-forward block (include/polyq_fp4.h) ----
+def _types():
+    import torch
+    return {torch.float32: T_F32, torch.bfloat16: T_BF16, torch.float16: T_F16}
+
+
+def _dense(t, name, shape=None, device=None, dtype=None):
+    """Descriptor of a 2-D CUDA tensor whose rows are contiguous (any row
+    stride), checked against what is given; it must be on the current device
+    (the stream and the library's per-device state are looked up for that)."""
+    import torch
+    ty = _types().get(getattr(t, "dtype", None))
+    if (not isinstance(t, torch.Tensor) or ty is None or t.dim() != 2 or not t.is_cuda
+            or (shape is not None and tuple(t.shape) != tuple(shape))
+            or (dtype is not None and t.dtype != dtype) or (device is not None and t.device != device)
+            or (t.shape[1] > 1 and t.stride(1) != 1)):
+        want = "" if shape is None else f" {list(shape)}"
+        kind = "fp32, bf16 or fp16" if dtype is None else str(dtype)
+        raise ValueError(f"{name} must be a CUDA {kind} tensor{want} with contiguous rows"
+                         + ("" if device is None else f" on {device}"))
+    if t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{name} is on {t.device}, not on the current device "
+                         f"cuda:{torch.cuda.current_device()}")
+    stride = t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+    if stride < t.shape[1]:
+        raise ValueError(f"{name}: rows overlap (stride {t.stride(0)})")
+    return Dense(t.data_ptr(), stride, ty)
+
+
+class Fp4Tensor:
+    """A [rows][K] tensor in microscaled 4-bit floating point on the device:
+    `codes` uint8 [rows][code_stride] and `scales` uint8 as polyq_fp4.h lays
+    them out, `format` FP4_MX or FP4_NV, `tensor_scale` (FP4_NV)."""
+
+    def __init__(self, codes, scales, rows, K, format, tensor_scale=1.0):
+        import torch
+        stride, nbytes = C.c_int64(), C.c_int64()
+        _check(_lib.polyq_fp4_bytes(int(rows), int(K), int(format), C.byref(stride), C.byref(nbytes)))
+        _require(codes, "codes", torch.uint8, (rows, stride.value), codes.device)
+        _require(scales, "scales", torch.uint8, (nbytes.value,), codes.device)
+        self.codes, self.scales = codes, scales
+        self.rows, self.K, self.format = int(rows), int(K), int(format)
+        self.tensor_scale = float(tensor_scale)
+        self.desc = Fp4Desc(codes.data_ptr(), scales.data_ptr(), self.rows, self.K, stride.value,
+                            self.format, self.tensor_scale)
+
+    @classmethod
+    def empty(cls, rows, K, format=FP4_MX, tensor_scale=1.0, device="cuda"):
+        """An unset tensor, to be written by fp4_quantize or fp4_ffn."""
+        import torch
+        stride, nbytes = C.c_int64(), C.c_int64()
+        _check(_lib.polyq_fp4_bytes(int(rows), int(K), int(format), C.byref(stride), C.byref(nbytes)))
+        return cls(torch.empty((rows, stride.value), dtype=torch.uint8, device=device),
+                   torch.empty(nbytes.value, dtype=torch.uint8, device=device), rows, K, format,
+                   tensor_scale)
+
+    @staticmethod
+    def _places(rows, blocks, device):
+        """Byte of each (row, block)'s scale: int64 [rows][blocks]."""
+        import torch
+        r = torch.arange(rows, device=device)[:, None]
+        b = torch.arange(blocks, device=device)[None]
+        return (r // 128 * ((blocks + 3) // 4) + b // 4) * 512 + r % 32 * 16 + r // 32 % 4 * 4 + b % 4
+
+    @classmethod
+    def pack(cls, codes, scales, format=FP4_MX, tensor_scale=1.0):
+        """From plain codes (uint8 [rows][K], 0..15) and scale bytes (uint8
+        [rows][blocks]), as a checkpoint holds them."""
+        import torch
+        rows, K = codes.shape
+        blocks = -(-K // (16 if format == FP4_NV else 32))
+        if codes.dtype != torch.uint8 or scales.dtype != torch.uint8 or tuple(scales.shape) != (rows, blocks):
+            raise ValueError(f"codes must be uint8 [rows][K], scales uint8 [{rows}][{blocks}]")
+        t = cls.empty(rows, K, format, tensor_scale, codes.device)
+        t.codes.zero_()
+        t.scales.zero_()
+        c = torch.nn.functional.pad(codes, (0, K % 2)) & 15
+        t.codes[:, :(K + 1) // 2] = c[:, 0::2] | c[:, 1::2] << 4
+        t.scales[cls._places(rows, blocks, codes.device)] = scales
+        return t
+
+    def unpack(self):
+        """Plain codes (uint8 [rows][K]) and scale bytes (uint8 [rows][blocks])."""
+        import torch
+        c = self.codes[:, :(self.K + 1) // 2]
+        codes = torch.stack((c & 15, c >> 4), 2).reshape(self.rows, -1)[:, :self.K].contiguous()
+        blocks = -(-self.K // (16 if self.format == FP4_NV else 32))
+        return codes, self.scales[self._places(self.rows, blocks, c.device)]
+
+
+def _fp4(t, name, device=None):
+    import torch
+    if not isinstance(t, Fp4Tensor) or not t.codes.is_cuda or (device is not None and t.codes.device != device):
+        raise ValueError(f"{name} must be an Fp4Tensor" + (" on a CUDA device" if device is None else f" on {device}"))
+    if t.codes.device.index != torch.cuda.current_device():
+        raise ValueError(f"{name} is on {t.codes.device}, not on the current device "
+                         f"cuda:{torch.cuda.current_device()}")
+    return C.byref(t.desc)
+
+
+def fp4_tensor_scale(amax: float) -> float:
+    """A tensor scale for FP4_NV: the smallest power of two (so that dividing
+    by it is exact) with which a block whose largest value is `amax` keeps its
+    scale within e4m3's range."""
+    import math
+    if not math.isfinite(amax) or amax < 0:
+        raise ValueError(f"amax must be finite and not negative, got {amax}")
+    if amax == 0:
+        return 1.0
+    m, e = math.frexp(amax / (6 * 448))
+    return 2.0 ** max(-126, e - 1 if m == 0.5 else e)
+
+
+def fp4_workspace(device="cuda"):
+    """A zeroed workspace for fp4_linear, fp4_ffn and ffn_forward."""
+    import torch
+    return torch.zeros(FP4_WORKSPACE_BYTES, dtype=torch.uint8, device=device)
+
+
+def fp4_quantize(x, format=FP4_MX, tensor_scale=1.0, out=None, stream=None):
+    """x [rows][K] (fp32, bf16 or fp16; any row stride) in 4 bits.  With `out`
+    its format and tensor scale are used."""
+    d = _dense(x, "x")
+    if out is None:
+        out = Fp4Tensor.empty(x.shape[0], x.shape[1], format, tensor_scale, x.device)
+    o = _fp4(out, "out", x.device)
+    if (out.rows, out.K) != tuple(x.shape):
+        raise ValueError(f"out is [{out.rows}][{out.K}], x {list(x.shape)}")
+    _check(_lib.polyq_fp4_quantize(C.byref(d), o, _stream_ptr(stream)))
+    return out
+
+
+def fp4_dequantize(t: Fp4Tensor, dtype=None, out=None, stream=None):
+    """The values of a 4-bit tensor (default fp32)."""
+    import torch
+    p = _fp4(t, "t")
+    if out is None:
+        out = torch.empty((t.rows, t.K), dtype=dtype or torch.float32, device=t.codes.device)
+    d = _dense(out, "out", (t.rows, t.K), t.codes.device, dtype)
+    _check(_lib.polyq_fp4_dequantize(p, C.byref(d), _stream_ptr(stream)))
+    return out
+
+
+def _fp4_workspace(workspace, dev):
+    return _workspace_of(workspace, lambda: FP4_WORKSPACE_BYTES, True, dev)
+
+
+def fp4_linear(x: Fp4Tensor, w: Fp4Tensor, y=None, residual=None, dtype=None, workspace=None,
+               stream=None):
+    """y[m][n] = residual[m][n] + sum_k x[m][k] w[n][k], both operands in one
+    4-bit format.  y: fp32 (default), bf16 or fp16; residual of y's type, may be
+    y itself."""
+    import torch
+    dev = x.codes.device if isinstance(x, Fp4Tensor) else None
+    px, pw = _fp4(x, "x"), _fp4(w, "w", dev)
+    if y is None:
+        y = torch.empty((x.rows, w.rows), dtype=dtype or (residual.dtype if residual is not None
+                                                          else torch.float32), device=dev)
+    dy = _dense(y, "y", (x.rows, w.rows), dev, dtype)
+    dr = None if residual is None else _dense(residual, "residual", (x.rows, w.rows), dev, y.dtype)
+    workspace = _fp4_workspace(workspace, dev)
+    _check(_lib.polyq_fp4_linear(px, pw, C.byref(dr) if dr is not None else None, C.byref(dy),
+                                 workspace.data_ptr(), workspace.numel(), _stream_ptr(stream)))
+    return y
+
+
+def fp4_ffn(x: Fp4Tensor, gate: Fp4Tensor, up: Fp4Tensor, h=None, dtype=None, workspace=None,
+            stream=None):
+    """h = silu(x gate^T) * (x up^T) in one kernel.  h: a tensor (default bf16)
+    or an Fp4Tensor, which receives h quantised as fp4_quantize does."""
+    import torch
+    dev = x.codes.device if isinstance(x, Fp4Tensor) else None
+    px, pg, pu = _fp4(x, "x"), _fp4(gate, "gate", dev), _fp4(up, "up", dev)
+    if h is None:
+        h = torch.empty((x.rows, gate.rows), dtype=dtype or torch.bfloat16, device=dev)
+    workspace = _fp4_workspace(workspace, dev)
+    dh = dq = None
+    if isinstance(h, Fp4Tensor):
+        dq = _fp4(h, "h", dev)
+    else:
+        d = _dense(h, "h", (x.rows, gate.rows), dev, dtype)
+        dh = C.byref(d)
+    _check(_lib.polyq_fp4_ffn(px, pg, pu, dh, dq, workspace.data_ptr(), workspace.numel(),
+                              _stream_ptr(stream)))
+    return h
+
+
+def ffn_saved(T, F, dtype, device="cuda"):
+    """The buffer that ffn_forward fills for ffn_backward."""
+    import torch
+    return torch.empty((2, T, _lib.polyq_ffn_saved_stride(F)), dtype=dtype, device=device)
+
+
+def ffn_workspace(T, F, K=None, device="cuda"):
+    """A zeroed workspace for ffn_forward and ffn_backward (K does not matter)."""
+    import torch
+    n = C.c_size_t()
+    _check(_lib.polyq_ffn_backward_workspace_bytes(int(T), int(F), C.byref(n)))
+    ws = torch.empty(n.value, dtype=torch.uint8, device=device)
+    ws[:FP4_WORKSPACE_BYTES].zero_()
+    return ws
+
+
+def _ffn_inputs(x, gate, up):
+    dx = _dense(x, "x")
+    T, K = x.shape
+    dg = _dense(gate, "gate", None, x.device, x.dtype)
+    F = gate.shape[0]
+    if gate.shape[1] != K:
+        raise ValueError(f"gate is {list(gate.shape)}, x {list(x.shape)}")
+    return dx, dg, _dense(up, "up", (F, K), x.device, x.dtype), T, F, K
+
+
+def ffn_forward(x, gate, up, h=None, saved=None, workspace=None, stream=None):
+    """h = silu(x gate^T) * (x up^T) on bf16 or fp16 operands, one kernel.
+    `saved` (ffn_saved) receives what ffn_backward needs."""
+    import torch
+    dx, dg, du, T, F, K = _ffn_inputs(x, gate, up)
+    if h is None:
+        h = torch.empty((T, F), dtype=x.dtype, device=x.device)
+    dh = _dense(h, "h", (T, F), x.device, x.dtype)
+    if saved is not None:
+        _require(saved, "saved", x.dtype, (2, T, _lib.polyq_ffn_saved_stride(F)), x.device)
+    workspace = _fp4_workspace(workspace, x.device)
+    _check(_lib.polyq_ffn_forward(C.byref(dx), C.byref(dg), C.byref(du), T, F, K, C.byref(dh),
+                                  saved.data_ptr() if saved is not None else None,
+                                  workspace.data_ptr(), workspace.numel(), _stream_ptr(stream)))
+    return h
+
+
+def ffn_backward(x, gate, up, saved, dh, dx=None, dgate=None, dup=None, need_dx=True,
+                 need_weights=True, workspace=None, stream=None):
+    """Gradients (dx, dgate, dup) of ffn_forward for the gradient dh of h; each
+    of x's type or, where a buffer of that type is passed, fp32.  Those not
+    needed are None."""
+    import torch
+    ix, ig, iu, T, F, K = _ffn_inputs(x, gate, up)
+    dev, ty = x.device, x.dtype
+    idh = _dense(dh, "dh", (T, F), dev, ty)
+    _require(saved, "saved", ty, (2, T, _lib.polyq_ffn_saved_stride(F)), dev)
+    if dx is None and need_dx:
+        dx = torch.empty((T, K), dtype=ty, device=dev)
+    if dgate is None and need_weights:
+        dgate = torch.empty((F, K), dtype=ty if dup is None else dup.dtype, device=dev)
+    if dup is None and need_weights:
+        dup = torch.empty((F, K), dtype=dgate.dtype, device=dev)
+    outs = [None if t is None else _dense(t, n, s, dev) for t, n, s in
+            ((dx, "dx", (T, K)), (dgate, "dgate", (F, K)), (dup, "dup", (F, K)))]
+    if workspace is None:
+        workspace = ffn_workspace(T, F, K, dev)
+    _require(workspace, "workspace", torch.uint8, (workspace.numel(),), dev)
+    _check(_lib.polyq_ffn_backward(C.byref(ix), C.byref(ig), C.byref(iu), T, F, K,
+                                   saved.data_ptr(), C.byref(idh),
+                                   *[C.byref(o) if o is not None else None for o in outs],
+                                   workspace.data_ptr(), workspace.numel(), _stream_ptr(stream)))
+    return dx, dgate, dup
