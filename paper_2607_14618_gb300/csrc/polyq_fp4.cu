@@ -6,9 +6,8 @@
 // A lane holds 8 consecutive elements of a row, so a warp takes 256 elements:
 // a block is four (MX) or two (NV) neighbouring lanes, its maximum two or one
 // shuffles, and the 8 codes of a lane one 4-byte store (a warp stores 128
-// consecutive bytes).  The scales of four blocks are gathered into the 4-byte
-// word that the tensor cores' scale layout keeps together.  Bound by HBM for
-// large tensors and by the launch for a token's.
+// consecutive bytes).  Bound by HBM for large tensors and by the launch for a
+// token's.
 #include <algorithm>
 #include <cmath>
 #include <cstring>
@@ -21,7 +20,7 @@ namespace {
 
 using namespace polyq;
 
-constexpr int kWarps = 8;
+constexpr int kWarps = 4;  // of a CTA, side by side along a row: 1024 elements
 
 struct QuantParams {
   const void* x;
@@ -29,8 +28,9 @@ struct QuantParams {
   uint8_t* codes;
   uint8_t* scales;
   int64_t x_stride, y_stride, code_stride, rows, K, A;
-  int64_t chunks, tasks;  // 256-element chunks of a row; (row group, chunk) pairs
+  int64_t row_groups;     // of 1 or 4 rows
   float g, inv_g;         // tensor scale; its reciprocal where that is exact, else 0
+  int short_ok;           // and no product of it with a block scale's leaves fp32's range
 };
 
 template <typename T>
@@ -51,82 +51,127 @@ struct Elem<__half> {
   static __device__ __forceinline__ __half from(float v) { return __float2half_rn(v); }
 };
 
-// 8 elements from k on; zeros past K.  VEC: rows start on 16 bytes.
-template <typename T, bool VEC>
-__device__ __forceinline__ void load8(const T* __restrict__ row, int64_t k, int64_t K, float (&v)[8]) {
-  if (VEC && k + 8 <= K) {
-    constexpr int N16 = sizeof(T) * 8 / 16;
-    uint4 raw[N16];
+// 8 elements from k on as they lie in memory, and as floats; zeros past K.  VEC:
+// rows start on 16 bytes.  (Two steps, so that the loads of several rows are in
+// flight before the first is converted: 13824 x 5120 bf16 63 us with one.)
+template <typename T>
+struct Raw8 {
+  uint4 w[sizeof(T) * 8 / 16];
+};
+template <typename T, bool VEC, bool FULL>
+__device__ __forceinline__ void load8(const T* __restrict__ row, int64_t k, int64_t K, Raw8<T>& r) {
+  constexpr int N16 = sizeof(T) * 8 / 16;
+  if (VEC && (FULL || k + 8 <= K)) {
 #pragma unroll
-    for (int i = 0; i < N16; ++i) raw[i] = __ldg(reinterpret_cast<const uint4*>(row + k) + i);
-    const T* e = reinterpret_cast<const T*>(raw);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = Elem<T>::to(e[i]);
+    for (int i = 0; i < N16; ++i) r.w[i] = __ldg(reinterpret_cast<const uint4*>(row + k) + i);
   } else {
+    alignas(16) T e[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = k + i < K ? Elem<T>::to(row[k + i]) : 0.f;
+    for (int i = 0; i < 8; ++i) e[i] = FULL || k + i < K ? row[k + i] : Elem<T>::from(0.f);
+#pragma unroll
+    for (int i = 0; i < N16; ++i) r.w[i] = reinterpret_cast<const uint4*>(e)[i];
   }
 }
+// Bits of the largest |element| as a float's (NaN above infinity).
+__device__ __forceinline__ uint32_t abs_max(const Raw8<float>& r) {
+  const uint32_t* e = reinterpret_cast<const uint32_t*>(r.w);
+  uint32_t m = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) m = max(m, e[i] & 0x7FFFFFFFu);
+  return m;
+}
+template <typename T>
+__device__ __forceinline__ uint32_t abs_max(const Raw8<T>& r) {
+  const uint32_t* e = reinterpret_cast<const uint32_t*>(r.w);
+  uint32_t m = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) m = __vmaxu2(m, e[i] & 0x7FFF7FFFu);
+  const uint16_t h = (uint16_t)max(m & 0xFFFFu, m >> 16);
+  return __float_as_uint(Elem<T>::to(*reinterpret_cast<const T*>(&h))) & 0x7FFFFFFFu;
+}
+template <typename T>
+__device__ __forceinline__ void to_float(const Raw8<T>& r, float (&v)[8]) {
+  const T* e = reinterpret_cast<const T*>(r.w);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = Elem<T>::to(e[i]);
+}
 
-// ROWS rows of a chunk per warp, their loads in flight together.
+// A CTA takes 1024 elements of ROWS consecutive rows, a warp 256, the loads of
+// its rows in flight together.  FULL: all of a warp's elements exist (the
+// checks took a third of the instructions, which bound 16-bit inputs: 13824 x
+// 5120 bf16 MX 34 us with them, 29.5 without, 6.1 TB/s).  A flat index of
+// (rows, chunk) pairs needs two 64-bit divisions a warp: 55 us.
+template <typename T, bool NV, bool VEC, int ROWS, bool FULL>
+__device__ __forceinline__ void quantize_rows(const QuantParams& P, int64_t r0, int64_t k) {
+  constexpr int LPB = NV ? 2 : 4;  // lanes of a block
+  const int64_t b = k / (8 * LPB);
+  const int n = FULL ? ROWS : (int)min((int64_t)ROWS, P.rows - r0);
+  const bool scale = threadIdx.x % LPB == 0 && (FULL || (b >> 2) < P.A), code = FULL || k < P.K;
+  Raw8<T> raw[ROWS];
+  const T* x = (const T*)P.x + r0 * P.x_stride;
+#pragma unroll
+  for (int i = 0; i < ROWS; ++i) {  // (a row past the last: the last one again, not stored)
+    load8<T, VEC, FULL>(x, k, P.K, raw[i]);
+    if (FULL || i + 1 < n) x += P.x_stride;
+  }
+  // ROWS consecutive rows from a multiple of ROWS lie in one group of 32: 16 bytes apart
+  uint8_t* sp = P.scales + fp4::scale_off(r0, b, P.A);
+  uint8_t* cp = P.codes + r0 * P.code_stride + k / 2;
+#pragma unroll
+  for (int i = 0; i < ROWS; ++i) {
+    if (!FULL && i >= n) break;  // the same for the whole warp
+    uint32_t m = abs_max(raw[i]);
+    m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
+    if (!NV) m = max(m, __shfl_xor_sync(0xffffffffu, m, 2));
+    float v[8];
+    to_float(raw[i], v);
+    // NV: dividing by the tensor scale keeps the order, the largest stays the largest
+    if (NV) m = __float_as_uint(P.inv_g != 0.f ? __uint_as_float(m) * P.inv_g : __fdiv_rn(__uint_as_float(m), P.g));
+    const fp4::Scale<NV> sc(m);
+    uint32_t c;
+    if (NV && sizeof(T) == 2 && P.short_ok) {
+      c = sc.codes_short(v, sc.r * P.inv_g);
+    } else {
+      if (NV) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = P.inv_g != 0.f ? v[j] * P.inv_g : __fdiv_rn(v[j], P.g);
+      }
+      c = sc.codes(v);
+    }
+    if (code) *reinterpret_cast<uint32_t*>(cp) = c;
+    if (scale) sp[16 * i] = (uint8_t)sc.byte;
+    cp += P.code_stride;
+  }
+}
 template <typename T, bool NV, bool VEC, int ROWS>
 __global__ void __launch_bounds__(32 * kWarps) quantize_kernel(const __grid_constant__ QuantParams P) {
-  const int lane = threadIdx.x & 31;
+  const int64_t k = (int64_t)blockIdx.x * (256 * kWarps) + threadIdx.x * 8;
+  const bool cols = k - threadIdx.x % 32 * 8 + 256 <= P.K;
   pdl_trigger();
   pdl_wait();
-  for (int64_t task = (int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5); task < P.tasks;
-       task += (int64_t)gridDim.x * kWarps) {
-    const int64_t r0 = task / P.chunks * ROWS, k = (task % P.chunks) * 256 + lane * 8;
-    float v[ROWS][8];
-#pragma unroll
-    for (int i = 0; i < ROWS; ++i)
-      if (r0 + i < P.rows) load8<T, VEC>((const T*)P.x + (r0 + i) * P.x_stride, k, P.K, v[i]);
-#pragma unroll
-    for (int i = 0; i < ROWS; ++i) {
-      const int64_t r = r0 + i;
-      if (r >= P.rows) break;  // the same for the whole warp
-      uint32_t m = 0;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        if (NV) v[i][j] = P.inv_g != 0.f ? v[i][j] * P.inv_g : __fdiv_rn(v[i][j], P.g);
-        m = max(m, __float_as_uint(v[i][j]) & 0x7FFFFFFFu);
-      }
-      m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
-      if (!NV) m = max(m, __shfl_xor_sync(0xffffffffu, m, 2));
-      const fp4::Scale<NV> sc(m);
-      float q[8];
-#pragma unroll
-      for (int j = 0; j < 8; ++j) q[j] = sc.div(v[i][j]);
-      if (k < P.K) *reinterpret_cast<uint32_t*>(P.codes + r * P.code_stride + k / 2) = fp4::codes8(q);
-      // the word of four blocks: byte b % 4 from each
-      constexpr int LPB = NV ? 2 : 4;  // lanes of a block
-      uint32_t w = sc.byte << (8 * (lane / LPB % 4));
-      w |= __shfl_xor_sync(0xffffffffu, w, LPB);
-      w |= __shfl_xor_sync(0xffffffffu, w, 2 * LPB);
-      const int64_t b = k / (8 * LPB);
-      if (lane % (4 * LPB) == 0 && (b >> 2) < P.A)
-        *reinterpret_cast<uint32_t*>(P.scales + fp4::scale_off(r, b, P.A)) = w;
-    }
+  for (int64_t rg = blockIdx.y; rg < P.row_groups; rg += gridDim.y) {
+    if (cols && (rg + 1) * ROWS <= P.rows) quantize_rows<T, NV, VEC, ROWS, true>(P, rg * ROWS, k);
+    else quantize_rows<T, NV, VEC, ROWS, false>(P, rg * ROWS, k);
   }
 }
 
 template <typename T, bool NV, bool VEC, int ROWS>
 __global__ void __launch_bounds__(32 * kWarps) dequantize_kernel(const __grid_constant__ QuantParams P) {
-  const int lane = threadIdx.x & 31;
+  const int64_t k = (int64_t)blockIdx.x * (256 * kWarps) + threadIdx.x * 8, b = k / fp4::block_len(NV);
   pdl_trigger();
   pdl_wait();
-  for (int64_t task = (int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5); task < P.tasks;
-       task += (int64_t)gridDim.x * kWarps) {
-    const int64_t r0 = task / P.chunks * ROWS, k = (task % P.chunks) * 256 + lane * 8;
-    if (k >= P.K) continue;
+  if (k >= P.K) return;
+  for (int64_t rg = blockIdx.y; rg < P.row_groups; rg += gridDim.y) {
+    const int64_t r0 = rg * ROWS;
+    const uint8_t* sp = P.scales + fp4::scale_off(r0, b, P.A);
+    const uint8_t* cp = P.codes + r0 * P.code_stride + k / 2;
     uint32_t c[ROWS], sb[ROWS];
 #pragma unroll
-    for (int i = 0; i < ROWS; ++i)
-      if (r0 + i < P.rows) {
-        // rows are padded to 16 bytes, so a lane's 4 bytes exist
-        c[i] = __ldg(reinterpret_cast<const uint32_t*>(P.codes + (r0 + i) * P.code_stride + k / 2));
-        sb[i] = __ldg(P.scales + fp4::scale_off(r0 + i, k / fp4::block_len(NV), P.A));
-      }
+    for (int i = 0; i < ROWS; ++i) {
+      const int at = (int)min((int64_t)i, P.rows - 1 - r0);  // (past the last row: the last one again)
+      c[i] = __ldg(reinterpret_cast<const uint32_t*>(cp + at * P.code_stride));  // rows are padded to 16 bytes
+      sb[i] = __ldg(sp + 16 * at);
+    }
 #pragma unroll
     for (int i = 0; i < ROWS; ++i) {
       if (r0 + i >= P.rows) break;
@@ -180,10 +225,11 @@ int launch(QuantParams& P, const polyq_fp4* t, const polyq_dense* d, bool quanti
   int e;
   P.inv_g = std::frexp(P.g, &e) == 0.5f ? 1.f / P.g : 0.f;
   if (!std::isfinite(P.inv_g)) P.inv_g = 0.f;
-  P.chunks = (P.K + 255) / 256;
+  P.short_ok = P.inv_g != 0.f && P.g >= 0x1p-100f && P.g <= 0x1p100f;
+  const int64_t chunks = (P.K + 255) / 256;
   // four rows a warp once that still gives every SM a full set of warps
-  const bool rows4 = P.rows * P.chunks >= (int64_t)sms * 64 * 4;
-  P.tasks = (P.rows + (rows4 ? 3 : 0)) / (rows4 ? 4 : 1) * P.chunks;
+  const bool rows4 = P.rows * chunks >= (int64_t)sms * 64 * 4;
+  P.row_groups = rows4 ? (P.rows + 3) / 4 : P.rows;
   const int eb = elem_bytes(d->type);
   const bool vec = (uintptr_t)d->data % 16 == 0 && d->stride * eb % 16 == 0;
   void* f;
@@ -198,7 +244,7 @@ int launch(QuantParams& P, const polyq_fp4* t, const polyq_dense* d, bool quanti
   cfg.stream = (cudaStream_t)stream;
   cfg.attrs = at;
   cfg.numAttrs = 1;
-  cfg.gridDim = dim3((unsigned)std::min<int64_t>((P.tasks + kWarps - 1) / kWarps, 1 << 30));
+  cfg.gridDim = dim3((unsigned)((chunks + kWarps - 1) / kWarps), (unsigned)std::min<int64_t>(P.row_groups, 65535));
   cfg.blockDim = dim3(32 * kWarps);
   void* args[] = {&P};
   cudaError_t ce = cudaLaunchKernelExC(&cfg, f, args);

@@ -57,6 +57,22 @@ __device__ __forceinline__ float from_e8m0(uint32_t byte) {
                                                                 : __uint_as_float(byte << 23);
 }
 
+// a / d for a small integer or e4m3 d, from r = 1 / d to a unit: one residual
+// step (Markstein 1990).  Its error, 2^-44, is far less than what a quotient that
+// is not on a border of the next rounding (an e2m1 or e4m3 midpoint, at most 5
+// significant bits) is away from it: a differs from border * d, which fp32
+// holds, by a unit, so the quotient by 2^-31 more than half a unit, and the two
+// roundings fall as one rounding of the exact quotient does.
+__device__ __forceinline__ float quotient(float a, float d, float r) {
+  const float q = a * r;
+  return __fmaf_rn(__fmaf_rn(-q, d, a), r, q);
+}
+__device__ __forceinline__ float rcp_approx(float v) {
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+  return r;
+}
+
 // A block's scale byte and how its elements are divided by the scale.
 template <bool NV>
 struct Scale {
@@ -67,27 +83,35 @@ struct Scale {
   __device__ __forceinline__ explicit Scale(uint32_t amax) {
     const bool bad = amax >= 0x7F800000u;
     if (NV) {
-      byte = bad ? 0x7Fu : to_e4m3(__fdiv_rn(__uint_as_float(amax), 6.f));
+      byte = bad ? 0x7Fu : to_e4m3(quotient(__uint_as_float(amax), 6.f, 1.f / 6.f));
       s = from_e4m3(byte);
       zero = bad || byte == 0;
-      r = zero ? 0.f : __frcp_rn(s);
+      r = zero ? 0.f : rcp_approx(s);
     } else {
       const int e = (int)(amax >> 23) - 2;  // floor(log2) - 2, biased; at least 2^-127
       byte = bad ? 255u : (uint32_t)max(e, 0);
       zero = bad;
-      r = __uint_as_float((254u - (byte & 0xFFu)) << 23);
+      r = bad ? 0.f : __uint_as_float((254u - byte) << 23);
       s = 0.f;
     }
   }
-  // t / scale.  MX: a power of two, exact.  NV: the quotient rounded to nearest
-  // (Markstein 1990: one residual step behind a correctly rounded reciprocal),
-  // so that a quotient on the border of two codes is on it in fp32, and one
-  // beside it stays beside it: t differs from border * s by 2^-24 of it or more.
-  __device__ __forceinline__ float div(float t) const {
-    if (zero) return 0.f;
-    if (!NV) return t * r;
-    const float q = t * r;
-    return __fmaf_rn(__fmaf_rn(-q, s, t), r, q);
+  // Codes of eight t.  MX: t / scale is exact, a power of two.
+  __device__ __forceinline__ uint32_t codes(const float (&t)[8]) const {
+    float q[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) q[i] = NV ? quotient(t[i], s, r) : t[i] * r;
+    return zero ? 0u : codes8(q);
+  }
+  // NV, eight elements v = t g of 16-bit types with r_g = 1 / (s g) to two units
+  // (g a power of two): t has at most 11 significant bits, so a quotient that is
+  // not on a border of two codes is 2^-13 or more from it, and rounding it to
+  // a multiple of 2^-16 (the sum with 192) leaves it on its side and puts one that
+  // is on the border there.
+  __device__ __forceinline__ uint32_t codes_short(const float (&v)[8], float r_g) const {
+    float q[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) q[i] = __fadd_rn(__fmaf_rn(v[i], r_g, 192.f), -192.f);
+    return zero ? 0u : codes8(q);
   }
 };
 

@@ -169,10 +169,10 @@ __device__ __forceinline__ void store_codes32(const MmParams& P, int64_t m, int6
     const fp4::Scale<NV> sc(mx);
 #pragma unroll
     for (int i = 0; i < BL / 8; ++i) {
-      float q[8];
+      float t[8];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) q[j] = sc.div(v[BL * b + 8 * i + j]);
-      c[b * BL / 8 + i] = fp4::codes8(q);
+      for (int j = 0; j < 8; ++j) t[j] = v[BL * b + 8 * i + j];
+      c[b * BL / 8 + i] = sc.codes(t);
     }
     const int64_t blk = f0 / BL + b;
     if (blk >> 2 < P.out_atoms) P.scales[fp4::scale_off(m, blk, P.out_atoms)] = (uint8_t)sc.byte;
@@ -197,15 +197,17 @@ struct Pair {
   static constexpr int kBOff = STAGES * kOpBytes, kSaOff = kBOff + STAGES * kB;
   static constexpr int kSbOff = kSaOff + STAGES * kSa;
   static constexpr size_t kSmem = (size_t)STAGES * kStage + 1024;
-  // Tensor memory: two accumulators of NT columns and two stages' scales.  With
-  // NT = 256 and scales the accumulators share OV columns: the epilogue drains
-  // those first and releases them for the next tile before the rest.
+  // Tensor memory: two accumulators of NT columns and a ring of SF stages'
+  // scales.  With NT = 256 and scales the accumulators share OV columns: the
+  // epilogue drains those first and releases them for the next tile before the
+  // rest.
+  static constexpr int SF = 2;
   static constexpr int kSfStage = ATOMS * 4 * (1 + GROUPS);
-  static constexpr int kSfCols = (2 * kSfStage + 31) / 32 * 32;
+  static constexpr int kSfCols = (SF * kSfStage + 31) / 32 * 32;
   static constexpr int kSfCol = NT == 256 ? 512 - kSfCols : 2 * NT;
   static constexpr int kAcc1 = NT == 256 ? kSfCol - 256 : NT;
   static constexpr int OV = NT - kAcc1;
-  static constexpr int kEpiWarp = 4, EPI = 8;
+  static constexpr int kEpiWarp = 4, EPI = 12, EPQ = EPI / 4;  // EPQ warps to a quarter of the lanes
   static constexpr int kThreads = 32 * (kEpiWarp + EPI);
   static_assert(kSfCol + kSfCols <= 512 && OV % 32 == 0 && STAGES >= 4, "");
 };
@@ -339,8 +341,10 @@ __global__ void __launch_bounds__(C::kThreads, 1) mm_pair(const __grid_constant_
   } else if (warp == 1 && rank == 0) {
     // ---------------- MMA issuer (leader CTA) ----------------
     if (elect_one()) {
-      int s = 0, it = 0, tc = 0;
-      uint32_t ph = 0;
+      int s = 0, tc = 0;
+      bool ready = false;            // stage s is known to have landed
+      int sf = 0, so = 0, held = 0;  // scales: next slot; the oldest stage in use, and how many are
+      uint32_t ph = 0, so_ph = 0;
       const uint64_t a0 = desc_sw128(smem_u32(smem), P.a_mn ? 8192 : 16);
       const uint64_t b0 = desc_sw128(smem_u32(smem + C::kBOff), P.b_mn ? 8192 : 16);
       const uint64_t sa0 = desc_scales(smem_u32(smem + C::kSaOff));
@@ -361,16 +365,29 @@ __global__ void __launch_bounds__(C::kThreads, 1) mm_pair(const __grid_constant_
         }
         tc_fence_after();
         const uint32_t acc = tmem + (buf ? C::kAcc1 : 0);
-        for (int i = 0; i < n_it; ++i, ++it) {
-          w = wait(smem_u32(&bar_full[s]), ph, &s_abort);
-          // the scale columns of two stages ago are free once that stage's MMAs are done
-          if (C::KIND != k16 && w == kOk && it >= 2)
-            w = wait(smem_u32(&bar_empty[(it - 2) % C::STAGES]), ((it - 2) / C::STAGES) & 1, &s_abort);
-          if (w != kOk) {
-            if (w == kTimeout) fail(kStatusTimeoutFull);
-            break;
+        for (int i = 0; i < n_it; ++i) {
+          if (!ready) {
+            w = wait(smem_u32(&bar_full[s]), ph, &s_abort);
+            if (w != kOk) {
+              if (w == kTimeout) fail(kStatusTimeoutFull);
+              break;
+            }
           }
           tc_fence_after();
+          // asked for here, needed when this stage's MMAs have been issued: a
+          // poll's answer takes 250 to 300 cycles beside the tensor core's traffic
+          const int s1 = s + 1 == C::STAGES ? 0 : s + 1;
+          const uint32_t ph1 = s1 == 0 ? ph ^ 1u : ph;
+          ready = mbar_test(smem_u32(&bar_full[s1]), ph1);
+          auto release = [&](int n) {
+            held -= n;
+            so += n;
+            if (so >= C::STAGES) {
+              so -= C::STAGES;
+              so_ph ^= 1u;
+            }
+          };
+          if (C::KIND != k16) release(min(held, poll_ahead<2, C::STAGES>(smem_u32(&bar_empty[0]), so, so_ph)));
           const int kt = i >= P.kt ? i - P.kt : i;
           const int n_mma = kt == P.kt - 1 ? P.k_last : 4;
           const uint64_t a = a0 + (uint64_t)((s * kOpBytes) >> 4), b = b0 + (uint64_t)((s * C::kB) >> 4);
@@ -378,28 +395,38 @@ __global__ void __launch_bounds__(C::kThreads, 1) mm_pair(const __grid_constant_
             for (int kk = 0; kk < n_mma; ++kk)
               mma_16<2>(acc, a + (uint64_t)(kk * a_step), b + (uint64_t)(kk * b_step), P.idesc, (i | kk) > 0);
           } else {
-            const uint32_t sf = tmem + C::kSfCol + (it & 1) * C::kSfStage;
+            constexpr bool NV = C::KIND == kNv;
             const uint64_t sa = sa0 + (uint64_t)((s * C::kSa) >> 4), sb = sb0 + (uint64_t)((s * C::kSb) >> 4);
+            if (held == C::SF) {  // a slot's scales stay until its stage's MMAs are done
+              w = wait(smem_u32(&bar_empty[so]), so_ph, &s_abort);
+              if (w != kOk) {
+                if (w == kTimeout) fail(kStatusTimeoutEmpty);
+                break;
+              }
+              release(1);
+            }
+            const uint32_t c0 = tmem + C::kSfCol + sf * C::kSfStage;
 #pragma unroll
             for (int q = 0; q < C::ATOMS; ++q) {
-              const uint32_t c = sf + q * 4 * (1 + C::GROUPS);
+              const uint32_t c = c0 + q * 4 * (1 + C::GROUPS);
               copy_scales<2>(c, sa + (uint64_t)(q * 32));
 #pragma unroll
               for (int j = 0; j < C::GROUPS; ++j)
                 copy_scales<2>(c + 4 + 4 * j, sb + (uint64_t)((j * C::ATOMS + q) * 32));
             }
-            for (int kk = 0; kk < n_mma; ++kk) {
-              constexpr bool NV = C::KIND == kNv;
-              const uint32_t c = sf + (NV ? kk : kk >> 1) * 4 * (1 + C::GROUPS);
-              const uint32_t id = NV || !(kk & 1) ? P.idesc : P.idesc | idesc_fp4(0, 0, false, 2);
-              mma_fp4<2, NV>(acc, a + (uint64_t)(2 * kk), b + (uint64_t)(2 * kk), id, c, c + 4, (i | kk) > 0);
+#pragma unroll
+            for (int kk = 0; kk < 4; ++kk) {
+              if (kk >= n_mma) break;
+              const uint32_t c = c0 + (NV ? kk : kk >> 1) * 4 * (1 + C::GROUPS);
+              mma_fp4<2, NV>(acc, a + (uint64_t)(2 * kk), b + (uint64_t)(2 * kk),
+                             NV || !(kk & 1) ? P.idesc : P.idesc | idesc_fp4(0, 0, false, 2), c, c + 4, (i | kk) > 0);
             }
+            if (++sf == C::SF) sf = 0;
+            ++held;
           }
           commit<2>(smem_u32(&bar_empty[s]));
-          if (++s == C::STAGES) {
-            s = 0;
-            ph ^= 1u;
-          }
+          s = s1;
+          ph = ph1;
         }
         commit<2>(smem_u32(&bar_accf[buf]));
       }
@@ -413,7 +440,7 @@ __global__ void __launch_bounds__(C::kThreads, 1) mm_pair(const __grid_constant_
     if (elect_one()) wait_stay(smem_u32(&bar_done), 0);
   } else if (warp >= C::kEpiWarp) {
     // ---------------- epilogue: a lane owns a row of the tile ----------------
-    const int q = warp & 3, half = (warp - C::kEpiWarp) >> 2;
+    const int q = warp & 3, e0 = (warp - C::kEpiWarp) >> 2;
     const uint32_t acce0 = mapa(smem_u32(&bar_acce[0]), 0);
     constexpr int kChunks = C::GATED ? C::NT / 64 : C::NT / 32;
     constexpr int kOvChunks = C::OV / 32;
@@ -437,7 +464,7 @@ __global__ void __launch_bounds__(C::kThreads, 1) mm_pair(const __grid_constant_
         released = true;
       };
 #pragma unroll 1
-      for (int i = half; i < kChunks; i += 2) {
+      for (int i = e0; i < kChunks; i += C::EPQ) {
         // the columns that the accumulators share are the first one's last, the second one's first
         const int c = C::OV > 0 && buf == 0 ? kChunks - 1 - i : i;
         uint32_t r0[32], r1[C::GATED ? 32 : 1];
@@ -446,7 +473,7 @@ __global__ void __launch_bounds__(C::kThreads, 1) mm_pair(const __grid_constant_
         tc_wait_ld();
         tc_regs_ready(r0);
         tc_regs_ready(r1);
-        if (C::OV > 0 && !released && i + 2 >= kOvChunks) release();
+        if (C::OV > 0 && !released && i + C::EPQ >= kOvChunks) release();
         const int n = n0 + 32 * c, cnt = min(32, P.N - n);
         if (m >= P.M || (cnt <= 0 && !P.qfmt)) continue;
         float v[32];
@@ -697,18 +724,18 @@ __global__ void __launch_bounds__(C::kThreads, 1) mm_few(const __grid_constant__
 #pragma unroll
         for (int d = 1; d < 16; d *= 2) mx = max(mx, __shfl_xor_sync(0xffffffffu, mx, d));
         if (!nv) mx = max(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
-        float z[8] = {};
-        uint32_t byte;
+        const float z[8] = {t};
+        uint32_t byte, w;
         if (nv) {
           const fp4::Scale<true> sc(mx);
           byte = sc.byte;
-          z[0] = sc.div(t);
+          w = sc.codes(z);
         } else {
           const fp4::Scale<false> sc(mx);
           byte = sc.byte;
-          z[0] = sc.div(t);
+          w = sc.codes(z);
         }
-        uint32_t w = (fp4::codes8(z) & 15u) << (4 * (lane & 7));  // 8 lanes make a word
+        w = (w & 15u) << (4 * (lane & 7));  // 8 lanes make a word
 #pragma unroll
         for (int d = 1; d < 8; d *= 2) w |= __shfl_xor_sync(0xffffffffu, w, d);
         if ((lane & 7) == 0 && n < P.N) *reinterpret_cast<uint32_t*>(P.codes + m * P.code_stride + n / 2) = w;

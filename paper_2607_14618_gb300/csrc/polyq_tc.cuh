@@ -105,6 +105,37 @@ __device__ __forceinline__ int wait(uint32_t bar, uint32_t parity, const volatil
   }
   return kTimeout;
 }
+__device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n .reg .pred p;\n mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n"
+      " selp.u32 %0, 1, 0, p;\n}\n"
+      : "=r"(ok)
+      : "r"(bar), "r"(parity)
+      : "memory");
+  return ok != 0;
+}
+// How many phases in a row, of the B slots from `s` on in a ring of N (parity
+// `ph` up to the ring's end, the other after it), have completed.  A poll's
+// answer takes 250 to 300 cycles beside the tensor core's shared-memory
+// traffic, but polls follow each other every few: a lone thread that asks for
+// several slots at once pays that once for all that are ready.
+template <int B, int N>
+__device__ __forceinline__ int poll_ahead(uint32_t bar0, int s, uint32_t ph) {
+  static_assert(B <= N, "one phase per slot");
+  uint32_t ok = 0;
+#pragma unroll
+  for (int i = 0; i < B; ++i) {
+    int k = s + i;
+    uint32_t p = ph;
+    if (k >= N) {
+      k -= N;
+      p ^= 1u;
+    }
+    ok |= (mbar_test(bar0 + 8 * k, p) ? 1u : 0u) << i;
+  }
+  return __ffs(~ok) - 1;
+}
 __device__ __forceinline__ void wait_stay(uint32_t bar, uint32_t parity) {
   for (uint32_t it = 0; it < kSleepLimit && !mbar_try_wait_hint(bar, parity); ++it) {
   }
@@ -201,6 +232,17 @@ __device__ __forceinline__ void commit(uint32_t bar) {
         " [%0], %1;" ::"r"(bar),
         "h"((uint16_t)3)
         : "memory");
+  else
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar)
+                 : "memory");
+}
+
+// The same on this CTA's barrier only.
+template <int CG>
+__device__ __forceinline__ void commit_here(uint32_t bar) {
+  if (CG == 2)
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar)
+                 : "memory");
   else
     asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar)
                  : "memory");

@@ -736,32 +736,51 @@ def workspace_status(workspace, stream=None):
 
 
 # ---- 4-bit floating point and the gated feed-forward block (include/polyq_fp4.h) ----
-def _types():
+# The argument checks below are on the way of every small call: a token's
+# quantisation took 6.7 us of host time with torch's device objects, shape tuples
+# and imports in them and 4.0 with plain numbers (2.4 of it the C call).
+_T = {}  # torch dtype -> T_*, filled by the first use
+
+
+def _type_of(dtype):
+    if not _T:
+        import torch
+        _T.update({torch.float32: T_F32, torch.bfloat16: T_BF16, torch.float16: T_F16})
+    return _T.get(dtype)
+
+
+def _current(index, name):
+    """Raises unless CUDA device `index` is the current one (the stream and the
+    library's per-device state are looked up for that)."""
     import torch
-    return {torch.float32: T_F32, torch.bfloat16: T_BF16, torch.float16: T_F16}
+    cur = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)()  # private: may lack
+    if index != cur:
+        raise ValueError(f"{name} is on cuda:{index}, not on the current device cuda:{cur}")
 
 
-def _dense(t, name, shape=None, device=None, dtype=None):
+def _dense(t, name, rows=None, cols=None, dev=None, dtype=None):
     """Descriptor of a 2-D CUDA tensor whose rows are contiguous (any row
-    stride), checked against what is given; it must be on the current device
-    (the stream and the library's per-device state are looked up for that)."""
-    import torch
-    ty = _types().get(getattr(t, "dtype", None))
-    if (not isinstance(t, torch.Tensor) or ty is None or t.dim() != 2 or not t.is_cuda
-            or (shape is not None and tuple(t.shape) != tuple(shape))
-            or (dtype is not None and t.dtype != dtype) or (device is not None and t.device != device)
-            or (t.shape[1] > 1 and t.stride(1) != 1)):
-        want = "" if shape is None else f" {list(shape)}"
-        kind = "fp32, bf16 or fp16" if dtype is None else str(dtype)
-        raise ValueError(f"{name} must be a CUDA {kind} tensor{want} with contiguous rows"
-                         + ("" if device is None else f" on {device}"))
-    if t.device.index != torch.cuda.current_device():
-        raise ValueError(f"{name} is on {t.device}, not on the current device "
-                         f"cuda:{torch.cuda.current_device()}")
-    stride = t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
-    if stride < t.shape[1]:
-        raise ValueError(f"{name}: rows overlap (stride {t.stride(0)})")
-    return Dense(t.data_ptr(), stride, ty)
+    stride), checked against the sizes, device index and type that are given."""
+    try:
+        ty = _T.get(t.dtype)
+        if ty is None:
+            ty = _type_of(t.dtype)
+        n, k = t.shape
+        s0, s1 = t.stride()
+        at = t.get_device()
+    except (AttributeError, ValueError):
+        ty = None
+    if (ty is None or at < 0 or (rows is not None and n != rows) or (cols is not None and k != cols)
+            or (dev is not None and at != dev) or (dtype is not None and t.dtype != dtype)
+            or (k > 1 and s1 != 1)):
+        raise ValueError(f"{name} must be a CUDA {'fp32, bf16 or fp16' if dtype is None else dtype} "
+                         f"tensor [{'rows' if rows is None else rows}][{'K' if cols is None else cols}]"
+                         f" with contiguous rows{'' if dev is None else f' on cuda:{dev}'}")
+    if n <= 1 and s0 < k:
+        s0 = k
+    if s0 < k:
+        raise ValueError(f"{name}: rows overlap (stride {s0})")
+    return Dense(t.data_ptr(), s0, ty)
 
 
 class Fp4Tensor:
@@ -780,6 +799,7 @@ class Fp4Tensor:
         self.tensor_scale = float(tensor_scale)
         self.desc = Fp4Desc(codes.data_ptr(), scales.data_ptr(), self.rows, self.K, stride.value,
                             self.format, self.tensor_scale)
+        self.device_index = codes.get_device()
 
     @classmethod
     def empty(cls, rows, K, format=FP4_MX, tensor_scale=1.0, device="cuda"):
@@ -825,13 +845,10 @@ class Fp4Tensor:
         return codes, self.scales[self._places(self.rows, blocks, c.device)]
 
 
-def _fp4(t, name, device=None):
-    import torch
-    if not isinstance(t, Fp4Tensor) or not t.codes.is_cuda or (device is not None and t.codes.device != device):
-        raise ValueError(f"{name} must be an Fp4Tensor" + (" on a CUDA device" if device is None else f" on {device}"))
-    if t.codes.device.index != torch.cuda.current_device():
-        raise ValueError(f"{name} is on {t.codes.device}, not on the current device "
-                         f"cuda:{torch.cuda.current_device()}")
+def _fp4(t, name, dev=None):
+    """The descriptor of a 4-bit tensor on CUDA device `dev` (default: any)."""
+    if not isinstance(t, Fp4Tensor) or t.device_index < 0 or (dev is not None and t.device_index != dev):
+        raise ValueError(f"{name} must be an Fp4Tensor on {'a CUDA device' if dev is None else f'cuda:{dev}'}")
     return C.byref(t.desc)
 
 
@@ -854,14 +871,27 @@ def fp4_workspace(device="cuda"):
     return torch.zeros(FP4_WORKSPACE_BYTES, dtype=torch.uint8, device=device)
 
 
+def _workspace_at(workspace, dev, make):
+    """The caller's workspace, checked, or a new one (the library checks its size)."""
+    if workspace is None:
+        return make()
+    import torch
+    if (workspace.dtype != torch.uint8 or workspace.get_device() != dev
+            or not workspace.is_contiguous()):
+        raise ValueError(f"workspace must be a contiguous uint8 tensor on cuda:{dev}")
+    return workspace
+
+
 def fp4_quantize(x, format=FP4_MX, tensor_scale=1.0, out=None, stream=None):
     """x [rows][K] (fp32, bf16 or fp16; any row stride) in 4 bits.  With `out`
     its format and tensor scale are used."""
     d = _dense(x, "x")
+    dev = x.get_device()
+    _current(dev, "x")
     if out is None:
         out = Fp4Tensor.empty(x.shape[0], x.shape[1], format, tensor_scale, x.device)
-    o = _fp4(out, "out", x.device)
-    if (out.rows, out.K) != tuple(x.shape):
+    o = _fp4(out, "out", dev)
+    if (out.rows, out.K) != x.shape:
         raise ValueError(f"out is [{out.rows}][{out.K}], x {list(x.shape)}")
     _check(_lib.polyq_fp4_quantize(C.byref(d), o, _stream_ptr(stream)))
     return out
@@ -869,17 +899,15 @@ def fp4_quantize(x, format=FP4_MX, tensor_scale=1.0, out=None, stream=None):
 
 def fp4_dequantize(t: Fp4Tensor, dtype=None, out=None, stream=None):
     """The values of a 4-bit tensor (default fp32)."""
-    import torch
     p = _fp4(t, "t")
+    dev = t.device_index
+    _current(dev, "t")
     if out is None:
+        import torch
         out = torch.empty((t.rows, t.K), dtype=dtype or torch.float32, device=t.codes.device)
-    d = _dense(out, "out", (t.rows, t.K), t.codes.device, dtype)
+    d = _dense(out, "out", t.rows, t.K, dev, dtype)
     _check(_lib.polyq_fp4_dequantize(p, C.byref(d), _stream_ptr(stream)))
     return out
-
-
-def _fp4_workspace(workspace, dev):
-    return _workspace_of(workspace, lambda: FP4_WORKSPACE_BYTES, True, dev)
 
 
 def fp4_linear(x: Fp4Tensor, w: Fp4Tensor, y=None, residual=None, dtype=None, workspace=None,
@@ -887,17 +915,18 @@ def fp4_linear(x: Fp4Tensor, w: Fp4Tensor, y=None, residual=None, dtype=None, wo
     """y[m][n] = residual[m][n] + sum_k x[m][k] w[n][k], both operands in one
     4-bit format.  y: fp32 (default), bf16 or fp16; residual of y's type, may be
     y itself."""
-    import torch
-    dev = x.codes.device if isinstance(x, Fp4Tensor) else None
-    px, pw = _fp4(x, "x"), _fp4(w, "w", dev)
+    px = _fp4(x, "x")
+    dev = x.device_index
+    pw = _fp4(w, "w", dev)
+    _current(dev, "x")
     if y is None:
+        import torch
         y = torch.empty((x.rows, w.rows), dtype=dtype or (residual.dtype if residual is not None
-                                                          else torch.float32), device=dev)
-    dy = _dense(y, "y", (x.rows, w.rows), dev, dtype)
-    dr = None if residual is None else _dense(residual, "residual", (x.rows, w.rows), dev, y.dtype)
-    workspace = _fp4_workspace(workspace, dev)
-    _check(_lib.polyq_fp4_linear(px, pw, C.byref(dr) if dr is not None else None, C.byref(dy),
-                                 workspace.data_ptr(), workspace.numel(), _stream_ptr(stream)))
+                                                          else torch.float32), device=x.codes.device)
+    dy = _dense(y, "y", x.rows, w.rows, dev, dtype)
+    dr = None if residual is None else C.byref(_dense(residual, "residual", x.rows, w.rows, dev, y.dtype))
+    ws = _workspace_at(workspace, dev, lambda: fp4_workspace(x.codes.device))
+    _check(_lib.polyq_fp4_linear(px, pw, dr, C.byref(dy), ws.data_ptr(), ws.numel(), _stream_ptr(stream)))
     return y
 
 
@@ -905,20 +934,20 @@ def fp4_ffn(x: Fp4Tensor, gate: Fp4Tensor, up: Fp4Tensor, h=None, dtype=None, wo
             stream=None):
     """h = silu(x gate^T) * (x up^T) in one kernel.  h: a tensor (default bf16)
     or an Fp4Tensor, which receives h quantised as fp4_quantize does."""
-    import torch
-    dev = x.codes.device if isinstance(x, Fp4Tensor) else None
-    px, pg, pu = _fp4(x, "x"), _fp4(gate, "gate", dev), _fp4(up, "up", dev)
+    px = _fp4(x, "x")
+    dev = x.device_index
+    pg, pu = _fp4(gate, "gate", dev), _fp4(up, "up", dev)
+    _current(dev, "x")
     if h is None:
-        h = torch.empty((x.rows, gate.rows), dtype=dtype or torch.bfloat16, device=dev)
-    workspace = _fp4_workspace(workspace, dev)
+        import torch
+        h = torch.empty((x.rows, gate.rows), dtype=dtype or torch.bfloat16, device=x.codes.device)
     dh = dq = None
     if isinstance(h, Fp4Tensor):
         dq = _fp4(h, "h", dev)
     else:
-        d = _dense(h, "h", (x.rows, gate.rows), dev, dtype)
-        dh = C.byref(d)
-    _check(_lib.polyq_fp4_ffn(px, pg, pu, dh, dq, workspace.data_ptr(), workspace.numel(),
-                              _stream_ptr(stream)))
+        dh = C.byref(_dense(h, "h", x.rows, gate.rows, dev, dtype))
+    ws = _workspace_at(workspace, dev, lambda: fp4_workspace(x.codes.device))
+    _check(_lib.polyq_fp4_ffn(px, pg, pu, dh, dq, ws.data_ptr(), ws.numel(), _stream_ptr(stream)))
     return h
 
 
@@ -940,28 +969,33 @@ def ffn_workspace(T, F, K=None, device="cuda"):
 
 def _ffn_inputs(x, gate, up):
     dx = _dense(x, "x")
+    dev = x.get_device()
+    _current(dev, "x")
     T, K = x.shape
-    dg = _dense(gate, "gate", None, x.device, x.dtype)
+    dg = _dense(gate, "gate", None, K, dev, x.dtype)
     F = gate.shape[0]
-    if gate.shape[1] != K:
-        raise ValueError(f"gate is {list(gate.shape)}, x {list(x.shape)}")
-    return dx, dg, _dense(up, "up", (F, K), x.device, x.dtype), T, F, K
+    return dx, dg, _dense(up, "up", F, K, dev, x.dtype), T, F, K, dev
+
+
+def _saved(saved, x, T, F, dev):
+    if (saved.dtype != x.dtype or saved.get_device() != dev or not saved.is_contiguous()
+            or saved.shape != (2, T, _lib.polyq_ffn_saved_stride(F))):
+        raise ValueError(f"saved must be ffn_saved({T}, {F}, {x.dtype}) on cuda:{dev}")
+    return saved.data_ptr()
 
 
 def ffn_forward(x, gate, up, h=None, saved=None, workspace=None, stream=None):
     """h = silu(x gate^T) * (x up^T) on bf16 or fp16 operands, one kernel.
     `saved` (ffn_saved) receives what ffn_backward needs."""
-    import torch
-    dx, dg, du, T, F, K = _ffn_inputs(x, gate, up)
+    ix, ig, iu, T, F, K, dev = _ffn_inputs(x, gate, up)
     if h is None:
+        import torch
         h = torch.empty((T, F), dtype=x.dtype, device=x.device)
-    dh = _dense(h, "h", (T, F), x.device, x.dtype)
-    if saved is not None:
-        _require(saved, "saved", x.dtype, (2, T, _lib.polyq_ffn_saved_stride(F)), x.device)
-    workspace = _fp4_workspace(workspace, x.device)
-    _check(_lib.polyq_ffn_forward(C.byref(dx), C.byref(dg), C.byref(du), T, F, K, C.byref(dh),
-                                  saved.data_ptr() if saved is not None else None,
-                                  workspace.data_ptr(), workspace.numel(), _stream_ptr(stream)))
+    ih = _dense(h, "h", T, F, dev, x.dtype)
+    ps = None if saved is None else _saved(saved, x, T, F, dev)
+    ws = _workspace_at(workspace, dev, lambda: fp4_workspace(x.device))
+    _check(_lib.polyq_ffn_forward(C.byref(ix), C.byref(ig), C.byref(iu), T, F, K, C.byref(ih), ps,
+                                  ws.data_ptr(), ws.numel(), _stream_ptr(stream)))
     return h
 
 
@@ -970,24 +1004,24 @@ def ffn_backward(x, gate, up, saved, dh, dx=None, dgate=None, dup=None, need_dx=
     """Gradients (dx, dgate, dup) of ffn_forward for the gradient dh of h; each
     of x's type or, where a buffer of that type is passed, fp32.  Those not
     needed are None."""
-    import torch
-    ix, ig, iu, T, F, K = _ffn_inputs(x, gate, up)
-    dev, ty = x.device, x.dtype
-    idh = _dense(dh, "dh", (T, F), dev, ty)
-    _require(saved, "saved", ty, (2, T, _lib.polyq_ffn_saved_stride(F)), dev)
+    ix, ig, iu, T, F, K, dev = _ffn_inputs(x, gate, up)
+    ty = x.dtype
+    idh = _dense(dh, "dh", T, F, dev, ty)
+    ps = _saved(saved, x, T, F, dev)
+
+    def new(n, like):
+        import torch
+        return torch.empty((n, K), dtype=ty if like is None else like.dtype, device=x.device)
+
     if dx is None and need_dx:
-        dx = torch.empty((T, K), dtype=ty, device=dev)
+        dx = new(T, None)
     if dgate is None and need_weights:
-        dgate = torch.empty((F, K), dtype=ty if dup is None else dup.dtype, device=dev)
+        dgate = new(F, dup)
     if dup is None and need_weights:
-        dup = torch.empty((F, K), dtype=dgate.dtype, device=dev)
-    outs = [None if t is None else _dense(t, n, s, dev) for t, n, s in
-            ((dx, "dx", (T, K)), (dgate, "dgate", (F, K)), (dup, "dup", (F, K)))]
-    if workspace is None:
-        workspace = ffn_workspace(T, F, K, dev)
-    _require(workspace, "workspace", torch.uint8, (workspace.numel(),), dev)
-    _check(_lib.polyq_ffn_backward(C.byref(ix), C.byref(ig), C.byref(iu), T, F, K,
-                                   saved.data_ptr(), C.byref(idh),
-                                   *[C.byref(o) if o is not None else None for o in outs],
-                                   workspace.data_ptr(), workspace.numel(), _stream_ptr(stream)))
+        dup = new(F, dgate)
+    outs = [None if t is None else C.byref(_dense(t, n, r, K, dev)) for t, n, r in
+            ((dx, "dx", T), (dgate, "dgate", F), (dup, "dup", F))]
+    ws = _workspace_at(workspace, dev, lambda: ffn_workspace(T, F, K, x.device))
+    _check(_lib.polyq_ffn_backward(C.byref(ix), C.byref(ig), C.byref(iu), T, F, K, ps, C.byref(idh),
+                                   *outs, ws.data_ptr(), ws.numel(), _stream_ptr(stream)))
     return dx, dgate, dup
