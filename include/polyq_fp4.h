@@ -85,11 +85,14 @@ int polyq_fp4_quantize(const polyq_dense* x, const polyq_fp4* out, void* stream)
 /* y[r][k] = the tensor's value, rounded once to y's type.  One launch. */
 int polyq_fp4_dequantize(const polyq_fp4* t, const polyq_dense* y, void* stream);
 
-/* Bytes of the workspace of the products below: a status word in its first 4
- * bytes (read it with polyq_workspace_status).  Zero it before its first use.
- * A workspace may serve calls that run at the same time; a wait that gave up
- * in one of them then shows for all. */
-#define POLYQ_FP4_WORKSPACE_BYTES 256
+/* Bytes of the workspace of the products below on the current device (it
+ * grows with its SM count): a status word in its first 4 bytes (read it with
+ * polyq_workspace_status), counters, and the parts of output tiles that several
+ * SMs share.  Its first POLYQ_FP4_WORKSPACE_ZERO bytes must be zero before its
+ * first use, and again after a wait that gave up.  A workspace may serve
+ * consecutive calls on one stream but not calls that run at the same time. */
+#define POLYQ_FP4_WORKSPACE_ZERO 16640
+int polyq_fp4_workspace_bytes(size_t* bytes);
 
 /* y[m][n] = residual[m][n] + sum_k x[m][k] w[n][k]: x [M][K] and w [N][K] in
  * one 4-bit format, y [M][N] of any type; residual NULL or [M][N] of y's type
@@ -121,9 +124,8 @@ int polyq_ffn_forward(const polyq_dense* x, const polyq_dense* gate, const polyq
                       int64_t T, int64_t F, int64_t K, const polyq_dense* h, void* saved,
                       void* workspace, size_t workspace_bytes, void* stream);
 
-/* Workspace of the backward pass: its first POLYQ_FP4_WORKSPACE_BYTES are the
- * status word's, the rest holds the gradients of a and u.  Calls that may run
- * at the same time need workspaces of their own. */
+/* Workspace of the backward pass on the current device: that of the products,
+ * which it begins with, and the gradients of a and u. */
 int polyq_ffn_backward_workspace_bytes(int64_t T, int64_t F, size_t* bytes);
 
 /* Gradients of the block for the gradient dh [T][F] of h (x's type) and the

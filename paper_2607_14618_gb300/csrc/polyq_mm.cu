@@ -6,8 +6,8 @@
 //
 // Every kind moves 128 bytes of each operand row per stage, four MMAs: 256
 // 4-bit or 64 16-bit elements of K.  Two kernels:
-//   mm_pair  many rows: persistent CTA pairs (cta_group::2), 256 rows of A by NT
-//            rows of B a tile, A the tokens, B the weights.
+//   mm_pair  many rows: persistent CTA pairs (cta_group::2), 256 rows of A by 256
+//            of B a tile, A the tokens, B the weights.
 //   mm_few   few tokens: the weights are A (128 rows a CTA), the tokens B; the
 //            CTAs of a cluster share the contraction and add their parts through
 //            distributed shared memory, in rank order.
@@ -36,8 +36,8 @@ using namespace polyq;
 using namespace polyq::tc;
 
 constexpr int k16 = 0, kMx = 1, kNv = 2;  // operand kinds
-constexpr int kTileM = 256;               // rows of A of a pair's tile
-constexpr int kHalf = 128;                // of which each CTA holds half
+constexpr int kTileM = 256, kTileN = 256;  // rows of A and of B of a pair's tile
+constexpr int kHalf = 128;                // of each of which a CTA holds half
 constexpr int kRowBytes = 128;            // an operand row in a stage
 constexpr int kOpBytes = kHalf * kRowBytes;
 constexpr int kSmemMax = 227 * 1024 - 1024;  // less the static barriers
@@ -51,6 +51,13 @@ struct MmParams {
   int segs;                // segments of the contraction: a[s] with b[s]
   int probs;               // problems: a[p] with b[0]
   int tiles_m, tiles_n, tiles;
+  // mm_pair: the first sk_tiles tiles are shared along the contraction by the
+  // pairs b < sk_pairs: sk_parts pairs a tile (even parts), or with sk_parts 0
+  // all of their stages in tile order, sk_share a pair (the first sk_extra pairs
+  // one more).  The other tiles are whole, strided over the pairs.
+  int sk_tiles, sk_pairs, sk_parts, sk_share, sk_extra;
+  float* parts;            // [2 pairs][64][256 rows][4 columns]: parts of shared tiles
+  int* counters;           // [sk_tiles][2 CTAs][warps]: parts in place
   int a_mn, b_mn;          // operand has M (N) contiguous instead of K
   int atoms;               // scale atoms of a row group
   uint32_t idesc;
@@ -59,7 +66,7 @@ struct MmParams {
   void* y[2];
   const void* res;
   int64_t y_stride, res_stride;
-  int type, vec;           // vec: rows of y and res start on 16 bytes
+  int type, vec, vec_saved;  // vec: rows of y and res start on 16 bytes (1), y's on 32 (2)
   uint8_t *codes, *scales;
   int64_t code_stride, out_atoms;
   int qfmt;                // 0, kMx or kNv
@@ -79,6 +86,12 @@ __device__ __forceinline__ uint32_t pack16(float lo, float hi, bool bf16) {
   const __half2 v = __floats2half2_rn(lo, hi);
   return *reinterpret_cast<const uint32_t*>(&v);
 }
+__device__ __forceinline__ float to_f32(float v) { return v; }
+__device__ __forceinline__ float to_f32(__nv_bfloat16 v) { return __bfloat162float(v); }
+__device__ __forceinline__ float to_f32(__half v) { return __half2float(v); }
+__device__ __forceinline__ void from_f32(float v, float* p) { *p = v; }
+__device__ __forceinline__ void from_f32(float v, __nv_bfloat16* p) { *p = __float2bfloat16_rn(v); }
+__device__ __forceinline__ void from_f32(float v, __half* p) { *p = __float2half_rn(v); }
 __device__ __forceinline__ float load_dense(const void* p, int64_t i, int type) {
   return type == POLYQ_F32    ? ((const float*)p)[i]
          : type == POLYQ_BF16 ? __bfloat162float(((const __nv_bfloat16*)p)[i])
@@ -94,61 +107,121 @@ __device__ __forceinline__ float saved_range(float v, bool bf16) {
   return bf16 || fabsf(v) == INFINITY ? v : v > 65504.f ? 65504.f : v < -65504.f ? -65504.f : v;
 }
 
-// 32 consecutive values of a row, the first n of them inside.
-__device__ __forceinline__ void store_row32(void* y, int64_t off, const float (&v)[32], int n, int type,
-                                            bool vec) {
-  if (vec && n == 32) {
-    if (type == POLYQ_F32) {
-      float4* d = reinterpret_cast<float4*>((float*)y + off);
+// Rows that start on 32 (vec = 2) or 16 bytes (1): a lane holds 32 consecutive
+// values of its row and stores, or adds from the residual, whole sectors.
+__device__ __forceinline__ void store32(void* p, const uint32_t (&w)[8]) {
+  asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]),
+               "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
+               : "memory");
+}
+__device__ __forceinline__ void store_row32(void* y, int64_t off, const float (&v)[32], int type, int vec) {
+  if (type == POLYQ_F32) {
+    float* d = (float*)y + off;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) d[i] = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
-    } else {
-      uint4* d = reinterpret_cast<uint4*>((uint16_t*)y + off);
-      const bool b = type == POLYQ_BF16;
+    for (int i = 0; i < 32; i += 8) {
+      uint32_t w[8];
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        d[i] = make_uint4(pack16(v[8 * i], v[8 * i + 1], b), pack16(v[8 * i + 2], v[8 * i + 3], b),
-                          pack16(v[8 * i + 4], v[8 * i + 5], b), pack16(v[8 * i + 6], v[8 * i + 7], b));
+      for (int j = 0; j < 8; ++j) w[j] = __float_as_uint(v[i + j]);
+      if (vec == 2) {
+        store32(d + i, w);
+      } else {
+        reinterpret_cast<uint4*>(d + i)[0] = make_uint4(w[0], w[1], w[2], w[3]);
+        reinterpret_cast<uint4*>(d + i)[1] = make_uint4(w[4], w[5], w[6], w[7]);
+      }
     }
   } else {
+    uint16_t* d = (uint16_t*)y + off;
 #pragma unroll
-    for (int i = 0; i < 32; ++i)
-      if (i < n) store_dense(y, off + i, v[i], type);
+    for (int i = 0; i < 32; i += 16) {
+      uint32_t w[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) w[j] = pack16(v[i + 2 * j], v[i + 2 * j + 1], type == POLYQ_BF16);
+      if (vec == 2) {
+        store32(d + i, w);
+      } else {
+        reinterpret_cast<uint4*>(d + i)[0] = make_uint4(w[0], w[1], w[2], w[3]);
+        reinterpret_cast<uint4*>(d + i)[1] = make_uint4(w[4], w[5], w[6], w[7]);
+      }
+    }
   }
 }
-__device__ __forceinline__ void add_row32(const void* r, int64_t off, float (&v)[32], int n, int type,
-                                          bool vec) {
-  if (vec && n == 32) {
-    if (type == POLYQ_F32) {
-      const float4* s = reinterpret_cast<const float4*>((const float*)r + off);
+__device__ __forceinline__ void add_row32(const void* r, int64_t off, float (&v)[32], int type) {
+  if (type == POLYQ_F32) {
+    const float4* s = reinterpret_cast<const float4*>((const float*)r + off);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const float4 f = s[i];
-        v[4 * i] += f.x;
-        v[4 * i + 1] += f.y;
-        v[4 * i + 2] += f.z;
-        v[4 * i + 3] += f.w;
-      }
-    } else {
-      const uint4* s = reinterpret_cast<const uint4*>((const uint16_t*)r + off);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const uint4 u = s[i];
-        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          float2 f;
-          if (type == POLYQ_BF16) f = make_float2(bf16_lo(w[j]), bf16_hi(w[j]));
-          else f = __half22float2(*reinterpret_cast<const __half2*>(&w[j]));
-          v[8 * i + 2 * j] += f.x;
-          v[8 * i + 2 * j + 1] += f.y;
-        }
-      }
+    for (int i = 0; i < 8; ++i) {
+      const float4 f = s[i];
+      v[4 * i] += f.x;
+      v[4 * i + 1] += f.y;
+      v[4 * i + 2] += f.z;
+      v[4 * i + 3] += f.w;
     }
   } else {
+    const uint4* s = reinterpret_cast<const uint4*>((const uint16_t*)r + off);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint4 u = s[i];
+      const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        float2 f;
+        if (type == POLYQ_BF16) f = make_float2(bf16_lo(w[j]), bf16_hi(w[j]));
+        else f = __half22float2(*reinterpret_cast<const __half2*>(&w[j]));
+        v[8 * i + 2 * j] += f.x;
+        v[8 * i + 2 * j + 1] += f.y;
+      }
+    }
+  }
+}
+// The warp's 32 x 32 values transposed: v[r] of lane c becomes v[c] of lane r.
+__device__ __forceinline__ void transpose32(float (&v)[32]) {
+  const int lane = threadIdx.x & 31;
+#pragma unroll
+  for (int d = 16; d >= 1; d /= 2)
 #pragma unroll
     for (int i = 0; i < 32; ++i)
-      if (i < n) v[i] += load_dense(r, off + i, type);
+      if (!(i & d)) {
+        const bool hi = lane & d;
+        const float got = __shfl_xor_sync(0xffffffffu, hi ? v[i] : v[i | d], d);
+        if (hi) v[i] = got;
+        else v[i | d] = got;
+      }
+}
+// The first `rows` values of a lane's column, of a matrix whose lanes' columns
+// are neighbours.
+template <typename T>
+__device__ __forceinline__ void store_column(T* y, int64_t stride, const T* res, int64_t res_stride, int rows,
+                                             const float (&v)[32]) {
+#pragma unroll
+  for (int r = 0; r < 32; ++r)
+    if (r < rows) {
+      const float f = res ? v[r] + to_f32(res[r * res_stride]) : v[r];
+      from_f32(f, y + r * stride);
+    }
+}
+// 32 values of each of the warp's 32 rows m.. from column n, of a matrix of M
+// by N.  Whole chunks of aligned rows go lane by lane; others (rows of odd
+// strides, the last columns) are transposed first, so that the lanes' elements
+// are neighbours: 301 x 2731 fp16 took 31 us with a lane's 32 elements of two
+// bytes stored one by one, 15 us so.
+__device__ __forceinline__ void store_chunk(void* y, int64_t stride, const void* res, int64_t res_stride, int64_t m,
+                                            int n, int64_t M, int64_t N, float (&v)[32], int type, int vec) {
+  const int lane = threadIdx.x & 31;
+  if (vec && n + 32 <= N) {
+    if (m + lane < M) {
+      if (res) add_row32(res, (m + lane) * res_stride + n, v, type);
+      store_row32(y, (m + lane) * stride + n, v, type, vec);
+    }
+  } else {
+    transpose32(v);
+    const int rows = n + lane < N ? (int)min((int64_t)32, M - m) : 0;
+    const int64_t at = m * stride + n + lane, from = m * res_stride + n + lane;
+    if (type == POLYQ_F32)
+      store_column((float*)y + at, stride, res ? (const float*)res + from : nullptr, res_stride, rows, v);
+    else if (type == POLYQ_BF16)
+      store_column((__nv_bfloat16*)y + at, stride, res ? (const __nv_bfloat16*)res + from : nullptr, res_stride, rows, v);
+    else
+      store_column((__half*)y + at, stride, res ? (const __half*)res + from : nullptr, res_stride, rows, v);
   }
 }
 
@@ -184,50 +257,101 @@ __device__ __forceinline__ void store_codes32(const MmParams& P, int64_t m, int6
 // ---------------------------------------------------------------------------
 // many rows: CTA pairs
 // ---------------------------------------------------------------------------
-template <int KIND_, int NT_, bool GATED_>
+template <int KIND_, bool GATED_>
 struct Pair {
-  static constexpr int KIND = KIND_, NT = NT_;
+  static constexpr int KIND = KIND_;
   static constexpr bool GATED = GATED_;
+  static constexpr int MATS = GATED ? 2 : 1;
   static constexpr int ATOMS = KIND == k16 ? 0 : KIND == kNv ? 4 : 2;  // scale atoms of a stage
-  static constexpr int GROUPS = NT / 128;                              // row groups of B's scales
-  static constexpr int kB = NT / 2 * kRowBytes;
-  static constexpr int kSa = ATOMS * 512, kSb = ATOMS * 512 * GROUPS;
-  static constexpr int kStage = kOpBytes + kB + kSa + kSb;
+  static constexpr int kSa = ATOMS * 512, kSb = ATOMS * 1024;          // of A's 128 rows, of B's 256
+  static constexpr int kStage = 2 * kOpBytes + kSa + kSb;
   static constexpr int STAGES = (kSmemMax - 1024) / kStage;
-  static constexpr int kBOff = STAGES * kOpBytes, kSaOff = kBOff + STAGES * kB;
+  static constexpr int kBOff = STAGES * kOpBytes, kSaOff = kBOff + STAGES * kOpBytes;
   static constexpr int kSbOff = kSaOff + STAGES * kSa;
   static constexpr size_t kSmem = (size_t)STAGES * kStage + 1024;
-  // Tensor memory: two accumulators of NT columns and a ring of SF stages'
-  // scales.  With NT = 256 and scales the accumulators share OV columns: the
-  // epilogue drains those first and releases them for the next tile before the
-  // rest.
+  // Tensor memory: two accumulators of 256 columns and SF stages' scales.  With
+  // scales the accumulators share OV columns: the epilogue drains those first
+  // and releases them for the next tile before the rest.
   static constexpr int SF = 2;
-  static constexpr int kSfStage = ATOMS * 4 * (1 + GROUPS);
+  static constexpr int kSfStage = ATOMS * 4 * 3;
   static constexpr int kSfCols = (SF * kSfStage + 31) / 32 * 32;
-  static constexpr int kSfCol = NT == 256 ? 512 - kSfCols : 2 * NT;
-  static constexpr int kAcc1 = NT == 256 ? kSfCol - 256 : NT;
-  static constexpr int OV = NT - kAcc1;
+  static constexpr int kSfCol = 512 - kSfCols;
+  static constexpr int kAcc1 = kSfCol - kTileN;
+  static constexpr int OV = kTileN - kAcc1;
   static constexpr int kEpiWarp = 4, EPI = 12, EPQ = EPI / 4;  // EPQ warps to a quarter of the lanes
   static constexpr int kThreads = 32 * (kEpiWarp + EPI);
-  static_assert(kSfCol + kSfCols <= 512 && OV % 32 == 0 && STAGES >= 4, "");
+  static_assert(OV % 32 == 0 && STAGES >= 4, "");
 };
+constexpr int kEpiWarps = 12;
 
-// The tiles of a pair, in order.  Tiles of eight row tiles are taken together,
-// rows fastest, so that the pairs at work share both operands through L2.
+// The pieces of work of a pair, in order: a tile and the stages [lo, hi) of its
+// contraction; the pair's share of the shared tiles comes first.  Tiles of eight
+// row tiles are taken together, rows fastest, so that the pairs at work share
+// both operands through L2.
 struct Tiles {
-  int t;
-  __device__ __forceinline__ void init() { t = (int)(blockIdx.x >> 1); }
-  __device__ __forceinline__ bool next(const MmParams& P, int& prob, int& tm, int& tn) {
-    if (t >= P.tiles) return false;
+  int g, g_hi, t;         // shared stages; next whole tile
+  int prob, tm, tn, lo, hi;
+  int shared, parts, own; // of a part: its tile, the tile's parts, which one it is; else shared is -1
+  // The first shared stage of pair b, and the pair that has shared stage x.
+  static __device__ __forceinline__ int share_of(const MmParams& P, int b) {
+    if (P.sk_parts == 0) return b * P.sk_share + min(b, P.sk_extra);
+    const int n_it = P.segs * P.kt, tile = b / P.sk_parts;
+    return tile * n_it + (int)((int64_t)(b - tile * P.sk_parts) * n_it / P.sk_parts);
+  }
+  static __device__ __forceinline__ int pair_of(const MmParams& P, int x) {
+    if (P.sk_parts == 0) {
+      const int y = x - P.sk_extra * (P.sk_share + 1);
+      return y < 0 ? x / (P.sk_share + 1) : P.sk_extra + y / P.sk_share;
+    }
+    const int n_it = P.segs * P.kt, tile = x / n_it;
+    return tile * P.sk_parts + (int)(((int64_t)(x - tile * n_it + 1) * P.sk_parts - 1) / n_it);
+  }
+  __device__ __forceinline__ void init(const MmParams& P) {
+    const int b = (int)(blockIdx.x >> 1);
+    g = g_hi = 0;
+    if (b < P.sk_pairs) {
+      g = share_of(P, b);
+      g_hi = share_of(P, b + 1);
+    }
+    t = P.sk_tiles + b;
+  }
+  __device__ __forceinline__ bool next(const MmParams& P) {
+    const int n_it = P.segs * P.kt;
+    int tile;
+    lo = 0;
+    hi = n_it;
+    shared = -1;
+    own = 0;
+    if (g < g_hi) {
+      tile = g / n_it;
+      lo = g - tile * n_it;
+      hi = min(n_it, lo + (g_hi - g));
+      g += hi - lo;
+      if (hi - lo < n_it) {
+        const int p0 = pair_of(P, tile * n_it);
+        shared = tile;
+        parts = pair_of(P, tile * n_it + n_it - 1) - p0 + 1;
+        own = (int)(blockIdx.x >> 1) - p0;
+      }
+    } else {
+      if (t >= P.tiles) return false;
+      tile = t;
+      t += (int)(gridDim.x >> 1);
+    }
     const int per = P.tiles_m * P.tiles_n;
-    prob = t / per;
-    const int r = t - prob * per;
-    const int g = r / (8 * P.tiles_n), rows = min(8, P.tiles_m - 8 * g);
-    const int i = r - g * 8 * P.tiles_n;
+    prob = tile / per;
+    const int r = tile - prob * per;
+    const int q = r / (8 * P.tiles_n), rows = min(8, P.tiles_m - 8 * q);
+    const int i = r - q * 8 * P.tiles_n;
     tn = i / rows;
-    tm = 8 * g + (i - tn * rows);
-    t += (int)(gridDim.x >> 1);
+    tm = 8 * q + (i - tn * rows);
     return true;
+  }
+  // Where part p of the tile lies: a pair has two slots, the second for a tile
+  // that its share did not begin in.
+  __device__ __forceinline__ int slot(const MmParams& P, int p) const {
+    const int b = (int)(blockIdx.x >> 1) - own + p;
+    return 2 * b + (share_of(P, b) < shared * (P.segs * P.kt));
   }
 };
 
@@ -280,9 +404,7 @@ __global__ void __launch_bounds__(C::kThreads, 1) mm_pair(const __grid_constant_
     for (const long long t0 = clock64(); clock64() - t0 < kStayCycles;) __nanosleep(1000);
   };
   Tiles T;
-  T.init();
-  int prob, tm, tn;
-  const int n_it = P.segs * P.kt;
+  T.init(P);
 
   if (warp == 0) {
     // ---------------- producer: this CTA's half of A, of B, and the scales ----------------
@@ -291,10 +413,10 @@ __global__ void __launch_bounds__(C::kThreads, 1) mm_pair(const __grid_constant_
       int s = 0;
       uint32_t ph = 1;
       const uint32_t full0 = mapa(smem_u32(&bar_full[0]), 0);
-      while (!s_abort && T.next(P, prob, tm, tn)) {
-        const int m0 = tm * kTileM + (int)rank * kHalf;
-        const int n0 = C::GATED ? tn * (C::NT / 2) : tn * C::NT + (int)rank * (C::NT / 2);
-        for (int i = 0; i < n_it; ++i) {
+      while (!s_abort && T.next(P)) {
+        const int m0 = T.tm * kTileM + (int)rank * kHalf;
+        const int n0 = C::GATED ? T.tn * kHalf : T.tn * kTileN + (int)rank * kHalf;
+        for (int i = T.lo; i < T.hi; ++i) {
           const int w = wait(smem_u32(&bar_empty[s]), ph, &s_abort);
           if (w != kOk) {
             if (w == kTimeout) fail(kStatusTimeoutEmpty);
@@ -304,8 +426,8 @@ __global__ void __launch_bounds__(C::kThreads, 1) mm_pair(const __grid_constant_
           if (rank == 0) mbar_expect_tx(smem_u32(&bar_full[s]), 2 * C::kStage);
           const uint32_t bar = full0 + 8 * s;
           const uint32_t da = smem_u32(smem + s * kOpBytes);
-          const uint32_t db = smem_u32(smem + C::kBOff + s * C::kB);
-          const CUtensorMap* ma = &P.a[C::GATED ? 0 : seg + prob];
+          const uint32_t db = smem_u32(smem + C::kBOff + s * kOpBytes);
+          const CUtensorMap* ma = &P.a[C::GATED ? 0 : seg + T.prob];
           const CUtensorMap* mb = &P.b[C::GATED ? (int)rank : seg];
           if (C::KIND == k16) {
             if (!P.a_mn) {
@@ -318,7 +440,7 @@ __global__ void __launch_bounds__(C::kThreads, 1) mm_pair(const __grid_constant_
               tma_load_2d_pair(db, mb, kt * 64, n0, bar);
             } else {
               tma_load_2d_pair(db, mb, n0, kt * 64, bar);
-              if (C::NT == 256) tma_load_2d_pair(db + 8192, mb, n0 + 64, kt * 64, bar);
+              tma_load_2d_pair(db + 8192, mb, n0 + 64, kt * 64, bar);
             }
           } else {
             tma_load_2d_pair(da, ma, kt * kRowBytes, m0, bar);
@@ -327,9 +449,9 @@ __global__ void __launch_bounds__(C::kThreads, 1) mm_pair(const __grid_constant_
             const uint32_t sb = smem_u32(smem + C::kSbOff + s * C::kSb);
             tma_load_2d_pair(sa, &P.sa, 0, (m0 / 128) * P.atoms + kt * C::ATOMS, bar);
 #pragma unroll
-            for (int j = 0; j < C::GROUPS; ++j)
+            for (int j = 0; j < 2; ++j)
               tma_load_2d_pair(sb + j * C::ATOMS * 512, &P.sb[C::GATED ? j : 0], 0,
-                               (C::GATED ? tn : tn * C::GROUPS + j) * P.atoms + kt * C::ATOMS, bar);
+                               (C::GATED ? T.tn : T.tn * 2 + j) * P.atoms + kt * C::ATOMS, bar);
           }
           if (++s == C::STAGES) {
             s = 0;
@@ -351,7 +473,7 @@ __global__ void __launch_bounds__(C::kThreads, 1) mm_pair(const __grid_constant_
       const uint64_t sb0 = desc_scales(smem_u32(smem + C::kSbOff));
       // K = 16 of 16-bit elements: 32 bytes on in a K-major row, 16 rows on otherwise
       const int a_step = P.a_mn ? 2048 >> 4 : 32 >> 4, b_step = P.b_mn ? 2048 >> 4 : 32 >> 4;
-      for (; !s_abort && T.next(P, prob, tm, tn); ++tc) {
+      for (; !s_abort && T.next(P); ++tc) {
         const int buf = tc & 1;
         int w = kOk;
         if (C::OV > 0) {
@@ -365,7 +487,7 @@ __global__ void __launch_bounds__(C::kThreads, 1) mm_pair(const __grid_constant_
         }
         tc_fence_after();
         const uint32_t acc = tmem + (buf ? C::kAcc1 : 0);
-        for (int i = 0; i < n_it; ++i) {
+        for (int i = T.lo; i < T.hi; ++i) {
           if (!ready) {
             w = wait(smem_u32(&bar_full[s]), ph, &s_abort);
             if (w != kOk) {
@@ -390,10 +512,10 @@ __global__ void __launch_bounds__(C::kThreads, 1) mm_pair(const __grid_constant_
           if (C::KIND != k16) release(min(held, poll_ahead<2, C::STAGES>(smem_u32(&bar_empty[0]), so, so_ph)));
           const int kt = i >= P.kt ? i - P.kt : i;
           const int n_mma = kt == P.kt - 1 ? P.k_last : 4;
-          const uint64_t a = a0 + (uint64_t)((s * kOpBytes) >> 4), b = b0 + (uint64_t)((s * C::kB) >> 4);
+          const uint64_t a = a0 + (uint64_t)((s * kOpBytes) >> 4), b = b0 + (uint64_t)((s * kOpBytes) >> 4);
           if constexpr (C::KIND == k16) {
             for (int kk = 0; kk < n_mma; ++kk)
-              mma_16<2>(acc, a + (uint64_t)(kk * a_step), b + (uint64_t)(kk * b_step), P.idesc, (i | kk) > 0);
+              mma_16<2>(acc, a + (uint64_t)(kk * a_step), b + (uint64_t)(kk * b_step), P.idesc, i > T.lo || kk > 0);
           } else {
             constexpr bool NV = C::KIND == kNv;
             const uint64_t sa = sa0 + (uint64_t)((s * C::kSa) >> 4), sb = sb0 + (uint64_t)((s * C::kSb) >> 4);
@@ -408,18 +530,18 @@ __global__ void __launch_bounds__(C::kThreads, 1) mm_pair(const __grid_constant_
             const uint32_t c0 = tmem + C::kSfCol + sf * C::kSfStage;
 #pragma unroll
             for (int q = 0; q < C::ATOMS; ++q) {
-              const uint32_t c = c0 + q * 4 * (1 + C::GROUPS);
+              const uint32_t c = c0 + q * 12;
               copy_scales<2>(c, sa + (uint64_t)(q * 32));
 #pragma unroll
-              for (int j = 0; j < C::GROUPS; ++j)
+              for (int j = 0; j < 2; ++j)
                 copy_scales<2>(c + 4 + 4 * j, sb + (uint64_t)((j * C::ATOMS + q) * 32));
             }
 #pragma unroll
             for (int kk = 0; kk < 4; ++kk) {
               if (kk >= n_mma) break;
-              const uint32_t c = c0 + (NV ? kk : kk >> 1) * 4 * (1 + C::GROUPS);
+              const uint32_t c = c0 + (NV ? kk : kk >> 1) * 12;
               mma_fp4<2, NV>(acc, a + (uint64_t)(2 * kk), b + (uint64_t)(2 * kk),
-                             NV || !(kk & 1) ? P.idesc : P.idesc | idesc_fp4(0, 0, false, 2), c, c + 4, (i | kk) > 0);
+                             NV || !(kk & 1) ? P.idesc : P.idesc | idesc_fp4(0, 0, false, 2), c, c + 4, i > T.lo || kk > 0);
             }
             if (++sf == C::SF) sf = 0;
             ++held;
@@ -442,13 +564,13 @@ __global__ void __launch_bounds__(C::kThreads, 1) mm_pair(const __grid_constant_
     // ---------------- epilogue: a lane owns a row of the tile ----------------
     const int q = warp & 3, e0 = (warp - C::kEpiWarp) >> 2;
     const uint32_t acce0 = mapa(smem_u32(&bar_acce[0]), 0);
-    constexpr int kChunks = C::GATED ? C::NT / 64 : C::NT / 32;
+    constexpr int kChunks = C::GATED ? kTileN / 64 : kTileN / 32;
     constexpr int kOvChunks = C::OV / 32;
     pdl_wait();
-    for (int tc = 0; !s_abort && T.next(P, prob, tm, tn); ++tc) {
+    for (int tc = 0; !s_abort && T.next(P); ++tc) {
       const int buf = tc & 1;
-      const int64_t m = (int64_t)tm * kTileM + (int)rank * kHalf + 32 * q + lane;
-      const int n0 = C::GATED ? tn * (C::NT / 2) : tn * C::NT;
+      const int64_t m = (int64_t)T.tm * kTileM + (int)rank * kHalf + 32 * q;  // the warp's first row
+      const int n0 = C::GATED ? T.tn * kHalf : T.tn * kTileN;
       const int w = wait(smem_u32(&bar_accf[buf]), (tc >> 1) & 1, &s_abort);
       if (w != kOk) {
         if (w == kTimeout) fail(kStatusTimeoutFull);
@@ -463,47 +585,132 @@ __global__ void __launch_bounds__(C::kThreads, 1) mm_pair(const __grid_constant_
         if (lane == 0) mbar_arrive_cluster(acce0 + (C::OV > 0 ? 0 : 8 * buf));
         released = true;
       };
-#pragma unroll 1
-      for (int i = e0; i < kChunks; i += C::EPQ) {
-        // the columns that the accumulators share are the first one's last, the second one's first
-        const int c = C::OV > 0 && buf == 0 ? kChunks - 1 - i : i;
-        uint32_t r0[32], r1[C::GATED ? 32 : 1];
-        tc_ld_32x32b_x32(t0 + 32 * c, r0);
-        if constexpr (C::GATED) tc_ld_32x32b_x32(t0 + C::NT / 2 + 32 * c, r1);
-        tc_wait_ld();
-        tc_regs_ready(r0);
-        tc_regs_ready(r1);
-        if (C::OV > 0 && !released && i + C::EPQ >= kOvChunks) release();
-        const int n = n0 + 32 * c, cnt = min(32, P.N - n);
-        if (m >= P.M || (cnt <= 0 && !P.qfmt)) continue;
+      // a chunk's outputs from its accumulators (GATED: of gate and of up)
+      auto finish = [&](int c, uint32_t (&r0)[32], uint32_t (&r1)[C::GATED ? 32 : 1]) {
+        const int n = n0 + 32 * c;
         float v[32];
         if constexpr (C::GATED) {
-          if (P.saved[0] && cnt > 0) {
+          if (P.saved[0]) {
             const bool bf = P.type == POLYQ_BF16;
-            float s[32];
 #pragma unroll
-            for (int j = 0; j < 32; ++j) s[j] = saved_range(__uint_as_float(r0[j]), bf);
-            store_row32(P.saved[0], m * P.saved_stride + n, s, cnt, P.type, true);
+            for (int j = 0; j < 32; ++j) v[j] = saved_range(__uint_as_float(r0[j]), bf);
+            store_chunk(P.saved[0], P.saved_stride, nullptr, 0, m, n, P.M, P.N, v, P.type, P.vec_saved);
 #pragma unroll
-            for (int j = 0; j < 32; ++j) s[j] = saved_range(__uint_as_float(r1[j]), bf);
-            store_row32(P.saved[1], m * P.saved_stride + n, s, cnt, P.type, true);
+            for (int j = 0; j < 32; ++j) v[j] = saved_range(__uint_as_float(r1[j]), bf);
+            store_chunk(P.saved[1], P.saved_stride, nullptr, 0, m, n, P.M, P.N, v, P.type, P.vec_saved);
           }
 #pragma unroll
           for (int j = 0; j < 32; ++j)
             v[j] = silu(__uint_as_float(r0[j]) * P.alpha[0]) * (__uint_as_float(r1[j]) * P.alpha[1]);
           if (P.qfmt) {
 #pragma unroll
-            for (int j = 0; j < 32; ++j) v[j] = j < cnt ? v[j] : 0.f;
-            if (P.qfmt == kNv) store_codes32<true>(P, m, n, v);
-            else store_codes32<false>(P, m, n, v);
-            continue;
+            for (int j = 0; j < 32; ++j) v[j] = n + j < P.N ? v[j] : 0.f;
+            if (m + lane >= P.M) return;
+            if (P.qfmt == kNv) store_codes32<true>(P, m + lane, n, v);
+            else store_codes32<false>(P, m + lane, n, v);
+            return;
           }
+          store_chunk(P.y[0], P.y_stride, nullptr, 0, m, n, P.M, P.N, v, P.type, P.vec);
         } else {
 #pragma unroll
           for (int j = 0; j < 32; ++j) v[j] = __uint_as_float(r0[j]) * P.alpha[0];
-          if (P.res) add_row32(P.res, m * P.res_stride + n, v, cnt, P.type, P.vec);
+          store_chunk(P.y[T.prob], P.y_stride, P.res, P.res_stride, m, n, P.M, P.N, v, P.type, P.vec);
         }
-        store_row32(P.y[C::GATED ? 0 : prob], m * P.y_stride + n, v, cnt, P.type, P.vec);
+      };
+      auto load = [&](int c, uint32_t (&r0)[32], uint32_t (&r1)[C::GATED ? 32 : 1]) {
+        tc_ld_32x32b_x32(t0 + 32 * c, r0);
+        if constexpr (C::GATED) tc_ld_32x32b_x32(t0 + kHalf + 32 * c, r1);
+        tc_wait_ld();
+        tc_regs_ready(r0);
+        tc_regs_ready(r1);
+      };
+      // A warp's i-th chunk (GATED: of gate, and of up): the columns that the
+      // accumulators share are the first one's last and the second one's first.
+      auto chunk = [&](int i) { return C::OV > 0 && buf == 0 && T.shared < 0 ? kChunks - 1 - i : i; };
+      // whether a chunk has an output (4 bits: a scale or a code) of this matrix
+      auto inside = [&](int c) { return m < P.M && (P.qfmt != 0 || n0 + 32 * c < P.N); };
+      // A part goes into its slot; the warp that finds the other parts of its
+      // chunks in place adds them all, in the order of the pairs.
+      auto part = [&](int slot, int col) {  // 4 columns of the lane's row
+        return reinterpret_cast<float4*>(P.parts) + ((int64_t)slot * (kTileN / 4) + col / 4) * kTileM +
+               (int)rank * kHalf + 32 * q + lane;
+      };
+      auto put = [&](int slot, int col, const uint32_t (&r)[32]) {
+        float4* d = part(slot, col);
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          __stcg(d + j * kTileM, make_float4(__uint_as_float(r[4 * j]), __uint_as_float(r[4 * j + 1]),
+                                             __uint_as_float(r[4 * j + 2]), __uint_as_float(r[4 * j + 3])));
+      };
+      auto add = [&](int slot, int col, uint32_t (&r)[32]) {
+        const float4* d = part(slot, col);
+        float4 f[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) f[j] = __ldcg(d + j * kTileM);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          r[4 * j] = __float_as_uint(__uint_as_float(r[4 * j]) + f[j].x);
+          r[4 * j + 1] = __float_as_uint(__uint_as_float(r[4 * j + 1]) + f[j].y);
+          r[4 * j + 2] = __float_as_uint(__uint_as_float(r[4 * j + 2]) + f[j].z);
+          r[4 * j + 3] = __float_as_uint(__uint_as_float(r[4 * j + 3]) + f[j].w);
+        }
+      };
+      const int slot0 = T.shared >= 0 ? T.slot(P, T.own) : 0;
+      int mine = 1;
+      if (T.shared >= 0) {
+#pragma unroll 1
+        for (int j = 0, i; (i = e0 + j / C::MATS * C::EPQ) < kChunks; ++j) {
+          const int c = chunk(i), col = 32 * c + j % C::MATS * kHalf;
+          if (!inside(c)) continue;
+          uint32_t r[32];
+          tc_ld_32x32b_x32(t0 + col, r);
+          tc_wait_ld();
+          tc_regs_ready(r);
+          if (m + lane < P.M) put(slot0, col, r);
+          __syncwarp();
+        }
+        __threadfence();
+        __syncwarp();
+        if (lane == 0) {
+          int* counter = P.counters + (T.shared * 2 + (int)rank) * C::EPI + (warp - C::kEpiWarp);
+          mine = atomicAdd(counter, 1) == T.parts - 1;
+          if (mine) *counter = 0;  // for the next launch
+        }
+        mine = __shfl_sync(0xffffffffu, mine, 0);
+        __threadfence();
+        if (mine) {  // the sums back into tensor memory
+#pragma unroll 1
+          for (int j = 0, i; (i = e0 + j / C::MATS * C::EPQ) < kChunks; ++j) {
+            const int c = chunk(i), col = 32 * c + j % C::MATS * kHalf;
+            if (!inside(c)) continue;
+            uint32_t r[32] = {};
+#pragma unroll 1
+            for (int p = 0; p < T.parts; ++p) {
+              if (p != T.own) {
+                if (m + lane < P.M) add(T.slot(P, p), col, r);
+                __syncwarp();
+              } else {
+                uint32_t f[32];
+                tc_ld_32x32b_x32(t0 + col, f);
+                tc_wait_ld();
+                tc_regs_ready(f);
+#pragma unroll
+                for (int k = 0; k < 32; ++k) r[k] = __float_as_uint(__uint_as_float(r[k]) + __uint_as_float(f[k]));
+              }
+            }
+            tmem_st32(t0 + col, r);
+          }
+        }
+      }
+      if (mine) {
+#pragma unroll 1
+        for (int i = e0; i < kChunks; i += C::EPQ) {
+          const int c = chunk(i);
+          uint32_t r0[32], r1[C::GATED ? 32 : 1];
+          load(c, r0, r1);
+          if (C::OV > 0 && !released && T.shared < 0 && i + C::EPQ >= kOvChunks) release();
+          if (inside(c)) finish(c, r0, r1);
+        }
       }
       __syncwarp();
       if (!released) release();
@@ -540,10 +747,11 @@ struct Few {
   static constexpr size_t kSmem = (size_t)STAGES * kStage + 1024;
   static constexpr int kSfStage = ATOMS * 4 * (MATS + 1);
   static constexpr int kSfCol = MATS * NT;
-  static constexpr int kCols = kSfCol + 2 * kSfStage;
+  static constexpr int SF = 4;  // stages' scales
+  static constexpr int kCols = kSfCol + SF * kSfStage;
   static constexpr int kTmem = kCols <= 32 ? 32 : kCols <= 64 ? 64 : kCols <= 128 ? 128 : kCols <= 256 ? 256 : 512;
   static constexpr int kThreads = 256;
-  static_assert(MATS * NT * kHalf * 4 <= STAGES * kStage && STAGES >= 4, "the parts fit where the stages were");
+  static_assert(MATS * NT * kHalf * 4 <= STAGES * kStage && STAGES >= SF && kCols <= 512, "parts where the stages were");
 };
 
 template <class C>
@@ -622,52 +830,74 @@ __global__ void __launch_bounds__(C::kThreads, 1) mm_few(const __grid_constant__
   } else if (warp == 1) {
     // ---------------- MMA issuer ----------------
     if (elect_one()) {
-      int s = 0;
-      uint32_t ph = 0;
+      int s = 0, sf = 0, so = 0, held = 0;  // as in mm_pair
+      uint32_t ph = 0, so_ph = 0;
+      bool ready = false;
       const uint64_t a0 = desc_sw128(smem_u32(smem), 16), b0 = desc_sw128(smem_u32(smem + C::kBOff), 16);
       const uint64_t sa0 = desc_scales(smem_u32(smem + C::kSaOff)), sb0 = desc_scales(smem_u32(smem + C::kSbOff));
       for (int kt = kt0; kt < kt1; ++kt) {
-        const int it = kt - kt0;
-        int w = wait(smem_u32(&bar_full[s]), ph, &s_abort);
-        if (C::KIND != k16 && w == kOk && it >= 2)
-          w = wait(smem_u32(&bar_empty[(it - 2) % C::STAGES]), ((it - 2) / C::STAGES) & 1, &s_abort);
+        int w = kOk;
+        if (!ready) w = wait(smem_u32(&bar_full[s]), ph, &s_abort);
         if (w != kOk) {
           if (w == kTimeout) fail(kStatusTimeoutFull);
           break;
         }
         tc_fence_after();
+        const int s1 = s + 1 == C::STAGES ? 0 : s + 1;
+        const uint32_t ph1 = s1 == 0 ? ph ^ 1u : ph;
+        ready = mbar_test(smem_u32(&bar_full[s1]), ph1);
         const int n_mma = kt == P.kt - 1 ? P.k_last : 4;
         const uint64_t a = a0 + (uint64_t)((s * C::MATS * kOpBytes) >> 4), b = b0 + (uint64_t)((s * C::kB) >> 4);
-        const uint32_t sf = tmem + C::kSfCol + (it & 1) * C::kSfStage;
+        const uint32_t c0 = tmem + C::kSfCol + sf * C::kSfStage;
         if constexpr (C::KIND != k16) {
+          auto release = [&](int n) {
+            held -= n;
+            so += n;
+            if (so >= C::STAGES) {
+              so -= C::STAGES;
+              so_ph ^= 1u;
+            }
+          };
+          if (held == C::SF) release(poll_ahead<2, C::STAGES>(smem_u32(&bar_empty[0]), so, so_ph));
+          if (held == C::SF) {
+            w = wait(smem_u32(&bar_empty[so]), so_ph, &s_abort);
+            if (w != kOk) {
+              if (w == kTimeout) fail(kStatusTimeoutEmpty);
+              break;
+            }
+            release(1);
+          }
           const uint64_t sa = sa0 + (uint64_t)((s * C::kSa) >> 4), sb = sb0 + (uint64_t)((s * C::kSb) >> 4);
 #pragma unroll
           for (int q = 0; q < C::ATOMS; ++q) {
-            const uint32_t c = sf + q * 4 * (C::MATS + 1);
+            const uint32_t c = c0 + q * 4 * (C::MATS + 1);
 #pragma unroll
             for (int j = 0; j < C::MATS; ++j) copy_scales<1>(c + 4 * j, sa + (uint64_t)((j * C::ATOMS + q) * 32));
             copy_scales<1>(c + 4 * C::MATS, sb + (uint64_t)(q * 32));
           }
+          if (++sf == C::SF) sf = 0;
+          ++held;
         }
-        for (int kk = 0; kk < n_mma; ++kk)
+#pragma unroll
+        for (int kk = 0; kk < 4; ++kk) {
+          if (kk >= n_mma) break;
 #pragma unroll
           for (int j = 0; j < C::MATS; ++j) {
             const uint64_t aj = a + (uint64_t)((j * kOpBytes) >> 4) + (uint64_t)(2 * kk);
+            const bool acc = kt > kt0 || kk > 0;
             if constexpr (C::KIND == k16) {
-              mma_16<1>(tmem + j * C::NT, aj, b + (uint64_t)(2 * kk), P.idesc, (it | kk) > 0);
+              mma_16<1>(tmem + j * C::NT, aj, b + (uint64_t)(2 * kk), P.idesc, acc);
             } else {
               constexpr bool NV = C::KIND == kNv;
-              const uint32_t c = sf + (NV ? kk : kk >> 1) * 4 * (C::MATS + 1);
+              const uint32_t c = c0 + (NV ? kk : kk >> 1) * 4 * (C::MATS + 1);
               const uint32_t id = NV || !(kk & 1) ? P.idesc : P.idesc | idesc_fp4(0, 0, false, 2);
-              mma_fp4<1, NV>(tmem + j * C::NT, aj, b + (uint64_t)(2 * kk), id, c + 4 * j, c + 4 * C::MATS,
-                             (it | kk) > 0);
+              mma_fp4<1, NV>(tmem + j * C::NT, aj, b + (uint64_t)(2 * kk), id, c + 4 * j, c + 4 * C::MATS, acc);
             }
           }
-        commit<1>(smem_u32(&bar_empty[s]));
-        if (++s == C::STAGES) {
-          s = 0;
-          ph ^= 1u;
         }
+        commit<1>(smem_u32(&bar_empty[s]));
+        s = s1;
+        ph = ph1;
       }
       commit<1>(smem_u32(&bar_acc));
       wait_stay(smem_u32(&bar_acc), 0);
@@ -696,59 +926,77 @@ __global__ void __launch_bounds__(C::kThreads, 1) mm_few(const __grid_constant__
   pdl_wait();
   const int n = n0 + 32 * q + lane;
   const uint32_t mine = smem_u32(part + 32 * q + lane);
-  auto sum = [&](int col) {
-    const uint32_t at = mine + col * (kHalf * 4);
-    if (split == 1) return part[col * kHalf + 32 * q + lane];
-    float v = 0.f;
-    for (int r = 0; r < split; ++r) v += ld_cluster_f32(mapa(at, r));
-    return v;
-  };
-#pragma unroll 2
-  for (int j = rank + split * half; j < C::NT; j += 2 * split) {
-    const int64_t m = m0 + j;
-    if (m >= P.M) break;
-    float v = sum(j) * P.alpha[0];
-    if constexpr (C::GATED) {
-      const float u = sum(C::NT + j) * P.alpha[1];
-      if (P.saved[0] && n < P.N) {
-        store_dense(P.saved[0], m * P.saved_stride + n, saved_range(v, P.type == POLYQ_BF16), P.type);
-        store_dense(P.saved[1], m * P.saved_stride + n, saved_range(u, P.type == POLYQ_BF16), P.type);
-      }
-      v = silu(v) * u;
-      if (P.qfmt) {
-        // a block is the warp (MX) or half of it (NV), a lane an element
-        const bool nv = P.qfmt == kNv;
-        float t = n < P.N ? v : 0.f;
-        if (nv) t = P.inv_g != 0.f ? t * P.inv_g : __fdiv_rn(t, P.g);
-        uint32_t mx = __float_as_uint(t) & 0x7FFFFFFFu;
+  // U columns at a time, so that the reads from the peers' shared memory are
+  // under way together (one at a time: 128 tokens, 5120 x 5120 15.2 us, 10.8 so)
+  constexpr int U = 4;
+  auto sums = [&](int col0, float (&v)[U]) {  // columns col0, col0 + split, ...
 #pragma unroll
-        for (int d = 1; d < 16; d *= 2) mx = max(mx, __shfl_xor_sync(0xffffffffu, mx, d));
-        if (!nv) mx = max(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
-        const float z[8] = {t};
-        uint32_t byte, w;
-        if (nv) {
-          const fp4::Scale<true> sc(mx);
-          byte = sc.byte;
-          w = sc.codes(z);
-        } else {
-          const fp4::Scale<false> sc(mx);
-          byte = sc.byte;
-          w = sc.codes(z);
-        }
-        w = (w & 15u) << (4 * (lane & 7));  // 8 lanes make a word
+    for (int i = 0; i < U; ++i) v[i] = 0.f;
+    if (split == 1) {
 #pragma unroll
-        for (int d = 1; d < 8; d *= 2) w |= __shfl_xor_sync(0xffffffffu, w, d);
-        if ((lane & 7) == 0 && n < P.N) *reinterpret_cast<uint32_t*>(P.codes + m * P.code_stride + n / 2) = w;
-        const int bl = nv ? 16 : 32;
-        const int64_t blk = n / bl;
-        if ((lane & (bl - 1)) == 0 && blk >> 2 < P.out_atoms)
-          P.scales[fp4::scale_off(m, blk, P.out_atoms)] = (uint8_t)byte;
-        continue;
+      for (int i = 0; i < U; ++i) v[i] = part[min(col0 + i, C::MATS * C::NT - 1) * kHalf + 32 * q + lane];
+    } else {
+#pragma unroll 4
+      for (int r = 0; r < split; ++r) {
+        const uint32_t at = mapa(mine, r);
+#pragma unroll
+        for (int i = 0; i < U; ++i)
+          v[i] += ld_cluster_f32(at + min(col0 + i * split, C::MATS * C::NT - 1) * (kHalf * 4));
       }
-    } else if (P.res && n < P.N) {
-      v += load_dense(P.res, m * P.res_stride + n, P.type);
     }
-    if (n < P.N) store_dense(P.y[0], m * P.y_stride + n, v, P.type);
+  };
+#pragma unroll 1
+  for (int j0 = rank + split * U * half; j0 < C::NT && m0 + j0 < P.M; j0 += 2 * U * split) {
+    float vs[U], us[U];
+    sums(j0, vs);
+    if (C::GATED) sums(C::NT + j0, us);
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      const int j = j0 + i * split;
+      const int64_t m = m0 + j;
+      if (j >= C::NT || m >= P.M) break;
+      float v = vs[i] * P.alpha[0];
+      if constexpr (C::GATED) {
+        const float u = us[i] * P.alpha[1];
+        if (P.saved[0] && n < P.N) {
+          store_dense(P.saved[0], m * P.saved_stride + n, saved_range(v, P.type == POLYQ_BF16), P.type);
+          store_dense(P.saved[1], m * P.saved_stride + n, saved_range(u, P.type == POLYQ_BF16), P.type);
+        }
+        v = silu(v) * u;
+        if (P.qfmt) {
+          // a block is the warp (MX) or half of it (NV), a lane an element
+          const bool nv = P.qfmt == kNv;
+          float t = n < P.N ? v : 0.f;
+          if (nv) t = P.inv_g != 0.f ? t * P.inv_g : __fdiv_rn(t, P.g);
+          uint32_t mx = __float_as_uint(t) & 0x7FFFFFFFu;
+          if (nv) mx = __reduce_max_sync(lane < 16 ? 0x0000FFFFu : 0xFFFF0000u, mx);
+          else mx = __reduce_max_sync(0xFFFFFFFFu, mx);
+          const float z[8] = {t};
+          uint32_t byte, w;
+          if (nv) {
+            const fp4::Scale<true> sc(mx);
+            byte = sc.byte;
+            w = sc.codes(z);
+          } else {
+            const fp4::Scale<false> sc(mx);
+            byte = sc.byte;
+            w = sc.codes(z);
+          }
+          w = (w & 15u) << (4 * (lane & 7));  // 8 lanes make a word
+#pragma unroll
+          for (int d = 1; d < 8; d *= 2) w |= __shfl_xor_sync(0xffffffffu, w, d);
+          if ((lane & 7) == 0 && n < P.N) *reinterpret_cast<uint32_t*>(P.codes + m * P.code_stride + n / 2) = w;
+          const int bl = nv ? 16 : 32;
+          const int64_t blk = n / bl;
+          if ((lane & (bl - 1)) == 0 && blk >> 2 < P.out_atoms)
+            P.scales[fp4::scale_off(m, blk, P.out_atoms)] = (uint8_t)byte;
+          continue;
+        }
+      } else if (P.res && n < P.N) {
+        v += load_dense(P.res, m * P.res_stride + n, P.type);
+      }
+      if (n < P.N) store_dense(P.y[0], m * P.y_stride + n, v, P.type);
+    }
   }
   __syncthreads();
   if (split > 1) cluster_sync();  // a peer may still read this CTA's part
@@ -872,22 +1120,66 @@ int launch_cluster(const void* f, dim3 grid, int threads, size_t smem, int clust
   return POLYQ_OK;
 }
 
+// The workspace: the status word, the counters of shared tiles' parts, and two
+// parts (256 x 256 fp32) for each pair of SMs.
+constexpr size_t kCountersOff = POLYQ_FP4_WORKSPACE_ZERO - 16384, kPartsOff = POLYQ_FP4_WORKSPACE_ZERO;
+constexpr int kMaxPairs = 16384 / (2 * kEpiWarps * 4);
+size_t workspace_bytes_of(int sms) { return kPartsOff + (size_t)sms * kTileM * kTileN * 4; }
+
+// How a pair launch shares its tiles (P.tiles, P.segs, P.kt are set): whole tiles
+// in whole waves; the last wave's along the contraction where pairs would be
+// idle and that is shorter.  In stages (0.3 us): writing a part and finding the
+// others in place cost kShareCost, each part that the last of a tile's pairs
+// adds kPartCost; where shares do not end with tiles a pair has two parts.
+// (256 x 1024 x 13824 4 bits, 4 tiles: 19.9 us whole, 18.0 / 17.0 / 18.6 in 2 / 3 / 6
+// parts; 5120 instead of 13824 11.1, 13.7 in 2.  16-bit, 4 tiles of 160 stages
+// beside 76 whole ones 105 us, 72 in 4.)
+constexpr double kShareCost = 11, kPartCost = 4.5;
+void plan_tiles(MmParams& P, int pairs) {
+  const int n_it = P.segs * P.kt, rest = P.tiles % pairs;
+  P.sk_tiles = P.sk_pairs = P.sk_parts = P.sk_share = P.sk_extra = 0;
+  if (rest == 0) return;
+  double best = 0.95 * n_it;
+  for (int s = 2; s * rest <= pairs && s <= n_it; ++s) {
+    const double t = (n_it + s - 1) / s + kShareCost + kPartCost * s;
+    if (t < best) {
+      best = t;
+      P.sk_tiles = rest;
+      P.sk_parts = s;
+      P.sk_pairs = s * rest;
+    }
+  }
+  const double share = (double)rest * n_it / pairs;
+  if (share >= 2 && share + 2 * kShareCost + kPartCost * (std::ceil(n_it / share) + 1) < 0.95 * best) {
+    P.sk_tiles = rest;
+    P.sk_parts = 0;
+    P.sk_pairs = pairs;
+    P.sk_share = (int)((int64_t)rest * n_it / pairs);
+    P.sk_extra = (int)((int64_t)rest * n_it % pairs);
+  }
+}
+
 // Tiles of a pair launch: P.M, P.N, P.probs are set.
 template <class C>
-int run_pair(MmParams& P, int dev, void* stream, const char* who) {
+int run_pair(MmParams& P, int dev, void* workspace, void* stream, const char* who) {
   static std::atomic<int> cached[kMaxDevices];
   int pairs = 0;
   const int rc = resident_clusters((const void*)mm_pair<C>, C::kThreads, C::kSmem, 2, &cached[dev], &pairs, who);
   if (rc) return rc;
-  const int cols = C::GATED ? C::NT / 2 : C::NT;
+  pairs = std::min(pairs, kMaxPairs);
+  const int cols = C::GATED ? kHalf : kTileN;
   P.tiles_m = (P.M + kTileM - 1) / kTileM;
   P.tiles_n = (P.N + cols - 1) / cols;
   const int64_t tiles = (int64_t)P.tiles_m * P.tiles_n * P.probs;
   if (tiles >= 1ll << 31) return polyq_set_error(POLYQ_EUNSUPPORTED, "%s: %lld tiles", who, (long long)tiles);
   P.tiles = (int)tiles;
+  P.counters = (int*)((uint8_t*)workspace + kCountersOff);
+  P.parts = (float*)((uint8_t*)workspace + kPartsOff);
+  plan_tiles(P, pairs);
+  const int grid = P.tiles > pairs ? pairs : std::max(P.tiles, P.sk_pairs);
   void* args[] = {&P};
-  return launch_cluster((const void*)mm_pair<C>, dim3((unsigned)(2 * std::min(P.tiles, pairs))), C::kThreads,
-                        C::kSmem, 2, args, stream, who);
+  return launch_cluster((const void*)mm_pair<C>, dim3((unsigned)(2 * grid)), C::kThreads, C::kSmem, 2, args, stream,
+                        who);
 }
 
 // Few tokens: P.M tokens, P.N weight rows.
@@ -915,7 +1207,11 @@ int run_few(MmParams& P, int dev, void* stream, const char* who) {
                         best, args, stream, who);
 }
 
-int check_workspace(const void* ws, size_t bytes, size_t need, const char* who) {
+int check_workspace(const void* ws, size_t bytes, size_t more, const char* who) {
+  size_t need = 0;
+  const int rc = polyq_fp4_workspace_bytes(&need);
+  if (rc) return rc;
+  need += more;
   if (!ws || bytes < need)
     return polyq_set_error(POLYQ_ENOMEM, "%s: workspace needs %zu bytes, got %zu", who, need, bytes);
   if ((uintptr_t)ws % 256) return polyq_set_error(POLYQ_EINVAL, "%s: workspace must be 256-byte aligned", who);
@@ -923,9 +1219,12 @@ int check_workspace(const void* ws, size_t bytes, size_t need, const char* who) 
 }
 
 int elem_bytes(int type) { return type == POLYQ_F32 ? 4 : 2; }
-bool vec_rows(const polyq_dense* d) {
-  return (uintptr_t)d->data % 16 == 0 && d->stride * elem_bytes(d->type) % 16 == 0;
+// Whether rows start on 32 (2), 16 (1) or fewer bytes (0).
+int vec_rows(const void* p, int64_t stride, int type) {
+  const uint64_t a = (uint64_t)(uintptr_t)p | (uint64_t)(stride * elem_bytes(type));
+  return a % 32 == 0 ? 2 : a % 16 == 0 ? 1 : 0;
 }
+int vec_rows(const polyq_dense* d) { return vec_rows(d->data, d->stride, d->type); }
 
 // Tensor maps of a 4-bit operand: its code tiles of `rows` rows, and its scales.
 int map_fp4(CUtensorMap* codes, CUtensorMap* scales, const polyq_fp4* t, int rows, const char* who) {
@@ -945,7 +1244,11 @@ int map_16(CUtensorMap* m, const void* data, int64_t stride, int64_t rows, int64
                              mn ? 64u : (uint32_t)box_rows, 128);
 }
 
-constexpr int kFewTokens = 128;  // at most this many tokens: mm_few
+// At most this many tokens (GATED: half): mm_few.  (MX, us, mm_few and mm_pair:
+// 13824 x 5120 48 tokens 11.0 / 14, 128 tokens 16.0 / 14.1; 5120 x 5120 128 tokens
+// 10.8 / 11.8, 5120 x 13824 64 tokens 11.3 / 18; gated 13824 x 5120 48 tokens 16.0 /
+// 23, 128 tokens 25.9 / 23, 5120 x 5120 128 tokens 16.3 / 12.)
+constexpr int kFewTokens = 128;
 int few_tile(int64_t M) { return M <= 16 ? 16 : M <= 32 ? 32 : M <= 64 ? 64 : 128; }
 
 template <int KIND, bool GATED>
@@ -954,8 +1257,10 @@ int dispatch_few(MmParams& P, int dev, void* stream, const char* who) {
     case 16: return run_few<Few<KIND, 16, GATED>>(P, dev, stream, who);
     case 32: return run_few<Few<KIND, 32, GATED>>(P, dev, stream, who);
     case 64: return run_few<Few<KIND, 64, GATED>>(P, dev, stream, who);
-    default: return run_few<Few<KIND, 128, GATED>>(P, dev, stream, who);
+    default: break;
   }
+  if constexpr (!GATED) return run_few<Few<KIND, 128, GATED>>(P, dev, stream, who);
+  return POLYQ_EUNSUPPORTED;  // not reached: kFewTokens
 }
 
 void set_quant_out(MmParams& P, const polyq_fp4* q) {
@@ -974,24 +1279,14 @@ float product_scale(const polyq_fp4* a, const polyq_fp4* b) {
   return (float)((double)a->tensor_scale * (double)b->tensor_scale);
 }
 
-// Whether the wide tile wins: waves of tiles of 256 columns against waves of
-// half of that, which take a little more than half the time each.
-bool wide_tile(const MmParams& P, int sms, bool gated) {
-  const int64_t tm = (P.M + kTileM - 1) / kTileM * (int64_t)P.probs, pairs = std::max(1, sms / 2);
-  const int c = gated ? 128 : 256;
-  const int64_t w = (tm * ((P.N + c - 1) / c) + pairs - 1) / pairs, h = (tm * ((P.N + c / 2 - 1) / (c / 2)) + pairs - 1) / pairs;
-  return w <= 0.58 * h;
-}
-
 // The product of 4-bit operands: x [M][K] with w0 (and w1) [N][K].
 template <int KIND, bool GATED>
-int run_fp4(MmParams& P, const polyq_fp4* x, const polyq_fp4* w0, const polyq_fp4* w1, void* stream,
-            const char* who) {
-  int dev = 0, sms = 0;
+int run_fp4(MmParams& P, const polyq_fp4* x, const polyq_fp4* w0, const polyq_fp4* w1, void* workspace,
+            void* stream, const char* who) {
+  int dev = 0;
   int rc = device_index(&dev, who);
-  if (!rc) rc = polyq_sm_count(&sms);
   if (rc) return rc;
-  const bool nv = KIND == kNv, few = x->rows <= kFewTokens;
+  const bool nv = KIND == kNv, few = x->rows <= (GATED ? kFewTokens / 2 : kFewTokens);
   P.M = (int)x->rows;
   P.N = (int)w0->rows;
   P.segs = P.probs = 1;
@@ -1008,19 +1303,12 @@ int run_fp4(MmParams& P, const polyq_fp4* x, const polyq_fp4* w0, const polyq_fp
     if (!rc && GATED) rc = map_fp4(&P.b[1], &P.sb[1], w1, kHalf, who);
     return rc ? rc : dispatch_few<KIND, GATED>(P, dev, stream, who);
   }
-  const bool wide = GATED || wide_tile(P, sms, GATED);
-  P.idesc = idesc_fp4(kTileM, wide ? 256 : 128, !nv, 0);
+  P.idesc = idesc_fp4(kTileM, kTileN, !nv, 0);
   rc = map_fp4(&P.a[0], &P.sa, x, kHalf, who);
-  if (!rc) rc = map_fp4(&P.b[0], &P.sb[0], w0, wide ? 128 : 64, who);
-  if (GATED) {
-    if (!rc) rc = map_fp4(&P.b[1], &P.sb[1], w1, 128, who);
-  } else {
-    P.b[1] = P.b[0];
-  }
+  if (!rc) rc = map_fp4(&P.b[0], &P.sb[0], w0, kHalf, who);
+  if (!rc && GATED) rc = map_fp4(&P.b[1], &P.sb[1], w1, kHalf, who);
   if (rc) return rc;
-  if constexpr (!GATED)
-    if (!wide) return run_pair<Pair<KIND, 128, false>>(P, dev, stream, who);
-  return run_pair<Pair<KIND, 256, GATED>>(P, dev, stream, who);
+  return run_pair<Pair<KIND, GATED>>(P, dev, workspace, stream, who);
 }
 
 int check_same(const polyq_fp4* x, const polyq_fp4* w, const char* who, const char* what) {
@@ -1046,20 +1334,23 @@ int check_operand(const polyq_dense* d, int64_t cols, int type, const char* who,
     return polyq_set_error(POLYQ_EINVAL, "%s: %s: rows must start on 16 bytes (address and stride)", who, what);
   return POLYQ_OK;
 }
+// Bytes of the gradients of a and u.
+size_t grad_bytes(int64_t T, int64_t F) { return (size_t)T * (size_t)polyq_ffn_saved_stride(F) * 4; }
 int check_sizes(int64_t T, int64_t F, int64_t K, const char* who) {
   if (T < 1 || F < 1 || K < 1 || T > (1 << 24) || F > (1 << 24) || K > (1 << 24))
     return polyq_set_error(POLYQ_EINVAL, "%s: T=%lld F=%lld K=%lld", who, (long long)T, (long long)F, (long long)K);
   return POLYQ_OK;
 }
 
-// A 16-bit product on pairs.
-template <bool GATED>
-int run_16(MmParams& P, bool wide, int dev, void* stream, const char* who) {
-  return wide ? run_pair<Pair<k16, 256, GATED>>(P, dev, stream, who)
-              : run_pair<Pair<k16, 128, GATED>>(P, dev, stream, who);
-}
-
 }  // namespace
+
+extern "C" int polyq_fp4_workspace_bytes(size_t* bytes) {
+  if (!bytes) return polyq_set_error(POLYQ_EINVAL, "polyq_fp4_workspace_bytes: bytes is NULL");
+  int sms = 0;
+  const int rc = polyq_sm_count(&sms);
+  if (!rc) *bytes = workspace_bytes_of(sms);
+  return rc;
+}
 
 extern "C" int polyq_fp4_linear(const polyq_fp4* x, const polyq_fp4* w, const polyq_dense* residual,
                                 const polyq_dense* y, void* workspace, size_t workspace_bytes, void* stream) {
@@ -1070,7 +1361,7 @@ extern "C" int polyq_fp4_linear(const polyq_fp4* x, const polyq_fp4* w, const po
   if (!rc) rc = check_same(x, w, who, "w");
   if (!rc) rc = polyq_check_dense(y, w->rows, who, "y");
   if (!rc && residual) rc = polyq_check_dense(residual, w->rows, who, "residual");
-  if (!rc) rc = check_workspace(workspace, workspace_bytes, POLYQ_FP4_WORKSPACE_BYTES, who);
+  if (!rc) rc = check_workspace(workspace, workspace_bytes, 0, who);
   if (rc) return rc;
   if (residual && residual->type != y->type)
     return polyq_set_error(POLYQ_EINVAL, "%s: residual has type %d, y %d", who, residual->type, y->type);
@@ -1081,12 +1372,12 @@ extern "C" int polyq_fp4_linear(const polyq_fp4* x, const polyq_fp4* w, const po
   P.y[0] = y->data;
   P.y_stride = y->stride;
   P.type = y->type;
-  P.vec = vec_rows(y) && (!residual || vec_rows(residual));
+  P.vec = residual && !vec_rows(residual) ? 0 : vec_rows(y);
   P.res = residual ? residual->data : nullptr;
   P.res_stride = residual ? residual->stride : 0;
   P.status = (int*)workspace;
-  return x->format == POLYQ_FP4_NV ? run_fp4<kNv, false>(P, x, w, nullptr, stream, who)
-                                   : run_fp4<kMx, false>(P, x, w, nullptr, stream, who);
+  return x->format == POLYQ_FP4_NV ? run_fp4<kNv, false>(P, x, w, nullptr, workspace, stream, who)
+                                   : run_fp4<kMx, false>(P, x, w, nullptr, workspace, stream, who);
 }
 
 extern "C" int polyq_fp4_ffn(const polyq_fp4* x, const polyq_fp4* gate, const polyq_fp4* up, const polyq_dense* h,
@@ -1106,7 +1397,7 @@ extern "C" int polyq_fp4_ffn(const polyq_fp4* x, const polyq_fp4* gate, const po
   else rc = polyq_check_fp4(hq, who, "hq");
   if (!rc && hq && (hq->rows != x->rows || hq->K != gate->rows))
     rc = polyq_set_error(POLYQ_EINVAL, "%s: hq is [%lld][%lld]", who, (long long)hq->rows, (long long)hq->K);
-  if (!rc) rc = check_workspace(workspace, workspace_bytes, POLYQ_FP4_WORKSPACE_BYTES, who);
+  if (!rc) rc = check_workspace(workspace, workspace_bytes, 0, who);
   if (rc) return rc;
   MmParams P;
   memset(&P, 0, sizeof P);
@@ -1119,8 +1410,8 @@ extern "C" int polyq_fp4_ffn(const polyq_fp4* x, const polyq_fp4* gate, const po
     set_quant_out(P, hq);
   }
   P.status = (int*)workspace;
-  return x->format == POLYQ_FP4_NV ? run_fp4<kNv, true>(P, x, gate, up, stream, who)
-                                   : run_fp4<kMx, true>(P, x, gate, up, stream, who);
+  return x->format == POLYQ_FP4_NV ? run_fp4<kNv, true>(P, x, gate, up, workspace, stream, who)
+                                   : run_fp4<kMx, true>(P, x, gate, up, workspace, stream, who);
 }
 
 extern "C" int64_t polyq_ffn_saved_stride(int64_t F) { return (F + 7) / 8 * 8; }
@@ -1136,12 +1427,11 @@ extern "C" int polyq_ffn_forward(const polyq_dense* x, const polyq_dense* gate, 
   if (!rc) rc = check_operand(gate, K, x->type, who, "gate");
   if (!rc) rc = check_operand(up, K, x->type, who, "up");
   if (!rc) rc = check_16(h, F, x->type, who, "h");
-  if (!rc) rc = check_workspace(workspace, workspace_bytes, POLYQ_FP4_WORKSPACE_BYTES, who);
+  if (!rc) rc = check_workspace(workspace, workspace_bytes, 0, who);
   if (rc) return rc;
   if ((uintptr_t)saved % 16) return polyq_set_error(POLYQ_EINVAL, "%s: saved must be 16-byte aligned", who);
-  int dev = 0, sms = 0;
+  int dev = 0;
   rc = device_index(&dev, who);
-  if (!rc) rc = polyq_sm_count(&sms);
   if (rc) return rc;
   MmParams P;
   memset(&P, 0, sizeof P);
@@ -1159,18 +1449,18 @@ extern "C" int polyq_ffn_forward(const polyq_dense* x, const polyq_dense* gate, 
     P.saved_stride = polyq_ffn_saved_stride(F);
     P.saved[0] = saved;
     P.saved[1] = (uint16_t*)saved + T * P.saved_stride;
+    P.vec_saved = std::min(vec_rows(P.saved[0], P.saved_stride, x->type), vec_rows(P.saved[1], P.saved_stride, x->type));
   }
   P.status = (int*)workspace;
-  const bool bf16 = x->type == POLYQ_BF16, few = T <= kFewTokens;
-  const bool wide = !few && wide_tile(P, sms, true);
+  const bool bf16 = x->type == POLYQ_BF16, few = T <= kFewTokens / 2;
   const int nt = few_tile(T);
-  P.idesc = few ? idesc_16(kHalf, nt, bf16, false, false) : idesc_16(kTileM, wide ? 256 : 128, bf16, false, false);
+  P.idesc = few ? idesc_16(kHalf, nt, bf16, false, false) : idesc_16(kTileM, kTileN, bf16, false, false);
   rc = map_16(&P.a[0], x->data, x->stride, T, K, false, few ? nt : kHalf);
-  const int brows = few || wide ? 128 : 64;
-  if (!rc) rc = map_16(&P.b[0], gate->data, gate->stride, F, K, false, brows);
-  if (!rc) rc = map_16(&P.b[1], up->data, up->stride, F, K, false, brows);
+  if (!rc) rc = map_16(&P.b[0], gate->data, gate->stride, F, K, false, kHalf);
+  if (!rc) rc = map_16(&P.b[1], up->data, up->stride, F, K, false, kHalf);
   if (rc) return rc;
-  return few ? dispatch_few<k16, true>(P, dev, stream, who) : run_16<true>(P, wide, dev, stream, who);
+  return few ? dispatch_few<k16, true>(P, dev, stream, who)
+             : run_pair<Pair<k16, true>>(P, dev, workspace, stream, who);
 }
 
 extern "C" int polyq_ffn_backward_workspace_bytes(int64_t T, int64_t F, size_t* bytes) {
@@ -1178,8 +1468,9 @@ extern "C" int polyq_ffn_backward_workspace_bytes(int64_t T, int64_t F, size_t* 
   int rc = check_sizes(T, F, 1, "polyq_ffn_backward_workspace_bytes");
   if (rc) return rc;
   if (!bytes) return polyq_set_error(POLYQ_EINVAL, "polyq_ffn_backward_workspace_bytes: bytes is NULL");
-  *bytes = POLYQ_FP4_WORKSPACE_BYTES + (size_t)T * (size_t)polyq_ffn_saved_stride(F) * 4;
-  return POLYQ_OK;
+  rc = polyq_fp4_workspace_bytes(bytes);
+  if (!rc) *bytes += grad_bytes(T, F);
+  return rc;
 }
 
 extern "C" int polyq_ffn_backward(const polyq_dense* x, const polyq_dense* gate, const polyq_dense* up, int64_t T,
@@ -1188,15 +1479,13 @@ extern "C" int polyq_ffn_backward(const polyq_dense* x, const polyq_dense* gate,
                                   void* workspace, size_t workspace_bytes, void* stream) {
   polyq_clear_error();
   const char* who = "polyq_ffn_backward";
-  size_t need = 0;
   int rc = check_sizes(T, F, K, who);
   if (!rc) rc = polyq_check_dense(x, K, who, "x");
   if (!rc) rc = check_operand(x, K, x->type, who, "x");
   if (!rc) rc = check_operand(gate, K, x->type, who, "gate");
   if (!rc) rc = check_operand(up, K, x->type, who, "up");
   if (!rc) rc = check_16(dh, F, x->type, who, "dh");
-  if (!rc) rc = polyq_ffn_backward_workspace_bytes(T, F, &need);
-  if (!rc) rc = check_workspace(workspace, workspace_bytes, need, who);
+  if (!rc) rc = check_workspace(workspace, workspace_bytes, grad_bytes(T, F), who);
   if (rc) return rc;
   if (!saved || (uintptr_t)saved % 16)
     return polyq_set_error(POLYQ_EINVAL, "%s: saved must be given, 16-byte aligned", who);
@@ -1211,14 +1500,15 @@ extern "C" int polyq_ffn_backward(const polyq_dense* x, const polyq_dense* gate,
       return polyq_set_error(POLYQ_EINVAL, "%s: a gradient of type %d", who, d->type);
   if (dgate && (dgate->type != dup->type || dgate->stride != dup->stride))
     return polyq_set_error(POLYQ_EINVAL, "%s: dgate and dup must have one type and stride", who);
-  int dev = 0, sms = 0;
+  int dev = 0;
+  size_t head = 0;
   rc = device_index(&dev, who);
-  if (!rc) rc = polyq_sm_count(&sms);
+  if (!rc) rc = polyq_fp4_workspace_bytes(&head);
   if (rc) return rc;
 
   const bool bf16 = x->type == POLYQ_BF16;
   const int64_t fs = polyq_ffn_saved_stride(F);
-  uint16_t* da = (uint16_t*)((uint8_t*)workspace + POLYQ_FP4_WORKSPACE_BYTES);
+  uint16_t* da = (uint16_t*)((uint8_t*)workspace + head);
   uint16_t* du = da + T * fs;
   {
     ActParams A;
@@ -1255,13 +1545,12 @@ extern "C" int polyq_ffn_backward(const polyq_dense* x, const polyq_dense* gate,
     P.y_stride = dx->stride;
     P.type = dx->type;
     P.vec = vec_rows(dx);
-    const bool wide = wide_tile(P, sms, false);
-    P.idesc = idesc_16(kTileM, wide ? 256 : 128, bf16, false, true);
+    P.idesc = idesc_16(kTileM, kTileN, bf16, false, true);
     rc = map_16(&P.a[0], da, fs, T, F, false, kHalf);
     if (!rc) rc = map_16(&P.a[1], du, fs, T, F, false, kHalf);
     if (!rc) rc = map_16(&P.b[0], gate->data, gate->stride, F, K, true, 0);
     if (!rc) rc = map_16(&P.b[1], up->data, up->stride, F, K, true, 0);
-    if (!rc) rc = run_16<false>(P, wide, dev, stream, who);
+    if (!rc) rc = run_pair<Pair<k16, false>>(P, dev, workspace, stream, who);
     if (rc) return rc;
   }
   if (dgate) {
@@ -1277,14 +1566,13 @@ extern "C" int polyq_ffn_backward(const polyq_dense* x, const polyq_dense* gate,
     P.y[1] = dup->data;
     P.y_stride = dgate->stride;
     P.type = dgate->type;
-    P.vec = vec_rows(dgate) && vec_rows(dup);
-    const bool wide = wide_tile(P, sms, false);
-    P.idesc = idesc_16(kTileM, wide ? 256 : 128, bf16, true, true);
+    P.vec = std::min(vec_rows(dgate), vec_rows(dup));
+    P.idesc = idesc_16(kTileM, kTileN, bf16, true, true);
     rc = map_16(&P.a[0], da, fs, T, F, true, 0);
     if (!rc) rc = map_16(&P.a[1], du, fs, T, F, true, 0);
     if (!rc) rc = map_16(&P.b[0], x->data, x->stride, T, K, true, 0);
     P.b[1] = P.b[0];
-    if (!rc) rc = run_16<false>(P, wide, dev, stream, who);
+    if (!rc) rc = run_pair<Pair<k16, false>>(P, dev, workspace, stream, who);
   }
   return rc;
 }

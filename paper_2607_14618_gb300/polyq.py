@@ -99,7 +99,7 @@ class GemvPhase(C.Structure):
 
 
 FP4_MX, FP4_NV = 0, 1
-FP4_WORKSPACE_BYTES = 256
+FP4_WORKSPACE_ZERO = 16640  # leading workspace bytes that must start at zero
 T_F32, T_BF16, T_F16 = 0, 1, 2
 
 
@@ -160,6 +160,7 @@ _SIGS = {
     # include/polyq_fp4.h
     "polyq_fp4_bytes": (C.c_int, [C.c_int64, C.c_int64, C.c_int32, C.POINTER(C.c_int64),
                                   C.POINTER(C.c_int64)]),
+    "polyq_fp4_workspace_bytes": (C.c_int, [C.POINTER(C.c_size_t)]),
     "polyq_fp4_quantize": (C.c_int, [_DENSE, _FP4, _P]),
     "polyq_fp4_dequantize": (C.c_int, [_FP4, _DENSE, _P]),
     "polyq_fp4_linear": (C.c_int, [_FP4, _FP4, _DENSE, _DENSE, _P, C.c_size_t, _P]),
@@ -865,10 +866,18 @@ def fp4_tensor_scale(amax: float) -> float:
     return 2.0 ** max(-126, e - 1 if m == 0.5 else e)
 
 
-def fp4_workspace(device="cuda"):
-    """A zeroed workspace for fp4_linear, fp4_ffn and ffn_forward."""
+def _zero_headed(n, device):
     import torch
-    return torch.zeros(FP4_WORKSPACE_BYTES, dtype=torch.uint8, device=device)
+    ws = torch.empty(n.value, dtype=torch.uint8, device=device)
+    ws[:FP4_WORKSPACE_ZERO].zero_()
+    return ws
+
+
+def fp4_workspace(device="cuda"):
+    """A workspace for fp4_linear, fp4_ffn and ffn_forward on the current device."""
+    n = C.c_size_t()
+    _check(_lib.polyq_fp4_workspace_bytes(C.byref(n)))
+    return _zero_headed(n, device)
 
 
 def _workspace_at(workspace, dev, make):
@@ -958,13 +967,10 @@ def ffn_saved(T, F, dtype, device="cuda"):
 
 
 def ffn_workspace(T, F, K=None, device="cuda"):
-    """A zeroed workspace for ffn_forward and ffn_backward (K does not matter)."""
-    import torch
+    """A workspace for ffn_forward and ffn_backward (K does not matter)."""
     n = C.c_size_t()
     _check(_lib.polyq_ffn_backward_workspace_bytes(int(T), int(F), C.byref(n)))
-    ws = torch.empty(n.value, dtype=torch.uint8, device=device)
-    ws[:FP4_WORKSPACE_BYTES].zero_()
-    return ws
+    return _zero_headed(n, device)
 
 
 def _ffn_inputs(x, gate, up):
