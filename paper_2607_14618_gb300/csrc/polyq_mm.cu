@@ -272,7 +272,7 @@ struct Pair {
   // Tensor memory: two accumulators of 256 columns and SF stages' scales.  With
   // scales the accumulators share OV columns: the epilogue drains those first
   // and releases them for the next tile before the rest.
-  static constexpr int SF = 2;
+  static constexpr int SF = KIND == kNv ? 2 : 3;
   static constexpr int kSfStage = ATOMS * 4 * 3;
   static constexpr int kSfCols = (SF * kSfStage + 31) / 32 * 32;
   static constexpr int kSfCol = 512 - kSfCols;
@@ -290,7 +290,7 @@ constexpr int kEpiWarps = 12;
 // both operands through L2.
 struct Tiles {
   int g, g_hi, t;         // shared stages; next whole tile
-  int prob, tm, tn, lo, hi;
+  int tile, lo, hi, prob, tm, tn;
   int shared, parts, own; // of a part: its tile, the tile's parts, which one it is; else shared is -1
   // The first shared stage of pair b, and the pair that has shared stage x.
   static __device__ __forceinline__ int share_of(const MmParams& P, int b) {
@@ -317,7 +317,6 @@ struct Tiles {
   }
   __device__ __forceinline__ bool next(const MmParams& P) {
     const int n_it = P.segs * P.kt;
-    int tile;
     lo = 0;
     hi = n_it;
     shared = -1;
@@ -338,6 +337,11 @@ struct Tiles {
       tile = t;
       t += (int)(gridDim.x >> 1);
     }
+    return true;
+  }
+  // Where the piece's tile lies.  (Four divisions, 600 cycles of a lone thread:
+  // the MMA issuer does not need them, and the producer asks while its ring is full.)
+  __device__ __forceinline__ void place(const MmParams& P) {
     const int per = P.tiles_m * P.tiles_n;
     prob = tile / per;
     const int r = tile - prob * per;
@@ -345,7 +349,6 @@ struct Tiles {
     const int i = r - q * 8 * P.tiles_n;
     tn = i / rows;
     tm = 8 * q + (i - tn * rows);
-    return true;
   }
   // Where part p of the tile lies: a pair has two slots, the second for a tile
   // that its share did not begin in.
@@ -413,10 +416,12 @@ __global__ void __launch_bounds__(C::kThreads, 1) mm_pair(const __grid_constant_
       int s = 0;
       uint32_t ph = 1;
       const uint32_t full0 = mapa(smem_u32(&bar_full[0]), 0);
-      while (!s_abort && T.next(P)) {
-        const int m0 = T.tm * kTileM + (int)rank * kHalf;
-        const int n0 = C::GATED ? T.tn * kHalf : T.tn * kTileN + (int)rank * kHalf;
-        for (int i = T.lo; i < T.hi; ++i) {
+      bool more = T.next(P);
+      if (more) T.place(P);
+      while (more && !s_abort) {
+        const int m0 = T.tm * kTileM + (int)rank * kHalf, prob = T.prob, tn = T.tn, lo = T.lo, hi = T.hi;
+        const int n0 = C::GATED ? tn * kHalf : tn * kTileN + (int)rank * kHalf;
+        for (int i = lo; i < hi; ++i) {
           const int w = wait(smem_u32(&bar_empty[s]), ph, &s_abort);
           if (w != kOk) {
             if (w == kTimeout) fail(kStatusTimeoutEmpty);
@@ -427,7 +432,7 @@ __global__ void __launch_bounds__(C::kThreads, 1) mm_pair(const __grid_constant_
           const uint32_t bar = full0 + 8 * s;
           const uint32_t da = smem_u32(smem + s * kOpBytes);
           const uint32_t db = smem_u32(smem + C::kBOff + s * kOpBytes);
-          const CUtensorMap* ma = &P.a[C::GATED ? 0 : seg + T.prob];
+          const CUtensorMap* ma = &P.a[C::GATED ? 0 : seg + prob];
           const CUtensorMap* mb = &P.b[C::GATED ? (int)rank : seg];
           if (C::KIND == k16) {
             if (!P.a_mn) {
@@ -451,11 +456,15 @@ __global__ void __launch_bounds__(C::kThreads, 1) mm_pair(const __grid_constant_
 #pragma unroll
             for (int j = 0; j < 2; ++j)
               tma_load_2d_pair(sb + j * C::ATOMS * 512, &P.sb[C::GATED ? j : 0], 0,
-                               (C::GATED ? T.tn : T.tn * 2 + j) * P.atoms + kt * C::ATOMS, bar);
+                               (C::GATED ? tn : tn * 2 + j) * P.atoms + kt * C::ATOMS, bar);
           }
           if (++s == C::STAGES) {
             s = 0;
             ph ^= 1u;
+          }
+          if (i == lo) {
+            more = T.next(P);
+            if (more) T.place(P);
           }
         }
       }
@@ -466,6 +475,7 @@ __global__ void __launch_bounds__(C::kThreads, 1) mm_pair(const __grid_constant_
       int s = 0, tc = 0;
       bool ready = false;            // stage s is known to have landed
       int sf = 0, so = 0, held = 0;  // scales: next slot; the oldest stage in use, and how many are
+      int freed = 0;                 // and how many of them were found done
       uint32_t ph = 0, so_ph = 0;
       const uint64_t a0 = desc_sw128(smem_u32(smem), P.a_mn ? 8192 : 16);
       const uint64_t b0 = desc_sw128(smem_u32(smem + C::kBOff), P.b_mn ? 8192 : 16);
@@ -509,7 +519,11 @@ __global__ void __launch_bounds__(C::kThreads, 1) mm_pair(const __grid_constant_
               so_ph ^= 1u;
             }
           };
-          if (C::KIND != k16) release(min(held, poll_ahead<2, C::STAGES>(smem_u32(&bar_empty[0]), so, so_ph)));
+          if (C::KIND != k16) {
+            if (C::SF > 2) release(freed);  // asked for a stage ago: the answer is not waited for
+            freed = min(held, poll_ahead<2, C::STAGES>(smem_u32(&bar_empty[0]), so, so_ph));
+            if (C::SF == 2) release(freed);
+          }
           const int kt = i >= P.kt ? i - P.kt : i;
           const int n_mma = kt == P.kt - 1 ? P.k_last : 4;
           const uint64_t a = a0 + (uint64_t)((s * kOpBytes) >> 4), b = b0 + (uint64_t)((s * kOpBytes) >> 4);
@@ -526,6 +540,7 @@ __global__ void __launch_bounds__(C::kThreads, 1) mm_pair(const __grid_constant_
                 break;
               }
               release(1);
+              freed = 0;
             }
             const uint32_t c0 = tmem + C::kSfCol + sf * C::kSfStage;
 #pragma unroll
@@ -568,6 +583,7 @@ __global__ void __launch_bounds__(C::kThreads, 1) mm_pair(const __grid_constant_
     constexpr int kOvChunks = C::OV / 32;
     pdl_wait();
     for (int tc = 0; !s_abort && T.next(P); ++tc) {
+      T.place(P);
       const int buf = tc & 1;
       const int64_t m = (int64_t)T.tm * kTileM + (int)rank * kHalf + 32 * q;  // the warp's first row
       const int n0 = C::GATED ? T.tn * kHalf : T.tn * kTileN;

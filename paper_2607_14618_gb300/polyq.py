@@ -750,13 +750,23 @@ def _type_of(dtype):
     return _T.get(dtype)
 
 
-def _current(index, name):
-    """Raises unless CUDA device `index` is the current one (the stream and the
-    library's per-device state are looked up for that)."""
-    import torch
-    cur = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)()  # private: may lack
-    if index != cur:
-        raise ValueError(f"{name} is on cuda:{index}, not on the current device cuda:{cur}")
+_calls = []  # the current device's index, a device's current stream; filled by the first use
+
+
+def _stream_on(dev, name, stream):
+    """The cudaStream_t of `stream` (default: the current one).  Raises unless
+    CUDA device `dev`, on which `name` lies, is the current one: the stream and
+    the library's per-device state are looked up for that."""
+    if not _calls:
+        import torch
+        c = torch._C  # private calls, which a torch may lack
+        _calls[:] = (getattr(c, "_cuda_getDevice", torch.cuda.current_device),
+                     getattr(c, "_cuda_getCurrentRawStream",
+                             lambda d: torch.cuda.current_stream(d).cuda_stream))
+    cur = _calls[0]()
+    if dev != cur:
+        raise ValueError(f"{name} is on cuda:{dev}, not on the current device cuda:{cur}")
+    return _calls[1](dev) if stream is None else stream.cuda_stream
 
 
 def _dense(t, name, rows=None, cols=None, dev=None, dtype=None):
@@ -896,13 +906,13 @@ def fp4_quantize(x, format=FP4_MX, tensor_scale=1.0, out=None, stream=None):
     its format and tensor scale are used."""
     d = _dense(x, "x")
     dev = x.get_device()
-    _current(dev, "x")
+    st = _stream_on(dev, "x", stream)
     if out is None:
         out = Fp4Tensor.empty(x.shape[0], x.shape[1], format, tensor_scale, x.device)
     o = _fp4(out, "out", dev)
     if (out.rows, out.K) != x.shape:
         raise ValueError(f"out is [{out.rows}][{out.K}], x {list(x.shape)}")
-    _check(_lib.polyq_fp4_quantize(C.byref(d), o, _stream_ptr(stream)))
+    _check(_lib.polyq_fp4_quantize(C.byref(d), o, st))
     return out
 
 
@@ -910,12 +920,12 @@ def fp4_dequantize(t: Fp4Tensor, dtype=None, out=None, stream=None):
     """The values of a 4-bit tensor (default fp32)."""
     p = _fp4(t, "t")
     dev = t.device_index
-    _current(dev, "t")
+    st = _stream_on(dev, "t", stream)
     if out is None:
         import torch
         out = torch.empty((t.rows, t.K), dtype=dtype or torch.float32, device=t.codes.device)
     d = _dense(out, "out", t.rows, t.K, dev, dtype)
-    _check(_lib.polyq_fp4_dequantize(p, C.byref(d), _stream_ptr(stream)))
+    _check(_lib.polyq_fp4_dequantize(p, C.byref(d), st))
     return out
 
 
@@ -927,7 +937,7 @@ def fp4_linear(x: Fp4Tensor, w: Fp4Tensor, y=None, residual=None, dtype=None, wo
     px = _fp4(x, "x")
     dev = x.device_index
     pw = _fp4(w, "w", dev)
-    _current(dev, "x")
+    st = _stream_on(dev, "x", stream)
     if y is None:
         import torch
         y = torch.empty((x.rows, w.rows), dtype=dtype or (residual.dtype if residual is not None
@@ -935,7 +945,7 @@ def fp4_linear(x: Fp4Tensor, w: Fp4Tensor, y=None, residual=None, dtype=None, wo
     dy = _dense(y, "y", x.rows, w.rows, dev, dtype)
     dr = None if residual is None else C.byref(_dense(residual, "residual", x.rows, w.rows, dev, y.dtype))
     ws = _workspace_at(workspace, dev, lambda: fp4_workspace(x.codes.device))
-    _check(_lib.polyq_fp4_linear(px, pw, dr, C.byref(dy), ws.data_ptr(), ws.numel(), _stream_ptr(stream)))
+    _check(_lib.polyq_fp4_linear(px, pw, dr, C.byref(dy), ws.data_ptr(), ws.numel(), st))
     return y
 
 
@@ -946,7 +956,7 @@ def fp4_ffn(x: Fp4Tensor, gate: Fp4Tensor, up: Fp4Tensor, h=None, dtype=None, wo
     px = _fp4(x, "x")
     dev = x.device_index
     pg, pu = _fp4(gate, "gate", dev), _fp4(up, "up", dev)
-    _current(dev, "x")
+    st = _stream_on(dev, "x", stream)
     if h is None:
         import torch
         h = torch.empty((x.rows, gate.rows), dtype=dtype or torch.bfloat16, device=x.codes.device)
@@ -956,7 +966,7 @@ def fp4_ffn(x: Fp4Tensor, gate: Fp4Tensor, up: Fp4Tensor, h=None, dtype=None, wo
     else:
         dh = C.byref(_dense(h, "h", x.rows, gate.rows, dev, dtype))
     ws = _workspace_at(workspace, dev, lambda: fp4_workspace(x.codes.device))
-    _check(_lib.polyq_fp4_ffn(px, pg, pu, dh, dq, ws.data_ptr(), ws.numel(), _stream_ptr(stream)))
+    _check(_lib.polyq_fp4_ffn(px, pg, pu, dh, dq, ws.data_ptr(), ws.numel(), st))
     return h
 
 
@@ -973,14 +983,14 @@ def ffn_workspace(T, F, K=None, device="cuda"):
     return _zero_headed(n, device)
 
 
-def _ffn_inputs(x, gate, up):
+def _ffn_inputs(x, gate, up, stream):
     dx = _dense(x, "x")
     dev = x.get_device()
-    _current(dev, "x")
+    st = _stream_on(dev, "x", stream)
     T, K = x.shape
     dg = _dense(gate, "gate", None, K, dev, x.dtype)
     F = gate.shape[0]
-    return dx, dg, _dense(up, "up", F, K, dev, x.dtype), T, F, K, dev
+    return dx, dg, _dense(up, "up", F, K, dev, x.dtype), T, F, K, dev, st
 
 
 def _saved(saved, x, T, F, dev):
@@ -993,7 +1003,7 @@ def _saved(saved, x, T, F, dev):
 def ffn_forward(x, gate, up, h=None, saved=None, workspace=None, stream=None):
     """h = silu(x gate^T) * (x up^T) on bf16 or fp16 operands, one kernel.
     `saved` (ffn_saved) receives what ffn_backward needs."""
-    ix, ig, iu, T, F, K, dev = _ffn_inputs(x, gate, up)
+    ix, ig, iu, T, F, K, dev, st = _ffn_inputs(x, gate, up, stream)
     if h is None:
         import torch
         h = torch.empty((T, F), dtype=x.dtype, device=x.device)
@@ -1001,7 +1011,7 @@ def ffn_forward(x, gate, up, h=None, saved=None, workspace=None, stream=None):
     ps = None if saved is None else _saved(saved, x, T, F, dev)
     ws = _workspace_at(workspace, dev, lambda: fp4_workspace(x.device))
     _check(_lib.polyq_ffn_forward(C.byref(ix), C.byref(ig), C.byref(iu), T, F, K, C.byref(ih), ps,
-                                  ws.data_ptr(), ws.numel(), _stream_ptr(stream)))
+                                  ws.data_ptr(), ws.numel(), st))
     return h
 
 
@@ -1010,7 +1020,7 @@ def ffn_backward(x, gate, up, saved, dh, dx=None, dgate=None, dup=None, need_dx=
     """Gradients (dx, dgate, dup) of ffn_forward for the gradient dh of h; each
     of x's type or, where a buffer of that type is passed, fp32.  Those not
     needed are None."""
-    ix, ig, iu, T, F, K, dev = _ffn_inputs(x, gate, up)
+    ix, ig, iu, T, F, K, dev, st = _ffn_inputs(x, gate, up, stream)
     ty = x.dtype
     idh = _dense(dh, "dh", T, F, dev, ty)
     ps = _saved(saved, x, T, F, dev)
@@ -1029,5 +1039,5 @@ def ffn_backward(x, gate, up, saved, dh, dx=None, dgate=None, dup=None, need_dx=
             ((dx, "dx", T), (dgate, "dgate", F), (dup, "dup", F))]
     ws = _workspace_at(workspace, dev, lambda: ffn_workspace(T, F, K, x.device))
     _check(_lib.polyq_ffn_backward(C.byref(ix), C.byref(ig), C.byref(iu), T, F, K, ps, C.byref(idh),
-                                   *outs, ws.data_ptr(), ws.numel(), _stream_ptr(stream)))
+                                   *outs, ws.data_ptr(), ws.numel(), st))
     return dx, dgate, dup
