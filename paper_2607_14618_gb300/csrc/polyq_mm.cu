@@ -66,12 +66,12 @@ struct MmParams {
   void* y[2];
   const void* res;
   int64_t y_stride, res_stride;
-  int type, vec, vec_saved;  // vec: rows of y and res start on 16 bytes (1), y's on 32 (2)
+  int type, vec;           // vec: rows of y and res start on 16 bytes (1), y's on 32 (2)
   uint8_t *codes, *scales;
   int64_t code_stride, out_atoms;
   int qfmt;                // 0, kMx or kNv
   float g, inv_g;
-  void* saved[2];
+  uint8_t* saved;          // see save_row32
   int64_t saved_stride;
   int* status;
 };
@@ -102,11 +102,6 @@ __device__ __forceinline__ void store_dense(void* p, int64_t i, float v, int typ
   else if (type == POLYQ_BF16) ((__nv_bfloat16*)p)[i] = __float2bfloat16_rn(v);
   else ((__half*)p)[i] = __float2half_rn(v);
 }
-// fp16 keeps a saved finite value finite.
-__device__ __forceinline__ float saved_range(float v, bool bf16) {
-  return bf16 || fabsf(v) == INFINITY ? v : v > 65504.f ? 65504.f : v < -65504.f ? -65504.f : v;
-}
-
 // Rows that start on 32 (vec = 2) or 16 bytes (1): a lane holds 32 consecutive
 // values of its row and stores, or adds from the residual, whole sectors.
 __device__ __forceinline__ void store32(void* p, const uint32_t (&w)[8]) {
@@ -173,6 +168,34 @@ __device__ __forceinline__ void add_row32(const void* r, int64_t off, float (&v)
     }
   }
 }
+// The values of gate and up that the backward pass needs are saved as the upper
+// 24 bits of their fp32 (16 significant bits, off by at most 2^-15 of the value,
+// and fp32's range): with 16-bit types their rounding was most of the
+// gradients' error (relative 0.0030, now 0.0024, where rounding the plain form's
+// result once gives 0.0017).  Four planes of M rows of `stride` elements: the
+// upper 16 bits of gate and of up, the next 8 of gate and of up; `which` is 0 for
+// gate.  Rows are padded to 32 elements, so whole chunks of 32 always fit.
+__device__ __forceinline__ uint8_t* saved_hi(const MmParams& P, int which, int64_t i) {
+  return P.saved + 2 * ((int64_t)which * P.M * P.saved_stride + i);
+}
+__device__ __forceinline__ uint8_t* saved_lo(const MmParams& P, int which, int64_t i) {
+  return P.saved + (4 + which) * (int64_t)P.M * P.saved_stride + i;
+}
+__device__ __forceinline__ void save_row32(const MmParams& P, int which, int64_t m, int n, const uint32_t (&v)[32]) {
+  const int64_t at = m * P.saved_stride + n;
+  uint32_t w[8];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) w[i] = __byte_perm(v[16 * h + 2 * i], v[16 * h + 2 * i + 1], 0x7632);
+    store32(saved_hi(P, which, at + 16 * h), w);
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+    w[i] = __byte_perm(__byte_perm(v[4 * i], v[4 * i + 1], 0x0051), __byte_perm(v[4 * i + 2], v[4 * i + 3], 0x0051), 0x5410);
+  store32(saved_lo(P, which, at), w);
+}
+
 // The warp's 32 x 32 values transposed: v[r] of lane c becomes v[c] of lane r.
 __device__ __forceinline__ void transpose32(float (&v)[32]) {
   const int lane = threadIdx.x & 31;
@@ -606,15 +629,11 @@ __global__ void __launch_bounds__(C::kThreads, 1) mm_pair(const __grid_constant_
         const int n = n0 + 32 * c;
         float v[32];
         if constexpr (C::GATED) {
-          if (P.saved[0]) {
-            const bool bf = P.type == POLYQ_BF16;
-#pragma unroll
-            for (int j = 0; j < 32; ++j) v[j] = saved_range(__uint_as_float(r0[j]), bf);
-            store_chunk(P.saved[0], P.saved_stride, nullptr, 0, m, n, P.M, P.N, v, P.type, P.vec_saved);
-#pragma unroll
-            for (int j = 0; j < 32; ++j) v[j] = saved_range(__uint_as_float(r1[j]), bf);
-            store_chunk(P.saved[1], P.saved_stride, nullptr, 0, m, n, P.M, P.N, v, P.type, P.vec_saved);
+          if (P.saved && m + lane < P.M && n < P.N) {
+            save_row32(P, 0, m + lane, n, r0);
+            save_row32(P, 1, m + lane, n, r1);
           }
+          __syncwarp();
 #pragma unroll
           for (int j = 0; j < 32; ++j)
             v[j] = silu(__uint_as_float(r0[j]) * P.alpha[0]) * (__uint_as_float(r1[j]) * P.alpha[1]);
@@ -974,9 +993,13 @@ __global__ void __launch_bounds__(C::kThreads, 1) mm_few(const __grid_constant__
       float v = vs[i] * P.alpha[0];
       if constexpr (C::GATED) {
         const float u = us[i] * P.alpha[1];
-        if (P.saved[0] && n < P.N) {
-          store_dense(P.saved[0], m * P.saved_stride + n, saved_range(v, P.type == POLYQ_BF16), P.type);
-          store_dense(P.saved[1], m * P.saved_stride + n, saved_range(u, P.type == POLYQ_BF16), P.type);
+        if (P.saved && n < P.N) {
+          const int64_t at = m * P.saved_stride + n;
+          const uint32_t a = __float_as_uint(v), b = __float_as_uint(u);
+          *reinterpret_cast<uint16_t*>(saved_hi(P, 0, at)) = (uint16_t)(a >> 16);
+          *reinterpret_cast<uint16_t*>(saved_hi(P, 1, at)) = (uint16_t)(b >> 16);
+          *saved_lo(P, 0, at) = (uint8_t)(a >> 8);
+          *saved_lo(P, 1, at) = (uint8_t)(b >> 8);
         }
         v = silu(v) * u;
         if (P.qfmt) {
@@ -1028,7 +1051,8 @@ __global__ void __launch_bounds__(C::kThreads, 1) mm_few(const __grid_constant__
 // da = dh u s (1 + a (1 - s)), du = dh a s with s = 1 / (1 + exp(-a)); 8
 // elements a thread.  One pass over a, u, dh; bound by HBM.
 struct ActParams {
-  const void *a, *u, *dh;
+  const uint8_t* saved;  // save_row32's planes
+  const void* dh;
   void *da, *du;
   int64_t T, F, stride, dh_stride, items;  // stride: of a, u, da, du
   int vec;                                 // rows of dh start on 16 bytes
@@ -1037,46 +1061,52 @@ template <bool BF16>
 __global__ void __launch_bounds__(256) act_backward(const __grid_constant__ ActParams P) {
   pdl_trigger();
   pdl_wait();
-  const int64_t per = P.stride / 8;
+  const int64_t per = P.stride / 8, plane = P.T * P.stride;
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < P.items; i += (int64_t)gridDim.x * 256) {
     const int64_t t = i / per, f = (i - t * per) * 8;
     if (f >= P.F) continue;
-    uint32_t a[4], u[4], d[4], da[4], du[4];
-    const uint4 av = *reinterpret_cast<const uint4*>((const uint16_t*)P.a + t * P.stride + f);
-    const uint4 uv = *reinterpret_cast<const uint4*>((const uint16_t*)P.u + t * P.stride + f);
-    a[0] = av.x, a[1] = av.y, a[2] = av.z, a[3] = av.w;
-    u[0] = uv.x, u[1] = uv.y, u[2] = uv.z, u[3] = uv.w;
+    const int64_t at = t * P.stride + f;
+    uint4 hi[2];
+    uint2 lo[2];
+#pragma unroll
+    for (int w = 0; w < 2; ++w) {
+      hi[w] = __ldg(reinterpret_cast<const uint4*>(P.saved + 2 * (w * plane + at)));
+      lo[w] = __ldg(reinterpret_cast<const uint2*>(P.saved + (4 + w) * plane + at));
+    }
+    uint32_t d[4], da[4], du[4];
     const uint16_t* dr = (const uint16_t*)P.dh + t * P.dh_stride + f;
     const int n = (int)(P.F - f < 8 ? P.F - f : 8);
     if (P.vec && n == 8) {
-      const uint4 dv = *reinterpret_cast<const uint4*>(dr);
+      const uint4 dv = __ldg(reinterpret_cast<const uint4*>(dr));
       d[0] = dv.x, d[1] = dv.y, d[2] = dv.z, d[3] = dv.w;
     } else {
 #pragma unroll
       for (int j = 0; j < 4; ++j)
         d[j] = (2 * j < n ? dr[2 * j] : 0u) | (uint32_t)(2 * j + 1 < n ? dr[2 * j + 1] : 0u) << 16;
     }
-    auto get = [](uint32_t w) {
-      if (BF16) return make_float2(bf16_lo(w), bf16_hi(w));
-      return __half22float2(*reinterpret_cast<const __half2*>(&w));
+    auto value = [](const uint4& h, const uint2& l, int j) {  // element j of the eight
+      const uint32_t hw = j < 2 ? h.x : j < 4 ? h.y : j < 6 ? h.z : h.w, lw = j < 4 ? l.x : l.y;
+      // bytes: 0, the low byte, the two high bytes
+      return __uint_as_float(__byte_perm(hw, __byte_perm(lw, 0, 0x4440 | (j & 3)), j & 1 ? 0x3245 : 0x1045));
+    };
+    auto grad = [](float x, float y, float g, float& ga, float& gu) {
+      const float s = __fdividef(1.f, 1.f + __expf(-x)), xs = x * s;
+      gu = g * xs;
+      ga = g * y * (s + xs * (1.f - s));
     };
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const float2 x = get(a[j]), y = get(u[j]), g = get(d[j]);
-      auto grad = [](float x, float y, float g, float& ga, float& gu) {
-        const float s = __fdividef(1.f, 1.f + __expf(-x)), xs = x * s;
-        gu = g * xs;
-        ga = g * y * (s + xs * (1.f - s));
-      };
-      float2 ga, gu;
-      grad(x.x, y.x, g.x, ga.x, gu.x);
-      grad(x.y, y.y, g.y, ga.y, gu.y);
+      float2 g, ga, gu;
+      if (BF16) g = make_float2(bf16_lo(d[j]), bf16_hi(d[j]));
+      else g = __half22float2(*reinterpret_cast<const __half2*>(&d[j]));
+      grad(value(hi[0], lo[0], 2 * j), value(hi[1], lo[1], 2 * j), g.x, ga.x, gu.x);
+      grad(value(hi[0], lo[0], 2 * j + 1), value(hi[1], lo[1], 2 * j + 1), g.y, ga.y, gu.y);
       da[j] = pack16(ga.x, ga.y, BF16);
       du[j] = pack16(gu.x, gu.y, BF16);
     }
     // columns past F of a row's last 8 are padding that nothing reads
-    *reinterpret_cast<uint4*>((uint16_t*)P.da + t * P.stride + f) = make_uint4(da[0], da[1], da[2], da[3]);
-    *reinterpret_cast<uint4*>((uint16_t*)P.du + t * P.stride + f) = make_uint4(du[0], du[1], du[2], du[3]);
+    *reinterpret_cast<uint4*>((uint16_t*)P.da + at) = make_uint4(da[0], da[1], da[2], da[3]);
+    *reinterpret_cast<uint4*>((uint16_t*)P.du + at) = make_uint4(du[0], du[1], du[2], du[3]);
   }
 }
 
@@ -1350,8 +1380,10 @@ int check_operand(const polyq_dense* d, int64_t cols, int type, const char* who,
     return polyq_set_error(POLYQ_EINVAL, "%s: %s: rows must start on 16 bytes (address and stride)", who, what);
   return POLYQ_OK;
 }
-// Bytes of the gradients of a and u.
-size_t grad_bytes(int64_t T, int64_t F) { return (size_t)T * (size_t)polyq_ffn_saved_stride(F) * 4; }
+// Row length of the saved values and of the gradients of a and u, and the bytes
+// of the latter.
+int64_t saved_stride(int64_t F) { return (F + 31) / 32 * 32; }
+size_t grad_bytes(int64_t T, int64_t F) { return (size_t)T * (size_t)saved_stride(F) * 4; }
 int check_sizes(int64_t T, int64_t F, int64_t K, const char* who) {
   if (T < 1 || F < 1 || K < 1 || T > (1 << 24) || F > (1 << 24) || K > (1 << 24))
     return polyq_set_error(POLYQ_EINVAL, "%s: T=%lld F=%lld K=%lld", who, (long long)T, (long long)F, (long long)K);
@@ -1430,7 +1462,14 @@ extern "C" int polyq_fp4_ffn(const polyq_fp4* x, const polyq_fp4* gate, const po
                                    : run_fp4<kMx, true>(P, x, gate, up, workspace, stream, who);
 }
 
-extern "C" int64_t polyq_ffn_saved_stride(int64_t F) { return (F + 7) / 8 * 8; }
+extern "C" int polyq_ffn_saved_bytes(int64_t T, int64_t F, size_t* bytes) {
+  polyq_clear_error();
+  const int rc = check_sizes(T, F, 1, "polyq_ffn_saved_bytes");
+  if (rc) return rc;
+  if (!bytes) return polyq_set_error(POLYQ_EINVAL, "polyq_ffn_saved_bytes: bytes is NULL");
+  *bytes = (size_t)T * (size_t)saved_stride(F) * 6;
+  return POLYQ_OK;
+}
 
 extern "C" int polyq_ffn_forward(const polyq_dense* x, const polyq_dense* gate, const polyq_dense* up, int64_t T,
                                  int64_t F, int64_t K, const polyq_dense* h, void* saved, void* workspace,
@@ -1445,7 +1484,7 @@ extern "C" int polyq_ffn_forward(const polyq_dense* x, const polyq_dense* gate, 
   if (!rc) rc = check_16(h, F, x->type, who, "h");
   if (!rc) rc = check_workspace(workspace, workspace_bytes, 0, who);
   if (rc) return rc;
-  if ((uintptr_t)saved % 16) return polyq_set_error(POLYQ_EINVAL, "%s: saved must be 16-byte aligned", who);
+  if ((uintptr_t)saved % 32) return polyq_set_error(POLYQ_EINVAL, "%s: saved must be 32-byte aligned", who);
   int dev = 0;
   rc = device_index(&dev, who);
   if (rc) return rc;
@@ -1461,12 +1500,8 @@ extern "C" int polyq_ffn_forward(const polyq_dense* x, const polyq_dense* gate, 
   P.y_stride = h->stride;
   P.type = h->type;
   P.vec = vec_rows(h);
-  if (saved) {
-    P.saved_stride = polyq_ffn_saved_stride(F);
-    P.saved[0] = saved;
-    P.saved[1] = (uint16_t*)saved + T * P.saved_stride;
-    P.vec_saved = std::min(vec_rows(P.saved[0], P.saved_stride, x->type), vec_rows(P.saved[1], P.saved_stride, x->type));
-  }
+  P.saved = (uint8_t*)saved;
+  P.saved_stride = saved_stride(F);
   P.status = (int*)workspace;
   const bool bf16 = x->type == POLYQ_BF16, few = T <= kFewTokens / 2;
   const int nt = few_tile(T);
@@ -1503,8 +1538,8 @@ extern "C" int polyq_ffn_backward(const polyq_dense* x, const polyq_dense* gate,
   if (!rc) rc = check_16(dh, F, x->type, who, "dh");
   if (!rc) rc = check_workspace(workspace, workspace_bytes, grad_bytes(T, F), who);
   if (rc) return rc;
-  if (!saved || (uintptr_t)saved % 16)
-    return polyq_set_error(POLYQ_EINVAL, "%s: saved must be given, 16-byte aligned", who);
+  if (!saved || (uintptr_t)saved % 32)
+    return polyq_set_error(POLYQ_EINVAL, "%s: saved must be given, 32-byte aligned", who);
   if (!dgate != !dup || (!dx && !dgate))
     return polyq_set_error(POLYQ_EINVAL, "%s: dx, or dgate and dup, or all three are wanted", who);
   if (dx) rc = polyq_check_dense(dx, K, who, "dx");
@@ -1523,13 +1558,12 @@ extern "C" int polyq_ffn_backward(const polyq_dense* x, const polyq_dense* gate,
   if (rc) return rc;
 
   const bool bf16 = x->type == POLYQ_BF16;
-  const int64_t fs = polyq_ffn_saved_stride(F);
+  const int64_t fs = saved_stride(F);
   uint16_t* da = (uint16_t*)((uint8_t*)workspace + head);
   uint16_t* du = da + T * fs;
   {
     ActParams A;
-    A.a = saved;
-    A.u = (const uint16_t*)saved + T * fs;
+    A.saved = (const uint8_t*)saved;
     A.dh = dh->data;
     A.da = da;
     A.du = du;

@@ -165,7 +165,7 @@ _SIGS = {
     "polyq_fp4_dequantize": (C.c_int, [_FP4, _DENSE, _P]),
     "polyq_fp4_linear": (C.c_int, [_FP4, _FP4, _DENSE, _DENSE, _P, C.c_size_t, _P]),
     "polyq_fp4_ffn": (C.c_int, [_FP4, _FP4, _FP4, _DENSE, _FP4, _P, C.c_size_t, _P]),
-    "polyq_ffn_saved_stride": (C.c_int64, [C.c_int64]),
+    "polyq_ffn_saved_bytes": (C.c_int, [C.c_int64, C.c_int64, C.POINTER(C.c_size_t)]),
     "polyq_ffn_forward": (C.c_int, [_DENSE, _DENSE, _DENSE, C.c_int64, C.c_int64, C.c_int64,
                                     _DENSE, _P, _P, C.c_size_t, _P]),
     "polyq_ffn_backward_workspace_bytes": (C.c_int, [C.c_int64, C.c_int64,
@@ -970,10 +970,17 @@ def fp4_ffn(x: Fp4Tensor, gate: Fp4Tensor, up: Fp4Tensor, h=None, dtype=None, wo
     return h
 
 
-def ffn_saved(T, F, dtype, device="cuda"):
-    """The buffer that ffn_forward fills for ffn_backward."""
+def _saved_bytes(T, F):
+    n = C.c_size_t()
+    _check(_lib.polyq_ffn_saved_bytes(int(T), int(F), C.byref(n)))
+    return n.value
+
+
+def ffn_saved(T, F, dtype=None, device="cuda"):
+    """The buffer that ffn_forward fills for ffn_backward (the same for every
+    dtype of the operands)."""
     import torch
-    return torch.empty((2, T, _lib.polyq_ffn_saved_stride(F)), dtype=dtype, device=device)
+    return torch.empty(_saved_bytes(T, F), dtype=torch.uint8, device=device)
 
 
 def ffn_workspace(T, F, K=None, device="cuda"):
@@ -993,10 +1000,10 @@ def _ffn_inputs(x, gate, up, stream):
     return dx, dg, _dense(up, "up", F, K, dev, x.dtype), T, F, K, dev, st
 
 
-def _saved(saved, x, T, F, dev):
-    if (saved.dtype != x.dtype or saved.get_device() != dev or not saved.is_contiguous()
-            or saved.shape != (2, T, _lib.polyq_ffn_saved_stride(F))):
-        raise ValueError(f"saved must be ffn_saved({T}, {F}, {x.dtype}) on cuda:{dev}")
+def _saved(saved, T, F, dev):
+    if (saved.element_size() != 1 or saved.get_device() != dev or not saved.is_contiguous()
+            or saved.numel() != _saved_bytes(T, F)):
+        raise ValueError(f"saved must be ffn_saved({T}, {F}) on cuda:{dev}")
     return saved.data_ptr()
 
 
@@ -1008,7 +1015,7 @@ def ffn_forward(x, gate, up, h=None, saved=None, workspace=None, stream=None):
         import torch
         h = torch.empty((T, F), dtype=x.dtype, device=x.device)
     ih = _dense(h, "h", T, F, dev, x.dtype)
-    ps = None if saved is None else _saved(saved, x, T, F, dev)
+    ps = None if saved is None else _saved(saved, T, F, dev)
     ws = _workspace_at(workspace, dev, lambda: fp4_workspace(x.device))
     _check(_lib.polyq_ffn_forward(C.byref(ix), C.byref(ig), C.byref(iu), T, F, K, C.byref(ih), ps,
                                   ws.data_ptr(), ws.numel(), st))
@@ -1023,7 +1030,7 @@ def ffn_backward(x, gate, up, saved, dh, dx=None, dgate=None, dup=None, need_dx=
     ix, ig, iu, T, F, K, dev, st = _ffn_inputs(x, gate, up, stream)
     ty = x.dtype
     idh = _dense(dh, "dh", T, F, dev, ty)
-    ps = _saved(saved, x, T, F, dev)
+    ps = _saved(saved, T, F, dev)
 
     def new(n, like):
         import torch
