@@ -789,6 +789,57 @@ struct Few {
   static_assert(MATS * NT * kHalf * 4 <= STAGES * kStage && STAGES >= SF && kCols <= 512, "parts where the stages were");
 };
 
+// A lane's four consecutive values of an output row.
+__device__ __forceinline__ void store4(void* y, int64_t i, const float (&v)[4], int type) {
+  if (type == POLYQ_F32) *reinterpret_cast<float4*>((float*)y + i) = make_float4(v[0], v[1], v[2], v[3]);
+  else *reinterpret_cast<uint2*>((uint16_t*)y + i) =
+      make_uint2(pack16(v[0], v[1], type == POLYQ_BF16), pack16(v[2], v[3], type == POLYQ_BF16));
+}
+__device__ __forceinline__ void add4(const void* r, int64_t i, float (&v)[4], int type) {
+  if (type == POLYQ_F32) {
+    const float4 f = *reinterpret_cast<const float4*>((const float*)r + i);
+    v[0] += f.x, v[1] += f.y, v[2] += f.z, v[3] += f.w;
+  } else {
+    const uint2 w = *reinterpret_cast<const uint2*>((const uint16_t*)r + i);
+    if (type == POLYQ_BF16) {
+      v[0] += bf16_lo(w.x), v[1] += bf16_hi(w.x), v[2] += bf16_lo(w.y), v[3] += bf16_hi(w.y);
+    } else {
+      const float2 a = __half22float2(*reinterpret_cast<const __half2*>(&w.x));
+      const float2 b = __half22float2(*reinterpret_cast<const __half2*>(&w.y));
+      v[0] += a.x, v[1] += a.y, v[2] += b.x, v[3] += b.y;
+    }
+  }
+}
+__device__ __forceinline__ void save4(const MmParams& P, int which, int64_t at, const float (&v)[4]) {
+  uint32_t w[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) w[e] = __float_as_uint(v[e]);
+  *reinterpret_cast<uint2*>(saved_hi(P, which, at)) =
+      make_uint2(__byte_perm(w[0], w[1], 0x7632), __byte_perm(w[2], w[3], 0x7632));
+  *reinterpret_cast<uint32_t*>(saved_lo(P, which, at)) =
+      __byte_perm(__byte_perm(w[0], w[1], 0x0051), __byte_perm(w[2], w[3], 0x0051), 0x5410);
+}
+// In 4 bits: a block is eight (MX) or four (NV) neighbouring lanes.  The whole
+// warp calls; values past the row's end count as 0.
+template <bool NV>
+__device__ __forceinline__ void store_codes4(const MmParams& P, int64_t m, int n, const float (&v)[4]) {
+  constexpr int BL = NV ? 16 : 32;
+  float t[8] = {};
+  uint32_t mx = 0;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    t[e] = n + e < P.N ? v[e] : 0.f;
+    if (NV) t[e] = P.inv_g != 0.f ? t[e] * P.inv_g : __fdiv_rn(t[e], P.g);
+    mx = max(mx, __float_as_uint(t[e]) & 0x7FFFFFFFu);
+  }
+#pragma unroll
+  for (int d = 1; d < BL / 4; d *= 2) mx = max(mx, __shfl_xor_sync(0xffffffffu, mx, d));
+  const fp4::Scale<NV> sc(mx);
+  if (n < P.N) *reinterpret_cast<uint16_t*>(P.codes + m * P.code_stride + n / 2) = (uint16_t)sc.codes(t);
+  const int64_t blk = n / BL;
+  if (n % BL == 0 && blk >> 2 < P.out_atoms) P.scales[fp4::scale_off(m, blk, P.out_atoms)] = (uint8_t)sc.byte;
+}
+
 template <class C>
 __global__ void __launch_bounds__(C::kThreads, 1) mm_few(const __grid_constant__ MmParams P, int split) {
   extern __shared__ __align__(1024) uint8_t smem_raw[];
@@ -803,7 +854,8 @@ __global__ void __launch_bounds__(C::kThreads, 1) mm_few(const __grid_constant__
   const int rank = split > 1 ? (int)cluster_ctarank() : 0;
   const int tile = (int)blockIdx.x / split;
   const int n0 = tile * kHalf, m0 = (int)blockIdx.y * C::NT;  // weight rows, tokens
-  const int kt0 = (int)((int64_t)rank * P.kt / split), kt1 = (int)((int64_t)(rank + 1) * P.kt / split);
+  const int n_it = P.segs * P.kt;
+  const int it0 = (int)((int64_t)rank * n_it / split), it1 = (int)((int64_t)(rank + 1) * n_it / split);
 
   if (threadIdx.x == 0) {
     s_abort = 0;
@@ -835,7 +887,7 @@ __global__ void __launch_bounds__(C::kThreads, 1) mm_few(const __grid_constant__
       pdl_wait();
       int s = 0;
       uint32_t ph = 1;
-      for (int kt = kt0; kt < kt1; ++kt) {
+      for (int i = it0; i < it1; ++i) {
         const int w = wait(smem_u32(&bar_empty[s]), ph, &s_abort);
         if (w != kOk) {
           if (w == kTimeout) fail(kStatusTimeoutEmpty);
@@ -844,10 +896,19 @@ __global__ void __launch_bounds__(C::kThreads, 1) mm_few(const __grid_constant__
         const uint32_t bar = smem_u32(&bar_full[s]);
         mbar_expect_tx(bar, C::kStage);
         const uint32_t da = smem_u32(smem + s * C::MATS * kOpBytes), db = smem_u32(smem + C::kBOff + s * C::kB);
+        const int seg = i >= P.kt, kt = seg ? i - P.kt : i;
         const int k = C::KIND == k16 ? kt * 64 : kt * kRowBytes;
 #pragma unroll
-        for (int j = 0; j < C::MATS; ++j) tma_load_2d(da + j * kOpBytes, &P.b[j], k, n0, bar);
-        tma_load_2d(db, &P.a[0], k, m0, bar);
+        for (int j = 0; j < C::MATS; ++j) {
+          const CUtensorMap* map = &P.b[C::GATED ? j : seg];
+          if (C::KIND == k16 && P.a_mn) {
+            tma_load_2d(da + j * kOpBytes, map, n0, k, bar);
+            tma_load_2d(da + j * kOpBytes + 8192, map, n0 + 64, k, bar);
+          } else {
+            tma_load_2d(da + j * kOpBytes, map, k, n0, bar);
+          }
+        }
+        tma_load_2d(db, &P.a[C::GATED ? 0 : seg], k, m0, bar);
         if (C::KIND != k16) {
           const uint32_t sa = smem_u32(smem + C::kSaOff + s * C::kSa);
           const int row = kt * C::ATOMS;
@@ -868,9 +929,12 @@ __global__ void __launch_bounds__(C::kThreads, 1) mm_few(const __grid_constant__
       int s = 0, sf = 0, so = 0, held = 0;  // as in mm_pair
       uint32_t ph = 0, so_ph = 0;
       bool ready = false;
-      const uint64_t a0 = desc_sw128(smem_u32(smem), 16), b0 = desc_sw128(smem_u32(smem + C::kBOff), 16);
+      const uint64_t a0 = desc_sw128(smem_u32(smem), P.a_mn ? 8192 : 16), b0 = desc_sw128(smem_u32(smem + C::kBOff), 16);
+      const int a_step = P.a_mn ? 2048 >> 4 : 32 >> 4;
+      const uint32_t b_col = (uint32_t)(m0 & 127) >> 5;  // of the tokens' scales in their group of 128
       const uint64_t sa0 = desc_scales(smem_u32(smem + C::kSaOff)), sb0 = desc_scales(smem_u32(smem + C::kSbOff));
-      for (int kt = kt0; kt < kt1; ++kt) {
+      for (int i = it0; i < it1; ++i) {
+        const int kt = i >= P.kt ? i - P.kt : i;
         int w = kOk;
         if (!ready) w = wait(smem_u32(&bar_full[s]), ph, &s_abort);
         if (w != kOk) {
@@ -918,15 +982,15 @@ __global__ void __launch_bounds__(C::kThreads, 1) mm_few(const __grid_constant__
           if (kk >= n_mma) break;
 #pragma unroll
           for (int j = 0; j < C::MATS; ++j) {
-            const uint64_t aj = a + (uint64_t)((j * kOpBytes) >> 4) + (uint64_t)(2 * kk);
-            const bool acc = kt > kt0 || kk > 0;
+            const uint64_t aj = a + (uint64_t)((j * kOpBytes) >> 4) + (uint64_t)(kk * a_step);
+            const bool acc = i > it0 || kk > 0;
             if constexpr (C::KIND == k16) {
               mma_16<1>(tmem + j * C::NT, aj, b + (uint64_t)(2 * kk), P.idesc, acc);
             } else {
               constexpr bool NV = C::KIND == kNv;
               const uint32_t c = c0 + (NV ? kk : kk >> 1) * 4 * (C::MATS + 1);
               const uint32_t id = NV || !(kk & 1) ? P.idesc : P.idesc | idesc_fp4(0, 0, false, 2);
-              mma_fp4<1, NV>(tmem + j * C::NT, aj, b + (uint64_t)(2 * kk), id, c + 4 * j, c + 4 * C::MATS, acc);
+              mma_fp4<1, NV>(tmem + j * C::NT, aj, b + (uint64_t)(2 * kk), id, c + 4 * j, c + 4 * C::MATS + b_col, acc);
             }
           }
         }
@@ -943,98 +1007,93 @@ __global__ void __launch_bounds__(C::kThreads, 1) mm_few(const __grid_constant__
 
   // ---------------- epilogue ----------------
   // The CTA's part into shared memory, [column][weight row]; then CTA r of the
-  // cluster adds the parts of the columns r, r + split, ... in rank order.
-  const int q = warp & 3, half = warp >> 2;
+  // cluster adds the parts of the columns r, r + split, ... in rank order, a warp
+  // a column, a lane four rows.
   float* part = reinterpret_cast<float*>(smem);
+  {
+    const int q = warp & 3;
 #pragma unroll 1
-  for (int c = half * 16; c < C::MATS * C::NT; c += 32) {
-    uint32_t r[16];
-    tmem_ld16(tmem + ((uint32_t)(32 * q) << 16) + c, r);
-    tc_wait_ld();
-    tc_regs_ready(r);
+    for (int c = (warp >> 2) * 16; c < C::MATS * C::NT; c += 32) {
+      uint32_t r[16];
+      tmem_ld16(tmem + ((uint32_t)(32 * q) << 16) + c, r);
+      tc_wait_ld();
+      tc_regs_ready(r);
 #pragma unroll
-    for (int j = 0; j < 16; ++j) part[(c + j) * kHalf + 32 * q + lane] = __uint_as_float(r[j]);
+      for (int j = 0; j < 16; ++j) part[(c + j) * kHalf + 32 * q + lane] = __uint_as_float(r[j]);
+    }
   }
   tc_fence_before();
   __syncthreads();
   if (split > 1) cluster_sync();
   pdl_wait();
-  const int n = n0 + 32 * q + lane;
-  const uint32_t mine = smem_u32(part + 32 * q + lane);
-  // U columns at a time, so that the reads from the peers' shared memory are
-  // under way together (one at a time: 128 tokens, 5120 x 5120 15.2 us, 10.8 so)
-  constexpr int U = 4;
-  auto sums = [&](int col0, float (&v)[U]) {  // columns col0, col0 + split, ...
+  const int n = n0 + 4 * lane, cnt = min(4, P.N - n);  // the lane's columns of the output
+  const uint32_t mine = smem_u32(part + 4 * lane);
+  auto sum = [&](int col, float (&v)[4]) {
 #pragma unroll
-    for (int i = 0; i < U; ++i) v[i] = 0.f;
-    if (split == 1) {
+    for (int i = 0; i < 4; ++i) v[i] = 0.f;
 #pragma unroll
-      for (int i = 0; i < U; ++i) v[i] = part[min(col0 + i, C::MATS * C::NT - 1) * kHalf + 32 * q + lane];
-    } else {
-#pragma unroll 4
-      for (int r = 0; r < split; ++r) {
-        const uint32_t at = mapa(mine, r);
+    for (int r0 = 0; r0 < kMaxSplit; r0 += 4) {  // (four reads under way together)
+      if (r0 >= split) break;
+      float4 f[4];
 #pragma unroll
-        for (int i = 0; i < U; ++i)
-          v[i] += ld_cluster_f32(at + min(col0 + i * split, C::MATS * C::NT - 1) * (kHalf * 4));
-      }
+      for (int r = 0; r < 4; ++r)
+        if (r0 + r < split) f[r] = ld_cluster_f32x4(mapa(mine, r0 + r) + col * (kHalf * 4));
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        if (r0 + r < split) v[0] += f[r].x, v[1] += f[r].y, v[2] += f[r].z, v[3] += f[r].w;
     }
   };
+  // two columns at a time, so that their reads from the peers are under way together
+  constexpr int U = 2, kStep = C::kThreads / 32;
 #pragma unroll 1
-  for (int j0 = rank + split * U * half; j0 < C::NT && m0 + j0 < P.M; j0 += 2 * U * split) {
-    float vs[U], us[U];
-    sums(j0, vs);
-    if (C::GATED) sums(C::NT + j0, us);
+  for (int j0 = rank + split * warp; j0 < C::NT && m0 + j0 < P.M; j0 += U * kStep * split) {
+    float vs[U][4], us[C::GATED ? U : 1][4];
 #pragma unroll
     for (int i = 0; i < U; ++i) {
-      const int j = j0 + i * split;
+      const int j = min(j0 + i * kStep * split, C::NT - 1);
+      sum(j, vs[i]);
+      if constexpr (C::GATED) sum(C::NT + j, us[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      const int j = j0 + i * kStep * split;
       const int64_t m = m0 + j;
       if (j >= C::NT || m >= P.M) break;
-      float v = vs[i] * P.alpha[0];
-      if constexpr (C::GATED) {
-        const float u = us[i] * P.alpha[1];
-        if (P.saved && n < P.N) {
-          const int64_t at = m * P.saved_stride + n;
-          const uint32_t a = __float_as_uint(v), b = __float_as_uint(u);
-          *reinterpret_cast<uint16_t*>(saved_hi(P, 0, at)) = (uint16_t)(a >> 16);
-          *reinterpret_cast<uint16_t*>(saved_hi(P, 1, at)) = (uint16_t)(b >> 16);
-          *saved_lo(P, 0, at) = (uint8_t)(a >> 8);
-          *saved_lo(P, 1, at) = (uint8_t)(b >> 8);
-        }
-        v = silu(v) * u;
-        if (P.qfmt) {
-          // a block is the warp (MX) or half of it (NV), a lane an element
-          const bool nv = P.qfmt == kNv;
-          float t = n < P.N ? v : 0.f;
-          if (nv) t = P.inv_g != 0.f ? t * P.inv_g : __fdiv_rn(t, P.g);
-          uint32_t mx = __float_as_uint(t) & 0x7FFFFFFFu;
-          if (nv) mx = __reduce_max_sync(lane < 16 ? 0x0000FFFFu : 0xFFFF0000u, mx);
-          else mx = __reduce_max_sync(0xFFFFFFFFu, mx);
-          const float z[8] = {t};
-          uint32_t byte, w;
-          if (nv) {
-            const fp4::Scale<true> sc(mx);
-            byte = sc.byte;
-            w = sc.codes(z);
-          } else {
-            const fp4::Scale<false> sc(mx);
-            byte = sc.byte;
-            w = sc.codes(z);
-          }
-          w = (w & 15u) << (4 * (lane & 7));  // 8 lanes make a word
+      float (&v)[4] = vs[i];
 #pragma unroll
-          for (int d = 1; d < 8; d *= 2) w |= __shfl_xor_sync(0xffffffffu, w, d);
-          if ((lane & 7) == 0 && n < P.N) *reinterpret_cast<uint32_t*>(P.codes + m * P.code_stride + n / 2) = w;
-          const int bl = nv ? 16 : 32;
-          const int64_t blk = n / bl;
-          if ((lane & (bl - 1)) == 0 && blk >> 2 < P.out_atoms)
-            P.scales[fp4::scale_off(m, blk, P.out_atoms)] = (uint8_t)byte;
+      for (int e = 0; e < 4; ++e) v[e] *= P.alpha[0];
+      if constexpr (C::GATED) {
+        float (&u)[4] = us[i];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) u[e] *= P.alpha[1];
+        if (P.saved && cnt > 0) {  // (rows are padded to 32)
+          const int64_t at = m * P.saved_stride + n;
+          save4(P, 0, at, v);
+          save4(P, 1, at, u);
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = silu(v[e]) * u[e];
+        if (P.qfmt) {
+          if (P.qfmt == kNv) store_codes4<true>(P, m, n, v);
+          else store_codes4<false>(P, m, n, v);
           continue;
         }
-      } else if (P.res && n < P.N) {
-        v += load_dense(P.res, m * P.res_stride + n, P.type);
+      } else if (P.res && cnt > 0) {
+        if (P.vec && cnt == 4) {
+          add4(P.res, m * P.res_stride + n, v, P.type);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (e < cnt) v[e] += load_dense(P.res, m * P.res_stride + n + e, P.type);
+        }
       }
-      if (n < P.N) store_dense(P.y[0], m * P.y_stride + n, v, P.type);
+      if (P.vec && cnt == 4) {
+        store4(P.y[0], m * P.y_stride + n, v, P.type);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (e < cnt) store_dense(P.y[0], m * P.y_stride + n + e, v[e], P.type);
+      }
     }
   }
   __syncthreads();
@@ -1236,13 +1295,14 @@ int run_few(MmParams& P, int dev, void* stream, const char* who) {
   if (ty > 65535) return polyq_set_error(POLYQ_EUNSUPPORTED, "%s: %d tokens", who, P.M);
   // the split with the shortest longest CTA: waves of tiles times stages, and
   // about two stages' time for a cluster's exchange
+  const int n_it = P.segs * P.kt;
   int best = 1;
   double t_best = 1e30;
-  for (int s = 1; s <= kMaxSplit && s <= P.kt; ++s) {
+  for (int s = 1; s <= kMaxSplit && s <= n_it; ++s) {
     int fit = 0;
     const int rc = resident_clusters((const void*)mm_few<C>, C::kThreads, C::kSmem, s, &cached[dev][s - 1], &fit, who);
     if (rc) return rc;
-    const double t = (double)((tiles * ty + fit - 1) / fit) * ((P.kt + s - 1) / s + 4.0 + (s > 1 ? 2.0 : 0.0));
+    const double t = (double)((tiles * ty + fit - 1) / fit) * ((n_it + s - 1) / s + 4.0 + (s > 1 ? 2.0 : 0.0));
     if (t < 0.97 * t_best) {
       t_best = t;
       best = s;
