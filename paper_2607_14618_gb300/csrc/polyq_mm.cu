@@ -56,6 +56,7 @@ struct MmParams {
   // all of their stages in tile order, sk_share a pair (the first sk_extra pairs
   // one more).  The other tiles are whole, strided over the pairs.
   int sk_tiles, sk_pairs, sk_parts, sk_share, sk_extra;
+  int grid_pairs;
   float* parts;            // [2 pairs][64][256 rows][4 columns]: parts of shared tiles
   int* counters;           // [sk_tiles][2 CTAs][warps]: parts in place
   int a_mn, b_mn;          // operand has M (N) contiguous instead of K
@@ -66,7 +67,7 @@ struct MmParams {
   void* y[2];
   const void* res;
   int64_t y_stride, res_stride;
-  int type, vec;           // vec: rows of y and res start on 16 bytes (1), y's on 32 (2)
+  int type, vec;           // vec: rows of y start on 8 (1), 16 (2) or 32 bytes (3), and of res on 8
   uint8_t *codes, *scales;
   int64_t code_stride, out_atoms;
   int qfmt;                // 0, kMx or kNv
@@ -102,69 +103,68 @@ __device__ __forceinline__ void store_dense(void* p, int64_t i, float v, int typ
   else if (type == POLYQ_BF16) ((__nv_bfloat16*)p)[i] = __float2bfloat16_rn(v);
   else ((__half*)p)[i] = __float2half_rn(v);
 }
-// Rows that start on 32 (vec = 2) or 16 bytes (1): a lane holds 32 consecutive
-// values of its row and stores, or adds from the residual, whole sectors.
+// Rows that start on 32 (vec = 3), 16 (2) or 8 bytes (1): a lane holds 32
+// consecutive values of its row and stores whole sectors, or 8 bytes at a time.
 __device__ __forceinline__ void store32(void* p, const uint32_t (&w)[8]) {
   asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]),
                "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
                : "memory");
 }
+__device__ __forceinline__ void store32(void* p, const uint32_t (&w)[8], int vec) {
+  if (vec == 3) {
+    store32(p, w);
+  } else if (vec == 2) {
+    reinterpret_cast<uint4*>(p)[0] = make_uint4(w[0], w[1], w[2], w[3]);
+    reinterpret_cast<uint4*>(p)[1] = make_uint4(w[4], w[5], w[6], w[7]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) reinterpret_cast<uint2*>(p)[i] = make_uint2(w[2 * i], w[2 * i + 1]);
+  }
+}
 __device__ __forceinline__ void store_row32(void* y, int64_t off, const float (&v)[32], int type, int vec) {
+  uint32_t w[8];
   if (type == POLYQ_F32) {
-    float* d = (float*)y + off;
 #pragma unroll
     for (int i = 0; i < 32; i += 8) {
-      uint32_t w[8];
 #pragma unroll
       for (int j = 0; j < 8; ++j) w[j] = __float_as_uint(v[i + j]);
-      if (vec == 2) {
-        store32(d + i, w);
-      } else {
-        reinterpret_cast<uint4*>(d + i)[0] = make_uint4(w[0], w[1], w[2], w[3]);
-        reinterpret_cast<uint4*>(d + i)[1] = make_uint4(w[4], w[5], w[6], w[7]);
-      }
+      store32((float*)y + off + i, w, vec);
     }
   } else {
-    uint16_t* d = (uint16_t*)y + off;
 #pragma unroll
     for (int i = 0; i < 32; i += 16) {
-      uint32_t w[8];
 #pragma unroll
       for (int j = 0; j < 8; ++j) w[j] = pack16(v[i + 2 * j], v[i + 2 * j + 1], type == POLYQ_BF16);
-      if (vec == 2) {
-        store32(d + i, w);
-      } else {
-        reinterpret_cast<uint4*>(d + i)[0] = make_uint4(w[0], w[1], w[2], w[3]);
-        reinterpret_cast<uint4*>(d + i)[1] = make_uint4(w[4], w[5], w[6], w[7]);
-      }
+      store32((uint16_t*)y + off + i, w, vec);
     }
   }
 }
 __device__ __forceinline__ void add_row32(const void* r, int64_t off, float (&v)[32], int type) {
   if (type == POLYQ_F32) {
-    const float4* s = reinterpret_cast<const float4*>((const float*)r + off);
+    const float2* s = reinterpret_cast<const float2*>((const float*)r + off);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float4 f = s[i];
-      v[4 * i] += f.x;
-      v[4 * i + 1] += f.y;
-      v[4 * i + 2] += f.z;
-      v[4 * i + 3] += f.w;
+    for (int i = 0; i < 16; ++i) {
+      const float2 f = s[i];
+      v[2 * i] += f.x;
+      v[2 * i + 1] += f.y;
     }
   } else {
-    const uint4* s = reinterpret_cast<const uint4*>((const uint16_t*)r + off);
+    const uint2* s = reinterpret_cast<const uint2*>((const uint16_t*)r + off);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const uint4 u = s[i];
-      const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        float2 f;
-        if (type == POLYQ_BF16) f = make_float2(bf16_lo(w[j]), bf16_hi(w[j]));
-        else f = __half22float2(*reinterpret_cast<const __half2*>(&w[j]));
-        v[8 * i + 2 * j] += f.x;
-        v[8 * i + 2 * j + 1] += f.y;
+    for (int i = 0; i < 8; ++i) {
+      const uint2 u = s[i];
+      float2 a, b;
+      if (type == POLYQ_BF16) {
+        a = make_float2(bf16_lo(u.x), bf16_hi(u.x));
+        b = make_float2(bf16_lo(u.y), bf16_hi(u.y));
+      } else {
+        a = __half22float2(*reinterpret_cast<const __half2*>(&u.x));
+        b = __half22float2(*reinterpret_cast<const __half2*>(&u.y));
       }
+      v[4 * i] += a.x;
+      v[4 * i + 1] += a.y;
+      v[4 * i + 2] += b.x;
+      v[4 * i + 3] += b.y;
     }
   }
 }
@@ -791,14 +791,17 @@ struct Few {
 
 // A lane's four consecutive values of an output row.
 __device__ __forceinline__ void store4(void* y, int64_t i, const float (&v)[4], int type) {
-  if (type == POLYQ_F32) *reinterpret_cast<float4*>((float*)y + i) = make_float4(v[0], v[1], v[2], v[3]);
-  else *reinterpret_cast<uint2*>((uint16_t*)y + i) =
+  if (type == POLYQ_F32) {
+    reinterpret_cast<float2*>((float*)y + i)[0] = make_float2(v[0], v[1]);
+    reinterpret_cast<float2*>((float*)y + i)[1] = make_float2(v[2], v[3]);
+  } else *reinterpret_cast<uint2*>((uint16_t*)y + i) =
       make_uint2(pack16(v[0], v[1], type == POLYQ_BF16), pack16(v[2], v[3], type == POLYQ_BF16));
 }
 __device__ __forceinline__ void add4(const void* r, int64_t i, float (&v)[4], int type) {
   if (type == POLYQ_F32) {
-    const float4 f = *reinterpret_cast<const float4*>((const float*)r + i);
-    v[0] += f.x, v[1] += f.y, v[2] += f.z, v[3] += f.w;
+    const float2 a = reinterpret_cast<const float2*>((const float*)r + i)[0];
+    const float2 b = reinterpret_cast<const float2*>((const float*)r + i)[1];
+    v[0] += a.x, v[1] += a.y, v[2] += b.x, v[3] += b.y;
   } else {
     const uint2 w = *reinterpret_cast<const uint2*>((const uint16_t*)r + i);
     if (type == POLYQ_BF16) {
@@ -1236,37 +1239,87 @@ size_t workspace_bytes_of(int sms) { return kPartsOff + (size_t)sms * kTileM * k
 // idle and that is shorter.  In stages (0.3 us): writing a part and finding the
 // others in place cost kShareCost, each part that the last of a tile's pairs
 // adds kPartCost; where shares do not end with tiles a pair has two parts.
+// Returns the last wave's stages.
 // (256 x 1024 x 13824 4 bits, 4 tiles: 19.9 us whole, 18.0 / 17.0 / 18.6 in 2 / 3 / 6
 // parts; 5120 instead of 13824 11.1, 13.7 in 2.  16-bit, 4 tiles of 160 stages
 // beside 76 whole ones 105 us, 72 in 4.)
 constexpr double kShareCost = 11, kPartCost = 4.5;
-void plan_tiles(MmParams& P, int pairs) {
+double plan_tiles(MmParams& P, int pairs) {
   const int n_it = P.segs * P.kt, rest = P.tiles % pairs;
   P.sk_tiles = P.sk_pairs = P.sk_parts = P.sk_share = P.sk_extra = 0;
-  if (rest == 0) return;
-  double best = 0.95 * n_it;
+  if (rest == 0) return 0;
+  double best = 0.95 * n_it, last = n_it;
   for (int s = 2; s * rest <= pairs && s <= n_it; ++s) {
     const double t = (n_it + s - 1) / s + kShareCost + kPartCost * s;
     if (t < best) {
-      best = t;
+      best = last = t;
       P.sk_tiles = rest;
       P.sk_parts = s;
       P.sk_pairs = s * rest;
     }
   }
   const double share = (double)rest * n_it / pairs;
-  if (share >= 2 && share + 2 * kShareCost + kPartCost * (std::ceil(n_it / share) + 1) < 0.95 * best) {
+  const double t = share + 2 * kShareCost + kPartCost * (std::ceil(n_it / share) + 1);
+  if (share >= 2 && t < 0.95 * best) {
+    last = t;
     P.sk_tiles = rest;
     P.sk_parts = 0;
     P.sk_pairs = pairs;
     P.sk_share = (int)((int64_t)rest * n_it / pairs);
     P.sk_extra = (int)((int64_t)rest * n_it % pairs);
   }
+  return last;
 }
 
-// Tiles of a pair launch: P.M, P.N, P.probs are set.
+// What a call launches: mm_few with a token tile and a split of the
+// contraction, or mm_pair (tokens 0), whichever the model below says is
+// shorter.  Times in us, of products whose operands lie in L2, both sides as
+// measured (MX; gated after the stroke), few with 64 tokens a tile / few with
+// 128 / pair:
+//   13824 x 5120, 128 tokens  19.2/26.6  11.5/17.6  11.6/19.0
+//   5120 x 5120, 192 tokens    9.8/13.2  11.3/16.9  11.3/11.8
+//   5120 x 13824, 96 tokens   19.5/25.6  10.8/15.4  18.3/21.4
+//   1024 x 5120, 1024 tokens   9.8/13.2   9.2/13.2  11.2/11.6
+//   4096 x 512, 256 tokens     4.6/6.6    6.1/9.3    6.3/6.5
+constexpr int kFewTokens = 2048;
+struct Plan {
+  int tokens, split;
+  double us;
+};
+
+// A wave of mm_few's CTAs: launch, first loads and epilogue, and a stage.
 template <class C>
-int run_pair(MmParams& P, int dev, void* workspace, void* stream, const char* who) {
+constexpr double few_base() {
+  return C::GATED ? (C::NT == 16 ? 4.2 : C::NT == 32 ? 4.6 : C::NT == 64 ? 5.5 : 8.0)
+                  : (C::NT == 16 ? 3.3 : C::NT == 32 ? 3.5 : C::NT == 64 ? 3.8 : 5.2);
+}
+template <class C>
+constexpr double few_stage() {
+  if (C::KIND == k16) return C::GATED ? (C::NT == 128 ? 0.75 : C::NT == 64 ? 0.57 : 0.45) : (C::NT == 128 ? 0.40 : 0.32);
+  return C::GATED ? (C::NT == 128 ? 0.55 : C::NT == 64 ? 0.385 : 0.35) : (C::NT == 128 ? 0.30 : 0.28);
+}
+constexpr double kFewSplit = 0.5, kPairBase = 5.4, kPairStage = 0.27, kPairWave = 1.6;
+
+// P.M tokens, P.N weight rows, P.segs and P.kt are set.
+template <class C>
+int consider_few(const MmParams& P, int dev, Plan* best, const char* who) {
+  static std::atomic<int> cached[kMaxDevices][kMaxSplit];
+  const int64_t tiles = (int64_t)((P.N + kHalf - 1) / kHalf) * ((P.M + C::NT - 1) / C::NT);
+  const int n_it = P.segs * P.kt;
+  for (int s = 1; s <= kMaxSplit && s <= n_it; ++s) {
+    int fit = 0;
+    const int rc = resident_clusters((const void*)mm_few<C>, C::kThreads, C::kSmem, s, &cached[dev][s - 1], &fit, who);
+    if (rc) return rc;
+    const double us = (double)((tiles + fit - 1) / fit) *
+                      (few_base<C>() + few_stage<C>() * ((n_it + s - 1) / s) + (s > 1 ? kFewSplit : 0.0));
+    if (us < 0.98 * best->us) *best = {C::NT, s, us};
+  }
+  return POLYQ_OK;
+}
+
+// P.probs is set too; fills in the tiles and how they are shared.
+template <class C>
+int consider_pair(MmParams& P, int dev, Plan* best, const char* who) {
   static std::atomic<int> cached[kMaxDevices];
   int pairs = 0;
   const int rc = resident_clusters((const void*)mm_pair<C>, C::kThreads, C::kSmem, 2, &cached[dev], &pairs, who);
@@ -1278,39 +1331,50 @@ int run_pair(MmParams& P, int dev, void* workspace, void* stream, const char* wh
   const int64_t tiles = (int64_t)P.tiles_m * P.tiles_n * P.probs;
   if (tiles >= 1ll << 31) return polyq_set_error(POLYQ_EUNSUPPORTED, "%s: %lld tiles", who, (long long)tiles);
   P.tiles = (int)tiles;
-  P.counters = (int*)((uint8_t*)workspace + kCountersOff);
-  P.parts = (float*)((uint8_t*)workspace + kPartsOff);
-  plan_tiles(P, pairs);
-  const int grid = P.tiles > pairs ? pairs : std::max(P.tiles, P.sk_pairs);
-  void* args[] = {&P};
-  return launch_cluster((const void*)mm_pair<C>, dim3((unsigned)(2 * grid)), C::kThreads, C::kSmem, 2, args, stream,
-                        who);
+  const double last = plan_tiles(P, pairs);
+  P.grid_pairs = P.tiles > pairs ? pairs : std::max(P.tiles, P.sk_pairs);
+  const double waves = (double)(P.tiles / pairs);
+  const double us = kPairBase + kPairStage * (waves * P.segs * P.kt + last) + kPairWave * (waves + (last > 0) - 1);
+  if (us < best->us) *best = {0, 1, us};
+  return POLYQ_OK;
 }
 
-// Few tokens: P.M tokens, P.N weight rows.
+template <int KIND, bool GATED>
+int plan_product(MmParams& P, int dev, Plan* plan, const char* who) {
+  *plan = {0, 1, 1e30};
+  int rc = consider_pair<Pair<KIND, GATED>>(P, dev, plan, who);
+  if (!rc && P.M <= 16) rc = consider_few<Few<KIND, 16, GATED>>(P, dev, plan, who);
+  if (!rc && P.M > 16 && P.M <= 32) rc = consider_few<Few<KIND, 32, GATED>>(P, dev, plan, who);
+  // (with more tokens than fill every SM's tile the pairs are far ahead)
+  if (!rc && P.M > 32 && P.M <= kFewTokens) rc = consider_few<Few<KIND, 64, GATED>>(P, dev, plan, who);
+  if (!rc && P.M > 64 && P.M <= kFewTokens) rc = consider_few<Few<KIND, 128, GATED>>(P, dev, plan, who);
+  return rc;
+}
+
 template <class C>
-int run_few(MmParams& P, int dev, void* stream, const char* who) {
-  static std::atomic<int> cached[kMaxDevices][kMaxSplit];
-  const int64_t tiles = (P.N + kHalf - 1) / kHalf, ty = (P.M + C::NT - 1) / C::NT;
-  if (ty > 65535) return polyq_set_error(POLYQ_EUNSUPPORTED, "%s: %d tokens", who, P.M);
-  // the split with the shortest longest CTA: waves of tiles times stages, and
-  // about two stages' time for a cluster's exchange
-  const int n_it = P.segs * P.kt;
-  int best = 1;
-  double t_best = 1e30;
-  for (int s = 1; s <= kMaxSplit && s <= n_it; ++s) {
-    int fit = 0;
-    const int rc = resident_clusters((const void*)mm_few<C>, C::kThreads, C::kSmem, s, &cached[dev][s - 1], &fit, who);
-    if (rc) return rc;
-    const double t = (double)((tiles * ty + fit - 1) / fit) * ((n_it + s - 1) / s + 4.0 + (s > 1 ? 2.0 : 0.0));
-    if (t < 0.97 * t_best) {
-      t_best = t;
-      best = s;
-    }
+int launch_few(MmParams& P, const Plan& plan, void* stream, const char* who) {
+  int split = plan.split;
+  void* args[] = {&P, &split};
+  const unsigned tiles = (unsigned)((P.N + kHalf - 1) / kHalf), ty = (unsigned)((P.M + C::NT - 1) / C::NT);
+  return launch_cluster((const void*)mm_few<C>, dim3(tiles * split, ty), C::kThreads, C::kSmem, split, args, stream, who);
+}
+template <class C>
+int launch_pair(MmParams& P, void* workspace, void* stream, const char* who) {
+  P.counters = (int*)((uint8_t*)workspace + kCountersOff);
+  P.parts = (float*)((uint8_t*)workspace + kPartsOff);
+  void* args[] = {&P};
+  return launch_cluster((const void*)mm_pair<C>, dim3(2u * (unsigned)P.grid_pairs), C::kThreads, C::kSmem, 2, args,
+                        stream, who);
+}
+template <int KIND, bool GATED>
+int launch_product(MmParams& P, const Plan& plan, void* workspace, void* stream, const char* who) {
+  switch (plan.tokens) {
+    case 16: return launch_few<Few<KIND, 16, GATED>>(P, plan, stream, who);
+    case 32: return launch_few<Few<KIND, 32, GATED>>(P, plan, stream, who);
+    case 64: return launch_few<Few<KIND, 64, GATED>>(P, plan, stream, who);
+    case 128: return launch_few<Few<KIND, 128, GATED>>(P, plan, stream, who);
+    default: return launch_pair<Pair<KIND, GATED>>(P, workspace, stream, who);
   }
-  void* args[] = {&P, &best};
-  return launch_cluster((const void*)mm_few<C>, dim3((unsigned)(tiles * best), (unsigned)ty), C::kThreads, C::kSmem,
-                        best, args, stream, who);
 }
 
 int check_workspace(const void* ws, size_t bytes, size_t more, const char* who) {
@@ -1325,10 +1389,10 @@ int check_workspace(const void* ws, size_t bytes, size_t more, const char* who) 
 }
 
 int elem_bytes(int type) { return type == POLYQ_F32 ? 4 : 2; }
-// Whether rows start on 32 (2), 16 (1) or fewer bytes (0).
+// Whether rows start on 32 (3), 16 (2), 8 (1) or fewer bytes (0).
 int vec_rows(const void* p, int64_t stride, int type) {
   const uint64_t a = (uint64_t)(uintptr_t)p | (uint64_t)(stride * elem_bytes(type));
-  return a % 32 == 0 ? 2 : a % 16 == 0 ? 1 : 0;
+  return a % 32 == 0 ? 3 : a % 16 == 0 ? 2 : a % 8 == 0 ? 1 : 0;
 }
 int vec_rows(const polyq_dense* d) { return vec_rows(d->data, d->stride, d->type); }
 
@@ -1348,25 +1412,6 @@ int map_fp4(CUtensorMap* codes, CUtensorMap* scales, const polyq_fp4* t, int row
 int map_16(CUtensorMap* m, const void* data, int64_t stride, int64_t rows, int64_t cols, bool mn, int box_rows) {
   return polyq_tensor_map_2d(m, data, 2, (uint64_t)cols, (uint64_t)rows, (uint64_t)stride * 2, 64,
                              mn ? 64u : (uint32_t)box_rows, 128);
-}
-
-// At most this many tokens (GATED: half): mm_few.  (MX, us, mm_few and mm_pair:
-// 13824 x 5120 48 tokens 11.0 / 14, 128 tokens 16.0 / 14.1; 5120 x 5120 128 tokens
-// 10.8 / 11.8, 5120 x 13824 64 tokens 11.3 / 18; gated 13824 x 5120 48 tokens 16.0 /
-// 23, 128 tokens 25.9 / 23, 5120 x 5120 128 tokens 16.3 / 12.)
-constexpr int kFewTokens = 128;
-int few_tile(int64_t M) { return M <= 16 ? 16 : M <= 32 ? 32 : M <= 64 ? 64 : 128; }
-
-template <int KIND, bool GATED>
-int dispatch_few(MmParams& P, int dev, void* stream, const char* who) {
-  switch (few_tile(P.M)) {
-    case 16: return run_few<Few<KIND, 16, GATED>>(P, dev, stream, who);
-    case 32: return run_few<Few<KIND, 32, GATED>>(P, dev, stream, who);
-    case 64: return run_few<Few<KIND, 64, GATED>>(P, dev, stream, who);
-    default: break;
-  }
-  if constexpr (!GATED) return run_few<Few<KIND, 128, GATED>>(P, dev, stream, who);
-  return POLYQ_EUNSUPPORTED;  // not reached: kFewTokens
 }
 
 void set_quant_out(MmParams& P, const polyq_fp4* q) {
@@ -1392,7 +1437,7 @@ int run_fp4(MmParams& P, const polyq_fp4* x, const polyq_fp4* w0, const polyq_fp
   int dev = 0;
   int rc = device_index(&dev, who);
   if (rc) return rc;
-  const bool nv = KIND == kNv, few = x->rows <= (GATED ? kFewTokens / 2 : kFewTokens);
+  const bool nv = KIND == kNv;
   P.M = (int)x->rows;
   P.N = (int)w0->rows;
   P.segs = P.probs = 1;
@@ -1401,20 +1446,14 @@ int run_fp4(MmParams& P, const polyq_fp4* x, const polyq_fp4* w0, const polyq_fp
   P.atoms = (int)fp4::atoms(x->K, nv);
   P.alpha[0] = product_scale(x, w0);
   P.alpha[1] = GATED ? product_scale(x, w1) : 1.f;
-  if (few) {
-    const int nt = few_tile(P.M);
-    P.idesc = idesc_fp4(kHalf, nt, !nv, 0);
-    rc = map_fp4(&P.a[0], &P.sa, x, nt, who);
-    if (!rc) rc = map_fp4(&P.b[0], &P.sb[0], w0, kHalf, who);
-    if (!rc && GATED) rc = map_fp4(&P.b[1], &P.sb[1], w1, kHalf, who);
-    return rc ? rc : dispatch_few<KIND, GATED>(P, dev, stream, who);
-  }
-  P.idesc = idesc_fp4(kTileM, kTileN, !nv, 0);
-  rc = map_fp4(&P.a[0], &P.sa, x, kHalf, who);
+  Plan plan;
+  rc = plan_product<KIND, GATED>(P, dev, &plan, who);
+  if (rc) return rc;
+  P.idesc = plan.tokens ? idesc_fp4(kHalf, plan.tokens, !nv, 0) : idesc_fp4(kTileM, kTileN, !nv, 0);
+  rc = map_fp4(&P.a[0], &P.sa, x, plan.tokens ? plan.tokens : kHalf, who);
   if (!rc) rc = map_fp4(&P.b[0], &P.sb[0], w0, kHalf, who);
   if (!rc && GATED) rc = map_fp4(&P.b[1], &P.sb[1], w1, kHalf, who);
-  if (rc) return rc;
-  return run_pair<Pair<KIND, GATED>>(P, dev, workspace, stream, who);
+  return rc ? rc : launch_product<KIND, GATED>(P, plan, workspace, stream, who);
 }
 
 int check_same(const polyq_fp4* x, const polyq_fp4* w, const char* who, const char* what) {
@@ -1436,7 +1475,7 @@ int check_16(const polyq_dense* d, int64_t cols, int type, const char* who, cons
 int check_operand(const polyq_dense* d, int64_t cols, int type, const char* who, const char* what) {
   int rc = check_16(d, cols, type, who, what);
   if (rc) return rc;
-  if (!vec_rows(d))
+  if (vec_rows(d) < 2)
     return polyq_set_error(POLYQ_EINVAL, "%s: %s: rows must start on 16 bytes (address and stride)", who, what);
   return POLYQ_OK;
 }
@@ -1563,15 +1602,15 @@ extern "C" int polyq_ffn_forward(const polyq_dense* x, const polyq_dense* gate, 
   P.saved = (uint8_t*)saved;
   P.saved_stride = saved_stride(F);
   P.status = (int*)workspace;
-  const bool bf16 = x->type == POLYQ_BF16, few = T <= kFewTokens / 2;
-  const int nt = few_tile(T);
-  P.idesc = few ? idesc_16(kHalf, nt, bf16, false, false) : idesc_16(kTileM, kTileN, bf16, false, false);
-  rc = map_16(&P.a[0], x->data, x->stride, T, K, false, few ? nt : kHalf);
+  const bool bf16 = x->type == POLYQ_BF16;
+  Plan plan;
+  rc = plan_product<k16, true>(P, dev, &plan, who);
+  if (rc) return rc;
+  P.idesc = plan.tokens ? idesc_16(kHalf, plan.tokens, bf16, false, false) : idesc_16(kTileM, kTileN, bf16, false, false);
+  rc = map_16(&P.a[0], x->data, x->stride, T, K, false, plan.tokens ? plan.tokens : kHalf);
   if (!rc) rc = map_16(&P.b[0], gate->data, gate->stride, F, K, false, kHalf);
   if (!rc) rc = map_16(&P.b[1], up->data, up->stride, F, K, false, kHalf);
-  if (rc) return rc;
-  return few ? dispatch_few<k16, true>(P, dev, stream, who)
-             : run_pair<Pair<k16, true>>(P, dev, workspace, stream, who);
+  return rc ? rc : launch_product<k16, true>(P, plan, workspace, stream, who);
 }
 
 extern "C" int polyq_ffn_backward_workspace_bytes(int64_t T, int64_t F, size_t* bytes) {
@@ -1632,7 +1671,7 @@ extern "C" int polyq_ffn_backward(const polyq_dense* x, const polyq_dense* gate,
     A.stride = fs;
     A.dh_stride = dh->stride;
     A.items = T * (fs / 8);
-    A.vec = vec_rows(dh);
+    A.vec = vec_rows(dh) >= 2;
     void* args[] = {&A};
     rc = launch_cluster(bf16 ? (const void*)act_backward<true> : (const void*)act_backward<false>,
                         dim3((unsigned)std::min<int64_t>((A.items + 255) / 256, 1 << 30)), 256, 0, 1, args, stream, who);
@@ -1650,17 +1689,23 @@ extern "C" int polyq_ffn_backward(const polyq_dense* x, const polyq_dense* gate,
     P.probs = 1;
     P.kt = (int)((F + 63) / 64);
     P.k_last = (int)((F - (int64_t)(P.kt - 1) * 64 + 15) / 16);
-    P.b_mn = 1;
     P.y[0] = dx->data;
     P.y_stride = dx->stride;
     P.type = dx->type;
     P.vec = vec_rows(dx);
-    P.idesc = idesc_16(kTileM, kTileN, bf16, false, true);
-    rc = map_16(&P.a[0], da, fs, T, F, false, kHalf);
-    if (!rc) rc = map_16(&P.a[1], du, fs, T, F, false, kHalf);
+    Plan plan;
+    rc = plan_product<k16, false>(P, dev, &plan, who);
+    if (rc) return rc;
+    // mm_few: the weights are the MMAs' A, else their B
+    P.a_mn = plan.tokens != 0;
+    P.b_mn = plan.tokens == 0;
+    P.idesc = plan.tokens ? idesc_16(kHalf, plan.tokens, bf16, true, false) : idesc_16(kTileM, kTileN, bf16, false, true);
+    const int rows = plan.tokens ? plan.tokens : kHalf;
+    rc = map_16(&P.a[0], da, fs, T, F, false, rows);
+    if (!rc) rc = map_16(&P.a[1], du, fs, T, F, false, rows);
     if (!rc) rc = map_16(&P.b[0], gate->data, gate->stride, F, K, true, 0);
     if (!rc) rc = map_16(&P.b[1], up->data, up->stride, F, K, true, 0);
-    if (!rc) rc = run_pair<Pair<k16, false>>(P, dev, workspace, stream, who);
+    if (!rc) rc = launch_product<k16, false>(P, plan, workspace, stream, who);
     if (rc) return rc;
   }
   if (dgate) {
@@ -1682,7 +1727,9 @@ extern "C" int polyq_ffn_backward(const polyq_dense* x, const polyq_dense* gate,
     if (!rc) rc = map_16(&P.a[1], du, fs, T, F, true, 0);
     if (!rc) rc = map_16(&P.b[0], x->data, x->stride, T, K, true, 0);
     P.b[1] = P.b[0];
-    if (!rc) rc = run_pair<Pair<k16, false>>(P, dev, workspace, stream, who);
+    Plan plan = {0, 1, 1e30};
+    if (!rc) rc = consider_pair<Pair<k16, false>>(P, dev, &plan, who);
+    if (!rc) rc = launch_pair<Pair<k16, false>>(P, workspace, stream, who);
   }
   return rc;
 }
