@@ -1378,13 +1378,14 @@ int launch_product(MmParams& P, const Plan& plan, void* workspace, void* stream,
 }
 
 int check_workspace(const void* ws, size_t bytes, size_t more, const char* who) {
+  if (!ws) return polyq_set_error(POLYQ_ENOMEM, "%s: workspace is NULL", who);
+  if ((uintptr_t)ws % 256) return polyq_set_error(POLYQ_EINVAL, "%s: workspace must be 256-byte aligned", who);
   size_t need = 0;
   const int rc = polyq_fp4_workspace_bytes(&need);
   if (rc) return rc;
   need += more;
-  if (!ws || bytes < need)
+  if (bytes < need)
     return polyq_set_error(POLYQ_ENOMEM, "%s: workspace needs %zu bytes, got %zu", who, need, bytes);
-  if ((uintptr_t)ws % 256) return polyq_set_error(POLYQ_EINVAL, "%s: workspace must be 256-byte aligned", who);
   return POLYQ_OK;
 }
 
@@ -1492,6 +1493,7 @@ int check_sizes(int64_t T, int64_t F, int64_t K, const char* who) {
 }  // namespace
 
 extern "C" int polyq_fp4_workspace_bytes(size_t* bytes) {
+  polyq_clear_error();
   if (!bytes) return polyq_set_error(POLYQ_EINVAL, "polyq_fp4_workspace_bytes: bytes is NULL");
   int sms = 0;
   const int rc = polyq_sm_count(&sms);
@@ -1508,12 +1510,13 @@ extern "C" int polyq_fp4_linear(const polyq_fp4* x, const polyq_fp4* w, const po
   if (!rc) rc = check_same(x, w, who, "w");
   if (!rc) rc = polyq_check_dense(y, w->rows, who, "y");
   if (!rc && residual) rc = polyq_check_dense(residual, w->rows, who, "residual");
-  if (!rc) rc = check_workspace(workspace, workspace_bytes, 0, who);
   if (rc) return rc;
   if (residual && residual->type != y->type)
     return polyq_set_error(POLYQ_EINVAL, "%s: residual has type %d, y %d", who, residual->type, y->type);
   if (residual && residual->data == y->data && residual->stride != y->stride)
     return polyq_set_error(POLYQ_EINVAL, "%s: residual is y with another stride", who);
+  rc = check_workspace(workspace, workspace_bytes, 0, who);
+  if (rc) return rc;
   MmParams P;
   memset(&P, 0, sizeof P);
   P.y[0] = y->data;
@@ -1581,11 +1584,11 @@ extern "C" int polyq_ffn_forward(const polyq_dense* x, const polyq_dense* gate, 
   if (!rc) rc = check_operand(gate, K, x->type, who, "gate");
   if (!rc) rc = check_operand(up, K, x->type, who, "up");
   if (!rc) rc = check_16(h, F, x->type, who, "h");
-  if (!rc) rc = check_workspace(workspace, workspace_bytes, 0, who);
   if (rc) return rc;
   if ((uintptr_t)saved % 32) return polyq_set_error(POLYQ_EINVAL, "%s: saved must be 32-byte aligned", who);
+  rc = check_workspace(workspace, workspace_bytes, 0, who);
   int dev = 0;
-  rc = device_index(&dev, who);
+  if (!rc) rc = device_index(&dev, who);
   if (rc) return rc;
   MmParams P;
   memset(&P, 0, sizeof P);
@@ -1635,7 +1638,6 @@ extern "C" int polyq_ffn_backward(const polyq_dense* x, const polyq_dense* gate,
   if (!rc) rc = check_operand(gate, K, x->type, who, "gate");
   if (!rc) rc = check_operand(up, K, x->type, who, "up");
   if (!rc) rc = check_16(dh, F, x->type, who, "dh");
-  if (!rc) rc = check_workspace(workspace, workspace_bytes, grad_bytes(T, F), who);
   if (rc) return rc;
   if (!saved || (uintptr_t)saved % 32)
     return polyq_set_error(POLYQ_EINVAL, "%s: saved must be given, 32-byte aligned", who);
@@ -1652,7 +1654,8 @@ extern "C" int polyq_ffn_backward(const polyq_dense* x, const polyq_dense* gate,
     return polyq_set_error(POLYQ_EINVAL, "%s: dgate and dup must have one type and stride", who);
   int dev = 0;
   size_t head = 0;
-  rc = device_index(&dev, who);
+  rc = check_workspace(workspace, workspace_bytes, grad_bytes(T, F), who);
+  if (!rc) rc = device_index(&dev, who);
   if (!rc) rc = polyq_fp4_workspace_bytes(&head);
   if (rc) return rc;
 
