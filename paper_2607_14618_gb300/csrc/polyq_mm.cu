@@ -508,23 +508,13 @@ __global__ void __launch_bounds__(C::kThreads, 1) mm_pair(const __grid_constant_
       const int a_step = P.a_mn ? 2048 >> 4 : 32 >> 4, b_step = P.b_mn ? 2048 >> 4 : 32 >> 4;
       for (; !s_abort && T.next(P); ++tc) {
         const int buf = tc & 1;
-        int w = kOk;
-        if (C::OV > 0) {
-          if (tc >= 1) w = wait(smem_u32(&bar_acce[0]), (tc - 1) & 1, &s_abort);
-        } else if (tc >= 2) {
-          w = wait(smem_u32(&bar_acce[buf]), ((tc >> 1) - 1) & 1, &s_abort);
-        }
-        if (w != kOk) {
-          if (w == kTimeout) fail(kStatusTimeoutEmpty);
-          break;
-        }
-        tc_fence_after();
+        int w = kOk, why = kStatusTimeoutEmpty;
         const uint32_t acc = tmem + (buf ? C::kAcc1 : 0);
         for (int i = T.lo; i < T.hi; ++i) {
           if (!ready) {
             w = wait(smem_u32(&bar_full[s]), ph, &s_abort);
             if (w != kOk) {
-              if (w == kTimeout) fail(kStatusTimeoutFull);
+              why = kStatusTimeoutFull;
               break;
             }
           }
@@ -550,7 +540,19 @@ __global__ void __launch_bounds__(C::kThreads, 1) mm_pair(const __grid_constant_
           const int kt = i >= P.kt ? i - P.kt : i;
           const int n_mma = kt == P.kt - 1 ? P.k_last : 4;
           const uint64_t a = a0 + (uint64_t)((s * kOpBytes) >> 4), b = b0 + (uint64_t)((s * kOpBytes) >> 4);
+          // the accumulator's columns, of a tile's first stage
+          auto columns = [&]() {
+            if (i != T.lo) return true;
+            if (C::OV > 0) {
+              if (tc >= 1) w = wait(smem_u32(&bar_acce[0]), (tc - 1) & 1, &s_abort);
+            } else if (tc >= 2) {
+              w = wait(smem_u32(&bar_acce[buf]), ((tc >> 1) - 1) & 1, &s_abort);
+            }
+            tc_fence_after();
+            return w == kOk;
+          };
           if constexpr (C::KIND == k16) {
+            if (!columns()) break;
             for (int kk = 0; kk < n_mma; ++kk)
               mma_16<2>(acc, a + (uint64_t)(kk * a_step), b + (uint64_t)(kk * b_step), P.idesc, i > T.lo || kk > 0);
           } else {
@@ -558,10 +560,7 @@ __global__ void __launch_bounds__(C::kThreads, 1) mm_pair(const __grid_constant_
             const uint64_t sa = sa0 + (uint64_t)((s * C::kSa) >> 4), sb = sb0 + (uint64_t)((s * C::kSb) >> 4);
             if (held == C::SF) {  // a slot's scales stay until its stage's MMAs are done
               w = wait(smem_u32(&bar_empty[so]), so_ph, &s_abort);
-              if (w != kOk) {
-                if (w == kTimeout) fail(kStatusTimeoutEmpty);
-                break;
-              }
+              if (w != kOk) break;
               release(1);
               freed = 0;
             }
@@ -574,6 +573,7 @@ __global__ void __launch_bounds__(C::kThreads, 1) mm_pair(const __grid_constant_
               for (int j = 0; j < 2; ++j)
                 copy_scales<2>(c + 4 + 4 * j, sb + (uint64_t)((j * C::ATOMS + q) * 32));
             }
+            if (!columns()) break;  // (the scales are on their way meanwhile)
 #pragma unroll
             for (int kk = 0; kk < 4; ++kk) {
               if (kk >= n_mma) break;
@@ -588,6 +588,7 @@ __global__ void __launch_bounds__(C::kThreads, 1) mm_pair(const __grid_constant_
           s = s1;
           ph = ph1;
         }
+        if (w == kTimeout) fail(why);
         commit<2>(smem_u32(&bar_accf[buf]));
       }
       // the pair's shared and tensor memory stay in use until the last MMA is done
