@@ -23,8 +23,8 @@
  *           do not matter (an entry point that writes codes may set them to 0).
  *   scales  one byte per block of a row: 32 consecutive elements and a power
  *           of two 2^(byte-127) (e8m0; 255 is NaN) for POLYQ_FP4_MX, 16
- *           consecutive elements and an e4m3 number (0x7F is NaN) for
- *           POLYQ_FP4_NV.  They are stored as the tensor cores take them: the
+ *           consecutive elements and a non-negative e4m3 number (bit 7 clear;
+ *           0x7F is NaN) for POLYQ_FP4_NV.  They are stored as the tensor cores take them: the
  *           scale of block b of row r is byte
  *             ((r/128)*A + b/4)*512 + (r%32)*16 + ((r/32)%4)*4 + b%4
  *           with A = ceil(blocks per row / 4).  Bytes of blocks past a row's
@@ -95,9 +95,10 @@ int polyq_fp4_dequantize(const polyq_fp4* t, const polyq_dense* y, void* stream)
 int polyq_fp4_workspace_bytes(size_t* bytes);
 
 /* y[m][n] = residual[m][n] + sum_k x[m][k] w[n][k]: x [M][K] and w [N][K] in
- * one 4-bit format, y [M][N] of any type; residual NULL or [M][N] of y's type
- * (its data may be y's, with y's stride).  Products are exact and summed in
- * fp32; one rounding to y's type.  One launch; the result does not change from
+ * one 4-bit format, whose tensor scales' product is a normal fp32 number, y
+ * [M][N] of any type; residual NULL or [M][N] of y's type (its data may be y's,
+ * with y's stride).  Products are exact and summed in fp32; one rounding to y's
+ * type.  One launch; the result does not change from
  * run to run. */
 int polyq_fp4_linear(const polyq_fp4* x, const polyq_fp4* w, const polyq_dense* residual,
                      const polyq_dense* y, void* workspace, size_t workspace_bytes, void* stream);

@@ -28,7 +28,7 @@ struct QuantParams {
   uint8_t* codes;
   uint8_t* scales;
   int64_t x_stride, y_stride, code_stride, rows, K, A;
-  int64_t row_groups;     // of 1 or 4 rows
+  int64_t row_groups;     // of as many rows as a warp takes together
   float g, inv_g;         // tensor scale; its reciprocal where that is exact, else 0
   int short_ok;           // and no product of it with a block scale's leaves fp32's range
 };
@@ -248,14 +248,19 @@ __global__ void __launch_bounds__(32 * kWarps) dequantize_kernel(const __grid_co
   }
 }
 
-template <typename T, bool NV, bool VEC, int ROWS>
-void* pick(bool quantize) {
-  return quantize ? (void*)quantize_kernel<T, NV, VEC, ROWS> : (void*)dequantize_kernel<T, NV, VEC, ROWS>;
+// Rows a warp takes together once there are enough of them: their loads in
+// flight hide each other's latency (dequantising 13824 x 5120 to bf16: 33.0 us
+// with 4, 31.2 with 8).
+constexpr int kQuantRows = 4, kDequantRows = 8;
+
+template <typename T, bool NV, bool VEC>
+void* pick(bool quantize, bool many) {
+  if (quantize) return many ? (void*)quantize_kernel<T, NV, VEC, kQuantRows> : (void*)quantize_kernel<T, NV, VEC, 1>;
+  return many ? (void*)dequantize_kernel<T, NV, VEC, kDequantRows> : (void*)dequantize_kernel<T, NV, VEC, 1>;
 }
 template <typename T, bool NV>
-void* pick(bool quantize, bool vec, bool rows4) {
-  return vec ? (rows4 ? pick<T, NV, true, 4>(quantize) : pick<T, NV, true, 1>(quantize))
-             : (rows4 ? pick<T, NV, false, 4>(quantize) : pick<T, NV, false, 1>(quantize));
+void* pick(bool quantize, bool vec, bool many) {
+  return vec ? pick<T, NV, true>(quantize, many) : pick<T, NV, false>(quantize, many);
 }
 
 int elem_bytes(int type) { return type == POLYQ_F32 ? 4 : 2; }
@@ -278,16 +283,17 @@ int launch(QuantParams& P, const polyq_fp4* t, const polyq_dense* d, bool quanti
   if (!std::isfinite(P.inv_g)) P.inv_g = 0.f;
   P.short_ok = P.inv_g != 0.f && P.g >= 0x1p-100f && P.g <= 0x1p100f;
   const int64_t chunks = (P.K + 255) / 256;
-  // four rows a warp once that still gives every SM a full set of warps
-  const bool rows4 = P.rows * chunks >= (int64_t)sms * 64 * 4;
-  P.row_groups = rows4 ? (P.rows + 3) / 4 : P.rows;
+  // several rows a warp once that still gives every SM a full set of warps
+  const bool many = P.rows * chunks >= (int64_t)sms * 64 * 4;
+  const int rows = many ? (quantize ? kQuantRows : kDequantRows) : 1;
+  P.row_groups = (P.rows + rows - 1) / rows;
   const int eb = elem_bytes(d->type);
   const bool vec = (uintptr_t)d->data % 16 == 0 && d->stride * eb % 16 == 0;
   void* f;
-  if (d->type == POLYQ_F32) f = nv ? pick<float, true>(quantize, vec, rows4) : pick<float, false>(quantize, vec, rows4);
+  if (d->type == POLYQ_F32) f = nv ? pick<float, true>(quantize, vec, many) : pick<float, false>(quantize, vec, many);
   else if (d->type == POLYQ_BF16)
-    f = nv ? pick<__nv_bfloat16, true>(quantize, vec, rows4) : pick<__nv_bfloat16, false>(quantize, vec, rows4);
-  else f = nv ? pick<__half, true>(quantize, vec, rows4) : pick<__half, false>(quantize, vec, rows4);
+    f = nv ? pick<__nv_bfloat16, true>(quantize, vec, many) : pick<__nv_bfloat16, false>(quantize, vec, many);
+  else f = nv ? pick<__half, true>(quantize, vec, many) : pick<__half, false>(quantize, vec, many);
   cudaLaunchAttribute at[1];
   at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   at[0].val.programmaticStreamSerializationAllowed = 1;

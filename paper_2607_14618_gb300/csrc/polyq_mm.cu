@@ -1428,6 +1428,7 @@ void set_quant_out(MmParams& P, const polyq_fp4* q) {
   P.inv_g = std::frexp(P.g, &e) == 0.5f && std::isfinite(1.f / P.g) ? 1.f / P.g : 0.f;
 }
 
+// The product's tensor scale, which has to be a normal fp32 number.
 float product_scale(const polyq_fp4* a, const polyq_fp4* b) {
   return (float)((double)a->tensor_scale * (double)b->tensor_scale);
 }
@@ -1463,6 +1464,9 @@ int check_same(const polyq_fp4* x, const polyq_fp4* w, const char* who, const ch
     return polyq_set_error(POLYQ_EINVAL, "%s: %s [%lld][%lld] format %d against x [%lld][%lld] format %d", who,
                            what, (long long)w->rows, (long long)w->K, w->format, (long long)x->rows,
                            (long long)x->K, x->format);
+  if (!std::isnormal(product_scale(x, w)))
+    return polyq_set_error(POLYQ_EINVAL, "%s: %s: tensor scales %g and %g", who, what, (double)x->tensor_scale,
+                           (double)w->tensor_scale);
   return POLYQ_OK;
 }
 

@@ -91,6 +91,11 @@ def test_operands_that_do_not_fit(polyq_lib):
         assert _rc(polyq_lib, "polyq_fp4_ffn", q, w, q, y, None, A, 1 << 30, None) == EINVAL
         assert _rc(polyq_lib, "polyq_fp4_ffn", q, q, w, y, None, A, 1 << 30, None) == EINVAL
     assert _rc(polyq_lib, "polyq_fp4_ffn", q, q, _fp4(polyq_lib, rows=65), y, None, A, 1 << 30, None) == EINVAL
+    # tensor scales whose product leaves fp32
+    for g in (2.0 ** 100, 2.0 ** -100):
+        t = _fp4(polyq_lib, format=1, tensor_scale=g)
+        assert _rc(polyq_lib, "polyq_fp4_linear", t, t, None, y, A, 1 << 30, None) == EINVAL
+        assert _rc(polyq_lib, "polyq_fp4_ffn", t, t, t, y, None, A, 1 << 30, None) == EINVAL
     # one of the two outputs
     out = _fp4(polyq_lib, rows=64, K=64)
     assert _rc(polyq_lib, "polyq_fp4_ffn", q, q, q, None, None, A, 1 << 30, None) == EINVAL

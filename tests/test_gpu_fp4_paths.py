@@ -273,6 +273,42 @@ def test_offsets_beyond_32_bits(polyq_lib):
     assert not bool(y[300:-300].any())
 
 
+@pytest.mark.parametrize("fmt", [MX, NV])
+def test_code_rows_of_a_wider_buffer(polyq_lib, fmt):
+    """Codes with a stride of their own: what lies behind a row does not matter."""
+    import ctypes as C
+    g = _gen(9)
+    M, N, K = 150, 140, 333
+    x, w = _q(polyq_lib, g, M, K, fmt), _q(polyq_lib, g, N, K, fmt)
+    y = polyq_lib.fp4_linear(x, w)
+    for t in (x, w):
+        wide = torch.full((t.rows, 512), 0x77, dtype=torch.uint8, device="cuda")
+        wide[:, :t.codes.shape[1]] = t.codes
+        wide[:, (K + 1) // 2:] = 0x77  # also the padding of the narrow rows
+        t.codes, t.desc.codes, t.desc.code_stride = wide, wide.data_ptr(), 512
+    assert torch.equal(y, polyq_lib.fp4_linear(x, w))
+    src = torch.randn(M, K, generator=g, device="cuda")
+    d = polyq_lib._dense(src, "x")
+    rc = polyq_lib._lib.polyq_fp4_quantize(C.byref(d), C.byref(x.desc), polyq_lib._stream_ptr(None))
+    assert rc == 0
+    want = polyq_lib.fp4_quantize(src, fmt, x.tensor_scale)
+    assert torch.equal(x.codes[:, :(K + 1) // 2], want.codes[:, :(K + 1) // 2])
+    assert bool((x.codes[:, 176:] == 0x77).all())  # 16-byte rows: 176 bytes of 333 codes
+
+
+@pytest.mark.parametrize("fmt", [MX, NV])
+@pytest.mark.parametrize("M,N", [(1, 8), (40, 130), (300, 257)])
+def test_long_contraction(polyq_lib, fmt, M, N):
+    """A million products a sum."""
+    K = (1 << 20) + 37
+    g = _gen(M)
+    x, w = _q(polyq_lib, g, M, K, fmt), _q(polyq_lib, g, N, K, fmt)
+    xv, wv = _values(polyq_lib, x), _values(polyq_lib, w)
+    ref, S = xv @ wv.T, xv.abs() @ wv.abs().T
+    _check(polyq_lib.fp4_linear(x, w), ref, _sum_bound(S, K, 64, 100), "y")
+    assert float((polyq_lib.fp4_linear(x, w).double() - ref).norm() / ref.norm()) < 1e-3
+
+
 def test_python_refusals_on_the_gpu(polyq_lib):
     x = torch.randn(8, 64, device="cuda")
     q = polyq_lib.fp4_quantize(x)
