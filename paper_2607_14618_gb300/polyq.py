@@ -970,17 +970,13 @@ def fp4_ffn(x: Fp4Tensor, gate: Fp4Tensor, up: Fp4Tensor, h=None, dtype=None, wo
     return h
 
 
-def _saved_bytes(T, F):
-    n = C.c_size_t()
-    _check(_lib.polyq_ffn_saved_bytes(int(T), int(F), C.byref(n)))
-    return n.value
-
-
 def ffn_saved(T, F, dtype=None, device="cuda"):
     """The buffer that ffn_forward fills for ffn_backward (the same for every
     dtype of the operands)."""
     import torch
-    return torch.empty(_saved_bytes(T, F), dtype=torch.uint8, device=device)
+    n = C.c_size_t()
+    _check(_lib.polyq_ffn_saved_bytes(int(T), int(F), C.byref(n)))
+    return torch.empty(n.value, dtype=torch.uint8, device=device)
 
 
 def ffn_workspace(T, F, K=None, device="cuda"):
@@ -1001,8 +997,9 @@ def _ffn_inputs(x, gate, up, stream):
 
 
 def _saved(saved, T, F, dev):
+    # the size that polyq_ffn_saved_bytes gives: 6 bytes an element of rows padded to 32
     if (saved.element_size() != 1 or saved.get_device() != dev or not saved.is_contiguous()
-            or saved.numel() != _saved_bytes(T, F)):
+            or saved.numel() != 6 * T * ((F + 31) & -32)):
         raise ValueError(f"saved must be ffn_saved({T}, {F}) on cuda:{dev}")
     return saved.data_ptr()
 
@@ -1042,9 +1039,10 @@ def ffn_backward(x, gate, up, saved, dh, dx=None, dgate=None, dup=None, need_dx=
         dgate = new(F, dup)
     if dup is None and need_weights:
         dup = new(F, dgate)
-    outs = [None if t is None else C.byref(_dense(t, n, r, K, dev)) for t, n, r in
-            ((dx, "dx", T), (dgate, "dgate", F), (dup, "dup", F))]
+    ox = None if dx is None else C.byref(_dense(dx, "dx", T, K, dev))
+    og = None if dgate is None else C.byref(_dense(dgate, "dgate", F, K, dev))
+    ou = None if dup is None else C.byref(_dense(dup, "dup", F, K, dev))
     ws = _workspace_at(workspace, dev, lambda: ffn_workspace(T, F, K, x.device))
     _check(_lib.polyq_ffn_backward(C.byref(ix), C.byref(ig), C.byref(iu), T, F, K, ps, C.byref(idh),
-                                   *outs, ws.data_ptr(), ws.numel(), st))
+                                   ox, og, ou, ws.data_ptr(), ws.numel(), st))
     return dx, dgate, dup
