@@ -67,7 +67,7 @@ struct MmParams {
   void* y[2];
   const void* res;
   int64_t y_stride, res_stride;
-  int type, vec;           // vec: rows of y start on 8 (1), 16 (2) or 32 bytes (3), and of res on 8
+  int type, vec;           // vec: rows of y and res start on 8 (1), 16 (2) or 32 bytes (3)
   uint8_t *codes, *scales;
   int64_t code_stride, out_atoms;
   int qfmt;                // 0, kMx or kNv
@@ -139,32 +139,41 @@ __device__ __forceinline__ void store_row32(void* y, int64_t off, const float (&
     }
   }
 }
-__device__ __forceinline__ void add_row32(const void* r, int64_t off, float (&v)[32], int type) {
+// The lane's 32 consecutive residual values as they lie in memory (16-bit types:
+// the first half of w), and their sum with v.
+__device__ __forceinline__ void load_row32(const void* r, int64_t off, uint32_t (&w)[32], int type, int vec) {
+  const uint8_t* p = (const uint8_t*)r + off * (type == POLYQ_F32 ? 4 : 2);
+#pragma unroll
+  for (int i = 0; i < 32; i += 8) {
+    if (i == 16 && type != POLYQ_F32) break;
+    if (vec == 3) {
+      asm volatile("ld.global.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                   : "=r"(w[i]), "=r"(w[i + 1]), "=r"(w[i + 2]), "=r"(w[i + 3]), "=r"(w[i + 4]), "=r"(w[i + 5]),
+                     "=r"(w[i + 6]), "=r"(w[i + 7])
+                   : "l"(p + 4 * i)
+                   : "memory");
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; j += 2) {
+        const uint2 u = *reinterpret_cast<const uint2*>(p + 4 * (i + j));
+        w[i + j] = u.x;
+        w[i + j + 1] = u.y;
+      }
+    }
+  }
+}
+__device__ __forceinline__ void add_row32(const uint32_t (&w)[32], float (&v)[32], int type) {
   if (type == POLYQ_F32) {
-    const float2* s = reinterpret_cast<const float2*>((const float*)r + off);
+#pragma unroll
+    for (int i = 0; i < 32; ++i) v[i] += __uint_as_float(w[i]);
+  } else {
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-      const float2 f = s[i];
+      float2 f;
+      if (type == POLYQ_BF16) f = make_float2(bf16_lo(w[i]), bf16_hi(w[i]));
+      else f = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
       v[2 * i] += f.x;
       v[2 * i + 1] += f.y;
-    }
-  } else {
-    const uint2* s = reinterpret_cast<const uint2*>((const uint16_t*)r + off);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const uint2 u = s[i];
-      float2 a, b;
-      if (type == POLYQ_BF16) {
-        a = make_float2(bf16_lo(u.x), bf16_hi(u.x));
-        b = make_float2(bf16_lo(u.y), bf16_hi(u.y));
-      } else {
-        a = __half22float2(*reinterpret_cast<const __half2*>(&u.x));
-        b = __half22float2(*reinterpret_cast<const __half2*>(&u.y));
-      }
-      v[4 * i] += a.x;
-      v[4 * i + 1] += a.y;
-      v[4 * i + 2] += b.x;
-      v[4 * i + 3] += b.y;
     }
   }
 }
@@ -230,11 +239,8 @@ __device__ __forceinline__ void store_column(T* y, int64_t stride, const T* res,
 __device__ __forceinline__ void store_chunk(void* y, int64_t stride, const void* res, int64_t res_stride, int64_t m,
                                             int n, int64_t M, int64_t N, float (&v)[32], int type, int vec) {
   const int lane = threadIdx.x & 31;
-  if (vec && n + 32 <= N) {
-    if (m + lane < M) {
-      if (res) add_row32(res, (m + lane) * res_stride + n, v, type);
-      store_row32(y, (m + lane) * stride + n, v, type, vec);
-    }
+  if (vec && n + 32 <= N) {  // (the residual has been added)
+    if (m + lane < M) store_row32(y, (m + lane) * stride + n, v, type, vec);
   } else {
     transpose32(v);
     const int rows = n + lane < N ? (int)min((int64_t)32, M - m) : 0;
@@ -611,6 +617,21 @@ __global__ void __launch_bounds__(C::kThreads, 1) mm_pair(const __grid_constant_
       const int buf = tc & 1;
       const int64_t m = (int64_t)T.tm * kTileM + (int)rank * kHalf + 32 * q;  // the warp's first row
       const int n0 = C::GATED ? T.tn * kHalf : T.tn * kTileN;
+      // A warp's i-th chunk (GATED: of gate, and of up): the columns that the
+      // accumulators share are the first one's last and the second one's first.
+      auto chunk = [&](int i) { return C::OV > 0 && buf == 0 && T.shared < 0 ? kChunks - 1 - i : i; };
+      // A chunk's residual is asked for before its accumulator is complete, the
+      // next chunk's before this one's stores (512 x 5120 x 13824 MX: 28.2 us with
+      // loads of 8 bytes when they are needed, 23.5 so, 22.6 without a residual).
+      uint32_t res[C::GATED ? 1 : 32];
+      auto fetch_res = [&](int c) {
+        if constexpr (!C::GATED) {
+          const int n = n0 + 32 * c;
+          if (P.res && P.vec && n + 32 <= P.N && m + lane < P.M)
+            load_row32(P.res, (m + lane) * P.res_stride + n, res, P.type, P.vec);
+        }
+      };
+      fetch_res(chunk(e0));
       const int w = wait(smem_u32(&bar_accf[buf]), (tc >> 1) & 1, &s_abort);
       if (w != kOk) {
         if (w == kTimeout) fail(kStatusTimeoutFull);
@@ -626,7 +647,7 @@ __global__ void __launch_bounds__(C::kThreads, 1) mm_pair(const __grid_constant_
         released = true;
       };
       // a chunk's outputs from its accumulators (GATED: of gate and of up)
-      auto finish = [&](int c, uint32_t (&r0)[32], uint32_t (&r1)[C::GATED ? 32 : 1]) {
+      auto finish = [&](int c, int next, uint32_t (&r0)[32], uint32_t (&r1)[C::GATED ? 32 : 1]) {
         const int n = n0 + 32 * c;
         float v[32];
         if constexpr (C::GATED) {
@@ -650,6 +671,8 @@ __global__ void __launch_bounds__(C::kThreads, 1) mm_pair(const __grid_constant_
         } else {
 #pragma unroll
           for (int j = 0; j < 32; ++j) v[j] = __uint_as_float(r0[j]) * P.alpha[0];
+          if (P.res && P.vec && n + 32 <= P.N) add_row32(res, v, P.type);
+          if (next < kChunks) fetch_res(chunk(next));
           store_chunk(P.y[T.prob], P.y_stride, P.res, P.res_stride, m, n, P.M, P.N, v, P.type, P.vec);
         }
       };
@@ -660,9 +683,6 @@ __global__ void __launch_bounds__(C::kThreads, 1) mm_pair(const __grid_constant_
         tc_regs_ready(r0);
         tc_regs_ready(r1);
       };
-      // A warp's i-th chunk (GATED: of gate, and of up): the columns that the
-      // accumulators share are the first one's last and the second one's first.
-      auto chunk = [&](int i) { return C::OV > 0 && buf == 0 && T.shared < 0 ? kChunks - 1 - i : i; };
       // whether a chunk has an output (4 bits: a scale or a code) of this matrix
       auto inside = [&](int c) { return m < P.M && (P.qfmt != 0 || n0 + 32 * c < P.N); };
       // A part goes into its slot; the warp that finds the other parts of its
@@ -745,7 +765,8 @@ __global__ void __launch_bounds__(C::kThreads, 1) mm_pair(const __grid_constant_
           uint32_t r0[32], r1[C::GATED ? 32 : 1];
           load(c, r0, r1);
           if (C::OV > 0 && !released && T.shared < 0 && i + C::EPQ >= kOvChunks) release();
-          if (inside(c)) finish(c, r0, r1);
+          if (inside(c)) finish(c, i + C::EPQ, r0, r1);
+          else if (i + C::EPQ < kChunks) fetch_res(chunk(i + C::EPQ));
         }
       }
       __syncwarp();
@@ -1527,7 +1548,7 @@ extern "C" int polyq_fp4_linear(const polyq_fp4* x, const polyq_fp4* w, const po
   P.y[0] = y->data;
   P.y_stride = y->stride;
   P.type = y->type;
-  P.vec = residual && !vec_rows(residual) ? 0 : vec_rows(y);
+  P.vec = std::min(vec_rows(y), residual ? vec_rows(residual) : 3);
   P.res = residual ? residual->data : nullptr;
   P.res_stride = residual ? residual->stride : 0;
   P.status = (int*)workspace;

@@ -130,7 +130,8 @@ def test_linear_matches_oracle(polyq_lib, fmt, M, N, K):
 @pytest.mark.parametrize("fmt", [O.MX, O.NV])
 @pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
 @pytest.mark.parametrize("M,N,K,pad,offset", [(5, 300, 512, 0, 0), (5, 77, 512, 3, 1), (300, 256, 320, 0, 0),
-                                              (300, 200, 320, 8, 8), (300, 77, 320, 3, 1), (513, 600, 64, 1, 0)])
+                                              (300, 200, 320, 8, 8), (300, 77, 320, 3, 1), (513, 600, 64, 1, 0),
+                                              (2500, 200, 320, 0, 0), (2500, 136, 320, 4, 4), (2500, 300, 320, 24, 8)])
 def test_linear_types_strides_residual(polyq_lib, fmt, dtype, M, N, K, pad, offset):
     rng = np.random.default_rng(M + N + K)
     qx, x = _tensor(polyq_lib, rng, M, K, fmt)
