@@ -890,10 +890,20 @@ def fp4_workspace(device="cuda"):
     return _zero_headed(n, device)
 
 
-def _workspace_at(workspace, dev, make):
+def _made(stream, make, *args, **kw):
+    """A buffer of make(*args, **kw) that belongs to `stream`: with one that is not
+    the current stream, zeroing and reuse of its memory are ordered with the call."""
+    if stream is None:
+        return make(*args, **kw)
+    import torch
+    with torch.cuda.stream(stream):
+        return make(*args, **kw)
+
+
+def _workspace_at(workspace, dev, stream, make, *args):
     """The caller's workspace, checked, or a new one (the library checks its size)."""
     if workspace is None:
-        return make()
+        return _made(stream, make, *args)
     import torch
     if (workspace.dtype != torch.uint8 or workspace.get_device() != dev
             or not workspace.is_contiguous()):
@@ -908,7 +918,7 @@ def fp4_quantize(x, format=FP4_MX, tensor_scale=1.0, out=None, stream=None):
     dev = x.get_device()
     st = _stream_on(dev, "x", stream)
     if out is None:
-        out = Fp4Tensor.empty(x.shape[0], x.shape[1], format, tensor_scale, x.device)
+        out = _made(stream, Fp4Tensor.empty, x.shape[0], x.shape[1], format, tensor_scale, x.device)
     o = _fp4(out, "out", dev)
     if (out.rows, out.K) != x.shape:
         raise ValueError(f"out is [{out.rows}][{out.K}], x {list(x.shape)}")
@@ -923,7 +933,8 @@ def fp4_dequantize(t: Fp4Tensor, dtype=None, out=None, stream=None):
     st = _stream_on(dev, "t", stream)
     if out is None:
         import torch
-        out = torch.empty((t.rows, t.K), dtype=dtype or torch.float32, device=t.codes.device)
+        out = _made(stream, torch.empty, (t.rows, t.K), dtype=dtype or torch.float32,
+                    device=t.codes.device)
     d = _dense(out, "out", t.rows, t.K, dev, dtype)
     _check(_lib.polyq_fp4_dequantize(p, C.byref(d), st))
     return out
@@ -940,11 +951,11 @@ def fp4_linear(x: Fp4Tensor, w: Fp4Tensor, y=None, residual=None, dtype=None, wo
     st = _stream_on(dev, "x", stream)
     if y is None:
         import torch
-        y = torch.empty((x.rows, w.rows), dtype=dtype or (residual.dtype if residual is not None
-                                                          else torch.float32), device=x.codes.device)
+        y = _made(stream, torch.empty, (x.rows, w.rows), device=x.codes.device,
+                  dtype=dtype or (residual.dtype if residual is not None else torch.float32))
     dy = _dense(y, "y", x.rows, w.rows, dev, dtype)
     dr = None if residual is None else C.byref(_dense(residual, "residual", x.rows, w.rows, dev, y.dtype))
-    ws = _workspace_at(workspace, dev, lambda: fp4_workspace(x.codes.device))
+    ws = _workspace_at(workspace, dev, stream, fp4_workspace, x.codes.device)
     _check(_lib.polyq_fp4_linear(px, pw, dr, C.byref(dy), ws.data_ptr(), ws.numel(), st))
     return y
 
@@ -959,13 +970,14 @@ def fp4_ffn(x: Fp4Tensor, gate: Fp4Tensor, up: Fp4Tensor, h=None, dtype=None, wo
     st = _stream_on(dev, "x", stream)
     if h is None:
         import torch
-        h = torch.empty((x.rows, gate.rows), dtype=dtype or torch.bfloat16, device=x.codes.device)
+        h = _made(stream, torch.empty, (x.rows, gate.rows), dtype=dtype or torch.bfloat16,
+                  device=x.codes.device)
     dh = dq = None
     if isinstance(h, Fp4Tensor):
         dq = _fp4(h, "h", dev)
     else:
         dh = C.byref(_dense(h, "h", x.rows, gate.rows, dev, dtype))
-    ws = _workspace_at(workspace, dev, lambda: fp4_workspace(x.codes.device))
+    ws = _workspace_at(workspace, dev, stream, fp4_workspace, x.codes.device)
     _check(_lib.polyq_fp4_ffn(px, pg, pu, dh, dq, ws.data_ptr(), ws.numel(), st))
     return h
 
@@ -1010,10 +1022,10 @@ def ffn_forward(x, gate, up, h=None, saved=None, workspace=None, stream=None):
     ix, ig, iu, T, F, K, dev, st = _ffn_inputs(x, gate, up, stream)
     if h is None:
         import torch
-        h = torch.empty((T, F), dtype=x.dtype, device=x.device)
+        h = _made(stream, torch.empty, (T, F), dtype=x.dtype, device=x.device)
     ih = _dense(h, "h", T, F, dev, x.dtype)
     ps = None if saved is None else _saved(saved, T, F, dev)
-    ws = _workspace_at(workspace, dev, lambda: fp4_workspace(x.device))
+    ws = _workspace_at(workspace, dev, stream, fp4_workspace, x.device)
     _check(_lib.polyq_ffn_forward(C.byref(ix), C.byref(ig), C.byref(iu), T, F, K, C.byref(ih), ps,
                                   ws.data_ptr(), ws.numel(), st))
     return h
@@ -1031,7 +1043,8 @@ def ffn_backward(x, gate, up, saved, dh, dx=None, dgate=None, dup=None, need_dx=
 
     def new(n, like):
         import torch
-        return torch.empty((n, K), dtype=ty if like is None else like.dtype, device=x.device)
+        return _made(stream, torch.empty, (n, K), dtype=ty if like is None else like.dtype,
+                     device=x.device)
 
     if dx is None and need_dx:
         dx = new(T, None)
@@ -1042,7 +1055,7 @@ def ffn_backward(x, gate, up, saved, dh, dx=None, dgate=None, dup=None, need_dx=
     ox = None if dx is None else C.byref(_dense(dx, "dx", T, K, dev))
     og = None if dgate is None else C.byref(_dense(dgate, "dgate", F, K, dev))
     ou = None if dup is None else C.byref(_dense(dup, "dup", F, K, dev))
-    ws = _workspace_at(workspace, dev, lambda: ffn_workspace(T, F, K, x.device))
+    ws = _workspace_at(workspace, dev, stream, ffn_workspace, T, F, K, x.device)
     _check(_lib.polyq_ffn_backward(C.byref(ix), C.byref(ig), C.byref(iu), T, F, K, ps, C.byref(idh),
                                    ox, og, ou, ws.data_ptr(), ws.numel(), st))
     return dx, dgate, dup

@@ -198,6 +198,26 @@ def test_streams_with_their_own_workspaces(polyq_lib):
     assert all(torch.equal(p, q) for p, q in zip(alone, outs))
 
 
+def test_buffers_made_for_a_given_stream(polyq_lib):
+    """Without buffers of the caller's, on a stream that is not the current one,
+    while the current one is busy: the new workspace is zeroed on that stream."""
+    g = _gen(4)
+    x, w = _q(polyq_lib, g, 2304, 7000, MX), _q(polyq_lib, g, 2560, 7000, MX)  # shares its last wave
+    h = torch.randn(300, 512, generator=g, device="cuda").bfloat16()
+    want = (polyq_lib.fp4_linear(x, w), polyq_lib.fp4_ffn(x, w, w), polyq_lib.ffn_forward(h, h, h))
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for _ in range(3):
+        junk = torch.full((64 << 20,), 255, dtype=torch.uint8, device="cuda")  # what new memory may hold
+        del junk
+        torch.cuda._sleep(20_000_000)
+        got = (polyq_lib.fp4_linear(x, w, stream=side), polyq_lib.fp4_ffn(x, w, w, stream=side),
+               polyq_lib.ffn_forward(h, h, h, stream=side))
+        side.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+    torch.cuda.synchronize()
+
+
 def test_training_step_captured(polyq_lib):
     """Forward and backward in a CUDA graph, replayed after the inputs changed."""
     T, F, K, t = 300, 264, 136, torch.bfloat16
