@@ -1264,13 +1264,13 @@ size_t workspace_bytes_of(int sms) { return kPartsOff + (size_t)sms * kTileM * k
 // Returns the last wave's stages.
 // (256 x 1024 x 13824 4 bits, 4 tiles: 19.9 us whole, 18.0 / 17.0 / 18.6 in 2 / 3 / 6
 // parts; 5120 instead of 13824 11.1, 13.7 in 2.  16-bit, 4 tiles of 160 stages
-// beside 76 whole ones 105 us, 72 in 4.)
-constexpr double kShareCost = 11, kPartCost = 4.5;
+// beside 76 whole ones 105 us, 72 in 4; 24 tiles of 48 stages 21 us, 25 in 3.)
+constexpr double kShareCost = 13, kPartCost = 4.5;
 double plan_tiles(MmParams& P, int pairs) {
   const int n_it = P.segs * P.kt, rest = P.tiles % pairs;
   P.sk_tiles = P.sk_pairs = P.sk_parts = P.sk_share = P.sk_extra = 0;
   if (rest == 0) return 0;
-  double best = 0.95 * n_it, last = n_it;
+  double best = 0.85 * n_it, last = n_it;
   for (int s = 2; s * rest <= pairs && s <= n_it; ++s) {
     const double t = (n_it + s - 1) / s + kShareCost + kPartCost * s;
     if (t < best) {
@@ -1313,14 +1313,26 @@ struct Plan {
 template <class C>
 constexpr double few_base() {
   return C::GATED ? (C::NT == 16 ? 4.2 : C::NT == 32 ? 4.6 : C::NT == 64 ? 5.5 : 8.0)
-                  : (C::NT == 16 ? 3.3 : C::NT == 32 ? 3.5 : C::NT == 64 ? 3.8 : 5.2);
+                  : (C::NT == 16 ? 3.3 : C::NT == 32 ? 3.5 : C::NT == 64 ? 3.8 : 5.6);
 }
 template <class C>
 constexpr double few_stage() {
-  if (C::KIND == k16) return C::GATED ? (C::NT == 128 ? 0.75 : C::NT == 64 ? 0.57 : 0.45) : (C::NT == 128 ? 0.40 : 0.32);
+  if (C::KIND == k16) return C::GATED ? (C::NT == 128 ? 0.50 : 0.36) : (C::NT == 128 ? 0.38 : 0.28);
   return C::GATED ? (C::NT == 128 ? 0.55 : C::NT == 64 ? 0.385 : 0.35) : (C::NT == 128 ? 0.30 : 0.28);
 }
-constexpr double kFewSplit = 0.5, kPairBase = 5.4, kPairStage = 0.27, kPairWave = 1.6;
+// A cluster's exchange; a pair launch, its stages and each further wave; what
+// saved values and rows that start on 8 or fewer bytes (16-bit outputs of N % 8
+// columns) add to its epilogue; the weights from HBM, bytes a us.  The plan goes
+// by formats and sizes alone: outputs of another type or stride, or in 4 bits,
+// and a call without saved values are the same sums in the same order.
+constexpr double kFewSplit = 0.5, kPairBase = 5.4, kPairStage = 0.27, kPairStage16 = 0.30, kPairWave = 1.6;
+constexpr double kPairSaved = 1.5, kPairRows8 = 1.5, kPairRowsOdd = 3.0, kHbm = 6.4e6;
+
+// Bytes of the weights: P.N rows of every matrix or segment.
+template <class C>
+double weight_bytes(const MmParams& P) {
+  return (double)P.N * P.kt * P.segs * C::MATS * kRowBytes;
+}
 
 // P.M tokens, P.N weight rows, P.segs and P.kt are set.
 template <class C>
@@ -1332,8 +1344,9 @@ int consider_few(const MmParams& P, int dev, Plan* best, const char* who) {
     int fit = 0;
     const int rc = resident_clusters((const void*)mm_few<C>, C::kThreads, C::kSmem, s, &cached[dev][s - 1], &fit, who);
     if (rc) return rc;
-    const double us = (double)((tiles + fit - 1) / fit) *
-                      (few_base<C>() + few_stage<C>() * ((n_it + s - 1) / s) + (s > 1 ? kFewSplit : 0.0));
+    const double us = std::max((double)((tiles + fit - 1) / fit) * (few_base<C>() + few_stage<C>() * ((n_it + s - 1) / s) +
+                                                                    (s > 1 ? kFewSplit : 0.0)),
+                               few_base<C>() + weight_bytes<C>(P) / kHbm);
     if (us < 0.98 * best->us) *best = {C::NT, s, us};
   }
   return POLYQ_OK;
@@ -1356,7 +1369,9 @@ int consider_pair(MmParams& P, int dev, Plan* best, const char* who) {
   const double last = plan_tiles(P, pairs);
   P.grid_pairs = P.tiles > pairs ? pairs : std::max(P.tiles, P.sk_pairs);
   const double waves = (double)(P.tiles / pairs);
-  const double us = kPairBase + kPairStage * (waves * P.segs * P.kt + last) + kPairWave * (waves + (last > 0) - 1);
+  const double epilogue = (C::KIND == k16 && C::GATED ? kPairSaved : 0.0) + (P.N % 8 == 0 ? 0.0 : P.N % 4 == 0 ? kPairRows8 : kPairRowsOdd);
+  const double us = kPairBase + epilogue + (C::KIND == k16 ? kPairStage16 : kPairStage) * (waves * P.segs * P.kt + last) +
+                    kPairWave * (waves + (last > 0) - 1);
   if (us < best->us) *best = {0, 1, us};
   return POLYQ_OK;
 }
@@ -1369,7 +1384,7 @@ int plan_product(MmParams& P, int dev, Plan* plan, const char* who) {
   if (!rc && P.M > 16 && P.M <= 32) rc = consider_few<Few<KIND, 32, GATED>>(P, dev, plan, who);
   // (with more tokens than fill every SM's tile the pairs are far ahead)
   if (!rc && P.M > 32 && P.M <= kFewTokens) rc = consider_few<Few<KIND, 64, GATED>>(P, dev, plan, who);
-  if (!rc && P.M > 64 && P.M <= kFewTokens) rc = consider_few<Few<KIND, 128, GATED>>(P, dev, plan, who);
+  if (!rc && P.M > 32 && P.M <= kFewTokens) rc = consider_few<Few<KIND, 128, GATED>>(P, dev, plan, who);
   return rc;
 }
 
