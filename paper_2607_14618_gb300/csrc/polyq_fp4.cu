@@ -54,6 +54,9 @@ struct Elem<__half> {
 // 8 elements from k on as they lie in memory, and as floats; zeros past K.  VEC:
 // rows start on 16 bytes.  (Two steps, so that the loads of several rows are in
 // flight before the first is converted: 13824 x 5120 bf16 63 us with one.)
+// Inputs are read through L2: a grid may be on its SM before the one that writes
+// them has begun, and lines that an earlier grid left in that SM's L1, or read
+// only loads, would be older than the wait.
 template <typename T>
 struct Raw8 {
   uint4 w[sizeof(T) * 8 / 16];
@@ -63,11 +66,11 @@ __device__ __forceinline__ void load8(const T* __restrict__ row, int64_t k, int6
   constexpr int N16 = sizeof(T) * 8 / 16;
   if (FULL || k + 8 <= K) {
 #pragma unroll
-    for (int i = 0; i < N16; ++i) r.w[i] = __ldg(reinterpret_cast<const uint4*>(row + k) + i);
+    for (int i = 0; i < N16; ++i) r.w[i] = __ldcg(reinterpret_cast<const uint4*>(row + k) + i);
   } else {
     alignas(16) T e[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) e[i] = k + i < K ? row[k + i] : Elem<T>::from(0.f);
+    for (int i = 0; i < 8; ++i) e[i] = k + i < K ? __ldcg(row + k + i) : Elem<T>::from(0.f);
 #pragma unroll
     for (int i = 0; i < N16; ++i) r.w[i] = reinterpret_cast<const uint4*>(e)[i];
   }
@@ -80,7 +83,7 @@ template <typename T>
 __device__ __forceinline__ void strided_load(const T* __restrict__ row, int64_t k0, int64_t K, T (&e)[8]) {
   const int lane = threadIdx.x & 31;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) e[i] = k0 + 32 * i + lane < K ? row[k0 + 32 * i + lane] : Elem<T>::from(0.f);
+  for (int i = 0; i < 8; ++i) e[i] = k0 + 32 * i + lane < K ? __ldcg(row + k0 + 32 * i + lane) : Elem<T>::from(0.f);
 }
 template <typename T>
 __device__ __forceinline__ void strided_turn(const T (&e)[8], T* buf, Raw8<T>& r) {
@@ -207,8 +210,8 @@ __global__ void __launch_bounds__(32 * kWarps) dequantize_kernel(const __grid_co
 #pragma unroll
     for (int i = 0; i < ROWS; ++i) {
       const int at = (int)min((int64_t)i, P.rows - 1 - r0);  // (past the last row: the last one again)
-      c[i] = in ? __ldg(reinterpret_cast<const uint32_t*>(cp + at * P.code_stride)) : 0u;  // (rows are padded)
-      sb[i] = in ? __ldg(sp + 16 * at) : 0u;
+      c[i] = in ? __ldcg(reinterpret_cast<const uint32_t*>(cp + at * P.code_stride)) : 0u;  // (rows are padded)
+      sb[i] = in ? __ldcg(sp + 16 * at) : 0u;
     }
 #pragma unroll
     for (int i = 0; i < ROWS; ++i) {

@@ -1133,7 +1133,8 @@ __global__ void __launch_bounds__(C::kThreads, 1) mm_few(const __grid_constant__
 // gradients of the activation and the product
 // ---------------------------------------------------------------------------
 // da = dh u s (1 + a (1 - s)), du = dh a s with s = 1 / (1 + exp(-a)); 8
-// elements a thread.  One pass over a, u, dh; bound by HBM.
+// elements a thread.  One pass over a, u, dh; bound by HBM.  Read through L2, as
+// the grid may be on its SM before the one that writes them has begun.
 struct ActParams {
   const uint8_t* saved;  // save_row32's planes
   const void* dh;
@@ -1154,19 +1155,19 @@ __global__ void __launch_bounds__(256) act_backward(const __grid_constant__ ActP
     uint2 lo[2];
 #pragma unroll
     for (int w = 0; w < 2; ++w) {
-      hi[w] = __ldg(reinterpret_cast<const uint4*>(P.saved + 2 * (w * plane + at)));
-      lo[w] = __ldg(reinterpret_cast<const uint2*>(P.saved + (4 + w) * plane + at));
+      hi[w] = __ldcg(reinterpret_cast<const uint4*>(P.saved + 2 * (w * plane + at)));
+      lo[w] = __ldcg(reinterpret_cast<const uint2*>(P.saved + (4 + w) * plane + at));
     }
     uint32_t d[4], da[4], du[4];
     const uint16_t* dr = (const uint16_t*)P.dh + t * P.dh_stride + f;
     const int n = (int)(P.F - f < 8 ? P.F - f : 8);
     if (P.vec && n == 8) {
-      const uint4 dv = __ldg(reinterpret_cast<const uint4*>(dr));
+      const uint4 dv = __ldcg(reinterpret_cast<const uint4*>(dr));
       d[0] = dv.x, d[1] = dv.y, d[2] = dv.z, d[3] = dv.w;
     } else {
 #pragma unroll
       for (int j = 0; j < 4; ++j)
-        d[j] = (2 * j < n ? dr[2 * j] : 0u) | (uint32_t)(2 * j + 1 < n ? dr[2 * j + 1] : 0u) << 16;
+        d[j] = (2 * j < n ? __ldcg(dr + 2 * j) : 0u) | (uint32_t)(2 * j + 1 < n ? __ldcg(dr + 2 * j + 1) : 0u) << 16;
     }
     auto value = [](const uint4& h, const uint2& l, int j) {  // element j of the eight
       const uint32_t hw = j < 2 ? h.x : j < 4 ? h.y : j < 6 ? h.z : h.w, lw = j < 4 ? l.x : l.y;

@@ -185,6 +185,49 @@ def test_captured_and_replayed(polyq_lib, M):
         assert torch.equal(got, run())
 
 
+def test_short_calls_over_the_same_buffers(polyq_lib):
+    """Launches that overlap in a graph read what the one before them wrote, not
+    what the buffer held in an earlier call."""
+    n, T, F, K = 40, 8, 96, 64
+    g = _gen(11)
+    x = torch.randn(n, T, K, generator=g, device="cuda").bfloat16()
+    gate, up = (torch.randn(F, K, generator=g, device="cuda").bfloat16() for _ in range(2))
+    dh = torch.randn(T, F, generator=g, device="cuda").bfloat16()
+    w = _q(polyq_lib, g, 200, F, MX)
+    ws = polyq_lib.ffn_workspace(T, F)
+
+    def buffers():
+        return (torch.empty(T, F, dtype=torch.bfloat16, device="cuda"), polyq_lib.ffn_saved(T, F),
+                polyq_lib.Fp4Tensor.empty(T, F, MX), torch.empty(T, F, device="cuda"))
+
+    def run(x, h, saved, q, v, y, dx):
+        polyq_lib.ffn_forward(x, gate, up, h=h, saved=saved, workspace=ws)
+        polyq_lib.fp4_quantize(h, out=q)
+        polyq_lib.fp4_dequantize(q, out=v)
+        polyq_lib.fp4_linear(q, w, y=y, workspace=ws)
+        polyq_lib.ffn_backward(x, gate, up, saved, dh, dx=dx, need_weights=False, workspace=ws)
+        polyq_lib.fp4_quantize(v, out=q)
+
+    def outs():
+        return torch.empty(n, T, 200, device="cuda"), torch.empty(n, T, K, dtype=torch.bfloat16, device="cuda")
+
+    (y, dx), (y1, dx1) = outs(), outs()
+    for i in range(n):
+        run(x[i], *buffers(), y1[i], dx1[i])
+        torch.cuda.synchronize()
+    shared = buffers()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        for i in range(n):
+            run(x[i], *shared, y[i], dx[i])
+    for _ in range(3):
+        y.fill_(float("nan"))
+        dx.fill_(float("nan"))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(y, y1) and torch.equal(dx, dx1)
+
+
 def test_streams_with_their_own_workspaces(polyq_lib):
     """Two blocks at once on two streams, each with its buffers, give what they
     give alone; a given stream is used although another is current."""
