@@ -797,7 +797,9 @@ def _dense(t, name, rows=None, cols=None, dev=None, dtype=None):
 class Fp4Tensor:
     """A [rows][K] tensor in microscaled 4-bit floating point on the device:
     `codes` uint8 [rows][code_stride] and `scales` uint8 as polyq_fp4.h lays
-    them out, `format` FP4_MX or FP4_NV, `tensor_scale` (FP4_NV)."""
+    them out, `format` FP4_MX or FP4_NV, `tensor_scale` (FP4_NV).  The fields are
+    fixed, as the descriptor that the calls take holds them; the buffers' contents
+    are not."""
 
     def __init__(self, codes, scales, rows, K, format, tensor_scale=1.0):
         import torch
@@ -805,12 +807,14 @@ class Fp4Tensor:
         _check(_lib.polyq_fp4_bytes(int(rows), int(K), int(format), C.byref(stride), C.byref(nbytes)))
         _require(codes, "codes", torch.uint8, (rows, stride.value), codes.device)
         _require(scales, "scales", torch.uint8, (nbytes.value,), codes.device)
-        self.codes, self.scales = codes, scales
-        self.rows, self.K, self.format = int(rows), int(K), int(format)
-        self.tensor_scale = float(tensor_scale)
-        self.desc = Fp4Desc(codes.data_ptr(), scales.data_ptr(), self.rows, self.K, stride.value,
-                            self.format, self.tensor_scale)
-        self.device_index = codes.get_device()
+        rows, K, format, tensor_scale = int(rows), int(K), int(format), float(tensor_scale)
+        self.__dict__.update(
+            codes=codes, scales=scales, rows=rows, K=K, format=format, tensor_scale=tensor_scale,
+            desc=Fp4Desc(codes.data_ptr(), scales.data_ptr(), rows, K, stride.value, format, tensor_scale),
+            device_index=codes.get_device())
+
+    def __setattr__(self, name, value):
+        raise AttributeError(f"{name}: an Fp4Tensor's fields are fixed; make another one of its buffers")
 
     @classmethod
     def empty(cls, rows, K, format=FP4_MX, tensor_scale=1.0, device="cuda"):

@@ -209,3 +209,14 @@ def test_pack_and_unpack_on_the_host(polyq_lib):
     assert [int(t.scales[i]) for i in (0, 1, 16, 17, 32, 33)] == [1, 2, 3, 4, 5, 6]
     c, s = t.unpack()
     assert torch.equal(c, codes) and torch.equal(s, scales)
+
+
+@pytest.mark.parametrize("name", ["codes", "scales", "rows", "K", "format", "tensor_scale", "desc", "other"])
+def test_fields_are_fixed(polyq_lib, name):
+    """A field that changed behind the descriptor would be ignored, or free what it points to."""
+    t = polyq_lib.Fp4Tensor.empty(5, 40, polyq_lib.FP4_NV, 0.5, device="cpu")
+    with pytest.raises(AttributeError):
+        setattr(t, name, getattr(t, name, 1))
+    assert (t.rows, t.K, t.format, t.tensor_scale) == (5, 40, polyq_lib.FP4_NV, 0.5)
+    again = polyq_lib.Fp4Tensor(t.codes, t.scales, t.rows, t.K, t.format, 0.25)
+    assert again.desc.tensor_scale == 0.25 and again.desc.codes == t.desc.codes
