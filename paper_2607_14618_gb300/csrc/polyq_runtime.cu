@@ -5,6 +5,7 @@
 #include <cstring>
 #include <map>
 #include <mutex>
+#include <new>
 #include <tuple>
 
 #include "polyq_dev.cuh"
@@ -92,7 +93,10 @@ int polyq_tensor_map_2d(CUtensorMap* out, const void* base, int elem_bytes, uint
   if (r != CUDA_SUCCESS)
     return polyq_set_error(POLYQ_ECUDA, "cuTensorMapEncodeTiled failed (%d)", (int)r);
   if (g_maps.size() > 4096) g_maps.clear();
-  g_maps.emplace(k, m);
+  try {
+    g_maps.emplace(k, m);
+  } catch (const std::bad_alloc&) {  // the next call encodes it again
+  }
   *out = m;
   return POLYQ_OK;
 }
