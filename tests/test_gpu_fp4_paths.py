@@ -344,19 +344,22 @@ def test_code_rows_of_a_wider_buffer(polyq_lib, fmt):
     M, N, K = 150, 140, 333
     x, w = _q(polyq_lib, g, M, K, fmt), _q(polyq_lib, g, N, K, fmt)
     y = polyq_lib.fp4_linear(x, w)
+    buffers = []
     for t in (x, w):
         wide = torch.full((t.rows, 512), 0x77, dtype=torch.uint8, device="cuda")
         wide[:, :t.codes.shape[1]] = t.codes
         wide[:, (K + 1) // 2:] = 0x77  # also the padding of the narrow rows
-        t.codes, t.desc.codes, t.desc.code_stride = wide, wide.data_ptr(), 512
+        t.desc.codes, t.desc.code_stride = wide.data_ptr(), 512
+        buffers.append(wide)
     assert torch.equal(y, polyq_lib.fp4_linear(x, w))
     src = torch.randn(M, K, generator=g, device="cuda")
     d = polyq_lib._dense(src, "x")
     rc = polyq_lib._lib.polyq_fp4_quantize(C.byref(d), C.byref(x.desc), polyq_lib._stream_ptr(None))
     assert rc == 0
     want = polyq_lib.fp4_quantize(src, fmt, x.tensor_scale)
-    assert torch.equal(x.codes[:, :(K + 1) // 2], want.codes[:, :(K + 1) // 2])
-    assert bool((x.codes[:, 176:] == 0x77).all())  # 16-byte rows: 176 bytes of 333 codes
+    got = buffers[0]
+    assert torch.equal(got[:, :(K + 1) // 2], want.codes[:, :(K + 1) // 2])
+    assert bool((got[:, 176:] == 0x77).all())  # 16-byte rows: 176 bytes of 333 codes
 
 
 @pytest.mark.parametrize("fmt", [MX, NV])
