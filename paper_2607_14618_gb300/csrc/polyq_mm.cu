@@ -43,6 +43,15 @@ constexpr int kOpBytes = kHalf * kRowBytes;
 constexpr int kSmemMax = 227 * 1024 - 1024;  // less the static barriers
 constexpr int kMaxDevices = 64;
 
+// Division of 32-bit numbers by a d known at launch: n / d is the upper half of
+// n * ceil(2^64 / d), exact for every n (Lemire, Kaser, Kurz: Faster remainder by
+// direct computation, 2019).  mul is 0 for d = 1.
+struct Divisor {
+  uint64_t mul;
+  __host__ void set(uint32_t d) { mul = d > 1 ? ~0ull / d + 1 : 0; }
+  __device__ __forceinline__ int of(int n) const { return mul ? (int)__umul64hi(mul, (uint64_t)(uint32_t)n) : n; }
+};
+
 struct MmParams {
   CUtensorMap a[2], b[2];  // operand tiles (per segment, problem or matrix, see below)
   CUtensorMap sa, sb[2];   // scales, rows of one atom
@@ -51,6 +60,7 @@ struct MmParams {
   int segs;                // segments of the contraction: a[s] with b[s]
   int probs;               // problems: a[p] with b[0]
   int tiles_m, tiles_n, tiles;
+  Divisor per_prob, per_band, last_band;  // by tiles of a problem, of eight row tiles, by rows of the last band
   // mm_pair: the first sk_tiles tiles are shared along the contraction by the
   // pairs b < sk_pairs: sk_parts pairs a tile (even parts), or with sk_parts 0
   // all of their stages in tile order, sk_share a pair (the first sk_extra pairs
@@ -368,16 +378,15 @@ struct Tiles {
     }
     return true;
   }
-  // Where the piece's tile lies.  (Four divisions, 600 cycles of a lone thread:
-  // the MMA issuer does not need them, and the producer asks while its ring is full.)
+  // Where the piece's tile lies.  (Each warp of the epilogue asks before it waits
+  // for the tile, which is on the way where a tile has few stages.)
   __device__ __forceinline__ void place(const MmParams& P) {
-    const int per = P.tiles_m * P.tiles_n;
-    prob = tile / per;
-    const int r = tile - prob * per;
-    const int q = r / (8 * P.tiles_n), rows = min(8, P.tiles_m - 8 * q);
-    const int i = r - q * 8 * P.tiles_n;
-    tn = i / rows;
-    tm = 8 * q + (i - tn * rows);
+    prob = P.per_prob.of(tile);
+    const int r = tile - prob * (P.tiles_m * P.tiles_n);
+    const int q = P.per_band.of(r), i = r - q * 8 * P.tiles_n;
+    const bool whole = 8 * q + 8 <= P.tiles_m;
+    tn = whole ? i >> 3 : P.last_band.of(i);
+    tm = 8 * q + (i - tn * (whole ? 8 : P.tiles_m - 8 * q));
   }
   // Where part p of the tile lies: a pair has two slots, the second for a tile
   // that its share did not begin in.
@@ -1367,6 +1376,9 @@ int consider_pair(MmParams& P, int dev, Plan* best, const char* who) {
   const int64_t tiles = (int64_t)P.tiles_m * P.tiles_n * P.probs;
   if (tiles >= 1ll << 31) return polyq_set_error(POLYQ_EUNSUPPORTED, "%s: %lld tiles", who, (long long)tiles);
   P.tiles = (int)tiles;
+  P.per_prob.set((uint32_t)(P.tiles_m * P.tiles_n));
+  P.per_band.set(8u * (uint32_t)P.tiles_n);
+  P.last_band.set((uint32_t)(P.tiles_m % 8 ? P.tiles_m % 8 : 8));
   const double last = plan_tiles(P, pairs);
   P.grid_pairs = P.tiles > pairs ? pairs : std::max(P.tiles, P.sk_pairs);
   const double waves = (double)(P.tiles / pairs);
