@@ -317,7 +317,7 @@ struct Pair {
   static constexpr int kSfCol = 512 - kSfCols;
   static constexpr int kAcc1 = kSfCol - kTileN;
   static constexpr int OV = kTileN - kAcc1;
-  static constexpr int kEpiWarp = 4, EPI = 12, EPQ = EPI / 4;  // EPQ warps to a quarter of the lanes
+  static constexpr int kEpiWarp = 4, EPI = GATED && KIND != k16 ? 12 : 8, EPQ = EPI / 4;  // EPQ warps to a quarter of the lanes
   static constexpr int kThreads = 32 * (kEpiWarp + EPI);
   static_assert(OV % 32 == 0 && STAGES >= 4, "");
 };
