@@ -317,11 +317,14 @@ struct Pair {
   static constexpr int kSfCol = 512 - kSfCols;
   static constexpr int kAcc1 = kSfCol - kTileN;
   static constexpr int OV = kTileN - kAcc1;
-  static constexpr int kEpiWarp = 4, EPI = GATED && KIND != k16 ? 12 : 8, EPQ = EPI / 4;  // EPQ warps to a quarter of the lanes
+  // EPI epilogue warps, EPQ to a quarter of the lanes, as measured with 12 / 8 / 4:
+  // gradients of the weights of 64 tokens, 5120 / 13824, 70.5 / 67.1 / 79.8 us, 16-bit
+  // gated 1086 x 5504 x 384 22.1 / 20.6 / 23.0, NV gated 2048 x 13824 x 5120 98.6 / 104 / 108.
+  static constexpr int kEpiWarp = 4, EPI = GATED && KIND != k16 ? 12 : 8, EPQ = EPI / 4;
   static constexpr int kThreads = 32 * (kEpiWarp + EPI);
   static_assert(OV % 32 == 0 && STAGES >= 4, "");
 };
-constexpr int kEpiWarps = 12;
+constexpr int kEpiWarps = 12;  // the most
 
 // The pieces of work of a pair, in order: a tile and the stages [lo, hi) of its
 // contraction; the pair's share of the shared tiles comes first.  Tiles of eight
