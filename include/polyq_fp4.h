@@ -118,8 +118,8 @@ int polyq_fp4_ffn(const polyq_fp4* x, const polyq_fp4* gate, const polyq_fp4* up
  * are multiples of 8 elements; h [T][F] of the same type.
  *   a = x gate^T, u = x up^T, h = silu(a) * u
  * in one launch.  saved: NULL, or device memory of polyq_ffn_saved_bytes,
- * 32-byte aligned, which receives a and u for the backward pass, each with 16
- * significant bits in fp32's range. */
+ * 32-byte aligned, which receives a and u for the backward pass, each rounded to
+ * 16 significant bits in fp32's range. */
 int polyq_ffn_saved_bytes(int64_t T, int64_t F, size_t* bytes);
 int polyq_ffn_forward(const polyq_dense* x, const polyq_dense* gate, const polyq_dense* up,
                       int64_t T, int64_t F, int64_t K, const polyq_dense* h, void* saved,
