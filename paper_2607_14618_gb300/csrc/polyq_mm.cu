@@ -640,9 +640,10 @@ __global__ void __launch_bounds__(C::kThreads, 1) mm_pair(const __grid_constant_
       // A chunk's residual is asked for before its accumulator is complete, the
       // next chunk's before this one's stores (512 x 5120 x 13824 MX: 28.2 us with
       // loads of 8 bytes when they are needed, 23.5 so, 22.6 without a residual).
-      uint32_t res[C::GATED ? 1 : 32];
+      constexpr bool RES = !C::GATED && C::KIND != k16;  // may have a residual
+      uint32_t res[RES ? 32 : 1];
       auto fetch_res = [&](int c) {
-        if constexpr (!C::GATED) {
+        if constexpr (RES) {
           const int n = n0 + 32 * c;
           if (P.res && P.vec && n + 32 <= P.N && m + lane < P.M)
             load_row32(P.res, (m + lane) * P.res_stride + n, res, P.type, P.vec);
@@ -668,7 +669,7 @@ __global__ void __launch_bounds__(C::kThreads, 1) mm_pair(const __grid_constant_
         const int n = n0 + 32 * c;
         float v[32];
         if constexpr (C::GATED) {
-          if (P.saved && m + lane < P.M && n < P.N) {
+          if (C::KIND == k16 && P.saved && m + lane < P.M && n < P.N) {
             save_row32(P, 0, m + lane, n, r0);
             save_row32(P, 1, m + lane, n, r1);
           }
@@ -676,7 +677,7 @@ __global__ void __launch_bounds__(C::kThreads, 1) mm_pair(const __grid_constant_
 #pragma unroll
           for (int j = 0; j < 32; ++j)
             v[j] = silu(__uint_as_float(r0[j]) * P.alpha[0]) * (__uint_as_float(r1[j]) * P.alpha[1]);
-          if (P.qfmt) {
+          if (C::KIND != k16 && P.qfmt) {
 #pragma unroll
             for (int j = 0; j < 32; ++j) v[j] = n + j < P.N ? v[j] : 0.f;
             if (m + lane >= P.M) return;
@@ -688,9 +689,11 @@ __global__ void __launch_bounds__(C::kThreads, 1) mm_pair(const __grid_constant_
         } else {
 #pragma unroll
           for (int j = 0; j < 32; ++j) v[j] = __uint_as_float(r0[j]) * P.alpha[0];
-          if (P.res && P.vec && n + 32 <= P.N) add_row32(res, v, P.type);
-          if (next < kChunks) fetch_res(chunk(next));
-          store_chunk(P.y[T.prob], P.y_stride, P.res, P.res_stride, m, n, P.M, P.N, v, P.type, P.vec);
+          if constexpr (RES) {
+            if (P.res && P.vec && n + 32 <= P.N) add_row32(res, v, P.type);
+            if (next < kChunks) fetch_res(chunk(next));
+          }
+          store_chunk(P.y[T.prob], P.y_stride, RES ? P.res : nullptr, P.res_stride, m, n, P.M, P.N, v, P.type, P.vec);
         }
       };
       auto load = [&](int c, uint32_t (&r0)[32], uint32_t (&r1)[C::GATED ? 32 : 1]) {
@@ -701,7 +704,7 @@ __global__ void __launch_bounds__(C::kThreads, 1) mm_pair(const __grid_constant_
         tc_regs_ready(r1);
       };
       // whether a chunk has an output (4 bits: a scale or a code) of this matrix
-      auto inside = [&](int c) { return m < P.M && (P.qfmt != 0 || n0 + 32 * c < P.N); };
+      auto inside = [&](int c) { return m < P.M && ((C::GATED && C::KIND != k16 && P.qfmt != 0) || n0 + 32 * c < P.N); };
       // A part goes into its slot; the warp that finds the other parts of its
       // chunks in place adds them all, in the order of the pairs.
       auto part = [&](int slot, int col) {  // 4 columns of the lane's row
@@ -1108,19 +1111,19 @@ __global__ void __launch_bounds__(C::kThreads, 1) mm_few(const __grid_constant__
         float (&u)[4] = us[i];
 #pragma unroll
         for (int e = 0; e < 4; ++e) u[e] *= P.alpha[1];
-        if (P.saved && cnt > 0) {  // (rows are padded to 32)
+        if (C::KIND == k16 && P.saved && cnt > 0) {  // (rows are padded to 32)
           const int64_t at = m * P.saved_stride + n;
           save4(P, 0, at, v);
           save4(P, 1, at, u);
         }
 #pragma unroll
         for (int e = 0; e < 4; ++e) v[e] = silu(v[e]) * u[e];
-        if (P.qfmt) {
+        if (C::KIND != k16 && P.qfmt) {
           if (P.qfmt == kNv) store_codes4<true>(P, m, n, v);
           else store_codes4<false>(P, m, n, v);
           continue;
         }
-      } else if (P.res && cnt > 0) {
+      } else if (C::KIND != k16 && P.res && cnt > 0) {
         if (P.vec && cnt == 4) {
           add4(P.res, m * P.res_stride + n, v, P.type);
         } else {
