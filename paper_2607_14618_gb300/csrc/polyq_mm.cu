@@ -629,7 +629,7 @@ __global__ void __launch_bounds__(C::kThreads, 1) mm_pair(const __grid_constant_
     constexpr int kChunks = C::GATED ? kTileN / 64 : kTileN / 32;
     constexpr int kOvChunks = C::OV / 32;
     pdl_wait();
-    for (int tc = 0; !s_abort && T.next(P); ++tc) {
+    for (int tc = 0; T.next(P); ++tc) {
       T.place(P);
       const int buf = tc & 1;
       const int64_t m = (int64_t)T.tm * kTileM + (int)rank * kHalf + 32 * q;  // the warp's first row
@@ -650,8 +650,11 @@ __global__ void __launch_bounds__(C::kThreads, 1) mm_pair(const __grid_constant_
         }
       };
       fetch_res(chunk(e0));
+      // The warp goes on or gives up as a whole, whatever its lanes' polls saw: the
+      // loads of tensor memory, and its other steps together, are by all lanes.  (A
+      // second vote, on s_abort at the loop's head: 8192 x 5120 x 13824 MX +1.8%.)
       const int w = wait(smem_u32(&bar_accf[buf]), (tc >> 1) & 1, &s_abort);
-      if (w != kOk) {
+      if (!__all_sync(0xffffffffu, w == kOk)) {
         if (w == kTimeout) fail(kStatusTimeoutFull);
         break;
       }
@@ -782,6 +785,7 @@ __global__ void __launch_bounds__(C::kThreads, 1) mm_pair(const __grid_constant_
 #pragma unroll 1
         for (int i = e0; i < kChunks; i += C::EPQ) {
           const int c = chunk(i);
+          __syncwarp();  // (lanes without a row, or a residual, come on their own)
           uint32_t r0[32], r1[C::GATED ? 32 : 1];
           load(c, r0, r1);
           if (C::OV > 0 && !released && T.shared < 0 && i + C::EPQ >= kOvChunks) release();
@@ -797,6 +801,7 @@ __global__ void __launch_bounds__(C::kThreads, 1) mm_pair(const __grid_constant_
   __syncthreads();
   cluster_sync();
   if (warp == 1) {
+    __syncwarp();
     tc_fence_after();
     tmem_dealloc<2>(tmem, 512);
   }
@@ -1048,6 +1053,7 @@ __global__ void __launch_bounds__(C::kThreads, 1) mm_few(const __grid_constant__
     }
   }
   __syncthreads();  // every copy has landed and every MMA is done (or a role has given up)
+  __syncwarp();
   tc_fence_after();
 
   // ---------------- epilogue ----------------
@@ -1144,6 +1150,7 @@ __global__ void __launch_bounds__(C::kThreads, 1) mm_few(const __grid_constant__
   __syncthreads();
   if (split > 1) cluster_sync();  // a peer may still read this CTA's part
   if (warp == 1) {
+    __syncwarp();
     tc_fence_after();
     tmem_dealloc<1>(tmem, C::kTmem);
   }
