@@ -1233,11 +1233,16 @@ int device_index(int* dev, const char* who) {
   return POLYQ_OK;
 }
 
-// Clusters of `size` CTAs of a kernel that fit on the device at once (cached).
+#ifdef POLYQ_DEBUG
+std::atomic<int> g_largest_cluster{kMaxSplit};
+#endif
+
+// Clusters of `size` CTAs of a kernel that fit on the device at once: 0 where
+// none does, as in a context of few SMs.  `cached` holds one more, 0 until asked.
 int resident_clusters(const void* f, int threads, size_t smem, int size, std::atomic<int>* cached, int* out,
                       const char* who) {
-  int n = cached->load(std::memory_order_acquire);
-  if (n == 0) {
+  int n = cached->load(std::memory_order_acquire) - 1;
+  if (n < 0) {
     cudaError_t e = cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     cudaLaunchAttribute at[1];
     at[0].id = cudaLaunchAttributeClusterDimension;
@@ -1250,10 +1255,14 @@ int resident_clusters(const void* f, int threads, size_t smem, int size, std::at
     cfg.attrs = at;
     cfg.numAttrs = 1;
     if (e == cudaSuccess) e = cudaOccupancyMaxActiveClusters(&n, f, &cfg);
-    if (e != cudaSuccess || n < 1)
-      return polyq_set_error(POLYQ_ECUDA, "%s: %d clusters of %d fit: %s", who, n, size, cudaGetErrorString(e));
-    cached->store(n, std::memory_order_release);
+    if (e != cudaSuccess)
+      return polyq_set_error(POLYQ_ECUDA, "%s: clusters of %d that fit: %s", who, size, cudaGetErrorString(e));
+    n = std::max(n, 0);
+    cached->store(n + 1, std::memory_order_release);
   }
+#ifdef POLYQ_DEBUG
+  if (size > g_largest_cluster.load()) n = 0;
+#endif
   *out = n;
   return POLYQ_OK;
 }
@@ -1372,6 +1381,7 @@ int consider_few(const MmParams& P, int dev, Plan* best, const char* who) {
     int fit = 0;
     const int rc = resident_clusters((const void*)mm_few<C>, C::kThreads, C::kSmem, s, &cached[dev][s - 1], &fit, who);
     if (rc) return rc;
+    if (fit == 0) continue;
     const double us = std::max((double)((tiles + fit - 1) / fit) * (few_base<C>() + few_stage<C>() * ((n_it + s - 1) / s) +
                                                                     (s > 1 ? kFewSplit : 0.0)),
                                few_base<C>() + weight_bytes<C>(P) / kHbm);
@@ -1380,13 +1390,14 @@ int consider_few(const MmParams& P, int dev, Plan* best, const char* who) {
   return POLYQ_OK;
 }
 
-// P.probs is set too; fills in the tiles and how they are shared.
+// P.probs is set too; fills in the tiles and how they are shared, where a pair
+// fits on the device.
 template <class C>
 int consider_pair(MmParams& P, int dev, Plan* best, const char* who) {
   static std::atomic<int> cached[kMaxDevices];
   int pairs = 0;
   const int rc = resident_clusters((const void*)mm_pair<C>, C::kThreads, C::kSmem, 2, &cached[dev], &pairs, who);
-  if (rc) return rc;
+  if (rc || pairs == 0) return rc;
   pairs = std::min(pairs, kMaxPairs);
   const int cols = C::GATED ? kHalf : kTileN;
   P.tiles_m = (P.M + kTileM - 1) / kTileM;
@@ -1407,16 +1418,22 @@ int consider_pair(MmParams& P, int dev, Plan* best, const char* who) {
   return POLYQ_OK;
 }
 
+constexpr double kNoPlan = 1e30;
+int check_plan(const Plan& plan, const char* who) {
+  if (plan.us < kNoPlan) return POLYQ_OK;
+  return polyq_set_error(POLYQ_EUNSUPPORTED, "%s: no cluster of a kernel's thread blocks fits on the device", who);
+}
+
 template <int KIND, bool GATED>
 int plan_product(MmParams& P, int dev, Plan* plan, const char* who) {
-  *plan = {0, 1, 1e30};
+  *plan = {0, 1, kNoPlan};
   int rc = consider_pair<Pair<KIND, GATED>>(P, dev, plan, who);
   if (!rc && P.M <= 16) rc = consider_few<Few<KIND, 16, GATED>>(P, dev, plan, who);
   if (!rc && P.M > 16 && P.M <= 32) rc = consider_few<Few<KIND, 32, GATED>>(P, dev, plan, who);
   // (with more tokens than fill every SM's tile the pairs are far ahead)
   if (!rc && P.M > 32 && P.M <= kFewTokens) rc = consider_few<Few<KIND, 64, GATED>>(P, dev, plan, who);
   if (!rc && P.M > 32 && P.M <= kFewTokens) rc = consider_few<Few<KIND, 128, GATED>>(P, dev, plan, who);
-  return rc;
+  return rc ? rc : check_plan(*plan, who);
 }
 
 template <class C>
@@ -1802,9 +1819,15 @@ extern "C" int polyq_ffn_backward(const polyq_dense* x, const polyq_dense* gate,
     if (!rc) rc = map_16(&P.a[1], du, fs, T, F, true, 0);
     if (!rc) rc = map_16(&P.b[0], x->data, x->stride, T, K, true, 0);
     P.b[1] = P.b[0];
-    Plan plan = {0, 1, 1e30};
+    Plan plan = {0, 1, kNoPlan};
     if (!rc) rc = consider_pair<Pair<k16, false>>(P, dev, &plan, who);
+    if (!rc) rc = check_plan(plan, who);
     if (!rc) rc = launch_pair<Pair<k16, false>>(P, workspace, stream, who);
   }
   return rc;
 }
+
+#ifdef POLYQ_DEBUG
+#include "polyq_debug_mm.h"
+extern "C" void polyq_debug_mm_largest_cluster(int size) { g_largest_cluster = size; }
+#endif
