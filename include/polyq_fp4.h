@@ -135,9 +135,9 @@ int polyq_ffn_backward_workspace_bytes(int64_t T, int64_t F, size_t* bytes);
  *   dx [T][K] = da gate + du up, dgate [F][K] = da^T x, dup [F][K] = du^T x
  * da and du are rounded once to x's type (as the tensor cores take them), sums
  * are in fp32.  Any of dx, dgate, dup may be NULL (not wanted; dgate and dup
- * both or neither); each is of x's type or POLYQ_F32.  One launch for da and
- * du, one for dx, one for dgate and dup.  The result does not change from run
- * to run. */
+ * both or neither); each is of x's type or POLYQ_F32, dgate and dup of one type
+ * and stride (else POLYQ_EINVAL).  One launch for da and du, one for dx, one for
+ * dgate and dup.  The result does not change from run to run. */
 int polyq_ffn_backward(const polyq_dense* x, const polyq_dense* gate, const polyq_dense* up,
                        int64_t T, int64_t F, int64_t K, const void* saved, const polyq_dense* dh,
                        const polyq_dense* dx, const polyq_dense* dgate, const polyq_dense* dup,

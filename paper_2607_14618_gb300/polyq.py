@@ -1038,17 +1038,20 @@ def ffn_forward(x, gate, up, h=None, saved=None, workspace=None, stream=None):
 def ffn_backward(x, gate, up, saved, dh, dx=None, dgate=None, dup=None, need_dx=True,
                  need_weights=True, workspace=None, stream=None):
     """Gradients (dx, dgate, dup) of ffn_forward for the gradient dh of h; each
-    of x's type or, where a buffer of that type is passed, fp32.  Those not
-    needed are None."""
+    of x's type or, where a buffer of that type is passed, fp32 (dgate and dup of
+    one type and row stride).  Those not needed are None."""
     ix, ig, iu, T, F, K, dev, st = _ffn_inputs(x, gate, up, stream)
     ty = x.dtype
     idh = _dense(dh, "dh", T, F, dev, ty)
     ps = _saved(saved, T, F, dev)
 
     def new(n, like):
+        # dgate and dup have one type and stride: the other's, where that is given
         import torch
-        return _made(stream, torch.empty, (n, K), dtype=ty if like is None else like.dtype,
-                     device=x.device)
+        wide = K if like is None else _dense(like, "dgate or dup", n, K, dev).stride
+        t = _made(stream, torch.empty, (n, wide), dtype=ty if like is None else like.dtype,
+                  device=x.device)
+        return t if wide == K else t[:, :K]
 
     if dx is None and need_dx:
         dx = new(T, None)
