@@ -805,8 +805,9 @@ class Fp4Tensor:
         import torch
         stride, nbytes = C.c_int64(), C.c_int64()
         _check(_lib.polyq_fp4_bytes(int(rows), int(K), int(format), C.byref(stride), C.byref(nbytes)))
-        _require(codes, "codes", torch.uint8, (rows, stride.value), codes.device)
-        _require(scales, "scales", torch.uint8, (nbytes.value,), codes.device)
+        dev = getattr(codes, "device", None)
+        _require(codes, "codes", torch.uint8, (rows, stride.value), dev)
+        _require(scales, "scales", torch.uint8, (nbytes.value,), dev)
         rows, K, format, tensor_scale = int(rows), int(K), int(format), float(tensor_scale)
         self.__dict__.update(
             codes=codes, scales=scales, rows=rows, K=K, format=format, tensor_scale=tensor_scale,
@@ -839,6 +840,8 @@ class Fp4Tensor:
         """From plain codes (uint8 [rows][K], 0..15) and scale bytes (uint8
         [rows][blocks]), as a checkpoint holds them."""
         import torch
+        if not (isinstance(codes, torch.Tensor) and isinstance(scales, torch.Tensor) and codes.dim() == 2):
+            raise ValueError("codes and scales must be tensors, codes uint8 [rows][K]")
         rows, K = codes.shape
         blocks = -(-K // (16 if format == FP4_NV else 32))
         if codes.dtype != torch.uint8 or scales.dtype != torch.uint8 or tuple(scales.shape) != (rows, blocks):
@@ -909,8 +912,8 @@ def _workspace_at(workspace, dev, stream, make, *args):
     if workspace is None:
         return _made(stream, make, *args)
     import torch
-    if (workspace.dtype != torch.uint8 or workspace.get_device() != dev
-            or not workspace.is_contiguous()):
+    if (not isinstance(workspace, torch.Tensor) or workspace.dtype != torch.uint8
+            or workspace.get_device() != dev or not workspace.is_contiguous()):
         raise ValueError(f"workspace must be a contiguous uint8 tensor on cuda:{dev}")
     return workspace
 
@@ -953,12 +956,16 @@ def fp4_linear(x: Fp4Tensor, w: Fp4Tensor, y=None, residual=None, dtype=None, wo
     dev = x.device_index
     pw = _fp4(w, "w", dev)
     st = _stream_on(dev, "x", stream)
+    dr = None
+    if residual is not None:
+        dr = C.byref(_dense(residual, "residual", x.rows, w.rows, dev, dtype if y is None else None))
     if y is None:
         import torch
         y = _made(stream, torch.empty, (x.rows, w.rows), device=x.codes.device,
                   dtype=dtype or (residual.dtype if residual is not None else torch.float32))
     dy = _dense(y, "y", x.rows, w.rows, dev, dtype)
-    dr = None if residual is None else C.byref(_dense(residual, "residual", x.rows, w.rows, dev, y.dtype))
+    if residual is not None and residual.dtype != y.dtype:
+        raise ValueError(f"residual is {residual.dtype}, y {y.dtype}")
     ws = _workspace_at(workspace, dev, stream, fp4_workspace, x.codes.device)
     _check(_lib.polyq_fp4_linear(px, pw, dr, C.byref(dy), ws.data_ptr(), ws.numel(), st))
     return y
@@ -1014,8 +1021,12 @@ def _ffn_inputs(x, gate, up, stream):
 
 def _saved(saved, T, F, dev):
     # the size that polyq_ffn_saved_bytes gives: 6 bytes an element of rows padded to 32
-    if (saved.element_size() != 1 or saved.get_device() != dev or not saved.is_contiguous()
-            or saved.numel() != 6 * T * ((F + 31) & -32)):
+    try:
+        good = (saved.element_size() == 1 and saved.get_device() == dev and saved.is_contiguous()
+                and saved.numel() == 6 * T * ((F + 31) & -32))
+    except AttributeError:
+        good = False
+    if not good:
         raise ValueError(f"saved must be ffn_saved({T}, {F}) on cuda:{dev}")
     return saved.data_ptr()
 
