@@ -253,16 +253,5 @@ __device__ __forceinline__ void commit(uint32_t bar) {
                  : "memory");
 }
 
-// The same on this CTA's barrier only.
-template <int CG>
-__device__ __forceinline__ void commit_here(uint32_t bar) {
-  if (CG == 2)
-    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar)
-                 : "memory");
-  else
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar)
-                 : "memory");
-}
-
 }  // namespace tc
 }  // namespace polyq
