@@ -78,7 +78,8 @@ int polyq_fp4_bytes(int64_t rows, int64_t K, int32_t format, int64_t* code_strid
  * POLYQ_FP4_NV: t = fp32(x / tensor_scale); a block's scale s is the e4m3
  * number nearest to fp32(largest |t| / 6) (ties to even, at most 448), each
  * element the e2m1 number nearest to the exact t / s, 0 where s is 0.
- * A block that holds an infinity or a NaN gets the scale NaN, and codes 0.
+ * A block that holds an infinity or a NaN (POLYQ_FP4_NV: in t, which a small
+ * tensor scale may take beyond fp32) gets the scale NaN, and codes 0.
  * One launch. */
 int polyq_fp4_quantize(const polyq_dense* x, const polyq_fp4* out, void* stream);
 
@@ -105,7 +106,9 @@ int polyq_fp4_linear(const polyq_fp4* x, const polyq_fp4* w, const polyq_dense* 
 
 /* h[m][f] = silu(a) * u, a = sum_k x[m][k] gate[f][k], u = sum_k x[m][k]
  * up[f][k], silu(a) = a / (1 + exp(-a)): x [M][K], gate and up [F][K] in one
- * 4-bit format.  a, u and the activation stay in fp32; exactly one of the
+ * 4-bit format.  a, u and the activation stay in fp32, the activation by fast
+ * exponential and quotient (off by up to (8 + 1.2 |a|) 2^-23 of h; below a = -87,
+ * where exp(-a) nears fp32's largest number, it may be 0); exactly one of the
  * outputs is given: h [M][F] of any type, or hq [M][F] in 4 bits (either
  * format), which is h in fp32 quantised as polyq_fp4_quantize does.  One
  * launch; the result does not change from run to run. */
@@ -133,8 +136,9 @@ int polyq_ffn_backward_workspace_bytes(int64_t T, int64_t F, size_t* bytes);
  * `saved` of its forward pass:
  *   s = 1/(1+exp(-a)), da = dh u s (1 + a (1-s)), du = dh a s
  *   dx [T][K] = da gate + du up, dgate [F][K] = da^T x, dup [F][K] = du^T x
- * da and du are rounded once to x's type (as the tensor cores take them), sums
- * are in fp32.  Any of dx, dgate, dup may be NULL (not wanted; dgate and dup
+ * s is as exact as the activation of polyq_fp4_ffn; da and du are rounded once to
+ * x's type (as the tensor cores take them), also for gradients in fp32; sums are
+ * in fp32.  Any of dx, dgate, dup may be NULL (not wanted; dgate and dup
  * both or neither); each is of x's type or POLYQ_F32, dgate and dup of one type
  * and stride (else POLYQ_EINVAL).  One launch for da and du, one for dx, one for
  * dgate and dup.  The result does not change from run to run. */
