@@ -55,9 +55,9 @@ struct Elem<__half> {
 // 8 elements from k on as they lie in memory, and as floats; zeros past K.  VEC:
 // rows start on 16 bytes.  (Two steps, so that the loads of several rows are in
 // flight before the first is converted: 13824 x 5120 bf16 63 us with one.)
-// Inputs are read through L2: a grid may be on its SM before the one that writes
-// them has begun, and lines that an earlier grid left in that SM's L1, or read
-// only loads, would be older than the wait.
+// Inputs are read once, through L2, by ordinary loads: a grid may be on its SM
+// before the one that writes them has begun, and the grid dependency's wait orders
+// these with those writes, but not loads through the read-only path.
 template <typename T>
 struct Raw8 {
   uint4 w[sizeof(T) * 8 / 16];

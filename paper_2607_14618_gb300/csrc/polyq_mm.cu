@@ -150,7 +150,9 @@ __device__ __forceinline__ void store_row32(void* y, int64_t off, const float (&
   }
 }
 // The lane's 32 consecutive residual values as they lie in memory (16-bit types:
-// the first half of w), and their sum with v.
+// the first half of w), and their sum with v.  Ordinary loads, also where the
+// launch before writes the residual: every thread that reads one has waited for
+// that launch, and the wait makes its writes visible to them.
 __device__ __forceinline__ void load_row32(const void* r, int64_t off, uint32_t (&w)[32], int type, int vec) {
   const uint8_t* p = (const uint8_t*)r + off * (type == POLYQ_F32 ? 4 : 2);
 #pragma unroll
@@ -1160,8 +1162,9 @@ __global__ void __launch_bounds__(C::kThreads, 1) mm_few(const __grid_constant__
 // gradients of the activation and the product
 // ---------------------------------------------------------------------------
 // da = dh u s (1 + a (1 - s)), du = dh a s with s = 1 / (1 + exp(-a)); 8
-// elements a thread.  One pass over a, u, dh; bound by HBM.  Read through L2, as
-// the grid may be on its SM before the one that writes them has begun.
+// elements a thread.  One pass over a, u, dh; bound by HBM.  Read once, through L2
+// (by ordinary loads, which the grid dependency's wait orders with the writes of
+// the launch before).
 struct ActParams {
   const uint8_t* saved;  // save_row32's planes
   const void* dh;
