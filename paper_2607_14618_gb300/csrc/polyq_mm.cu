@@ -204,7 +204,9 @@ __device__ __forceinline__ uint8_t* saved_lo(const MmParams& P, int which, int64
 }
 // Those 24 bits are the upper ones of this.  NaN and infinities stay as they are,
 // and numbers next to the largest, which would become infinities.
-__device__ __forceinline__ uint32_t round24(uint32_t v) { return (v << 1) < 0xFEFFFF00u ? v + 0x80u : v; }
+__device__ __forceinline__ uint32_t round24(uint32_t v) {
+  return fabsf(__uint_as_float(v)) < __uint_as_float(0x7F7FFF80u) ? v + 0x80u : v;
+}
 __device__ __forceinline__ void save_row32(const MmParams& P, int which, int64_t m, int n, const uint32_t (&r)[32]) {
   const int64_t at = m * P.saved_stride + n;
   uint32_t v[32], w[8];
