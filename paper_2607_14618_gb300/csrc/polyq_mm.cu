@@ -326,9 +326,11 @@ struct Pair {
   static constexpr int kSfCol = 512 - kSfCols;
   static constexpr int kAcc1 = kSfCol - kTileN;
   static constexpr int OV = kTileN - kAcc1;
-  // EPI epilogue warps, EPQ to a quarter of the lanes, as measured with 12 / 8 / 4:
-  // gradients of the weights of 64 tokens, 5120 / 13824, 70.5 / 67.1 / 79.8 us, 16-bit
-  // gated 1086 x 5504 x 384 22.1 / 20.6 / 23.0, NV gated 2048 x 13824 x 5120 98.6 / 104 / 108.
+  // EPI epilogue warps, EPQ to a quarter of the lanes, as measured with 12 / 8 / 4
+  // (calls one after another over one set of operands): gradients of the weights
+  // of 64 tokens with da and du, 5120 / 13824, 69.9 / 69.0 / 71.2 us, in fp32 129.9
+  // / 130.9 / 131.1; 16-bit gated and saved, 1086 x 5504 x 384, 20.1 / 18.7 / 20.2;
+  // gated 2048 x 13824 x 5120, NV 98.6 / 103.5 / 105.1, MX 90.7 / 95.6 / 96.4.
   static constexpr int kEpiWarp = 4, EPI = GATED && KIND != k16 ? 12 : 8, EPQ = EPI / 4;
   static constexpr int kThreads = 32 * (kEpiWarp + EPI);
   static_assert(OV % 32 == 0 && STAGES >= 4, "");
