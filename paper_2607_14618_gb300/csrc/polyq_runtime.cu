@@ -52,7 +52,12 @@ int polyq_sm_count(int* out) {
     e = cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev);
     if (e != cudaSuccess || n <= 0)
       return polyq_set_error(POLYQ_ECUDA, "SM count: %s", cudaGetErrorString(e));
-    it = g_sms.emplace(dev, n).first;
+    try {
+      g_sms.emplace(dev, n);
+    } catch (const std::bad_alloc&) {  // the next call asks again
+    }
+    *out = n;
+    return POLYQ_OK;
   }
   *out = it->second;
   return POLYQ_OK;
