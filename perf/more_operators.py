@@ -324,14 +324,15 @@ def _decode(c, s, mantissa):
 
 
 def _encode(a, u, mantissa, top):
-    """Codes and scale bytes of fp32 magnitudes [blocks][256]: the largest one's binade is the
-    format's highest; rounded up where the 16-bit fraction u and what lies behind the last place
-    carry."""
+    """Codes and scale bytes of fp32 magnitudes [blocks][256]: the smallest scale with which the
+    largest one is within the codes; rounded up where the 16-bit fraction u and what lies behind
+    the last place carry."""
+    one = 1 << mantissa
     peak = a.amax(1)
-    s = torch.where(peak > 0, torch.frexp(peak).exponent + 112, 0).clamp(min=0)
+    f, e = torch.frexp(peak)
+    s = torch.where(peak > 0, e + 112 + (f > 1 - 0.5 / one), 0).clamp(min=0)
     t = a * torch.exp2(127 - s.double()).float()[:, None]
     f, e = torch.frexp(t)
-    one = 1 << mantissa
     part = torch.where(e > 0, f * (2 * one), t * one)
     c = torch.floor(part.double() + u.double() / 65536).int() + (e - 1).clamp(min=0) * one
     return c.clamp(max=top).to(torch.uint8), s.to(torch.uint8)
@@ -539,6 +540,7 @@ def _exact_round(a, frac, mantissa, top):
     peak = torch.amax(a, 1, True)
     e = torch.floor(torch.log2(torch.where(peak > 0, peak, torch.full_like(peak, 2.0 ** -126))))
     e = e + (torch.exp2(e + 1) <= peak).double() - (torch.exp2(e) > peak).double()
+    e = e + (peak > grid[top] * torch.exp2(e - 14)).double()
     unit = torch.exp2((e - 14).clamp(min=-127))
     t = a / unit
     low = torch.bucketize(t, grid, right=True) - 1
