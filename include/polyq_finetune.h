@@ -1,0 +1,144 @@
+/*
+ * polyq_finetune.h - C ABI of the operators that fine-tune a quantised model on
+ * GB300 (sm_103a) and serve the result: layer norm, AdamW and low-rank adapters.
+ *
+ * They stand around the products of polyq.h and polyq_fp4.h: the norm before a
+ * projection with its gradients, the adapters of many requests (or of a training
+ * step) beside a projection whose quantised weights stay as they are, and the
+ * optimiser's step over all trained tensors at once.
+ *
+ * The conventions of polyq.h hold: return codes and polyq_last_error(), caller
+ * owns every buffer, entry points check their arguments on the host, never
+ * allocate device memory and never synchronise, `stream` is a cudaStream_t.
+ * Every entry works on the current device and may be captured in a CUDA graph.
+ * Sizes are at least 1: an empty tensor is POLYQ_EINVAL.  Outputs must not
+ * overlap inputs or each other unless stated otherwise.  A workspace needs no
+ * initialisation and may serve consecutive calls on one stream, but not calls
+ * that run at the same time.  Results do not change from run to run.
+ */
+#ifndef POLYQ_FINETUNE_H
+#define POLYQ_FINETUNE_H
+
+#include "polyq_fp4.h"
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+/* ---- layer norm ---- */
+
+#define POLYQ_NORM_MAX_K 49152 /* widest row */
+
+/* y[r][k] = hat[r][k] weight[k] + bias[k] of x [rows][K],
+ *   hat = (x - mean) rstd, rstd = 1 / sqrt(mean of (x - mean)^2 + eps),
+ *   mean = the row's mean with center != 0 (layer norm), else 0 (RMS norm).
+ * x and y of any type and row stride; y may be x itself where both have one type
+ * and stride.  weight, bias: K elements (their
+ * stride does not matter) of any type, each may be NULL (1 and 0).  stats: NULL,
+ * or device memory of 2*rows floats, 8-byte aligned, which receives (mean, rstd)
+ * of every row for the backward pass.  The row is held in fp32, its mean is taken
+ * before the squares of what is left are summed (their sum must stay within fp32),
+ * and one rounding makes y.  One launch.
+ * K above POLYQ_NORM_MAX_K is POLYQ_EUNSUPPORTED. */
+int polyq_layernorm_forward(const polyq_dense* x, int64_t rows, int64_t K, const polyq_dense* weight,
+                            const polyq_dense* bias, float eps, int center, const polyq_dense* y,
+                            float* stats, void* stream);
+
+int polyq_layernorm_workspace_bytes(int64_t rows, int64_t K, size_t* bytes);
+
+/* Gradients for the gradient dy [rows][K] of y and the stats of the forward pass:
+ *   g = dy weight,  dx = residual + rstd (g - [mean of g] - hat mean of (g hat)),
+ *   dweight = sum over rows of dy hat, dbias = sum over rows of dy
+ * with the mean of g only where center != 0.  dx NULL (not wanted) or of x's type;
+ * residual NULL or [rows][K] of dx's type (the gradient that reaches x beside the
+ * norm; its data may be dx's, with dx's stride); dweight, dbias: NULL or K
+ * elements of any type; at least one of the three is wanted.  dx may be dy's
+ * memory where both have one type and stride.
+ * The workspace (polyq_layernorm_workspace_bytes, 16-byte aligned) is needed with
+ * dweight or dbias: every SM's sums over its rows, which a second launch adds in
+ * a fixed order. */
+int polyq_layernorm_backward(const polyq_dense* x, int64_t rows, int64_t K, const polyq_dense* weight,
+                             const float* stats, int center, const polyq_dense* dy,
+                             const polyq_dense* residual, const polyq_dense* dx,
+                             const polyq_dense* dweight, const polyq_dense* dbias, void* workspace,
+                             size_t workspace_bytes, void* stream);
+
+/* ---- AdamW ---- */
+
+#define POLYQ_ADAMW_BLOCK 256 /* elements of an 8-bit state that share a scale */
+
+/* A trained tensor of n elements without gaps: its parameters, its gradient and,
+ * where `copy` is not NULL, a second place for the new parameters in another type
+ * (16-bit weights made of fp32 ones).  Each aligned to its element size.  Its state
+ * begins at element `at` of the state's buffers, a multiple of POLYQ_ADAMW_BLOCK;
+ * tensors' states must not overlap, nor may any other buffers. */
+typedef struct {
+  void* p;
+  const void* grad;
+  void* copy;
+  int64_t n;    /* 1..2^38 */
+  int64_t at;   /* 0..2^38 */
+  float decay;  /* of the decoupled weight decay, >= 0 */
+  float rate;   /* factor of the learning rate, >= 0 */
+} polyq_adamw_tensor;
+
+/* The moments of all tensors.  bits 32: m and v are fp32, 16-byte aligned; m_scales
+ * and v_scales do not matter.  bits 8: m and v are uint8 codes, 16-byte aligned, with
+ * one scale byte per block of POLYQ_ADAMW_BLOCK elements, 2^(byte-127) (255 is NaN):
+ *   m        sign in bit 7, bits 0..6 a magnitude of 4 exponent and 3 mantissa bits
+ *   v        the root of the second moment, 4 exponent and 4 mantissa bits
+ * A magnitude with exponent bits E and mantissa F (a fraction) is F for E = 0 and
+ * (1 + F) 2^(E-1) else, so that its highest binade begins at 2^14.  A tensor's last
+ * block belongs to it whole: what lies past its n elements is set to 0. */
+typedef struct {
+  void* m;
+  void* v;
+  uint8_t* m_scales;
+  uint8_t* v_scales;
+  int64_t n;  /* elements of m and of v, a multiple of POLYQ_ADAMW_BLOCK */
+  int32_t bits;
+} polyq_adamw_state;
+
+typedef struct {
+  double lr, beta1, beta2, eps; /* lr >= 0, 0 <= beta < 1, 0 < eps <= 1e30 */
+  int64_t step;                 /* 1, 2, ...: this step's number */
+  uint64_t seed;                /* of the rounding of 8-bit states */
+  /* Device values, read when the step runs (so that a captured step can take new
+   * ones); each may be NULL. */
+  const float* lr_dev;          /* the learning rate in place of lr */
+  const int64_t* step_dev;      /* the step's number in place of step (below 1 counts as 1), also
+                                   added to the seed */
+  const float* grad_scale;      /* factor of every gradient; the step leaves everything as it
+                                   was where it is not finite */
+} polyq_adamw_hyper;
+
+/* One step of all tensors:
+ *   m = beta1 m + (1-beta1) g,  v = beta2 v + (1-beta2) g^2   (g the scaled gradient)
+ *   p = p (1 - lr rate decay) - lr rate / (1-beta1^t) m / (sqrt(v / (1-beta2^t)) + eps)
+ * in fp32, p rounded once to its type, copy once from p.  All tensors of a call have one
+ * type of p, one of the gradient and one of the copies (any of POLYQ_F32, POLYQ_BF16,
+ * POLYQ_F16).
+ * 8-bit states are rounded after p has been computed: a block's scale is the smallest with
+ * which its largest magnitude is at most the largest code, and a magnitude is rounded down
+ * after adding a fraction u of its last place (up with a probability that equals the part
+ * cut off, so that a moment's slow changes are not lost; a root that is not 0 is at least
+ * the smallest code).  u takes 16 bits of a hash of the seed and the element's
+ * place in the state, m the low and v the high half:
+ *   mix(h):  h = (h ^ h >> 16) * 0x9E2D58A5;  h = (h ^ h >> 15) * 0x6C62272D   (mod 2^32)
+ *   key = mix(mix(block ^ mix(seed + 1)) ^ block >> 32 ^ seed >> 32)
+ *   h = mix(key + 0x9E3779B1 * (element % 256));  bits = h ^ h >> 16
+ * A block with an infinity or a NaN gets the scale NaN and codes 0.
+ * Up to 640 tensors a launch. */
+int polyq_adamw_step(const polyq_adamw_tensor* tensors, int32_t n_tensors, int32_t p_type,
+                     int32_t grad_type, int32_t copy_type, const polyq_adamw_state* state,
+                     const polyq_adamw_hyper* hyper, void* stream);
+
+/* The values of an 8-bit state: m and the root of v, each NULL or state->n elements of any type, rounded
+ * once (bf16 and fp32 hold them exactly).  One launch. */
+int polyq_adamw_values(const polyq_adamw_state* state, const polyq_dense* m, const polyq_dense* root,
+                       void* stream);
+
+#ifdef __cplusplus
+}
+#endif
+#endif /* POLYQ_FINETUNE_H */

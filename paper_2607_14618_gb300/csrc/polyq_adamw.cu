@@ -1,0 +1,448 @@
+// AdamW over many tensors in one launch, with the moments in 32 or in 8 bits.
+//
+//   m = b1 m + (1-b1) g,  v = b2 v + (1-b2) g^2
+//   p = p (1 - lr decay) - lr / (1-b1^t) m / (sqrt(v / (1-b2^t)) + eps)
+//
+// Bound by HBM: parameters and moments in and out, gradients in.  A warp takes
+// 256 elements of one tensor, eight a lane, which are a block of an 8-bit state:
+// its largest magnitude is one reduction over the warp.  The tensors' pointers
+// are parameters of the kernel, so that a step needs no copy to the device; a
+// thread block finds its tensor by bisection.
+#include <algorithm>
+#include <cmath>
+#include <cstring>
+
+#include "polyq_dense_dev.cuh"
+#include "polyq_dev.cuh"
+#include "polyq_finetune.h"
+#include "polyq_fp4_dev.cuh"
+#include "polyq_internal.h"
+
+namespace {
+
+using namespace polyq;
+
+constexpr int kBlock = POLYQ_ADAMW_BLOCK;
+constexpr int kWarps = 8;  // of a thread block
+// Tensors of a launch: 4 KB of parameters for few of them, else what a kernel
+// may have (32 764 bytes).
+constexpr int kFew = 64, kMany = 640;
+
+struct Tensor {
+  void* p;
+  const void* grad;
+  void* copy;
+  int64_t n;
+  uint32_t at;     // first block of its state
+  uint32_t first;  // first block among the launch's
+  float decay, rate;
+};
+template <int N>
+struct AdamParams {
+  void* m;
+  void* v;
+  uint8_t* ms;
+  uint8_t* vs;
+  const float* lr_dev;
+  const int64_t* step_dev;
+  const float* grad_scale;
+  uint64_t seed;
+  float lr, inv_bc1, inv_root_bc2, b1, c1, b2, c2, eps, log_b1, log_b2;
+  uint32_t blocks;
+  int32_t n, copy_type;
+  Tensor t[N];
+};
+static_assert(sizeof(AdamParams<kMany>) <= 32764, "parameters of a kernel");
+
+__device__ __forceinline__ uint32_t mix(uint32_t h) {
+  h = (h ^ h >> 16) * 0x9E2D58A5u;
+  return (h ^ h >> 15) * 0x6C62272Du;
+}
+
+// Codes of magnitudes with MANT mantissa bits and one sign bit fewer than 8 bits
+// leave: a number whose smallest normal one is 1 is, scaled by 2^-126, an fp32
+// number of the same exponent field, subnormal ones included; its code is the
+// upper bits of that.
+template <int MANT>
+__device__ __forceinline__ float decode(uint32_t code, float unit) {  // unit: 2^(scale-127)
+  return __uint_as_float(code << (23 - MANT)) * 0x1p126f * unit;
+}
+// a times inv (2^(127-scale)), rounded down after adding u / 65536 of the last place.
+template <int MANT>
+__device__ __forceinline__ uint32_t encode(float a, float inv, uint32_t u) {
+  return (__float_as_uint(a * inv * 0x1p-126f) + (u << (23 - MANT - 16))) >> (23 - MANT);
+}
+// The smallest scale with which the largest magnitude `top` is within the codes (so
+// that none is cut off, which would bias the largest ones): the one that brings it to
+// 2^14 .. 2^15, or the next where it lies above the last code there.
+template <int MANT>
+__device__ __forceinline__ uint32_t scale_of(uint32_t top) {
+  const uint32_t past = top + (1u << (23 - MANT)) - 1;
+  return top >= 0x7F800000u ? 255u : (uint32_t)max((int)(past >> 23) - 14, 0);
+}
+__device__ __forceinline__ float unit_of(uint32_t s) {
+  return s == 255u ? __uint_as_float(0x7FC00000u) : s ? __uint_as_float(s << 23) : __uint_as_float(0x00400000u);
+}
+
+// What is the same for all elements of a tensor.
+struct Rates {
+  float gs, keep, step, inv_root_bc2;
+};
+
+// One block: elements i of the tensor from e0 on.  FULL: 256 of them, on 16 bytes.
+template <typename TP, typename TG, int BITS, bool FULL, int N>
+__device__ __forceinline__ void update_block(const AdamParams<N>& P, const Tensor& t, uint32_t block, const Rates& c,
+                                             uint32_t seed_key) {
+  const int lane = threadIdx.x & 31;
+  const int64_t e0 = (int64_t)block * kBlock, s0 = (int64_t)(t.at + block) * kBlock;
+  // the eight elements of a lane: neighbours, or every 32nd (see load8)
+  const int64_t col = FULL ? 8 * lane : lane;
+  const uint32_t mask = FULL ? 0xFFu : mask8<false>(e0 + col, 32, t.n);
+  Raw8<TP> rp;
+  Raw8<TG> rg;
+  load8<FULL>((const TP*)t.p + e0, col, 32, mask, rp);
+  load8<FULL>((const TG*)t.grad + e0, col, 32, mask, rg);
+  float m[8], v[8];
+  if constexpr (BITS == 32) {
+    Raw8<float> rm, rv;
+    load8<FULL>((const float*)P.m + s0, col, 32, mask, rm);
+    load8<FULL>((const float*)P.v + s0, col, 32, mask, rv);
+    to_float(rm, m);
+    to_float(rv, v);
+  } else {
+    uint8_t cm[8], cv[8];
+    const uint8_t *pm = (const uint8_t*)P.m + s0, *pv = (const uint8_t*)P.v + s0;
+    if constexpr (FULL) {
+      *reinterpret_cast<uint2*>(cm) = __ldcg(reinterpret_cast<const uint2*>(pm + col));
+      *reinterpret_cast<uint2*>(cv) = __ldcg(reinterpret_cast<const uint2*>(pv + col));
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        cm[i] = mask >> i & 1 ? __ldcg(pm + col + 32 * i) : 0;
+        cv[i] = mask >> i & 1 ? __ldcg(pv + col + 32 * i) : 0;
+      }
+    }
+    const float um = unit_of(__ldcg(P.ms + t.at + block)), uv = unit_of(__ldcg(P.vs + t.at + block));
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      m[i] = __uint_as_float(__float_as_uint(decode<3>(cm[i] & 127u, um)) | (uint32_t)(cm[i] >> 7) << 31);
+      v[i] = decode<4>(cv[i], uv);
+      v[i] *= v[i];
+    }
+  }
+  float p[8], g[8];
+  to_float(rp, p);
+  to_float(rg, g);
+  uint32_t top_m = 0, top_r = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const float s = g[i] * c.gs;
+    m[i] = fmaf(P.b1, m[i], P.c1 * s);
+    v[i] = fmaf(P.b2, v[i], P.c2 * s * s);
+    const float root = sqrtf(v[i]);
+    p[i] = fmaf(p[i], c.keep, -__fdividef(c.step * m[i], fmaf(root, c.inv_root_bc2, P.eps)));
+    if (BITS == 8) {
+      v[i] = root;
+      if (!FULL && !(mask >> i & 1)) m[i] = v[i] = 0.f;
+      top_m = max(top_m, __float_as_uint(m[i]) & 0x7FFFFFFFu);
+      top_r = max(top_r, __float_as_uint(root) & 0x7FFFFFFFu);
+    }
+  }
+  store8<FULL>((TP*)t.p + e0, col, 32, mask, p);
+  if (t.copy) {
+    if (sizeof(TP) < 4) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) p[i] = Elem<TP>::to(Elem<TP>::from(p[i]));  // once from p
+    }
+    const bool on16 = FULL && (uintptr_t)t.copy % 16 == 0;
+    if (FULL && !on16) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) any_store(t.copy, P.copy_type, e0 + col + i, p[i]);
+    } else if (P.copy_type == POLYQ_F32) {
+      store8<FULL>((float*)t.copy + e0, col, 32, mask, p);
+    } else if (P.copy_type == POLYQ_BF16) {
+      store8<FULL>((__nv_bfloat16*)t.copy + e0, col, 32, mask, p);
+    } else {
+      store8<FULL>((__half*)t.copy + e0, col, 32, mask, p);
+    }
+  }
+  if constexpr (BITS == 32) {
+    store8<FULL>((float*)P.m + s0, col, 32, mask, m);
+    store8<FULL>((float*)P.v + s0, col, 32, mask, v);
+  } else {
+    top_m = __reduce_max_sync(0xFFFFFFFFu, top_m);
+    top_r = __reduce_max_sync(0xFFFFFFFFu, top_r);
+    const uint32_t sm = scale_of<3>(top_m), sr = scale_of<4>(top_r);
+    const float im = sm == 255u ? 0.f : __uint_as_float((254u - sm) << 23);
+    const float ir = sr == 255u ? 0.f : __uint_as_float((254u - sr) << 23);
+    const uint64_t b64 = (uint64_t)t.at + block;
+    const uint32_t key = mix(mix((uint32_t)b64 ^ seed_key) ^ (uint32_t)(b64 >> 32) ^ (uint32_t)(P.seed >> 32));
+    uint8_t cm[8], cv[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const uint32_t e = FULL ? (uint32_t)(col + i) : (uint32_t)(col + 32 * i);
+      uint32_t u = mix(key + 0x9E3779B1u * e);
+      u ^= u >> 16;
+      const uint32_t sign = __float_as_uint(m[i]) >> 31;
+      uint32_t a = encode<3>(fabsf(m[i]), im, u & 0xFFFFu);
+      a |= a ? sign << 7 : 0u;
+      uint32_t r = encode<4>(v[i], ir, u >> 16);
+      r = v[i] > 0.f ? max(r, 1u) : r;
+      cm[i] = sm == 255u ? 0 : (uint8_t)a;
+      cv[i] = sr == 255u ? 0 : (uint8_t)r;
+    }
+    uint8_t *pm = (uint8_t*)P.m + s0, *pv = (uint8_t*)P.v + s0;
+    if constexpr (FULL) {
+      *reinterpret_cast<uint2*>(pm + col) = *reinterpret_cast<const uint2*>(cm);
+      *reinterpret_cast<uint2*>(pv + col) = *reinterpret_cast<const uint2*>(cv);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {  // (the whole block is the tensor's)
+        pm[col + 32 * i] = cm[i];
+        pv[col + 32 * i] = cv[i];
+      }
+    }
+    __syncwarp();  // every lane has read the block's scales
+    if (lane == 0) {
+      P.ms[t.at + block] = (uint8_t)sm;
+      P.vs[t.at + block] = (uint8_t)sr;
+    }
+  }
+}
+
+template <typename TP, typename TG, int BITS, int N>
+__global__ void __launch_bounds__(32 * kWarps) adamw_kernel(const __grid_constant__ AdamParams<N> P) {
+  pdl_trigger();
+  pdl_wait();
+  Rates c;
+  c.gs = 1.f;
+  if (P.grad_scale) {
+    c.gs = __ldcg(P.grad_scale);
+    if (!(fabsf(c.gs) < INFINITY)) return;
+  }
+  const float lr = P.lr_dev ? __ldcg(P.lr_dev) : P.lr;
+  float inv_bc1 = P.inv_bc1;
+  c.inv_root_bc2 = P.inv_root_bc2;
+  uint64_t seed = P.seed;
+  if (P.step_dev) {  // 1 - b^t = -expm1(t log b)
+    const int64_t t = max(__ldcg(P.step_dev), (int64_t)1);
+    seed += (uint64_t)t;
+    inv_bc1 = -1.f / expm1f((float)t * P.log_b1);
+    c.inv_root_bc2 = rsqrtf(-expm1f((float)t * P.log_b2));
+  }
+  const uint32_t seed_key = mix((uint32_t)seed + 1u);
+  const uint32_t stride = gridDim.x * kWarps;
+  for (uint32_t b0 = blockIdx.x * kWarps; b0 < P.blocks; b0 += stride) {
+    const uint32_t b = b0 + (threadIdx.x >> 5);
+    if (b >= P.blocks) return;
+    int lo = 0, hi = P.n - 1;  // the last tensor whose first block is b or before it
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if (P.t[mid].first <= b) lo = mid;
+      else hi = mid - 1;
+    }
+    const Tensor& t = P.t[lo];
+    const uint32_t block = b - t.first;
+    const float rate = lr * t.rate;
+    c.keep = 1.f - rate * t.decay;
+    c.step = rate * inv_bc1;
+    const bool full = ((int64_t)block + 1) * kBlock <= t.n && (((uintptr_t)t.p | (uintptr_t)t.grad) & 15) == 0;
+    if (full) update_block<TP, TG, BITS, true>(P, t, block, c, seed_key);
+    else update_block<TP, TG, BITS, false>(P, t, block, c, seed_key);
+  }
+}
+
+struct ValuesParams {
+  const uint8_t* m;
+  const uint8_t* v;
+  const uint8_t* ms;
+  const uint8_t* vs;
+  void* out[2];
+  int type[2];
+  uint32_t blocks;
+};
+template <int MANT>
+__device__ __forceinline__ void values_block(const uint8_t* codes, const uint8_t* scales, void* out, int type,
+                                             uint32_t b) {
+  const int lane = threadIdx.x & 31;
+  const int64_t e = (int64_t)b * kBlock + 8 * lane;
+  uint8_t c[8];
+  *reinterpret_cast<uint2*>(c) = __ldcg(reinterpret_cast<const uint2*>(codes + e));
+  const float unit = unit_of(__ldcg(scales + b));
+  float v[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    v[i] = decode<MANT>(MANT == 3 ? c[i] & 127u : c[i], unit);
+    if (MANT == 3 && c[i] > 127) v[i] = -v[i];
+  }
+  if ((uintptr_t)out % 16) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) any_store(out, type, e + i, v[i]);
+  } else if (type == POLYQ_F32) {
+    store8<true>((float*)out, e, 1, 0xFFu, v);
+  } else if (type == POLYQ_BF16) {
+    store8<true>((__nv_bfloat16*)out, e, 1, 0xFFu, v);
+  } else {
+    store8<true>((__half*)out, e, 1, 0xFFu, v);
+  }
+}
+__global__ void __launch_bounds__(32 * kWarps) adamw_values_kernel(const __grid_constant__ ValuesParams P) {
+  pdl_trigger();
+  pdl_wait();
+  for (uint32_t b = blockIdx.x * kWarps + (threadIdx.x >> 5); b < P.blocks; b += gridDim.x * kWarps) {
+    if (P.out[0]) values_block<3>(P.m, P.ms, P.out[0], P.type[0], b);
+    if (P.out[1]) values_block<4>(P.v, P.vs, P.out[1], P.type[1], b);
+  }
+}
+
+template <int N, int BITS, typename TP>
+void* pick(int tg) {
+  return tg == POLYQ_F32    ? (void*)adamw_kernel<TP, float, BITS, N>
+         : tg == POLYQ_BF16 ? (void*)adamw_kernel<TP, __nv_bfloat16, BITS, N>
+                            : (void*)adamw_kernel<TP, __half, BITS, N>;
+}
+template <int N, int BITS>
+void* pick(int tp, int tg) {
+  return tp == POLYQ_F32    ? pick<N, BITS, float>(tg)
+         : tp == POLYQ_BF16 ? pick<N, BITS, __nv_bfloat16>(tg)
+                            : pick<N, BITS, __half>(tg);
+}
+
+int launch(void* f, uint32_t blocks, void* params, void* stream, const char* who) {
+  int sms = 0;
+  int rc = polyq_sm_count(&sms);
+  if (rc) return rc;
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.stream = (cudaStream_t)stream;
+  cfg.attrs = at;
+  cfg.numAttrs = 1;
+  cfg.gridDim = dim3((unsigned)std::min<int64_t>(((int64_t)blocks + kWarps - 1) / kWarps, (int64_t)sms * 8));
+  cfg.blockDim = dim3(32 * kWarps);
+  void* args[] = {params};
+  cudaError_t ce = cudaLaunchKernelExC(&cfg, f, args);
+  if (ce != cudaSuccess) return polyq_set_error(POLYQ_ECUDA, "%s: launch: %s", who, cudaGetErrorString(ce));
+  return POLYQ_OK;
+}
+
+template <int N>
+int run_step(const polyq_adamw_tensor* tensors, int n, int p_type, int grad_type, int copy_type,
+             const polyq_adamw_state* state, const polyq_adamw_hyper* h, void* stream, const char* who) {
+  AdamParams<N> P;
+  P.m = state->m;
+  P.v = state->v;
+  P.ms = state->m_scales;
+  P.vs = state->v_scales;
+  P.lr_dev = h->lr_dev;
+  P.step_dev = h->step_dev;
+  P.grad_scale = h->grad_scale;
+  P.seed = h->seed;
+  P.lr = (float)h->lr;
+  P.inv_bc1 = (float)(1.0 / (1.0 - std::pow(h->beta1, (double)h->step)));
+  P.inv_root_bc2 = (float)(1.0 / std::sqrt(1.0 - std::pow(h->beta2, (double)h->step)));
+  P.b1 = (float)h->beta1;
+  P.c1 = (float)(1.0 - h->beta1);
+  P.b2 = (float)h->beta2;
+  P.c2 = (float)(1.0 - h->beta2);
+  P.eps = (float)h->eps;
+  P.log_b1 = (float)std::log(h->beta1);
+  P.log_b2 = (float)std::log(h->beta2);
+  P.copy_type = copy_type;
+  for (int i0 = 0; i0 < n;) {
+    int64_t blocks = 0;
+    int k = 0;
+    for (; k < N && i0 + k < n; ++k) {
+      const polyq_adamw_tensor& t = tensors[i0 + k];
+      const int64_t b = (t.n + kBlock - 1) / kBlock;
+      if (k && blocks + b > 0x7FFFFFFF) break;
+      P.t[k] = Tensor{t.p, t.grad, t.copy, t.n, (uint32_t)(t.at / kBlock), (uint32_t)blocks, t.decay, t.rate};
+      blocks += b;
+    }
+    P.n = k;
+    P.blocks = (uint32_t)blocks;
+    void* f = state->bits == 8 ? pick<N, 8>(p_type, grad_type) : pick<N, 32>(p_type, grad_type);
+    const int rc = launch(f, P.blocks, &P, stream, who);
+    if (rc) return rc;
+    i0 += k;
+  }
+  return POLYQ_OK;
+}
+
+bool good_type(int t) { return t == POLYQ_F32 || t == POLYQ_BF16 || t == POLYQ_F16; }
+bool misaligned(const void* p, int type) { return (uintptr_t)p % (type == POLYQ_F32 ? 4 : 2) != 0; }
+
+int check_state(const polyq_adamw_state* s, const char* who) {
+  if (!s || !s->m || !s->v || (uintptr_t)s->m % 16 || (uintptr_t)s->v % 16)
+    return polyq_set_error(POLYQ_EINVAL, "%s: the state's m and v must be 16-byte aligned and not NULL", who);
+  if (s->bits != 8 && s->bits != 32) return polyq_set_error(POLYQ_EINVAL, "%s: a state of %d bits", who, s->bits);
+  if (s->bits == 8 && (!s->m_scales || !s->v_scales))
+    return polyq_set_error(POLYQ_EINVAL, "%s: a state of 8 bits needs scales", who);
+  if (s->n < 1 || s->n % kBlock || s->n > (1ll << 38))
+    return polyq_set_error(POLYQ_EINVAL, "%s: a state of %lld elements", who, (long long)s->n);
+  return POLYQ_OK;
+}
+
+}  // namespace
+
+extern "C" int polyq_adamw_step(const polyq_adamw_tensor* tensors, int32_t n_tensors, int32_t p_type,
+                                int32_t grad_type, int32_t copy_type, const polyq_adamw_state* state,
+                                const polyq_adamw_hyper* hyper, void* stream) {
+  static const char* who = "polyq_adamw_step";
+  polyq_clear_error();
+  if (!tensors || n_tensors < 1 || !hyper)
+    return polyq_set_error(POLYQ_EINVAL, "%s: no tensors or no rates", who);
+  int rc = check_state(state, who);
+  if (rc) return rc;
+  if (!good_type(p_type) || !good_type(grad_type))
+    return polyq_set_error(POLYQ_EINVAL, "%s: types %d and %d", who, p_type, grad_type);
+  const polyq_adamw_hyper& h = *hyper;
+  if (!(h.lr >= 0.0) || !std::isfinite((float)h.lr) || !(h.beta1 >= 0.0 && h.beta1 < 1.0) ||
+      !(h.beta2 >= 0.0 && h.beta2 < 1.0) || !((float)h.eps > 0.f) || !(h.eps <= 1e30) || h.step < 1)
+    return polyq_set_error(POLYQ_EINVAL, "%s: lr %g, betas %g and %g, eps %g, step %lld", who, h.lr, h.beta1, h.beta2,
+                           h.eps, (long long)h.step);
+  if ((uintptr_t)h.lr_dev % 4 || (uintptr_t)h.step_dev % 8 || (uintptr_t)h.grad_scale % 4)
+    return polyq_set_error(POLYQ_EINVAL, "%s: device values must be aligned to their size", who);
+  for (int i = 0; i < n_tensors; ++i) {
+    const polyq_adamw_tensor& t = tensors[i];
+    if (!t.p || !t.grad || misaligned(t.p, p_type) || misaligned(t.grad, grad_type))
+      return polyq_set_error(POLYQ_EINVAL, "%s: tensor %d: p and grad must be aligned to their elements", who, i);
+    if (t.copy && (!good_type(copy_type) || misaligned(t.copy, copy_type)))
+      return polyq_set_error(POLYQ_EINVAL, "%s: tensor %d: copy of type %d", who, i, copy_type);
+    if (t.n < 1 || t.n > (1ll << 38) || t.at < 0 || t.at % kBlock || t.at > state->n ||
+        (t.n + kBlock - 1) / kBlock * kBlock > state->n - t.at)
+      return polyq_set_error(POLYQ_EINVAL, "%s: tensor %d: %lld elements at %lld of a state of %lld", who, i,
+                             (long long)t.n, (long long)t.at, (long long)state->n);
+    if (!(t.decay >= 0.f) || !std::isfinite(t.decay) || !(t.rate >= 0.f) || !std::isfinite(t.rate))
+      return polyq_set_error(POLYQ_EINVAL, "%s: tensor %d: decay %g, rate %g", who, i, (double)t.decay, (double)t.rate);
+  }
+  return n_tensors <= kFew ? run_step<kFew>(tensors, n_tensors, p_type, grad_type, copy_type, state, hyper, stream, who)
+                           : run_step<kMany>(tensors, n_tensors, p_type, grad_type, copy_type, state, hyper, stream, who);
+}
+
+extern "C" int polyq_adamw_values(const polyq_adamw_state* state, const polyq_dense* m, const polyq_dense* root,
+                                  void* stream) {
+  static const char* who = "polyq_adamw_values";
+  polyq_clear_error();
+  int rc = check_state(state, who);
+  if (rc) return rc;
+  if (state->bits != 8) return polyq_set_error(POLYQ_EINVAL, "%s: a state of %d bits", who, state->bits);
+  if (!m && !root) return polyq_set_error(POLYQ_EINVAL, "%s: neither m nor root is wanted", who);
+  ValuesParams P;
+  memset(&P, 0, sizeof P);
+  const polyq_dense* d[2] = {m, root};
+  for (int i = 0; i < 2; ++i) {
+    if (!d[i]) continue;
+    if (!d[i]->data || !good_type(d[i]->type) || misaligned(d[i]->data, d[i]->type))
+      return polyq_set_error(POLYQ_EINVAL, "%s: %s must be aligned to its elements", who, i ? "root" : "m");
+    P.out[i] = d[i]->data;
+    P.type[i] = d[i]->type;
+  }
+  P.m = (const uint8_t*)state->m;
+  P.v = (const uint8_t*)state->v;
+  P.ms = state->m_scales;
+  P.vs = state->v_scales;
+  P.blocks = (uint32_t)(state->n / kBlock);
+  return launch((void*)adamw_values_kernel, P.blocks, &P, stream, who);
+}

@@ -12,6 +12,7 @@
 #include <cmath>
 #include <cstring>
 
+#include "polyq_dense_dev.cuh"
 #include "polyq_dev.cuh"
 #include "polyq_fp4_dev.cuh"
 #include "polyq_internal.h"
@@ -34,34 +35,12 @@ struct QuantParams {
   float up;               // see scaled_to_odd
 };
 
-template <typename T>
-struct Elem;
-template <>
-struct Elem<float> {
-  static __device__ __forceinline__ float to(float v) { return v; }
-  static __device__ __forceinline__ float from(float v) { return v; }
-};
-template <>
-struct Elem<__nv_bfloat16> {
-  static __device__ __forceinline__ float to(__nv_bfloat16 v) { return __bfloat162float(v); }
-  static __device__ __forceinline__ __nv_bfloat16 from(float v) { return __float2bfloat16_rn(v); }
-};
-template <>
-struct Elem<__half> {
-  static __device__ __forceinline__ float to(__half v) { return __half2float(v); }
-  static __device__ __forceinline__ __half from(float v) { return __float2half_rn(v); }
-};
-
 // 8 elements from k on as they lie in memory, and as floats; zeros past K.  VEC:
 // rows start on 16 bytes.  (Two steps, so that the loads of several rows are in
 // flight before the first is converted: 13824 x 5120 bf16 63 us with one.)
 // Inputs are read once, through L2, by ordinary loads: a grid may be on its SM
 // before the one that writes them has begun, and the grid dependency's wait orders
 // these with those writes, but not loads through the read-only path.
-template <typename T>
-struct Raw8 {
-  uint4 w[sizeof(T) * 8 / 16];
-};
 template <typename T, bool FULL>
 __device__ __forceinline__ void load8(const T* __restrict__ row, int64_t k, int64_t K, Raw8<T>& r) {
   constexpr int N16 = sizeof(T) * 8 / 16;
@@ -114,13 +93,6 @@ __device__ __forceinline__ uint32_t abs_max(const Raw8<T>& r) {
   const uint16_t h = (uint16_t)max(m & 0xFFFFu, m >> 16);
   return __float_as_uint(Elem<T>::to(*reinterpret_cast<const T*>(&h))) & 0x7FFFFFFFu;
 }
-template <typename T>
-__device__ __forceinline__ void to_float(const Raw8<T>& r, float (&v)[8]) {
-  const T* e = reinterpret_cast<const T*>(r.w);
-#pragma unroll
-  for (int i = 0; i < 8; ++i) v[i] = Elem<T>::to(e[i]);
-}
-
 // A CTA takes 1024 elements of ROWS consecutive rows, a warp 256, the loads of
 // its rows in flight together.  FULL: all of a warp's elements exist (the
 // checks took a third of the instructions, which bound 16-bit inputs: 13824 x

@@ -113,6 +113,22 @@ class Dense(C.Structure):
     _fields_ = [("data", C.c_void_p), ("stride", C.c_int64), ("type", C.c_int32)]
 
 
+class AdamwTensor(C.Structure):
+    _fields_ = [("p", C.c_void_p), ("grad", C.c_void_p), ("copy", C.c_void_p), ("n", C.c_int64),
+                ("at", C.c_int64), ("decay", C.c_float), ("rate", C.c_float)]
+
+
+class AdamwState(C.Structure):
+    _fields_ = [("m", C.c_void_p), ("v", C.c_void_p), ("m_scales", C.c_void_p),
+                ("v_scales", C.c_void_p), ("n", C.c_int64), ("bits", C.c_int32)]
+
+
+class AdamwHyper(C.Structure):
+    _fields_ = [("lr", C.c_double), ("beta1", C.c_double), ("beta2", C.c_double),
+                ("eps", C.c_double), ("step", C.c_int64), ("seed", C.c_uint64),
+                ("lr_dev", C.c_void_p), ("step_dev", C.c_void_p), ("grad_scale", C.c_void_p)]
+
+
 _P = C.c_void_p
 _FP4, _DENSE = C.POINTER(Fp4Desc), C.POINTER(Dense)
 _SIGS = {
@@ -172,6 +188,16 @@ _SIGS = {
                                                      C.POINTER(C.c_size_t)]),
     "polyq_ffn_backward": (C.c_int, [_DENSE, _DENSE, _DENSE, C.c_int64, C.c_int64, C.c_int64, _P,
                                      _DENSE, _DENSE, _DENSE, _DENSE, _P, C.c_size_t, _P]),
+    # include/polyq_finetune.h
+    "polyq_layernorm_forward": (C.c_int, [_DENSE, C.c_int64, C.c_int64, _DENSE, _DENSE, C.c_float,
+                                          C.c_int, _DENSE, _P, _P]),
+    "polyq_layernorm_workspace_bytes": (C.c_int, [C.c_int64, C.c_int64, C.POINTER(C.c_size_t)]),
+    "polyq_layernorm_backward": (C.c_int, [_DENSE, C.c_int64, C.c_int64, _DENSE, _P, C.c_int,
+                                           _DENSE, _DENSE, _DENSE, _DENSE, _DENSE, _P, C.c_size_t,
+                                           _P]),
+    "polyq_adamw_step": (C.c_int, [C.POINTER(AdamwTensor), C.c_int32, C.c_int32, C.c_int32,
+                                   C.c_int32, C.POINTER(AdamwState), C.POINTER(AdamwHyper), _P]),
+    "polyq_adamw_values": (C.c_int, [C.POINTER(AdamwState), _DENSE, _DENSE, _P]),
 }
 for _name, (_res, _args) in _SIGS.items():
     _fn = getattr(_lib, _name)
@@ -1077,3 +1103,241 @@ def ffn_backward(x, gate, up, saved, dh, dx=None, dgate=None, dup=None, need_dx=
     _check(_lib.polyq_ffn_backward(C.byref(ix), C.byref(ig), C.byref(iu), T, F, K, ps, C.byref(idh),
                                    ox, og, ou, ws.data_ptr(), ws.numel(), st))
     return dx, dgate, dup
+
+
+# ---- layer norm, AdamW and low-rank adapters (include/polyq_finetune.h) ----
+ADAMW_BLOCK = 256  # elements of an 8-bit state that share a scale
+
+
+def _vector(t, name, K, dev):
+    """Descriptor of K contiguous elements on CUDA device `dev` (None: none)."""
+    if t is None:
+        return None
+    try:
+        ty = _type_of(t.dtype)
+        good = ty is not None and t.get_device() == dev and t.shape == (K,) and t.is_contiguous()
+    except AttributeError:
+        good = False
+    if not good:
+        raise ValueError(f"{name} must be a contiguous fp32, bf16 or fp16 tensor [{K}] on cuda:{dev}")
+    return C.byref(Dense(t.data_ptr(), K, ty))
+
+
+def layernorm_stats(rows, device="cuda"):
+    """The buffer that layernorm_forward fills for layernorm_backward: mean and
+    1 / standard deviation of every row."""
+    import torch
+    return torch.empty((rows, 2), dtype=torch.float32, device=device)
+
+
+def _stats(stats, rows, dev):
+    import torch
+    if (not isinstance(stats, torch.Tensor) or stats.dtype != torch.float32 or stats.get_device() != dev
+            or stats.shape != (rows, 2) or not stats.is_contiguous()):
+        raise ValueError(f"stats must be layernorm_stats({rows}) on cuda:{dev}")
+    return stats.data_ptr()
+
+
+def layernorm_workspace(rows, K, device="cuda"):
+    """A workspace for layernorm_backward on the current device."""
+    import torch
+    n = C.c_size_t()
+    _check(_lib.polyq_layernorm_workspace_bytes(int(rows), int(K), C.byref(n)))
+    return torch.empty(n.value, dtype=torch.uint8, device=device)
+
+
+def layernorm_forward(x, weight=None, bias=None, eps=1e-5, center=True, y=None, stats=None,
+                      dtype=None, stream=None):
+    """y = (x - mean) / sqrt(var + eps) * weight + bias over the rows of x (fp32,
+    bf16 or fp16, any row stride); center=False: RMS norm, with a mean of 0.  y:
+    x's type by default, may be x itself.  `stats` (layernorm_stats) receives what
+    layernorm_backward needs."""
+    dx = _dense(x, "x")
+    dev = x.get_device()
+    st = _stream_on(dev, "x", stream)
+    rows, K = x.shape
+    if y is None:
+        import torch
+        y = _made(stream, torch.empty, (rows, K), dtype=dtype or x.dtype, device=x.device)
+    dy = _dense(y, "y", rows, K, dev, dtype)
+    _check(_lib.polyq_layernorm_forward(
+        C.byref(dx), rows, K, _vector(weight, "weight", K, dev), _vector(bias, "bias", K, dev), eps,
+        1 if center else 0, C.byref(dy), None if stats is None else _stats(stats, rows, dev), st))
+    return y
+
+
+def layernorm_backward(x, weight, stats, dy, center=True, dx=None, dweight=None, dbias=None,
+                       need_dx=True, need_weight=True, need_bias=True, residual=None, workspace=None,
+                       stream=None):
+    """Gradients (dx, dweight, dbias) of layernorm_forward for the gradient dy of y
+    and the same x, weight (None: 1), center and its stats.  dx is of x's type, with
+    `residual` (of that type, may be dx) added to it: the gradient that reaches x
+    beside the norm.  dweight and dbias are of the weight's type (fp32 without one)
+    or of that of the buffers passed.  Those not needed are None."""
+    ix = _dense(x, "x")
+    dev = x.get_device()
+    st = _stream_on(dev, "x", stream)
+    rows, K = x.shape
+    idy = _dense(dy, "dy", rows, K, dev)
+    import torch
+    vt = torch.float32 if weight is None else weight.dtype
+    if dx is None and need_dx:
+        dx = _made(stream, torch.empty, (rows, K), dtype=x.dtype, device=x.device)
+    if dweight is None and need_weight:
+        dweight = _made(stream, torch.empty, K, dtype=vt, device=x.device)
+    if dbias is None and need_bias:
+        dbias = _made(stream, torch.empty, K, dtype=vt, device=x.device)
+    odx = None if dx is None else C.byref(_dense(dx, "dx", rows, K, dev, x.dtype))
+    if residual is not None and dx is None:
+        raise ValueError("a residual is added to dx, which is not wanted")
+    ires = None if residual is None else C.byref(_dense(residual, "residual", rows, K, dev, x.dtype))
+    wp = wn = 0
+    if dweight is not None or dbias is not None:
+        ws = _workspace_at(workspace, dev, stream, layernorm_workspace, rows, K, x.device)
+        wp, wn = ws.data_ptr(), ws.numel()
+    _check(_lib.polyq_layernorm_backward(
+        C.byref(ix), rows, K, _vector(weight, "weight", K, dev), _stats(stats, rows, dev),
+        1 if center else 0, C.byref(idy), ires, odx, _vector(dweight, "dweight", K, dev),
+        _vector(dbias, "dbias", K, dev), wp, wn, st))
+    return dx, dweight, dbias
+
+
+class AdamState:
+    """The moments of tensors of the given sizes, all zero: flat buffers `m` and `v`
+    in which tensor i begins at `offsets[i]`.  bits=32: fp32.  bits=8: uint8 codes,
+    `v` those of the second moment's root, with a scale byte per 256 elements in
+    `m_scales` and `v_scales` (the formats of polyq_finetune.h).  The buffers are
+    what a checkpoint holds."""
+
+    def __init__(self, sizes, bits=32, device="cuda"):
+        import torch
+        sizes = [int(n) for n in sizes]
+        if bits not in (8, 32):
+            raise ValueError(f"bits must be 8 or 32, not {bits}")
+        if not sizes or min(sizes) < 1:
+            raise ValueError("every tensor has at least one element, and there is at least one")
+        offsets, at = [], 0
+        for n in sizes:
+            offsets.append(at)
+            at += -(-n // ADAMW_BLOCK) * ADAMW_BLOCK
+
+        def new(n):
+            return torch.zeros(n, dtype=torch.uint8 if bits == 8 else torch.float32, device=device)
+
+        self.sizes, self.offsets, self.bits = tuple(sizes), tuple(offsets), bits
+        self.m, self.v = new(at), new(at)
+        self.m_scales, self.v_scales = (new(at // ADAMW_BLOCK), new(at // ADAMW_BLOCK)) \
+            if bits == 8 else (None, None)
+
+    def _desc(self, dev=None):
+        n = self.offsets[-1] + -(-self.sizes[-1] // ADAMW_BLOCK) * ADAMW_BLOCK
+        import torch
+        ty = torch.uint8 if self.bits == 8 else torch.float32
+        at = self.m.get_device() if dev is None else dev
+        for name, wide in (("m", n), ("v", n), ("m_scales", n // ADAMW_BLOCK),
+                           ("v_scales", n // ADAMW_BLOCK)):
+            t = getattr(self, name)
+            if self.bits == 32 and t is None:
+                continue
+            if (not isinstance(t, torch.Tensor) or t.dtype != ty or t.get_device() != at or at < 0
+                    or t.shape != (wide,) or not t.is_contiguous()):
+                raise ValueError(f"the state's {name} must be a contiguous {ty} tensor [{wide}] "
+                                 f"on {'a CUDA device' if at < 0 else f'cuda:{at}'}")
+        return AdamwState(self.m.data_ptr(), self.v.data_ptr(),
+                          self.m_scales.data_ptr() if self.bits == 8 else None,
+                          self.v_scales.data_ptr() if self.bits == 8 else None, n, self.bits)
+
+    def values(self, m=None, root=None, dtype=None, stream=None):
+        """What an 8-bit state's codes stand for: (m, root of v), flat like the codes,
+        bf16 by default (which holds them exactly), fp32 or fp16."""
+        import torch
+        d = self._desc()
+        dev = self.m.get_device()
+        st = _stream_on(dev, "the state", stream)
+        if m is None:
+            m = _made(stream, torch.empty, d.n, dtype=dtype or torch.bfloat16, device=self.m.device)
+        if root is None:
+            root = _made(stream, torch.empty, d.n, dtype=dtype or torch.bfloat16, device=self.m.device)
+        _check(_lib.polyq_adamw_values(C.byref(d), _vector(m, "m", d.n, dev),
+                                       _vector(root, "root", d.n, dev), st))
+        return m, root
+
+
+class AdamW:
+    """Steps of AdamW over tensors that stay where they are: their addresses are laid
+    out once, and a step is one launch per 640 tensors of the same types.
+
+    params, grads: contiguous CUDA tensors (fp32, bf16 or fp16) of the sizes of
+    `state`; copies: None or tensors (or None) that receive the new parameters in
+    another type; weight_decay, lr_scale: a number, or one for each tensor."""
+
+    def __init__(self, params, grads, state, copies=None, weight_decay=0.01, lr_scale=1.0):
+        params, grads = list(params), list(grads)
+        n = len(params)
+        copies = [None] * n if copies is None else list(copies)
+        decay = [float(weight_decay)] * n if isinstance(weight_decay, (int, float)) else list(weight_decay)
+        rate = [float(lr_scale)] * n if isinstance(lr_scale, (int, float)) else list(lr_scale)
+        if not isinstance(state, AdamState) or not (
+                n == len(state.sizes) == len(grads) == len(copies) == len(decay) == len(rate)):
+            raise ValueError("params, grads, copies, weight_decay and lr_scale must be as many as "
+                             "the state's tensors")
+        self.state, self._groups = state, {}
+        self._kept = (params, grads, copies)
+        dev = self._dev = params[0].get_device() if hasattr(params[0], "get_device") else -1
+        groups = {}
+        for i in range(n):
+            types = []
+            for name, t in (("params", params[i]), ("grads", grads[i]), ("copies", copies[i])):
+                if name == "copies" and t is None:
+                    types.append(-1)
+                    continue
+                try:
+                    ty = _type_of(t.dtype)
+                    good = (ty is not None and t.get_device() == dev and dev >= 0
+                            and t.is_contiguous() and t.numel() == state.sizes[i])
+                except AttributeError:
+                    good = False
+                if not good:
+                    raise ValueError(f"{name}[{i}] must be a contiguous fp32, bf16 or fp16 tensor of "
+                                     f"{state.sizes[i]} elements on the device of params[0], a CUDA one")
+                types.append(ty)
+            groups.setdefault(tuple(types), []).append(AdamwTensor(
+                params[i].data_ptr(), grads[i].data_ptr(),
+                None if copies[i] is None else copies[i].data_ptr(), state.sizes[i],
+                state.offsets[i], decay[i], rate[i]))
+        state._desc(dev)
+        self._groups = [(k, (AdamwTensor * len(v))(*v), len(v)) for k, v in groups.items()]
+
+    def _scalar(self, t, name, dtype):
+        import torch
+        if (not isinstance(t, torch.Tensor) or t.dtype != dtype or t.numel() != 1
+                or t.get_device() != self._dev):
+            raise ValueError(f"{name} must be a number or a {dtype} tensor of one element on "
+                             f"cuda:{self._dev}")
+        return t.data_ptr()
+
+    def step(self, lr, step, betas=(0.9, 0.999), eps=1e-8, seed=0, grad_scale=None, stream=None):
+        """One step.  `step` counts from 1.  lr and step may be tensors of one element on
+        the device (fp32 and int64), read when the step runs, as a captured one needs
+        them; the number of the step is then added to the seed.  grad_scale: a factor of
+        all gradients, an fp32 tensor of one element; where it is not finite the step
+        leaves everything as it was.  seed: of the rounding of 8-bit states, another one
+        for each step."""
+        h = AdamwHyper(beta1=betas[0], beta2=betas[1], eps=eps, seed=seed & 0xFFFFFFFFFFFFFFFF, step=1)
+        st = _stream_on(self._dev, "the tensors", stream)
+        if isinstance(lr, (int, float)):
+            h.lr = lr
+        else:
+            import torch
+            h.lr_dev = self._scalar(lr, "lr", torch.float32)
+        if isinstance(step, int):
+            h.step = step
+        else:
+            import torch
+            h.step_dev = self._scalar(step, "step", torch.int64)
+        if grad_scale is not None:
+            import torch
+            h.grad_scale = self._scalar(grad_scale, "grad_scale", torch.float32)
+        d = self.state._desc(self._dev)
+        for (tp, tg, tc), tensors, n in self._groups:
+            _check(_lib.polyq_adamw_step(tensors, n, tp, tg, tc, C.byref(d), C.byref(h), st))
