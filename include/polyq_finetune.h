@@ -138,6 +138,72 @@ int polyq_adamw_step(const polyq_adamw_tensor* tensors, int32_t n_tensors, int32
 int polyq_adamw_values(const polyq_adamw_state* state, const polyq_dense* m, const polyq_dense* root,
                        void* stream);
 
+/* ---- low-rank adapters ---- */
+
+#define POLYQ_ADAPTERS_MAX_RANK 128
+
+/* n adapters beside a projection from K to N channels, in one 16-bit type (POLYQ_BF16 or
+ * POLYQ_F16): a [n][R][K] and b [n][N][R], 16-byte aligned, rows of a_stride and b_stride
+ * elements, a_next and b_next elements from one adapter to the next, all multiples of 8.
+ * R is a multiple of 8 (above POLYQ_ADAPTERS_MAX_RANK POLYQ_EUNSUPPORTED); an adapter of a
+ * smaller rank has it in `ranks`, and what a and b hold past it does not matter. */
+typedef struct {
+  const void* a;
+  const void* b;
+  int64_t a_stride, a_next, b_stride, b_next;
+  int64_t K, N;
+  int32_t n, R, type;
+  const float* scales;   /* device [n], or NULL: 1 */
+  const int32_t* ranks;  /* device [n], 0..R, or NULL: R */
+} polyq_adapters;
+
+/* Which rows go through which adapter: segment i is rows offsets[i] .. offsets[i+1] - 1
+ * (ascending) and adapter ids[i]; a number outside 0..n-1 is none.  Segments may be empty,
+ * several may have one adapter, and rows before the first and behind the last are left
+ * as they are.  Both are device arrays, read when the call runs; offsets outside the
+ * tensors' rows are taken as their ends, and where they fall the rows that segments share
+ * are unspecified. */
+typedef struct {
+  const int32_t* offsets;  /* [n+1] */
+  const int32_t* ids;      /* [n] */
+  int32_t n;
+} polyq_segments;
+
+/* Bytes of the workspace of the calls below for T rows. */
+int polyq_adapters_workspace_bytes(int64_t T, int32_t R, size_t* bytes);
+
+/* y[t][n] = residual[t][n] + s sum_j v[t][j] b[n][j],  v[t][j] = sum_k x[t][k] a[j][k]
+ * of the row's adapter (scale s); rows of segments without one get the residual.  x [T][K] of the
+ * adapters' type, 16-byte aligned with a stride that is a multiple of 8; y [T][N] of
+ * that type or POLYQ_F32; residual NULL (0) or of y's type: the projection's result, its
+ * data may be y's, with y's stride.  Products of x and a are exact and their sums in
+ * fp32, as v is; v enters the second product with 16 (bf16) or 21 (fp16) significant
+ * bits; one rounding to y's type.  saved: NULL, or device memory of
+ * polyq_adapters_workspace_bytes, 16-byte aligned, which receives v [T][R] for the
+ * backward pass (rows without an adapter are left as they were); the workspace is not
+ * used then.  Two launches. */
+int polyq_adapters_forward(const polyq_dense* x, int64_t T, const polyq_adapters* adapters,
+                           const polyq_segments* segments, const polyq_dense* residual,
+                           const polyq_dense* y, float* saved, void* workspace,
+                           size_t workspace_bytes, void* stream);
+
+/* Gradients for the gradient dy [T][N] of y (as x is: type, alignment) and the `saved`
+ * of the forward pass:
+ *   dv[t][j] = s sum_n dy[t][n] b[n][j],  dx[t][k] = residual[t][k] + sum_j dv[t][j] a[j][k]
+ *   da[j][k] = sum over the adapter's rows of dv[t][j] x[t][k]
+ *   db[n][j] = s sum over the adapter's rows of dy[t][n] v[t][j]
+ * dx NULL or as y, with its residual (the gradient that reaches x through the
+ * projection); da [n][R][K] and db [n][N][R] without gaps, of grad_type (the adapters'
+ * type or POLYQ_F32), each may be NULL.  All adapters' gradients are written: zeros where no row
+ * has the adapter, and past its rank.  At least one of the three is wanted; saved
+ * may be NULL without db.  dv is in fp32, and enters its products as v does.  Up to three
+ * launches. */
+int polyq_adapters_backward(const polyq_dense* x, int64_t T, const polyq_adapters* adapters,
+                            const polyq_segments* segments, const float* saved,
+                            const polyq_dense* dy, const polyq_dense* residual,
+                            const polyq_dense* dx, void* da, void* db, int32_t grad_type,
+                            void* workspace, size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

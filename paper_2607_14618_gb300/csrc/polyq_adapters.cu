@@ -1,0 +1,268 @@
+// Entry points of the low-rank adapters: checks, tiles and launches.
+#include <algorithm>
+#include <atomic>
+#include <cstring>
+
+#include "polyq_adapters_dev.cuh"
+#include "polyq_fp4_dev.cuh"
+#include "polyq_internal.h"
+
+namespace polyq {
+namespace lora {
+extern template Kernel shrink_of<__nv_bfloat16>(int bm, int rn, bool trans);
+extern template Kernel expand_of<__nv_bfloat16>(int bm, int rn, bool trans, bool f32);
+extern template Kernel gradients_of<__nv_bfloat16>(int rn);
+extern template Kernel shrink_of<__half>(int bm, int rn, bool trans);
+extern template Kernel expand_of<__half>(int bm, int rn, bool trans, bool f32);
+extern template Kernel gradients_of<__half>(int rn);
+}  // namespace lora
+}  // namespace polyq
+
+namespace {
+
+using namespace polyq;
+using lora::Kernel;
+
+constexpr int64_t kMaxSize = 1 << 24;
+
+// Devices on which a kernel may use its shared memory (a bit each), by the kernel's tile.
+std::atomic<uint64_t> g_ready[256];
+
+int launch(const Kernel& k, int which, dim3 grid, int cluster, void* params, void* stream, const char* who) {
+  int dev = 0;
+  cudaError_t ce = cudaGetDevice(&dev);
+  if (ce == cudaSuccess) {
+    const uint64_t bit = dev < 64 ? 1ull << dev : 0;
+    if (!(g_ready[which].load(std::memory_order_acquire) & bit)) {
+      ce = cudaFuncSetAttribute(k.f, cudaFuncAttributeMaxDynamicSharedMemorySize, k.smem);
+      if (ce == cudaSuccess) g_ready[which].fetch_or(bit, std::memory_order_release);
+    }
+  }
+  if (ce == cudaSuccess) {
+    cudaLaunchAttribute at[2];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    at[1].id = cudaLaunchAttributeClusterDimension;
+    at[1].val.clusterDim.x = cluster;
+    at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.stream = (cudaStream_t)stream;
+    cfg.attrs = at;
+    cfg.numAttrs = cluster > 1 ? 2 : 1;
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(lora::kThreads);
+    cfg.dynamicSmemBytes = k.smem;
+    void* args[] = {params};
+    ce = cudaLaunchKernelExC(&cfg, k.f, args);
+  }
+  if (ce != cudaSuccess) return polyq_set_error(POLYQ_ECUDA, "%s: launch: %s", who, cudaGetErrorString(ce));
+  return POLYQ_OK;
+}
+
+int rank_tile(int R) { return R <= 16 ? 16 : R <= 32 ? 32 : R <= 64 ? 64 : 128; }
+int rank_index(int rn) { return rn == 16 ? 0 : rn == 32 ? 1 : rn == 64 ? 2 : 3; }
+
+// Tiles of bm rows in any T rows of n segments: each has at most one that is not full.
+int64_t most_tiles(int64_t T, int n, int bm) { return std::min<int64_t>(T, T / bm + n); }
+
+// v [T][R] of x times one of the adapters' matrices.
+int shrink(const polyq_dense* x, int64_t T, int64_t K, const polyq_adapters* ad, bool trans, const lora::Side& w,
+           const float* scales, const lora::Segments& seg, float* v, int sms, void* stream, const char* who) {
+  const int rn = rank_tile(ad->R);
+  const int64_t mean = T / seg.n;
+  const int bm = mean <= 32 ? 16 : rn >= 64 && mean >= 256 ? 128 : 64;
+  const bool half = ad->type == POLYQ_F16;
+  const Kernel k = half ? lora::shrink_of<__half>(bm, rn, trans) : lora::shrink_of<__nv_bfloat16>(bm, rn, trans);
+  const int64_t tiles = most_tiles(T, seg.n, bm), stages = K / (bm == 16 ? 128 : 64);
+  int cluster = 1;
+  while (cluster < lora::kMaxCluster && tiles * cluster < 2 * sms && stages >= 4 * cluster) cluster *= 2;
+  lora::ShrinkParams P;
+  memset(&P, 0, sizeof P);
+  P.x = x->data;
+  P.x_stride = x->stride;
+  P.w = w;
+  P.v = v;
+  P.scales = scales;
+  P.ranks = ad->ranks;
+  P.seg = seg;
+  P.K = K;
+  P.R = ad->R;
+  P.adapters = ad->n;
+  P.cluster = cluster;
+  const int which = (((half * 2 + trans) * 4 + rank_index(rn)) * 4) + (bm == 16 ? 0 : bm == 64 ? 1 : 2);
+  return launch(k, which, dim3((unsigned)(tiles * cluster)), cluster, &P, stream, who);
+}
+
+// y = residual + v times one of the adapters' matrices.
+int expand(const float* v, int64_t T, int64_t N, const polyq_adapters* ad, bool trans, const lora::Side& w,
+           const float* scales, const lora::Segments& seg, const polyq_dense* residual, const polyq_dense* y,
+           void* stream, const char* who) {
+  const int rn = rank_tile(ad->R), bm = T / seg.n <= 32 ? 16 : 64, bn = bm == 16 ? 256 : 128;
+  const bool half = ad->type == POLYQ_F16, f32 = y->type == POLYQ_F32;
+  const Kernel k = half ? lora::expand_of<__half>(bm, rn, trans, f32) : lora::expand_of<__nv_bfloat16>(bm, rn, trans, f32);
+  const int eb = f32 ? 4 : 2;
+  lora::ExpandParams P;
+  memset(&P, 0, sizeof P);
+  P.v = v;
+  P.w = w;
+  if (residual) P.res = residual->data, P.res_stride = residual->stride;
+  P.y = y->data;
+  P.y_stride = y->stride;
+  P.scales = scales;
+  P.ranks = ad->ranks;
+  P.seg = seg;
+  P.N = N;
+  P.R = ad->R;
+  P.adapters = ad->n;
+  P.tiles = (int32_t)most_tiles(T, seg.n, bm);
+  P.vec = (uintptr_t)y->data % 16 == 0 && y->stride * eb % 16 == 0 &&
+          (!residual || ((uintptr_t)residual->data % 16 == 0 && residual->stride * eb % 16 == 0));
+  const int which = 128 + (((half * 2 + trans) * 4 + rank_index(rn)) * 2 + (bm == 64)) * 2 + f32;
+  return launch(k, which, dim3((unsigned)((N + bn - 1) / bn), (unsigned)std::min(P.tiles, 65535)), 1, &P, stream, who);
+}
+
+bool rows_on_16(const polyq_dense* d) { return (uintptr_t)d->data % 16 == 0 && d->stride % 8 == 0; }
+
+int check(const polyq_dense* x, int64_t T, const polyq_adapters* ad, const polyq_segments* s, const char* who) {
+  if (!ad || !s) return polyq_set_error(POLYQ_EINVAL, "%s: adapters or segments are NULL", who);
+  if (T < 1 || T > kMaxSize || ad->K < 1 || ad->K > kMaxSize || ad->N < 1 || ad->N > kMaxSize)
+    return polyq_set_error(POLYQ_EINVAL, "%s: T=%lld K=%lld N=%lld", who, (long long)T, (long long)ad->K, (long long)ad->N);
+  if (ad->type != POLYQ_BF16 && ad->type != POLYQ_F16)
+    return polyq_set_error(POLYQ_EINVAL, "%s: adapters of type %d", who, ad->type);
+  if (ad->R < 1 || ad->R % 8)
+    return polyq_set_error(POLYQ_EINVAL, "%s: R=%d is not a multiple of 8", who, ad->R);
+  if (ad->R > POLYQ_ADAPTERS_MAX_RANK)
+    return polyq_set_error(POLYQ_EUNSUPPORTED, "%s: R=%d, at most %d", who, ad->R, POLYQ_ADAPTERS_MAX_RANK);
+  if (ad->n < 1 || ad->n > kMaxSize) return polyq_set_error(POLYQ_EINVAL, "%s: %d adapters", who, ad->n);
+  if (!ad->a || !ad->b || (uintptr_t)ad->a % 16 || (uintptr_t)ad->b % 16 || ad->a_stride < ad->K ||
+      ad->b_stride < ad->R || ad->a_stride % 8 || ad->b_stride % 8 || ad->a_next < 0 || ad->b_next < 0 ||
+      ad->a_next % 8 || ad->b_next % 8 || ad->a_stride > (1ll << 32) || ad->b_stride > (1ll << 32) ||
+      ad->a_next > (1ll << 40) || ad->b_next > (1ll << 40))
+    return polyq_set_error(POLYQ_EINVAL, "%s: a and b must be 16-byte aligned, with strides in multiples of 8 elements "
+                           "that hold their rows", who);
+  if ((uintptr_t)ad->scales % 4 || (uintptr_t)ad->ranks % 4)
+    return polyq_set_error(POLYQ_EINVAL, "%s: scales and ranks must be aligned to their elements", who);
+  if (!s->offsets || !s->ids || (uintptr_t)s->offsets % 4 || (uintptr_t)s->ids % 4 || s->n < 1 || s->n > kMaxSize)
+    return polyq_set_error(POLYQ_EINVAL, "%s: %d segments; offsets and ids must be given and aligned", who, s->n);
+  int rc = polyq_check_dense(x, ad->K, who, "x");
+  if (rc) return rc;
+  if (x->type != ad->type || !rows_on_16(x))
+    return polyq_set_error(POLYQ_EINVAL, "%s: x must be of the adapters' type, 16-byte aligned, with a stride that is a "
+                           "multiple of 8", who);
+  return POLYQ_OK;
+}
+
+// An output of x's type or fp32 and what it is added to.
+int check_sum(const polyq_dense* y, const polyq_dense* residual, int64_t cols, const polyq_adapters* ad, const char* who,
+              const char* what) {
+  int rc = polyq_check_dense(y, cols, who, what);
+  if (rc) return rc;
+  if (y->type != POLYQ_F32 && y->type != ad->type)
+    return polyq_set_error(POLYQ_EINVAL, "%s: %s must be of the adapters' type or fp32", who, what);
+  if (!residual) return POLYQ_OK;
+  rc = polyq_check_dense(residual, cols, who, "residual");
+  if (rc) return rc;
+  if (residual->type != y->type)
+    return polyq_set_error(POLYQ_EINVAL, "%s: the residual must be of %s's type", who, what);
+  if (residual->data == y->data && residual->stride != y->stride)
+    return polyq_set_error(POLYQ_EINVAL, "%s: a residual in %s's place must have its stride", who, what);
+  return POLYQ_OK;
+}
+
+size_t v_bytes(int64_t T, int R) { return (size_t)T * R * sizeof(float); }
+
+}  // namespace
+
+extern "C" int polyq_adapters_workspace_bytes(int64_t T, int32_t R, size_t* bytes) {
+  polyq_clear_error();
+  if (!bytes || T < 1 || T > kMaxSize || R < 1 || R % 8 || R > POLYQ_ADAPTERS_MAX_RANK)
+    return polyq_set_error(POLYQ_EINVAL, "polyq_adapters_workspace_bytes: T=%lld R=%d", (long long)T, R);
+  *bytes = v_bytes(T, R);
+  return POLYQ_OK;
+}
+
+extern "C" int polyq_adapters_forward(const polyq_dense* x, int64_t T, const polyq_adapters* adapters,
+                                      const polyq_segments* segments, const polyq_dense* residual,
+                                      const polyq_dense* y, float* saved, void* workspace, size_t workspace_bytes,
+                                      void* stream) {
+  static const char* who = "polyq_adapters_forward";
+  polyq_clear_error();
+  int rc = check(x, T, adapters, segments, who);
+  if (!rc) rc = check_sum(y, residual, adapters->N, adapters, who, "y");
+  if (rc) return rc;
+  float* v = saved ? saved : (float*)workspace;
+  if ((uintptr_t)v % 16) return polyq_set_error(POLYQ_EINVAL, "%s: saved and workspace must be 16-byte aligned", who);
+  if (!saved && (!workspace || workspace_bytes < v_bytes(T, adapters->R)))
+    return polyq_set_error(POLYQ_ENOMEM, "%s: workspace of %zu bytes needed", who, v_bytes(T, adapters->R));
+  int sms = 0;
+  rc = polyq_sm_count(&sms);
+  if (rc) return rc;
+  const lora::Segments seg{segments->offsets, segments->ids, segments->n, (int32_t)T};
+  rc = shrink(x, T, adapters->K, adapters, false, lora::Side{adapters->a, adapters->a_next, adapters->a_stride}, nullptr,
+              seg, v, sms, stream, who);
+  if (rc) return rc;
+  return expand(v, T, adapters->N, adapters, false, lora::Side{adapters->b, adapters->b_next, adapters->b_stride},
+                adapters->scales, seg, residual, y, stream, who);
+}
+
+extern "C" int polyq_adapters_backward(const polyq_dense* x, int64_t T, const polyq_adapters* adapters,
+                                       const polyq_segments* segments, const float* saved, const polyq_dense* dy,
+                                       const polyq_dense* residual, const polyq_dense* dx, void* da, void* db,
+                                       int32_t grad_type, void* workspace, size_t workspace_bytes, void* stream) {
+  static const char* who = "polyq_adapters_backward";
+  polyq_clear_error();
+  int rc = check(x, T, adapters, segments, who);
+  if (!rc) rc = polyq_check_dense(dy, adapters->N, who, "dy");
+  if (rc) return rc;
+  if (dy->type != adapters->type || !rows_on_16(dy))
+    return polyq_set_error(POLYQ_EINVAL, "%s: dy must be of the adapters' type, 16-byte aligned, with a stride that is a "
+                           "multiple of 8", who);
+  if (dx) rc = check_sum(dx, residual, adapters->K, adapters, who, "dx");
+  if (rc) return rc;
+  if (!dx && residual) return polyq_set_error(POLYQ_EINVAL, "%s: a residual needs a dx", who);
+  if (!dx && !da && !db) return polyq_set_error(POLYQ_EINVAL, "%s: no gradient is wanted", who);
+  if ((da || db) && grad_type != POLYQ_F32 && grad_type != adapters->type)
+    return polyq_set_error(POLYQ_EINVAL, "%s: da and db must be of the adapters' type or fp32", who);
+  const int eb = grad_type == POLYQ_F32 ? 4 : 2;
+  if ((uintptr_t)da % eb || (uintptr_t)db % eb)
+    return polyq_set_error(POLYQ_EINVAL, "%s: da and db must be aligned to their elements", who);
+  if ((db && !saved) || (uintptr_t)saved % 16 || (uintptr_t)workspace % 16)
+    return polyq_set_error(POLYQ_EINVAL, "%s: saved and workspace must be 16-byte aligned, and saved given for db", who);
+  const bool needs_dv = dx || da;
+  if (needs_dv && (!workspace || workspace_bytes < v_bytes(T, adapters->R)))
+    return polyq_set_error(POLYQ_ENOMEM, "%s: workspace of %zu bytes needed", who, v_bytes(T, adapters->R));
+  int sms = 0;
+  rc = polyq_sm_count(&sms);
+  if (rc) return rc;
+  const int rn = rank_tile(adapters->R), bc = rn <= 64 ? 128 : 64;
+  const bool half = adapters->type == POLYQ_F16;
+  const lora::Segments seg{segments->offsets, segments->ids, segments->n, (int32_t)T};
+  lora::GradParams G;
+  memset(&G, 0, sizeof G);
+  G.side[0] = lora::GradSide{(const float*)workspace, x->data, x->stride, adapters->K, da, nullptr, grad_type, 0,
+                             da ? (int32_t)((adapters->K + bc - 1) / bc) : 0};
+  G.side[1] = lora::GradSide{saved, dy->data, dy->stride, adapters->N, db, adapters->scales, grad_type, 1,
+                             db ? (int32_t)((adapters->N + bc - 1) / bc) : 0};
+  const int64_t blocks = (int64_t)adapters->n * (G.side[0].tiles + G.side[1].tiles);
+  if (blocks > 0x7FFFFFFF / lora::kMaxCluster)
+    return polyq_set_error(POLYQ_EUNSUPPORTED, "%s: gradients of %d adapters at once", who, adapters->n);
+  float* dv = (float*)workspace;
+  if (needs_dv) {
+    rc = shrink(dy, T, adapters->N, adapters, true, lora::Side{adapters->b, adapters->b_next, adapters->b_stride},
+                adapters->scales, seg, dv, sms, stream, who);
+    if (rc) return rc;
+  }
+  if (blocks) {
+    G.ranks = adapters->ranks;
+    G.seg = seg;
+    G.R = adapters->R;
+    G.cluster = 1;
+    while (G.cluster < lora::kMaxCluster && blocks * G.cluster < 2 * sms && T >= 128 * G.cluster) G.cluster *= 2;
+    const Kernel k = half ? lora::gradients_of<__half>(rn) : lora::gradients_of<__nv_bfloat16>(rn);
+    rc = launch(k, 192 + half * 4 + rank_index(rn), dim3((unsigned)(blocks * G.cluster)), G.cluster, &G, stream, who);
+    if (rc) return rc;
+  }
+  if (!dx) return POLYQ_OK;
+  return expand(dv, T, adapters->K, adapters, true, lora::Side{adapters->a, adapters->a_next, adapters->a_stride},
+                nullptr, seg, residual, dx, stream, who);
+}

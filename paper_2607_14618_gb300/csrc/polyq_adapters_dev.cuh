@@ -1,0 +1,752 @@
+// Low-rank adapters of many requests beside a shared projection, on operands of
+// one 16-bit type T.  For the rows of a segment with adapter i:
+//
+//   v = x A_i^T,  y = res + s_i v B_i^T              (forward)
+//   dv = s_i dy B_i,  dx = res + dv A_i              (backward)
+//   dA_i = dv^T x,  dB_i = s_i dy^T v                (sums over the adapter's rows)
+//
+// A rank is a few dozen, so that all of it is bound by HBM: x and dy in, y and dx
+// in and out, the adapters in.  Three kernels: `shrink` (a long row times a thin
+// matrix: v and dv), `expand` (a thin row times a wide matrix onto the residual: y
+// and dx) and `gradients` (a product over the rows: dA and dB).  Operands come
+// through shared memory by asynchronous copies, the products are mma.sync of
+// 16-bit operands with fp32 sums: at these ranks the legacy tensor path keeps up
+// with HBM, and needs no tensor memory, so that several small thread blocks share
+// an SM and cover each other's latency.
+//
+// v and dv are in fp32 between the kernels.  As an operand each is the sum of two
+// 16-bit numbers, v = h + l + O(2^-17 v) (bf16) or O(2^-22) (fp16), and both are
+// multiplied: rounded once to 16 bits it would be off by 2^-9 of what an adapter
+// adds.  fp16 has too few exponents for fp32's range: there v is scaled by a power
+// of two, of a row's largest magnitude (expand) or of 64 rows' (gradients).
+#pragma once
+#include <type_traits>
+
+#include "polyq_dense_dev.cuh"
+#include "polyq_dev.cuh"
+#include "polyq_finetune.h"
+
+namespace polyq {
+namespace lora {
+
+constexpr int kThreads = 256;
+constexpr int kMaxCluster = 8;
+
+struct Segments {
+  const int32_t* offsets;
+  const int32_t* ids;
+  int32_t n, rows;  // of segments, of the tensors' rows
+};
+
+// ---- instructions ----
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, uint32_t bytes) {  // the rest of 16: zeros
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void cp_wait() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
+template <bool TRANS>
+__device__ __forceinline__ void ldmatrix4(uint32_t addr, uint32_t (&r)[4]) {
+  if (TRANS)
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+                 : "r"(addr)
+                 : "memory");
+  else
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+                 : "r"(addr)
+                 : "memory");
+}
+template <typename T>
+__device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  if constexpr (sizeof(T) == 2 && std::is_same<T, __half>::value)
+    asm volatile(
+        "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+  else
+    asm volatile(
+        "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void cluster_sync() {
+  __syncwarp();
+  asm volatile("barrier.cluster.arrive.release.aligned;\n barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ uint32_t cluster_rank() {
+  uint32_t r;
+  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ float ld_cluster(uint32_t addr, uint32_t rank) {
+  uint32_t there;
+  float v;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(addr), "r"(rank));
+  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(there) : "memory");
+  return v;
+}
+
+// ---- tiles in shared memory ----
+// Rows of C 16-byte pieces, of which eight in a row of ldmatrix lie in different
+// banks: the pieces of rows that start in the same bank are permuted.
+template <int C>
+__device__ __forceinline__ uint32_t piece(int row, int c) {
+  const int s = C >= 8 ? row & 7 : (row / (8 / C)) & (C - 1);
+  return (uint32_t)(row * C + (c ^ s)) * 16u;
+}
+// A operand (16 rows m, 16 of the contraction k) from rows [m][k], or TRANS [k][m].
+template <int C, bool TRANS>
+__device__ __forceinline__ void frag_a(uint32_t tile, int m, int k, uint32_t (&r)[4]) {
+  const int lane = threadIdx.x & 31, i = lane >> 3, j = lane & 7;
+  if (TRANS) ldmatrix4<true>(tile + piece<C>(k + (i >> 1) * 8 + j, m / 8 + (i & 1)), r);
+  else ldmatrix4<false>(tile + piece<C>(m + (i & 1) * 8 + j, k / 8 + (i >> 1)), r);
+}
+// B operand of two tiles (8 columns n each; r[0..1], r[2..3]) from rows [n][k], or TRANS [k][n].
+template <int C, bool TRANS>
+__device__ __forceinline__ void frag_b(uint32_t tile, int n, int k, uint32_t (&r)[4]) {
+  const int lane = threadIdx.x & 31, i = lane >> 3, j = lane & 7;
+  if (TRANS) ldmatrix4<true>(tile + piece<C>(k + (i & 1) * 8 + j, n / 8 + (i >> 1)), r);
+  else ldmatrix4<false>(tile + piece<C>(n + (i >> 1) * 8 + j, k / 8 + (i & 1)), r);
+}
+// Copies ROWS x C pieces of a matrix (rows of `stride` elements) whose rows from
+// `rows` on and elements from `cols` on are zeros.
+template <int ROWS, int C>
+__device__ __forceinline__ void copy_tile(uint32_t tile, const void* src, int64_t stride, int64_t rows, int64_t cols) {
+#pragma unroll
+  for (int i0 = 0; i0 < ROWS * C; i0 += kThreads) {
+    const int i = i0 + threadIdx.x;
+    if (ROWS * C % kThreads && i >= ROWS * C) break;
+    const int row = i / C, c = i % C;
+    const int64_t left = row < rows ? cols - 8 * c : 0;
+    const uint32_t bytes = left >= 8 ? 16u : left > 0 ? (uint32_t)left * 2u : 0u;
+    cp_async16(tile + piece<C>(row, c), (const uint16_t*)src + (bytes ? row * stride + 8 * c : 0), bytes);
+  }
+}
+
+// ---- which rows ----
+// A tile of at most bm rows of one segment.
+struct Tile {
+  int32_t id, row, rows;
+};
+// Tile number `tile` of all segments' in turn (the whole warp calls; false: there
+// are fewer).  Offsets outside the tensors' rows are held at their ends.
+__device__ __forceinline__ bool find_tile(const Segments& s, int bm, int tile, Tile& t) {
+  const int lane = threadIdx.x & 31;
+  int before = 0;
+  for (int s0 = 0; s0 < s.n; s0 += 32) {
+    const int i = s0 + lane;
+    int from = 0, to = 0;
+    if (i < s.n) {
+      from = min(max(__ldcg(s.offsets + i), 0), s.rows);
+      to = min(max(__ldcg(s.offsets + i + 1), 0), s.rows);
+    }
+    const int n = to > from ? (to - from - 1) / bm + 1 : 0;
+    int sum = n;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int v = __shfl_up_sync(0xFFFFFFFFu, sum, o);
+      if (lane >= o) sum += v;
+    }
+    const int total = __shfl_sync(0xFFFFFFFFu, sum, 31);
+    if (tile < before + total) {
+      const int first = before + sum - n;
+      const int src = __ffs(__ballot_sync(0xFFFFFFFFu, n > 0 && first <= tile && tile < first + n)) - 1;
+      const int row = from + (tile - first) * bm;
+      t.row = __shfl_sync(0xFFFFFFFFu, row, src);
+      t.rows = min(bm, __shfl_sync(0xFFFFFFFFu, to, src) - t.row);
+      t.id = __ldcg(s.ids + s0 + src);
+      return true;
+    }
+    before += total;
+  }
+  return false;
+}
+// The tiles of all segments of one adapter, every `stride`-th from `first` on.
+struct AdapterTiles {
+  int s0, from, to, row, end, skip;
+  uint32_t mine;  // segments of the 32 from s0 on
+  __device__ __forceinline__ void begin(int first) {
+    s0 = -32;
+    mine = 0;
+    row = end = 0;
+    skip = first;
+  }
+  __device__ __forceinline__ bool next(const Segments& s, int id, int bm, int stride, int& at, int& rows) {
+    const int lane = threadIdx.x & 31;
+    for (;;) {
+      while (row >= end) {
+        while (!mine) {
+          s0 += 32;
+          if (s0 >= s.n) return false;
+          const int i = s0 + lane;
+          bool is = false;
+          from = to = 0;
+          if (i < s.n && __ldcg(s.ids + i) == id) {
+            from = min(max(__ldcg(s.offsets + i), 0), s.rows);
+            to = min(max(__ldcg(s.offsets + i + 1), 0), s.rows);
+            is = to > from;
+          }
+          mine = __ballot_sync(0xFFFFFFFFu, is);
+        }
+        const int src = __ffs(mine) - 1;
+        mine &= mine - 1;
+        row = __shfl_sync(0xFFFFFFFFu, from, src);
+        end = __shfl_sync(0xFFFFFFFFu, to, src);
+      }
+      at = row;
+      rows = min(bm, end - row);
+      row += bm;
+      if (skip-- == 0) {
+        skip = stride - 1;
+        return true;
+      }
+    }
+  }
+};
+
+// ---- v as two 16-bit numbers ----
+template <typename T>
+__device__ __forceinline__ void split8(const float (&v)[8], float scale, uint4& h, uint4& l) {
+  alignas(16) T eh[8], el[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const float x = v[i] * scale;
+    eh[i] = Elem<T>::from(x);
+    const float f = Elem<T>::to(eh[i]);
+    el[i] = Elem<T>::from(fabsf(f) < INFINITY ? x - f : 0.f);  // (what is not finite is so once)
+  }
+  h = *reinterpret_cast<const uint4*>(eh);
+  l = *reinterpret_cast<const uint4*>(el);
+}
+// 2^e and 2^-e that bring the largest magnitude (its bits) to 2^14 .. 2^15, both normal numbers.
+__device__ __forceinline__ uint32_t scale_bits(uint32_t top) {
+  return (uint32_t)min(max(127 + 14 + 127 - (int)(top >> 23), 1), 253);
+}
+__device__ __forceinline__ float scale_down(uint32_t top) { return __uint_as_float(scale_bits(top) << 23); }
+__device__ __forceinline__ float scale_up(uint32_t top) { return __uint_as_float((254u - scale_bits(top)) << 23); }
+__device__ __forceinline__ uint32_t abs_bits(const float (&v)[8]) {
+  uint32_t m = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(v[i]) & 0x7FFFFFFFu);
+  return m;
+}
+__device__ __forceinline__ void load_v8(const float* p, bool there, float (&v)[8]) {
+  float4 a = make_float4(0.f, 0.f, 0.f, 0.f), b = a;
+  if (there) {
+    a = __ldcg(reinterpret_cast<const float4*>(p));
+    b = __ldcg(reinterpret_cast<const float4*>(p) + 1);
+  }
+  v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w;
+  v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
+}
+
+struct Side {  // an adapter's matrix: `next` elements from one to the next, rows of `stride`
+  const void* w;
+  int64_t next, stride;
+};
+
+// ---------------------------------------------------------------------------
+// v[t][j] = s sum_k x[t][k] W[j][k]   (TRANS: W[k][j])
+// ---------------------------------------------------------------------------
+struct ShrinkParams {
+  const void* x;
+  Side w;
+  float* v;  // [rows][R]
+  const float* scales;  // NULL: s = 1
+  const int32_t* ranks;
+  Segments seg;
+  int64_t x_stride, K;
+  int32_t R, adapters, cluster;
+};
+
+// A cluster's blocks share the contraction of one tile of BM rows and add their
+// sums through distributed shared memory, each a part of the tile, in the blocks'
+// order.
+template <typename T, int BM, int RN, bool TRANS>
+struct Shrink {
+  static constexpr int KC = BM == 16 ? 128 : 64;  // contraction of a stage
+  static constexpr int STAGES = 4;
+  // warps along the rows, the rank and the contraction of a stage
+  static constexpr int WM = BM == 16 ? 1 : 4, WN = BM == 16 ? RN / 16 : RN == 16 ? 1 : 2, WK = 8 / (WM * WN);
+  static constexpr int MT = BM / 16 / WM, NT = RN / 8 / WN;
+  static constexpr int X_BYTES = BM * KC * 2, W_BYTES = RN * KC * 2;
+  static constexpr int RED_BYTES = WK * BM * RN * 4;
+  static constexpr int SMEM = STAGES * (X_BYTES + W_BYTES) > RED_BYTES ? STAGES * (X_BYTES + W_BYTES) : RED_BYTES;
+};
+
+template <typename T, int BM, int RN, bool TRANS>
+__global__ void __launch_bounds__(kThreads) shrink_kernel(const __grid_constant__ ShrinkParams P) {
+  using S = Shrink<T, BM, RN, TRANS>;
+  constexpr int KC = S::KC, CX = KC / 8, CW = TRANS ? RN / 8 : KC / 8;
+  extern __shared__ __align__(128) uint8_t smem[];
+  const uint32_t base = smem_u32(smem);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int rank = P.cluster > 1 ? (int)cluster_rank() : 0;
+  pdl_wait();
+  pdl_trigger();  // (not before the wait: what follows reads what this grid has waited for)
+  Tile t;
+  if (!find_tile(P.seg, BM, blockIdx.x / P.cluster, t)) return;  // the whole cluster
+  if (t.id < 0 || t.id >= P.adapters) return;
+  const int own = P.ranks ? min(max(__ldcg(P.ranks + t.id), 0), P.R) : P.R;
+  const T* x = (const T*)P.x + (int64_t)t.row * P.x_stride;
+  const T* w = (const T*)P.w.w + (int64_t)t.id * P.w.next;
+  const int64_t chunks = (P.K + KC - 1) / KC;
+  const int64_t c0 = chunks * rank / P.cluster, c1 = chunks * (rank + 1) / P.cluster;
+
+  auto copy = [&](int64_t c) {
+    const uint32_t at = base + (uint32_t)((c - c0) % S::STAGES) * (S::X_BYTES + S::W_BYTES);
+    const int64_t k = c * KC;
+    copy_tile<BM, CX>(at, x + k, P.x_stride, t.rows, P.K - k);
+    if (TRANS) copy_tile<KC, CW>(at + S::X_BYTES, w + k * P.w.stride, P.w.stride, P.K - k, own);
+    else copy_tile<RN, CW>(at + S::X_BYTES, w + k, P.w.stride, own, P.K - k);
+  };
+  float acc[S::MT][S::NT][4] = {};
+  const int wm = warp % S::WM, wn = warp / S::WM % S::WN, wk = warp / (S::WM * S::WN);
+  for (int i = 0; i < S::STAGES - 1; ++i) {
+    if (c0 + i < c1) copy(c0 + i);
+    cp_commit();
+  }
+  for (int64_t c = c0; c < c1; ++c) {
+    cp_wait<S::STAGES - 2>();
+    __syncthreads();
+    if (c + S::STAGES - 1 < c1) copy(c + S::STAGES - 1);
+    cp_commit();
+    const uint32_t at = base + (uint32_t)((c - c0) % S::STAGES) * (S::X_BYTES + S::W_BYTES);
+#pragma unroll
+    for (int k = wk * 16; k < KC; k += 16 * S::WK) {
+      uint32_t a[S::MT][4];
+#pragma unroll
+      for (int i = 0; i < S::MT; ++i) frag_a<CX, false>(at, (wm * S::MT + i) * 16, k, a[i]);
+#pragma unroll
+      for (int j = 0; j < S::NT; j += 2) {
+        uint32_t b[4];
+        frag_b<CW, TRANS>(at + S::X_BYTES, (wn * S::NT + j) * 8, k, b);
+#pragma unroll
+        for (int i = 0; i < S::MT; ++i) {
+          mma<T>(acc[i][j], a[i], b[0], b[1]);
+          mma<T>(acc[i][j + 1], a[i], b[2], b[3]);
+        }
+      }
+    }
+  }
+  cp_wait<0>();
+  __syncthreads();
+  float* red = reinterpret_cast<float*>(smem) + wk * BM * RN;
+#pragma unroll
+  for (int i = 0; i < S::MT; ++i)
+#pragma unroll
+    for (int j = 0; j < S::NT; ++j) {
+      const int row = (wm * S::MT + i) * 16 + lane / 4, col = (wn * S::NT + j) * 8 + lane % 4 * 2;
+      *reinterpret_cast<float2*>(red + row * RN + col) = make_float2(acc[i][j][0], acc[i][j][1]);
+      *reinterpret_cast<float2*>(red + (row + 8) * RN + col) = make_float2(acc[i][j][2], acc[i][j][3]);
+    }
+  if (P.cluster > 1) cluster_sync();
+  else __syncthreads();
+  const float s = P.scales ? __ldcg(P.scales + t.id) : 1.f;
+  const int part = BM * RN / P.cluster;
+  for (int i = rank * part + threadIdx.x; i < (rank + 1) * part; i += kThreads) {
+    const int row = i / RN, col = i % RN;
+    if (row >= t.rows) break;
+    if (col >= P.R) continue;
+    float v = 0.f;
+    for (int r = 0; r < P.cluster; ++r)
+#pragma unroll
+      for (int q = 0; q < S::WK; ++q) {
+        const int at = q * BM * RN + i;
+        v += P.cluster > 1 ? ld_cluster(base + at * 4, r) : reinterpret_cast<const float*>(smem)[at];
+      }
+    P.v[(int64_t)(t.row + row) * P.R + col] = col < own ? v * s : 0.f;
+  }
+  if (P.cluster > 1) cluster_sync();  // (another block may still read this one's sums)
+}
+
+// ---------------------------------------------------------------------------
+// y[t][n] = res[t][n] + s sum_j v[t][j] W[n][j]   (TRANS: W[j][n])
+// ---------------------------------------------------------------------------
+struct ExpandParams {
+  const float* v;
+  Side w;
+  const void* res;
+  void* y;
+  const float* scales;
+  const int32_t* ranks;
+  Segments seg;
+  int64_t res_stride, y_stride, N;
+  int32_t R, adapters, tiles, vec;
+};
+
+template <typename T, int BM, int RN, bool TRANS, typename TY>
+struct Expand {
+  static constexpr int BN = BM == 16 ? 256 : 128;
+  static constexpr int WM = BM == 16 ? 1 : 2, WN = 8 / WM;
+  static constexpr int MT = BM / 16 / WM, NT = BN / 8 / WN;
+  static constexpr int PITCH = BN + 8;  // floats of a row of sums: rows of a quad in different banks
+  static constexpr int V_BYTES = BM * RN * 2, W_BYTES = BN * RN * 2;
+  static constexpr int OUT_BYTES = BM * PITCH * 4;
+  static constexpr int SMEM = 2 * V_BYTES + W_BYTES > OUT_BYTES ? 2 * V_BYTES + W_BYTES : OUT_BYTES;
+};
+
+template <typename T, int BM, int RN, bool TRANS, typename TY, bool VEC>
+__device__ __forceinline__ void expand_tile(const ExpandParams& P, const Tile& t, uint8_t* smem, float* row_scale,
+                                            bool first) {
+  using E = Expand<T, BM, RN, TRANS, TY>;
+  constexpr int CV = RN / 8, CW = TRANS ? E::BN / 8 : RN / 8;
+  constexpr int GROUPS = BM * E::BN / 8 / kThreads;  // of eight outputs a thread
+  const uint32_t base = smem_u32(smem), wt = base + 2 * E::V_BYTES;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int64_t n0 = (int64_t)blockIdx.x * E::BN;
+  const bool bare = t.id < 0 || t.id >= P.adapters;
+  if (bare && P.res == P.y) {  // nothing to add
+    if (first) pdl_wait();
+    return;
+  }
+  const int own = bare ? 0 : P.ranks ? min(max(__ldcg(P.ranks + t.id), 0), P.R) : P.R;
+  if (!bare) {
+    const T* w = (const T*)P.w.w + (int64_t)t.id * P.w.next;
+    if (TRANS) copy_tile<RN, CW>(wt, w + n0, P.w.stride, own, P.N - n0);
+    else copy_tile<E::BN, CW>(wt, w + n0 * P.w.stride, P.w.stride, P.N - n0, own);
+  }
+  cp_commit();
+  Raw8<TY> res[GROUPS];
+  constexpr int PER_ROW = E::BN / 8;
+#pragma unroll
+  for (int i = 0; i < GROUPS; ++i) {
+    const int g = i * kThreads + threadIdx.x, row = g / PER_ROW;
+    const int64_t col = n0 + (VEC ? g % PER_ROW * 8 : g % PER_ROW);
+    const uint32_t m = P.res && row < t.rows ? mask8<VEC>(col, PER_ROW, P.N) : 0u;
+    load8<VEC>((const TY*)P.res + (int64_t)(t.row + row) * P.res_stride, col, PER_ROW, m, res[i]);
+  }
+  if (first) pdl_wait();  // v comes from the launch before
+  float acc[E::MT][E::NT][4] = {};
+  const int wm = warp % E::WM, wn = warp / E::WM;
+  if (!bare) {
+#pragma unroll
+    for (int i0 = 0; i0 < BM * CV; i0 += kThreads) {
+      const int i = i0 + threadIdx.x;
+      if (BM * CV % kThreads && i >= BM * CV) break;  // (whole warps)
+      const int row = i / CV, c = i % CV;
+      float v[8];
+      load_v8(P.v + (int64_t)(t.row + row) * P.R + 8 * c, row < t.rows && 8 * c < P.R, v);
+      float scale = 1.f;
+      if constexpr (std::is_same<T, __half>::value) {
+        uint32_t top = abs_bits(v);
+#pragma unroll
+        for (int o = CV / 2; o; o >>= 1) top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
+        scale = scale_down(top);
+        if (c == 0) row_scale[row] = scale_up(top);
+      }
+      uint4 h, l;
+      split8<T>(v, scale, h, l);
+      *reinterpret_cast<uint4*>(smem + piece<CV>(row, c)) = h;
+      *reinterpret_cast<uint4*>(smem + E::V_BYTES + piece<CV>(row, c)) = l;
+    }
+    cp_wait<0>();
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < RN; k += 16) {
+      uint32_t h[E::MT][4], l[E::MT][4];
+#pragma unroll
+      for (int i = 0; i < E::MT; ++i) {
+        frag_a<CV, false>(base, (wm * E::MT + i) * 16, k, h[i]);
+        frag_a<CV, false>(base + E::V_BYTES, (wm * E::MT + i) * 16, k, l[i]);
+      }
+#pragma unroll
+      for (int j = 0; j < E::NT; j += 2) {
+        uint32_t b[4];
+        frag_b<CW, TRANS>(wt, (wn * E::NT + j) * 8, k, b);
+#pragma unroll
+        for (int i = 0; i < E::MT; ++i)
+#pragma unroll
+          for (int q = 0; q < 2; ++q) {
+            mma<T>(acc[i][j + q], l[i], b[2 * q], b[2 * q + 1]);
+            mma<T>(acc[i][j + q], h[i], b[2 * q], b[2 * q + 1]);
+          }
+      }
+    }
+    __syncthreads();
+  }
+  // Sums through shared memory to threads that hold eight neighbours (or, of rows
+  // that start anywhere, every sixteenth) of a row.
+  float* out = reinterpret_cast<float*>(smem);
+  const float s = bare ? 0.f : P.scales ? __ldcg(P.scales + t.id) : 1.f;
+  if (!bare) {
+#pragma unroll
+    for (int i = 0; i < E::MT; ++i) {
+      const int row = (wm * E::MT + i) * 16 + lane / 4;
+      float s0 = s, s1 = s;
+      if constexpr (std::is_same<T, __half>::value) s0 *= row_scale[row], s1 *= row_scale[row + 8];
+#pragma unroll
+      for (int j = 0; j < E::NT; ++j) {
+        const int col = (wn * E::NT + j) * 8 + lane % 4 * 2;
+        *reinterpret_cast<float2*>(out + row * E::PITCH + col) = make_float2(acc[i][j][0] * s0, acc[i][j][1] * s0);
+        *reinterpret_cast<float2*>(out + (row + 8) * E::PITCH + col) = make_float2(acc[i][j][2] * s1, acc[i][j][3] * s1);
+      }
+    }
+    __syncthreads();
+  }
+#pragma unroll
+  for (int i = 0; i < GROUPS; ++i) {
+    const int g = i * kThreads + threadIdx.x, row = g / PER_ROW, c = VEC ? g % PER_ROW * 8 : g % PER_ROW;
+    if (row >= t.rows) break;
+    float v[8];
+    to_float(res[i], v);
+    if (!bare) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] += out[row * E::PITCH + c + (VEC ? e : e * PER_ROW)];
+    }
+    store8<VEC>((TY*)P.y + (int64_t)(t.row + row) * P.y_stride, n0 + c, PER_ROW,
+                mask8<VEC>(n0 + c, PER_ROW, P.N), v);
+  }
+}
+
+template <typename T, int BM, int RN, bool TRANS, typename TY>
+__global__ void __launch_bounds__(kThreads) expand_kernel(const __grid_constant__ ExpandParams P) {
+  extern __shared__ __align__(128) uint8_t smem[];
+  __shared__ float row_scale[BM];
+  bool first = true;
+  for (int tile = blockIdx.y; tile < P.tiles; tile += gridDim.y) {
+    Tile t;
+    if (!find_tile(P.seg, BM, tile, t)) break;
+    if (!first) __syncthreads();  // (the tile before has been read)
+    if (P.vec) expand_tile<T, BM, RN, TRANS, TY, true>(P, t, smem, row_scale, first);
+    else expand_tile<T, BM, RN, TRANS, TY, false>(P, t, smem, row_scale, first);
+    first = false;
+  }
+  if (first) pdl_wait();
+  pdl_trigger();
+}
+
+// ---------------------------------------------------------------------------
+// out[j][c] = s sum_t v[t][j] x[t][c] over the rows t of an adapter (dA), or
+// out[c][j] (dB)
+// ---------------------------------------------------------------------------
+struct GradSide {
+  const float* v;       // [rows][R]
+  const void* x;
+  int64_t x_stride, C;  // columns
+  void* out;            // of adapter i from element i * R * C on
+  const float* scales;
+  int32_t type, by_column;  // by_column: out[c][j]
+  int32_t tiles;            // of columns, 0: not wanted
+};
+struct GradParams {
+  GradSide side[2];
+  const int32_t* ranks;
+  Segments seg;
+  int32_t R, cluster;
+};
+
+template <typename T, int RN>
+struct Grad {
+  static constexpr int BT = 64;                    // rows of a stage
+  static constexpr int BC = RN <= 64 ? 128 : 64;   // columns of a block
+  static constexpr int WR = RN <= 32 ? 1 : RN / 32, WC = 8 / WR;
+  static constexpr int MT = RN / 16 / WR, NT = BC / 8 / WC;
+  static constexpr int STAGES = 3;
+  static constexpr int X_BYTES = BT * BC * 2, V_BYTES = BT * RN * 2;
+  static constexpr int PITCH = BC + 1;
+  static constexpr int RED_BYTES = RN * PITCH * 4;
+  static constexpr int MAIN = STAGES * X_BYTES + 2 * V_BYTES;
+  static constexpr int SMEM = MAIN > RED_BYTES ? MAIN : RED_BYTES;
+};
+
+template <typename T, int RN>
+__global__ void __launch_bounds__(kThreads) gradients_kernel(const __grid_constant__ GradParams P) {
+  using G = Grad<T, RN>;
+  constexpr int CX = G::BC / 8, CV = RN / 8, BT = G::BT;
+  constexpr int VG = (BT * CV + kThreads - 1) / kThreads;  // groups of eight v of a thread
+  constexpr bool SCALED = std::is_same<T, __half>::value;
+  extern __shared__ __align__(128) uint8_t smem[];
+  __shared__ uint32_t tops[8];
+  const uint32_t base = smem_u32(smem), vt = base + G::STAGES * G::X_BYTES;
+  uint8_t* vs = smem + G::STAGES * G::X_BYTES;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int rank = P.cluster > 1 ? (int)cluster_rank() : 0;
+  const int per = P.side[0].tiles + P.side[1].tiles, block = blockIdx.x / P.cluster;
+  const int id = block / per, which = block % per >= P.side[0].tiles;
+  const GradSide& D = P.side[which];
+  const int64_t n0 = (int64_t)(block % per - (which ? P.side[0].tiles : 0)) * G::BC;
+  pdl_wait();
+  pdl_trigger();
+  const int own = P.ranks ? min(max(__ldcg(P.ranks + id), 0), P.R) : P.R;
+  AdapterTiles ahead, now;
+  ahead.begin(rank);
+  now.begin(rank);
+  auto copy = [&](int stage) {
+    int row, rows;
+    if (ahead.next(P.seg, id, BT, P.cluster, row, rows))
+      copy_tile<BT, CX>(base + stage * G::X_BYTES, (const T*)D.x + (int64_t)row * D.x_stride + n0, D.x_stride, rows,
+                        D.C - n0);
+    cp_commit();
+  };
+  float v[VG][8];
+  auto load_v = [&]() {
+    int row, rows;
+    if (!now.next(P.seg, id, BT, P.cluster, row, rows)) return false;
+#pragma unroll
+    for (int i = 0; i < VG; ++i) {
+      const int g = i * kThreads + threadIdx.x, r = g / CV, c = g % CV;
+      load_v8(D.v + (int64_t)(row + r) * P.R + 8 * c, r < rows && 8 * c < P.R, v[i]);
+    }
+    return true;
+  };
+  float acc[G::MT][G::NT][4] = {};
+  const int wr = warp % G::WR, wc = warp / G::WR;
+#pragma unroll
+  for (int i = 0; i < G::STAGES - 1; ++i) copy(i);
+  bool more = load_v();
+  for (int stage = 0; more; stage = (stage + 1) % G::STAGES) {
+    float down = 1.f, up = 1.f;
+    if constexpr (SCALED) {
+      uint32_t top = 0;
+#pragma unroll
+      for (int i = 0; i < VG; ++i) top = max(top, abs_bits(v[i]));
+      top = __reduce_max_sync(0xFFFFFFFFu, top);
+      if (lane == 0) tops[warp] = top;
+      __syncthreads();
+      top = __reduce_max_sync(0xFFFFFFFFu, tops[lane & 7]);
+      down = scale_down(top);
+      up = scale_up(top);
+    }
+#pragma unroll
+    for (int i = 0; i < VG; ++i) {
+      const int g = i * kThreads + threadIdx.x;
+      if (BT * CV % kThreads && g >= BT * CV) break;
+      uint4 h, l;
+      split8<T>(v[i], down, h, l);
+      *reinterpret_cast<uint4*>(vs + piece<CV>(g / CV, g % CV)) = h;
+      *reinterpret_cast<uint4*>(vs + G::V_BYTES + piece<CV>(g / CV, g % CV)) = l;
+    }
+    more = load_v();
+    cp_wait<G::STAGES - 2>();
+    __syncthreads();
+    copy((stage + G::STAGES - 1) % G::STAGES);
+    const uint32_t at = base + stage * G::X_BYTES;
+    float part[SCALED ? G::MT : 1][SCALED ? G::NT : 1][4] = {};
+#pragma unroll
+    for (int k = 0; k < BT; k += 16) {
+      uint32_t h[G::MT][4], l[G::MT][4];
+#pragma unroll
+      for (int i = 0; i < G::MT; ++i) {
+        frag_a<CV, true>(vt, (wr * G::MT + i) * 16, k, h[i]);
+        frag_a<CV, true>(vt + G::V_BYTES, (wr * G::MT + i) * 16, k, l[i]);
+      }
+#pragma unroll
+      for (int j = 0; j < G::NT; j += 2) {
+        uint32_t b[4];
+        frag_b<CX, true>(at, (wc * G::NT + j) * 8, k, b);
+#pragma unroll
+        for (int i = 0; i < G::MT; ++i)
+#pragma unroll
+          for (int q = 0; q < 2; ++q) {
+            float(&d)[4] = SCALED ? part[SCALED ? i : 0][SCALED ? j + q : 0] : acc[i][j + q];
+            mma<T>(d, l[i], b[2 * q], b[2 * q + 1]);
+            mma<T>(d, h[i], b[2 * q], b[2 * q + 1]);
+          }
+      }
+    }
+    if constexpr (SCALED) {
+#pragma unroll
+      for (int i = 0; i < G::MT; ++i)
+#pragma unroll
+        for (int j = 0; j < G::NT; ++j)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) acc[i][j][e] = fmaf(part[i][j][e], up, acc[i][j][e]);
+    }
+    __syncthreads();  // v has been read
+  }
+  cp_wait<0>();
+  __syncthreads();
+  float* red = reinterpret_cast<float*>(smem);
+#pragma unroll
+  for (int i = 0; i < G::MT; ++i)
+#pragma unroll
+    for (int j = 0; j < G::NT; ++j) {
+      const int row = (wr * G::MT + i) * 16 + lane / 4, col = (wc * G::NT + j) * 8 + lane % 4 * 2;
+      red[row * G::PITCH + col] = acc[i][j][0];
+      red[row * G::PITCH + col + 1] = acc[i][j][1];
+      red[(row + 8) * G::PITCH + col] = acc[i][j][2];
+      red[(row + 8) * G::PITCH + col + 1] = acc[i][j][3];
+    }
+  if (P.cluster > 1) cluster_sync();
+  else __syncthreads();
+  const float s = D.scales ? __ldcg(D.scales + id) : 1.f;
+  const int part = RN * G::BC / P.cluster;
+  for (int i = rank * part + threadIdx.x; i < (rank + 1) * part; i += kThreads) {
+    const int j = D.by_column ? i % RN : i / G::BC, c = D.by_column ? i / RN : i % G::BC;
+    if (j >= P.R || n0 + c >= D.C) continue;
+    float sum = 0.f;
+    const int at = j * G::PITCH + c;
+    for (int r = 0; r < P.cluster; ++r) sum += P.cluster > 1 ? ld_cluster(base + at * 4, r) : red[at];
+    const int64_t o = (int64_t)id * P.R * D.C + (D.by_column ? (n0 + c) * P.R + j : j * D.C + n0 + c);
+    any_store(D.out, D.type, o, j < own ? sum * s : 0.f);
+  }
+  if (P.cluster > 1) cluster_sync();
+}
+
+// ---------------------------------------------------------------------------
+// host: kernels by their tile
+// ---------------------------------------------------------------------------
+struct Kernel {
+  void* f;
+  int smem;
+};
+// rn: the rank rounded up to 16, 32, 64 or 128; bm: 16, 64 or (shrink, rn >= 64) 128.
+template <typename T>
+Kernel shrink_of(int bm, int rn, bool trans);
+template <typename T>
+Kernel expand_of(int bm, int rn, bool trans, bool f32);
+template <typename T>
+Kernel gradients_of(int rn);
+
+template <typename T, int BM, int RN>
+Kernel shrink_at(bool trans) {
+  return trans ? Kernel{(void*)shrink_kernel<T, BM, RN, true>, Shrink<T, BM, RN, true>::SMEM}
+               : Kernel{(void*)shrink_kernel<T, BM, RN, false>, Shrink<T, BM, RN, false>::SMEM};
+}
+template <typename T, int RN>
+Kernel shrink_for(int bm, bool trans) {
+  if constexpr (RN >= 64) {
+    if (bm == 128) return shrink_at<T, 128, RN>(trans);
+  }
+  return bm == 16 ? shrink_at<T, 16, RN>(trans) : shrink_at<T, 64, RN>(trans);
+}
+template <typename T, int BM, int RN, bool TRANS>
+Kernel expand_at(bool f32) {
+  return f32 ? Kernel{(void*)expand_kernel<T, BM, RN, TRANS, float>, Expand<T, BM, RN, TRANS, float>::SMEM}
+             : Kernel{(void*)expand_kernel<T, BM, RN, TRANS, T>, Expand<T, BM, RN, TRANS, T>::SMEM};
+}
+template <typename T, int RN>
+Kernel expand_for(int bm, bool trans, bool f32) {
+  if (bm == 16) return trans ? expand_at<T, 16, RN, true>(f32) : expand_at<T, 16, RN, false>(f32);
+  return trans ? expand_at<T, 64, RN, true>(f32) : expand_at<T, 64, RN, false>(f32);
+}
+template <typename T>
+Kernel shrink_of(int bm, int rn, bool trans) {
+  return rn == 16   ? shrink_for<T, 16>(bm, trans)
+         : rn == 32 ? shrink_for<T, 32>(bm, trans)
+         : rn == 64 ? shrink_for<T, 64>(bm, trans)
+                    : shrink_for<T, 128>(bm, trans);
+}
+template <typename T>
+Kernel expand_of(int bm, int rn, bool trans, bool f32) {
+  return rn == 16   ? expand_for<T, 16>(bm, trans, f32)
+         : rn == 32 ? expand_for<T, 32>(bm, trans, f32)
+         : rn == 64 ? expand_for<T, 64>(bm, trans, f32)
+                    : expand_for<T, 128>(bm, trans, f32);
+}
+template <typename T, int RN>
+Kernel gradients_at() {
+  return Kernel{(void*)gradients_kernel<T, RN>, Grad<T, RN>::SMEM};
+}
+template <typename T>
+Kernel gradients_of(int rn) {
+  return rn == 16 ? gradients_at<T, 16>() : rn == 32 ? gradients_at<T, 32>() : rn == 64 ? gradients_at<T, 64>() : gradients_at<T, 128>();
+}
+
+}  // namespace lora
+}  // namespace polyq

@@ -129,6 +129,17 @@ class AdamwHyper(C.Structure):
                 ("lr_dev", C.c_void_p), ("step_dev", C.c_void_p), ("grad_scale", C.c_void_p)]
 
 
+class Adapters(C.Structure):
+    _fields_ = [("a", C.c_void_p), ("b", C.c_void_p), ("a_stride", C.c_int64),
+                ("a_next", C.c_int64), ("b_stride", C.c_int64), ("b_next", C.c_int64),
+                ("K", C.c_int64), ("N", C.c_int64), ("n", C.c_int32), ("R", C.c_int32),
+                ("type", C.c_int32), ("scales", C.c_void_p), ("ranks", C.c_void_p)]
+
+
+class Segments(C.Structure):
+    _fields_ = [("offsets", C.c_void_p), ("ids", C.c_void_p), ("n", C.c_int32)]
+
+
 _P = C.c_void_p
 _FP4, _DENSE = C.POINTER(Fp4Desc), C.POINTER(Dense)
 _SIGS = {
@@ -198,6 +209,12 @@ _SIGS = {
     "polyq_adamw_step": (C.c_int, [C.POINTER(AdamwTensor), C.c_int32, C.c_int32, C.c_int32,
                                    C.c_int32, C.POINTER(AdamwState), C.POINTER(AdamwHyper), _P]),
     "polyq_adamw_values": (C.c_int, [C.POINTER(AdamwState), _DENSE, _DENSE, _P]),
+    "polyq_adapters_workspace_bytes": (C.c_int, [C.c_int64, C.c_int32, C.POINTER(C.c_size_t)]),
+    "polyq_adapters_forward": (C.c_int, [_DENSE, C.c_int64, C.POINTER(Adapters), C.POINTER(Segments),
+                                         _DENSE, _DENSE, _P, _P, C.c_size_t, _P]),
+    "polyq_adapters_backward": (C.c_int, [_DENSE, C.c_int64, C.POINTER(Adapters),
+                                          C.POINTER(Segments), _P, _DENSE, _DENSE, _DENSE, _P, _P,
+                                          C.c_int32, _P, C.c_size_t, _P]),
 }
 for _name, (_res, _args) in _SIGS.items():
     _fn = getattr(_lib, _name)
@@ -1341,3 +1358,143 @@ class AdamW:
         d = self.state._desc(self._dev)
         for (tp, tg, tc), tensors, n in self._groups:
             _check(_lib.polyq_adamw_step(tensors, n, tp, tg, tc, C.byref(d), C.byref(h), st))
+
+
+def adapters_workspace(T, R, device="cuda"):
+    """A workspace for adapters_forward and adapters_backward of T rows."""
+    import torch
+    n = C.c_size_t()
+    _check(_lib.polyq_adapters_workspace_bytes(int(T), int(R), C.byref(n)))
+    return torch.empty(n.value, dtype=torch.uint8, device=device)
+
+
+def adapters_saved(T, R, device="cuda"):
+    """The buffer that adapters_forward fills for adapters_backward: v = x A^T."""
+    import torch
+    _check(_lib.polyq_adapters_workspace_bytes(int(T), int(R), C.byref(C.c_size_t())))
+    return torch.empty((T, R), dtype=torch.float32, device=device)
+
+
+def _plain(t, name, dtype, shape, dev):
+    """The address of a contiguous tensor of that type and shape on CUDA device `dev`."""
+    try:
+        good = (t.dtype == dtype and t.shape == shape and t.get_device() == dev and t.is_contiguous())
+    except AttributeError:
+        good = False
+    if not good:
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor {list(shape)} on cuda:{dev}")
+    return t.data_ptr()
+
+
+def _adapters(x, a, b, offsets, ids, scales, ranks, dev):
+    """Descriptors of the adapters a [n][R][K] and b [n][N][R] and of the segments."""
+    import torch
+    K = x.shape[1]
+    try:
+        n, R, ka = a.shape
+        nb, N, rb = b.shape
+        (an, ar, a1), (bn, br, b1) = a.stride(), b.stride()
+        good = (a.dtype == b.dtype == x.dtype and a.get_device() == b.get_device() == dev
+                and (nb, rb, ka) == (n, R, K) and (a1 == 1 or K == 1) and (b1 == 1 or R == 1)
+                and x.dtype in (torch.bfloat16, torch.float16))
+    except (AttributeError, ValueError):
+        good = False
+    if not good:
+        raise ValueError(f"a and b must be tensors [n][R][{K}] and [n][N][R] with contiguous rows of "
+                         f"x's type, bf16 or fp16, on cuda:{dev}")
+    if R == 1 and ar < K:
+        ar = K
+    if N == 1 and br < R:
+        br = R
+    if n == 1:  # (one adapter: the stride to the next does not matter)
+        an = bn = 0
+    d = Adapters(a.data_ptr(), b.data_ptr(), ar, an, br, bn, K, N, n, R, _type_of(x.dtype),
+                 None if scales is None else _plain(scales, "scales", torch.float32, (n,), dev),
+                 None if ranks is None else _plain(ranks, "ranks", torch.int32, (n,), dev))
+    try:
+        m = ids.shape[0]
+    except (AttributeError, IndexError):
+        m = -1
+    s = Segments(_plain(offsets, "offsets", torch.int32, (m + 1,), dev),
+                 _plain(ids, "ids", torch.int32, (m,), dev), m)
+    return d, s
+
+
+def adapters_forward(x, a, b, offsets, ids, scales=None, ranks=None, residual=None, y=None,
+                     saved=None, dtype=None, workspace=None, stream=None):
+    """y = residual + scale * (x A^T) B^T, each row of x [T][K] (bf16 or fp16) with its own
+    low-rank adapter: rows offsets[i] .. offsets[i+1] - 1 with adapter ids[i] (-1: none, y is
+    the residual) of a [n][R][K] and b [n][N][R].  R is a multiple of 8 up to 128; `ranks`
+    holds smaller ranks, `scales` a factor per adapter.  offsets, ids and ranks are int32,
+    scales fp32, all on the device and read when the call runs.  residual: the shared
+    projection's result, of y's type (x's or fp32), may be y itself.  Rows of no segment are
+    left as they were: without a `y` they are not set.  `saved` (adapters_saved) receives what
+    adapters_backward needs."""
+    ix = _dense(x, "x")
+    dev = x.get_device()
+    st = _stream_on(dev, "x", stream)
+    d, s = _adapters(x, a, b, offsets, ids, scales, ranks, dev)
+    T, R, N = x.shape[0], d.R, d.N
+    ir = None
+    if residual is not None:
+        ir = C.byref(_dense(residual, "residual", T, N, dev, dtype if y is None else None))
+    if y is None:
+        import torch
+        y = _made(stream, torch.empty, (T, N), device=x.device,
+                  dtype=dtype or (residual.dtype if residual is not None else x.dtype))
+    iy = _dense(y, "y", T, N, dev, dtype)
+    ps, wp, wn = None, None, 0
+    if saved is not None:
+        import torch
+        ps = _plain(saved, "saved", torch.float32, (T, R), dev)
+    else:
+        ws = _workspace_at(workspace, dev, stream, adapters_workspace, T, R, x.device)
+        wp, wn = ws.data_ptr(), ws.numel()
+    _check(_lib.polyq_adapters_forward(C.byref(ix), T, C.byref(d), C.byref(s), ir, C.byref(iy), ps,
+                                       wp, wn, st))
+    return y
+
+
+def adapters_backward(x, a, b, saved, dy, offsets, ids, scales=None, ranks=None, residual=None,
+                      dx=None, da=None, db=None, need_dx=True, need_weights=True, workspace=None,
+                      stream=None):
+    """Gradients (dx, da, db) of adapters_forward for the gradient dy of y.  dx [T][K] is of
+    x's type, or fp32 where a buffer of that type is passed, with `residual` added (of dx's
+    type, may be dx: the gradient that reaches x through the shared projection); rows of no
+    segment are left as they were.  da [n][R][K] and db [n][N][R] are of x's type or those
+    of the buffers passed (contiguous, both of one type, x's or fp32): sums over all rows of
+    an adapter, zeros past its rank and for an adapter without rows.  Those not needed are None."""
+    import torch
+    ix = _dense(x, "x")
+    dev = x.get_device()
+    st = _stream_on(dev, "x", stream)
+    d, s = _adapters(x, a, b, offsets, ids, scales, ranks, dev)
+    T, K, N, R, n = x.shape[0], d.K, d.N, d.R, d.n
+    idy = _dense(dy, "dy", T, N, dev, x.dtype)
+    ir = None
+    if dx is None and need_dx:
+        dx = _made(stream, torch.empty, (T, K), device=x.device,
+                   dtype=x.dtype if residual is None else residual.dtype)
+    if residual is not None:
+        if dx is None:
+            raise ValueError("a residual is added to dx, which is not wanted")
+        ir = C.byref(_dense(residual, "residual", T, K, dev))
+    odx = None if dx is None else C.byref(_dense(dx, "dx", T, K, dev))
+    gt = next((t.dtype for t in (da, db) if isinstance(t, torch.Tensor)), x.dtype)
+    if da is None and need_weights:
+        da = _made(stream, torch.empty, (n, R, K), dtype=gt, device=x.device)
+    if db is None and need_weights:
+        db = _made(stream, torch.empty, (n, N, R), dtype=gt, device=x.device)
+    pa = None if da is None else _plain(da, "da", gt, (n, R, K), dev)
+    pb = None if db is None else _plain(db, "db", gt, (n, N, R), dev)
+    ps = None if saved is None else _plain(saved, "saved", torch.float32, (T, R), dev)
+    wp, wn = None, 0
+    if dx is not None or da is not None:
+        ws = _workspace_at(workspace, dev, stream, adapters_workspace, T, R, x.device)
+        wp, wn = ws.data_ptr(), ws.numel()
+    ty = _type_of(gt)
+    if ty is None:
+        raise ValueError(f"da and db must be {x.dtype} or fp32")
+    _check(_lib.polyq_adapters_backward(C.byref(ix), T, C.byref(d), C.byref(s), ps, C.byref(idy), ir,
+                                        odx, pa, pb, ty, wp, wn, st))
+    return dx, da, db

@@ -135,3 +135,75 @@ def adamw_bounds(p, g, m0, v0, upd, pn, m, v, b1, b2, lr, decay, dtype):
 
 def tiny_f32():
     return 2.0 ** -149
+
+
+# ---- adapters ----
+U32 = 2.0 ** -23
+
+
+def _split(dtype):
+    """What v loses as two 16-bit numbers: relative to itself, and (fp16, scaled by its rows' largest
+    magnitude into 2^14 .. 2^15, half a subnormal step of 2^-24) to that magnitude."""
+    import torch
+    return (2.0 ** -17, 0.0) if dtype == torch.bfloat16 else (2.0 ** -22, 2.0 ** -38)
+
+
+def adapters(x, a, b, off, ids, scales, ranks, y, dy=None, dx=None, out=None, dxt=None, gt=None):
+    """64-bit results of the adapters (torch, any device) and how far a kernel's may be off: lists of
+    (value, bound) for y and, with dy, dx, da, db.  y, dx: the residuals (fp64).
+
+    A sum of n products on the tensor cores is off by two units of 2^-23 of the magnitudes for each 16
+    of them, and 26 for what adds its parts (8 blocks, 8 warps, ten)."""
+    import torch
+
+    def sums(n, s):
+        return (2 * (-(-n // 16)) + 26) * U32 * s
+
+    T, K = x.shape
+    n, R = a.shape[:2]
+    N = b.shape[1]
+    rel, floor = _split(x.dtype)
+    X, A, B = x.double(), a.double(), b.double()
+    Y, EY = y.clone(), torch.zeros_like(y)
+    back = dy is not None
+    if back:
+        D = dy.double()
+        DX, EDX = dx.clone(), torch.zeros_like(dx)
+        DA, DB = torch.zeros_like(A), torch.zeros_like(B)
+        EDA, EDB, LA, LB = (torch.zeros_like(t) for t in (A, B, A, B))
+        count = torch.zeros(n, dtype=torch.int64)
+    for s0, s1, i in zip(off, off[1:], ids):
+        if not 0 <= i < n or s1 <= s0:
+            continue
+        r, s = int(ranks[i]), float(scales[i])
+        t, Ai, Bi = slice(s0, s1), A[i, :r], B[i, :, :r]
+        v = X[t] @ Ai.T
+        ev = sums(K, X[t].abs() @ Ai.T.abs())
+        loss = ev + rel * v.abs() + (floor * v.abs().amax(1, keepdim=True) if r else 0)
+        Y[t] += s * v @ Bi.T
+        EY[t] += abs(s) * (loss @ Bi.T.abs() + sums(2 * R, v.abs() @ Bi.T.abs()))
+        if not back:
+            continue
+        dv = s * D[t] @ Bi
+        edv = abs(s) * sums(N, D[t].abs() @ Bi.abs())
+        DX[t] += dv @ Ai
+        loss_d = edv + rel * dv.abs()
+        EDX[t] += ((loss_d + (floor * dv.abs().amax(1, keepdim=True) if r else 0)) @ Ai.abs()
+                   + sums(2 * R, dv.abs() @ Ai.abs()))
+        DA[i, :r] += dv.T @ X[t]
+        DB[i, :, :r] += s * D[t].T @ v
+        if r:
+            EDA[i, :r] += (loss_d + floor * dv.abs().max()).T @ X[t].abs()
+            EDB[i, :, :r] += abs(s) * D[t].T.abs() @ (ev + rel * v.abs() + floor * v.abs().max())
+            LA[i, :r] += dv.T.abs() @ X[t].abs()
+            LB[i, :, :r] += abs(s) * D[t].T.abs() @ v.abs()
+        count[i] += -(-(s1 - s0) // 64) * 64
+    def final(value, e, dtype):
+        e = e + 2 * U32 * value.abs()
+        return value, e + half_step(dtype) * (value.abs() + e) + tiny(dtype)
+
+    res = [final(Y, EY, out)]
+    if back:
+        m = int(count.max()) if len(count) else 0
+        res += [final(DX, EDX, dxt), final(DA, EDA + sums(2 * m, LA), gt), final(DB, EDB + sums(2 * m, LB), gt)]
+    return res
