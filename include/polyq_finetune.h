@@ -115,7 +115,8 @@ typedef struct {
 /* One step of all tensors:
  *   m = beta1 m + (1-beta1) g,  v = beta2 v + (1-beta2) g^2   (g the scaled gradient)
  *   p = p (1 - lr rate decay) - lr rate / (1-beta1^t) m / (sqrt(v / (1-beta2^t)) + eps)
- * in fp32, p rounded once to its type, copy once from p.  All tensors of a call have one
+ * in fp32, p rounded once to its type, copy once from p; m and v as (beta1 m) + ((1-beta1) g)
+ * and (beta2 v) + (((1-beta2) g) g), each operation rounded, and the root to nearest.  All tensors of a call have one
  * type of p, one of the gradient and one of the copies (any of POLYQ_F32, POLYQ_BF16,
  * POLYQ_F16).
  * 8-bit states are rounded after p has been computed: a block's scale is the smallest with

@@ -136,10 +136,11 @@ __device__ __forceinline__ void update_block(const AdamParams<N>& P, const Tenso
   uint32_t top_m = 0, top_r = 0;
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    const float s = g[i] * c.gs;
-    m[i] = fmaf(P.b1, m[i], P.c1 * s);
-    v[i] = fmaf(P.b2, v[i], P.c2 * s * s);
-    const float root = sqrtf(v[i]);
+    // each operation rounded by itself: the codes of an 8-bit state follow from this order
+    const float s = __fmul_rn(g[i], c.gs);
+    m[i] = __fadd_rn(__fmul_rn(P.b1, m[i]), __fmul_rn(P.c1, s));
+    v[i] = __fadd_rn(__fmul_rn(P.b2, v[i]), __fmul_rn(__fmul_rn(P.c2, s), s));
+    const float root = __fsqrt_rn(v[i]);
     p[i] = fmaf(p[i], c.keep, -__fdividef(c.step * m[i], fmaf(root, c.inv_root_bc2, P.eps)));
     if (BITS == 8) {
       v[i] = root;
