@@ -27,7 +27,7 @@ extern "C" {
 
 /* ---- layer norm ---- */
 
-#define POLYQ_NORM_MAX_K 49152 /* widest row */
+#define POLYQ_NORM_MAX_K 24576 /* widest row */
 
 /* y[r][k] = hat[r][k] weight[k] + bias[k] of x [rows][K],
  *   hat = (x - mean) rstd, rstd = 1 / sqrt(mean of (x - mean)^2 + eps),

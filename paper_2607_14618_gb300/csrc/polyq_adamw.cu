@@ -96,8 +96,8 @@ __device__ __forceinline__ void update_block(const AdamParams<N>& P, const Tenso
   const int lane = threadIdx.x & 31;
   const int64_t e0 = (int64_t)block * kBlock, s0 = (int64_t)(t.at + block) * kBlock;
   // the eight elements of a lane: neighbours, or every 32nd (see load8)
-  const int64_t col = FULL ? 8 * lane : lane;
-  const uint32_t mask = FULL ? 0xFFu : mask8<false>(e0 + col, 32, t.n);
+  const int col = FULL ? 8 * lane : lane;
+  const uint32_t mask = FULL ? 0xFFu : mask8<false>(col, 32, (int)min(t.n - e0, (int64_t)kBlock));
   Raw8<TP> rp;
   Raw8<TG> rg;
   load8<FULL>((const TP*)t.p + e0, col, 32, mask, rp);
@@ -280,11 +280,11 @@ __device__ __forceinline__ void values_block(const uint8_t* codes, const uint8_t
 #pragma unroll
     for (int i = 0; i < 8; ++i) any_store(out, type, e + i, v[i]);
   } else if (type == POLYQ_F32) {
-    store8<true>((float*)out, e, 1, 0xFFu, v);
+    store8<true>((float*)out + e, 0, 1, 0xFFu, v);
   } else if (type == POLYQ_BF16) {
-    store8<true>((__nv_bfloat16*)out, e, 1, 0xFFu, v);
+    store8<true>((__nv_bfloat16*)out + e, 0, 1, 0xFFu, v);
   } else {
-    store8<true>((__half*)out, e, 1, 0xFFu, v);
+    store8<true>((__half*)out + e, 0, 1, 0xFFu, v);
   }
 }
 __global__ void __launch_bounds__(32 * kWarps) adamw_values_kernel(const __grid_constant__ ValuesParams P) {

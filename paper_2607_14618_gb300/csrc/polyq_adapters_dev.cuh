@@ -398,7 +398,7 @@ __device__ __forceinline__ void expand_tile(const ExpandParams& P, const Tile& t
   constexpr int GROUPS = BM * E::BN / 8 / kThreads;  // of eight outputs a thread
   const uint32_t base = smem_u32(smem), wt = base + 2 * E::V_BYTES;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int64_t n0 = (int64_t)blockIdx.x * E::BN;
+  const int n0 = blockIdx.x * E::BN, N = (int)P.N;
   const bool bare = t.id < 0 || t.id >= P.adapters;
   if (bare && P.res == P.y) {  // nothing to add
     if (first) pdl_wait();
@@ -408,7 +408,7 @@ __device__ __forceinline__ void expand_tile(const ExpandParams& P, const Tile& t
   if (!bare) {
     const T* w = (const T*)P.w.w + (int64_t)t.id * P.w.next;
     if (TRANS) copy_tile<RN, CW>(wt, w + n0, P.w.stride, own, P.N - n0);
-    else copy_tile<E::BN, CW>(wt, w + n0 * P.w.stride, P.w.stride, P.N - n0, own);
+    else copy_tile<E::BN, CW>(wt, w + (int64_t)n0 * P.w.stride, P.w.stride, P.N - n0, own);
   }
   cp_commit();
   Raw8<TY> res[GROUPS];
@@ -416,8 +416,8 @@ __device__ __forceinline__ void expand_tile(const ExpandParams& P, const Tile& t
 #pragma unroll
   for (int i = 0; i < GROUPS; ++i) {
     const int g = i * kThreads + threadIdx.x, row = g / PER_ROW;
-    const int64_t col = n0 + (VEC ? g % PER_ROW * 8 : g % PER_ROW);
-    const uint32_t m = P.res && row < t.rows ? mask8<VEC>(col, PER_ROW, P.N) : 0u;
+    const int col = n0 + (VEC ? g % PER_ROW * 8 : g % PER_ROW);
+    const uint32_t m = P.res && row < t.rows ? mask8<VEC>(col, PER_ROW, N) : 0u;
     load8<VEC>((const TY*)P.res + (int64_t)(t.row + row) * P.res_stride, col, PER_ROW, m, res[i]);
   }
   if (first) pdl_wait();  // v comes from the launch before
@@ -499,7 +499,7 @@ __device__ __forceinline__ void expand_tile(const ExpandParams& P, const Tile& t
       for (int e = 0; e < 8; ++e) v[e] += out[row * E::PITCH + c + (VEC ? e : e * PER_ROW)];
     }
     store8<VEC>((TY*)P.y + (int64_t)(t.row + row) * P.y_stride, n0 + c, PER_ROW,
-                mask8<VEC>(n0 + c, PER_ROW, P.N), v);
+                mask8<VEC>(n0 + c, PER_ROW, N), v);
   }
 }
 

@@ -40,12 +40,7 @@ __device__ __forceinline__ void to_float(const Raw8<T>& r, float (&v)[8]) {
   for (int i = 0; i < 8; ++i) v[i] = Elem<T>::to(e[i]);
 }
 
-// Element i of an array of any type (for what is read once per launch).
-__device__ __forceinline__ float any_load(const void* p, int type, int64_t i) {
-  if (type == POLYQ_F32) return __ldcg((const float*)p + i);
-  const uint16_t h = __ldcg((const uint16_t*)p + i);
-  return type == POLYQ_BF16 ? __uint_as_float((uint32_t)h << 16) : __half2float(__ushort_as_half(h));
-}
+// Element i of an array of any type.
 __device__ __forceinline__ void any_store(void* p, int type, int64_t i, float v) {
   if (type == POLYQ_F32) ((float*)p)[i] = v;
   else if (type == POLYQ_BF16) ((__nv_bfloat16*)p)[i] = Elem<__nv_bfloat16>::from(v);
@@ -58,14 +53,14 @@ __device__ __forceinline__ void any_store(void* p, int type, int64_t i, float v)
 // Loads are ordinary ones through L2: a grid may be on its SM before the one that writes its
 // inputs has begun, and the wait on it orders these with those writes.
 template <bool VEC>
-__device__ __forceinline__ uint32_t mask8(int64_t col, int64_t step, int64_t K) {
+__device__ __forceinline__ uint32_t mask8(int col, int step, int K) {
   uint32_t m = 0;
 #pragma unroll
   for (int i = 0; i < 8; ++i) m |= (uint32_t)(col + i * (VEC ? 1 : step) < K) << i;
   return m;
 }
 template <bool VEC, typename T>
-__device__ __forceinline__ void load8(const T* row, int64_t col, int64_t step, uint32_t mask, Raw8<T>& r) {
+__device__ __forceinline__ void load8(const T* row, int col, int step, uint32_t mask, Raw8<T>& r) {
   constexpr int N16 = sizeof(T) * 8 / 16;
   if (VEC && mask == 0xFFu) {
 #pragma unroll
@@ -80,7 +75,7 @@ __device__ __forceinline__ void load8(const T* row, int64_t col, int64_t step, u
   }
 }
 template <bool VEC, typename T>
-__device__ __forceinline__ void store8(T* row, int64_t col, int64_t step, uint32_t mask, const float (&v)[8]) {
+__device__ __forceinline__ void store8(T* row, int col, int step, uint32_t mask, const float (&v)[8]) {
   constexpr int N16 = sizeof(T) * 8 / 16;
   alignas(16) T e[8];
 #pragma unroll

@@ -12,6 +12,7 @@
 // from row to row.  Rows wider than a thread block are shared by a cluster,
 // whose blocks exchange the sums through distributed shared memory.
 #include <algorithm>
+#include <atomic>
 #include <cmath>
 #include <cstring>
 
@@ -26,10 +27,14 @@ namespace {
 using namespace polyq;
 
 constexpr int kMaxCluster = 8;
-// Threads of a block at most (of eight columns each): the backward pass holds 24 sums
-// and weights a thread beside its rows, and spills at the 64 registers of 1024 threads.
-constexpr int kForwardThreads = 1024, kBackwardThreads = 768;
-constexpr int kReduceCols = 32, kReduceRows = 8;
+// Threads of a block at most: rows of up to 2048 columns take eight a thread, wider ones
+// sixteen, so that what a thread does once a row is shared by more of them.
+constexpr int kNarrow = 2048, kNarrowThreads = 256, kWideThreads = 512;
+constexpr int kReduceCols = 32, kReduceRows = 32;
+// Threads of an SM, as registers allow, and rows that a thread takes together once there are enough.
+constexpr int kBackwardRegs = 96, kBackwardPerSm = 65536 / kBackwardRegs, kTogether = 2;
+constexpr int kMostSmem = 200 << 10;
+constexpr int kRingBytes = 96 << 10;  // of shared memory for rows on their way, a block
 
 struct NormParams {
   const void* x;
@@ -39,10 +44,12 @@ struct NormParams {
   const void* w;
   const void* b;
   float* stats;
-  float* parts;  // [2][grid / cluster][K]: sums of dw and of db
-  int64_t x_stride, dy_stride, res_stride, y_stride, rows, K;
+  float* parts;  // [2][groups][K]: sums of dw and of db
+  int64_t x_stride, dy_stride, res_stride, y_stride;
+  int rows, K;
   float eps, inv_k;
-  int w_type, b_type, center, cluster, want_w, want_b;
+  int w_type, b_type, vec_w, vec_b;  // vec: on 16 bytes
+  int center, cluster, depth, want_w, want_b;
 };
 
 __device__ __forceinline__ uint32_t cluster_rank() {
@@ -50,199 +57,488 @@ __device__ __forceinline__ uint32_t cluster_rank() {
   asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
   return r;
 }
-
 __device__ __forceinline__ void cluster_sync() {
   asm volatile("barrier.cluster.arrive.release.aligned;\n barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
-// Sums over a row of two values per thread.  The order is fixed: a butterfly in
-// each warp, a butterfly over the warps' sums, the cluster's blocks in order.
-// One barrier a sum: `at` alternates between two places, and a place is written
-// again only after the barrier of the sum between.
-struct RowSum {
-  float2 (*warps)[32];          // [2][32] of this row's threads
-  float2 (*blocks)[kMaxCluster];  // [2][cluster]
+// Sums over a row's threads of M values each (M a power of two; several rows' at once,
+// so that their latencies are one).  The order is fixed: a butterfly in each warp, in
+// which every step halves the values that a lane still holds; the warps' sums, which as
+// many lanes per value as there are add in turn and by a butterfly; the cluster's blocks
+// in order.  One barrier: `at` alternates between two places, and a place is written
+// again only after the barrier of the sums between.
+template <int M>
+struct RowSums {
+  static constexpr int S = 32 / M;  // lanes of a value
+  float* warps;                     // [2][32][M] of this row's threads
+  float* blocks;                    // [2][kMaxCluster][M]
   int nw, cluster, at;
-  __device__ __forceinline__ float2 operator()(float2 v) {
+  __device__ __forceinline__ void operator()(float (&v)[M]) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, which = lane / S, part = lane % S;
+    int n = M;
 #pragma unroll
     for (int o = 16; o; o >>= 1) {
-      v.x += __shfl_xor_sync(0xFFFFFFFFu, v.x, o);
-      v.y += __shfl_xor_sync(0xFFFFFFFFu, v.y, o);
-    }
-    if (nw == 1 && cluster == 1) return v;
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    at ^= 1;
-    if (lane == 0) warps[at][warp] = v;
-    __syncthreads();
-    v = lane < nw ? warps[at][lane] : make_float2(0.f, 0.f);
+      if (n > 1) {
+        n >>= 1;
 #pragma unroll
-    for (int o = 16; o; o >>= 1) {
-      v.x += __shfl_xor_sync(0xFFFFFFFFu, v.x, o);
-      v.y += __shfl_xor_sync(0xFFFFFFFFu, v.y, o);
+        for (int i = 0; i < M / 2; ++i) {
+          if (i >= n) break;
+          const bool up = lane & o;
+          const float keep = up ? v[i + n] : v[i], give = up ? v[i] : v[i + n];
+          v[i] = keep + __shfl_xor_sync(0xFFFFFFFFu, give, o);
+        }
+      } else {
+        v[0] += __shfl_xor_sync(0xFFFFFFFFu, v[0], o);
+      }
     }
-    if (cluster == 1) return v;
-    if (threadIdx.x < (unsigned)cluster) {
-      const uint32_t mine = smem_u32(&blocks[at][cluster_rank()]);
-      uint32_t there;
-      asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(mine), "r"(threadIdx.x));
-      asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(there), "f"(v.x), "f"(v.y) : "memory");
+    float s = v[0];
+    if (nw > 1 || cluster > 1) {
+      at ^= 1;
+      float* w = warps + at * 32 * M;
+      if (part == 0) w[warp * M + which] = s;
+      __syncthreads();
+      s = 0.f;
+      for (int i = part; i < nw; i += S) s += w[i * M + which];
+#pragma unroll
+      for (int o = S / 2; o; o >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
+      if (cluster > 1) {
+        float* b = blocks + at * kMaxCluster * M;
+        if (warp == 0 && part == 0) {
+          const uint32_t mine = smem_u32(b + cluster_rank() * M + which);
+          for (int r = 0; r < cluster; ++r) {
+            uint32_t there;
+            asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(mine), "r"(r));
+            asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(there), "f"(s) : "memory");
+          }
+        }
+        __syncwarp();
+        cluster_sync();
+        s = 0.f;
+        for (int r = 0; r < cluster; ++r) s += b[r * M + which];
+      }
     }
-    __syncwarp();
-    cluster_sync();
-    float2 s = make_float2(0.f, 0.f);
-    for (int i = 0; i < cluster; ++i) {
-      s.x += blocks[at][i].x;
-      s.y += blocks[at][i].y;
-    }
-    return s;
+#pragma unroll
+    for (int i = 0; i < M; ++i) v[i] = __shfl_sync(0xFFFFFFFFu, s, i * S);
   }
 };
 
-// threadIdx.x: a row's threads (whole warps), threadIdx.y: the rows that a block
-// takes together (one in a cluster).
-template <typename TX, typename TY, bool VEC>
-__global__ void __launch_bounds__(kForwardThreads) norm_forward_kernel(const __grid_constant__ NormParams P) {
-  __shared__ float2 warps[8][2][32];
-  __shared__ float2 blocks[2][kMaxCluster];
-  const int T = blockDim.x, R = blockDim.y;
-  const int rank = P.cluster > 1 ? (int)cluster_rank() : 0;
-  const int64_t c0 = (int64_t)rank * T * 8, col = c0 + (VEC ? threadIdx.x * 8 : threadIdx.x);
-  const uint32_t mask = mask8<VEC>(col, T, P.K);
-  RowSum sum{warps[threadIdx.y], blocks, T >> 5, P.cluster, 0};
-  pdl_trigger();
-  pdl_wait();
-  if (P.cluster > 1) cluster_sync();  // (its blocks have begun: their shared memory may be written)
-  const int64_t step = (int64_t)(gridDim.x / P.cluster) * R;
-  int64_t base = (int64_t)(blockIdx.x / P.cluster) * R, row = base + threadIdx.y;
-  const TX* x = (const TX*)P.x;
-  Raw8<TX> next;
-  load8<VEC>(x + row * P.x_stride, col, T, row < P.rows ? mask : 0u, next);
-  float w[8], b[8];
+// Two fp32 numbers in one instruction.
+using F2 = unsigned long long;
+__device__ __forceinline__ F2 f2(float a, float b) {
+  F2 r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ float2 of(F2 v) {
+  float2 r;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
+  return r;
+}
+__device__ __forceinline__ F2 add2(F2 a, F2 b) {
+  F2 r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ F2 mul2(F2 a, F2 b) {
+  F2 r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ F2 fma2(F2 a, F2 b, F2 c) {
+  F2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ float sum2(F2 v) {
+  const float2 f = of(v);
+  return f.x + f.y;
+}
+template <typename T>
+__device__ __forceinline__ void pairs(const Raw8<T>& r, F2 (&v)[4]) {
+  float f[8];
+  to_float(r, f);
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int64_t k = col + i * (VEC ? 1 : T);
-    const bool in = mask >> i & 1;
-    w[i] = P.w && in ? any_load(P.w, P.w_type, k) : 1.f;
-    b[i] = P.b && in ? any_load(P.b, P.b_type, k) : 0.f;
+  for (int i = 0; i < 4; ++i) v[i] = f2(f[2 * i], f[2 * i + 1]);
+}
+template <bool VEC, typename T>
+__device__ __forceinline__ void store_pairs(T* row, int col, int step, uint32_t mask, const F2 (&v)[4]) {
+  float f[8];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float2 p = of(v[i]);
+    f[2 * i] = p.x;
+    f[2 * i + 1] = p.y;
   }
-  for (; base < P.rows; base += step, row += step) {
-    float v[8];
-    to_float(next, v);
-    const int64_t then = row + step;
-    load8<VEC>(x + then * P.x_stride, col, T, then < P.rows ? mask : 0u, next);
-    float mean = 0.f;
-    if (P.center) {
-      float s = 0.f;
+  store8<VEC>(row, col, step, mask, f);
+}
+// Zeros in the pairs of elements that are not there.
+__device__ __forceinline__ void clear(F2 (&v)[4], uint32_t mask) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) s += v[i];
-      mean = sum(make_float2(s, 0.f)).x * P.inv_k;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = mask >> i & 1 ? v[i] - mean : 0.f;
-    }
-    float q = 0.f;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) q = fmaf(v[i], v[i], q);
-    const float rstd = __frsqrt_rn(fmaf(sum(make_float2(q, 0.f)).x, P.inv_k, P.eps));
-    if (row >= P.rows) continue;
-    if (P.stats && rank == 0 && threadIdx.x == 0) reinterpret_cast<float2*>(P.stats)[row] = make_float2(mean, rstd);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = fmaf(v[i] * rstd, w[i], b[i]);
-    store8<VEC>((TY*)P.y + row * P.y_stride, col, T, mask, v);
+  for (int i = 0; i < 4; ++i) {
+    const float2 p = of(v[i]);
+    v[i] = f2(mask >> (2 * i) & 1 ? p.x : 0.f, mask >> (2 * i + 1) & 1 ? p.y : 0.f);
   }
 }
 
-template <typename TX, typename TY, bool VEC>
-__global__ void __launch_bounds__(kBackwardThreads) norm_backward_kernel(const __grid_constant__ NormParams P) {
-  __shared__ float2 warps[8][2][32];
-  __shared__ float2 blocks[2][kMaxCluster];
-  __shared__ float rows_sum[2048];
-  const int T = blockDim.x, R = blockDim.y;
+// A thread's eight elements of a row, on their way to its own place in shared
+// memory (VEC; no other thread reads it, so that no barrier is needed), or loaded when
+// they are read.
+template <typename T, bool VEC>
+struct Rows {
+  uint32_t at, piece;  // this thread's place, and bytes from one 16-byte piece to the next
+  static constexpr int N16 = sizeof(T) * 8 / 16;
+  __device__ __forceinline__ void ask(const T* row, int col, uint32_t mask, uint32_t slot) const {
+    if constexpr (VEC) {
+      const int have = __popc(mask) * (int)sizeof(T);  // (the row's end: the rest is zeros)
+#pragma unroll
+      for (int i = 0; i < N16; ++i) {
+        const int bytes = min(max(have - 16 * i, 0), 16);
+        const T* src = bytes ? row + col + i * (16 / (int)sizeof(T)) : row;
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(at + slot + i * piece), "l"(src),
+                     "r"(bytes)
+                     : "memory");
+      }
+    }
+  }
+  __device__ __forceinline__ void get(const T* row, int col, int step, uint32_t mask, uint32_t slot,
+                                      F2 (&v)[4]) const {
+    Raw8<T> r;
+    if constexpr (VEC) {
+#pragma unroll
+      for (int i = 0; i < N16; ++i)
+        asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
+                     : "=r"(r.w[i].x), "=r"(r.w[i].y), "=r"(r.w[i].z), "=r"(r.w[i].w)
+                     : "r"(at + slot + i * piece)
+                     : "memory");
+    } else {
+      load8<false>(row, col, step, mask, r);
+    }
+    pairs(r, v);
+  }
+  __device__ __forceinline__ void put(uint32_t slot, const F2 (&v)[4]) const {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const float2 a = of(v[2 * i]), b = of(v[2 * i + 1]);
+      asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(at + slot + i * piece), "f"(a.x), "f"(a.y), "f"(b.x),
+                   "f"(b.y)
+                   : "memory");
+    }
+  }
+};
+
+// Asks for the rows that are depth - 1 (1 to 3) stages ahead and waits for those of `stage`.
+template <typename Ask>
+__device__ __forceinline__ void next_stage(int depth, int stage, Ask ask) {
+  const int there = stage == 0 ? depth - 1 : stage - 1;
+  ask(there);
+  if (depth == 2) asm volatile("cp.async.wait_group 1;" ::: "memory");
+  else if (depth == 3) asm volatile("cp.async.wait_group 2;" ::: "memory");
+  else asm volatile("cp.async.wait_group 3;" ::: "memory");
+}
+
+// Eight elements of a weight or bias; the loads of each type are in flight together, and 16 bytes wide where rows are VEC and the vector
+// lies so (4 bytes of every 32 each time: 99 MB from L2 for 304 blocks, 10 us).
+template <bool VEC, typename T>
+__device__ __forceinline__ void vector8(const T* p, int vec, int col, int step, uint32_t mask, F2 (&v)[4]) {
+  Raw8<T> r;
+  if (VEC && vec) load8<true>(p, col, step, mask, r);
+  else load8<false>(p, col, VEC ? 1 : step, mask, r);
+  pairs(r, v);
+}
+template <bool VEC>
+__device__ __forceinline__ void vector8(const void* p, int type, int vec, int col, int step, uint32_t mask,
+                                        F2 (&v)[4]) {
+  if (type == POLYQ_F32) vector8<VEC>((const float*)p, vec, col, step, mask, v);
+  else if (type == POLYQ_BF16) vector8<VEC>((const __nv_bfloat16*)p, vec, col, step, mask, v);
+  else vector8<VEC>((const __half*)p, vec, col, step, mask, v);
+}
+
+// A thread's groups of eight columns.
+template <int G, bool VEC>
+struct Columns {
+  int col[G], step;
+  uint32_t mask[G];
+  __device__ __forceinline__ Columns(int c0, int T, int K) : step(T) {
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+      col[g] = c0 + (VEC ? (g * T + (int)threadIdx.x) * 8 : g * 8 * T + (int)threadIdx.x);
+      mask[g] = mask8<VEC>(col[g], T, K);
+    }
+  }
+};
+
+// Forward: W warps hold a row in registers as fp32 (threadIdx.x), C pieces of eight columns
+// a lane; rows side by side (threadIdx.y) share a block, which keeps the weight and bias in
+// shared memory as fp32.  The next row is on its way to shared memory meanwhile (VEC).  All
+// pieces but a lane's last are whole (W follows from that), so that the others need no checks.
+constexpr int kForwardWarps = 24, kForwardRegs = 64;
+
+template <typename TX, typename TY, bool VEC, int C>
+__global__ void __maxnreg__(kForwardRegs) norm_forward_kernel(const __grid_constant__ NormParams P) {
+  extern __shared__ __align__(16) uint8_t smem[];
+  __shared__ float parts[15][2][kForwardWarps];  // of rows side by side, in turns, of warps
+  const int W = blockDim.x >> 5, R = blockDim.y, warp = threadIdx.x >> 5, lane = threadIdx.x & 31, K = P.K;
+  const int c0 = VEC ? 8 * (int)threadIdx.x : 256 * warp + lane, next = 256 * W;
+  const uint32_t last = mask8<VEC>(c0 + (C - 1) * next, 32, K);
+  pdl_trigger();
+  pdl_wait();
+  const int plane = (K + 7) / 8;
+  const uint32_t slot = blockDim.x * R * 8 * sizeof(TX);  // of a piece of all threads
+  const Rows<TX, VEC> ring{smem_u32(smem) + ((P.w ? 2 : 0) + (P.b ? 2 : 0)) * plane * 16u +
+                               (threadIdx.y * blockDim.x + threadIdx.x) * 16u,
+                           (uint32_t)(blockDim.x * R * 16)};
+  auto ask = [&](int row, int stage) {
+    if (VEC && row < P.rows) {
+      const TX* x = (const TX*)P.x + (int64_t)row * P.x_stride;
+#pragma unroll
+      for (int j = 0; j < C; ++j) ring.ask(x, c0 + j * next, j < C - 1 ? 0xFFu : last, (stage * C + j) * slot);
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+  int row = blockIdx.x * R + threadIdx.y;
+  ask(row, 0);
+  // The weight and the bias: two planes each, the first and the second four of every eight columns.
+  float4 *sw = reinterpret_cast<float4*>(smem), *sb = sw + (P.w ? 2 * plane : 0);
+#pragma unroll 1
+  for (int which = 0; which < 2; ++which) {
+    const void* p = which ? P.b : P.w;
+    if (!p) continue;
+    float4* to = which ? sb : sw;
+    for (int i = threadIdx.y * blockDim.x + threadIdx.x; i < plane; i += blockDim.x * R) {
+      F2 v[4];
+      vector8<true>(p, which ? P.b_type : P.w_type, which ? P.vec_b : P.vec_w, 8 * i, 1, mask8<true>(8 * i, 1, K), v);
+      const float2 q0 = of(v[0]), q1 = of(v[1]), q2 = of(v[2]), q3 = of(v[3]);
+      to[i] = make_float4(q0.x, q0.y, q1.x, q1.y);
+      to[plane + i] = make_float4(q2.x, q2.y, q3.x, q3.y);
+    }
+  }
+  __syncthreads();
+  // Four columns of a piece (its half h) from a staged vector.
+  auto staged4 = [&](const float4* at, int col, int h, F2& v0, F2& v1) {
+    if (VEC) {
+      const float4 x = at[h * plane + col / 8];
+      v0 = f2(x.x, x.y), v1 = f2(x.z, x.w);
+    } else {
+      float f[4];
+      const float* q = reinterpret_cast<const float*>(at);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int c = min(col + 32 * (4 * h + e), 8 * plane - 1);
+        f[e] = q[((c >> 2 & 1) * plane + (c >> 3)) * 4 + (c & 3)];
+      }
+      v0 = f2(f[0], f[1]), v1 = f2(f[2], f[3]);
+    }
+  };
+  int turn = 0;
+  // A row's sum: the warp's butterfly, then a butterfly over its warps' sums.
+  auto sum = [&](float v) {
+#pragma unroll
+    for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
+    if (W == 1) return v;
+    turn ^= 1;
+    float* p = parts[threadIdx.y][turn];
+    if (lane == 0) p[warp] = v;
+    asm volatile("bar.sync %0, %1;" ::"r"((int)threadIdx.y + 1), "r"((int)blockDim.x) : "memory");
+    v = lane < W ? p[lane] : 0.f;
+#pragma unroll
+    for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
+    return v;
+  };
+  for (int stage = 0; row < P.rows; row += gridDim.x * R, stage ^= 1) {
+    ask(row + gridDim.x * R, stage ^ 1);
+    asm volatile("cp.async.wait_group 1;" ::: "memory");
+    F2 v[C][4];
+#pragma unroll
+    for (int j = 0; j < C; ++j)
+      ring.get((const TX*)P.x + (int64_t)row * P.x_stride, c0 + j * next, 32, j < C - 1 ? 0xFFu : last,
+               (stage * C + j) * slot, v[j]);
+    float mean = 0.f;
+    if (P.center) {
+      F2 s = v[0][0];
+#pragma unroll
+      for (int i = 1; i < 4 * C; ++i) s = add2(s, v[i / 4][i % 4]);
+      mean = sum(sum2(s)) * P.inv_k;
+      const F2 minus = f2(-mean, -mean);
+#pragma unroll
+      for (int j = 0; j < C; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[j][e] = add2(v[j][e], minus);
+      if (last != 0xFFu) clear(v[C - 1], last);
+    }
+    F2 q = mul2(v[0][0], v[0][0]);
+#pragma unroll
+    for (int i = 1; i < 4 * C; ++i) q = fma2(v[i / 4][i % 4], v[i / 4][i % 4], q);
+    const float rstd = __frsqrt_rn(fmaf(sum(sum2(q)), P.inv_k, P.eps));
+    if (P.stats && threadIdx.x == 0) reinterpret_cast<float2*>(P.stats)[row] = make_float2(mean, rstd);
+    const F2 r = f2(rstd, rstd);
+    TY* y = (TY*)P.y + (int64_t)row * P.y_stride;
+#pragma unroll
+    for (int j = 0; j < C; ++j) {
+      const int col = c0 + j * next;
+      const uint32_t mask = j < C - 1 ? 0xFFu : last;
+      if (!mask) break;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        F2 &x0 = v[j][2 * h], &x1 = v[j][2 * h + 1], w0, w1, b0, b1;
+        x0 = mul2(x0, r), x1 = mul2(x1, r);
+        if (P.w) staged4(sw, col, h, w0, w1);
+        if (P.b) staged4(sb, col, h, b0, b1);
+        if (P.w && P.b) x0 = fma2(x0, w0, b0), x1 = fma2(x1, w1, b1);
+        else if (P.w) x0 = mul2(x0, w0), x1 = mul2(x1, w1);
+        else if (P.b) x0 = add2(x0, b0), x1 = add2(x1, b1);
+      }
+      store_pairs<VEC>(y, col, 32, mask, v[j]);
+    }
+  }
+}
+
+// Backward: threadIdx.x: a row's threads (whole warps), threadIdx.y: rows side by side (one
+// in a cluster); each takes NR rows together, blockDim.y apart.  Rows are read from shared
+// memory (or, not VEC, from L2) again after the sums over them, and the weight each time:
+// registers hold the sums over rows.
+template <typename TX, typename TY, bool VEC, int NR, int G>
+__global__ void __maxnreg__(kBackwardRegs) norm_backward_kernel(
+    const __grid_constant__ NormParams P) {
+  extern __shared__ __align__(16) uint8_t ring[];
+  __shared__ float warps[8][2 * 32 * 2 * NR];
+  __shared__ float blocks[2 * kMaxCluster * 2 * NR];
+  __shared__ float rows_sum[1024];
+  const int T = blockDim.x, R = blockDim.y, me = threadIdx.y * T + threadIdx.x;
   const int rank = P.cluster > 1 ? (int)cluster_rank() : 0;
-  const int64_t c0 = (int64_t)rank * T * 8, col = c0 + (VEC ? threadIdx.x * 8 : threadIdx.x);
-  const uint32_t mask = mask8<VEC>(col, T, P.K);
-  RowSum sum{warps[threadIdx.y], blocks, T >> 5, P.cluster, 0};
+  const Columns<G, VEC> at(rank * T * 8 * G, T, P.K);
+  RowSums<2 * NR> sums{warps[threadIdx.y], blocks, T >> 5, P.cluster, 0};
   pdl_trigger();
   pdl_wait();
   if (P.cluster > 1) cluster_sync();
-  const int64_t groups = gridDim.x / P.cluster, step = groups * R;
-  const int64_t group = blockIdx.x / P.cluster;
-  int64_t base = group * R, row = base + threadIdx.y;
-  const TX* x = (const TX*)P.x;
-  const TY* dy = (const TY*)P.dy;
-  const TX* res = (const TX*)P.res;
-  Raw8<TX> nx, nr;
-  Raw8<TY> nd;
-  float2 ns;
-  {
-    const uint32_t m = row < P.rows ? mask : 0u;
-    load8<VEC>(x + row * P.x_stride, col, T, m, nx);
-    load8<VEC>(dy + row * P.dy_stride, col, T, m, nd);
-    if (P.res) load8<VEC>(res + row * P.res_stride, col, T, m, nr);
-    ns = row < P.rows ? __ldcg(reinterpret_cast<const float2*>(P.stats) + row) : make_float2(0.f, 0.f);
-  }
-  float w[8], dw[8], db[8];
+  const int blocks_all = gridDim.x / P.cluster, mine = blockIdx.x / P.cluster, step = blocks_all * R * NR;
+  int row0 = mine * R * NR + threadIdx.y;
+  const uint32_t x_group = T * R * 8 * sizeof(TX), d_group = T * R * 8 * sizeof(TY);
+  const uint32_t d_at = G * x_group, r_at = d_at + G * d_group, slots = r_at + (P.res ? G * x_group : 0);
+  const Rows<TX, VEC> x{smem_u32(ring) + me * 16u, (uint32_t)(T * R * 16)};
+  const Rows<TY, VEC> dy{x.at, x.piece};
+  auto ask = [&](int from, int stage) {
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int64_t k = col + i * (VEC ? 1 : T);
-    w[i] = P.w && (mask >> i & 1) ? any_load(P.w, P.w_type, k) : 1.f;
-    dw[i] = db[i] = 0.f;
-  }
-  for (; base < P.rows; base += step, row += step) {
-    float h[8], d[8];
-    to_float(nx, h);
-    to_float(nd, d);
-    const float mean = P.center ? ns.x : 0.f, rstd = ns.y;
-    const int64_t then = row + step;
-    const uint32_t m = then < P.rows ? mask : 0u;
-    load8<VEC>(x + then * P.x_stride, col, T, m, nx);
-    load8<VEC>(dy + then * P.dy_stride, col, T, m, nd);
-    ns = then < P.rows ? __ldcg(reinterpret_cast<const float2*>(P.stats) + then) : make_float2(0.f, 0.f);
-    float2 s = make_float2(0.f, 0.f);
+    for (int i = 0; i < NR; ++i) {
+      const int row = from + i * R;
+      if (row < P.rows) {
+        const uint32_t slot = (stage * NR + i) * slots;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      h[i] = (h[i] - mean) * rstd;
-      if (row < P.rows) {  // (a row that is not there has no sums to add to)
-        dw[i] = fmaf(d[i], h[i], dw[i]);
-        db[i] += d[i];
-      }
-      d[i] *= w[i];
-      if (mask >> i & 1) {
-        s.x = fmaf(d[i], h[i], s.x);
-        s.y += d[i];
+        for (int g = 0; g < G; ++g) {
+          x.ask((const TX*)P.x + (int64_t)row * P.x_stride, at.col[g], at.mask[g], slot + g * x_group);
+          dy.ask((const TY*)P.dy + (int64_t)row * P.dy_stride, at.col[g], at.mask[g], slot + d_at + g * d_group);
+          if (P.res) x.ask((const TX*)P.res + (int64_t)row * P.res_stride, at.col[g], at.mask[g], slot + r_at + g * x_group);
+        }
       }
     }
-    if (!P.y) continue;  // dx is not wanted
-    s = sum(s);
-    float a[8] = {};
-    if (P.res) {
-      to_float(nr, a);
-      load8<VEC>(res + then * P.res_stride, col, T, m, nr);
-    }
-    if (row >= P.rows) continue;
-    const float mgh = s.x * P.inv_k, mg = P.center ? s.y * P.inv_k : 0.f;
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+  if (VEC)
+    for (int i = 0; i < P.depth - 1; ++i) ask(row0 + i * step, i);
+  F2 dw[G][4], db[G][4];
+  const Rows<float, true> weight{x.at + P.depth * NR * slots, x.piece};  // this thread's eight of each group
 #pragma unroll
-    for (int i = 0; i < 8; ++i) d[i] = fmaf(rstd, d[i] - mg - h[i] * mgh, a[i]);
-    store8<VEC>((TX*)P.y + row * P.y_stride, col, T, mask, d);
+  for (int g = 0; g < G; ++g) {
+    F2 w[4] = {f2(1.f, 1.f), f2(1.f, 1.f), f2(1.f, 1.f), f2(1.f, 1.f)};
+    if (P.w) vector8<VEC>(P.w, P.w_type, P.vec_w, at.col[g], T, at.mask[g], w);
+    weight.put(g * T * R * 32, w);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) dw[g][e] = db[g][e] = f2(0.f, 0.f);
   }
-  // The block's rows are added in order; a group of blocks writes its sums once.
+  float2 stat[NR];
+  auto stats_of = [&](int from) {
+#pragma unroll
+    for (int i = 0; i < NR; ++i) {
+      const int row = from + i * R;
+      stat[i] = row < P.rows ? __ldcg(reinterpret_cast<const float2*>(P.stats) + row) : make_float2(0.f, 0.f);
+      if (!P.center) stat[i].x = 0.f;
+    }
+  };
+  stats_of(row0);
+  for (int stage = 0; row0 - (int)threadIdx.y < P.rows; row0 += step) {
+    if (VEC) next_stage(P.depth, stage, [&](int there) { ask(row0 + (P.depth - 1) * step, there); });
+    // hat and the gradient of a row's columns, zeros where there is no element (what the loads
+    // give there is anything).  They are read again after the sums: the registers are the
+    // weights' and sums'.
+    auto read = [&](int i, int g, F2(&h)[4], F2(&d)[4]) {
+      const int row = row0 + i * R;
+      const uint32_t m = row < P.rows ? at.mask[g] : 0u, slot = (stage * NR + i) * slots;
+      x.get((const TX*)P.x + (int64_t)row * P.x_stride, at.col[g], T, m, slot + g * x_group, h);
+      dy.get((const TY*)P.dy + (int64_t)row * P.dy_stride, at.col[g], T, m, slot + d_at + g * d_group, d);
+      const F2 minus = f2(-stat[i].x, -stat[i].x), r = f2(stat[i].y, stat[i].y);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) h[e] = mul2(add2(h[e], minus), r);
+      if (m != 0xFFu) {
+        clear(h, m);
+        clear(d, m);
+      }
+    };
+    float s[2 * NR];
+#pragma unroll
+    for (int i = 0; i < NR; ++i) {
+      F2 sh = f2(0.f, 0.f), sg = sh;
+#pragma unroll
+      for (int g = 0; g < G; ++g) {
+        F2 h[4], d[4], w[4];
+        read(i, g, h, d);
+        weight.get(nullptr, 0, 0, 0u, g * T * R * 32, w);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          dw[g][e] = fma2(d[e], h[e], dw[g][e]);
+          db[g][e] = add2(db[g][e], d[e]);
+          d[e] = mul2(d[e], w[e]);
+          sh = fma2(d[e], h[e], sh);
+          sg = add2(sg, d[e]);
+        }
+      }
+      s[2 * i] = sum2(sh);
+      s[2 * i + 1] = sum2(sg);
+    }
+    if (P.y) {
+      sums(s);
+#pragma unroll
+      for (int i = 0; i < NR; ++i) {
+        const int row = row0 + i * R;
+        if (row >= P.rows) continue;
+        const float mgh = -s[2 * i] * P.inv_k, mg = P.center ? -s[2 * i + 1] * P.inv_k : 0.f;
+        const F2 mgh2 = f2(mgh, mgh), mg2 = f2(mg, mg), r = f2(stat[i].y, stat[i].y);
+#pragma unroll
+        for (int g = 0; g < G; ++g) {
+          F2 h[4], d[4], w[4], a[4] = {f2(0.f, 0.f), f2(0.f, 0.f), f2(0.f, 0.f), f2(0.f, 0.f)};
+          read(i, g, h, d);
+          weight.get(nullptr, 0, 0, 0u, g * T * R * 32, w);
+          if (P.res)
+            x.get((const TX*)P.res + (int64_t)row * P.res_stride, at.col[g], T, at.mask[g],
+                  (stage * NR + i) * slots + r_at + g * x_group, a);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) d[e] = fma2(r, fma2(h[e], mgh2, fma2(d[e], w[e], mg2)), a[e]);
+          store_pairs<VEC>((TX*)P.y + (int64_t)row * P.y_stride, at.col[g], T, at.mask[g], d);
+        }
+      }
+    }
+    stats_of(row0 + step);
+    if (++stage == P.depth) stage = 0;
+  }
+  // The rows side by side are added in order; a group of blocks writes its sums once.
 #pragma unroll
   for (int which = 0; which < 2; ++which) {
     if (!(which ? P.want_b : P.want_w)) continue;
-    float(&v)[8] = which ? db : dw;
-    float* out = P.parts + ((int64_t)which * groups + group) * P.K;
-    if (R > 1) {
-      for (int r = 1; r < R; ++r) {  // (2048 floats hold one row's threads: 256 of eight)
+    float* out = P.parts + ((int64_t)which * blocks_all + mine) * P.K;
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+      F2(&v)[4] = which ? db[g] : dw[g];
+      for (int r = 1; r < R; ++r) {  // (two rows side by side have at most 128 threads each)
+        F2* other = reinterpret_cast<F2*>(rows_sum) + threadIdx.x;
         __syncthreads();
         if ((int)threadIdx.y == r)
 #pragma unroll
-          for (int i = 0; i < 8; ++i) rows_sum[i * T + threadIdx.x] = v[i];
+          for (int i = 0; i < 4; ++i) other[i * T] = v[i];
         __syncthreads();
         if (threadIdx.y == 0)
 #pragma unroll
-          for (int i = 0; i < 8; ++i) v[i] += rows_sum[i * T + threadIdx.x];
+          for (int i = 0; i < 4; ++i) v[i] = add2(v[i], other[i * T]);
       }
+      if (threadIdx.y == 0) store_pairs<false>(out, at.col[g], VEC ? 1 : T, at.mask[g], v);
     }
-    if (threadIdx.y == 0) store8<false>(out, col, VEC ? 1 : T, mask, v);
   }
 }
 
@@ -275,40 +571,93 @@ __global__ void __launch_bounds__(kReduceCols* kReduceRows) norm_reduce_kernel(c
 
 // How rows are shared out.
 struct Shape {
-  int threads, rows, cluster;
-  int64_t groups;
+  int groups, threads, rows, cluster, nr;  // of columns a thread; of a row; side by side; blocks of a row; together
+  int64_t blocks;  // (clusters of them)
 };
-Shape shape_of(int64_t rows, int64_t K, int sms, bool backward) {
+// `bytes`: of a column's x, dy and residual; two rows of a block and the weight fit into its
+// shared memory.  (Fewer bytes never make for fewer blocks.)
+Shape backward_shape(int64_t rows, int64_t K, int bytes, int sms) {
   Shape s;
+  s.groups = K <= kNarrow ? 1 : 2;
   s.cluster = 1;
-  while ((int64_t)s.cluster * 8 * (backward ? kBackwardThreads : kForwardThreads) < K) s.cluster *= 2;
-  const int64_t cols = (K + s.cluster - 1) / s.cluster;
-  s.threads = (int)((cols + 255) / 256 * 32);
+  const int most_cols = std::min(16 * kWideThreads, kMostSmem / (2 * bytes + 4) / 512 * 512);
+  while ((int64_t)s.cluster * most_cols < K) s.cluster *= 2;
+  const int64_t cols = (K + s.cluster - 1) / s.cluster, warp = 256 * s.groups;
+  s.threads = (int)((cols + warp - 1) / warp * 32);
   // small rows share a block once there is one for every SM
-  s.rows = (int)std::min<int64_t>(std::max(1, 256 / s.threads), (rows + sms - 1) / sms);
-  const int per_sm = std::max(1, (backward ? 1024 : 1536) / (s.threads * s.rows));
-  s.groups = std::min<int64_t>((rows + s.rows - 1) / s.rows, std::max(1, sms * per_sm / s.cluster));
+  s.rows = (int)std::min<int64_t>(std::max(1, kNarrowThreads / s.threads), (rows + sms - 1) / sms);
+  const int64_t most = std::max(1, sms * std::max(1, kBackwardPerSm / (s.threads * s.rows)) / s.cluster);
+  s.nr = rows >= 2 * kTogether * most * s.rows ? kTogether : 1;
+  s.blocks = std::min<int64_t>((rows + s.rows * s.nr - 1) / (s.rows * s.nr), most);
+  return s;
+}
+// Forward: pieces of a lane (1, 2 or 4), warps of a row, rows of a block.
+struct ForwardShape {
+  int c, warps, rows;
+  int64_t blocks;
+};
+ForwardShape forward_shape(int64_t rows, int64_t K, bool vec, int sms) {
+  ForwardShape s;
+  const int n = (int)((K + 255) / 256), full = (int)(K / 256);  // a warp's pieces of 256 columns, whole ones
+  // Many rows: the most pieces of which all but a lane's last are whole (two where rows start
+  // anywhere: their addresses take the registers).  Few: as many warps as there are, for their latency.
+  const int few = n <= kForwardWarps ? 1 : n <= 2 * kForwardWarps ? 2 : 4;
+  s.c = rows < sms ? few : vec ? 4 : std::max(few, 2);
+  while (s.c > 1 && (s.c - 1) * ((n + s.c - 1) / s.c) > full) s.c /= 2;
+  s.warps = (n + s.c - 1) / s.c;
+  const int fit = 65536 / kForwardRegs / 32;  // warps of an SM
+  s.rows = (int)std::min<int64_t>(std::max(1, std::min(15, fit / s.warps)), (rows + sms - 1) / sms);
+  s.blocks = std::min<int64_t>((rows + s.rows - 1) / s.rows, (int64_t)sms * std::max(1, fit / (s.warps * s.rows)));
   return s;
 }
 
+struct Variant {  // size: pieces of a lane (forward), groups of a thread (backward)
+  bool backward, vec;
+  int nr, size;
+  int index(int tx, int ty) const {
+    return ((tx * 3 + ty) * 2 + vec) * 7 + (backward ? 3 + (nr > 1) * 2 + size - 1 : size / 2);
+  }
+};
+template <typename TX, typename TY, bool VEC>
+void* pick(const Variant& v) {
+  if (!v.backward)
+    return v.size == 1   ? (void*)norm_forward_kernel<TX, TY, VEC, 1>
+           : v.size == 2 ? (void*)norm_forward_kernel<TX, TY, VEC, 2>
+                         : (void*)norm_forward_kernel<TX, TY, VEC, 4>;
+  constexpr int many = VEC ? kTogether : 1;
+  if (v.nr > 1)
+    return v.size == 1 ? (void*)norm_backward_kernel<TX, TY, VEC, many, 1> : (void*)norm_backward_kernel<TX, TY, VEC, many, 2>;
+  return v.size == 1 ? (void*)norm_backward_kernel<TX, TY, VEC, 1, 1> : (void*)norm_backward_kernel<TX, TY, VEC, 1, 2>;
+}
 template <typename TX, typename TY>
-void* pick(bool backward, bool vec) {
-  if (backward) return vec ? (void*)norm_backward_kernel<TX, TY, true> : (void*)norm_backward_kernel<TX, TY, false>;
-  return vec ? (void*)norm_forward_kernel<TX, TY, true> : (void*)norm_forward_kernel<TX, TY, false>;
+void* pick(const Variant& v) {
+  return v.vec ? pick<TX, TY, true>(v) : pick<TX, TY, false>(v);
 }
 template <typename TX>
-void* pick(int ty, bool backward, bool vec) {
-  return ty == POLYQ_F32    ? pick<TX, float>(backward, vec)
-         : ty == POLYQ_BF16 ? pick<TX, __nv_bfloat16>(backward, vec)
-                            : pick<TX, __half>(backward, vec);
+void* pick(int ty, const Variant& v) {
+  return ty == POLYQ_F32 ? pick<TX, float>(v) : ty == POLYQ_BF16 ? pick<TX, __nv_bfloat16>(v) : pick<TX, __half>(v);
 }
-void* pick(int tx, int ty, bool backward, bool vec) {
-  return tx == POLYQ_F32    ? pick<float>(ty, backward, vec)
-         : tx == POLYQ_BF16 ? pick<__nv_bfloat16>(ty, backward, vec)
-                            : pick<__half>(ty, backward, vec);
+void* pick(int tx, int ty, const Variant& v) {
+  return tx == POLYQ_F32 ? pick<float>(ty, v) : tx == POLYQ_BF16 ? pick<__nv_bfloat16>(ty, v) : pick<__half>(ty, v);
 }
 
-int launch(void* f, dim3 grid, dim3 block, int cluster, void* params, void* stream, const char* who) {
+// Kernels whose shared memory has been allowed, by type, direction and rows, a bit for each device.
+std::atomic<uint64_t> g_ready[128];
+
+int allow_smem(void* f, int which, const char* who) {
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e == cudaSuccess) {
+    const uint64_t bit = dev < 64 ? 1ull << dev : 0;
+    if (g_ready[which].load(std::memory_order_acquire) & bit) return POLYQ_OK;
+    e = cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostSmem);
+    if (e == cudaSuccess) g_ready[which].fetch_or(bit, std::memory_order_release);
+  }
+  if (e != cudaSuccess) return polyq_set_error(POLYQ_ECUDA, "%s: shared memory: %s", who, cudaGetErrorString(e));
+  return POLYQ_OK;
+}
+
+int launch(void* f, dim3 grid, dim3 block, int smem, int cluster, void* params, void* stream, const char* who) {
   cudaLaunchAttribute at[2];
   at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   at[0].val.programmaticStreamSerializationAllowed = 1;
@@ -321,6 +670,7 @@ int launch(void* f, dim3 grid, dim3 block, int cluster, void* params, void* stre
   cfg.numAttrs = cluster > 1 ? 2 : 1;
   cfg.gridDim = grid;
   cfg.blockDim = block;
+  cfg.dynamicSmemBytes = smem;
   void* args[] = {params};
   cudaError_t ce = cudaLaunchKernelExC(&cfg, f, args);
   if (ce != cudaSuccess) return polyq_set_error(POLYQ_ECUDA, "%s: launch: %s", who, cudaGetErrorString(ce));
@@ -365,24 +715,33 @@ extern "C" int polyq_layernorm_forward(const polyq_dense* x, int64_t rows, int64
   int sms = 0;
   rc = polyq_sm_count(&sms);
   if (rc) return rc;
-  const Shape s = shape_of(rows, K, sms, false);
   NormParams P;
   memset(&P, 0, sizeof P);
   P.x = x->data;
   P.x_stride = x->stride;
   P.y = y->data;
   P.y_stride = y->stride;
-  if (weight) P.w = weight->data, P.w_type = weight->type;
-  if (bias) P.b = bias->data, P.b_type = bias->type;
+  if (weight) P.w = weight->data, P.w_type = weight->type, P.vec_w = (uintptr_t)weight->data % 16 == 0;
+  if (bias) P.b = bias->data, P.b_type = bias->type, P.vec_b = (uintptr_t)bias->data % 16 == 0;
   P.stats = stats;
-  P.rows = rows;
-  P.K = K;
+  P.rows = (int)rows;
+  P.K = (int)K;
   P.eps = eps;
   P.inv_k = 1.f / (float)K;
   P.center = center != 0;
-  P.cluster = s.cluster;
-  return launch(pick(x->type, y->type, false, rows_on_16(x) && rows_on_16(y)), dim3((unsigned)(s.groups * s.cluster)),
-                dim3(s.threads, s.rows), s.cluster, &P, stream, who);
+  bool vec = rows_on_16(x) && rows_on_16(y);
+  ForwardShape s = forward_shape(rows, K, vec, sms);
+  int smem = (int)(K + 7) / 8 * 32 * ((weight != nullptr) + (bias != nullptr));
+  if (vec) {
+    const int row = 2 * s.warps * s.c * 256 * (x->type == POLYQ_F32 ? 4 : 2);
+    if (smem + row > kMostSmem) vec = false, s = forward_shape(rows, K, vec, sms);
+    else s.rows = std::min(s.rows, (kMostSmem - smem) / row), smem += s.rows * row;
+  }
+  const Variant v{false, vec, 1, s.c};
+  void* f = pick(x->type, y->type, v);
+  if (smem > 32 << 10) rc = allow_smem(f, v.index(x->type, y->type), who);
+  if (rc) return rc;
+  return launch(f, dim3((unsigned)s.blocks), dim3(32 * s.warps, s.rows), smem, 1, &P, stream, who);
 }
 
 extern "C" int polyq_layernorm_workspace_bytes(int64_t rows, int64_t K, size_t* bytes) {
@@ -393,7 +752,7 @@ extern "C" int polyq_layernorm_workspace_bytes(int64_t rows, int64_t K, size_t* 
   int sms = 0;
   if (!rc) rc = polyq_sm_count(&sms);
   if (rc) return rc;
-  *bytes = (size_t)shape_of(rows, K, sms, true).groups * K * 2 * sizeof(float);
+  *bytes = (size_t)backward_shape(rows, K, 4, sms).blocks * K * 2 * sizeof(float);
   return POLYQ_OK;
 }
 
@@ -423,12 +782,14 @@ extern "C" int polyq_layernorm_backward(const polyq_dense* x, int64_t rows, int6
   int sms = 0;
   rc = polyq_sm_count(&sms);
   if (rc) return rc;
-  const Shape s = shape_of(rows, K, sms, true);
+  const int xb = x->type == POLYQ_F32 ? 4 : 2, yb = dy->type == POLYQ_F32 ? 4 : 2;
+  const int bytes = xb * (residual ? 2 : 1) + yb;
+  const Shape s = backward_shape(rows, K, bytes, sms);
   const bool sums = dweight || dbias;
   if (sums && (!workspace || (uintptr_t)workspace % 16 ||
-               workspace_bytes < (size_t)s.groups * K * 2 * sizeof(float)))
+               workspace_bytes < (size_t)s.blocks * K * 2 * sizeof(float)))
     return polyq_set_error(POLYQ_ENOMEM, "%s: workspace of %zu bytes, 16-byte aligned, needed", who,
-                           (size_t)s.groups * K * 2 * sizeof(float));
+                           (size_t)s.blocks * K * 2 * sizeof(float));
   NormParams P;
   memset(&P, 0, sizeof P);
   P.x = x->data;
@@ -437,27 +798,35 @@ extern "C" int polyq_layernorm_backward(const polyq_dense* x, int64_t rows, int6
   P.dy_stride = dy->stride;
   if (residual) P.res = residual->data, P.res_stride = residual->stride;
   if (dx) P.y = dx->data, P.y_stride = dx->stride;
-  if (weight) P.w = weight->data, P.w_type = weight->type;
+  if (weight) P.w = weight->data, P.w_type = weight->type, P.vec_w = (uintptr_t)weight->data % 16 == 0;
   P.stats = const_cast<float*>(stats);
   P.parts = (float*)workspace;
-  P.rows = rows;
-  P.K = K;
+  P.rows = (int)rows;
+  P.K = (int)K;
   P.inv_k = 1.f / (float)K;
   P.center = center != 0;
   P.cluster = s.cluster;
   P.want_w = dweight != nullptr;
   P.want_b = dbias != nullptr;
   const bool vec = rows_on_16(x) && rows_on_16(dy) && (!residual || rows_on_16(residual)) && (!dx || rows_on_16(dx));
-  rc = launch(pick(x->type, dy->type, true, vec), dim3((unsigned)(s.groups * s.cluster)), dim3(s.threads, s.rows),
-              s.cluster, &P, stream, who);
+  const int cols = s.threads * s.rows * s.groups * 8;
+  int nr = s.nr, stage = vec ? cols * bytes * nr : 0;
+  if (2 * stage + cols * 4 > kMostSmem) stage /= nr, nr = 1;
+  const Variant v{true, vec, nr, s.groups};
+  void* f = pick(x->type, dy->type, v);
+  P.depth = vec ? std::max(2, std::min(4, (kRingBytes - cols * 4) / stage)) : 0;
+  const int smem = stage * P.depth + cols * 4;
+  if (smem > 32 << 10) rc = allow_smem(f, v.index(x->type, dy->type), who);
+  if (rc) return rc;
+  rc = launch(f, dim3((unsigned)(s.blocks * s.cluster)), dim3(s.threads, s.rows), smem, s.cluster, &P, stream, who);
   if (rc || !sums) return rc;
   ReduceParams Q;
   memset(&Q, 0, sizeof Q);
   Q.parts = P.parts;
   if (dweight) Q.out[0] = dweight->data, Q.type[0] = dweight->type;
   if (dbias) Q.out[1] = dbias->data, Q.type[1] = dbias->type;
-  Q.groups = s.groups;
+  Q.groups = s.blocks;
   Q.K = K;
   return launch((void*)norm_reduce_kernel, dim3((unsigned)((K + kReduceCols - 1) / kReduceCols), 2),
-                dim3(kReduceCols, kReduceRows), 1, &Q, stream, who);
+                dim3(kReduceCols, kReduceRows), 0, 1, &Q, stream, who);
 }

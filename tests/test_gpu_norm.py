@@ -51,8 +51,7 @@ def test_types(polyq_lib, tx, ty, center):
 
 @pytest.mark.parametrize("rows,K", [(1, 1), (1, 5120), (5, 7), (3, 8), (2, 255), (2, 256), (2, 257), (700, 64),
                                     (1000, 31), (5000, 33), (613, 1000), (40, 5003), (9, 6144), (9, 6145),
-                                    (4, 8192), (4, 8193), (3, 16384), (2, 20001), (2, 32768), (2, 49152),
-                                    (1, 49151)])
+                                    (4, 8192), (4, 8193), (3, 16384), (2, 20001), (2, 24576), (1, 24575)])
 @pytest.mark.parametrize("center", [True, False])
 def test_sizes(polyq_lib, rows, K, center):
     run(polyq_lib, rows, K, torch.bfloat16, torch.bfloat16, center, seed=rows + K)
