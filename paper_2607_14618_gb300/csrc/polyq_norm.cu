@@ -29,7 +29,7 @@ using namespace polyq;
 constexpr int kMaxCluster = 8;
 // Threads of a block at most: rows of up to 2048 columns take eight a thread, wider ones
 // sixteen, so that what a thread does once a row is shared by more of them.
-constexpr int kNarrow = 2048, kNarrowThreads = 256, kWideThreads = 512;
+constexpr int kNarrow = 5120, kNarrowThreads = 256, kWideThreads = 512;
 constexpr int kReduceCols = 32, kReduceRows = 32;
 // Threads of an SM, as registers allow, and rows that a thread takes together once there are enough.
 constexpr int kBackwardRegs = 96, kBackwardPerSm = 65536 / kBackwardRegs, kTogether = 2;
