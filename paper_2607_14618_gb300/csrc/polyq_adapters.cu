@@ -95,9 +95,9 @@ int shrink(const polyq_dense* x, int64_t T, int64_t K, const polyq_adapters* ad,
 
 // y = residual + v times one of the adapters' matrices.
 int expand(const float* v, int64_t T, int64_t N, const polyq_adapters* ad, bool trans, const lora::Side& w,
-           const float* scales, const lora::Segments& seg, const polyq_dense* residual, const polyq_dense* y,
+           const float* scales, const lora::Segments& seg, const polyq_dense* residual, const polyq_dense* y, int sms,
            void* stream, const char* who) {
-  const int rn = rank_tile(ad->R), bm = T / seg.n <= 32 ? 16 : 64, bn = bm == 16 ? 256 : 128;
+  const int rn = rank_tile(ad->R), bm = T / seg.n <= 32 ? 16 : 64, bn = rn == 128 && bm == 64 ? 64 : 128;
   const bool half = ad->type == POLYQ_F16, f32 = y->type == POLYQ_F32;
   const Kernel k = half ? lora::expand_of<__half>(bm, rn, trans, f32) : lora::expand_of<__nv_bfloat16>(bm, rn, trans, f32);
   const int eb = f32 ? 4 : 2;
@@ -118,7 +118,9 @@ int expand(const float* v, int64_t T, int64_t N, const polyq_adapters* ad, bool 
   P.vec = (uintptr_t)y->data % 16 == 0 && y->stride * eb % 16 == 0 &&
           (!residual || ((uintptr_t)residual->data % 16 == 0 && residual->stride * eb % 16 == 0));
   const int which = 128 + (((half * 2 + trans) * 4 + rank_index(rn)) * 2 + (bm == 64)) * 2 + f32;
-  return launch(k, which, dim3((unsigned)((N + bn - 1) / bn), (unsigned)std::min(P.tiles, 65535)), 1, &P, stream, who);
+  // Blocks for two rounds of the SMs (two to an SM, more of few rows), each with several column tiles.
+  const int64_t columns = (N + bn - 1) / bn, share = std::max<int64_t>(1, (int64_t)sms * (bm == 16 ? 3 : 4) / P.tiles);
+  return launch(k, which, dim3((unsigned)std::min(columns, share), (unsigned)std::min(P.tiles, 65535)), 1, &P, stream, who);
 }
 
 bool rows_on_16(const polyq_dense* d) { return (uintptr_t)d->data % 16 == 0 && d->stride % 8 == 0; }
@@ -202,7 +204,7 @@ extern "C" int polyq_adapters_forward(const polyq_dense* x, int64_t T, const pol
               seg, v, sms, stream, who);
   if (rc) return rc;
   return expand(v, T, adapters->N, adapters, false, lora::Side{adapters->b, adapters->b_next, adapters->b_stride},
-                adapters->scales, seg, residual, y, stream, who);
+                adapters->scales, seg, residual, y, sms, stream, who);
 }
 
 extern "C" int polyq_adapters_backward(const polyq_dense* x, int64_t T, const polyq_adapters* adapters,
@@ -264,5 +266,5 @@ extern "C" int polyq_adapters_backward(const polyq_dense* x, int64_t T, const po
   }
   if (!dx) return POLYQ_OK;
   return expand(dv, T, adapters->K, adapters, true, lora::Side{adapters->a, adapters->a_next, adapters->a_stride},
-                nullptr, seg, residual, dx, stream, who);
+                nullptr, seg, residual, dx, sms, stream, who);
 }

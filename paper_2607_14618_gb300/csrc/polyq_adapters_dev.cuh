@@ -379,132 +379,192 @@ struct ExpandParams {
   int32_t R, adapters, tiles, vec;
 };
 
+// A block takes BM rows of a segment and every G-th tile of BN columns.  v is held in
+// registers as two operands; the tiles' weights and residuals are on their way to shared
+// memory STAGES - 1 tiles ahead.  A warp's sums are added to the residual in its place
+// there, and go out in whole 128-byte lines (BM = 64): without a barrier, as no other
+// warp touches them.
 template <typename T, int BM, int RN, bool TRANS, typename TY>
 struct Expand {
-  static constexpr int BN = BM == 16 ? 256 : 128;
-  static constexpr int WM = BM == 16 ? 1 : 2, WN = 8 / WM;
-  static constexpr int MT = BM / 16 / WM, NT = BN / 8 / WN;
-  static constexpr int PITCH = BN + 8;  // floats of a row of sums: rows of a quad in different banks
-  static constexpr int V_BYTES = BM * RN * 2, W_BYTES = BN * RN * 2;
-  static constexpr int OUT_BYTES = BM * PITCH * 4;
-  static constexpr int SMEM = 2 * V_BYTES + W_BYTES > OUT_BYTES ? 2 * V_BYTES + W_BYTES : OUT_BYTES;
+  static constexpr int BN = RN == 128 && BM == 64 ? 64 : 128;
+  static constexpr int WM = BM / 16, WN = 8 / WM, NW = BN / WN, NT = NW / 8;  // warps; columns of a warp
+  static constexpr int STAGES = sizeof(TY) == 4 && BM == 64 ? 2 : 3;
+  static constexpr int V_BYTES = BM * RN * 2, W_BYTES = BN * RN * 2, Y_BYTES = BM * BN * (int)sizeof(TY);
+  static constexpr int SMEM = 2 * V_BYTES + STAGES * (W_BYTES + Y_BYTES);
 };
+
+// The 16-byte piece of a tile of outputs (rows of C pieces) in which column c of a row
+// lies: those that a warp's accumulators go to are in different banks.
+template <typename TY, int C>
+__device__ __forceinline__ uint32_t out_piece(int row, int p) {
+  const int s = (sizeof(TY) == 4 ? 2 * row : row) & (C >= 8 ? 7 : C - 1);
+  return (uint32_t)(row * C + (p ^ s)) * 16u;
+}
+
+// `rows` rows of `cols` columns from src to dst as the whole block (rows without an adapter).
+template <typename TY, bool VEC>
+__device__ __forceinline__ void copy_rows(const TY* src, int64_t src_stride, TY* dst, int64_t dst_stride, int rows,
+                                          int cols) {
+  constexpr int E = VEC ? 8 : 1;
+  const int per = (cols + E - 1) / E;
+  for (int i = threadIdx.x; i < rows * per; i += kThreads) {
+    const int row = i / per, c = i % per * E;
+    if constexpr (VEC) {
+      const uint32_t mask = mask8<true>(c, 1, cols);
+      Raw8<TY> r;
+      float v[8];
+      load8<true>(src + row * src_stride, c, 1, src ? mask : 0u, r);
+      to_float(r, v);
+      store8<true>(dst + row * dst_stride, c, 1, mask, v);
+    } else {
+      dst[row * dst_stride + c] = src ? __ldcg(src + row * src_stride + c) : Elem<TY>::from(0.f);
+    }
+  }
+}
 
 template <typename T, int BM, int RN, bool TRANS, typename TY, bool VEC>
 __device__ __forceinline__ void expand_tile(const ExpandParams& P, const Tile& t, uint8_t* smem, float* row_scale,
                                             bool first) {
   using E = Expand<T, BM, RN, TRANS, TY>;
-  constexpr int CV = RN / 8, CW = TRANS ? E::BN / 8 : RN / 8;
-  constexpr int GROUPS = BM * E::BN / 8 / kThreads;  // of eight outputs a thread
-  const uint32_t base = smem_u32(smem), wt = base + 2 * E::V_BYTES;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int n0 = blockIdx.x * E::BN, N = (int)P.N;
-  const bool bare = t.id < 0 || t.id >= P.adapters;
-  if (bare && P.res == P.y) {  // nothing to add
+  constexpr int CV = RN / 8, CW = TRANS ? E::BN / 8 : RN / 8, EP = 16 / sizeof(TY), CY = E::BN / EP;
+  const uint32_t base = smem_u32(smem), ring = base + 2 * E::V_BYTES;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, N = (int)P.N;
+  const int tiles = (N + E::BN - 1) / E::BN, G = gridDim.x;
+  const TY* res = (const TY*)P.res + (int64_t)t.row * P.res_stride;
+  TY* y = (TY*)P.y + (int64_t)t.row * P.y_stride;
+  if (t.id < 0 || t.id >= P.adapters) {
     if (first) pdl_wait();
+    if (P.res == P.y) return;  // nothing to add
+    for (int n0 = blockIdx.x * E::BN; n0 < N; n0 += G * E::BN)
+      copy_rows<TY, VEC>(P.res ? res + n0 : nullptr, P.res_stride, y + n0, P.y_stride, t.rows, min(E::BN, N - n0));
     return;
   }
-  const int own = bare ? 0 : P.ranks ? min(max(__ldcg(P.ranks + t.id), 0), P.R) : P.R;
-  if (!bare) {
-    const T* w = (const T*)P.w.w + (int64_t)t.id * P.w.next;
-    if (TRANS) copy_tile<RN, CW>(wt, w + n0, P.w.stride, own, P.N - n0);
-    else copy_tile<E::BN, CW>(wt, w + (int64_t)n0 * P.w.stride, P.w.stride, P.N - n0, own);
-  }
-  cp_commit();
-  Raw8<TY> res[GROUPS];
-  constexpr int PER_ROW = E::BN / 8;
+  const int own = P.ranks ? min(max(__ldcg(P.ranks + t.id), 0), P.R) : P.R;
+  const T* w = (const T*)P.w.w + (int64_t)t.id * P.w.next;
+  auto ask = [&](int tile, int stage) {
+    if (tile < tiles) {
+      const int n0 = tile * E::BN;
+      const uint32_t at = ring + stage * (E::W_BYTES + E::Y_BYTES), ry = at + E::W_BYTES;
+      if (TRANS) copy_tile<RN, CW>(at, w + n0, P.w.stride, own, N - n0);
+      else copy_tile<E::BN, CW>(at, w + (int64_t)n0 * P.w.stride, P.w.stride, N - n0, own);
+      if (VEC && P.res) {
 #pragma unroll
-  for (int i = 0; i < GROUPS; ++i) {
-    const int g = i * kThreads + threadIdx.x, row = g / PER_ROW;
-    const int col = n0 + (VEC ? g % PER_ROW * 8 : g % PER_ROW);
-    const uint32_t m = P.res && row < t.rows ? mask8<VEC>(col, PER_ROW, N) : 0u;
-    load8<VEC>((const TY*)P.res + (int64_t)(t.row + row) * P.res_stride, col, PER_ROW, m, res[i]);
-  }
-  if (first) pdl_wait();  // v comes from the launch before
-  float acc[E::MT][E::NT][4] = {};
-  const int wm = warp % E::WM, wn = warp / E::WM;
-  if (!bare) {
-#pragma unroll
-    for (int i0 = 0; i0 < BM * CV; i0 += kThreads) {
-      const int i = i0 + threadIdx.x;
-      if (BM * CV % kThreads && i >= BM * CV) break;  // (whole warps)
-      const int row = i / CV, c = i % CV;
-      float v[8];
-      load_v8(P.v + (int64_t)(t.row + row) * P.R + 8 * c, row < t.rows && 8 * c < P.R, v);
-      float scale = 1.f;
-      if constexpr (std::is_same<T, __half>::value) {
-        uint32_t top = abs_bits(v);
-#pragma unroll
-        for (int o = CV / 2; o; o >>= 1) top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
-        scale = scale_down(top);
-        if (c == 0) row_scale[row] = scale_up(top);
+        for (int i0 = 0; i0 < BM * CY; i0 += kThreads) {
+          const int i = i0 + threadIdx.x, row = i / CY, c = i % CY;
+          const int left = row < t.rows ? N - n0 - c * EP : 0;
+          const uint32_t bytes = (uint32_t)min(max(left, 0), EP) * (uint32_t)sizeof(TY);
+          cp_async16(ry + out_piece<TY, CY>(row, c), bytes ? res + row * P.res_stride + n0 + c * EP : res, bytes);
+        }
       }
-      uint4 h, l;
-      split8<T>(v, scale, h, l);
-      *reinterpret_cast<uint4*>(smem + piece<CV>(row, c)) = h;
-      *reinterpret_cast<uint4*>(smem + E::V_BYTES + piece<CV>(row, c)) = l;
     }
-    cp_wait<0>();
+    cp_commit();
+  };
+  int tile = blockIdx.x;
+#pragma unroll
+  for (int i = 0; i < E::STAGES - 1; ++i) ask(tile + i * G, i);
+  if (first) pdl_wait();  // v comes from the launch before
+#pragma unroll
+  for (int i0 = 0; i0 < BM * CV; i0 += kThreads) {
+    const int i = i0 + threadIdx.x;
+    if (BM * CV % kThreads && i >= BM * CV) break;  // (whole warps)
+    const int row = i / CV, c = i % CV;
+    float v[8];
+    load_v8(P.v + (int64_t)(t.row + row) * P.R + 8 * c, row < t.rows && 8 * c < P.R, v);
+    float scale = 1.f;
+    if constexpr (std::is_same<T, __half>::value) {
+      uint32_t top = abs_bits(v);
+#pragma unroll
+      for (int o = CV / 2; o; o >>= 1) top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
+      scale = scale_down(top);
+      if (c == 0) row_scale[row] = scale_up(top);
+    }
+    uint4 h, l;
+    split8<T>(v, scale, h, l);
+    *reinterpret_cast<uint4*>(smem + piece<CV>(row, c)) = h;
+    *reinterpret_cast<uint4*>(smem + E::V_BYTES + piece<CV>(row, c)) = l;
+  }
+  __syncthreads();
+  const int wm = warp % E::WM, wn = warp / E::WM, r0 = wm * 16 + lane / 4;
+  uint32_t h[RN / 16][4], l[RN / 16][4];
+#pragma unroll
+  for (int k = 0; k < RN / 16; ++k) {
+    frag_a<CV, false>(base, wm * 16, k * 16, h[k]);
+    frag_a<CV, false>(base + E::V_BYTES, wm * 16, k * 16, l[k]);
+  }
+  float s0 = P.scales ? __ldcg(P.scales + t.id) : 1.f, s1 = s0;
+  if constexpr (std::is_same<T, __half>::value) s0 *= row_scale[r0], s1 *= row_scale[r0 + 8];
+  for (int stage = 0; tile < tiles; tile += G) {
+    cp_wait<E::STAGES - 2>();
     __syncthreads();
+    ask(tile + (E::STAGES - 1) * G, stage == 0 ? E::STAGES - 1 : stage - 1);
+    const uint32_t at = ring + stage * (E::W_BYTES + E::Y_BYTES);
+    uint8_t* out = smem + (at - base) + E::W_BYTES;
+    float acc[E::NT][4] = {};
 #pragma unroll
-    for (int k = 0; k < RN; k += 16) {
-      uint32_t h[E::MT][4], l[E::MT][4];
-#pragma unroll
-      for (int i = 0; i < E::MT; ++i) {
-        frag_a<CV, false>(base, (wm * E::MT + i) * 16, k, h[i]);
-        frag_a<CV, false>(base + E::V_BYTES, (wm * E::MT + i) * 16, k, l[i]);
-      }
+    for (int k = 0; k < RN / 16; ++k)
 #pragma unroll
       for (int j = 0; j < E::NT; j += 2) {
         uint32_t b[4];
-        frag_b<CW, TRANS>(wt, (wn * E::NT + j) * 8, k, b);
+        frag_b<CW, TRANS>(at, wn * E::NW + j * 8, k * 16, b);
+        mma<T>(acc[j], l[k], b[0], b[1]);
+        mma<T>(acc[j + 1], l[k], b[2], b[3]);
+        mma<T>(acc[j], h[k], b[0], b[1]);
+        mma<T>(acc[j + 1], h[k], b[2], b[3]);
+      }
+    const int n0 = tile * E::BN + wn * E::NW;  // this warp's first column
 #pragma unroll
-        for (int i = 0; i < E::MT; ++i)
+    for (int j = 0; j < E::NT; ++j)
 #pragma unroll
-          for (int q = 0; q < 2; ++q) {
-            mma<T>(acc[i][j + q], l[i], b[2 * q], b[2 * q + 1]);
-            mma<T>(acc[i][j + q], h[i], b[2 * q], b[2 * q + 1]);
-          }
+      for (int q = 0; q < 2; ++q) {  // a row of the accumulators' two
+        const int row = r0 + 8 * q, c = wn * E::NW + j * 8 + lane % 4 * 2;
+        TY* o = reinterpret_cast<TY*>(out + out_piece<TY, CY>(row, c / EP)) + c % EP;
+        float a = acc[j][2 * q] * (q ? s1 : s0), b = acc[j][2 * q + 1] * (q ? s1 : s0);
+        if (VEC && P.res) {
+          a += Elem<TY>::to(o[0]);
+          b += Elem<TY>::to(o[1]);
+        } else if (!VEC && P.res && row < t.rows) {
+          const int n = tile * E::BN + c;
+          if (n < N) a += Elem<TY>::to(__ldcg(res + row * P.res_stride + n));
+          if (n + 1 < N) b += Elem<TY>::to(__ldcg(res + row * P.res_stride + n + 1));
+        }
+        o[0] = Elem<TY>::from(a);
+        o[1] = Elem<TY>::from(b);
+      }
+    __syncwarp();
+    if constexpr (VEC) {
+      constexpr int PW = E::NW / EP;  // pieces of the warp's part of a row
+#pragma unroll
+      for (int i = lane; i < 16 * PW; i += 32) {
+        const int row = wm * 16 + i / PW, c = i % PW;
+        if (row >= t.rows) continue;
+        const uint4 v = *reinterpret_cast<const uint4*>(out + out_piece<TY, CY>(row, wn * E::NW / EP + c));
+        const int n = n0 + c * EP, left = N - n;
+        TY* to = y + row * P.y_stride + n;
+        if (left >= EP) {
+          *reinterpret_cast<uint4*>(to) = v;
+        } else {
+          const TY* e = reinterpret_cast<const TY*>(&v);
+#pragma unroll
+          for (int k = 0; k < EP - 1; ++k)
+            if (k < left) to[k] = e[k];
+        }
+      }
+    } else {
+#pragma unroll 4
+      for (int i = lane; i < 16 * E::NW; i += 32) {
+        const int row = wm * 16 + i / E::NW, c = wn * E::NW + i % E::NW;
+        if (row < t.rows && tile * E::BN + c < N)
+          y[row * P.y_stride + tile * E::BN + c] =
+              reinterpret_cast<const TY*>(out + out_piece<TY, CY>(row, c / EP))[c % EP];
       }
     }
-    __syncthreads();
+    if (++stage == E::STAGES) stage = 0;
   }
-  // Sums through shared memory to threads that hold eight neighbours (or, of rows
-  // that start anywhere, every sixteenth) of a row.
-  float* out = reinterpret_cast<float*>(smem);
-  const float s = bare ? 0.f : P.scales ? __ldcg(P.scales + t.id) : 1.f;
-  if (!bare) {
-#pragma unroll
-    for (int i = 0; i < E::MT; ++i) {
-      const int row = (wm * E::MT + i) * 16 + lane / 4;
-      float s0 = s, s1 = s;
-      if constexpr (std::is_same<T, __half>::value) s0 *= row_scale[row], s1 *= row_scale[row + 8];
-#pragma unroll
-      for (int j = 0; j < E::NT; ++j) {
-        const int col = (wn * E::NT + j) * 8 + lane % 4 * 2;
-        *reinterpret_cast<float2*>(out + row * E::PITCH + col) = make_float2(acc[i][j][0] * s0, acc[i][j][1] * s0);
-        *reinterpret_cast<float2*>(out + (row + 8) * E::PITCH + col) = make_float2(acc[i][j][2] * s1, acc[i][j][3] * s1);
-      }
-    }
-    __syncthreads();
-  }
-#pragma unroll
-  for (int i = 0; i < GROUPS; ++i) {
-    const int g = i * kThreads + threadIdx.x, row = g / PER_ROW, c = VEC ? g % PER_ROW * 8 : g % PER_ROW;
-    if (row >= t.rows) break;
-    float v[8];
-    to_float(res[i], v);
-    if (!bare) {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] += out[row * E::PITCH + c + (VEC ? e : e * PER_ROW)];
-    }
-    store8<VEC>((TY*)P.y + (int64_t)(t.row + row) * P.y_stride, n0 + c, PER_ROW,
-                mask8<VEC>(n0 + c, PER_ROW, N), v);
-  }
+  cp_wait<0>();
 }
 
 template <typename T, int BM, int RN, bool TRANS, typename TY>
-__global__ void __launch_bounds__(kThreads) expand_kernel(const __grid_constant__ ExpandParams P) {
+__global__ void __launch_bounds__(kThreads, 2) expand_kernel(const __grid_constant__ ExpandParams P) {
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ float row_scale[BM];
   bool first = true;
