@@ -112,19 +112,44 @@ __device__ __forceinline__ void frag_b(uint32_t tile, int n, int k, uint32_t (&r
   if (TRANS) ldmatrix4<true>(tile + piece<C>(k + (i & 1) * 8 + j, n / 8 + (i >> 1)), r);
   else ldmatrix4<false>(tile + piece<C>(n + (i >> 1) * 8 + j, k / 8 + (i & 1)), r);
 }
-// Copies ROWS x C pieces of a matrix (rows of `stride` elements) whose rows from
-// `rows` on and elements from `cols` on are zeros.
-template <int ROWS, int C>
-__device__ __forceinline__ void copy_tile(uint32_t tile, const void* src, int64_t stride, int64_t rows, int64_t cols) {
-#pragma unroll
-  for (int i0 = 0; i0 < ROWS * C; i0 += kThreads) {
-    const int i = i0 + threadIdx.x;
-    if (ROWS * C % kThreads && i >= ROWS * C) break;
-    const int row = i / C, c = i % C;
-    const int64_t left = row < rows ? cols - 8 * c : 0;
-    const uint32_t bytes = left >= 8 ? 16u : left > 0 ? (uint32_t)left * 2u : 0u;
-    cp_async16(tile + piece<C>(row, c), (const uint16_t*)src + (bytes ? row * stride + 8 * c : 0), bytes);
+// A thread's pieces of a tile of ROWS x C pieces that comes from rows of `stride`
+// elements: the same piece of every kThreads / C-th row, so that one pointer, one place and
+// one length serve them all (with an address, a bound and a swizzle computed for each
+// piece, copies took 60 instructions and bound the kernels).  Elements from `cols` on
+// (counted from the tile's first) and rows from `rows` on are zeros.
+template <int ROWS, int C, int ELEM = 2>
+struct Mover {
+  static constexpr int E = 16 / ELEM, EACH = kThreads / C;  // elements of a piece; rows from one to the next
+  const char* p;
+  int64_t step;  // bytes of EACH rows
+  uint32_t dst, bytes;
+  int row;
+  __device__ __forceinline__ Mover(const void* src, int64_t stride, int cols, uint32_t place) {
+    const int c = threadIdx.x % C;
+    row = threadIdx.x / C;
+    p = (const char*)src + ((int64_t)row * stride + c * E) * ELEM;
+    step = stride * EACH * ELEM;
+    dst = place;
+    limit(cols);
   }
+  __device__ __forceinline__ void limit(int cols) {
+    bytes = (uint32_t)(min(max(cols - (int)(threadIdx.x % C) * E, 0), E) * ELEM);
+  }
+  // The tile that begins `off` bytes after src.
+  __device__ __forceinline__ void copy(uint32_t tile, int64_t off, int rows) const {
+    if (ROWS * C < kThreads && threadIdx.x >= ROWS * C) return;
+    const char* q = p + off;
+#pragma unroll
+    for (int i = 0; i < (ROWS * C + kThreads - 1) / kThreads; ++i) {
+      const bool in = row + i * EACH < rows && bytes;
+      cp_async16(tile + dst + i * kThreads * 16, in ? q : p, in ? bytes : 0u);
+      q += step;
+    }
+  }
+};
+template <int C>
+__device__ __forceinline__ uint32_t my_piece() {
+  return piece<C>(threadIdx.x / C, threadIdx.x % C);
 }
 
 // ---- which rows ----
@@ -297,25 +322,33 @@ __global__ void __launch_bounds__(kThreads) shrink_kernel(const __grid_constant_
   const int64_t chunks = (P.K + KC - 1) / KC;
   const int64_t c0 = chunks * rank / P.cluster, c1 = chunks * (rank + 1) / P.cluster;
 
-  auto copy = [&](int64_t c) {
-    const uint32_t at = base + (uint32_t)((c - c0) % S::STAGES) * (S::X_BYTES + S::W_BYTES);
-    const int64_t k = c * KC;
-    copy_tile<BM, CX>(at, x + k, P.x_stride, t.rows, P.K - k);
-    if (TRANS) copy_tile<KC, CW>(at + S::X_BYTES, w + k * P.w.stride, P.w.stride, P.K - k, own);
-    else copy_tile<RN, CW>(at + S::X_BYTES, w + k, P.w.stride, own, P.K - k);
+  Mover<BM, CX> mx(x, P.x_stride, KC, my_piece<CX>());
+  Mover<TRANS ? KC : RN, CW> mw(w, P.w.stride, TRANS ? own : KC, my_piece<CW>());
+  const int64_t x_step = KC * 2, w_step = TRANS ? P.w.stride * KC * 2 : KC * 2;
+  auto copy = [&](int64_t c, int stage) {
+    const uint32_t at = base + stage * (S::X_BYTES + S::W_BYTES);
+    const int left = (int)min(P.K - c * KC, (int64_t)KC);
+    if (left < KC) {  // the contraction's end
+      mx.limit(left);
+      if (!TRANS) mw.limit(left);
+    }
+    mx.copy(at, c * x_step, t.rows);
+    mw.copy(at + S::X_BYTES, c * w_step, TRANS ? left : own);
   };
   float acc[S::MT][S::NT][4] = {};
   const int wm = warp % S::WM, wn = warp / S::WM % S::WN, wk = warp / (S::WM * S::WN);
   for (int i = 0; i < S::STAGES - 1; ++i) {
-    if (c0 + i < c1) copy(c0 + i);
+    if (c0 + i < c1) copy(c0 + i, i);
     cp_commit();
   }
+  int stage = 0;
   for (int64_t c = c0; c < c1; ++c) {
     cp_wait<S::STAGES - 2>();
     __syncthreads();
-    if (c + S::STAGES - 1 < c1) copy(c + S::STAGES - 1);
+    if (c + S::STAGES - 1 < c1) copy(c + S::STAGES - 1, stage == 0 ? S::STAGES - 1 : stage - 1);
     cp_commit();
-    const uint32_t at = base + (uint32_t)((c - c0) % S::STAGES) * (S::X_BYTES + S::W_BYTES);
+    const uint32_t at = base + stage * (S::X_BYTES + S::W_BYTES);
+    if (++stage == S::STAGES) stage = 0;
 #pragma unroll
     for (int k = wk * 16; k < KC; k += 16 * S::WK) {
       uint32_t a[S::MT][4];
@@ -441,21 +474,19 @@ __device__ __forceinline__ void expand_tile(const ExpandParams& P, const Tile& t
   }
   const int own = P.ranks ? min(max(__ldcg(P.ranks + t.id), 0), P.R) : P.R;
   const T* w = (const T*)P.w.w + (int64_t)t.id * P.w.next;
+  Mover<TRANS ? RN : E::BN, CW> mw(w, P.w.stride, TRANS ? E::BN : own, my_piece<CW>());
+  Mover<BM, CY, (int)sizeof(TY)> mr(P.res ? res : y, P.res_stride, E::BN,
+                                    out_piece<TY, CY>(threadIdx.x / CY, threadIdx.x % CY));
   auto ask = [&](int tile, int stage) {
     if (tile < tiles) {
-      const int n0 = tile * E::BN;
-      const uint32_t at = ring + stage * (E::W_BYTES + E::Y_BYTES), ry = at + E::W_BYTES;
-      if (TRANS) copy_tile<RN, CW>(at, w + n0, P.w.stride, own, N - n0);
-      else copy_tile<E::BN, CW>(at, w + (int64_t)n0 * P.w.stride, P.w.stride, N - n0, own);
-      if (VEC && P.res) {
-#pragma unroll
-        for (int i0 = 0; i0 < BM * CY; i0 += kThreads) {
-          const int i = i0 + threadIdx.x, row = i / CY, c = i % CY;
-          const int left = row < t.rows ? N - n0 - c * EP : 0;
-          const uint32_t bytes = (uint32_t)min(max(left, 0), EP) * (uint32_t)sizeof(TY);
-          cp_async16(ry + out_piece<TY, CY>(row, c), bytes ? res + row * P.res_stride + n0 + c * EP : res, bytes);
-        }
+      const int left = min(N - tile * E::BN, E::BN);
+      const uint32_t at = ring + stage * (E::W_BYTES + E::Y_BYTES);
+      if (left < E::BN) {  // the columns' end
+        if (TRANS) mw.limit(left);
+        mr.limit(left);
       }
+      mw.copy(at, (int64_t)tile * E::BN * 2 * (TRANS ? 1 : P.w.stride), TRANS ? own : left);
+      if (VEC && P.res) mr.copy(at + E::W_BYTES, (int64_t)tile * E::BN * (int)sizeof(TY), t.rows);
     }
     cp_commit();
   };
@@ -636,11 +667,11 @@ __global__ void __launch_bounds__(kThreads) gradients_kernel(const __grid_consta
   AdapterTiles ahead, now;
   ahead.begin(rank);
   now.begin(rank);
+  const Mover<BT, CX> mx((const T*)D.x + n0, D.x_stride, (int)min(D.C - n0, (int64_t)G::BC), my_piece<CX>());
   auto copy = [&](int stage) {
     int row, rows;
     if (ahead.next(P.seg, id, BT, P.cluster, row, rows))
-      copy_tile<BT, CX>(base + stage * G::X_BYTES, (const T*)D.x + (int64_t)row * D.x_stride + n0, D.x_stride, rows,
-                        D.C - n0);
+      mx.copy(base + stage * G::X_BYTES, (int64_t)row * D.x_stride * 2, rows);
     cp_commit();
   };
   float v[VG][8];
