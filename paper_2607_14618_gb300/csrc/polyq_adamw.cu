@@ -59,40 +59,69 @@ __device__ __forceinline__ uint32_t mix(uint32_t h) {
   return (h ^ h >> 15) * 0x6C62272Du;
 }
 
-// Codes of magnitudes with MANT mantissa bits and one sign bit fewer than 8 bits
-// leave: a number whose smallest normal one is 1 is, scaled by 2^-126, an fp32
-// number of the same exponent field, subnormal ones included; its code is the
-// upper bits of that.
+// A magnitude with MANT mantissa bits, whose smallest normal number is 1, is, scaled by
+// 2^-126, an fp32 number of the same exponent field, subnormal ones included: its code is
+// that number's upper bits.  Between it and the block's scale, 2^(scale-127), lies the power
+// 2^(scale-1): fp32 holds it or its reciprocal for scales up to 127, which one product then
+// takes; others take two.  Both are exact but for numbers that fp32 holds as subnormal.
+struct Scale {
+  float one, rest;  // the power of two, as two factors
+  bool two;
+  static __device__ __forceinline__ float pow2(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
+  // 2^(s-1), codes to values
+  static __device__ __forceinline__ Scale up(int s) { return Scale{pow2(min(s, 128) - 1), pow2(max(s - 128, 0)), s > 128}; }
+  // 2^(1-s), values to codes
+  static __device__ __forceinline__ Scale down(int s) {
+    return Scale{pow2(1 - min(s, 127)), pow2(min(127 - s, 0)), s > 127};
+  }
+  __device__ __forceinline__ void apply(float (&v)[8]) const {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] *= one;
+    if (two)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] *= rest;
+  }
+};
+// Values of eight codes (a byte each): MANT 3 with a sign in bit 7, MANT 4 without.
 template <int MANT>
-__device__ __forceinline__ float decode(uint32_t code, float unit) {  // unit: 2^(scale-127)
-  return __uint_as_float(code << (23 - MANT)) * 0x1p126f * unit;
-}
-// a times inv (2^(127-scale)), rounded down after adding u / 65536 of the last place.
-template <int MANT>
-__device__ __forceinline__ uint32_t encode(float a, float inv, uint32_t u) {
-  return (__float_as_uint(a * inv * 0x1p-126f) + (u << (23 - MANT - 16))) >> (23 - MANT);
+__device__ __forceinline__ void decode(uint2 codes, int scale, float (&v)[8]) {
+  constexpr uint32_t MASK = (MANT == 3 ? 0x7Fu : 0xFFu) << (23 - MANT);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const uint32_t w = i < 4 ? codes.x : codes.y;
+    const int at = 23 - MANT - 8 * (i & 3);  // from a byte's place to the code's
+    uint32_t b = (at >= 0 ? w << at : w >> -at) & MASK;
+    if (MANT == 3) b |= w << (24 - 8 * (i & 3)) & 0x80000000u;
+    v[i] = __uint_as_float(b);
+  }
+  if (scale == 255) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(0x7FC00000u);
+  } else {
+    Scale::up(scale).apply(v);
+  }
 }
 // The smallest scale with which the largest magnitude `top` is within the codes (so
 // that none is cut off, which would bias the largest ones): the one that brings it to
 // 2^14 .. 2^15, or the next where it lies above the last code there.
 template <int MANT>
-__device__ __forceinline__ uint32_t scale_of(uint32_t top) {
+__device__ __forceinline__ int scale_of(uint32_t top) {
   const uint32_t past = top + (1u << (23 - MANT)) - 1;
-  return top >= 0x7F800000u ? 255u : (uint32_t)max((int)(past >> 23) - 14, 0);
+  return top >= 0x7F800000u ? 255 : max((int)(past >> 23) - 14, 0);
 }
-__device__ __forceinline__ float unit_of(uint32_t s) {
-  return s == 255u ? __uint_as_float(0x7FC00000u) : s ? __uint_as_float(s << 23) : __uint_as_float(0x00400000u);
+__device__ __forceinline__ uint32_t pack4(const uint32_t (&c)[8], int i) {
+  return c[i] | c[i + 1] << 8 | c[i + 2] << 16 | c[i + 3] << 24;
 }
 
 // What is the same for all elements of a tensor.
 struct Rates {
   float gs, keep, step, inv_root_bc2;
+  uint32_t seed_key, seed_high;
 };
 
 // One block: elements i of the tensor from e0 on.  FULL: 256 of them, on 16 bytes.
 template <typename TP, typename TG, int BITS, bool FULL, int N>
-__device__ __forceinline__ void update_block(const AdamParams<N>& P, const Tensor& t, uint32_t block, const Rates& c,
-                                             uint32_t seed_key) {
+__device__ __forceinline__ void update_block(const AdamParams<N>& P, const Tensor& t, uint32_t block, const Rates& c) {
   const int lane = threadIdx.x & 31;
   const int64_t e0 = (int64_t)block * kBlock, s0 = (int64_t)(t.at + block) * kBlock;
   // the eight elements of a lane: neighbours, or every 32nd (see load8)
@@ -110,25 +139,26 @@ __device__ __forceinline__ void update_block(const AdamParams<N>& P, const Tenso
     to_float(rm, m);
     to_float(rv, v);
   } else {
-    uint8_t cm[8], cv[8];
+    uint2 cm, cv;
     const uint8_t *pm = (const uint8_t*)P.m + s0, *pv = (const uint8_t*)P.v + s0;
     if constexpr (FULL) {
-      *reinterpret_cast<uint2*>(cm) = __ldcg(reinterpret_cast<const uint2*>(pm + col));
-      *reinterpret_cast<uint2*>(cv) = __ldcg(reinterpret_cast<const uint2*>(pv + col));
+      cm = __ldcg(reinterpret_cast<const uint2*>(pm + col));
+      cv = __ldcg(reinterpret_cast<const uint2*>(pv + col));
     } else {
+      uint32_t bm[8], bv[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        cm[i] = mask >> i & 1 ? __ldcg(pm + col + 32 * i) : 0;
-        cv[i] = mask >> i & 1 ? __ldcg(pv + col + 32 * i) : 0;
+        bm[i] = mask >> i & 1 ? __ldcg(pm + col + 32 * i) : 0u;
+        bv[i] = mask >> i & 1 ? __ldcg(pv + col + 32 * i) : 0u;
       }
+      cm = make_uint2(pack4(bm, 0), pack4(bm, 4));
+      cv = make_uint2(pack4(bv, 0), pack4(bv, 4));
     }
-    const float um = unit_of(__ldcg(P.ms + t.at + block)), uv = unit_of(__ldcg(P.vs + t.at + block));
+    const int sm = __ldcg(P.ms + t.at + block), sv = __ldcg(P.vs + t.at + block);
+    decode<3>(cm, sm, m);
+    decode<4>(cv, sv, v);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      m[i] = __uint_as_float(__float_as_uint(decode<3>(cm[i] & 127u, um)) | (uint32_t)(cm[i] >> 7) << 31);
-      v[i] = decode<4>(cv[i], uv);
-      v[i] *= v[i];
-    }
+    for (int i = 0; i < 8; ++i) v[i] = __fmul_rn(v[i], v[i]);
   }
   float p[8], g[8];
   to_float(rp, p);
@@ -141,12 +171,13 @@ __device__ __forceinline__ void update_block(const AdamParams<N>& P, const Tenso
     m[i] = __fadd_rn(__fmul_rn(P.b1, m[i]), __fmul_rn(P.c1, s));
     v[i] = __fadd_rn(__fmul_rn(P.b2, v[i]), __fmul_rn(__fmul_rn(P.c2, s), s));
     const float root = __fsqrt_rn(v[i]);
-    p[i] = fmaf(p[i], c.keep, -__fdividef(c.step * m[i], fmaf(root, c.inv_root_bc2, P.eps)));
+    // (the denominator is eps or more, and at most 2^65 / (1 - b2^t): within the reciprocal's range)
+    p[i] = fmaf(-c.step * m[i], fp4::rcp_approx(fmaf(root, c.inv_root_bc2, P.eps)), p[i] * c.keep);
     if (BITS == 8) {
       v[i] = root;
       if (!FULL && !(mask >> i & 1)) m[i] = v[i] = 0.f;
       top_m = max(top_m, __float_as_uint(m[i]) & 0x7FFFFFFFu);
-      top_r = max(top_r, __float_as_uint(root) & 0x7FFFFFFFu);
+      top_r = max(top_r, __float_as_uint(v[i]) & 0x7FFFFFFFu);
     }
   }
   store8<FULL>((TP*)t.p + e0, col, 32, mask, p);
@@ -173,34 +204,40 @@ __device__ __forceinline__ void update_block(const AdamParams<N>& P, const Tenso
   } else {
     top_m = __reduce_max_sync(0xFFFFFFFFu, top_m);
     top_r = __reduce_max_sync(0xFFFFFFFFu, top_r);
-    const uint32_t sm = scale_of<3>(top_m), sr = scale_of<4>(top_r);
-    const float im = sm == 255u ? 0.f : __uint_as_float((254u - sm) << 23);
-    const float ir = sr == 255u ? 0.f : __uint_as_float((254u - sr) << 23);
+    const int sm = scale_of<3>(top_m), sr = scale_of<4>(top_r);
     const uint64_t b64 = (uint64_t)t.at + block;
-    const uint32_t key = mix(mix((uint32_t)b64 ^ seed_key) ^ (uint32_t)(b64 >> 32) ^ (uint32_t)(P.seed >> 32));
-    uint8_t cm[8], cv[8];
+    const uint32_t key = mix(mix((uint32_t)b64 ^ c.seed_key) ^ (uint32_t)(b64 >> 32) ^ c.seed_high);
+    uint32_t cm[8] = {}, cv[8] = {};
+    uint32_t some[8];  // 1 where the root is not 0
+#pragma unroll
+    for (int i = 0; i < 8; ++i) some[i] = min(__float_as_uint(v[i]), 1u);
+    Scale::down(sm).apply(m);
+    Scale::down(sr).apply(v);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const uint32_t e = FULL ? (uint32_t)(col + i) : (uint32_t)(col + 32 * i);
       uint32_t u = mix(key + 0x9E3779B1u * e);
       u ^= u >> 16;
-      const uint32_t sign = __float_as_uint(m[i]) >> 31;
-      uint32_t a = encode<3>(fabsf(m[i]), im, u & 0xFFFFu);
-      a |= a ? sign << 7 : 0u;
-      uint32_t r = encode<4>(v[i], ir, u >> 16);
-      r = v[i] > 0.f ? max(r, 1u) : r;
-      cm[i] = sm == 255u ? 0 : (uint8_t)a;
-      cv[i] = sr == 255u ? 0 : (uint8_t)r;
+      // (the sign stays above: no magnitude of the block carries into it)
+      const uint32_t a = __float_as_uint(m[i]) + ((u & 0xFFFFu) << 4);
+      cm[i] = (a >> 20 & 0x7Fu) | (a >> 24 & 0x80u);
+      cv[i] = max((__float_as_uint(v[i]) + (u >> 13 & 0x7FFF8u)) >> 19, some[i]);
     }
+    if (sm == 255 || sr == 255)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        if (sm == 255) cm[i] = 0u;
+        if (sr == 255) cv[i] = 0u;
+      }
     uint8_t *pm = (uint8_t*)P.m + s0, *pv = (uint8_t*)P.v + s0;
     if constexpr (FULL) {
-      *reinterpret_cast<uint2*>(pm + col) = *reinterpret_cast<const uint2*>(cm);
-      *reinterpret_cast<uint2*>(pv + col) = *reinterpret_cast<const uint2*>(cv);
+      *reinterpret_cast<uint2*>(pm + col) = make_uint2(pack4(cm, 0), pack4(cm, 4));
+      *reinterpret_cast<uint2*>(pv + col) = make_uint2(pack4(cv, 0), pack4(cv, 4));
     } else {
 #pragma unroll
       for (int i = 0; i < 8; ++i) {  // (the whole block is the tensor's)
-        pm[col + 32 * i] = cm[i];
-        pv[col + 32 * i] = cv[i];
+        pm[col + 32 * i] = (uint8_t)cm[i];
+        pv[col + 32 * i] = (uint8_t)cv[i];
       }
     }
     __syncwarp();  // every lane has read the block's scales
@@ -211,8 +248,15 @@ __device__ __forceinline__ void update_block(const AdamParams<N>& P, const Tenso
   }
 }
 
+// Thread blocks of an SM.  32 bits: bound by HBM, and nearest to it with short ones that the
+// SMs take as they come (212 M elements: 996 us with 8 an SM, 870 with 64, 848 with 256: 7.0
+// TB/s).  8 bits: bound by instructions, 100 an element (as many as fit at once: 833 us with 4,
+// 939 with 8; a warp that asks for its next block ahead has room for 3: 893 us).
+constexpr int kBlocks32 = 256, kBlocks8 = 4;
+
 template <typename TP, typename TG, int BITS, int N>
-__global__ void __launch_bounds__(32 * kWarps) adamw_kernel(const __grid_constant__ AdamParams<N> P) {
+__global__ void __launch_bounds__(32 * kWarps, 4)
+    adamw_kernel(const __grid_constant__ AdamParams<N> P) {
   pdl_trigger();
   pdl_wait();
   Rates c;
@@ -231,11 +275,10 @@ __global__ void __launch_bounds__(32 * kWarps) adamw_kernel(const __grid_constan
     inv_bc1 = -1.f / expm1f((float)t * P.log_b1);
     c.inv_root_bc2 = rsqrtf(-expm1f((float)t * P.log_b2));
   }
-  const uint32_t seed_key = mix((uint32_t)seed + 1u);
+  c.seed_key = mix((uint32_t)seed + 1u);
+  c.seed_high = (uint32_t)(seed >> 32);
   const uint32_t stride = gridDim.x * kWarps;
-  for (uint32_t b0 = blockIdx.x * kWarps; b0 < P.blocks; b0 += stride) {
-    const uint32_t b = b0 + (threadIdx.x >> 5);
-    if (b >= P.blocks) return;
+  for (uint32_t b = blockIdx.x * kWarps + (threadIdx.x >> 5); b < P.blocks; b += stride) {
     int lo = 0, hi = P.n - 1;  // the last tensor whose first block is b or before it
     while (lo < hi) {
       const int mid = (lo + hi + 1) >> 1;
@@ -248,8 +291,8 @@ __global__ void __launch_bounds__(32 * kWarps) adamw_kernel(const __grid_constan
     c.keep = 1.f - rate * t.decay;
     c.step = rate * inv_bc1;
     const bool full = ((int64_t)block + 1) * kBlock <= t.n && (((uintptr_t)t.p | (uintptr_t)t.grad) & 15) == 0;
-    if (full) update_block<TP, TG, BITS, true>(P, t, block, c, seed_key);
-    else update_block<TP, TG, BITS, false>(P, t, block, c, seed_key);
+    if (full) update_block<TP, TG, BITS, true>(P, t, block, c);
+    else update_block<TP, TG, BITS, false>(P, t, block, c);
   }
 }
 
@@ -267,15 +310,8 @@ __device__ __forceinline__ void values_block(const uint8_t* codes, const uint8_t
                                              uint32_t b) {
   const int lane = threadIdx.x & 31;
   const int64_t e = (int64_t)b * kBlock + 8 * lane;
-  uint8_t c[8];
-  *reinterpret_cast<uint2*>(c) = __ldcg(reinterpret_cast<const uint2*>(codes + e));
-  const float unit = unit_of(__ldcg(scales + b));
   float v[8];
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    v[i] = decode<MANT>(MANT == 3 ? c[i] & 127u : c[i], unit);
-    if (MANT == 3 && c[i] > 127) v[i] = -v[i];
-  }
+  decode<MANT>(__ldcg(reinterpret_cast<const uint2*>(codes + e)), __ldcg(scales + b), v);
   if ((uintptr_t)out % 16) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) any_store(out, type, e + i, v[i]);
@@ -309,7 +345,7 @@ void* pick(int tp, int tg) {
                             : pick<N, BITS, __half>(tg);
 }
 
-int launch(void* f, uint32_t blocks, void* params, void* stream, const char* who) {
+int launch(void* f, uint32_t blocks, int per_sm, void* params, void* stream, const char* who) {
   int sms = 0;
   int rc = polyq_sm_count(&sms);
   if (rc) return rc;
@@ -320,7 +356,7 @@ int launch(void* f, uint32_t blocks, void* params, void* stream, const char* who
   cfg.stream = (cudaStream_t)stream;
   cfg.attrs = at;
   cfg.numAttrs = 1;
-  cfg.gridDim = dim3((unsigned)std::min<int64_t>(((int64_t)blocks + kWarps - 1) / kWarps, (int64_t)sms * 8));
+  cfg.gridDim = dim3((unsigned)std::min<int64_t>(((int64_t)blocks + kWarps - 1) / kWarps, (int64_t)sms * per_sm));
   cfg.blockDim = dim3(32 * kWarps);
   void* args[] = {params};
   cudaError_t ce = cudaLaunchKernelExC(&cfg, f, args);
@@ -364,7 +400,7 @@ int run_step(const polyq_adamw_tensor* tensors, int n, int p_type, int grad_type
     P.n = k;
     P.blocks = (uint32_t)blocks;
     void* f = state->bits == 8 ? pick<N, 8>(p_type, grad_type) : pick<N, 32>(p_type, grad_type);
-    const int rc = launch(f, P.blocks, &P, stream, who);
+    const int rc = launch(f, P.blocks, state->bits == 8 ? kBlocks8 : kBlocks32, &P, stream, who);
     if (rc) return rc;
     i0 += k;
   }
@@ -445,5 +481,5 @@ extern "C" int polyq_adamw_values(const polyq_adamw_state* state, const polyq_de
   P.ms = state->m_scales;
   P.vs = state->v_scales;
   P.blocks = (uint32_t)(state->n / kBlock);
-  return launch((void*)adamw_values_kernel, P.blocks, &P, stream, who);
+  return launch((void*)adamw_values_kernel, P.blocks, 8, &P, stream, who);
 }
