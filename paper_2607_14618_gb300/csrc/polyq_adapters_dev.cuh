@@ -164,8 +164,9 @@ __device__ __forceinline__ bool find_tile(const Segments& s, int bm, int tile, T
   int before = 0;
   for (int s0 = 0; s0 < s.n; s0 += 32) {
     const int i = s0 + lane;
-    int from = 0, to = 0;
+    int from = 0, to = 0, id = -1;
     if (i < s.n) {
+      id = __ldcg(s.ids + i);
       from = min(max(__ldcg(s.offsets + i), 0), s.rows);
       to = min(max(__ldcg(s.offsets + i + 1), 0), s.rows);
     }
@@ -183,7 +184,7 @@ __device__ __forceinline__ bool find_tile(const Segments& s, int bm, int tile, T
       const int row = from + (tile - first) * bm;
       t.row = __shfl_sync(0xFFFFFFFFu, row, src);
       t.rows = min(bm, __shfl_sync(0xFFFFFFFFu, to, src) - t.row);
-      t.id = __ldcg(s.ids + s0 + src);
+      t.id = __shfl_sync(0xFFFFFFFFu, id, src);
       return true;
     }
     before += total;
@@ -294,7 +295,7 @@ struct ShrinkParams {
 template <typename T, int BM, int RN, bool TRANS>
 struct Shrink {
   static constexpr int KC = BM == 16 ? 128 : 64;  // contraction of a stage
-  static constexpr int STAGES = 4;
+  static constexpr int STAGES = BM == 16 && RN == 64 ? 3 : 4;  // (three blocks to an SM)
   // warps along the rows, the rank and the contraction of a stage
   static constexpr int WM = BM == 16 ? 1 : 4, WN = BM == 16 ? RN / 16 : RN == 16 ? 1 : 2, WK = 8 / (WM * WN);
   static constexpr int MT = BM / 16 / WM, NT = RN / 8 / WN;
@@ -316,36 +317,44 @@ __global__ void __launch_bounds__(kThreads) shrink_kernel(const __grid_constant_
   Tile t;
   if (!find_tile(P.seg, BM, blockIdx.x / P.cluster, t)) return;  // the whole cluster
   if (t.id < 0 || t.id >= P.adapters) return;
-  const int own = P.ranks ? min(max(__ldcg(P.ranks + t.id), 0), P.R) : P.R;
+  const int rank_of = P.ranks ? __ldcg(P.ranks + t.id) : P.R;  // (used once the copies of x are under way)
+  const float s = P.scales ? __ldcg(P.scales + t.id) : 1.f;
   const T* x = (const T*)P.x + (int64_t)t.row * P.x_stride;
   const T* w = (const T*)P.w.w + (int64_t)t.id * P.w.next;
   const int64_t chunks = (P.K + KC - 1) / KC;
   const int64_t c0 = chunks * rank / P.cluster, c1 = chunks * (rank + 1) / P.cluster;
 
   Mover<BM, CX> mx(x, P.x_stride, KC, my_piece<CX>());
-  Mover<TRANS ? KC : RN, CW> mw(w, P.w.stride, TRANS ? own : KC, my_piece<CW>());
-  const int64_t x_step = KC * 2, w_step = TRANS ? P.w.stride * KC * 2 : KC * 2;
-  auto copy = [&](int64_t c, int stage) {
-    const uint32_t at = base + stage * (S::X_BYTES + S::W_BYTES);
+  auto copy_x = [&](int64_t c, int stage) {
     const int left = (int)min(P.K - c * KC, (int64_t)KC);
-    if (left < KC) {  // the contraction's end
-      mx.limit(left);
-      if (!TRANS) mw.limit(left);
-    }
-    mx.copy(at, c * x_step, t.rows);
-    mw.copy(at + S::X_BYTES, c * w_step, TRANS ? left : own);
+    if (left < KC) mx.limit(left);  // the contraction's end
+    mx.copy(base + stage * (S::X_BYTES + S::W_BYTES), c * (KC * 2), t.rows);
+  };
+  for (int i = 0; i < S::STAGES - 1; ++i)
+    if (c0 + i < c1) copy_x(c0 + i, i);
+  const int own = min(max(rank_of, 0), P.R);
+  Mover<TRANS ? KC : RN, CW> mw(w, P.w.stride, TRANS ? own : KC, my_piece<CW>());
+  auto copy_w = [&](int64_t c, int stage) {
+    const int left = (int)min(P.K - c * KC, (int64_t)KC);
+    if (!TRANS && left < KC) mw.limit(left);
+    mw.copy(base + stage * (S::X_BYTES + S::W_BYTES) + S::X_BYTES, c * (TRANS ? P.w.stride * KC * 2 : KC * 2),
+            TRANS ? left : own);
   };
   float acc[S::MT][S::NT][4] = {};
   const int wm = warp % S::WM, wn = warp / S::WM % S::WN, wk = warp / (S::WM * S::WN);
   for (int i = 0; i < S::STAGES - 1; ++i) {
-    if (c0 + i < c1) copy(c0 + i, i);
-    cp_commit();
+    if (c0 + i < c1) copy_w(c0 + i, i);
+    cp_commit();  // (the first with all that x has asked for)
   }
   int stage = 0;
   for (int64_t c = c0; c < c1; ++c) {
     cp_wait<S::STAGES - 2>();
     __syncthreads();
-    if (c + S::STAGES - 1 < c1) copy(c + S::STAGES - 1, stage == 0 ? S::STAGES - 1 : stage - 1);
+    if (c + S::STAGES - 1 < c1) {
+      const int there = stage == 0 ? S::STAGES - 1 : stage - 1;
+      copy_x(c + S::STAGES - 1, there);
+      copy_w(c + S::STAGES - 1, there);
+    }
     cp_commit();
     const uint32_t at = base + stage * (S::X_BYTES + S::W_BYTES);
     if (++stage == S::STAGES) stage = 0;
@@ -379,7 +388,6 @@ __global__ void __launch_bounds__(kThreads) shrink_kernel(const __grid_constant_
     }
   if (P.cluster > 1) cluster_sync();
   else __syncthreads();
-  const float s = P.scales ? __ldcg(P.scales + t.id) : 1.f;
   const int part = BM * RN / P.cluster;
   for (int i = rank * part + threadIdx.x; i < (rank + 1) * part; i += kThreads) {
     const int row = i / RN, col = i % RN;
@@ -472,27 +480,34 @@ __device__ __forceinline__ void expand_tile(const ExpandParams& P, const Tile& t
       copy_rows<TY, VEC>(P.res ? res + n0 : nullptr, P.res_stride, y + n0, P.y_stride, t.rows, min(E::BN, N - n0));
     return;
   }
-  const int own = P.ranks ? min(max(__ldcg(P.ranks + t.id), 0), P.R) : P.R;
+  const int rank_of = P.ranks ? __ldcg(P.ranks + t.id) : P.R;  // (used once the residuals are under way)
+  float s0 = P.scales ? __ldcg(P.scales + t.id) : 1.f, s1;
   const T* w = (const T*)P.w.w + (int64_t)t.id * P.w.next;
-  Mover<TRANS ? RN : E::BN, CW> mw(w, P.w.stride, TRANS ? E::BN : own, my_piece<CW>());
   Mover<BM, CY, (int)sizeof(TY)> mr(P.res ? res : y, P.res_stride, E::BN,
                                     out_piece<TY, CY>(threadIdx.x / CY, threadIdx.x % CY));
-  auto ask = [&](int tile, int stage) {
-    if (tile < tiles) {
-      const int left = min(N - tile * E::BN, E::BN);
-      const uint32_t at = ring + stage * (E::W_BYTES + E::Y_BYTES);
-      if (left < E::BN) {  // the columns' end
-        if (TRANS) mw.limit(left);
-        mr.limit(left);
-      }
-      mw.copy(at, (int64_t)tile * E::BN * 2 * (TRANS ? 1 : P.w.stride), TRANS ? own : left);
-      if (VEC && P.res) mr.copy(at + E::W_BYTES, (int64_t)tile * E::BN * (int)sizeof(TY), t.rows);
-    }
-    cp_commit();
+  auto ask_res = [&](int tile, int stage) {
+    if (!VEC || !P.res || tile >= tiles) return;
+    const int left = N - tile * E::BN;
+    if (left < E::BN) mr.limit(left);  // the columns' end
+    mr.copy(ring + stage * (E::W_BYTES + E::Y_BYTES) + E::W_BYTES, (int64_t)tile * E::BN * (int)sizeof(TY), t.rows);
   };
   int tile = blockIdx.x;
 #pragma unroll
-  for (int i = 0; i < E::STAGES - 1; ++i) ask(tile + i * G, i);
+  for (int i = 0; i < E::STAGES - 1; ++i) ask_res(tile + i * G, i);
+  const int own = min(max(rank_of, 0), P.R);
+  Mover<TRANS ? RN : E::BN, CW> mw(w, P.w.stride, TRANS ? E::BN : own, my_piece<CW>());
+  auto ask_w = [&](int tile, int stage) {
+    if (tile >= tiles) return;
+    const int left = min(N - tile * E::BN, E::BN);
+    if (TRANS && left < E::BN) mw.limit(left);
+    mw.copy(ring + stage * (E::W_BYTES + E::Y_BYTES), (int64_t)tile * E::BN * 2 * (TRANS ? 1 : P.w.stride),
+            TRANS ? own : left);
+  };
+#pragma unroll
+  for (int i = 0; i < E::STAGES - 1; ++i) {
+    ask_w(tile + i * G, i);
+    cp_commit();  // (the first with all residuals that have been asked for)
+  }
   if (first) pdl_wait();  // v comes from the launch before
 #pragma unroll
   for (int i0 = 0; i0 < BM * CV; i0 += kThreads) {
@@ -522,12 +537,15 @@ __device__ __forceinline__ void expand_tile(const ExpandParams& P, const Tile& t
     frag_a<CV, false>(base, wm * 16, k * 16, h[k]);
     frag_a<CV, false>(base + E::V_BYTES, wm * 16, k * 16, l[k]);
   }
-  float s0 = P.scales ? __ldcg(P.scales + t.id) : 1.f, s1 = s0;
+  s1 = s0;
   if constexpr (std::is_same<T, __half>::value) s0 *= row_scale[r0], s1 *= row_scale[r0 + 8];
   for (int stage = 0; tile < tiles; tile += G) {
     cp_wait<E::STAGES - 2>();
     __syncthreads();
-    ask(tile + (E::STAGES - 1) * G, stage == 0 ? E::STAGES - 1 : stage - 1);
+    const int there = stage == 0 ? E::STAGES - 1 : stage - 1;
+    ask_res(tile + (E::STAGES - 1) * G, there);
+    ask_w(tile + (E::STAGES - 1) * G, there);
+    cp_commit();
     const uint32_t at = ring + stage * (E::W_BYTES + E::Y_BYTES);
     uint8_t* out = smem + (at - base) + E::W_BYTES;
     float acc[E::NT][4] = {};
@@ -595,7 +613,7 @@ __device__ __forceinline__ void expand_tile(const ExpandParams& P, const Tile& t
 }
 
 template <typename T, int BM, int RN, bool TRANS, typename TY>
-__global__ void __launch_bounds__(kThreads, 2) expand_kernel(const __grid_constant__ ExpandParams P) {
+__global__ void __launch_bounds__(kThreads, BM == 16 && RN <= 64 ? 3 : 2) expand_kernel(const __grid_constant__ ExpandParams P) {
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ float row_scale[BM];
   bool first = true;
