@@ -73,7 +73,7 @@ int shrink(const polyq_dense* x, int64_t T, int64_t K, const polyq_adapters* ad,
   const int bm = mean <= 32 ? 16 : rn >= 64 && mean >= 256 ? 128 : 64;
   const bool half = ad->type == POLYQ_F16;
   const Kernel k = half ? lora::shrink_of<__half>(bm, rn, trans) : lora::shrink_of<__nv_bfloat16>(bm, rn, trans);
-  const int64_t tiles = most_tiles(T, seg.n, bm), stages = K / (bm == 16 ? 128 : 64);
+  const int64_t tiles = most_tiles(T, seg.n, bm), stages = K / (bm == 128 ? 64 : 128);
   int cluster = 1;
   while (cluster < lora::kMaxCluster && tiles * cluster < 2 * sms && stages >= 4 * cluster) cluster *= 2;
   lora::ShrinkParams P;
@@ -118,9 +118,13 @@ int expand(const float* v, int64_t T, int64_t N, const polyq_adapters* ad, bool 
   P.vec = (uintptr_t)y->data % 16 == 0 && y->stride * eb % 16 == 0 &&
           (!residual || ((uintptr_t)residual->data % 16 == 0 && residual->stride * eb % 16 == 0));
   const int which = 128 + (((half * 2 + trans) * 4 + rank_index(rn)) * 2 + (bm == 64)) * 2 + f32;
-  // Blocks for two rounds of the SMs (two to an SM, more of few rows), each with several column tiles.
-  const int64_t columns = (N + bn - 1) / bn, share = std::max<int64_t>(1, (int64_t)sms * (bm == 16 ? 3 : 4) / P.tiles);
-  return launch(k, which, dim3((unsigned)std::min(columns, share), (unsigned)std::min(P.tiles, 65535)), 1, &P, stream, who);
+  // Blocks of a row tile: two rounds of the SMs' blocks, one where rows are few.  (Tiles: one for
+  // each segment at least, and half a tile more than full ones.)  4096 x 13824, rank 64: 67 us with 8, 60 with
+  // 9; 6007 x 5120, rank 32: 46 us with 3, 31 with 5; 48 rows of rank 64: 21 us with 9, 23 with 16.
+  const int64_t columns = (N + bn - 1) / bn, slots = (int64_t)sms * (bm != 16 ? 4 : rn <= 64 ? 3 : 2);
+  const int64_t rows = std::min<int64_t>(P.tiles, std::max<int64_t>(seg.n, (T + bm - 1) / bm + seg.n / 2));
+  const int64_t share = std::min(columns, std::max<int64_t>(1, slots / rows));
+  return launch(k, which, dim3((unsigned)share, (unsigned)std::min(P.tiles, 65535)), 1, &P, stream, who);
 }
 
 bool rows_on_16(const polyq_dense* d) { return (uintptr_t)d->data % 16 == 0 && d->stride % 8 == 0; }

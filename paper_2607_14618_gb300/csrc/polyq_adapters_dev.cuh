@@ -236,17 +236,38 @@ struct AdapterTiles {
 
 // ---- v as two 16-bit numbers ----
 template <typename T>
+__device__ __forceinline__ uint32_t pack2(float a, float b) {  // a in the lower half
+  uint32_t r;
+  if constexpr (std::is_same<T, __half>::value) asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(b), "f"(a));
+  else asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(b), "f"(a));
+  return r;
+}
+template <typename T>
+__device__ __forceinline__ float2 unpack2(uint32_t w) {
+  if constexpr (std::is_same<T, __half>::value) return __half22float2(*reinterpret_cast<const __half2*>(&w));
+  return make_float2(bf16_lo(w), bf16_hi(w));
+}
+template <typename T>
 __device__ __forceinline__ void split8(const float (&v)[8], float scale, uint4& h, uint4& l) {
-  alignas(16) T eh[8], el[8];
+  constexpr uint32_t INF = std::is_same<T, __half>::value ? 0x7C00u : 0x7F80u;
+  uint32_t eh[4], el[4], top = 0;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const float x = v[i] * scale;
-    eh[i] = Elem<T>::from(x);
-    const float f = Elem<T>::to(eh[i]);
-    el[i] = Elem<T>::from(fabsf(f) < INFINITY ? x - f : 0.f);  // (what is not finite is so once)
+  for (int i = 0; i < 4; ++i) {
+    const float a = v[2 * i] * scale, b = v[2 * i + 1] * scale;
+    eh[i] = pack2<T>(a, b);
+    const float2 f = unpack2<T>(eh[i]);
+    el[i] = pack2<T>(a - f.x, b - f.y);
+    top = __vmaxu2(top, eh[i] & 0x7FFF7FFFu);
   }
-  h = *reinterpret_cast<const uint4*>(eh);
-  l = *reinterpret_cast<const uint4*>(el);
+  if (max(top & 0xFFFFu, top >> 16) >= INF) {  // what is not finite is so once
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if ((eh[i] & 0x7FFFu) >= INF) el[i] &= 0xFFFF0000u;
+      if ((eh[i] >> 16 & 0x7FFFu) >= INF) el[i] &= 0xFFFFu;
+    }
+  }
+  h = make_uint4(eh[0], eh[1], eh[2], eh[3]);
+  l = make_uint4(el[0], el[1], el[2], el[3]);
 }
 // 2^e and 2^-e that bring the largest magnitude (its bits) to 2^14 .. 2^15, both normal numbers.
 __device__ __forceinline__ uint32_t scale_bits(uint32_t top) {
@@ -294,8 +315,8 @@ struct ShrinkParams {
 // order.
 template <typename T, int BM, int RN, bool TRANS>
 struct Shrink {
-  static constexpr int KC = BM == 16 ? 128 : 64;  // contraction of a stage
-  static constexpr int STAGES = BM == 16 && RN == 64 ? 3 : 4;  // (three blocks to an SM)
+  static constexpr int KC = BM == 128 ? 64 : 128;  // contraction of a stage
+  static constexpr int STAGES = BM == 128 || (BM == 16 && RN != 64) ? 4 : 3;  // (three blocks to an SM for few rows)
   // warps along the rows, the rank and the contraction of a stage
   static constexpr int WM = BM == 16 ? 1 : 4, WN = BM == 16 ? RN / 16 : RN == 16 ? 1 : 2, WK = 8 / (WM * WN);
   static constexpr int MT = BM / 16 / WM, NT = RN / 8 / WN;
@@ -358,6 +379,7 @@ __global__ void __launch_bounds__(kThreads) shrink_kernel(const __grid_constant_
     cp_commit();
     const uint32_t at = base + stage * (S::X_BYTES + S::W_BYTES);
     if (++stage == S::STAGES) stage = 0;
+    float sum[S::MT][S::NT][4] = {};  // of the stage: the tensor cores cut running sums off
 #pragma unroll
     for (int k = wk * 16; k < KC; k += 16 * S::WK) {
       uint32_t a[S::MT][4];
@@ -369,11 +391,17 @@ __global__ void __launch_bounds__(kThreads) shrink_kernel(const __grid_constant_
         frag_b<CW, TRANS>(at + S::X_BYTES, (wn * S::NT + j) * 8, k, b);
 #pragma unroll
         for (int i = 0; i < S::MT; ++i) {
-          mma<T>(acc[i][j], a[i], b[0], b[1]);
-          mma<T>(acc[i][j + 1], a[i], b[2], b[3]);
+          mma<T>(sum[i][j], a[i], b[0], b[1]);
+          mma<T>(sum[i][j + 1], a[i], b[2], b[3]);
         }
       }
     }
+#pragma unroll
+    for (int i = 0; i < S::MT; ++i)
+#pragma unroll
+      for (int j = 0; j < S::NT; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[i][j][e] += sum[i][j][e];
   }
   cp_wait<0>();
   __syncthreads();
@@ -655,24 +683,26 @@ struct Grad {
   static constexpr int BC = RN <= 64 ? 128 : 64;   // columns of a block
   static constexpr int WR = RN <= 32 ? 1 : RN / 32, WC = 8 / WR;
   static constexpr int MT = RN / 16 / WR, NT = BC / 8 / WC;
-  static constexpr int STAGES = 3;
-  static constexpr int X_BYTES = BT * BC * 2, V_BYTES = BT * RN * 2;
+  static constexpr int STAGES = RN <= 64 ? 3 : 2;  // (two blocks to an SM)
+  static constexpr int X_BYTES = BT * BC * 2, F_BYTES = BT * RN * 4, V_BYTES = BT * RN * 2;
   static constexpr int PITCH = BC + 1;
   static constexpr int RED_BYTES = RN * PITCH * 4;
-  static constexpr int MAIN = STAGES * X_BYTES + 2 * V_BYTES;
+  static constexpr int MAIN = STAGES * (X_BYTES + F_BYTES) + 2 * V_BYTES;
   static constexpr int SMEM = MAIN > RED_BYTES ? MAIN : RED_BYTES;
 };
 
+// The sums of 128 rows (fp16: of a stage's 64, which have a scale of their own) start anew and are
+// added to the block's in fp32: the tensor cores cut their running sums off, and over thousands of
+// rows that adds up (4096 rows of two adapters: 5e-6 off without it, 2.4e-6 with it).
 template <typename T, int RN>
-__global__ void __launch_bounds__(kThreads) gradients_kernel(const __grid_constant__ GradParams P) {
+__global__ void __launch_bounds__(kThreads, 2) gradients_kernel(const __grid_constant__ GradParams P) {
   using G = Grad<T, RN>;
-  constexpr int CX = G::BC / 8, CV = RN / 8, BT = G::BT;
-  constexpr int VG = (BT * CV + kThreads - 1) / kThreads;  // groups of eight v of a thread
+  constexpr int CX = G::BC / 8, CV = RN / 8, CF = RN / 4, BT = G::BT;
   constexpr bool SCALED = std::is_same<T, __half>::value;
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ uint32_t tops[8];
-  const uint32_t base = smem_u32(smem), vt = base + G::STAGES * G::X_BYTES;
-  uint8_t* vs = smem + G::STAGES * G::X_BYTES;
+  const uint32_t base = smem_u32(smem), vt = base + G::STAGES * (G::X_BYTES + G::F_BYTES);
+  uint8_t* vs = smem + G::STAGES * (G::X_BYTES + G::F_BYTES);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int rank = P.cluster > 1 ? (int)cluster_rank() : 0;
   const int per = P.side[0].tiles + P.side[1].tiles, block = blockIdx.x / P.cluster;
@@ -681,39 +711,48 @@ __global__ void __launch_bounds__(kThreads) gradients_kernel(const __grid_consta
   const int64_t n0 = (int64_t)(block % per - (which ? P.side[0].tiles : 0)) * G::BC;
   pdl_wait();
   pdl_trigger();
-  const int own = P.ranks ? min(max(__ldcg(P.ranks + id), 0), P.R) : P.R;
-  AdapterTiles ahead, now;
+  const int rank_of = P.ranks ? __ldcg(P.ranks + id) : P.R;
+  const float s = D.scales ? __ldcg(D.scales + id) : 1.f;
+  AdapterTiles ahead;
   ahead.begin(rank);
-  now.begin(rank);
   const Mover<BT, CX> mx((const T*)D.x + n0, D.x_stride, (int)min(D.C - n0, (int64_t)G::BC), my_piece<CX>());
+  const Mover<BT, CF, 4> mv(D.v, P.R, P.R, threadIdx.x * 16u);  // (rows as they lie)
+  int asked = 0;  // stages that have been asked for
+  bool any = true;
   auto copy = [&](int stage) {
     int row, rows;
-    if (ahead.next(P.seg, id, BT, P.cluster, row, rows))
-      mx.copy(base + stage * G::X_BYTES, (int64_t)row * D.x_stride * 2, rows);
+    any = any && ahead.next(P.seg, id, BT, P.cluster, row, rows);
+    if (any) {
+      const uint32_t at = base + stage * (G::X_BYTES + G::F_BYTES);
+      mx.copy(at, (int64_t)row * D.x_stride * 2, rows);
+      mv.copy(at + G::X_BYTES, (int64_t)row * P.R * 4, rows);
+      ++asked;
+    }
     cp_commit();
   };
-  float v[VG][8];
-  auto load_v = [&]() {
-    int row, rows;
-    if (!now.next(P.seg, id, BT, P.cluster, row, rows)) return false;
-#pragma unroll
-    for (int i = 0; i < VG; ++i) {
-      const int g = i * kThreads + threadIdx.x, r = g / CV, c = g % CV;
-      load_v8(D.v + (int64_t)(row + r) * P.R + 8 * c, r < rows && 8 * c < P.R, v[i]);
-    }
-    return true;
-  };
-  float acc[G::MT][G::NT][4] = {};
+  float acc[G::MT][G::NT][4] = {}, part[G::MT][G::NT][4] = {};
   const int wr = warp % G::WR, wc = warp / G::WR;
 #pragma unroll
   for (int i = 0; i < G::STAGES - 1; ++i) copy(i);
-  bool more = load_v();
-  for (int stage = 0; more; stage = (stage + 1) % G::STAGES) {
+  for (int done = 0, stage = 0; done < asked; ++done) {
+    cp_wait<G::STAGES - 2>();
+    __syncthreads();  // the stage is here, and the one before has been read
+    copy(stage == 0 ? G::STAGES - 1 : stage - 1);
+    const uint32_t at = base + stage * (G::X_BYTES + G::F_BYTES);
+    const uint8_t* f = smem + (at - base) + G::X_BYTES;
+    auto v8 = [&](int g, float(&v)[8]) {
+      const float4 a = reinterpret_cast<const float4*>(f)[2 * g], b = reinterpret_cast<const float4*>(f)[2 * g + 1];
+      v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
+    };
     float down = 1.f, up = 1.f;
     if constexpr (SCALED) {
       uint32_t top = 0;
 #pragma unroll
-      for (int i = 0; i < VG; ++i) top = max(top, abs_bits(v[i]));
+      for (int g = threadIdx.x; g < BT * CV; g += kThreads) {
+        float v[8];
+        v8(g, v);
+        top = max(top, abs_bits(v));
+      }
       top = __reduce_max_sync(0xFFFFFFFFu, top);
       if (lane == 0) tops[warp] = top;
       __syncthreads();
@@ -722,20 +761,15 @@ __global__ void __launch_bounds__(kThreads) gradients_kernel(const __grid_consta
       up = scale_up(top);
     }
 #pragma unroll
-    for (int i = 0; i < VG; ++i) {
-      const int g = i * kThreads + threadIdx.x;
-      if (BT * CV % kThreads && g >= BT * CV) break;
+    for (int g = threadIdx.x; g < BT * CV; g += kThreads) {
+      float v[8];
       uint4 h, l;
-      split8<T>(v[i], down, h, l);
+      v8(g, v);
+      split8<T>(v, down, h, l);
       *reinterpret_cast<uint4*>(vs + piece<CV>(g / CV, g % CV)) = h;
       *reinterpret_cast<uint4*>(vs + G::V_BYTES + piece<CV>(g / CV, g % CV)) = l;
     }
-    more = load_v();
-    cp_wait<G::STAGES - 2>();
     __syncthreads();
-    copy((stage + G::STAGES - 1) % G::STAGES);
-    const uint32_t at = base + stage * G::X_BYTES;
-    float part[SCALED ? G::MT : 1][SCALED ? G::NT : 1][4] = {};
 #pragma unroll
     for (int k = 0; k < BT; k += 16) {
       uint32_t h[G::MT][4], l[G::MT][4];
@@ -749,25 +783,29 @@ __global__ void __launch_bounds__(kThreads) gradients_kernel(const __grid_consta
         uint32_t b[4];
         frag_b<CX, true>(at, (wc * G::NT + j) * 8, k, b);
 #pragma unroll
-        for (int i = 0; i < G::MT; ++i)
+        for (int q = 0; q < 2; ++q)
 #pragma unroll
-          for (int q = 0; q < 2; ++q) {
-            float(&d)[4] = SCALED ? part[SCALED ? i : 0][SCALED ? j + q : 0] : acc[i][j + q];
-            mma<T>(d, l[i], b[2 * q], b[2 * q + 1]);
-            mma<T>(d, h[i], b[2 * q], b[2 * q + 1]);
-          }
+          for (int i = 0; i < G::MT; ++i) mma<T>(part[i][j + q], l[i], b[2 * q], b[2 * q + 1]);
+#pragma unroll
+        for (int q = 0; q < 2; ++q)
+#pragma unroll
+          for (int i = 0; i < G::MT; ++i) mma<T>(part[i][j + q], h[i], b[2 * q], b[2 * q + 1]);
       }
     }
-    if constexpr (SCALED) {
+    if (SCALED || (done & 1) || done + 1 == asked) {  // (asked counts this stage's successors by now)
 #pragma unroll
       for (int i = 0; i < G::MT; ++i)
 #pragma unroll
         for (int j = 0; j < G::NT; ++j)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) acc[i][j][e] = fmaf(part[i][j][e], up, acc[i][j][e]);
+          for (int e = 0; e < 4; ++e) {
+            acc[i][j][e] = fmaf(part[i][j][e], up, acc[i][j][e]);
+            part[i][j][e] = 0.f;
+          }
     }
-    __syncthreads();  // v has been read
+    if (++stage == G::STAGES) stage = 0;
   }
+  const int own = min(max(rank_of, 0), P.R);
   cp_wait<0>();
   __syncthreads();
   float* red = reinterpret_cast<float*>(smem);
@@ -783,9 +821,8 @@ __global__ void __launch_bounds__(kThreads) gradients_kernel(const __grid_consta
     }
   if (P.cluster > 1) cluster_sync();
   else __syncthreads();
-  const float s = D.scales ? __ldcg(D.scales + id) : 1.f;
-  const int part = RN * G::BC / P.cluster;
-  for (int i = rank * part + threadIdx.x; i < (rank + 1) * part; i += kThreads) {
+  const int share = RN * G::BC / P.cluster;
+  for (int i = rank * share + threadIdx.x; i < (rank + 1) * share; i += kThreads) {
     const int j = D.by_column ? i % RN : i / G::BC, c = D.by_column ? i / RN : i % G::BC;
     if (j >= P.R || n0 + c >= D.C) continue;
     float sum = 0.f;
