@@ -1131,13 +1131,35 @@ def _vector(t, name, K, dev):
     if t is None:
         return None
     try:
-        ty = _type_of(t.dtype)
-        good = ty is not None and t.get_device() == dev and t.shape == (K,) and t.is_contiguous()
-    except AttributeError:
+        ty = _T.get(t.dtype)
+        if ty is None:
+            ty = _type_of(t.dtype)
+        n, = t.shape
+        good = ty is not None and n == K and t.get_device() == dev and t.is_contiguous()
+    except (AttributeError, ValueError):
         good = False
     if not good:
         raise ValueError(f"{name} must be a contiguous fp32, bf16 or fp16 tensor [{K}] on cuda:{dev}")
     return C.byref(Dense(t.data_ptr(), K, ty))
+
+
+T_I32, T_I64 = 3, 4  # (of this binding's checks only)
+_dtypes = []  # torch dtypes by T_*, filled by the first use
+
+
+def _plain(t, name, ty, shape, dev):
+    """The address of a contiguous tensor of that type (T_*) and shape on CUDA device `dev`."""
+    if not _dtypes:
+        import torch
+        _dtypes[:] = (torch.float32, torch.bfloat16, torch.float16, torch.int32, torch.int64)
+    try:
+        good = (t.dtype == _dtypes[ty] and t.shape == shape and t.get_device() == dev and t.is_contiguous())
+    except AttributeError:
+        good = False
+    if not good:
+        what = ("fp32", "bf16", "fp16", "int32", "int64")[ty]
+        raise ValueError(f"{name} must be a contiguous {what} tensor {list(shape)} on cuda:{dev}")
+    return t.data_ptr()
 
 
 def layernorm_stats(rows, device="cuda"):
@@ -1148,11 +1170,7 @@ def layernorm_stats(rows, device="cuda"):
 
 
 def _stats(stats, rows, dev):
-    import torch
-    if (not isinstance(stats, torch.Tensor) or stats.dtype != torch.float32 or stats.get_device() != dev
-            or stats.shape != (rows, 2) or not stats.is_contiguous()):
-        raise ValueError(f"stats must be layernorm_stats({rows}) on cuda:{dev}")
-    return stats.data_ptr()
+    return _plain(stats, "stats (layernorm_stats)", T_F32, (rows, 2), dev)
 
 
 def layernorm_workspace(rows, K, device="cuda"):
@@ -1196,14 +1214,15 @@ def layernorm_backward(x, weight, stats, dy, center=True, dx=None, dweight=None,
     st = _stream_on(dev, "x", stream)
     rows, K = x.shape
     idy = _dense(dy, "dy", rows, K, dev)
-    import torch
-    vt = torch.float32 if weight is None else weight.dtype
-    if dx is None and need_dx:
-        dx = _made(stream, torch.empty, (rows, K), dtype=x.dtype, device=x.device)
-    if dweight is None and need_weight:
-        dweight = _made(stream, torch.empty, K, dtype=vt, device=x.device)
-    if dbias is None and need_bias:
-        dbias = _made(stream, torch.empty, K, dtype=vt, device=x.device)
+    if (dx is None and need_dx) or (dweight is None and need_weight) or (dbias is None and need_bias):
+        import torch
+        vt = torch.float32 if weight is None else weight.dtype
+        if dx is None and need_dx:
+            dx = _made(stream, torch.empty, (rows, K), dtype=x.dtype, device=x.device)
+        if dweight is None and need_weight:
+            dweight = _made(stream, torch.empty, K, dtype=vt, device=x.device)
+        if dbias is None and need_bias:
+            dbias = _made(stream, torch.empty, K, dtype=vt, device=x.device)
     odx = None if dx is None else C.byref(_dense(dx, "dx", rows, K, dev, x.dtype))
     if residual is not None and dx is None:
         raise ValueError("a residual is added to dx, which is not wanted")
@@ -1224,7 +1243,8 @@ class AdamState:
     in which tensor i begins at `offsets[i]`.  bits=32: fp32.  bits=8: uint8 codes,
     `v` those of the second moment's root, with a scale byte per 256 elements in
     `m_scales` and `v_scales` (the formats of polyq_finetune.h).  The buffers are
-    what a checkpoint holds."""
+    what a checkpoint holds; their contents may be set, the fields are fixed, as the
+    descriptor that the calls take holds them."""
 
     def __init__(self, sizes, bits=32, device="cuda"):
         import torch
@@ -1241,40 +1261,29 @@ class AdamState:
         def new(n):
             return torch.zeros(n, dtype=torch.uint8 if bits == 8 else torch.float32, device=device)
 
-        self.sizes, self.offsets, self.bits = tuple(sizes), tuple(offsets), bits
-        self.m, self.v = new(at), new(at)
-        self.m_scales, self.v_scales = (new(at // ADAMW_BLOCK), new(at // ADAMW_BLOCK)) \
-            if bits == 8 else (None, None)
+        m, v = new(at), new(at)
+        ms, vs = (new(at // ADAMW_BLOCK), new(at // ADAMW_BLOCK)) if bits == 8 else (None, None)
+        self.__dict__.update(
+            sizes=tuple(sizes), offsets=tuple(offsets), bits=bits, m=m, v=v, m_scales=ms, v_scales=vs,
+            device_index=m.get_device(),
+            desc=AdamwState(m.data_ptr(), v.data_ptr(), None if ms is None else ms.data_ptr(),
+                            None if vs is None else vs.data_ptr(), at, bits))
 
-    def _desc(self, dev=None):
-        n = self.offsets[-1] + -(-self.sizes[-1] // ADAMW_BLOCK) * ADAMW_BLOCK
-        import torch
-        ty = torch.uint8 if self.bits == 8 else torch.float32
-        at = self.m.get_device() if dev is None else dev
-        for name, wide in (("m", n), ("v", n), ("m_scales", n // ADAMW_BLOCK),
-                           ("v_scales", n // ADAMW_BLOCK)):
-            t = getattr(self, name)
-            if self.bits == 32 and t is None:
-                continue
-            if (not isinstance(t, torch.Tensor) or t.dtype != ty or t.get_device() != at or at < 0
-                    or t.shape != (wide,) or not t.is_contiguous()):
-                raise ValueError(f"the state's {name} must be a contiguous {ty} tensor [{wide}] "
-                                 f"on {'a CUDA device' if at < 0 else f'cuda:{at}'}")
-        return AdamwState(self.m.data_ptr(), self.v.data_ptr(),
-                          self.m_scales.data_ptr() if self.bits == 8 else None,
-                          self.v_scales.data_ptr() if self.bits == 8 else None, n, self.bits)
+    def __setattr__(self, name, value):
+        raise AttributeError(f"{name}: an AdamState's fields are fixed; copy into its buffers")
 
     def values(self, m=None, root=None, dtype=None, stream=None):
         """What an 8-bit state's codes stand for: (m, root of v), flat like the codes,
         bf16 by default (which holds them exactly), fp32 or fp16."""
-        import torch
-        d = self._desc()
-        dev = self.m.get_device()
+        d, dev = self.desc, self.device_index
+        if dev < 0:
+            raise ValueError("the state must be on a CUDA device")
         st = _stream_on(dev, "the state", stream)
-        if m is None:
-            m = _made(stream, torch.empty, d.n, dtype=dtype or torch.bfloat16, device=self.m.device)
-        if root is None:
-            root = _made(stream, torch.empty, d.n, dtype=dtype or torch.bfloat16, device=self.m.device)
+        if m is None or root is None:
+            import torch
+            m, root = (t if t is not None else
+                       _made(stream, torch.empty, d.n, dtype=dtype or torch.bfloat16, device=self.m.device)
+                       for t in (m, root))
         _check(_lib.polyq_adamw_values(C.byref(d), _vector(m, "m", d.n, dev),
                                        _vector(root, "root", d.n, dev), st))
         return m, root
@@ -1322,16 +1331,13 @@ class AdamW:
                 params[i].data_ptr(), grads[i].data_ptr(),
                 None if copies[i] is None else copies[i].data_ptr(), state.sizes[i],
                 state.offsets[i], decay[i], rate[i]))
-        state._desc(dev)
-        self._groups = [(k, (AdamwTensor * len(v))(*v), len(v)) for k, v in groups.items()]
+        if state.device_index != dev:
+            raise ValueError(f"the state is not on cuda:{dev}, the device of params[0]")
+        self._state_ref = C.byref(state.desc)
+        self._groups = [(*k, (AdamwTensor * len(v))(*v), len(v)) for k, v in groups.items()]
 
     def _scalar(self, t, name, dtype):
-        import torch
-        if (not isinstance(t, torch.Tensor) or t.dtype != dtype or t.numel() != 1
-                or t.get_device() != self._dev):
-            raise ValueError(f"{name} must be a number or a {dtype} tensor of one element on "
-                             f"cuda:{self._dev}")
-        return t.data_ptr()
+        return _plain(t.reshape(()) if hasattr(t, "numel") and t.numel() == 1 else t, name, dtype, (), self._dev)
 
     def step(self, lr, step, betas=(0.9, 0.999), eps=1e-8, seed=0, grad_scale=None, stream=None):
         """One step.  `step` counts from 1.  lr and step may be tensors of one element on
@@ -1340,24 +1346,19 @@ class AdamW:
         all gradients, an fp32 tensor of one element; where it is not finite the step
         leaves everything as it was.  seed: of the rounding of 8-bit states, another one
         for each step."""
-        h = AdamwHyper(beta1=betas[0], beta2=betas[1], eps=eps, seed=seed & 0xFFFFFFFFFFFFFFFF, step=1)
         st = _stream_on(self._dev, "the tensors", stream)
-        if isinstance(lr, (int, float)):
-            h.lr = lr
-        else:
-            import torch
-            h.lr_dev = self._scalar(lr, "lr", torch.float32)
-        if isinstance(step, int):
-            h.step = step
-        else:
-            import torch
-            h.step_dev = self._scalar(step, "step", torch.int64)
+        lr_dev = step_dev = scale = None
+        if not isinstance(lr, (int, float)):
+            lr_dev, lr = self._scalar(lr, "lr", T_F32), 0.0
+        if not isinstance(step, int):
+            step_dev, step = self._scalar(step, "step", T_I64), 1
         if grad_scale is not None:
-            import torch
-            h.grad_scale = self._scalar(grad_scale, "grad_scale", torch.float32)
-        d = self.state._desc(self._dev)
-        for (tp, tg, tc), tensors, n in self._groups:
-            _check(_lib.polyq_adamw_step(tensors, n, tp, tg, tc, C.byref(d), C.byref(h), st))
+            scale = self._scalar(grad_scale, "grad_scale", T_F32)
+        h = C.byref(AdamwHyper(lr, betas[0], betas[1], eps, step, seed & 0xFFFFFFFFFFFFFFFF, lr_dev, step_dev,
+                               scale))
+        for tp, tg, tc, tensors, n in self._groups:
+            _check(_lib.polyq_adamw_step(tensors, n, tp, tg, tc, self._state_ref, h, st))
+
 
 
 def adapters_workspace(T, R, device="cuda"):
@@ -1375,28 +1376,18 @@ def adapters_saved(T, R, device="cuda"):
     return torch.empty((T, R), dtype=torch.float32, device=device)
 
 
-def _plain(t, name, dtype, shape, dev):
-    """The address of a contiguous tensor of that type and shape on CUDA device `dev`."""
-    try:
-        good = (t.dtype == dtype and t.shape == shape and t.get_device() == dev and t.is_contiguous())
-    except AttributeError:
-        good = False
-    if not good:
-        raise ValueError(f"{name} must be a contiguous {dtype} tensor {list(shape)} on cuda:{dev}")
-    return t.data_ptr()
-
-
 def _adapters(x, a, b, offsets, ids, scales, ranks, dev):
     """Descriptors of the adapters a [n][R][K] and b [n][N][R] and of the segments."""
-    import torch
     K = x.shape[1]
     try:
+        ty = _type_of(x.dtype)
         n, R, ka = a.shape
         nb, N, rb = b.shape
-        (an, ar, a1), (bn, br, b1) = a.stride(), b.stride()
-        good = (a.dtype == b.dtype == x.dtype and a.get_device() == b.get_device() == dev
-                and (nb, rb, ka) == (n, R, K) and (a1 == 1 or K == 1) and (b1 == 1 or R == 1)
-                and x.dtype in (torch.bfloat16, torch.float16))
+        an, ar, a1 = a.stride()
+        bn, br, b1 = b.stride()
+        good = (a.dtype == b.dtype == x.dtype and a.get_device() == b.get_device() == dev and nb == n
+                and rb == R and ka == K and (a1 == 1 or K == 1) and (b1 == 1 or R == 1)
+                and (ty == T_BF16 or ty == T_F16))
     except (AttributeError, ValueError):
         good = False
     if not good:
@@ -1408,15 +1399,11 @@ def _adapters(x, a, b, offsets, ids, scales, ranks, dev):
         br = R
     if n == 1:  # (one adapter: the stride to the next does not matter)
         an = bn = 0
-    d = Adapters(a.data_ptr(), b.data_ptr(), ar, an, br, bn, K, N, n, R, _type_of(x.dtype),
-                 None if scales is None else _plain(scales, "scales", torch.float32, (n,), dev),
-                 None if ranks is None else _plain(ranks, "ranks", torch.int32, (n,), dev))
-    try:
-        m = ids.shape[0]
-    except (AttributeError, IndexError):
-        m = -1
-    s = Segments(_plain(offsets, "offsets", torch.int32, (m + 1,), dev),
-                 _plain(ids, "ids", torch.int32, (m,), dev), m)
+    m = ids.shape[0] if getattr(ids, "ndim", 0) == 1 else -1
+    d = Adapters(a.data_ptr(), b.data_ptr(), ar, an, br, bn, K, N, n, R, ty,
+                 None if scales is None else _plain(scales, "scales", T_F32, (n,), dev),
+                 None if ranks is None else _plain(ranks, "ranks", T_I32, (n,), dev))
+    s = Segments(_plain(offsets, "offsets", T_I32, (m + 1,), dev), _plain(ids, "ids", T_I32, (m,), dev), m)
     return d, s
 
 
@@ -1445,8 +1432,7 @@ def adapters_forward(x, a, b, offsets, ids, scales=None, ranks=None, residual=No
     iy = _dense(y, "y", T, N, dev, dtype)
     ps, wp, wn = None, None, 0
     if saved is not None:
-        import torch
-        ps = _plain(saved, "saved", torch.float32, (T, R), dev)
+        ps = _plain(saved, "saved", T_F32, (T, R), dev)
     else:
         ws = _workspace_at(workspace, dev, stream, adapters_workspace, T, R, x.device)
         wp, wn = ws.data_ptr(), ws.numel()
@@ -1464,7 +1450,6 @@ def adapters_backward(x, a, b, saved, dy, offsets, ids, scales=None, ranks=None,
     segment are left as they were.  da [n][R][K] and db [n][N][R] are of x's type or those
     of the buffers passed (contiguous, both of one type, x's or fp32): sums over all rows of
     an adapter, zeros past its rank and for an adapter without rows.  Those not needed are None."""
-    import torch
     ix = _dense(x, "x")
     dev = x.get_device()
     st = _stream_on(dev, "x", stream)
@@ -1472,6 +1457,7 @@ def adapters_backward(x, a, b, saved, dy, offsets, ids, scales=None, ranks=None,
     T, K, N, R, n = x.shape[0], d.K, d.N, d.R, d.n
     idy = _dense(dy, "dy", T, N, dev, x.dtype)
     ir = None
+    import torch
     if dx is None and need_dx:
         dx = _made(stream, torch.empty, (T, K), device=x.device,
                    dtype=x.dtype if residual is None else residual.dtype)
@@ -1480,21 +1466,20 @@ def adapters_backward(x, a, b, saved, dy, offsets, ids, scales=None, ranks=None,
             raise ValueError("a residual is added to dx, which is not wanted")
         ir = C.byref(_dense(residual, "residual", T, K, dev))
     odx = None if dx is None else C.byref(_dense(dx, "dx", T, K, dev))
-    gt = next((t.dtype for t in (da, db) if isinstance(t, torch.Tensor)), x.dtype)
-    if da is None and need_weights:
-        da = _made(stream, torch.empty, (n, R, K), dtype=gt, device=x.device)
-    if db is None and need_weights:
-        db = _made(stream, torch.empty, (n, N, R), dtype=gt, device=x.device)
-    pa = None if da is None else _plain(da, "da", gt, (n, R, K), dev)
-    pb = None if db is None else _plain(db, "db", gt, (n, N, R), dev)
-    ps = None if saved is None else _plain(saved, "saved", torch.float32, (T, R), dev)
+    gt = x.dtype if da is None and db is None else getattr(db if da is None else da, "dtype", None)
+    ty = _type_of(gt)
+    if ty is None or (ty != T_F32 and gt != x.dtype):
+        raise ValueError(f"da and db must be {x.dtype} or fp32 tensors")
+    if need_weights and (da is None or db is None):
+        da, db = (t if t is not None else _made(stream, torch.empty, shape, dtype=gt, device=x.device)
+                  for t, shape in ((da, (n, R, K)), (db, (n, N, R))))
+    pa = None if da is None else _plain(da, "da", ty, (n, R, K), dev)
+    pb = None if db is None else _plain(db, "db", ty, (n, N, R), dev)
+    ps = None if saved is None else _plain(saved, "saved", T_F32, (T, R), dev)
     wp, wn = None, 0
     if dx is not None or da is not None:
         ws = _workspace_at(workspace, dev, stream, adapters_workspace, T, R, x.device)
         wp, wn = ws.data_ptr(), ws.numel()
-    ty = _type_of(gt)
-    if ty is None:
-        raise ValueError(f"da and db must be {x.dtype} or fp32")
     _check(_lib.polyq_adapters_backward(C.byref(ix), T, C.byref(d), C.byref(s), ps, C.byref(idy), ir,
                                         odx, pa, pb, ty, wp, wn, st))
     return dx, da, db
