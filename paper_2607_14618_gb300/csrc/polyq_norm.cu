@@ -30,7 +30,7 @@ constexpr int kMaxCluster = 8;
 // Threads of a block at most: rows of up to 2048 columns take eight a thread, wider ones
 // sixteen, so that what a thread does once a row is shared by more of them.
 constexpr int kNarrow = 5120, kNarrowThreads = 256, kWideThreads = 512;
-constexpr int kReduceCols = 32, kReduceRows = 32;
+constexpr int kReduceCols = 32, kReduceRows = 16;
 // Threads of an SM, as registers allow, and rows that a thread takes together once there are enough.
 constexpr int kBackwardRegs = 96, kBackwardPerSm = 65536 / kBackwardRegs, kTogether = 2;
 constexpr int kMostSmem = 200 << 10;
@@ -587,7 +587,7 @@ Shape backward_shape(int64_t rows, int64_t K, int bytes, int sms) {
   // small rows share a block once there is one for every SM
   s.rows = (int)std::min<int64_t>(std::max(1, kNarrowThreads / s.threads), (rows + sms - 1) / sms);
   const int64_t most = std::max(1, sms * std::max(1, kBackwardPerSm / (s.threads * s.rows)) / s.cluster);
-  s.nr = rows >= 2 * kTogether * most * s.rows ? kTogether : 1;
+  s.nr = rows >= kTogether * most * s.rows ? kTogether : 1;
   s.blocks = std::min<int64_t>((rows + s.rows * s.nr - 1) / (s.rows * s.nr), most);
   return s;
 }
@@ -624,9 +624,8 @@ void* pick(const Variant& v) {
     return v.size == 1   ? (void*)norm_forward_kernel<TX, TY, VEC, 1>
            : v.size == 2 ? (void*)norm_forward_kernel<TX, TY, VEC, 2>
                          : (void*)norm_forward_kernel<TX, TY, VEC, 4>;
-  constexpr int many = VEC ? kTogether : 1;
   if (v.nr > 1)
-    return v.size == 1 ? (void*)norm_backward_kernel<TX, TY, VEC, many, 1> : (void*)norm_backward_kernel<TX, TY, VEC, many, 2>;
+    return v.size == 1 ? (void*)norm_backward_kernel<TX, TY, VEC, kTogether, 1> : (void*)norm_backward_kernel<TX, TY, VEC, kTogether, 2>;
   return v.size == 1 ? (void*)norm_backward_kernel<TX, TY, VEC, 1, 1> : (void*)norm_backward_kernel<TX, TY, VEC, 1, 2>;
 }
 template <typename TX, typename TY>
