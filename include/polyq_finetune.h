@@ -12,9 +12,8 @@
  * allocate device memory and never synchronise, `stream` is a cudaStream_t.
  * Every entry works on the current device and may be captured in a CUDA graph.
  * Sizes are at least 1: an empty tensor is POLYQ_EINVAL.  Outputs must not
- * overlap inputs or each other unless stated otherwise.  A workspace needs no
- * initialisation and may serve consecutive calls on one stream, but not calls
- * that run at the same time.  Results do not change from run to run.
+ * overlap inputs or each other unless stated otherwise.  A workspace may serve
+ * consecutive calls on one stream, but not calls that run at the same time.  Results do not change from run to run.
  */
 #ifndef POLYQ_FINETUNE_H
 #define POLYQ_FINETUNE_H
@@ -170,7 +169,11 @@ typedef struct {
   int32_t n;
 } polyq_segments;
 
-/* Bytes of the workspace of the calls below for T rows. */
+/* Bytes of the workspace of the calls below for T rows: a status word in its first 4 bytes
+ * (read it with polyq_workspace_status), and v or dv.  Its first
+ * POLYQ_ADAPTERS_WORKSPACE_ZERO bytes must be zero before its first use, and again after a
+ * wait that gave up; 16-byte aligned. */
+#define POLYQ_ADAPTERS_WORKSPACE_ZERO 256
 int polyq_adapters_workspace_bytes(int64_t T, int32_t R, size_t* bytes);
 
 /* y[t][n] = residual[t][n] + s sum_j v[t][j] b[n][j],  v[t][j] = sum_k x[t][k] a[j][k]
@@ -179,10 +182,9 @@ int polyq_adapters_workspace_bytes(int64_t T, int32_t R, size_t* bytes);
  * that type or POLYQ_F32; residual NULL (0) or of y's type: the projection's result, its
  * data may be y's, with y's stride.  Products of x and a are exact and their sums in
  * fp32, as v is; v enters the second product with 16 (bf16) or 21 (fp16) significant
- * bits; one rounding to y's type.  saved: NULL, or device memory of
- * polyq_adapters_workspace_bytes, 16-byte aligned, which receives v [T][R] for the
- * backward pass (rows without an adapter are left as they were); the workspace is not
- * used then.  Two launches. */
+ * bits; one rounding to y's type.  saved: NULL, or device memory of T*R floats, 16-byte
+ * aligned, which receives v [T][R] for the backward pass (rows without an adapter are left
+ * as they were).  Two launches. */
 int polyq_adapters_forward(const polyq_dense* x, int64_t T, const polyq_adapters* adapters,
                            const polyq_segments* segments, const polyq_dense* residual,
                            const polyq_dense* y, float* saved, void* workspace,

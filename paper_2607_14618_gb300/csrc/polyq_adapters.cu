@@ -28,7 +28,7 @@ constexpr int64_t kMaxSize = 1 << 24;
 // Devices on which a kernel may use its shared memory (a bit each), by the kernel's tile.
 std::atomic<uint64_t> g_ready[256];
 
-int launch(const Kernel& k, int which, dim3 grid, int cluster, void* params, void* stream, const char* who) {
+int launch(const Kernel& k, int which, dim3 grid, int threads, int cluster, void* params, void* stream, const char* who) {
   int dev = 0;
   cudaError_t ce = cudaGetDevice(&dev);
   if (ce == cudaSuccess) {
@@ -50,7 +50,7 @@ int launch(const Kernel& k, int which, dim3 grid, int cluster, void* params, voi
     cfg.attrs = at;
     cfg.numAttrs = cluster > 1 ? 2 : 1;
     cfg.gridDim = grid;
-    cfg.blockDim = dim3(lora::kThreads);
+    cfg.blockDim = dim3(threads);
     cfg.dynamicSmemBytes = k.smem;
     void* args[] = {params};
     ce = cudaLaunchKernelExC(&cfg, k.f, args);
@@ -67,7 +67,8 @@ int64_t most_tiles(int64_t T, int n, int bm) { return std::min<int64_t>(T, T / b
 
 // v [T][R] of x times one of the adapters' matrices.
 int shrink(const polyq_dense* x, int64_t T, int64_t K, const polyq_adapters* ad, bool trans, const lora::Side& w,
-           const float* scales, const lora::Segments& seg, float* v, int sms, void* stream, const char* who) {
+           const float* scales, const lora::Segments& seg, float* v, int* status, int sms, void* stream,
+           const char* who) {
   const int rn = rank_tile(ad->R);
   const int64_t mean = T / seg.n;
   const int bm = mean <= 32 ? 16 : rn >= 64 && mean >= 256 ? 128 : 64;
@@ -89,8 +90,21 @@ int shrink(const polyq_dense* x, int64_t T, int64_t K, const polyq_adapters* ad,
   P.R = ad->R;
   P.adapters = ad->n;
   P.cluster = cluster;
+  P.status = status;
+  if (bm != 16) {
+    const int rc_x = polyq_tensor_map_2d(&P.x_map, x->data, 2, (uint64_t)K, (uint64_t)T, (uint64_t)x->stride * 2, 64,
+                                         (uint32_t)bm, 128);
+    if (rc_x) return rc_x;
+    const uint64_t cols = trans ? ad->R : K, rows = trans ? K : ad->R, stride = (uint64_t)w.stride * 2;
+    const int rc_w = polyq_tensor_map_3d(&P.w_map, w.w, cols, rows, (uint64_t)ad->n, stride,
+                                         ad->n > 1 ? (uint64_t)w.next * 2 : rows * stride,
+                                         trans ? (uint32_t)std::min(rn, 64) : 64u,
+                                         trans ? (uint32_t)(bm == 128 ? 64 : 128) : (uint32_t)rn);
+    if (rc_w) return rc_w;
+  }
   const int which = (((half * 2 + trans) * 4 + rank_index(rn)) * 4) + (bm == 16 ? 0 : bm == 64 ? 1 : 2);
-  return launch(k, which, dim3((unsigned)(tiles * cluster)), cluster, &P, stream, who);
+  return launch(k, which, dim3((unsigned)(tiles * cluster)), lora::kThreads + (bm != 16 ? 32 : 0), cluster, &P, stream,
+                who);
 }
 
 // y = residual + v times one of the adapters' matrices.
@@ -124,7 +138,8 @@ int expand(const float* v, int64_t T, int64_t N, const polyq_adapters* ad, bool 
   const int64_t columns = (N + bn - 1) / bn, slots = (int64_t)sms * (bm != 16 ? 4 : rn <= 64 ? 3 : 2);
   const int64_t rows = std::min<int64_t>(P.tiles, std::max<int64_t>(seg.n, (T + bm - 1) / bm + seg.n / 2));
   const int64_t share = std::min(columns, std::max<int64_t>(1, slots / rows));
-  return launch(k, which, dim3((unsigned)share, (unsigned)std::min(P.tiles, 65535)), 1, &P, stream, who);
+  return launch(k, which, dim3((unsigned)share, (unsigned)std::min(P.tiles, 65535)), lora::kThreads, 1, &P, stream,
+                who);
 }
 
 bool rows_on_16(const polyq_dense* d) { return (uintptr_t)d->data % 16 == 0 && d->stride % 8 == 0; }
@@ -175,7 +190,8 @@ int check_sum(const polyq_dense* y, const polyq_dense* residual, int64_t cols, c
   return POLYQ_OK;
 }
 
-size_t v_bytes(int64_t T, int R) { return (size_t)T * R * sizeof(float); }
+constexpr size_t kHead = 256;  // of the workspace: its status word
+size_t workspace_size(int64_t T, int R) { return kHead + (size_t)T * R * sizeof(float); }
 
 }  // namespace
 
@@ -183,7 +199,7 @@ extern "C" int polyq_adapters_workspace_bytes(int64_t T, int32_t R, size_t* byte
   polyq_clear_error();
   if (!bytes || T < 1 || T > kMaxSize || R < 1 || R % 8 || R > POLYQ_ADAPTERS_MAX_RANK)
     return polyq_set_error(POLYQ_EINVAL, "polyq_adapters_workspace_bytes: T=%lld R=%d", (long long)T, R);
-  *bytes = v_bytes(T, R);
+  *bytes = workspace_size(T, R);
   return POLYQ_OK;
 }
 
@@ -196,16 +212,17 @@ extern "C" int polyq_adapters_forward(const polyq_dense* x, int64_t T, const pol
   int rc = check(x, T, adapters, segments, who);
   if (!rc) rc = check_sum(y, residual, adapters->N, adapters, who, "y");
   if (rc) return rc;
-  float* v = saved ? saved : (float*)workspace;
-  if ((uintptr_t)v % 16) return polyq_set_error(POLYQ_EINVAL, "%s: saved and workspace must be 16-byte aligned", who);
-  if (!saved && (!workspace || workspace_bytes < v_bytes(T, adapters->R)))
-    return polyq_set_error(POLYQ_ENOMEM, "%s: workspace of %zu bytes needed", who, v_bytes(T, adapters->R));
+  if ((uintptr_t)saved % 16 || (uintptr_t)workspace % 16)
+    return polyq_set_error(POLYQ_EINVAL, "%s: saved and workspace must be 16-byte aligned", who);
+  if (!workspace || workspace_bytes < workspace_size(T, adapters->R))
+    return polyq_set_error(POLYQ_ENOMEM, "%s: workspace of %zu bytes needed", who, workspace_size(T, adapters->R));
+  float* v = saved ? saved : (float*)((char*)workspace + kHead);
   int sms = 0;
   rc = polyq_sm_count(&sms);
   if (rc) return rc;
   const lora::Segments seg{segments->offsets, segments->ids, segments->n, (int32_t)T};
   rc = shrink(x, T, adapters->K, adapters, false, lora::Side{adapters->a, adapters->a_next, adapters->a_stride}, nullptr,
-              seg, v, sms, stream, who);
+              seg, v, (int*)workspace, sms, stream, who);
   if (rc) return rc;
   return expand(v, T, adapters->N, adapters, false, lora::Side{adapters->b, adapters->b_next, adapters->b_stride},
                 adapters->scales, seg, residual, y, sms, stream, who);
@@ -235,8 +252,8 @@ extern "C" int polyq_adapters_backward(const polyq_dense* x, int64_t T, const po
   if ((db && !saved) || (uintptr_t)saved % 16 || (uintptr_t)workspace % 16)
     return polyq_set_error(POLYQ_EINVAL, "%s: saved and workspace must be 16-byte aligned, and saved given for db", who);
   const bool needs_dv = dx || da;
-  if (needs_dv && (!workspace || workspace_bytes < v_bytes(T, adapters->R)))
-    return polyq_set_error(POLYQ_ENOMEM, "%s: workspace of %zu bytes needed", who, v_bytes(T, adapters->R));
+  if (needs_dv && (!workspace || workspace_bytes < workspace_size(T, adapters->R)))
+    return polyq_set_error(POLYQ_ENOMEM, "%s: workspace of %zu bytes needed", who, workspace_size(T, adapters->R));
   int sms = 0;
   rc = polyq_sm_count(&sms);
   if (rc) return rc;
@@ -245,17 +262,17 @@ extern "C" int polyq_adapters_backward(const polyq_dense* x, int64_t T, const po
   const lora::Segments seg{segments->offsets, segments->ids, segments->n, (int32_t)T};
   lora::GradParams G;
   memset(&G, 0, sizeof G);
-  G.side[0] = lora::GradSide{(const float*)workspace, x->data, x->stride, adapters->K, da, nullptr, grad_type, 0,
+  G.side[0] = lora::GradSide{(const float*)((const char*)workspace + kHead), x->data, x->stride, adapters->K, da, nullptr, grad_type, 0,
                              da ? (int32_t)((adapters->K + bc - 1) / bc) : 0};
   G.side[1] = lora::GradSide{saved, dy->data, dy->stride, adapters->N, db, adapters->scales, grad_type, 1,
                              db ? (int32_t)((adapters->N + bc - 1) / bc) : 0};
   const int64_t blocks = (int64_t)adapters->n * (G.side[0].tiles + G.side[1].tiles);
   if (blocks > 0x7FFFFFFF / lora::kMaxCluster)
     return polyq_set_error(POLYQ_EUNSUPPORTED, "%s: gradients of %d adapters at once", who, adapters->n);
-  float* dv = (float*)workspace;
+  float* dv = (float*)((char*)workspace + kHead);
   if (needs_dv) {
     rc = shrink(dy, T, adapters->N, adapters, true, lora::Side{adapters->b, adapters->b_next, adapters->b_stride},
-                adapters->scales, seg, dv, sms, stream, who);
+                adapters->scales, seg, dv, (int*)workspace, sms, stream, who);
     if (rc) return rc;
   }
   if (blocks) {
@@ -265,7 +282,8 @@ extern "C" int polyq_adapters_backward(const polyq_dense* x, int64_t T, const po
     G.cluster = 1;
     while (G.cluster < lora::kMaxCluster && blocks * G.cluster < 2 * sms && T >= 128 * G.cluster) G.cluster *= 2;
     const Kernel k = half ? lora::gradients_of<__half>(rn) : lora::gradients_of<__nv_bfloat16>(rn);
-    rc = launch(k, 192 + half * 4 + rank_index(rn), dim3((unsigned)(blocks * G.cluster)), G.cluster, &G, stream, who);
+    rc = launch(k, 192 + half * 4 + rank_index(rn), dim3((unsigned)(blocks * G.cluster)), lora::kThreads, G.cluster, &G, stream,
+                who);
     if (rc) return rc;
   }
   if (!dx) return POLYQ_OK;

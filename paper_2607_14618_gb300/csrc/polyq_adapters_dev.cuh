@@ -82,12 +82,39 @@ __device__ __forceinline__ uint32_t cluster_rank() {
   asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
   return r;
 }
-__device__ __forceinline__ float ld_cluster(uint32_t addr, uint32_t rank) {
+// The sum over a cluster's blocks, in their order, of what lies at one place in their shared
+// memory; all loads are under way before the first is added (one after another, eight blocks
+// cost 0.3 us each for every number of a thread).
+__device__ __forceinline__ uint32_t mapa(uint32_t addr, uint32_t rank) {
   uint32_t there;
-  float v;
-  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(addr), "r"(rank));
-  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(there) : "memory");
-  return v;
+  asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(addr), "r"(rank));
+  return there;
+}
+__device__ __forceinline__ float sum_cluster(uint32_t addr, int blocks) {
+  float v[kMaxCluster], s = 0.f;
+#pragma unroll
+  for (int r = 0; r < kMaxCluster; ++r) {
+    v[r] = 0.f;
+    if (r < blocks) asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v[r]) : "r"(mapa(addr, r)) : "memory");
+  }
+#pragma unroll
+  for (int r = 0; r < kMaxCluster; ++r) s += v[r];
+  return s;
+}
+__device__ __forceinline__ float4 sum_cluster4(uint32_t addr, int blocks) {
+  float4 v[kMaxCluster], s = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+  for (int r = 0; r < kMaxCluster; ++r) {
+    v[r] = s;
+    if (r < blocks)
+      asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+                   : "=f"(v[r].x), "=f"(v[r].y), "=f"(v[r].z), "=f"(v[r].w)
+                   : "r"(mapa(addr, r))
+                   : "memory");
+  }
+#pragma unroll
+  for (int r = 0; r < kMaxCluster; ++r) s.x += v[r].x, s.y += v[r].y, s.z += v[r].z, s.w += v[r].w;
+  return s;
 }
 
 // ---- tiles in shared memory ----
@@ -305,9 +332,11 @@ struct ShrinkParams {
   float* v;  // [rows][R]
   const float* scales;  // NULL: s = 1
   const int32_t* ranks;
+  int* status;
   Segments seg;
   int64_t x_stride, K;
   int32_t R, adapters, cluster;
+  CUtensorMap x_map, w_map;  // (shrink_tiled_kernel)
 };
 
 // A cluster's blocks share the contraction of one tile of BM rows and add their
@@ -315,15 +344,46 @@ struct ShrinkParams {
 // order.
 template <typename T, int BM, int RN, bool TRANS>
 struct Shrink {
-  static constexpr int KC = BM == 128 ? 64 : 128;  // contraction of a stage
-  static constexpr int STAGES = BM == 128 || (BM == 16 && RN != 64) ? 4 : 3;  // (three blocks to an SM for few rows)
+  static_assert(BM == 16, "tiles of few rows");
+  static constexpr int KC = 128;                  // contraction of a stage
+  static constexpr int STAGES = RN == 64 ? 3 : 4;  // (three blocks to an SM)
   // warps along the rows, the rank and the contraction of a stage
-  static constexpr int WM = BM == 16 ? 1 : 4, WN = BM == 16 ? RN / 16 : RN == 16 ? 1 : 2, WK = 8 / (WM * WN);
-  static constexpr int MT = BM / 16 / WM, NT = RN / 8 / WN;
+  static constexpr int WM = 1, WN = RN / 16, WK = 8 / WN;
+  static constexpr int MT = 1, NT = 2;
   static constexpr int X_BYTES = BM * KC * 2, W_BYTES = RN * KC * 2;
   static constexpr int RED_BYTES = WK * BM * RN * 4;
   static constexpr int SMEM = STAGES * (X_BYTES + W_BYTES) > RED_BYTES ? STAGES * (X_BYTES + W_BYTES) : RED_BYTES;
 };
+
+// Adds the tile's sums [WK][BM][RN] of the cluster's blocks, each block a part of the tile.
+template <int BM, int RN, int WK>
+__device__ __forceinline__ void shrink_finish(const ShrinkParams& P, const Tile& t, uint32_t base, const uint8_t* smem,
+                                              int rank) {
+  const int own = P.ranks ? min(max(__ldcg(P.ranks + t.id), 0), P.R) : P.R;
+  const float s = P.scales ? __ldcg(P.scales + t.id) : 1.f;
+  if (P.cluster > 1) cluster_sync();
+  else __syncthreads();
+  const int part = BM * RN / 4 / P.cluster;  // four columns each
+  for (int i = rank * part + threadIdx.x; i < (rank + 1) * part; i += blockDim.x) {
+    const int row = 4 * i / RN, col = 4 * i % RN;
+    if (row >= t.rows) break;
+    if (col >= P.R) continue;
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int q = 0; q < WK; ++q) {
+      const int at = q * BM * RN + 4 * i;
+      const float4 w = P.cluster > 1 ? sum_cluster4(base + at * 4, P.cluster)
+                                     : *reinterpret_cast<const float4*>(smem + at * 4);
+      v.x += w.x, v.y += w.y, v.z += w.z, v.w += w.w;
+    }
+    v.x = col < own ? v.x * s : 0.f;
+    v.y = col + 1 < own ? v.y * s : 0.f;
+    v.z = col + 2 < own ? v.z * s : 0.f;
+    v.w = col + 3 < own ? v.w * s : 0.f;
+    *reinterpret_cast<float4*>(P.v + (int64_t)(t.row + row) * P.R + col) = v;  // (R is a multiple of 8)
+  }
+  if (P.cluster > 1) cluster_sync();  // (another block may still read this one's sums)
+}
 
 template <typename T, int BM, int RN, bool TRANS>
 __global__ void __launch_bounds__(kThreads) shrink_kernel(const __grid_constant__ ShrinkParams P) {
@@ -339,7 +399,6 @@ __global__ void __launch_bounds__(kThreads) shrink_kernel(const __grid_constant_
   if (!find_tile(P.seg, BM, blockIdx.x / P.cluster, t)) return;  // the whole cluster
   if (t.id < 0 || t.id >= P.adapters) return;
   const int rank_of = P.ranks ? __ldcg(P.ranks + t.id) : P.R;  // (used once the copies of x are under way)
-  const float s = P.scales ? __ldcg(P.scales + t.id) : 1.f;
   const T* x = (const T*)P.x + (int64_t)t.row * P.x_stride;
   const T* w = (const T*)P.w.w + (int64_t)t.id * P.w.next;
   const int64_t chunks = (P.K + KC - 1) / KC;
@@ -414,23 +473,135 @@ __global__ void __launch_bounds__(kThreads) shrink_kernel(const __grid_constant_
       *reinterpret_cast<float2*>(red + row * RN + col) = make_float2(acc[i][j][0], acc[i][j][1]);
       *reinterpret_cast<float2*>(red + (row + 8) * RN + col) = make_float2(acc[i][j][2], acc[i][j][3]);
     }
-  if (P.cluster > 1) cluster_sync();
-  else __syncthreads();
-  const int part = BM * RN / P.cluster;
-  for (int i = rank * part + threadIdx.x; i < (rank + 1) * part; i += kThreads) {
-    const int row = i / RN, col = i % RN;
-    if (row >= t.rows) break;
-    if (col >= P.R) continue;
-    float v = 0.f;
-    for (int r = 0; r < P.cluster; ++r)
-#pragma unroll
-      for (int q = 0; q < S::WK; ++q) {
-        const int at = q * BM * RN + i;
-        v += P.cluster > 1 ? ld_cluster(base + at * 4, r) : reinterpret_cast<const float*>(smem)[at];
-      }
-    P.v[(int64_t)(t.row + row) * P.R + col] = col < own ? v * s : 0.f;
+  shrink_finish<BM, RN, S::WK>(P, t, base, smem, rank);
+}
+
+// The same for tiles of 64 or 128 rows: a ninth warp asks the TMA unit for whole stages, whose
+// barriers the eight others wait on, each by itself.  (With copies by all threads and a barrier
+// of the block for every stage, half of the instructions were the copies'.)  A tile's rows past
+// its segment, and columns past its rank, are what lies there: their sums are not used.
+template <typename T, int BM, int RN, bool TRANS>
+struct Tiled {
+  static constexpr int KC = BM == 128 ? 64 : 128;  // contraction of a stage, in panels of 64
+  static constexpr int PANELS = KC / 64;
+  static constexpr int WM = 4, WN = RN == 16 ? 1 : 2, WK = 8 / (WM * WN);
+  static constexpr int MT = BM / 64, NT = RN / 8 / WN;
+  static constexpr int X_BYTES = BM * KC * 2, W_BYTES = RN * KC * 2, STAGE = X_BYTES + W_BYTES;
+  static constexpr int STAGES = BM == 128 ? (RN == 64 ? 4 : 3) : RN == 128 ? 2 : 3;  // (two or three blocks to an SM)
+  static constexpr int RED_BYTES = WK * BM * RN * 4;
+  static constexpr int SMEM = 1024 + (STAGES * STAGE > RED_BYTES ? STAGES * STAGE : RED_BYTES);
+};
+
+template <typename T, int BM, int RN, bool TRANS>
+__global__ void __launch_bounds__(kThreads + 32, RN == 128 ? 1 : BM == 64 && RN <= 32 ? 3 : 2) shrink_tiled_kernel(const __grid_constant__ ShrinkParams P) {
+  using S = Tiled<T, BM, RN, TRANS>;
+  constexpr int KC = S::KC, CW = TRANS && RN < 64 ? RN / 8 : 8;
+  extern __shared__ uint8_t raw_smem[];
+  __shared__ __align__(8) uint64_t bars[2 * S::STAGES];
+  const uint32_t base = (smem_u32(raw_smem) + 1023u) & ~1023u, full = smem_u32(bars), empty = full + 8 * S::STAGES;
+  uint8_t* smem = raw_smem + (base - smem_u32(raw_smem));
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int rank = P.cluster > 1 ? (int)cluster_rank() : 0;
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < S::STAGES; ++i) {
+      mbar_init(full + 8 * i, 1);
+      mbar_init(empty + 8 * i, 8);
+    }
+    mbar_fence_init();
   }
-  if (P.cluster > 1) cluster_sync();  // (another block may still read this one's sums)
+  if (warp == 8 && elect_one()) {
+    prefetch_tmap(&P.x_map);
+    prefetch_tmap(&P.w_map);
+  }
+  pdl_wait();
+  pdl_trigger();  // (not before the wait: what follows reads what this grid has waited for)
+  Tile t;
+  if (!find_tile(P.seg, BM, blockIdx.x / P.cluster, t)) return;  // the whole cluster
+  if (t.id < 0 || t.id >= P.adapters) return;
+  __syncthreads();
+  const int chunks = (int)((P.K + KC - 1) / KC);
+  const int c0 = (int)((int64_t)chunks * rank / P.cluster), c1 = (int)((int64_t)chunks * (rank + 1) / P.cluster);
+  float acc[S::MT][S::NT][4] = {};
+  const int wm = warp % S::WM, wn = warp / S::WM % S::WN, wk = warp / (S::WM * S::WN);
+  if (warp == 8) {
+    if (elect_one()) {
+      int asked = 0;
+      for (int c = c0; c < c1; ++c, ++asked) {
+        const int stage = asked % S::STAGES;
+        const uint32_t bar = full + 8 * stage, at = base + stage * S::STAGE;
+        if (asked >= S::STAGES && !mbar_wait(empty + 8 * stage, (asked / S::STAGES - 1) & 1)) {
+          atomicExch(P.status, kStatusTimeoutEmpty);
+          break;
+        }
+        mbar_expect_tx(bar, S::STAGE);
+#pragma unroll
+        for (int q = 0; q < S::PANELS; ++q) {
+          tma_load_2d(at + q * BM * 128, &P.x_map, c * KC + q * 64, t.row, bar);
+          if (!TRANS) tma_load_3d(at + S::X_BYTES + q * RN * 128, &P.w_map, c * KC + q * 64, 0, t.id, bar);
+        }
+        if (TRANS)
+#pragma unroll
+          for (int q = 0; q < (RN + 63) / 64; ++q)
+            tma_load_3d(at + S::X_BYTES + q * KC * 128, &P.w_map, q * 64, c * KC, t.id, bar);
+      }
+      // no copy is under way when the block ends, whether its stages were awaited or not
+      for (int i = asked > S::STAGES ? asked - S::STAGES : 0; i < asked; ++i)
+        if (!mbar_wait(full + 8 * (i % S::STAGES), (i / S::STAGES) & 1)) break;
+    }
+    __syncwarp();
+  } else {
+    bool ok = true;
+    for (int i = 0; i < c1 - c0; ++i) {
+      const int stage = i % S::STAGES;
+      const uint32_t at = base + stage * S::STAGE;
+      if (ok && !mbar_wait(full + 8 * stage, (i / S::STAGES) & 1)) {
+        ok = false;
+        atomicExch(P.status, kStatusTimeoutFull);
+      }
+      if (!ok) continue;
+      float sum[S::MT][S::NT][4] = {};  // of the stage: the tensor cores cut running sums off
+#pragma unroll
+      for (int k = wk * 16; k < KC; k += 16 * S::WK) {
+        const uint32_t xt = at + k / 64 * (BM * 128), wt = at + S::X_BYTES + (TRANS ? 0 : k / 64 * (RN * 128));
+        uint32_t a[S::MT][4];
+#pragma unroll
+        for (int m = 0; m < S::MT; ++m) frag_a<8, false>(xt, (wm * S::MT + m) * 16, k % 64, a[m]);
+#pragma unroll
+        for (int j = 0; j < S::NT; j += 2) {
+          const int n = (wn * S::NT + j) * 8;
+          uint32_t b[4];
+          if (TRANS) frag_b<CW, true>(wt + n / 64 * (KC * 128), n % 64, k, b);
+          else frag_b<8, false>(wt, n, k % 64, b);
+#pragma unroll
+          for (int m = 0; m < S::MT; ++m) {
+            mma<T>(sum[m][j], a[m], b[0], b[1]);
+            mma<T>(sum[m][j + 1], a[m], b[2], b[3]);
+          }
+        }
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(empty + 8 * stage);
+#pragma unroll
+      for (int m = 0; m < S::MT; ++m)
+#pragma unroll
+        for (int j = 0; j < S::NT; ++j)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) acc[m][j][e] += sum[m][j][e];
+    }
+  }
+  __syncthreads();
+  if (warp < 8) {
+    float* red = reinterpret_cast<float*>(smem) + wk * BM * RN;
+#pragma unroll
+    for (int i = 0; i < S::MT; ++i)
+#pragma unroll
+      for (int j = 0; j < S::NT; ++j) {
+        const int row = (wm * S::MT + i) * 16 + lane / 4, col = (wn * S::NT + j) * 8 + lane % 4 * 2;
+        *reinterpret_cast<float2*>(red + row * RN + col) = make_float2(acc[i][j][0], acc[i][j][1]);
+        *reinterpret_cast<float2*>(red + (row + 8) * RN + col) = make_float2(acc[i][j][2], acc[i][j][3]);
+      }
+  }
+  shrink_finish<BM, RN, S::WK>(P, t, base, smem, rank);
 }
 
 // ---------------------------------------------------------------------------
@@ -683,11 +854,11 @@ struct Grad {
   static constexpr int BC = RN <= 64 ? 128 : 64;   // columns of a block
   static constexpr int WR = RN <= 32 ? 1 : RN / 32, WC = 8 / WR;
   static constexpr int MT = RN / 16 / WR, NT = BC / 8 / WC;
-  static constexpr int STAGES = RN <= 64 ? 3 : 2;  // (two blocks to an SM)
+  // x of three stages (multiplied, here, on its way), v of two as it lies and of two split
   static constexpr int X_BYTES = BT * BC * 2, F_BYTES = BT * RN * 4, V_BYTES = BT * RN * 2;
   static constexpr int PITCH = BC + 1;
   static constexpr int RED_BYTES = RN * PITCH * 4;
-  static constexpr int MAIN = STAGES * (X_BYTES + F_BYTES) + 2 * V_BYTES;
+  static constexpr int MAIN = 3 * X_BYTES + 2 * F_BYTES + 4 * V_BYTES;
   static constexpr int SMEM = MAIN > RED_BYTES ? MAIN : RED_BYTES;
 };
 
@@ -695,14 +866,14 @@ struct Grad {
 // added to the block's in fp32: the tensor cores cut their running sums off, and over thousands of
 // rows that adds up (4096 rows of two adapters: 5e-6 off without it, 2.4e-6 with it).
 template <typename T, int RN>
-__global__ void __launch_bounds__(kThreads, 2) gradients_kernel(const __grid_constant__ GradParams P) {
+__global__ void __launch_bounds__(kThreads, RN <= 64 ? 2 : 1) gradients_kernel(const __grid_constant__ GradParams P) {
   using G = Grad<T, RN>;
   constexpr int CX = G::BC / 8, CV = RN / 8, CF = RN / 4, BT = G::BT;
   constexpr bool SCALED = std::is_same<T, __half>::value;
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ uint32_t tops[8];
-  const uint32_t base = smem_u32(smem), vt = base + G::STAGES * (G::X_BYTES + G::F_BYTES);
-  uint8_t* vs = smem + G::STAGES * (G::X_BYTES + G::F_BYTES);
+  constexpr int F_AT = 3 * G::X_BYTES, V_AT = F_AT + 2 * G::F_BYTES;
+  const uint32_t base = smem_u32(smem);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int rank = P.cluster > 1 ? (int)cluster_rank() : 0;
   const int per = P.side[0].tiles + P.side[1].tiles, block = blockIdx.x / P.cluster;
@@ -723,28 +894,21 @@ __global__ void __launch_bounds__(kThreads, 2) gradients_kernel(const __grid_con
     int row, rows;
     any = any && ahead.next(P.seg, id, BT, P.cluster, row, rows);
     if (any) {
-      const uint32_t at = base + stage * (G::X_BYTES + G::F_BYTES);
-      mx.copy(at, (int64_t)row * D.x_stride * 2, rows);
-      mv.copy(at + G::X_BYTES, (int64_t)row * P.R * 4, rows);
+      mx.copy(base + stage % 3 * G::X_BYTES, (int64_t)row * D.x_stride * 2, rows);
+      mv.copy(base + F_AT + stage % 2 * G::F_BYTES, (int64_t)row * P.R * 4, rows);
       ++asked;
     }
     cp_commit();
   };
-  float acc[G::MT][G::NT][4] = {}, part[G::MT][G::NT][4] = {};
-  const int wr = warp % G::WR, wc = warp / G::WR;
-#pragma unroll
-  for (int i = 0; i < G::STAGES - 1; ++i) copy(i);
-  for (int done = 0, stage = 0; done < asked; ++done) {
-    cp_wait<G::STAGES - 2>();
-    __syncthreads();  // the stage is here, and the one before has been read
-    copy(stage == 0 ? G::STAGES - 1 : stage - 1);
-    const uint32_t at = base + stage * (G::X_BYTES + G::F_BYTES);
-    const uint8_t* f = smem + (at - base) + G::X_BYTES;
+  float down = 1.f, up = 1.f;
+  // v of a stage as two numbers; `up` is what undoes its scale.
+  auto split = [&](int stage) {
+    const float4* f = reinterpret_cast<const float4*>(smem + F_AT + stage % 2 * G::F_BYTES);
+    uint8_t* to = smem + V_AT + stage % 2 * 2 * G::V_BYTES;
     auto v8 = [&](int g, float(&v)[8]) {
-      const float4 a = reinterpret_cast<const float4*>(f)[2 * g], b = reinterpret_cast<const float4*>(f)[2 * g + 1];
+      const float4 a = f[2 * g], b = f[2 * g + 1];
       v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
     };
-    float down = 1.f, up = 1.f;
     if constexpr (SCALED) {
       uint32_t top = 0;
 #pragma unroll
@@ -766,10 +930,24 @@ __global__ void __launch_bounds__(kThreads, 2) gradients_kernel(const __grid_con
       uint4 h, l;
       v8(g, v);
       split8<T>(v, down, h, l);
-      *reinterpret_cast<uint4*>(vs + piece<CV>(g / CV, g % CV)) = h;
-      *reinterpret_cast<uint4*>(vs + G::V_BYTES + piece<CV>(g / CV, g % CV)) = l;
+      *reinterpret_cast<uint4*>(to + piece<CV>(g / CV, g % CV)) = h;
+      *reinterpret_cast<uint4*>(to + G::V_BYTES + piece<CV>(g / CV, g % CV)) = l;
     }
+  };
+  float acc[G::MT][G::NT][4] = {}, part[G::MT][G::NT][4] = {};
+  const int wr = warp % G::WR, wc = warp / G::WR;
+  copy(0);
+  copy(1);
+  if (asked) {
+    cp_wait<1>();
     __syncthreads();
+    split(0);
+  }
+  for (int done = 0; done < asked; ++done) {
+    cp_wait<0>();
+    __syncthreads();  // the next stage is here, this one is split, the one before has been read
+    copy(done + 2);
+    const uint32_t at = base + done % 3 * G::X_BYTES, vt = base + V_AT + done % 2 * 2 * G::V_BYTES;
 #pragma unroll
     for (int k = 0; k < BT; k += 16) {
       uint32_t h[G::MT][4], l[G::MT][4];
@@ -792,18 +970,19 @@ __global__ void __launch_bounds__(kThreads, 2) gradients_kernel(const __grid_con
           for (int i = 0; i < G::MT; ++i) mma<T>(part[i][j + q], h[i], b[2 * q], b[2 * q + 1]);
       }
     }
-    if (SCALED || (done & 1) || done + 1 == asked) {  // (asked counts this stage's successors by now)
+    const float mine = up;
+    if (done + 1 < asked) split(done + 1);
+    if (SCALED || (done & 1) || done + 1 == asked) {
 #pragma unroll
       for (int i = 0; i < G::MT; ++i)
 #pragma unroll
         for (int j = 0; j < G::NT; ++j)
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            acc[i][j][e] = fmaf(part[i][j][e], up, acc[i][j][e]);
+            acc[i][j][e] = fmaf(part[i][j][e], mine, acc[i][j][e]);
             part[i][j][e] = 0.f;
           }
     }
-    if (++stage == G::STAGES) stage = 0;
   }
   const int own = min(max(rank_of, 0), P.R);
   cp_wait<0>();
@@ -825,9 +1004,8 @@ __global__ void __launch_bounds__(kThreads, 2) gradients_kernel(const __grid_con
   for (int i = rank * share + threadIdx.x; i < (rank + 1) * share; i += kThreads) {
     const int j = D.by_column ? i % RN : i / G::BC, c = D.by_column ? i / RN : i % G::BC;
     if (j >= P.R || n0 + c >= D.C) continue;
-    float sum = 0.f;
     const int at = j * G::PITCH + c;
-    for (int r = 0; r < P.cluster; ++r) sum += P.cluster > 1 ? ld_cluster(base + at * 4, r) : red[at];
+    const float sum = P.cluster > 1 ? sum_cluster(base + at * 4, P.cluster) : red[at];
     const int64_t o = (int64_t)id * P.R * D.C + (D.by_column ? (n0 + c) * P.R + j : j * D.C + n0 + c);
     any_store(D.out, D.type, o, j < own ? sum * s : 0.f);
   }
@@ -849,17 +1027,21 @@ Kernel expand_of(int bm, int rn, bool trans, bool f32);
 template <typename T>
 Kernel gradients_of(int rn);
 
-template <typename T, int BM, int RN>
-Kernel shrink_at(bool trans) {
-  return trans ? Kernel{(void*)shrink_kernel<T, BM, RN, true>, Shrink<T, BM, RN, true>::SMEM}
-               : Kernel{(void*)shrink_kernel<T, BM, RN, false>, Shrink<T, BM, RN, false>::SMEM};
+template <typename T, int BM, int RN, bool TRANS>
+Kernel shrink_at() {
+  if constexpr (BM == 16) return Kernel{(void*)shrink_kernel<T, BM, RN, TRANS>, Shrink<T, BM, RN, TRANS>::SMEM};
+  else return Kernel{(void*)shrink_tiled_kernel<T, BM, RN, TRANS>, Tiled<T, BM, RN, TRANS>::SMEM};
+}
+template <typename T, int RN, bool TRANS>
+Kernel shrink_for(int bm) {
+  if constexpr (RN >= 64) {
+    if (bm == 128) return shrink_at<T, 128, RN, TRANS>();
+  }
+  return bm == 16 ? shrink_at<T, 16, RN, TRANS>() : shrink_at<T, 64, RN, TRANS>();
 }
 template <typename T, int RN>
 Kernel shrink_for(int bm, bool trans) {
-  if constexpr (RN >= 64) {
-    if (bm == 128) return shrink_at<T, 128, RN>(trans);
-  }
-  return bm == 16 ? shrink_at<T, 16, RN>(trans) : shrink_at<T, 64, RN>(trans);
+  return trans ? shrink_for<T, RN, true>(bm) : shrink_for<T, RN, false>(bm);
 }
 template <typename T, int BM, int RN, bool TRANS>
 Kernel expand_at(bool f32) {

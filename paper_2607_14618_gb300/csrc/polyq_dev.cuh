@@ -69,6 +69,16 @@ __device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap* map
       : "memory");
 }
 
+// The same of a 3-D box {x, y, z}.
+__device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map, int32_t x,
+                                            int32_t y, int32_t z, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes"
+      " [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst),
+      "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(bar)
+      : "memory");
+}
+
 // Contiguous bulk copy global -> shared (16-byte aligned, size % 16 == 0).
 __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes,
                                           uint32_t bar) {
@@ -185,3 +195,8 @@ int polyq_sm_count(int* out);
 int polyq_tensor_map_2d(CUtensorMap* out, const void* base, int elem_bytes, uint64_t cols,
                         uint64_t rows, uint64_t row_stride_bytes, uint32_t box_cols,
                         uint32_t box_rows, int swizzle_bytes = 0);
+// 3-D tensor map over `depth` row-major [rows][cols] arrays of 16-bit elements with a box of
+// {box_cols, box_rows, 1}, swizzled over the box's rows of 32, 64 or 128 bytes.  Cached likewise.
+int polyq_tensor_map_3d(CUtensorMap* out, const void* base, uint64_t cols, uint64_t rows, uint64_t depth,
+                        uint64_t row_stride_bytes, uint64_t depth_stride_bytes, uint32_t box_cols,
+                        uint32_t box_rows);

@@ -1123,6 +1123,7 @@ def ffn_backward(x, gate, up, saved, dh, dx=None, dgate=None, dup=None, need_dx=
 
 
 # ---- layer norm, AdamW and low-rank adapters (include/polyq_finetune.h) ----
+ADAPTERS_WORKSPACE_ZERO = 256  # leading workspace bytes that must start at zero
 ADAMW_BLOCK = 256  # elements of an 8-bit state that share a scale
 
 
@@ -1366,7 +1367,9 @@ def adapters_workspace(T, R, device="cuda"):
     import torch
     n = C.c_size_t()
     _check(_lib.polyq_adapters_workspace_bytes(int(T), int(R), C.byref(n)))
-    return torch.empty(n.value, dtype=torch.uint8, device=device)
+    ws = torch.empty(n.value, dtype=torch.uint8, device=device)
+    ws[:ADAPTERS_WORKSPACE_ZERO].zero_()
+    return ws
 
 
 def adapters_saved(T, R, device="cuda"):
@@ -1430,14 +1433,10 @@ def adapters_forward(x, a, b, offsets, ids, scales=None, ranks=None, residual=No
         y = _made(stream, torch.empty, (T, N), device=x.device,
                   dtype=dtype or (residual.dtype if residual is not None else x.dtype))
     iy = _dense(y, "y", T, N, dev, dtype)
-    ps, wp, wn = None, None, 0
-    if saved is not None:
-        ps = _plain(saved, "saved", T_F32, (T, R), dev)
-    else:
-        ws = _workspace_at(workspace, dev, stream, adapters_workspace, T, R, x.device)
-        wp, wn = ws.data_ptr(), ws.numel()
+    ps = None if saved is None else _plain(saved, "saved", T_F32, (T, R), dev)
+    ws = _workspace_at(workspace, dev, stream, adapters_workspace, T, R, x.device)
     _check(_lib.polyq_adapters_forward(C.byref(ix), T, C.byref(d), C.byref(s), ir, C.byref(iy), ps,
-                                       wp, wn, st))
+                                       ws.data_ptr(), ws.numel(), st))
     return y
 
 
