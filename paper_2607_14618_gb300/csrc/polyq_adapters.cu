@@ -92,8 +92,9 @@ int shrink(const polyq_dense* x, int64_t T, int64_t K, const polyq_adapters* ad,
   P.cluster = cluster;
   P.status = status;
   if (bm != 16) {
-    const int rc_x = polyq_tensor_map_2d(&P.x_map, x->data, 2, (uint64_t)K, (uint64_t)T, (uint64_t)x->stride * 2, 64,
-                                         (uint32_t)bm, 128);
+    const uint64_t x_stride = (uint64_t)x->stride * 2;
+    const int rc_x = polyq_tensor_map_3d(&P.x_map, x->data, (uint64_t)K, (uint64_t)T, 1, x_stride, x_stride * T, 64,
+                                         (uint32_t)bm);
     if (rc_x) return rc_x;
     const uint64_t cols = trans ? ad->R : K, rows = trans ? K : ad->R, stride = (uint64_t)w.stride * 2;
     const int rc_w = polyq_tensor_map_3d(&P.w_map, w.w, cols, rows, (uint64_t)ad->n, stride,

@@ -189,29 +189,37 @@ struct Tile {
 __device__ __forceinline__ bool find_tile(const Segments& s, int bm, int tile, Tile& t) {
   const int lane = threadIdx.x & 31;
   int before = 0;
-  for (int s0 = 0; s0 < s.n; s0 += 32) {
-    const int i = s0 + lane;
-    int from = 0, to = 0, id = -1;
-    if (i < s.n) {
-      id = __ldcg(s.ids + i);
-      from = min(max(__ldcg(s.offsets + i), 0), s.rows);
-      to = min(max(__ldcg(s.offsets + i + 1), 0), s.rows);
-    }
-    const int n = to > from ? (to - from - 1) / bm + 1 : 0;
-    int sum = n;
+  for (int s0 = 0; s0 < s.n; s0 += 128) {  // four segments a lane, all loads under way together
+    const int i = s0 + 4 * lane;
+    int o[5], id[4], n[4], own = 0;
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int v = __shfl_up_sync(0xFFFFFFFFu, sum, o);
-      if (lane >= o) sum += v;
+    for (int k = 0; k < 5; ++k) o[k] = i + k <= s.n ? min(max(__ldcg(s.offsets + i + k), 0), s.rows) : 0;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) id[k] = i + k < s.n ? __ldcg(s.ids + i + k) : -1;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      n[k] = i + k < s.n && o[k + 1] > o[k] ? (o[k + 1] - o[k] - 1) / bm + 1 : 0;
+      own += n[k];
+    }
+    int sum = own;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const int v = __shfl_up_sync(0xFFFFFFFFu, sum, d);
+      if (lane >= d) sum += v;
     }
     const int total = __shfl_sync(0xFFFFFFFFu, sum, 31);
     if (tile < before + total) {
-      const int first = before + sum - n;
-      const int src = __ffs(__ballot_sync(0xFFFFFFFFu, n > 0 && first <= tile && tile < first + n)) - 1;
-      const int row = from + (tile - first) * bm;
+      int at = tile - (before + sum - own);  // counted from this lane's first
+      const int src = __ffs(__ballot_sync(0xFFFFFFFFu, at >= 0 && at < own)) - 1;
+      int row = 0, to = 0, of = -1;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        if (at >= 0 && at < n[k]) row = o[k] + at * bm, to = o[k + 1], of = id[k];
+        at -= n[k];
+      }
       t.row = __shfl_sync(0xFFFFFFFFu, row, src);
       t.rows = min(bm, __shfl_sync(0xFFFFFFFFu, to, src) - t.row);
-      t.id = __shfl_sync(0xFFFFFFFFu, id, src);
+      t.id = __shfl_sync(0xFFFFFFFFu, of, src);
       return true;
     }
     before += total;
@@ -236,14 +244,14 @@ struct AdapterTiles {
           s0 += 32;
           if (s0 >= s.n) return false;
           const int i = s0 + lane;
-          bool is = false;
+          int whose = -1;
           from = to = 0;
-          if (i < s.n && __ldcg(s.ids + i) == id) {
+          if (i < s.n) {
+            whose = __ldcg(s.ids + i);
             from = min(max(__ldcg(s.offsets + i), 0), s.rows);
             to = min(max(__ldcg(s.offsets + i + 1), 0), s.rows);
-            is = to > from;
           }
-          mine = __ballot_sync(0xFFFFFFFFu, is);
+          mine = __ballot_sync(0xFFFFFFFFu, whose == id && to > from);
         }
         const int src = __ffs(mine) - 1;
         mine &= mine - 1;
@@ -536,7 +544,7 @@ __global__ void __launch_bounds__(kThreads + 32, RN == 128 ? 1 : BM == 64 && RN 
         mbar_expect_tx(bar, S::STAGE);
 #pragma unroll
         for (int q = 0; q < S::PANELS; ++q) {
-          tma_load_2d(at + q * BM * 128, &P.x_map, c * KC + q * 64, t.row, bar);
+          tma_load_3d(at + q * BM * 128, &P.x_map, c * KC + q * 64, t.row, 0, bar);
           if (!TRANS) tma_load_3d(at + S::X_BYTES + q * RN * 128, &P.w_map, c * KC + q * 64, 0, t.id, bar);
         }
         if (TRANS)

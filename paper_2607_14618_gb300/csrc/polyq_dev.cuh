@@ -196,7 +196,8 @@ int polyq_tensor_map_2d(CUtensorMap* out, const void* base, int elem_bytes, uint
                         uint64_t rows, uint64_t row_stride_bytes, uint32_t box_cols,
                         uint32_t box_rows, int swizzle_bytes = 0);
 // 3-D tensor map over `depth` row-major [rows][cols] arrays of 16-bit elements with a box of
-// {box_cols, box_rows, 1}, swizzled over the box's rows of 32, 64 or 128 bytes.  Cached likewise.
+// {box_cols, box_rows, 1}, swizzled over the box's rows of 32, 64 or 128 bytes.  Made anew by every
+// call: nothing is kept of activations' addresses.
 int polyq_tensor_map_3d(CUtensorMap* out, const void* base, uint64_t cols, uint64_t rows, uint64_t depth,
                         uint64_t row_stride_bytes, uint64_t depth_stride_bytes, uint32_t box_cols,
                         uint32_t box_rows);

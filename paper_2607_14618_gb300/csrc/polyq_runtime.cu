@@ -23,8 +23,6 @@ EncodeFn g_encode = nullptr;
 std::map<int, int> g_sms;
 using Key = std::tuple<uintptr_t, int, uint64_t, uint64_t, uint64_t, uint32_t, uint32_t, int>;
 std::map<Key, CUtensorMap> g_maps;
-using Key3 = std::tuple<Key, uint64_t, uint64_t>;
-std::map<Key3, CUtensorMap> g_maps3;
 
 int get_encode(EncodeFn* fn) {
   if (!g_encode) {
@@ -111,25 +109,18 @@ int polyq_tensor_map_2d(CUtensorMap* out, const void* base, int elem_bytes, uint
 int polyq_tensor_map_3d(CUtensorMap* out, const void* base, uint64_t cols, uint64_t rows, uint64_t depth,
                         uint64_t row_stride_bytes, uint64_t depth_stride_bytes, uint32_t box_cols,
                         uint32_t box_rows) {
-  const uint32_t inner = box_cols * 2;
-  Key3 k{Key{(uintptr_t)base, 2, cols, rows, row_stride_bytes, box_cols, box_rows, (int)inner}, depth,
-         depth_stride_bytes};
-  std::lock_guard<std::mutex> lk(g_mu);
-  auto it = g_maps3.find(k);
-  if (it != g_maps3.end()) {
-    *out = it->second;
-    return POLYQ_OK;
-  }
   EncodeFn enc;
-  int rc = get_encode(&enc);
-  if (rc) return rc;
+  {
+    std::lock_guard<std::mutex> lk(g_mu);
+    const int rc = get_encode(&enc);
+    if (rc) return rc;
+  }
+  const uint32_t inner = box_cols * 2;
   cuuint64_t dims[3] = {cols, rows, depth};
   cuuint64_t strides[2] = {row_stride_bytes, depth_stride_bytes};
   cuuint32_t box[3] = {box_cols, box_rows, 1};
   cuuint32_t es[3] = {1, 1, 1};
-  CUtensorMap m;
-  std::memset(&m, 0, sizeof m);
-  CUresult r = enc(&m, CU_TENSOR_MAP_DATA_TYPE_UINT16, 3, const_cast<void*>(base), dims, strides, box, es,
+  CUresult r = enc(out, CU_TENSOR_MAP_DATA_TYPE_UINT16, 3, const_cast<void*>(base), dims, strides, box, es,
                    CU_TENSOR_MAP_INTERLEAVE_NONE,
                    inner == 128  ? CU_TENSOR_MAP_SWIZZLE_128B
                    : inner == 64 ? CU_TENSOR_MAP_SWIZZLE_64B
@@ -137,12 +128,6 @@ int polyq_tensor_map_3d(CUtensorMap* out, const void* base, uint64_t cols, uint6
                    CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   if (r != CUDA_SUCCESS)
     return polyq_set_error(POLYQ_ECUDA, "cuTensorMapEncodeTiled failed (%d)", (int)r);
-  if (g_maps3.size() > 4096) g_maps3.clear();
-  try {
-    g_maps3.emplace(k, m);
-  } catch (const std::bad_alloc&) {  // the next call encodes it again
-  }
-  *out = m;
   return POLYQ_OK;
 }
 

@@ -1338,7 +1338,9 @@ class AdamW:
         self._groups = [(*k, (AdamwTensor * len(v))(*v), len(v)) for k, v in groups.items()]
 
     def _scalar(self, t, name, dtype):
-        return _plain(t.reshape(()) if hasattr(t, "numel") and t.numel() == 1 else t, name, dtype, (), self._dev)
+        if not hasattr(t, "data_ptr") or t.numel() != 1:
+            raise ValueError(f"{name} must be a tensor of one element on cuda:{self._dev}")
+        return _plain(t.reshape(()), name, dtype, (), self._dev)
 
     def step(self, lr, step, betas=(0.9, 0.999), eps=1e-8, seed=0, grad_scale=None, stream=None):
         """One step.  `step` counts from 1.  lr and step may be tensors of one element on
@@ -1349,14 +1351,14 @@ class AdamW:
         for each step."""
         st = _stream_on(self._dev, "the tensors", stream)
         lr_dev = step_dev = scale = None
-        if not isinstance(lr, (int, float)):
+        if hasattr(lr, "data_ptr"):
             lr_dev, lr = self._scalar(lr, "lr", T_F32), 0.0
-        if not isinstance(step, int):
+        if hasattr(step, "data_ptr"):
             step_dev, step = self._scalar(step, "step", T_I64), 1
         if grad_scale is not None:
             scale = self._scalar(grad_scale, "grad_scale", T_F32)
-        h = C.byref(AdamwHyper(lr, betas[0], betas[1], eps, step, seed & 0xFFFFFFFFFFFFFFFF, lr_dev, step_dev,
-                               scale))
+        h = C.byref(AdamwHyper(float(lr), betas[0], betas[1], eps, int(step), seed & 0xFFFFFFFFFFFFFFFF, lr_dev,
+                               step_dev, scale))
         for tp, tg, tc, tensors, n in self._groups:
             _check(_lib.polyq_adamw_step(tensors, n, tp, tg, tc, self._state_ref, h, st))
 
