@@ -184,47 +184,51 @@ __device__ __forceinline__ uint32_t my_piece() {
 struct Tile {
   int32_t id, row, rows;
 };
-// Tile number `tile` of all segments' in turn (the whole warp calls; false: there
-// are fewer).  Offsets outside the tensors' rows are held at their ends.
+// Tile number `tile` of all segments' in turn (the whole block calls; false: there are
+// fewer).  Offsets outside the tensors' rows are held at their ends.  One warp looks: every
+// block reads the same few lines, and with all warps at it the lines' slice of L2 was
+// what 48 rows of rank 64 waited for (41 us, 30 with fewer requests).
 __device__ __forceinline__ bool find_tile(const Segments& s, int bm, int tile, Tile& t) {
+  __shared__ Tile found;
   const int lane = threadIdx.x & 31;
-  int before = 0;
-  for (int s0 = 0; s0 < s.n; s0 += 128) {  // four segments a lane, all loads under way together
-    const int i = s0 + 4 * lane;
-    int o[5], id[4], n[4], own = 0;
-#pragma unroll
-    for (int k = 0; k < 5; ++k) o[k] = i + k <= s.n ? min(max(__ldcg(s.offsets + i + k), 0), s.rows) : 0;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) id[k] = i + k < s.n ? __ldcg(s.ids + i + k) : -1;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      n[k] = i + k < s.n && o[k + 1] > o[k] ? (o[k + 1] - o[k] - 1) / bm + 1 : 0;
-      own += n[k];
-    }
-    int sum = own;
-#pragma unroll
-    for (int d = 1; d < 32; d <<= 1) {
-      const int v = __shfl_up_sync(0xFFFFFFFFu, sum, d);
-      if (lane >= d) sum += v;
-    }
-    const int total = __shfl_sync(0xFFFFFFFFu, sum, 31);
-    if (tile < before + total) {
-      int at = tile - (before + sum - own);  // counted from this lane's first
-      const int src = __ffs(__ballot_sync(0xFFFFFFFFu, at >= 0 && at < own)) - 1;
-      int row = 0, to = 0, of = -1;
+  if (threadIdx.x < 32) {
+    int before = 0;
+    bool there = false;
+    for (int s0 = 0; s0 < s.n && !there; s0 += 128) {  // four segments a lane, all loads under way together
+      int from[4], to[4], id[4];
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        if (at >= 0 && at < n[k]) row = o[k] + at * bm, to = o[k + 1], of = id[k];
-        at -= n[k];
+        const int i = s0 + 32 * k + lane;
+        from[k] = to[k] = 0, id[k] = -1;
+        if (i < s.n) {
+          id[k] = __ldcg(s.ids + i);
+          from[k] = min(max(__ldcg(s.offsets + i), 0), s.rows);
+          to[k] = min(max(__ldcg(s.offsets + i + 1), 0), s.rows);
+        }
       }
-      t.row = __shfl_sync(0xFFFFFFFFu, row, src);
-      t.rows = min(bm, __shfl_sync(0xFFFFFFFFu, to, src) - t.row);
-      t.id = __shfl_sync(0xFFFFFFFFu, of, src);
-      return true;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int n = to[k] > from[k] ? (to[k] - from[k] - 1) / bm + 1 : 0;
+        int sum = n;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+          const int v = __shfl_up_sync(0xFFFFFFFFu, sum, o);
+          if (lane >= o) sum += v;
+        }
+        const int first = before + sum - n;
+        if (first <= tile && tile < first + n) {
+          const int row = from[k] + (tile - first) * bm;
+          found = Tile{id[k], row, min(bm, to[k] - row)};
+        }
+        before += __shfl_sync(0xFFFFFFFFu, sum, 31);
+        there = there || tile < before;
+      }
     }
-    before += total;
+    if (lane == 0 && !there) found.rows = 0;
   }
-  return false;
+  __syncthreads();
+  t = found;
+  return t.rows > 0;
 }
 // The tiles of all segments of one adapter, every `stride`-th from `first` on.
 struct AdapterTiles {
@@ -526,7 +530,6 @@ __global__ void __launch_bounds__(kThreads + 32, RN == 128 ? 1 : BM == 64 && RN 
   Tile t;
   if (!find_tile(P.seg, BM, blockIdx.x / P.cluster, t)) return;  // the whole cluster
   if (t.id < 0 || t.id >= P.adapters) return;
-  __syncthreads();
   const int chunks = (int)((P.K + KC - 1) / KC);
   const int c0 = (int)((int64_t)chunks * rank / P.cluster), c1 = (int)((int64_t)chunks * (rank + 1) / P.cluster);
   float acc[S::MT][S::NT][4] = {};
@@ -826,8 +829,8 @@ __global__ void __launch_bounds__(kThreads, BM == 16 && RN <= 64 ? 3 : 2) expand
   bool first = true;
   for (int tile = blockIdx.y; tile < P.tiles; tile += gridDim.y) {
     Tile t;
-    if (!find_tile(P.seg, BM, tile, t)) break;
     if (!first) __syncthreads();  // (the tile before has been read)
+    if (!find_tile(P.seg, BM, tile, t)) break;
     if (P.vec) expand_tile<T, BM, RN, TRANS, TY, true>(P, t, smem, row_scale, first);
     else expand_tile<T, BM, RN, TRANS, TY, false>(P, t, smem, row_scale, first);
     first = false;
