@@ -178,8 +178,8 @@ int polyq_adapters_workspace_bytes(int64_t T, int32_t R, size_t* bytes);
 
 /* y[t][n] = residual[t][n] + s sum_j v[t][j] b[n][j],  v[t][j] = sum_k x[t][k] a[j][k]
  * of the row's adapter (scale s); rows of segments without one get the residual.  x [T][K] of the
- * adapters' type, 16-byte aligned with a stride that is a multiple of 8; y [T][N] of
- * that type or POLYQ_F32; residual NULL (0) or of y's type: the projection's result, its
+ * adapters' type (fastest where it is 16-byte aligned with a stride that is a multiple of 8); y
+ * [T][N] of that type or POLYQ_F32; residual NULL (0) or of y's type: the projection's result, its
  * data may be y's, with y's stride.  Products of x and a are exact and their sums in
  * fp32, as v is; v enters the second product with 16 (bf16) or 21 (fp16) significant
  * bits; one rounding to y's type.  saved: NULL, or device memory of T*R floats, 16-byte
@@ -190,7 +190,7 @@ int polyq_adapters_forward(const polyq_dense* x, int64_t T, const polyq_adapters
                            const polyq_dense* y, float* saved, void* workspace,
                            size_t workspace_bytes, void* stream);
 
-/* Gradients for the gradient dy [T][N] of y (as x is: type, alignment) and the `saved`
+/* Gradients for the gradient dy [T][N] of y (of the adapters' type, best aligned as x) and the `saved`
  * of the forward pass:
  *   dv[t][j] = s sum_n dy[t][n] b[n][j],  dx[t][k] = residual[t][k] + sum_j dv[t][j] a[j][k]
  *   da[j][k] = sum over the adapter's rows of dv[t][j] x[t][k]

@@ -9,12 +9,12 @@
 
 namespace polyq {
 namespace lora {
-extern template Kernel shrink_of<__nv_bfloat16>(int bm, int rn, bool trans);
+extern template Kernel shrink_of<__nv_bfloat16>(int bm, int rn, bool trans, bool any);
 extern template Kernel expand_of<__nv_bfloat16>(int bm, int rn, bool trans, bool f32);
-extern template Kernel gradients_of<__nv_bfloat16>(int rn);
-extern template Kernel shrink_of<__half>(int bm, int rn, bool trans);
+extern template Kernel gradients_of<__nv_bfloat16>(int rn, bool any);
+extern template Kernel shrink_of<__half>(int bm, int rn, bool trans, bool any);
 extern template Kernel expand_of<__half>(int bm, int rn, bool trans, bool f32);
-extern template Kernel gradients_of<__half>(int rn);
+extern template Kernel gradients_of<__half>(int rn, bool any);
 }  // namespace lora
 }  // namespace polyq
 
@@ -26,7 +26,7 @@ using lora::Kernel;
 constexpr int64_t kMaxSize = 1 << 24;
 
 // Devices on which a kernel may use its shared memory (a bit each), by the kernel's tile.
-std::atomic<uint64_t> g_ready[256];
+std::atomic<uint64_t> g_ready[320];
 
 int launch(const Kernel& k, int which, dim3 grid, int threads, int cluster, void* params, void* stream, const char* who) {
   int dev = 0;
@@ -59,6 +59,9 @@ int launch(const Kernel& k, int which, dim3 grid, int threads, int cluster, void
   return POLYQ_OK;
 }
 
+// Rows of 16-bit elements that start on 16 bytes, as asynchronous copies want them.
+bool rows_on_16(const polyq_dense* d) { return (uintptr_t)d->data % 16 == 0 && d->stride % 8 == 0; }
+
 int rank_tile(int R) { return R <= 16 ? 16 : R <= 32 ? 32 : R <= 64 ? 64 : 128; }
 int rank_index(int rn) { return rn == 16 ? 0 : rn == 32 ? 1 : rn == 64 ? 2 : 3; }
 
@@ -71,9 +74,10 @@ int shrink(const polyq_dense* x, int64_t T, int64_t K, const polyq_adapters* ad,
            const char* who) {
   const int rn = rank_tile(ad->R);
   const int64_t mean = T / seg.n;
-  const int bm = mean <= 32 ? 16 : rn >= 64 && mean >= 256 ? 128 : 64;
+  const bool any = !rows_on_16(x);
+  const int bm = any || mean <= 32 ? 16 : rn >= 64 && mean >= 256 ? 128 : 64;
   const bool half = ad->type == POLYQ_F16;
-  const Kernel k = half ? lora::shrink_of<__half>(bm, rn, trans) : lora::shrink_of<__nv_bfloat16>(bm, rn, trans);
+  const Kernel k = half ? lora::shrink_of<__half>(bm, rn, trans, any) : lora::shrink_of<__nv_bfloat16>(bm, rn, trans, any);
   const int64_t tiles = most_tiles(T, seg.n, bm), stages = K / (bm == 128 ? 64 : 128);
   int cluster = 1;
   while (cluster < lora::kMaxCluster && tiles * cluster < 2 * sms && stages >= 4 * cluster) cluster *= 2;
@@ -103,7 +107,7 @@ int shrink(const polyq_dense* x, int64_t T, int64_t K, const polyq_adapters* ad,
                                          trans ? (uint32_t)(bm == 128 ? 64 : 128) : (uint32_t)rn);
     if (rc_w) return rc_w;
   }
-  const int which = (((half * 2 + trans) * 4 + rank_index(rn)) * 4) + (bm == 16 ? 0 : bm == 64 ? 1 : 2);
+  const int which = (((half * 2 + trans) * 4 + rank_index(rn)) * 4) + (any ? 3 : bm == 16 ? 0 : bm == 64 ? 1 : 2);
   return launch(k, which, dim3((unsigned)(tiles * cluster)), lora::kThreads + (bm != 16 ? 32 : 0), cluster, &P, stream,
                 who);
 }
@@ -143,8 +147,6 @@ int expand(const float* v, int64_t T, int64_t N, const polyq_adapters* ad, bool 
                 who);
 }
 
-bool rows_on_16(const polyq_dense* d) { return (uintptr_t)d->data % 16 == 0 && d->stride % 8 == 0; }
-
 int check(const polyq_dense* x, int64_t T, const polyq_adapters* ad, const polyq_segments* s, const char* who) {
   if (!ad || !s) return polyq_set_error(POLYQ_EINVAL, "%s: adapters or segments are NULL", who);
   if (T < 1 || T > kMaxSize || ad->K < 1 || ad->K > kMaxSize || ad->N < 1 || ad->N > kMaxSize)
@@ -168,9 +170,7 @@ int check(const polyq_dense* x, int64_t T, const polyq_adapters* ad, const polyq
     return polyq_set_error(POLYQ_EINVAL, "%s: %d segments; offsets and ids must be given and aligned", who, s->n);
   int rc = polyq_check_dense(x, ad->K, who, "x");
   if (rc) return rc;
-  if (x->type != ad->type || !rows_on_16(x))
-    return polyq_set_error(POLYQ_EINVAL, "%s: x must be of the adapters' type, 16-byte aligned, with a stride that is a "
-                           "multiple of 8", who);
+  if (x->type != ad->type) return polyq_set_error(POLYQ_EINVAL, "%s: x must be of the adapters' type", who);
   return POLYQ_OK;
 }
 
@@ -238,9 +238,7 @@ extern "C" int polyq_adapters_backward(const polyq_dense* x, int64_t T, const po
   int rc = check(x, T, adapters, segments, who);
   if (!rc) rc = polyq_check_dense(dy, adapters->N, who, "dy");
   if (rc) return rc;
-  if (dy->type != adapters->type || !rows_on_16(dy))
-    return polyq_set_error(POLYQ_EINVAL, "%s: dy must be of the adapters' type, 16-byte aligned, with a stride that is a "
-                           "multiple of 8", who);
+  if (dy->type != adapters->type) return polyq_set_error(POLYQ_EINVAL, "%s: dy must be of the adapters' type", who);
   if (dx) rc = check_sum(dx, residual, adapters->K, adapters, who, "dx");
   if (rc) return rc;
   if (!dx && residual) return polyq_set_error(POLYQ_EINVAL, "%s: a residual needs a dx", who);
@@ -282,9 +280,10 @@ extern "C" int polyq_adapters_backward(const polyq_dense* x, int64_t T, const po
     G.R = adapters->R;
     G.cluster = 1;
     while (G.cluster < lora::kMaxCluster && blocks * G.cluster < 2 * sms && T >= 128 * G.cluster) G.cluster *= 2;
-    const Kernel k = half ? lora::gradients_of<__half>(rn) : lora::gradients_of<__nv_bfloat16>(rn);
-    rc = launch(k, 192 + half * 4 + rank_index(rn), dim3((unsigned)(blocks * G.cluster)), lora::kThreads, G.cluster, &G, stream,
-                who);
+    const bool any = (da && !rows_on_16(x)) || (db && !rows_on_16(dy));
+    const Kernel k = half ? lora::gradients_of<__half>(rn, any) : lora::gradients_of<__nv_bfloat16>(rn, any);
+    rc = launch(k, 256 + (any * 2 + half) * 4 + rank_index(rn), dim3((unsigned)(blocks * G.cluster)), lora::kThreads,
+                G.cluster, &G, stream, who);
     if (rc) return rc;
   }
   if (!dx) return POLYQ_OK;

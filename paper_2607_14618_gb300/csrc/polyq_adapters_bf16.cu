@@ -4,8 +4,8 @@
 
 namespace polyq {
 namespace lora {
-template Kernel shrink_of<__nv_bfloat16>(int bm, int rn, bool trans);
+template Kernel shrink_of<__nv_bfloat16>(int bm, int rn, bool trans, bool any);
 template Kernel expand_of<__nv_bfloat16>(int bm, int rn, bool trans, bool f32);
-template Kernel gradients_of<__nv_bfloat16>(int rn);
+template Kernel gradients_of<__nv_bfloat16>(int rn, bool any);
 }  // namespace lora
 }  // namespace polyq

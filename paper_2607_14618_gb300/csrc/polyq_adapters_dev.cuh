@@ -174,6 +174,27 @@ struct Mover {
     }
   }
 };
+// The same of rows that start anywhere: neighbouring elements by neighbouring threads, through
+// registers (asynchronous copies want 16 bytes, and eight loads of a piece by one thread would
+// ask L2 for its sector eight times).
+template <int ROWS, int C>
+__device__ __forceinline__ void copy_any(uint8_t* tile, const void* src, int64_t stride, int rows, int cols) {
+  constexpr int COLS = 8 * C, EACH = ROWS * COLS / kThreads, PART = EACH < 16 ? EACH : 16;
+#pragma unroll 1
+  for (int i0 = 0; i0 < EACH; i0 += PART) {
+    uint16_t v[PART];
+#pragma unroll
+    for (int i = 0; i < PART; ++i) {
+      const int e = (i0 + i) * kThreads + threadIdx.x, row = e / COLS, c = e % COLS;
+      v[i] = row < rows && c < cols ? __ldcg((const uint16_t*)src + row * stride + c) : (uint16_t)0;
+    }
+#pragma unroll
+    for (int i = 0; i < PART; ++i) {
+      const int e = (i0 + i) * kThreads + threadIdx.x, row = e / COLS, c = e % COLS;
+      *reinterpret_cast<uint16_t*>(tile + piece<C>(row, c / 8) + c % 8 * 2) = v[i];
+    }
+  }
+}
 template <int C>
 __device__ __forceinline__ uint32_t my_piece() {
   return piece<C>(threadIdx.x / C, threadIdx.x % C);
@@ -397,7 +418,8 @@ __device__ __forceinline__ void shrink_finish(const ShrinkParams& P, const Tile&
   if (P.cluster > 1) cluster_sync();  // (another block may still read this one's sums)
 }
 
-template <typename T, int BM, int RN, bool TRANS>
+// ANY: rows of x start anywhere.
+template <typename T, int BM, int RN, bool TRANS, bool ANY>
 __global__ void __launch_bounds__(kThreads) shrink_kernel(const __grid_constant__ ShrinkParams P) {
   using S = Shrink<T, BM, RN, TRANS>;
   constexpr int KC = S::KC, CX = KC / 8, CW = TRANS ? RN / 8 : KC / 8;
@@ -419,8 +441,12 @@ __global__ void __launch_bounds__(kThreads) shrink_kernel(const __grid_constant_
   Mover<BM, CX> mx(x, P.x_stride, KC, my_piece<CX>());
   auto copy_x = [&](int64_t c, int stage) {
     const int left = (int)min(P.K - c * KC, (int64_t)KC);
-    if (left < KC) mx.limit(left);  // the contraction's end
-    mx.copy(base + stage * (S::X_BYTES + S::W_BYTES), c * (KC * 2), t.rows);
+    if constexpr (ANY) {
+      copy_any<BM, CX>(smem + stage * (S::X_BYTES + S::W_BYTES), x + c * KC, P.x_stride, t.rows, left);
+    } else {
+      if (left < KC) mx.limit(left);  // the contraction's end
+      mx.copy(base + stage * (S::X_BYTES + S::W_BYTES), c * (KC * 2), t.rows);
+    }
   };
   for (int i = 0; i < S::STAGES - 1; ++i)
     if (c0 + i < c1) copy_x(c0 + i, i);
@@ -876,7 +902,7 @@ struct Grad {
 // The sums of 128 rows (fp16: of a stage's 64, which have a scale of their own) start anew and are
 // added to the block's in fp32: the tensor cores cut their running sums off, and over thousands of
 // rows that adds up (4096 rows of two adapters: 5e-6 off without it, 2.4e-6 with it).
-template <typename T, int RN>
+template <typename T, int RN, bool ANY>
 __global__ void __launch_bounds__(kThreads, RN <= 64 ? 2 : 1) gradients_kernel(const __grid_constant__ GradParams P) {
   using G = Grad<T, RN>;
   constexpr int CX = G::BC / 8, CV = RN / 8, CF = RN / 4, BT = G::BT;
@@ -905,7 +931,11 @@ __global__ void __launch_bounds__(kThreads, RN <= 64 ? 2 : 1) gradients_kernel(c
     int row, rows;
     any = any && ahead.next(P.seg, id, BT, P.cluster, row, rows);
     if (any) {
-      mx.copy(base + stage % 3 * G::X_BYTES, (int64_t)row * D.x_stride * 2, rows);
+      if constexpr (ANY)
+        copy_any<BT, CX>(smem + stage % 3 * G::X_BYTES, (const T*)D.x + (int64_t)row * D.x_stride + n0, D.x_stride, rows,
+                         (int)min(D.C - n0, (int64_t)G::BC));
+      else
+        mx.copy(base + stage % 3 * G::X_BYTES, (int64_t)row * D.x_stride * 2, rows);
       mv.copy(base + F_AT + stage % 2 * G::F_BYTES, (int64_t)row * P.R * 4, rows);
       ++asked;
     }
@@ -1030,29 +1060,27 @@ struct Kernel {
   void* f;
   int smem;
 };
-// rn: the rank rounded up to 16, 32, 64 or 128; bm: 16, 64 or (shrink, rn >= 64) 128.
+// rn: the rank rounded up to 16, 32, 64 or 128; bm: 16, 64 or (shrink, rn >= 64) 128; any: rows of
+// x start anywhere (shrink: bm 16).
 template <typename T>
-Kernel shrink_of(int bm, int rn, bool trans);
+Kernel shrink_of(int bm, int rn, bool trans, bool any);
 template <typename T>
 Kernel expand_of(int bm, int rn, bool trans, bool f32);
 template <typename T>
-Kernel gradients_of(int rn);
+Kernel gradients_of(int rn, bool any);
 
-template <typename T, int BM, int RN, bool TRANS>
-Kernel shrink_at() {
-  if constexpr (BM == 16) return Kernel{(void*)shrink_kernel<T, BM, RN, TRANS>, Shrink<T, BM, RN, TRANS>::SMEM};
-  else return Kernel{(void*)shrink_tiled_kernel<T, BM, RN, TRANS>, Tiled<T, BM, RN, TRANS>::SMEM};
-}
 template <typename T, int RN, bool TRANS>
-Kernel shrink_for(int bm) {
+Kernel shrink_for(int bm, bool any) {
   if constexpr (RN >= 64) {
-    if (bm == 128) return shrink_at<T, 128, RN, TRANS>();
+    if (bm == 128) return Kernel{(void*)shrink_tiled_kernel<T, 128, RN, TRANS>, Tiled<T, 128, RN, TRANS>::SMEM};
   }
-  return bm == 16 ? shrink_at<T, 16, RN, TRANS>() : shrink_at<T, 64, RN, TRANS>();
+  if (bm == 64) return Kernel{(void*)shrink_tiled_kernel<T, 64, RN, TRANS>, Tiled<T, 64, RN, TRANS>::SMEM};
+  return Kernel{any ? (void*)shrink_kernel<T, 16, RN, TRANS, true> : (void*)shrink_kernel<T, 16, RN, TRANS, false>,
+                Shrink<T, 16, RN, TRANS>::SMEM};
 }
 template <typename T, int RN>
-Kernel shrink_for(int bm, bool trans) {
-  return trans ? shrink_for<T, RN, true>(bm) : shrink_for<T, RN, false>(bm);
+Kernel shrink_for(int bm, bool trans, bool any) {
+  return trans ? shrink_for<T, RN, true>(bm, any) : shrink_for<T, RN, false>(bm, any);
 }
 template <typename T, int BM, int RN, bool TRANS>
 Kernel expand_at(bool f32) {
@@ -1065,11 +1093,11 @@ Kernel expand_for(int bm, bool trans, bool f32) {
   return trans ? expand_at<T, 64, RN, true>(f32) : expand_at<T, 64, RN, false>(f32);
 }
 template <typename T>
-Kernel shrink_of(int bm, int rn, bool trans) {
-  return rn == 16   ? shrink_for<T, 16>(bm, trans)
-         : rn == 32 ? shrink_for<T, 32>(bm, trans)
-         : rn == 64 ? shrink_for<T, 64>(bm, trans)
-                    : shrink_for<T, 128>(bm, trans);
+Kernel shrink_of(int bm, int rn, bool trans, bool any) {
+  return rn == 16   ? shrink_for<T, 16>(bm, trans, any)
+         : rn == 32 ? shrink_for<T, 32>(bm, trans, any)
+         : rn == 64 ? shrink_for<T, 64>(bm, trans, any)
+                    : shrink_for<T, 128>(bm, trans, any);
 }
 template <typename T>
 Kernel expand_of(int bm, int rn, bool trans, bool f32) {
@@ -1079,12 +1107,15 @@ Kernel expand_of(int bm, int rn, bool trans, bool f32) {
                     : expand_for<T, 128>(bm, trans, f32);
 }
 template <typename T, int RN>
-Kernel gradients_at() {
-  return Kernel{(void*)gradients_kernel<T, RN>, Grad<T, RN>::SMEM};
+Kernel gradients_at(bool any) {
+  return Kernel{any ? (void*)gradients_kernel<T, RN, true> : (void*)gradients_kernel<T, RN, false>, Grad<T, RN>::SMEM};
 }
 template <typename T>
-Kernel gradients_of(int rn) {
-  return rn == 16 ? gradients_at<T, 16>() : rn == 32 ? gradients_at<T, 32>() : rn == 64 ? gradients_at<T, 64>() : gradients_at<T, 128>();
+Kernel gradients_of(int rn, bool any) {
+  return rn == 16   ? gradients_at<T, 16>(any)
+         : rn == 32 ? gradients_at<T, 32>(any)
+         : rn == 64 ? gradients_at<T, 64>(any)
+                    : gradients_at<T, 128>(any);
 }
 
 }  // namespace lora

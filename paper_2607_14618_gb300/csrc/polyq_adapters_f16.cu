@@ -4,8 +4,8 @@
 
 namespace polyq {
 namespace lora {
-template Kernel shrink_of<__half>(int bm, int rn, bool trans);
+template Kernel shrink_of<__half>(int bm, int rn, bool trans, bool any);
 template Kernel expand_of<__half>(int bm, int rn, bool trans, bool f32);
-template Kernel gradients_of<__half>(int rn);
+template Kernel gradients_of<__half>(int rn, bool any);
 }  // namespace lora
 }  // namespace polyq

@@ -185,12 +185,12 @@ def test_bad_segments(polyq_lib, bad, back):
 
 
 @pytest.mark.parametrize("back", [False, True])
-@pytest.mark.parametrize("bad", BAD + [dict(type=0), dict(type=2), dict(stride=132), dict(data=A + 8)])
+@pytest.mark.parametrize("bad", BAD + [dict(type=0), dict(type=2)])
 def test_adapters_of_a_bad_tensor(polyq_lib, bad, back):
     d = _dense(polyq_lib, **bad)
     assert _lora(polyq_lib, back, x=d) == EINVAL
     if back:
-        if bad != dict(stride=127):  # (127 holds the 64 columns of dy, but is no multiple of 8)
+        if bad != dict(stride=127):  # (127 holds the 64 columns of dy)
             assert _lora(polyq_lib, True, dy=d) == EINVAL
         assert _lora(polyq_lib, True, dy=_dense(polyq_lib, stride=60)) == EINVAL
     if bad in BAD[:2] + BAD[4:]:

@@ -19,15 +19,15 @@ def within(got, ref, bound, what, rows=None):
     assert (over <= 0).all(), f"{what}: {(over > 0).sum()} off, worst {over.max():.3g} over the bound"
 
 
-def make(T, K, N, R, n, dtype, seed=0, pad=0, out=None, x_scale=1.0):
+def make(T, K, N, R, n, dtype, seed=0, pad=0, out=None, x_scale=1.0, xpad=None):
     g = torch.Generator("cuda").manual_seed(seed)
 
     def rnd(*s):
         return torch.randn(*s, generator=g, device="cuda")
 
-    x = dense(T, K, dtype, (-K) % 8 + 8 * pad)
+    x = dense(T, K, dtype, (-K) % 8 + 8 * pad if xpad is None else xpad[0], 0 if xpad is None else xpad[1])
     x.copy_(rnd(T, K) * x_scale)
-    dy = dense(T, N, dtype, (-N) % 8 + 8 * pad)
+    dy = dense(T, N, dtype, (-N) % 8 + 8 * pad if xpad is None else xpad[0], 0 if xpad is None else xpad[1])
     dy.copy_(rnd(T, N))
     a = torch.zeros(n, R, K + (-K) % 8 + 8 * pad, dtype=dtype, device="cuda")[:, :, :K]
     a.copy_(rnd(n, R, K) * K ** -0.5)
@@ -42,9 +42,10 @@ def segments(lengths, first=0):
 
 
 def run(polyq, lengths, ids, T, K, N, R, n, dtype=torch.bfloat16, out=None, dxt=None, gt=torch.float32, ranks=None,
-        pad=0, ypad=0, first=0, seed=0, in_place=False, train=True, x_scale=1.0, residual=True):
+        pad=0, ypad=0, first=0, seed=0, in_place=False, train=True, x_scale=1.0, residual=True,
+        xpad=None):
     out, dxt = out or dtype, dxt or dtype
-    x, a, b, dy, y0, dx0 = make(T, K, N, R, n, dtype, seed, pad, x_scale=x_scale)
+    x, a, b, dy, y0, dx0 = make(T, K, N, R, n, dtype, seed, pad, x_scale=x_scale, xpad=xpad)
     off, d_off = segments(lengths, first)
     d_ids = torch.tensor(ids, dtype=torch.int32, device="cuda")
     r = np.random.default_rng(seed)
@@ -125,6 +126,16 @@ def test_strides(polyq_lib, pad, ypad):
     for lengths in ([3, 4], [70, 90]):
         run(polyq_lib, lengths, [0, 1], sum(lengths), 200, 304, 24, 2, pad=pad, ypad=ypad)
         run(polyq_lib, lengths, [0, 1], sum(lengths), 200, 304, 24, 2, pad=pad, ypad=ypad, out=torch.float32)
+
+
+@pytest.mark.parametrize("dtype", list(T16))
+@pytest.mark.parametrize("R", [8, 32, 64, 128])
+@pytest.mark.parametrize("K,N,xpad", [(1000, 321, (0, 0)), (133, 1001, (0, 0)), (64, 128, (1, 0)), (64, 128, (0, 1)),
+                                      (200, 135, (3, 5))])
+def test_rows_that_start_anywhere(polyq_lib, K, N, xpad, R, dtype):
+    """x and dy of odd widths without gaps, and of buffers that start on any element."""
+    for lengths, ids in (([9, 1, 14], [1, 0, -1]), ([150, 70, 33], [0, 1, 0])):
+        run(polyq_lib, lengths, ids, sum(lengths) + 2, K, N, R, 2, T16[dtype], xpad=xpad, ranks=[R, max(1, R - 3)])
 
 
 @pytest.mark.parametrize("lengths", [[3, 4, 2], [70, 90, 10]])

@@ -232,7 +232,8 @@ def test_tensors_that_do_not_fit(polyq_lib):
             call()
     # alignment, types of outputs, workspaces: the library's own checks
     wide = torch.zeros(6, 72, dtype=torch.bfloat16, device="cuda")
-    for call in (lambda: fwd(wide[:, 1:65], a, b, off, ids), lambda: fwd(x, a, b, off, ids, dtype=torch.float16),
+    for call in (lambda: fwd(x, wide[None, :2, 1:65].expand(2, 2, 64), b[:, :, :2], off, ids),
+                 lambda: fwd(x, a, b, off, ids, dtype=torch.float16),
                  lambda: fwd(x, a, b, off, ids, workspace=torch.zeros(300, dtype=torch.uint8, device="cuda")),
                  lambda: fwd(x[:0], a, b, off, ids), lambda: fwd(x, a, b, off[:1], ids[:0])):
         with pytest.raises(polyq_lib.PolyqError):
