@@ -41,6 +41,11 @@ __device__ __forceinline__ void to_float(const Raw8<T>& r, float (&v)[8]) {
 }
 
 // Element i of an array of any type.
+__device__ __forceinline__ float any_load(const void* p, int type, int64_t i) {
+  if (type == POLYQ_F32) return __ldcg((const float*)p + i);
+  const uint16_t h = __ldcg((const uint16_t*)p + i);
+  return type == POLYQ_BF16 ? __uint_as_float((uint32_t)h << 16) : __half2float(__ushort_as_half(h));
+}
 __device__ __forceinline__ void any_store(void* p, int type, int64_t i, float v) {
   if (type == POLYQ_F32) ((float*)p)[i] = v;
   else if (type == POLYQ_BF16) ((__nv_bfloat16*)p)[i] = Elem<__nv_bfloat16>::from(v);

@@ -49,7 +49,7 @@ struct NormParams {
   int rows, K;
   float eps, inv_k;
   int w_type, b_type, vec_w, vec_b;  // vec: on 16 bytes
-  int center, cluster, depth, want_w, want_b;
+  int center, cluster, depth, staged, want_w, want_b;
 };
 
 __device__ __forceinline__ uint32_t cluster_rank() {
@@ -180,39 +180,32 @@ __device__ __forceinline__ void clear(F2 (&v)[4], uint32_t mask) {
   }
 }
 
-// A thread's eight elements of a row, on their way to its own place in shared
-// memory (VEC; no other thread reads it, so that no barrier is needed), or loaded when
-// they are read.
-template <typename T, bool VEC>
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src, int bytes) {  // the rest of 16: zeros
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+
+// A thread's eight elements of a row, on their way to its own place in shared memory (VEC; no
+// other thread reads it, so that no barrier is needed).
+template <typename T>
 struct Rows {
   uint32_t at, piece;  // this thread's place, and bytes from one 16-byte piece to the next
   static constexpr int N16 = sizeof(T) * 8 / 16;
   __device__ __forceinline__ void ask(const T* row, int col, uint32_t mask, uint32_t slot) const {
-    if constexpr (VEC) {
-      const int have = __popc(mask) * (int)sizeof(T);  // (the row's end: the rest is zeros)
+    const int have = __popc(mask) * (int)sizeof(T);  // (the row's end: the rest is zeros)
 #pragma unroll
-      for (int i = 0; i < N16; ++i) {
-        const int bytes = min(max(have - 16 * i, 0), 16);
-        const T* src = bytes ? row + col + i * (16 / (int)sizeof(T)) : row;
-        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(at + slot + i * piece), "l"(src),
-                     "r"(bytes)
-                     : "memory");
-      }
+    for (int i = 0; i < N16; ++i) {
+      const int bytes = min(max(have - 16 * i, 0), 16);
+      copy16(at + slot + i * piece, bytes ? row + col + i * (16 / (int)sizeof(T)) : row, bytes);
     }
   }
-  __device__ __forceinline__ void get(const T* row, int col, int step, uint32_t mask, uint32_t slot,
-                                      F2 (&v)[4]) const {
+  __device__ __forceinline__ void get(uint32_t slot, F2 (&v)[4]) const {
     Raw8<T> r;
-    if constexpr (VEC) {
 #pragma unroll
-      for (int i = 0; i < N16; ++i)
-        asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
-                     : "=r"(r.w[i].x), "=r"(r.w[i].y), "=r"(r.w[i].z), "=r"(r.w[i].w)
-                     : "r"(at + slot + i * piece)
-                     : "memory");
-    } else {
-      load8<false>(row, col, step, mask, r);
-    }
+    for (int i = 0; i < N16; ++i)
+      asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
+                   : "=r"(r.w[i].x), "=r"(r.w[i].y), "=r"(r.w[i].z), "=r"(r.w[i].w)
+                   : "r"(at + slot + i * piece)
+                   : "memory");
     pairs(r, v);
   }
   __device__ __forceinline__ void put(uint32_t slot, const F2 (&v)[4]) const {
@@ -225,14 +218,56 @@ struct Rows {
     }
   }
 };
+// A row that starts anywhere (not VEC): the 16-byte pieces of memory that hold it, copied by the
+// row's threads together, of which each reads every T-th element; a barrier of theirs lies
+// between.  A row begins up to 15 bytes into its place.  Nothing outside the tensor is read:
+// before its first element (`first`) the piece is copied by elements, and none goes past the row.
+template <typename T>
+struct AnyRow {
+  static __host__ __device__ constexpr uint32_t bytes(int cols) { return (cols * (uint32_t)sizeof(T) + 30) / 16 * 16; }
+  static __device__ __forceinline__ void ask(const T* row, int cols, const void* first, uint32_t place) {
+    const uintptr_t from = (uintptr_t)row, to = from + cols * sizeof(T), base = from & ~(uintptr_t)15;
+    for (int i = threadIdx.x; base + 16 * i < to; i += blockDim.x) {
+      const uintptr_t src = base + 16 * i;
+      if (src >= (uintptr_t)first) {
+        copy16(place + 16 * i, (const void*)src, (int)min((uintptr_t)16, to - src));
+      } else {
+        for (uintptr_t q = from; q < min(src + 16, to); q += sizeof(T)) {
+          const uint32_t dst = place + (uint32_t)(q - base);
+          if (sizeof(T) == 4) asm volatile("st.shared.u32 [%0], %1;" ::"r"(dst), "r"(__ldcg((const uint32_t*)q)) : "memory");
+          else asm volatile("st.shared.u16 [%0], %1;" ::"r"(dst), "h"(__ldcg((const uint16_t*)q)) : "memory");
+        }
+      }
+    }
+  }
+  // Elements col, col + step, ... of the row (those of `mask`).
+  static __device__ __forceinline__ void get(const T* row, uint32_t place, int col, int step, uint32_t mask, F2 (&v)[4]) {
+    const uint32_t at = place + (uint32_t)((uintptr_t)row & 15);
+    Raw8<T> r;
+    T* e = reinterpret_cast<T*>(r.w);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const uint32_t src = at + (mask >> i & 1 ? (uint32_t)(col + i * step) * (uint32_t)sizeof(T) : 0u);
+      if constexpr (sizeof(T) == 4) {
+        float f;
+        asm volatile("ld.shared.f32 %0, [%1];" : "=f"(f) : "r"(src) : "memory");
+        e[i] = mask >> i & 1 ? f : 0.f;
+      } else {
+        uint16_t h;
+        asm volatile("ld.shared.u16 %0, [%1];" : "=h"(h) : "r"(src) : "memory");
+        h = mask >> i & 1 ? h : (uint16_t)0;
+        e[i] = *reinterpret_cast<const T*>(&h);
+      }
+    }
+    pairs(r, v);
+  }
+};
 
-// Asks for the rows that are depth - 1 (1 to 3) stages ahead and waits for those of `stage`.
-template <typename Ask>
-__device__ __forceinline__ void next_stage(int depth, int stage, Ask ask) {
-  const int there = stage == 0 ? depth - 1 : stage - 1;
-  ask(there);
-  if (depth == 2) asm volatile("cp.async.wait_group 1;" ::: "memory");
-  else if (depth == 3) asm volatile("cp.async.wait_group 2;" ::: "memory");
+// Waits for all but the last `left` (0 to 3) stages that have been asked for.
+__device__ __forceinline__ void wait_stages(int left) {
+  if (left == 0) asm volatile("cp.async.wait_group 0;" ::: "memory");
+  else if (left == 1) asm volatile("cp.async.wait_group 1;" ::: "memory");
+  else if (left == 2) asm volatile("cp.async.wait_group 2;" ::: "memory");
   else asm volatile("cp.async.wait_group 3;" ::: "memory");
 }
 
@@ -283,15 +318,20 @@ __global__ void __maxnreg__(kForwardRegs) norm_forward_kernel(const __grid_const
   pdl_trigger();
   pdl_wait();
   const int plane = (K + 7) / 8;
+  const uint32_t ring = smem_u32(smem) + (VEC || P.staged ? ((P.w ? 2 : 0) + (P.b ? 2 : 0)) * plane * 16u : 0u);
   const uint32_t slot = blockDim.x * R * 8 * sizeof(TX);  // of a piece of all threads
-  const Rows<TX, VEC> ring{smem_u32(smem) + ((P.w ? 2 : 0) + (P.b ? 2 : 0)) * plane * 16u +
-                               (threadIdx.y * blockDim.x + threadIdx.x) * 16u,
-                           (uint32_t)(blockDim.x * R * 16)};
+  const Rows<TX> mine{ring + (threadIdx.y * blockDim.x + threadIdx.x) * 16u, (uint32_t)(blockDim.x * R * 16)};
+  const uint32_t any_slot = AnyRow<TX>::bytes(K);
+  auto any_place = [&](int stage) { return ring + (uint32_t)(stage * R + threadIdx.y) * any_slot; };
   auto ask = [&](int row, int stage) {
-    if (VEC && row < P.rows) {
+    if (row < P.rows) {
       const TX* x = (const TX*)P.x + (int64_t)row * P.x_stride;
+      if constexpr (VEC) {
 #pragma unroll
-      for (int j = 0; j < C; ++j) ring.ask(x, c0 + j * next, j < C - 1 ? 0xFFu : last, (stage * C + j) * slot);
+        for (int j = 0; j < C; ++j) mine.ask(x, c0 + j * next, j < C - 1 ? 0xFFu : last, (stage * C + j) * slot);
+      } else {
+        AnyRow<TX>::ask(x, K, P.x, any_place(stage));
+      }
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
   };
@@ -302,7 +342,7 @@ __global__ void __maxnreg__(kForwardRegs) norm_forward_kernel(const __grid_const
 #pragma unroll 1
   for (int which = 0; which < 2; ++which) {
     const void* p = which ? P.b : P.w;
-    if (!p) continue;
+    if (!p || (!VEC && !P.staged)) continue;
     float4* to = which ? sb : sw;
     for (int i = threadIdx.y * blockDim.x + threadIdx.x; i < plane; i += blockDim.x * R) {
       F2 v[4];
@@ -313,9 +353,18 @@ __global__ void __maxnreg__(kForwardRegs) norm_forward_kernel(const __grid_const
     }
   }
   __syncthreads();
-  // Four columns of a piece (its half h) from a staged vector.
-  auto staged4 = [&](const float4* at, int col, int h, F2& v0, F2& v1) {
-    if (VEC) {
+  // Four columns of a piece (its half h) from a staged vector (or, not VEC, of rows so wide that
+  // it has no room beside them, from L2).
+  auto staged4 = [&](const float4* at, const void* p, int type, int col, int h, F2& v0, F2& v1) {
+    if (!VEC && !P.staged) {
+      float f[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int c = col + 32 * (4 * h + e);
+        f[e] = c < K ? any_load(p, type, c) : 0.f;
+      }
+      v0 = f2(f[0], f[1]), v1 = f2(f[2], f[3]);
+    } else if (VEC) {
       const float4 x = at[h * plane + col / 8];
       v0 = f2(x.x, x.y), v1 = f2(x.z, x.w);
     } else {
@@ -346,12 +395,20 @@ __global__ void __maxnreg__(kForwardRegs) norm_forward_kernel(const __grid_const
   };
   for (int stage = 0; row < P.rows; row += gridDim.x * R, stage ^= 1) {
     ask(row + gridDim.x * R, stage ^ 1);
-    asm volatile("cp.async.wait_group 1;" ::: "memory");
+    wait_stages(1);
+    if (!VEC) {  // (the row's pieces come from all of its threads)
+      if (W == 1) __syncwarp();
+      else asm volatile("bar.sync %0, %1;" ::"r"((int)threadIdx.y + 1), "r"((int)blockDim.x) : "memory");
+    }
     F2 v[C][4];
 #pragma unroll
-    for (int j = 0; j < C; ++j)
-      ring.get((const TX*)P.x + (int64_t)row * P.x_stride, c0 + j * next, 32, j < C - 1 ? 0xFFu : last,
-               (stage * C + j) * slot, v[j]);
+    for (int j = 0; j < C; ++j) {
+      if constexpr (VEC) mine.get((stage * C + j) * slot, v[j]);
+      else
+        AnyRow<TX>::get((const TX*)P.x + (int64_t)row * P.x_stride, any_place(stage), c0 + j * next, 32,
+                        j < C - 1 ? 0xFFu : last, v[j]);
+    }
+    if (!VEC && W == 1) __syncwarp();  // (read before the next but one is asked for)
     float mean = 0.f;
     if (P.center) {
       F2 s = v[0][0];
@@ -381,8 +438,8 @@ __global__ void __maxnreg__(kForwardRegs) norm_forward_kernel(const __grid_const
       for (int h = 0; h < 2; ++h) {
         F2 &x0 = v[j][2 * h], &x1 = v[j][2 * h + 1], w0, w1, b0, b1;
         x0 = mul2(x0, r), x1 = mul2(x1, r);
-        if (P.w) staged4(sw, col, h, w0, w1);
-        if (P.b) staged4(sb, col, h, b0, b1);
+        if (P.w) staged4(sw, P.w, P.w_type, col, h, w0, w1);
+        if (P.b) staged4(sb, P.b, P.b_type, col, h, b0, b1);
         if (P.w && P.b) x0 = fma2(x0, w0, b0), x1 = fma2(x1, w1, b1);
         else if (P.w) x0 = mul2(x0, w0), x1 = mul2(x1, w1);
         else if (P.b) x0 = add2(x0, b0), x1 = add2(x1, b1);
@@ -412,30 +469,43 @@ __global__ void __maxnreg__(kBackwardRegs) norm_backward_kernel(
   if (P.cluster > 1) cluster_sync();
   const int blocks_all = gridDim.x / P.cluster, mine = blockIdx.x / P.cluster, step = blocks_all * R * NR;
   int row0 = mine * R * NR + threadIdx.y;
-  const uint32_t x_group = T * R * 8 * sizeof(TX), d_group = T * R * 8 * sizeof(TY);
-  const uint32_t d_at = G * x_group, r_at = d_at + G * d_group, slots = r_at + (P.res ? G * x_group : 0);
-  const Rows<TX, VEC> x{smem_u32(ring) + me * 16u, (uint32_t)(T * R * 16)};
-  const Rows<TY, VEC> dy{x.at, x.piece};
+  // VEC: groups of x, of dy and of the residual, of all threads; else rows, R of each
+  const int c0 = rank * T * 8 * G, cols = min(T * 8 * G, P.K - c0);  // this block's columns
+  const uint32_t x_group = VEC ? T * R * 8 * sizeof(TX) : AnyRow<TX>::bytes(T * 8 * G);
+  const uint32_t d_group = VEC ? T * R * 8 * sizeof(TY) : AnyRow<TY>::bytes(T * 8 * G);
+  const uint32_t d_at = (VEC ? G : R) * x_group, r_at = d_at + (VEC ? G : R) * d_group;
+  const uint32_t slots = r_at + (P.res ? (VEC ? G : R) * x_group : 0);
+  const Rows<TX> x{smem_u32(ring) + me * 16u, (uint32_t)(T * R * 16)};
+  const Rows<TY> dy{x.at, x.piece};
+  auto x_row = [&](int row) { return (const TX*)P.x + (int64_t)row * P.x_stride + (VEC ? 0 : c0); };
+  auto d_row = [&](int row) { return (const TY*)P.dy + (int64_t)row * P.dy_stride + (VEC ? 0 : c0); };
+  auto r_row = [&](int row) { return (const TX*)P.res + (int64_t)row * P.res_stride + (VEC ? 0 : c0); };
+  auto any_place = [&](uint32_t slot, uint32_t part, uint32_t size) { return smem_u32(ring) + slot + part + threadIdx.y * size; };
   auto ask = [&](int from, int stage) {
 #pragma unroll
     for (int i = 0; i < NR; ++i) {
       const int row = from + i * R;
       if (row < P.rows) {
         const uint32_t slot = (stage * NR + i) * slots;
+        if constexpr (VEC) {
 #pragma unroll
-        for (int g = 0; g < G; ++g) {
-          x.ask((const TX*)P.x + (int64_t)row * P.x_stride, at.col[g], at.mask[g], slot + g * x_group);
-          dy.ask((const TY*)P.dy + (int64_t)row * P.dy_stride, at.col[g], at.mask[g], slot + d_at + g * d_group);
-          if (P.res) x.ask((const TX*)P.res + (int64_t)row * P.res_stride, at.col[g], at.mask[g], slot + r_at + g * x_group);
+          for (int g = 0; g < G; ++g) {
+            x.ask(x_row(row), at.col[g], at.mask[g], slot + g * x_group);
+            dy.ask(d_row(row), at.col[g], at.mask[g], slot + d_at + g * d_group);
+            if (P.res) x.ask(r_row(row), at.col[g], at.mask[g], slot + r_at + g * x_group);
+          }
+        } else {
+          AnyRow<TX>::ask(x_row(row), cols, P.x, any_place(slot, 0, x_group));
+          AnyRow<TY>::ask(d_row(row), cols, P.dy, any_place(slot, d_at, d_group));
+          if (P.res) AnyRow<TX>::ask(r_row(row), cols, P.res, any_place(slot, r_at, x_group));
         }
       }
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
   };
-  if (VEC)
-    for (int i = 0; i < P.depth - 1; ++i) ask(row0 + i * step, i);
+  for (int i = 0; i < P.depth - 1; ++i) ask(row0 + i * step, i);
   F2 dw[G][4], db[G][4];
-  const Rows<float, true> weight{x.at + P.depth * NR * slots, x.piece};  // this thread's eight of each group
+  const Rows<float> weight{x.at + P.depth * NR * slots, x.piece};  // this thread's eight of each group
 #pragma unroll
   for (int g = 0; g < G; ++g) {
     F2 w[4] = {f2(1.f, 1.f), f2(1.f, 1.f), f2(1.f, 1.f), f2(1.f, 1.f)};
@@ -455,15 +525,28 @@ __global__ void __maxnreg__(kBackwardRegs) norm_backward_kernel(
   };
   stats_of(row0);
   for (int stage = 0; row0 - (int)threadIdx.y < P.rows; row0 += step) {
-    if (VEC) next_stage(P.depth, stage, [&](int there) { ask(row0 + (P.depth - 1) * step, there); });
+    const int there = stage == 0 ? P.depth - 1 : stage - 1;
+    if (VEC) {
+      ask(row0 + (P.depth - 1) * step, there);
+      wait_stages(P.depth - 1);
+    } else {
+      wait_stages(P.depth - 2);
+      __syncthreads();  // the pieces of all threads are here, and the rows before have been read
+      ask(row0 + (P.depth - 1) * step, there);
+    }
     // hat and the gradient of a row's columns, zeros where there is no element (what the loads
     // give there is anything).  They are read again after the sums: the registers are the
     // weights' and sums'.
     auto read = [&](int i, int g, F2(&h)[4], F2(&d)[4]) {
       const int row = row0 + i * R;
       const uint32_t m = row < P.rows ? at.mask[g] : 0u, slot = (stage * NR + i) * slots;
-      x.get((const TX*)P.x + (int64_t)row * P.x_stride, at.col[g], T, m, slot + g * x_group, h);
-      dy.get((const TY*)P.dy + (int64_t)row * P.dy_stride, at.col[g], T, m, slot + d_at + g * d_group, d);
+      if constexpr (VEC) {
+        x.get(slot + g * x_group, h);
+        dy.get(slot + d_at + g * d_group, d);
+      } else {
+        AnyRow<TX>::get(x_row(row), any_place(slot, 0, x_group), at.col[g] - c0, T, m, h);
+        AnyRow<TY>::get(d_row(row), any_place(slot, d_at, d_group), at.col[g] - c0, T, m, d);
+      }
       const F2 minus = f2(-stat[i].x, -stat[i].x), r = f2(stat[i].y, stat[i].y);
 #pragma unroll
       for (int e = 0; e < 4; ++e) h[e] = mul2(add2(h[e], minus), r);
@@ -480,7 +563,7 @@ __global__ void __maxnreg__(kBackwardRegs) norm_backward_kernel(
       for (int g = 0; g < G; ++g) {
         F2 h[4], d[4], w[4];
         read(i, g, h, d);
-        weight.get(nullptr, 0, 0, 0u, g * T * R * 32, w);
+        weight.get(g * T * R * 32, w);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           dw[g][e] = fma2(d[e], h[e], dw[g][e]);
@@ -505,10 +588,12 @@ __global__ void __maxnreg__(kBackwardRegs) norm_backward_kernel(
         for (int g = 0; g < G; ++g) {
           F2 h[4], d[4], w[4], a[4] = {f2(0.f, 0.f), f2(0.f, 0.f), f2(0.f, 0.f), f2(0.f, 0.f)};
           read(i, g, h, d);
-          weight.get(nullptr, 0, 0, 0u, g * T * R * 32, w);
-          if (P.res)
-            x.get((const TX*)P.res + (int64_t)row * P.res_stride, at.col[g], T, at.mask[g],
-                  (stage * NR + i) * slots + r_at + g * x_group, a);
+          weight.get(g * T * R * 32, w);
+          if (P.res) {
+            const uint32_t slot = (stage * NR + i) * slots;
+            if constexpr (VEC) x.get(slot + r_at + g * x_group, a);
+            else AnyRow<TX>::get(r_row(row), any_place(slot, r_at, x_group), at.col[g] - c0, T, at.mask[g], a);
+          }
 #pragma unroll
           for (int e = 0; e < 4; ++e) d[e] = fma2(r, fma2(h[e], mgh2, fma2(d[e], w[e], mg2)), a[e]);
           store_pairs<VEC>((TX*)P.y + (int64_t)row * P.y_stride, at.col[g], T, at.mask[g], d);
@@ -580,7 +665,7 @@ Shape backward_shape(int64_t rows, int64_t K, int bytes, int sms) {
   Shape s;
   s.groups = K <= kNarrow ? 1 : 2;
   s.cluster = 1;
-  const int most_cols = std::min(16 * kWideThreads, kMostSmem / (2 * bytes + 4) / 512 * 512);
+  const int most_cols = std::min(16 * kWideThreads, (kMostSmem - 512) / (2 * bytes + 4) / 512 * 512);
   while ((int64_t)s.cluster * most_cols < K) s.cluster *= 2;
   const int64_t cols = (K + s.cluster - 1) / s.cluster, warp = 256 * s.groups;
   s.threads = (int)((cols + warp - 1) / warp * 32);
@@ -731,10 +816,13 @@ extern "C" int polyq_layernorm_forward(const polyq_dense* x, int64_t rows, int64
   bool vec = rows_on_16(x) && rows_on_16(y);
   ForwardShape s = forward_shape(rows, K, vec, sms);
   int smem = (int)(K + 7) / 8 * 32 * ((weight != nullptr) + (bias != nullptr));
-  if (vec) {
-    const int row = 2 * s.warps * s.c * 256 * (x->type == POLYQ_F32 ? 4 : 2);
-    if (smem + row > kMostSmem) vec = false, s = forward_shape(rows, K, vec, sms);
-    else s.rows = std::min(s.rows, (kMostSmem - smem) / row), smem += s.rows * row;
+  {  // two rows of each that lie side by side, on their way
+    const int xb = x->type == POLYQ_F32 ? 4 : 2, any = ((int)K * xb + 30) / 16 * 16;
+    if (vec && smem + 2 * s.warps * s.c * 256 * xb > kMostSmem) vec = false, s = forward_shape(rows, K, vec, sms);
+    const int row = 2 * (vec ? s.warps * s.c * 256 * xb : any);  // (at most 196 640 bytes)
+    P.staged = smem + row <= kMostSmem;
+    if (!P.staged) smem = 0;
+    s.rows = std::min(s.rows, (kMostSmem - smem) / row), smem += s.rows * row;
   }
   const Variant v{false, vec, 1, s.c};
   void* f = pick(x->type, y->type, v);
@@ -809,11 +897,12 @@ extern "C" int polyq_layernorm_backward(const polyq_dense* x, int64_t rows, int6
   P.want_b = dbias != nullptr;
   const bool vec = rows_on_16(x) && rows_on_16(dy) && (!residual || rows_on_16(residual)) && (!dx || rows_on_16(dx));
   const int cols = s.threads * s.rows * s.groups * 8;
-  int nr = s.nr, stage = vec ? cols * bytes * nr : 0;
+  const int slack = 32 * 3 * s.rows;  // of rows that start anywhere
+  int nr = s.nr, stage = (cols * bytes + (vec ? 0 : slack)) * nr;
   if (2 * stage + cols * 4 > kMostSmem) stage /= nr, nr = 1;
   const Variant v{true, vec, nr, s.groups};
   void* f = pick(x->type, dy->type, v);
-  P.depth = vec ? std::max(2, std::min(4, (kRingBytes - cols * 4) / stage)) : 0;
+  P.depth = std::max(2, std::min(4, (kRingBytes - cols * 4) / stage));
   const int smem = stage * P.depth + cols * 4;
   if (smem > 32 << 10) rc = allow_smem(f, v.index(x->type, dy->type), who);
   if (rc) return rc;
