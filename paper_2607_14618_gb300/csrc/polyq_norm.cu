@@ -4,13 +4,19 @@
 //   g = dy w,  dx = res + rstd (g - mean(g) - hat mean(g hat))
 //   dw = sum over rows of dy hat,  db = sum over rows of dy
 //
-// Bound by HBM: x in and y out (forward), x, dy (and a residual gradient) in and
-// dx out (backward), each once.  A row lies in the registers of a group of
-// threads, eight elements each, so that the sums over it and its result need one
-// reading; the next row's loads are in flight meanwhile.  A group keeps the
-// weight, and in the backward pass its rows' sums for dw and db, in registers
-// from row to row.  Rows wider than a thread block are shared by a cluster,
-// whose blocks exchange the sums through distributed shared memory.
+// What has to move is x in and y out (forward), x, dy (and a residual gradient) in and dx
+// out (backward), each once: 8192 x 5120 bf16 are 25 and 37 us of HBM.  A row's elements
+// stay in registers or shared memory between the sums over them and its result, so that they
+// are read once; the next rows are on their way meanwhile.  Forward and backward share rows
+// out differently (see the kernels): the forward keeps a row in registers, the weight in
+// shared memory; the backward keeps the rows' sums for dw and db in registers, and rows and
+// weight in shared memory.  Rows that start anywhere come as the 16-byte pieces that hold
+// them (fp32 3551 x 11811, training: 330 us, 508 with element loads).
+//
+// Measured, forward and backward with the residual gradient (by the profiler, operands from
+// HBM): 8192 x 5120 bf16 33 + 80 + 4.3 us, 5.1 and 4.2 TB/s, bound by instructions: 20 for an
+// element forward, 38 backward, in packed fp32 pairs.  1001 x 4100: 12.8 + 18.8 + 4.6 us,
+// bound by the latency of three launches.  One row: 3.2 us, a launch.
 #include <algorithm>
 #include <atomic>
 #include <cmath>
@@ -304,7 +310,9 @@ struct Columns {
 
 // Forward: W warps hold a row in registers as fp32 (threadIdx.x), C pieces of eight columns
 // a lane; rows side by side (threadIdx.y) share a block, which keeps the weight and bias in
-// shared memory as fp32.  The next row is on its way to shared memory meanwhile (VEC).  All
+// shared memory as fp32 (from L2 for each row they were the L2's bound: 2048 x 5120 RMS norm
+// 42 us, 37 now).  The next row is on its way to shared memory meanwhile.  The variance is of
+// the differences from the mean, not of squares: nothing cancels.  All
 // pieces but a lane's last are whole (W follows from that), so that the others need no checks.
 constexpr int kForwardWarps = 24, kForwardRegs = 64;
 
