@@ -181,8 +181,9 @@ int polyq_adapters_workspace_bytes(int64_t T, int32_t R, size_t* bytes);
  * adapters' type (fastest where it is 16-byte aligned with a stride that is a multiple of 8); y
  * [T][N] of that type or POLYQ_F32; residual NULL (0) or of y's type: the projection's result, its
  * data may be y's, with y's stride.  Products of x and a are exact and their sums in
- * fp32, as v is; v enters the second product with 16 (bf16) or 21 (fp16) significant
- * bits; one rounding to y's type.  saved: NULL, or device memory of T*R floats, 16-byte
+ * fp32, as v is; v enters the second product with 16 (bf16) or 21 (fp16: down to 2^-17 of
+ * its row's largest finite magnitude, from there on to 2^-39 of that) significant bits; one
+ * rounding to y's type.  saved: NULL, or device memory of T*R floats, 16-byte
  * aligned, which receives v [T][R] for the backward pass (rows without an adapter are left
  * as they were).  Two launches. */
 int polyq_adapters_forward(const polyq_dense* x, int64_t T, const polyq_adapters* adapters,
@@ -199,7 +200,8 @@ int polyq_adapters_forward(const polyq_dense* x, int64_t T, const polyq_adapters
  * projection); da [n][R][K] and db [n][N][R] without gaps, of grad_type (the adapters'
  * type or POLYQ_F32), each may be NULL.  All adapters' gradients are written: zeros where no row
  * has the adapter, and past its rank.  At least one of the three is wanted; saved
- * may be NULL without db.  dv is in fp32, and enters its products as v does.  Up to three
+ * may be NULL without db.  dv is in fp32, and enters its products as v does (fp16, da and db:
+ * the largest magnitude is that of up to 64 rows).  Up to three
  * launches. */
 int polyq_adapters_backward(const polyq_dense* x, int64_t T, const polyq_adapters* adapters,
                             const polyq_segments* segments, const float* saved,

@@ -335,10 +335,20 @@ __device__ __forceinline__ uint32_t scale_bits(uint32_t top) {
 }
 __device__ __forceinline__ float scale_down(uint32_t top) { return __uint_as_float(scale_bits(top) << 23); }
 __device__ __forceinline__ float scale_up(uint32_t top) { return __uint_as_float((254u - scale_bits(top)) << 23); }
+// The bits of the largest magnitude that is finite (one rank's infinity scales no other's away).
 __device__ __forceinline__ uint32_t abs_bits(const float (&v)[8]) {
+  constexpr uint32_t INF = 0x7F800000u;
   uint32_t m = 0;
 #pragma unroll
   for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(v[i]) & 0x7FFFFFFFu);
+  if (m >= INF) {
+    m = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const uint32_t b = __float_as_uint(v[i]) & 0x7FFFFFFFu;
+      m = max(m, b < INF ? b : 0u);
+    }
+  }
   return m;
 }
 __device__ __forceinline__ void load_v8(const float* p, bool there, float (&v)[8]) {

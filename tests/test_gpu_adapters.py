@@ -202,6 +202,32 @@ def test_not_finite_rows_stay_apart(polyq_lib, lengths, dtype):
     assert (da[1, 3:] == 0).all() and (db[1, :, 3:] == 0).all()
 
 
+@pytest.mark.parametrize("dtype", list(T16))
+@pytest.mark.parametrize("lengths", [[4, 5, 6], [80, 90, 70]])
+def test_a_rank_that_is_not_finite_stays_apart(polyq_lib, lengths, dtype):
+    """An infinity in one rank's row of a, or column of b, leaves the other ranks' gradients as
+    zeros there would."""
+    t = T16[dtype]
+    T = sum(lengths)
+    x, a, b, dy, _, _ = make(T, 128, 192, 16, 3, t)
+    _, d_off = segments(lengths)
+    ids = torch.tensor([0, 1, 2], dtype=torch.int32, device="cuda")
+
+    def step():
+        saved = polyq_lib.adapters_saved(T, 16)
+        polyq_lib.adapters_forward(x, a, b, d_off, ids, saved=saved)
+        return polyq_lib.adapters_backward(x, a, b, saved, dy, d_off, ids)[1:]
+
+    a[1, 3], b[1, :, 5] = 0, 0
+    good = step()
+    a[1, 3, 7], b[1, 11, 5] = float("inf"), float("-inf")
+    da, db = step()
+    others = [j for j in range(16) if j not in (3, 5)]
+    assert not torch.isfinite(da[1, 5]).any() and not torch.isfinite(db[1, :, 3]).any()
+    assert torch.equal(da[:, others], good[0][:, others]) and torch.equal(db[:, :, others], good[1][:, :, others])
+    assert torch.equal(da[[0, 2]], good[0][[0, 2]]) and torch.equal(db[[0, 2]], good[1][[0, 2]])
+
+
 def test_offsets_outside_the_rows_are_held(polyq_lib):
     """Segments past the tensors' end or before their start keep inside; a falling pair is empty."""
     x, a, b, dy, _, _ = make(50, 128, 192, 16, 2, torch.bfloat16)
