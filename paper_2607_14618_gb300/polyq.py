@@ -7,6 +7,7 @@ module fails loudly when the library has not been built.
 from __future__ import annotations
 
 import ctypes as C
+import struct
 import os
 
 import numpy as np
@@ -199,21 +200,21 @@ _SIGS = {
                                                      C.POINTER(C.c_size_t)]),
     "polyq_ffn_backward": (C.c_int, [_DENSE, _DENSE, _DENSE, C.c_int64, C.c_int64, C.c_int64, _P,
                                      _DENSE, _DENSE, _DENSE, _DENSE, _P, C.c_size_t, _P]),
-    # include/polyq_finetune.h
-    "polyq_layernorm_forward": (C.c_int, [_DENSE, C.c_int64, C.c_int64, _DENSE, _DENSE, C.c_float,
-                                          C.c_int, _DENSE, _P, _P]),
+    # include/polyq_finetune.h (descriptors as packed bytes: see _packed)
+    "polyq_layernorm_forward": (C.c_int, [_P, C.c_int64, C.c_int64, _P, _P, C.c_float,
+                                          C.c_int, _P, _P, _P]),
     "polyq_layernorm_workspace_bytes": (C.c_int, [C.c_int64, C.c_int64, C.POINTER(C.c_size_t)]),
-    "polyq_layernorm_backward": (C.c_int, [_DENSE, C.c_int64, C.c_int64, _DENSE, _P, C.c_int,
-                                           _DENSE, _DENSE, _DENSE, _DENSE, _DENSE, _P, C.c_size_t,
+    "polyq_layernorm_backward": (C.c_int, [_P, C.c_int64, C.c_int64, _P, _P, C.c_int,
+                                           _P, _P, _P, _P, _P, _P, C.c_size_t,
                                            _P]),
     "polyq_adamw_step": (C.c_int, [C.POINTER(AdamwTensor), C.c_int32, C.c_int32, C.c_int32,
-                                   C.c_int32, C.POINTER(AdamwState), C.POINTER(AdamwHyper), _P]),
-    "polyq_adamw_values": (C.c_int, [C.POINTER(AdamwState), _DENSE, _DENSE, _P]),
+                                   C.c_int32, C.POINTER(AdamwState), _P, _P]),
+    "polyq_adamw_values": (C.c_int, [C.POINTER(AdamwState), _P, _P, _P]),
     "polyq_adapters_workspace_bytes": (C.c_int, [C.c_int64, C.c_int32, C.POINTER(C.c_size_t)]),
-    "polyq_adapters_forward": (C.c_int, [_DENSE, C.c_int64, C.POINTER(Adapters), C.POINTER(Segments),
-                                         _DENSE, _DENSE, _P, _P, C.c_size_t, _P]),
-    "polyq_adapters_backward": (C.c_int, [_DENSE, C.c_int64, C.POINTER(Adapters),
-                                          C.POINTER(Segments), _P, _DENSE, _DENSE, _DENSE, _P, _P,
+    "polyq_adapters_forward": (C.c_int, [_P, C.c_int64, _P, _P,
+                                         _P, _P, _P, _P, C.c_size_t, _P]),
+    "polyq_adapters_backward": (C.c_int, [_P, C.c_int64, _P,
+                                          _P, _P, _P, _P, _P, _P, _P,
                                           C.c_int32, _P, C.c_size_t, _P]),
 }
 for _name, (_res, _args) in _SIGS.items():
@@ -793,6 +794,16 @@ def _type_of(dtype):
     return _T.get(dtype)
 
 
+T_I32, T_I64, T_U8 = 3, 4, 5  # (of this binding's checks only)
+_dtypes = []  # torch dtypes by T_*, filled by the first use
+
+
+def _all_dtypes():
+    import torch
+    _dtypes[:] = (torch.float32, torch.bfloat16, torch.float16, torch.int32, torch.int64, torch.uint8)
+    return _dtypes
+
+
 _calls = []  # the current device's index, a device's current stream; filled by the first use
 
 
@@ -812,9 +823,10 @@ def _stream_on(dev, name, stream):
     return _calls[1](dev) if stream is None else stream.cuda_stream
 
 
-def _dense(t, name, rows=None, cols=None, dev=None, dtype=None):
-    """Descriptor of a 2-D CUDA tensor whose rows are contiguous (any row
-    stride), checked against the sizes, device index and type that are given."""
+def _rows(t, name, rows=None, cols=None, dev=None, dtype=None):
+    """Address, row stride, T_*, sizes and device index of a 2-D CUDA tensor whose rows
+    are contiguous (any row stride), checked against the sizes, device index and type
+    that are given."""
     try:
         ty = _T.get(t.dtype)
         if ty is None:
@@ -834,7 +846,12 @@ def _dense(t, name, rows=None, cols=None, dev=None, dtype=None):
         s0 = k
     if s0 < k:
         raise ValueError(f"{name}: rows overlap (stride {s0})")
-    return Dense(t.data_ptr(), s0, ty)
+    return t.data_ptr(), s0, ty, n, k, at
+
+
+def _dense(t, name, rows=None, cols=None, dev=None, dtype=None):
+    """The descriptor of such a tensor."""
+    return Dense(*_rows(t, name, rows, cols, dev, dtype)[:3])
 
 
 class Fp4Tensor:
@@ -954,9 +971,12 @@ def _workspace_at(workspace, dev, stream, make, *args):
     """The caller's workspace, checked, or a new one (the library checks its size)."""
     if workspace is None:
         return _made(stream, make, *args)
-    import torch
-    if (not isinstance(workspace, torch.Tensor) or workspace.dtype != torch.uint8
-            or workspace.get_device() != dev or not workspace.is_contiguous()):
+    try:
+        good = (workspace.dtype == (_dtypes or _all_dtypes())[T_U8] and workspace.get_device() == dev
+                and workspace.is_contiguous())
+    except AttributeError:
+        good = False
+    if not good:
         raise ValueError(f"workspace must be a contiguous uint8 tensor on cuda:{dev}")
     return workspace
 
@@ -1126,6 +1146,19 @@ def ffn_backward(x, gate, up, saved, dh, dx=None, dgate=None, dup=None, need_dx=
 ADAPTERS_WORKSPACE_ZERO = 256  # leading workspace bytes that must start at zero
 ADAMW_BLOCK = 256  # elements of an 8-bit state that share a scale
 
+# Descriptors as bytes, laid out as Dense, Adapters, Segments and AdamwHyper: packing one takes a
+# quarter of the time of a ctypes structure with its fields (Adapters 0.8 -> 0.2 us).
+_pack_dense = struct.Struct("@Pqi4x").pack
+_pack_adapters = struct.Struct("@PPqqqqqqiii4xPP").pack
+_pack_segments = struct.Struct("@PPi4x").pack
+_pack_hyper = struct.Struct("@ddddqQPPP").pack
+
+
+def _packed(t, name, rows, cols, dev, dtype=None):
+    """The descriptor of a tensor that _rows checks."""
+    p, stride, ty, _, _, _ = _rows(t, name, rows, cols, dev, dtype)
+    return _pack_dense(p, stride, ty)
+
 
 def _vector(t, name, K, dev):
     """Descriptor of K contiguous elements on CUDA device `dev` (None: none)."""
@@ -1141,20 +1174,13 @@ def _vector(t, name, K, dev):
         good = False
     if not good:
         raise ValueError(f"{name} must be a contiguous fp32, bf16 or fp16 tensor [{K}] on cuda:{dev}")
-    return C.byref(Dense(t.data_ptr(), K, ty))
-
-
-T_I32, T_I64 = 3, 4  # (of this binding's checks only)
-_dtypes = []  # torch dtypes by T_*, filled by the first use
+    return _pack_dense(t.data_ptr(), K, ty)
 
 
 def _plain(t, name, ty, shape, dev):
     """The address of a contiguous tensor of that type (T_*) and shape on CUDA device `dev`."""
-    if not _dtypes:
-        import torch
-        _dtypes[:] = (torch.float32, torch.bfloat16, torch.float16, torch.int32, torch.int64)
     try:
-        good = (t.dtype == _dtypes[ty] and t.shape == shape and t.get_device() == dev and t.is_contiguous())
+        good = (t.dtype == (_dtypes or _all_dtypes())[ty] and t.shape == shape and t.get_device() == dev and t.is_contiguous())
     except AttributeError:
         good = False
     if not good:
@@ -1188,17 +1214,14 @@ def layernorm_forward(x, weight=None, bias=None, eps=1e-5, center=True, y=None, 
     bf16 or fp16, any row stride); center=False: RMS norm, with a mean of 0.  y:
     x's type by default, may be x itself.  `stats` (layernorm_stats) receives what
     layernorm_backward needs."""
-    dx = _dense(x, "x")
-    dev = x.get_device()
+    px, sx, tx, rows, K, dev = _rows(x, "x")
     st = _stream_on(dev, "x", stream)
-    rows, K = x.shape
     if y is None:
         import torch
         y = _made(stream, torch.empty, (rows, K), dtype=dtype or x.dtype, device=x.device)
-    dy = _dense(y, "y", rows, K, dev, dtype)
     _check(_lib.polyq_layernorm_forward(
-        C.byref(dx), rows, K, _vector(weight, "weight", K, dev), _vector(bias, "bias", K, dev), eps,
-        1 if center else 0, C.byref(dy), None if stats is None else _stats(stats, rows, dev), st))
+        _pack_dense(px, sx, tx), rows, K, _vector(weight, "weight", K, dev), _vector(bias, "bias", K, dev),
+        eps, 1 if center else 0, _packed(y, "y", rows, K, dev, dtype), None if stats is None else _stats(stats, rows, dev), st))
     return y
 
 
@@ -1210,11 +1233,9 @@ def layernorm_backward(x, weight, stats, dy, center=True, dx=None, dweight=None,
     `residual` (of that type, may be dx) added to it: the gradient that reaches x
     beside the norm.  dweight and dbias are of the weight's type (fp32 without one)
     or of that of the buffers passed.  Those not needed are None."""
-    ix = _dense(x, "x")
-    dev = x.get_device()
+    px, sx, tx, rows, K, dev = _rows(x, "x")
     st = _stream_on(dev, "x", stream)
-    rows, K = x.shape
-    idy = _dense(dy, "dy", rows, K, dev)
+    idy = _packed(dy, "dy", rows, K, dev)
     if (dx is None and need_dx) or (dweight is None and need_weight) or (dbias is None and need_bias):
         import torch
         vt = torch.float32 if weight is None else weight.dtype
@@ -1224,17 +1245,17 @@ def layernorm_backward(x, weight, stats, dy, center=True, dx=None, dweight=None,
             dweight = _made(stream, torch.empty, K, dtype=vt, device=x.device)
         if dbias is None and need_bias:
             dbias = _made(stream, torch.empty, K, dtype=vt, device=x.device)
-    odx = None if dx is None else C.byref(_dense(dx, "dx", rows, K, dev, x.dtype))
+    odx = None if dx is None else _packed(dx, "dx", rows, K, dev, x.dtype)
     if residual is not None and dx is None:
         raise ValueError("a residual is added to dx, which is not wanted")
-    ires = None if residual is None else C.byref(_dense(residual, "residual", rows, K, dev, x.dtype))
+    ires = None if residual is None else _packed(residual, "residual", rows, K, dev, x.dtype)
     wp = wn = 0
     if dweight is not None or dbias is not None:
         ws = _workspace_at(workspace, dev, stream, layernorm_workspace, rows, K, x.device)
         wp, wn = ws.data_ptr(), ws.numel()
     _check(_lib.polyq_layernorm_backward(
-        C.byref(ix), rows, K, _vector(weight, "weight", K, dev), _stats(stats, rows, dev),
-        1 if center else 0, C.byref(idy), ires, odx, _vector(dweight, "dweight", K, dev),
+        _pack_dense(px, sx, tx), rows, K, _vector(weight, "weight", K, dev), _stats(stats, rows, dev),
+        1 if center else 0, idy, ires, odx, _vector(dweight, "dweight", K, dev),
         _vector(dbias, "dbias", K, dev), wp, wn, st))
     return dx, dweight, dbias
 
@@ -1350,15 +1371,15 @@ class AdamW:
         leaves everything as it was.  seed: of the rounding of 8-bit states, another one
         for each step."""
         st = _stream_on(self._dev, "the tensors", stream)
-        lr_dev = step_dev = scale = None
+        lr_dev = step_dev = scale = 0
         if hasattr(lr, "data_ptr"):
             lr_dev, lr = self._scalar(lr, "lr", T_F32), 0.0
         if hasattr(step, "data_ptr"):
             step_dev, step = self._scalar(step, "step", T_I64), 1
         if grad_scale is not None:
             scale = self._scalar(grad_scale, "grad_scale", T_F32)
-        h = C.byref(AdamwHyper(float(lr), betas[0], betas[1], eps, int(step), seed & 0xFFFFFFFFFFFFFFFF, lr_dev,
-                               step_dev, scale))
+        h = _pack_hyper(float(lr), betas[0], betas[1], eps, int(step), seed & 0xFFFFFFFFFFFFFFFF, lr_dev,
+                        step_dev, scale)
         for tp, tg, tc, tensors, n in self._groups:
             _check(_lib.polyq_adamw_step(tensors, n, tp, tg, tc, self._state_ref, h, st))
 
@@ -1381,11 +1402,9 @@ def adapters_saved(T, R, device="cuda"):
     return torch.empty((T, R), dtype=torch.float32, device=device)
 
 
-def _adapters(x, a, b, offsets, ids, scales, ranks, dev):
-    """Descriptors of the adapters a [n][R][K] and b [n][N][R] and of the segments."""
-    K = x.shape[1]
+def _adapters(x, K, ty, a, b, offsets, ids, scales, ranks, dev):
+    """Descriptors of the adapters a [n][R][K] and b [n][N][R] and of the segments; n, R, N."""
     try:
-        ty = _type_of(x.dtype)
         n, R, ka = a.shape
         nb, N, rb = b.shape
         an, ar, a1 = a.stride()
@@ -1405,11 +1424,12 @@ def _adapters(x, a, b, offsets, ids, scales, ranks, dev):
     if n == 1:  # (one adapter: the stride to the next does not matter)
         an = bn = 0
     m = ids.shape[0] if getattr(ids, "ndim", 0) == 1 else -1
-    d = Adapters(a.data_ptr(), b.data_ptr(), ar, an, br, bn, K, N, n, R, ty,
-                 None if scales is None else _plain(scales, "scales", T_F32, (n,), dev),
-                 None if ranks is None else _plain(ranks, "ranks", T_I32, (n,), dev))
-    s = Segments(_plain(offsets, "offsets", T_I32, (m + 1,), dev), _plain(ids, "ids", T_I32, (m,), dev), m)
-    return d, s
+    d = _pack_adapters(a.data_ptr(), b.data_ptr(), ar, an, br, bn, K, N, n, R, ty,
+                       0 if scales is None else _plain(scales, "scales", T_F32, (n,), dev),
+                       0 if ranks is None else _plain(ranks, "ranks", T_I32, (n,), dev))
+    s = _pack_segments(_plain(offsets, "offsets", T_I32, (m + 1,), dev), _plain(ids, "ids", T_I32, (m,), dev),
+                       m)
+    return d, s, n, R, N
 
 
 def adapters_forward(x, a, b, offsets, ids, scales=None, ranks=None, residual=None, y=None,
@@ -1422,22 +1442,20 @@ def adapters_forward(x, a, b, offsets, ids, scales=None, ranks=None, residual=No
     projection's result, of y's type (x's or fp32), may be y itself.  Rows of no segment are
     left as they were: without a `y` they are not set.  `saved` (adapters_saved) receives what
     adapters_backward needs."""
-    ix = _dense(x, "x")
-    dev = x.get_device()
+    px, sx, tx, T, K, dev = _rows(x, "x")
     st = _stream_on(dev, "x", stream)
-    d, s = _adapters(x, a, b, offsets, ids, scales, ranks, dev)
-    T, R, N = x.shape[0], d.R, d.N
+    d, s, _, R, N = _adapters(x, K, tx, a, b, offsets, ids, scales, ranks, dev)
     ir = None
     if residual is not None:
-        ir = C.byref(_dense(residual, "residual", T, N, dev, dtype if y is None else None))
+        ir = _packed(residual, "residual", T, N, dev, dtype if y is None else None)
     if y is None:
         import torch
         y = _made(stream, torch.empty, (T, N), device=x.device,
                   dtype=dtype or (residual.dtype if residual is not None else x.dtype))
-    iy = _dense(y, "y", T, N, dev, dtype)
+    iy = _packed(y, "y", T, N, dev, dtype)
     ps = None if saved is None else _plain(saved, "saved", T_F32, (T, R), dev)
     ws = _workspace_at(workspace, dev, stream, adapters_workspace, T, R, x.device)
-    _check(_lib.polyq_adapters_forward(C.byref(ix), T, C.byref(d), C.byref(s), ir, C.byref(iy), ps,
+    _check(_lib.polyq_adapters_forward(_pack_dense(px, sx, tx), T, d, s, ir, iy, ps,
                                        ws.data_ptr(), ws.numel(), st))
     return y
 
@@ -1451,27 +1469,26 @@ def adapters_backward(x, a, b, saved, dy, offsets, ids, scales=None, ranks=None,
     segment are left as they were.  da [n][R][K] and db [n][N][R] are of x's type or those
     of the buffers passed (contiguous, both of one type, x's or fp32): sums over all rows of
     an adapter, zeros past its rank and for an adapter without rows.  Those not needed are None."""
-    ix = _dense(x, "x")
-    dev = x.get_device()
+    px, sx, tx, T, K, dev = _rows(x, "x")
     st = _stream_on(dev, "x", stream)
-    d, s = _adapters(x, a, b, offsets, ids, scales, ranks, dev)
-    T, K, N, R, n = x.shape[0], d.K, d.N, d.R, d.n
-    idy = _dense(dy, "dy", T, N, dev, x.dtype)
+    d, s, n, R, N = _adapters(x, K, tx, a, b, offsets, ids, scales, ranks, dev)
+    idy = _packed(dy, "dy", T, N, dev, x.dtype)
     ir = None
-    import torch
     if dx is None and need_dx:
+        import torch
         dx = _made(stream, torch.empty, (T, K), device=x.device,
                    dtype=x.dtype if residual is None else residual.dtype)
     if residual is not None:
         if dx is None:
             raise ValueError("a residual is added to dx, which is not wanted")
-        ir = C.byref(_dense(residual, "residual", T, K, dev))
-    odx = None if dx is None else C.byref(_dense(dx, "dx", T, K, dev))
+        ir = _packed(residual, "residual", T, K, dev)
+    odx = None if dx is None else _packed(dx, "dx", T, K, dev)
     gt = x.dtype if da is None and db is None else getattr(db if da is None else da, "dtype", None)
     ty = _type_of(gt)
     if ty is None or (ty != T_F32 and gt != x.dtype):
         raise ValueError(f"da and db must be {x.dtype} or fp32 tensors")
     if need_weights and (da is None or db is None):
+        import torch
         da, db = (t if t is not None else _made(stream, torch.empty, shape, dtype=gt, device=x.device)
                   for t, shape in ((da, (n, R, K)), (db, (n, N, R))))
     pa = None if da is None else _plain(da, "da", ty, (n, R, K), dev)
@@ -1481,6 +1498,6 @@ def adapters_backward(x, a, b, saved, dy, offsets, ids, scales=None, ranks=None,
     if dx is not None or da is not None:
         ws = _workspace_at(workspace, dev, stream, adapters_workspace, T, R, x.device)
         wp, wn = ws.data_ptr(), ws.numel()
-    _check(_lib.polyq_adapters_backward(C.byref(ix), T, C.byref(d), C.byref(s), ps, C.byref(idy), ir,
+    _check(_lib.polyq_adapters_backward(_pack_dense(px, sx, tx), T, d, s, ps, idy, ir,
                                         odx, pa, pb, ty, wp, wn, st))
     return dx, da, db

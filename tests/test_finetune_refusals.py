@@ -252,3 +252,13 @@ def test_adam_state_arguments(polyq_lib):
         s.values()
     with pytest.raises(ValueError):
         polyq_lib.AdamW([], [], s)
+
+
+@pytest.mark.parametrize("name,pack", [("Dense", "_pack_dense"), ("Adapters", "_pack_adapters"),
+                                       ("Segments", "_pack_segments"), ("AdamwHyper", "_pack_hyper")])
+def test_packed_descriptors(polyq_lib, name, pack):
+    """The bytes that calls pass are those of the structures of the header."""
+    import ctypes as C
+    kind = getattr(polyq_lib, name)
+    values = [(i + 1) * (0.25 if t is C.c_double else 3) for i, (_, t) in enumerate(kind._fields_)]
+    assert getattr(polyq_lib, pack)(*values) == bytes(kind(*values))
