@@ -14,8 +14,8 @@
 // them (fp32 3551 x 11811, training: 330 us, 508 with element loads).
 //
 // Measured, forward and backward with the residual gradient (by the profiler, operands from
-// HBM): 8192 x 5120 bf16 33 + 80 + 4.3 us, 5.1 and 4.2 TB/s, bound by instructions: 20 for an
-// element forward, 38 backward, in packed fp32 pairs.  1001 x 4100: 12.8 + 18.8 + 4.6 us,
+// HBM): 8192 x 5120 bf16 33 + 64 + 4.5 us, 5.1 and 5.2 TB/s, bound by instructions: 20 for an
+// element forward, 38 backward, in packed fp32 pairs.  777 x 5003 fp16: 12.6 + 16.7 + 4.7 us,
 // bound by the latency of three launches.  One row: 3.2 us, a launch.
 #include <algorithm>
 #include <atomic>
@@ -40,7 +40,7 @@ constexpr int kReduceCols = 32, kReduceRows = 16;
 // Threads of an SM, as registers allow, and rows that a thread takes together once there are enough.
 constexpr int kBackwardRegs = 96, kBackwardPerSm = 65536 / kBackwardRegs, kTogether = 2;
 constexpr int kMostSmem = 200 << 10;
-constexpr int kRingBytes = 96 << 10;  // of shared memory for rows on their way, a block
+constexpr int kSmSmem = 226 << 10, kStaticSmem = 14 << 10;  // of an SM; of a backward block, beside its rows
 
 struct NormParams {
   const void* x;
@@ -458,12 +458,14 @@ __global__ void __maxnreg__(kForwardRegs) norm_forward_kernel(const __grid_const
 }
 
 // Backward: threadIdx.x: a row's threads (whole warps), threadIdx.y: rows side by side (one
-// in a cluster); each takes NR rows together, blockDim.y apart.  Rows are read from shared
-// memory (or, not VEC, from L2) again after the sums over them, and the weight each time:
-// registers hold the sums over rows.
+// in a cluster); each takes NR rows together, blockDim.y apart.  Registers hold the sums over
+// rows, and, with one group of columns (G), hat and dy w of the rows at hand until the sums
+// over them are there; with two they are read from shared memory again.  A row's statistics
+// are asked for a round ahead (8192 x 5120 bf16 with a residual: 78 us without that, 64 with it).
 template <typename TX, typename TY, bool VEC, int NR, int G>
 __global__ void __maxnreg__(kBackwardRegs) norm_backward_kernel(
     const __grid_constant__ NormParams P) {
+  constexpr bool KEEP = G == 1;
   extern __shared__ __align__(16) uint8_t ring[];
   __shared__ float warps[8][2 * 32 * 2 * NR];
   __shared__ float blocks[2 * kMaxCluster * 2 * NR];
@@ -522,18 +524,20 @@ __global__ void __maxnreg__(kBackwardRegs) norm_backward_kernel(
 #pragma unroll
     for (int e = 0; e < 4; ++e) dw[g][e] = db[g][e] = f2(0.f, 0.f);
   }
-  float2 stat[NR];
+  float2 stat[NR], next[NR];  // (the next rows' are asked for before these rows are)
   auto stats_of = [&](int from) {
 #pragma unroll
     for (int i = 0; i < NR; ++i) {
       const int row = from + i * R;
-      stat[i] = row < P.rows ? __ldcg(reinterpret_cast<const float2*>(P.stats) + row) : make_float2(0.f, 0.f);
-      if (!P.center) stat[i].x = 0.f;
+      next[i] = row < P.rows ? __ldcg(reinterpret_cast<const float2*>(P.stats) + row) : make_float2(0.f, 0.f);
     }
   };
   stats_of(row0);
   for (int stage = 0; row0 - (int)threadIdx.y < P.rows; row0 += step) {
     const int there = stage == 0 ? P.depth - 1 : stage - 1;
+#pragma unroll
+    for (int i = 0; i < NR; ++i) stat[i] = make_float2(P.center ? next[i].x : 0.f, next[i].y);
+    stats_of(row0 + step);
     if (VEC) {
       ask(row0 + (P.depth - 1) * step, there);
       wait_stages(P.depth - 1);
@@ -543,33 +547,37 @@ __global__ void __maxnreg__(kBackwardRegs) norm_backward_kernel(
       ask(row0 + (P.depth - 1) * step, there);
     }
     // hat and the gradient of a row's columns, zeros where there is no element (what the loads
-    // give there is anything).  They are read again after the sums: the registers are the
-    // weights' and sums'.
+    // give there is anything).
     auto read = [&](int i, int g, F2(&h)[4], F2(&d)[4]) {
-      const int row = row0 + i * R;
-      const uint32_t m = row < P.rows ? at.mask[g] : 0u, slot = (stage * NR + i) * slots;
+      const uint32_t slot = (stage * NR + i) * slots;
       if constexpr (VEC) {
         x.get(slot + g * x_group, h);
         dy.get(slot + d_at + g * d_group, d);
       } else {
-        AnyRow<TX>::get(x_row(row), any_place(slot, 0, x_group), at.col[g] - c0, T, m, h);
-        AnyRow<TY>::get(d_row(row), any_place(slot, d_at, d_group), at.col[g] - c0, T, m, d);
+        const int row = row0 + i * R;
+        AnyRow<TX>::get(x_row(row), any_place(slot, 0, x_group), at.col[g] - c0, T, at.mask[g], h);
+        AnyRow<TY>::get(d_row(row), any_place(slot, d_at, d_group), at.col[g] - c0, T, at.mask[g], d);
       }
       const F2 minus = f2(-stat[i].x, -stat[i].x), r = f2(stat[i].y, stat[i].y);
 #pragma unroll
       for (int e = 0; e < 4; ++e) h[e] = mul2(add2(h[e], minus), r);
-      if (m != 0xFFu) {
-        clear(h, m);
-        clear(d, m);
+      if (at.mask[g] != 0xFFu) {
+        clear(h, at.mask[g]);
+        clear(d, at.mask[g]);
       }
     };
+    F2 hat[KEEP ? NR : 1][4], gw[KEEP ? NR : 1][4];  // hat and dy w
     float s[2 * NR];
 #pragma unroll
     for (int i = 0; i < NR; ++i) {
+      s[2 * i] = s[2 * i + 1] = 0.f;
+      if (row0 + i * R >= P.rows) continue;  // (all threads of the row)
       F2 sh = f2(0.f, 0.f), sg = sh;
 #pragma unroll
       for (int g = 0; g < G; ++g) {
-        F2 h[4], d[4], w[4];
+        F2(&h)[4] = hat[KEEP ? i : 0];
+        F2(&d)[4] = gw[KEEP ? i : 0];
+        F2 w[4];
         read(i, g, h, d);
         weight.get(g * T * R * 32, w);
 #pragma unroll
@@ -594,21 +602,27 @@ __global__ void __maxnreg__(kBackwardRegs) norm_backward_kernel(
         const F2 mgh2 = f2(mgh, mgh), mg2 = f2(mg, mg), r = f2(stat[i].y, stat[i].y);
 #pragma unroll
         for (int g = 0; g < G; ++g) {
-          F2 h[4], d[4], w[4], a[4] = {f2(0.f, 0.f), f2(0.f, 0.f), f2(0.f, 0.f), f2(0.f, 0.f)};
-          read(i, g, h, d);
-          weight.get(g * T * R * 32, w);
+          F2(&h)[4] = hat[KEEP ? i : 0];
+          F2(&d)[4] = gw[KEEP ? i : 0];
+          F2 a[4] = {f2(0.f, 0.f), f2(0.f, 0.f), f2(0.f, 0.f), f2(0.f, 0.f)};
+          if constexpr (!KEEP) {
+            F2 w[4];
+            read(i, g, h, d);
+            weight.get(g * T * R * 32, w);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) d[e] = mul2(d[e], w[e]);
+          }
           if (P.res) {
             const uint32_t slot = (stage * NR + i) * slots;
             if constexpr (VEC) x.get(slot + r_at + g * x_group, a);
             else AnyRow<TX>::get(r_row(row), any_place(slot, r_at, x_group), at.col[g] - c0, T, at.mask[g], a);
           }
 #pragma unroll
-          for (int e = 0; e < 4; ++e) d[e] = fma2(r, fma2(h[e], mgh2, fma2(d[e], w[e], mg2)), a[e]);
+          for (int e = 0; e < 4; ++e) d[e] = fma2(r, fma2(h[e], mgh2, add2(d[e], mg2)), a[e]);
           store_pairs<VEC>((TX*)P.y + (int64_t)row * P.y_stride, at.col[g], T, at.mask[g], d);
         }
       }
     }
-    stats_of(row0 + step);
     if (++stage == P.depth) stage = 0;
   }
   // The rows side by side are added in order; a group of blocks writes its sums once.
@@ -910,7 +924,10 @@ extern "C" int polyq_layernorm_backward(const polyq_dense* x, int64_t rows, int6
   if (2 * stage + cols * 4 > kMostSmem) stage /= nr, nr = 1;
   const Variant v{true, vec, nr, s.groups};
   void* f = pick(x->type, dy->type, v);
-  P.depth = std::max(2, std::min(4, (kRingBytes - cols * 4) / stage));
+  // As many rows on their way as the SM's blocks have room for (10817 x 1728 fp32 with two
+  // stages 70 us, with three 64; 8192 x 5120 bf16 the same with both).
+  const int share = std::min(kMostSmem, kSmSmem / std::max(1, kBackwardPerSm / (s.threads * s.rows)) - kStaticSmem);
+  P.depth = std::max(2, std::min(4, (share - cols * 4) / stage));
   const int smem = stage * P.depth + cols * 4;
   if (smem > 32 << 10) rc = allow_smem(f, v.index(x->type, dy->type), who);
   if (rc) return rc;
