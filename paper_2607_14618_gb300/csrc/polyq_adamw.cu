@@ -123,9 +123,51 @@ struct Rates {
   uint32_t seed_key, seed_high;
 };
 
-// One block: elements i of the tensor from e0 on.  FULL: 256 of them, on 16 bytes.
+// The whole blocks of an 8-bit state come through shared memory, a place for each block that a
+// warp has asked for: p, the gradient and the two moments' codes.  (Loads to registers waited:
+// 10 cycles of a warp for each that it issued; 212 M elements 795 us, 760 this way.)
+template <typename TP, typename TG>
+struct Staged {
+  static constexpr int P_BYTES = kBlock * sizeof(TP), G_BYTES = kBlock * sizeof(TG), STAGE = P_BYTES + G_BYTES + 2 * kBlock;
+  static constexpr int STAGES = STAGE <= 2048 ? 3 : 2;  // (48 KB of a thread block)
+  // Where the 16-byte piece j of a tensor's elements lies: a lane's pieces of fp32 lie in different banks.
+  template <typename T>
+  static __device__ __forceinline__ uint32_t piece(int j) {
+    return (sizeof(T) == 4 ? j ^ (j >> 3 & 1) : j) * 16u;
+  }
+  static __device__ __forceinline__ void copy16(uint32_t dst, const void* src) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+  }
+  template <typename T>
+  static __device__ __forceinline__ void ask(uint32_t place, const void* data, uint32_t block) {
+    const int lane = threadIdx.x & 31;
+    const char* from = (const char*)data + (int64_t)block * (kBlock * sizeof(T));
+#pragma unroll
+    for (int j = lane; j < (int)sizeof(T) * kBlock / 16; j += 32) copy16(place + piece<T>(j), from + 16 * j);
+  }
+  template <typename T>
+  static __device__ __forceinline__ void get(uint32_t place, Raw8<T>& r) {
+    constexpr int N16 = sizeof(T) * 8 / 16;
+#pragma unroll
+    for (int i = 0; i < N16; ++i)
+      asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
+                   : "=r"(r.w[i].x), "=r"(r.w[i].y), "=r"(r.w[i].z), "=r"(r.w[i].w)
+                   : "r"(place + piece<T>((threadIdx.x & 31) * N16 + i))
+                   : "memory");
+  }
+  static __device__ __forceinline__ uint2 codes(uint32_t place) {
+    uint2 v;
+    asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(place + (threadIdx.x & 31) * 8u) : "memory");
+    return v;
+  }
+};
+
+// One block: elements i of the tensor from e0 on.  FULL: 256 of them, on 16 bytes, which with 8
+// bits lie at `place`.  sm_was, sv_was: the scales of 8 bits.
 template <typename TP, typename TG, int BITS, bool FULL, int N>
-__device__ __forceinline__ void update_block(const AdamParams<N>& P, const Tensor& t, uint32_t block, const Rates& c) {
+__device__ __forceinline__ void update_block(const AdamParams<N>& P, const Tensor& t, uint32_t block, const Rates& c,
+                                             uint32_t place, int sm_was, int sv_was) {
+  using S = Staged<TP, TG>;
   const int lane = threadIdx.x & 31;
   const int64_t e0 = (int64_t)block * kBlock, s0 = (int64_t)(t.at + block) * kBlock;
   // the eight elements of a lane: neighbours, or every 32nd (see load8)
@@ -133,8 +175,13 @@ __device__ __forceinline__ void update_block(const AdamParams<N>& P, const Tenso
   const uint32_t mask = FULL ? 0xFFu : mask8<false>(col, 32, (int)min(t.n - e0, (int64_t)kBlock));
   Raw8<TP> rp;
   Raw8<TG> rg;
-  load8<FULL>((const TP*)t.p + e0, col, 32, mask, rp);
-  load8<FULL>((const TG*)t.grad + e0, col, 32, mask, rg);
+  if constexpr (FULL && BITS == 8) {
+    S::get(place, rp);
+    S::get(place + S::P_BYTES, rg);
+  } else {
+    load8<FULL>((const TP*)t.p + e0, col, 32, mask, rp);
+    load8<FULL>((const TG*)t.grad + e0, col, 32, mask, rg);
+  }
   float m[8], v[8];
   if constexpr (BITS == 32) {
     Raw8<float> rm, rv;
@@ -144,11 +191,11 @@ __device__ __forceinline__ void update_block(const AdamParams<N>& P, const Tenso
     to_float(rv, v);
   } else {
     uint2 cm, cv;
-    const uint8_t *pm = (const uint8_t*)P.m + s0, *pv = (const uint8_t*)P.v + s0;
     if constexpr (FULL) {
-      cm = __ldcg(reinterpret_cast<const uint2*>(pm + col));
-      cv = __ldcg(reinterpret_cast<const uint2*>(pv + col));
+      cm = S::codes(place + S::P_BYTES + S::G_BYTES);
+      cv = S::codes(place + S::P_BYTES + S::G_BYTES + kBlock);
     } else {
+      const uint8_t *pm = (const uint8_t*)P.m + s0, *pv = (const uint8_t*)P.v + s0;
       uint32_t bm[8], bv[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
@@ -158,9 +205,8 @@ __device__ __forceinline__ void update_block(const AdamParams<N>& P, const Tenso
       cm = make_uint2(pack4(bm, 0), pack4(bm, 4));
       cv = make_uint2(pack4(bv, 0), pack4(bv, 4));
     }
-    const int sm = __ldcg(P.ms + t.at + block), sv = __ldcg(P.vs + t.at + block);
-    decode<3>(cm, sm, m);
-    decode<4>(cv, sv, v);
+    decode<3>(cm, sm_was, m);
+    decode<4>(cv, sv_was, v);
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = __fmul_rn(v[i], v[i]);
   }
@@ -244,7 +290,7 @@ __device__ __forceinline__ void update_block(const AdamParams<N>& P, const Tenso
         pv[col + 32 * i] = (uint8_t)cv[i];
       }
     }
-    __syncwarp();  // every lane has read the block's scales
+    __syncwarp();  // every lane has read the block's scales, and its place in shared memory
     if (lane == 0) {
       P.ms[t.at + block] = (uint8_t)sm;
       P.vs[t.at + block] = (uint8_t)sr;
@@ -254,8 +300,8 @@ __device__ __forceinline__ void update_block(const AdamParams<N>& P, const Tenso
 
 // Thread blocks of an SM.  32 bits: bound by HBM, and nearest to it with short ones that the
 // SMs take as they come (212 M elements: 996 us with 8 an SM, 870 with 64, 848 with 256: 7.0
-// TB/s).  8 bits: bound by instructions, 100 an element (as many as fit at once: 833 us with 4,
-// 939 with 8; a warp that asks for its next block ahead has room for 3: 893 us).
+// TB/s).  8 bits: bound by instructions (as many as fit at once: 833 us with 4, 939 with 8, with
+// loads to registers; a warp that asks for its next block ahead into them has room for 3: 893).
 constexpr int kBlocks32 = 256, kBlocks8 = 4;
 
 template <typename TP, typename TG, int BITS, int N>
@@ -282,21 +328,72 @@ __global__ void __launch_bounds__(32 * kWarps, 4)
   c.seed_key = mix((uint32_t)seed + 1u);
   c.seed_high = (uint32_t)(seed >> 32);
   const uint32_t stride = gridDim.x * kWarps;
-  for (uint32_t b = blockIdx.x * kWarps + (threadIdx.x >> 5); b < P.blocks; b += stride) {
-    int lo = 0, hi = P.n - 1;  // the last tensor whose first block is b or before it
+  struct Place {
+    int which;  // tensor
+    uint32_t block;
+    bool full;
+    int sm, sv;
+  };
+  auto find = [&](uint32_t b) {  // the last tensor whose first block is b or before it
+    int lo = 0, hi = P.n - 1;
     while (lo < hi) {
       const int mid = (lo + hi + 1) >> 1;
       if (P.t[mid].first <= b) lo = mid;
       else hi = mid - 1;
     }
     const Tensor& t = P.t[lo];
-    const uint32_t block = b - t.first;
+    Place a{lo, b - t.first, false, 0, 0};
+    a.full = ((int64_t)a.block + 1) * kBlock <= t.n && (((uintptr_t)t.p | (uintptr_t)t.grad) & 15) == 0;
+    return a;
+  };
+  auto update = [&](const Place& a, uint32_t place) {
+    const Tensor& t = P.t[a.which];
     const float rate = lr * t.rate;
     c.keep = 1.f - rate * t.decay;
     c.step = rate * inv_bc1;
-    const bool full = ((int64_t)block + 1) * kBlock <= t.n && (((uintptr_t)t.p | (uintptr_t)t.grad) & 15) == 0;
-    if (full) update_block<TP, TG, BITS, true>(P, t, block, c);
-    else update_block<TP, TG, BITS, false>(P, t, block, c);
+    if (a.full) update_block<TP, TG, BITS, true>(P, t, a.block, c, place, a.sm, a.sv);
+    else update_block<TP, TG, BITS, false>(P, t, a.block, c, place, a.sm, a.sv);
+  };
+  uint32_t b = blockIdx.x * kWarps + (threadIdx.x >> 5);
+  if constexpr (BITS == 32) {
+    for (; b < P.blocks; b += stride) update(find(b), 0);
+  } else {
+    using S = Staged<TP, TG>;
+    __shared__ __align__(16) uint8_t smem[kWarps * S::STAGES * S::STAGE];
+    const uint32_t ring = smem_u32(smem) + (threadIdx.x >> 5) * (S::STAGES * S::STAGE);
+    const int lane = threadIdx.x & 31;
+    auto ask = [&](uint32_t b, uint32_t place) {
+      Place a{0, 0, false, 0, 0};
+      if (b < P.blocks) {
+        a = find(b);
+        const Tensor& t = P.t[a.which];
+        a.sm = __ldcg(P.ms + t.at + a.block);
+        a.sv = __ldcg(P.vs + t.at + a.block);
+        if (a.full) {
+          S::template ask<TP>(place, t.p, a.block);
+          S::template ask<TG>(place + S::P_BYTES, t.grad, a.block);
+          const int64_t s0 = (int64_t)(t.at + a.block) * kBlock;
+          const uint8_t* codes = (const uint8_t*)(lane < 16 ? P.m : P.v) + s0 + (lane & 15) * 16;
+          S::copy16(place + S::P_BYTES + S::G_BYTES + lane * 16, codes);
+        }
+      }
+      asm volatile("cp.async.commit_group;" ::: "memory");
+      return a;
+    };
+    // this block, and those on their way
+    Place at[S::STAGES];
+#pragma unroll
+    for (int i = 0; i < S::STAGES - 1; ++i) at[i] = ask(b + i * stride, ring + i * S::STAGE);
+    for (uint32_t slot = 0; b < P.blocks; b += stride) {
+      const uint32_t last = slot == 0 ? S::STAGES - 1 : slot - 1;
+      at[S::STAGES - 1] = ask(b + (S::STAGES - 1) * stride, ring + last * S::STAGE);
+      asm volatile("cp.async.wait_group %0;" ::"n"(S::STAGES - 1) : "memory");
+      __syncwarp();
+      update(at[0], ring + slot * S::STAGE);
+#pragma unroll
+      for (int i = 0; i < S::STAGES - 1; ++i) at[i] = at[i + 1];
+      if (++slot == S::STAGES) slot = 0;
+    }
   }
 }
 
