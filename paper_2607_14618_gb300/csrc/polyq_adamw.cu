@@ -9,9 +9,10 @@
 // are parameters of the kernel, so that a step needs no copy to the device; a
 // thread block finds its tensor by bisection.
 //
-// Measured: 212 M elements, fp32 with bf16 gradients and copies, 32-bit states 850 us, 7.0 TB/s; the same with
-// 8-bit states 833 us, bound by instructions, 100 an element; 560 tensors, 62 M elements, 258 us;
-// 81 vectors of 5120 5 us, a launch.
+// Measured: 212 M elements, fp32 with bf16 gradients and copies, 32-bit states 850 us, 7.0 TB/s;
+// the same with 8-bit states 740 us, bound by instructions, about 95 an element, in packed pairs
+// where the order of roundings allows (106 an element and 760 us one by one); 560 tensors, 62 M
+// elements, 258 us; 81 vectors of 5120 6 us, a launch.
 #include <algorithm>
 #include <cmath>
 #include <cstring>
@@ -78,29 +79,33 @@ struct Scale {
   static __device__ __forceinline__ Scale down(int s) {
     return Scale{pow2(1 - min(s, 127)), pow2(min(127 - s, 0)), s > 127};
   }
-  __device__ __forceinline__ void apply(float (&v)[8]) const {
+  __device__ __forceinline__ void apply(F2 (&v)[4]) const {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] *= one;
+    for (int i = 0; i < 4; ++i) v[i] = mul2(v[i], f2(one, one));
     if (two)
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] *= rest;
+      for (int i = 0; i < 4; ++i) v[i] = mul2(v[i], f2(rest, rest));
   }
 };
 // Values of eight codes (a byte each): MANT 3 with a sign in bit 7, MANT 4 without.
 template <int MANT>
-__device__ __forceinline__ void decode(uint2 codes, int scale, float (&v)[8]) {
+__device__ __forceinline__ void decode(uint2 codes, int scale, F2 (&v)[4]) {
   constexpr uint32_t MASK = (MANT == 3 ? 0x7Fu : 0xFFu) << (23 - MANT);
+  float f[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     const uint32_t w = i < 4 ? codes.x : codes.y;
     const int at = 23 - MANT - 8 * (i & 3);  // from a byte's place to the code's
     uint32_t b = (at >= 0 ? w << at : w >> -at) & MASK;
     if (MANT == 3) b |= w << (24 - 8 * (i & 3)) & 0x80000000u;
-    v[i] = __uint_as_float(b);
+    f[i] = __uint_as_float(b);
   }
-  if (scale == 255) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(0x7FC00000u);
+  for (int i = 0; i < 4; ++i) v[i] = f2(f[2 * i], f[2 * i + 1]);
+  if (scale == 255) {
+    const float nan = __uint_as_float(0x7FC00000u);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = f2(nan, nan);
   } else {
     Scale::up(scale).apply(v);
   }
@@ -112,6 +117,27 @@ template <int MANT>
 __device__ __forceinline__ int scale_of(uint32_t top) {
   const uint32_t past = top + (1u << (23 - MANT)) - 1;
   return top >= 0x7F800000u ? 255 : max((int)(past >> 23) - 14, 0);
+}
+// The largest magnitude of three; NaN where one is.
+__device__ __forceinline__ float most(float a, float b, float c) {
+  float r;
+  asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
+__device__ __forceinline__ void flat(const F2 (&v)[4], float (&f)[8]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float2 a = of(v[i]);
+    f[2 * i] = a.x;
+    f[2 * i + 1] = a.y;
+  }
+}
+template <typename T>
+__device__ __forceinline__ void pairs(const Raw8<T>& r, F2 (&v)[4]) {
+  float f[8];
+  to_float(r, f);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i] = f2(f[2 * i], f[2 * i + 1]);
 }
 __device__ __forceinline__ uint32_t pack4(const uint32_t (&c)[8], int i) {
   return c[i] | c[i + 1] << 8 | c[i + 2] << 16 | c[i + 3] << 24;
@@ -182,13 +208,13 @@ __device__ __forceinline__ void update_block(const AdamParams<N>& P, const Tenso
     load8<FULL>((const TP*)t.p + e0, col, 32, mask, rp);
     load8<FULL>((const TG*)t.grad + e0, col, 32, mask, rg);
   }
-  float m[8], v[8];
+  F2 m[4], v[4];
   if constexpr (BITS == 32) {
     Raw8<float> rm, rv;
     load8<FULL>((const float*)P.m + s0, col, 32, mask, rm);
     load8<FULL>((const float*)P.v + s0, col, 32, mask, rv);
-    to_float(rm, m);
-    to_float(rv, v);
+    pairs(rm, m);
+    pairs(rv, v);
   } else {
     uint2 cm, cv;
     if constexpr (FULL) {
@@ -208,28 +234,41 @@ __device__ __forceinline__ void update_block(const AdamParams<N>& P, const Tenso
     decode<3>(cm, sm_was, m);
     decode<4>(cv, sv_was, v);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = __fmul_rn(v[i], v[i]);
+    for (int i = 0; i < 4; ++i) v[i] = mul2(v[i], v[i]);
   }
-  float p[8], g[8];
-  to_float(rp, p);
-  to_float(rg, g);
-  uint32_t top_m = 0, top_r = 0;
+  F2 p2[4], g[4];
+  pairs(rp, p2);
+  pairs(rg, g);
+  const F2 gs = f2(c.gs, c.gs), b1 = f2(P.b1, P.b1), c1 = f2(P.c1, P.c1), b2 = f2(P.b2, P.b2), c2 = f2(P.c2, P.c2);
+  const F2 keep = f2(c.keep, c.keep), step = f2(-c.step, -c.step), eps = f2(P.eps, P.eps);
+  const F2 inv = f2(c.inv_root_bc2, c.inv_root_bc2);
+  float top_m = 0.f, top_r = 0.f;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
+  for (int i = 0; i < 4; ++i) {
     // each operation rounded by itself: the codes of an 8-bit state follow from this order
-    const float s = __fmul_rn(g[i], c.gs);
-    m[i] = __fadd_rn(__fmul_rn(P.b1, m[i]), __fmul_rn(P.c1, s));
-    v[i] = __fadd_rn(__fmul_rn(P.b2, v[i]), __fmul_rn(__fmul_rn(P.c2, s), s));
-    const float root = __fsqrt_rn(v[i]);
+    const F2 s = mul2(g[i], gs);
+    m[i] = add2(mul2(b1, m[i]), mul2(c1, s));
+    v[i] = add2(mul2(b2, v[i]), mul2(mul2(c2, s), s));
+    const float2 vs = of(v[i]), roots = make_float2(__fsqrt_rn(vs.x), __fsqrt_rn(vs.y));
+    const F2 root = f2(roots.x, roots.y);
     // (the denominator is eps or more, and at most 2^65 / (1 - b2^t): within the reciprocal's range)
-    p[i] = fmaf(-c.step * m[i], fp4::rcp_approx(fmaf(root, c.inv_root_bc2, P.eps)), p[i] * c.keep);
+    const float2 below = of(fma2(root, inv, eps));
+    p2[i] = fma2(mul2(step, m[i]), f2(fp4::rcp_approx(below.x), fp4::rcp_approx(below.y)), mul2(p2[i], keep));
     if (BITS == 8) {
       v[i] = root;
-      if (!FULL && !(mask >> i & 1)) m[i] = v[i] = 0.f;
-      top_m = max(top_m, __float_as_uint(m[i]) & 0x7FFFFFFFu);
-      top_r = max(top_r, __float_as_uint(v[i]) & 0x7FFFFFFFu);
+      if (!FULL) {
+        const bool x = mask >> (2 * i) & 1, y = mask >> (2 * i + 1) & 1;
+        const float2 ms = of(m[i]);
+        m[i] = f2(x ? ms.x : 0.f, y ? ms.y : 0.f);
+        v[i] = f2(x ? roots.x : 0.f, y ? roots.y : 0.f);
+      }
+      const float2 ms = of(m[i]), rs = of(v[i]);
+      top_m = most(ms.x, ms.y, top_m);
+      top_r = most(rs.x, rs.y, top_r);
     }
   }
+  float p[8];
+  flat(p2, p);
   store8<FULL>((TP*)t.p + e0, col, 32, mask, p);
   if (t.copy) {
     if (sizeof(TP) < 4) {
@@ -249,29 +288,35 @@ __device__ __forceinline__ void update_block(const AdamParams<N>& P, const Tenso
     }
   }
   if constexpr (BITS == 32) {
-    store8<FULL>((float*)P.m + s0, col, 32, mask, m);
-    store8<FULL>((float*)P.v + s0, col, 32, mask, v);
+    float fm[8], fv[8];
+    flat(m, fm);
+    flat(v, fv);
+    store8<FULL>((float*)P.m + s0, col, 32, mask, fm);
+    store8<FULL>((float*)P.v + s0, col, 32, mask, fv);
   } else {
-    top_m = __reduce_max_sync(0xFFFFFFFFu, top_m);
-    top_r = __reduce_max_sync(0xFFFFFFFFu, top_r);
-    const int sm = scale_of<3>(top_m), sr = scale_of<4>(top_r);
+    const int sm = scale_of<3>(__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(top_m)));
+    const int sr = scale_of<4>(__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(top_r)));
     const uint64_t b64 = (uint64_t)t.at + block;
     const uint32_t key = mix(mix((uint32_t)b64 ^ c.seed_key) ^ (uint32_t)(b64 >> 32) ^ c.seed_high);
     uint32_t cm[8] = {}, cv[8] = {};
     uint32_t some[8];  // 1 where the root is not 0
+    float fm[8], fr[8];
+    flat(v, fr);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) some[i] = min(__float_as_uint(v[i]), 1u);
+    for (int i = 0; i < 8; ++i) some[i] = min(__float_as_uint(fr[i]), 1u);
     Scale::down(sm).apply(m);
     Scale::down(sr).apply(v);
+    flat(m, fm);
+    flat(v, fr);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const uint32_t e = FULL ? (uint32_t)(col + i) : (uint32_t)(col + 32 * i);
-      uint32_t u = mix(key + 0x9E3779B1u * e);
-      u ^= u >> 16;
+      // 16 bits for the root, and 16 for m
+      const uint32_t h = mix(key + 0x9E3779B1u * e), high = h >> 16;
       // (the sign stays above: no magnitude of the block carries into it)
-      const uint32_t a = __float_as_uint(m[i]) + ((u & 0xFFFFu) << 4);
-      cm[i] = (a >> 20 & 0x7Fu) | (a >> 24 & 0x80u);
-      cv[i] = max((__float_as_uint(v[i]) + (u >> 13 & 0x7FFF8u)) >> 19, some[i]);
+      const uint32_t a = __float_as_uint(fm[i]) + (((h ^ high) & 0xFFFFu) << 4);
+      cm[i] = (a >> 20 & 0x7Fu) | (a >> 24 & ~0x7Fu);
+      cv[i] = max((__float_as_uint(fr[i]) + (high << 3)) >> 19, some[i]);
     }
     if (sm == 255 || sr == 255)
 #pragma unroll
@@ -411,8 +456,10 @@ __device__ __forceinline__ void values_block(const uint8_t* codes, const uint8_t
                                              uint32_t b) {
   const int lane = threadIdx.x & 31;
   const int64_t e = (int64_t)b * kBlock + 8 * lane;
+  F2 pairs_of[4];
+  decode<MANT>(__ldcg(reinterpret_cast<const uint2*>(codes + e)), __ldcg(scales + b), pairs_of);
   float v[8];
-  decode<MANT>(__ldcg(reinterpret_cast<const uint2*>(codes + e)), __ldcg(scales + b), v);
+  flat(pairs_of, v);
   if ((uintptr_t)out % 16) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) any_store(out, type, e + i, v[i]);
