@@ -124,6 +124,12 @@ __device__ __forceinline__ float most(float a, float b, float c) {
   asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
   return r;
 }
+// a + b, each sum by itself: of a packed sum and a product that it adds, the compiler makes one
+// rounding.
+__device__ __forceinline__ F2 sum_rn(F2 a, F2 b) {
+  const float2 x = of(a), y = of(b);
+  return f2(__fadd_rn(x.x, y.x), __fadd_rn(x.y, y.y));
+}
 __device__ __forceinline__ void flat(const F2 (&v)[4], float (&f)[8]) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -247,8 +253,8 @@ __device__ __forceinline__ void update_block(const AdamParams<N>& P, const Tenso
   for (int i = 0; i < 4; ++i) {
     // each operation rounded by itself: the codes of an 8-bit state follow from this order
     const F2 s = mul2(g[i], gs);
-    m[i] = add2(mul2(b1, m[i]), mul2(c1, s));
-    v[i] = add2(mul2(b2, v[i]), mul2(mul2(c2, s), s));
+    m[i] = sum_rn(mul2(b1, m[i]), mul2(c1, s));
+    v[i] = sum_rn(mul2(b2, v[i]), mul2(mul2(c2, s), s));
     const float2 vs = of(v[i]), roots = make_float2(__fsqrt_rn(vs.x), __fsqrt_rn(vs.y));
     const F2 root = f2(roots.x, roots.y);
     // (the denominator is eps or more, and at most 2^65 / (1 - b2^t): within the reciprocal's range)

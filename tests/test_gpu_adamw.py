@@ -253,3 +253,19 @@ def test_state_past_a_tensor_is_zero(polyq_lib):
     polyq_lib.AdamW(p, g, s).step(LR, 1)
     m, r = s.values()
     assert not s.m[300:].any() and not s.v[300:].any() and not m[300:].any() and not r[300:].any()
+
+
+def test_moments_are_rounded_after_each_operation(polyq_lib):
+    """m = b1 m + (1-b1) g and v = b2 v + ((1-b2) g) g, each product and sum rounded by itself: the
+    codes of an 8-bit state follow from this order, so that no product and sum may be one rounding."""
+    n, b1, b2 = 1 << 20, 0.9, 0.95
+    gen = torch.Generator("cuda").manual_seed(7)
+    p, g, m, v = (torch.randn(n, generator=gen, device="cuda") * s for s in (0.02, 1e-3, 1e-3, 1e-3))
+    state = polyq_lib.AdamState([n], bits=32)
+    state.m.copy_(m)
+    state.v.copy_(v.square())
+    one_b1, one_b2 = (torch.tensor(1 - b, dtype=torch.float64).float().cuda() for b in (b1, b2))
+    want_m = m * torch.tensor(b1).cuda() + one_b1 * g
+    want_v = v.square() * torch.tensor(b2).cuda() + (one_b2 * g) * g
+    polyq_lib.AdamW([p], [g], state).step(lr=1e-3, step=3, betas=(b1, b2))
+    assert torch.equal(state.m, want_m) and torch.equal(state.v, want_v)
