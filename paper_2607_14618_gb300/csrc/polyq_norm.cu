@@ -15,8 +15,9 @@
 //
 // Measured, forward and backward with the residual gradient (by the profiler, operands from
 // HBM): 8192 x 5120 bf16 33 + 64 + 4.5 us, 5.1 and 5.2 TB/s, bound by instructions: 20 for an
-// element forward, 38 backward, in packed fp32 pairs (61% of the issue slots backward).  777 x 5003 fp16: 12.6 + 16.7 + 4.7 us,
-// bound by the latency of three launches.  One row: 3.2 us, a launch.
+// element forward, 38 backward, in packed fp32 pairs (61% of the issue slots backward).
+// 777 x 5003 fp16: 12.6 + 16.7 + 4.7 us, bound by the latency of three launches.  One row:
+// 3.2 us, a launch.
 #include <algorithm>
 #include <atomic>
 #include <cmath>
@@ -33,8 +34,8 @@ namespace {
 using namespace polyq;
 
 constexpr int kMaxCluster = 8;
-// Threads of a block at most: rows of up to 2048 columns take eight a thread, wider ones
-// sixteen, so that what a thread does once a row is shared by more of them.
+// Backward: rows of up to kNarrow columns take eight a thread (8192 x 5120 bf16 80 us, 98 with
+// sixteen), wider ones sixteen in up to kWideThreads; small rows share up to kNarrowThreads.
 constexpr int kNarrow = 5120, kNarrowThreads = 256, kWideThreads = 512;
 constexpr int kReduceCols = 32, kReduceRows = 16;
 // Threads of an SM, as registers allow, and rows that a thread takes together once there are enough.
@@ -246,8 +247,9 @@ __device__ __forceinline__ void wait_stages(int left) {
   else asm volatile("cp.async.wait_group 3;" ::: "memory");
 }
 
-// Eight elements of a weight or bias; the loads of each type are in flight together, and 16 bytes wide where rows are VEC and the vector
-// lies so (4 bytes of every 32 each time: 99 MB from L2 for 304 blocks, 10 us).
+// Eight elements of a weight or bias; the loads of each type are in flight together, and 16
+// bytes wide where rows are VEC and the vector lies so (4 bytes of every 32 each time: 99 MB
+// from L2 for 304 blocks, 10 us).
 template <bool VEC, typename T>
 __device__ __forceinline__ void vector8(const T* p, int vec, int col, int step, uint32_t mask, F2 (&v)[4]) {
   Raw8<T> r;
