@@ -101,7 +101,9 @@ typedef struct {
 typedef struct {
   double lr, beta1, beta2, eps; /* lr >= 0, 0 <= beta < 1, 0 < eps <= 1e30 */
   int64_t step;                 /* 1, 2, ...: this step's number */
-  uint64_t seed;                /* of the rounding of 8-bit states */
+  uint64_t seed;                /* of the rounding of 8-bit states: another one for each step, or the
+                                   same elements are rounded the same way every time and small
+                                   moments never change.  (`step` does not enter; step_dev does.) */
   /* Device values, read when the step runs (so that a captured step can take new
    * ones); each may be NULL. */
   const float* lr_dev;          /* the learning rate in place of lr */

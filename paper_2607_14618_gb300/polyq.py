@@ -1363,19 +1363,25 @@ class AdamW:
             raise ValueError(f"{name} must be a tensor of one element on cuda:{self._dev}")
         return _plain(t.reshape(()), name, dtype, (), self._dev)
 
-    def step(self, lr, step, betas=(0.9, 0.999), eps=1e-8, seed=0, grad_scale=None, stream=None):
+    def step(self, lr, step, betas=(0.9, 0.999), eps=1e-8, seed=None, grad_scale=None, stream=None):
         """One step.  `step` counts from 1.  lr and step may be tensors of one element on
         the device (fp32 and int64), read when the step runs, as a captured one needs
         them; the number of the step is then added to the seed.  grad_scale: a factor of
         all gradients, an fp32 tensor of one element; where it is not finite the step
-        leaves everything as it was.  seed: of the rounding of 8-bit states, another one
-        for each step."""
+        leaves everything as it was.  seed: of the rounding of 8-bit states, which has to be
+        another one for each step (with one for all of them the same elements are rounded the
+        same way every time, and small moments never change); by default the step's number,
+        wherever that is."""
         st = _stream_on(self._dev, "the tensors", stream)
         lr_dev = step_dev = scale = 0
         if hasattr(lr, "data_ptr"):
             lr_dev, lr = self._scalar(lr, "lr", T_F32), 0.0
         if hasattr(step, "data_ptr"):
             step_dev, step = self._scalar(step, "step", T_I64), 1
+            if seed is None:  # (the number is added on the device)
+                seed = 0
+        elif seed is None:
+            seed = int(step)
         if grad_scale is not None:
             scale = self._scalar(grad_scale, "grad_scale", T_F32)
         h = _pack_hyper(float(lr), betas[0], betas[1], eps, int(step), seed & 0xFFFFFFFFFFFFFFFF, lr_dev,
