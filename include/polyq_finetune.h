@@ -32,7 +32,7 @@ extern "C" {
  *   hat = (x - mean) rstd, rstd = 1 / sqrt(mean of (x - mean)^2 + eps),
  *   mean = the row's mean with center != 0 (layer norm), else 0 (RMS norm).
  * x and y of any type and row stride; y may be x itself where both have one type
- * and stride.  weight, bias: K elements (their
+ * and stride (another one is POLYQ_EINVAL).  weight, bias: K elements (their
  * stride does not matter) of any type, each may be NULL (1 and 0).  stats: NULL,
  * or device memory of 2*rows floats, 8-byte aligned, which receives (mean, rstd)
  * of every row for the backward pass.  The row is held in fp32, its mean is taken
@@ -52,7 +52,8 @@ int polyq_layernorm_workspace_bytes(int64_t rows, int64_t K, size_t* bytes);
  * residual NULL or [rows][K] of dx's type (the gradient that reaches x beside the
  * norm; its data may be dx's, with dx's stride); dweight, dbias: NULL or K
  * elements of any type; at least one of the three is wanted.  dx may be dy's
- * memory where both have one type and stride.
+ * memory where both have one type and stride.  (Other strides or types in place are
+ * POLYQ_EINVAL; a single row's stride does not matter.)
  * The workspace (polyq_layernorm_workspace_bytes, 16-byte aligned) is needed with
  * dweight or dbias: every SM's sums over its rows, which a second launch adds in
  * a fixed order. */

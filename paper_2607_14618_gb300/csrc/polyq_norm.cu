@@ -774,6 +774,14 @@ int check_vector(const polyq_dense* d, const char* who, const char* what) {
   return polyq_check_dense(&one, 1, who, what);
 }
 
+// An output in the place of what it is made of: each row has to lie where its own input does, or a
+// block overwrites rows that another has yet to read.
+int check_in_place(const polyq_dense* out, const polyq_dense* in, int64_t rows, const char* who, const char* what) {
+  if (out && in && out->data == in->data && (out->type != in->type || (rows > 1 && out->stride != in->stride)))
+    return polyq_set_error(POLYQ_EINVAL, "%s: %s, in place, must have one type and stride", who, what);
+  return POLYQ_OK;
+}
+
 }  // namespace
 
 extern "C" int polyq_layernorm_forward(const polyq_dense* x, int64_t rows, int64_t K, const polyq_dense* weight,
@@ -786,6 +794,7 @@ extern "C" int polyq_layernorm_forward(const polyq_dense* x, int64_t rows, int64
   if (!rc) rc = polyq_check_dense(y, K, who, "y");
   if (!rc && weight) rc = check_vector(weight, who, "weight");
   if (!rc && bias) rc = check_vector(bias, who, "bias");
+  if (!rc) rc = check_in_place(y, x, rows, who, "x and y");
   if (rc) return rc;
   if (!(eps >= 0.f) || !std::isfinite(eps)) return polyq_set_error(POLYQ_EINVAL, "%s: eps %g", who, (double)eps);
   if ((uintptr_t)stats % 8) return polyq_set_error(POLYQ_EINVAL, "%s: stats must be 8-byte aligned", who);
@@ -851,6 +860,8 @@ extern "C" int polyq_layernorm_backward(const polyq_dense* x, int64_t rows, int6
   if (!rc && weight) rc = check_vector(weight, who, "weight");
   if (!rc && dweight) rc = check_vector(dweight, who, "dweight");
   if (!rc && dbias) rc = check_vector(dbias, who, "dbias");
+  if (!rc) rc = check_in_place(dx, dy, rows, who, "dy and dx");
+  if (!rc) rc = check_in_place(dx, residual, rows, who, "the residual and dx");
   if (rc) return rc;
   if (!dx && !dweight && !dbias) return polyq_set_error(POLYQ_EINVAL, "%s: no gradient is wanted", who);
   if (dx && dx->type != x->type)
