@@ -100,7 +100,7 @@ typedef struct {
 } polyq_adamw_state;
 
 typedef struct {
-  double lr, beta1, beta2, eps; /* lr >= 0, 0 <= beta < 1, 0 < eps <= 1e30 */
+  double lr, beta1, beta2, eps; /* lr >= 0, 0 <= beta < 1, 2^-126 <= eps <= 1e30 */
   int64_t step;                 /* 1, 2, ...: this step's number */
   uint64_t seed;                /* of the rounding of 8-bit states: another one for each step, or the
                                    same elements are rounded the same way every time and small

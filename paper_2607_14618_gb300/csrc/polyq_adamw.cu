@@ -14,6 +14,7 @@
 // where the order of roundings allows (106 an element and 760 us one by one); 560 tensors, 62 M
 // elements, 258 us; 81 vectors of 5120 6 us, a launch.
 #include <algorithm>
+#include <cfloat>
 #include <cmath>
 #include <cstring>
 
@@ -257,7 +258,8 @@ __device__ __forceinline__ void update_block(const AdamParams<N>& P, const Tenso
     v[i] = sum_rn(mul2(b2, v[i]), mul2(mul2(c2, s), s));
     const float2 vs = of(v[i]), roots = make_float2(__fsqrt_rn(vs.x), __fsqrt_rn(vs.y));
     const F2 root = f2(roots.x, roots.y);
-    // (the denominator is eps or more, and at most 2^65 / (1 - b2^t): within the reciprocal's range)
+    // (the denominator is eps or more, a normal number, and at most 2^65 / (1 - b2^t): within the
+    // reciprocal's range, which takes subnormal numbers for 0)
     const float2 below = of(fma2(root, inv, eps));
     p2[i] = fma2(mul2(step, m[i]), f2(fp4::rcp_approx(below.x), fp4::rcp_approx(below.y)), mul2(p2[i], keep));
     if (BITS == 8) {
@@ -590,7 +592,7 @@ extern "C" int polyq_adamw_step(const polyq_adamw_tensor* tensors, int32_t n_ten
     return polyq_set_error(POLYQ_EINVAL, "%s: types %d and %d", who, p_type, grad_type);
   const polyq_adamw_hyper& h = *hyper;
   if (!(h.lr >= 0.0) || !std::isfinite((float)h.lr) || !(h.beta1 >= 0.0 && h.beta1 < 1.0) ||
-      !(h.beta2 >= 0.0 && h.beta2 < 1.0) || !((float)h.eps > 0.f) || !(h.eps <= 1e30) || h.step < 1)
+      !(h.beta2 >= 0.0 && h.beta2 < 1.0) || !((float)h.eps >= FLT_MIN) || !(h.eps <= 1e30) || h.step < 1)
     return polyq_set_error(POLYQ_EINVAL, "%s: lr %g, betas %g and %g, eps %g, step %lld", who, h.lr, h.beta1, h.beta2,
                            h.eps, (long long)h.step);
   if ((uintptr_t)h.lr_dev % 4 || (uintptr_t)h.step_dev % 8 || (uintptr_t)h.grad_scale % 4)

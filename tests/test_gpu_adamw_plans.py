@@ -43,3 +43,11 @@ def test_default_rounding_is_that_of_a_step_on_the_device(polyq_lib):
             plan.step(1e-3, torch.tensor([t], device="cuda") if on_device else t)
         out.append([s.m, s.v, s.m_scales, s.v_scales])
     assert all(torch.equal(a, b) for a, b in zip(*out))
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_smallest_eps(polyq_lib, bits):
+    """Where m and v are 0 a parameter only decays, with the smallest eps too."""
+    p, g = [torch.full((700,), 2.0, device="cuda")], [torch.zeros(700, device="cuda")]
+    polyq_lib.AdamW(p, g, polyq_lib.AdamState([700], bits), weight_decay=0.5).step(0.25, 1, eps=2.0 ** -126)
+    assert torch.equal(p[0], torch.full_like(p[0], 2.0 * (1 - 0.25 * 0.5)))
