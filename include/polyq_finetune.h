@@ -147,7 +147,8 @@ int polyq_adamw_values(const polyq_adamw_state* state, const polyq_dense* m, con
 
 /* n adapters beside a projection from K to N channels, in one 16-bit type (POLYQ_BF16 or
  * POLYQ_F16): a [n][R][K] and b [n][N][R], 16-byte aligned, rows of a_stride and b_stride
- * elements, a_next and b_next elements from one adapter to the next, all multiples of 8.
+ * elements, a_next and b_next elements from one adapter to the next, all multiples of 8 (many
+ * rows are fastest where a_next and b_next are 0 or multiples of the rows' stride that hold a matrix).
  * R is a multiple of 8 (above POLYQ_ADAPTERS_MAX_RANK POLYQ_EUNSUPPORTED); an adapter of a
  * smaller rank has it in `ranks`, and what a and b hold past it does not matter. */
 typedef struct {

@@ -62,6 +62,15 @@ int launch(const Kernel& k, int which, dim3 grid, int threads, int cluster, void
 // Rows of 16-bit elements that start on 16 bytes, as asynchronous copies want them.
 bool rows_on_16(const polyq_dense* d) { return (uintptr_t)d->data % 16 == 0 && d->stride % 8 == 0; }
 
+// Adapters, of `rows` rows each, that one tensor map describes: as the driver documents its strides, an
+// outer one is the inner one times the rows between, and below 2^40 bytes.  Others, as with one buffer
+// of each adapter's a and b, are copied in the ordinary way in tiles of 16 rows (4096 rows of rank 64
+// forward 97 us, 76 by the map; 6007 of rank 32: 114 and 70).  One matrix of all adapters (a stride of
+// 0) is a map of one, see ShrinkParams.
+bool mapped(const lora::Side& w, int64_t rows, int n) {
+  return n == 1 || w.next == 0 || (w.next % w.stride == 0 && w.next / w.stride >= rows && w.next < (1ll << 39));
+}
+
 int rank_tile(int R) { return R <= 16 ? 16 : R <= 32 ? 32 : R <= 64 ? 64 : 128; }
 int rank_index(int rn) { return rn == 16 ? 0 : rn == 32 ? 1 : rn == 64 ? 2 : 3; }
 
@@ -75,7 +84,7 @@ int shrink(const polyq_dense* x, int64_t T, int64_t K, const polyq_adapters* ad,
   const int rn = rank_tile(ad->R);
   const int64_t mean = T / seg.n;
   const bool any = !rows_on_16(x);
-  const int bm = any || mean <= 32 ? 16 : rn >= 64 && mean >= 256 ? 128 : 64;
+  const int bm = any || !mapped(w, trans ? K : ad->R, ad->n) || mean <= 32 ? 16 : rn >= 64 && mean >= 256 ? 128 : 64;
   const bool half = ad->type == POLYQ_F16;
   const Kernel k = half ? lora::shrink_of<__half>(bm, rn, trans, any) : lora::shrink_of<__nv_bfloat16>(bm, rn, trans, any);
   const int64_t tiles = most_tiles(T, seg.n, bm), stages = K / (bm == 128 ? 64 : 128);
@@ -101,8 +110,10 @@ int shrink(const polyq_dense* x, int64_t T, int64_t K, const polyq_adapters* ad,
                                          (uint32_t)bm);
     if (rc_x) return rc_x;
     const uint64_t cols = trans ? ad->R : K, rows = trans ? K : ad->R, stride = (uint64_t)w.stride * 2;
-    const int rc_w = polyq_tensor_map_3d(&P.w_map, w.w, cols, rows, (uint64_t)ad->n, stride,
-                                         ad->n > 1 ? (uint64_t)w.next * 2 : rows * stride,
+    const bool one = ad->n == 1 || w.next == 0;
+    P.map_next = !one;
+    const int rc_w = polyq_tensor_map_3d(&P.w_map, w.w, cols, rows, one ? 1 : (uint64_t)ad->n, stride,
+                                         one ? rows * stride : (uint64_t)w.next * 2,
                                          trans ? (uint32_t)std::min(rn, 64) : 64u,
                                          trans ? (uint32_t)(bm == 128 ? 64 : 128) : (uint32_t)rn);
     if (rc_w) return rc_w;

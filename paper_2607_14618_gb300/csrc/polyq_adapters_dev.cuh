@@ -379,6 +379,7 @@ struct ShrinkParams {
   Segments seg;
   int64_t x_stride, K;
   int32_t R, adapters, cluster;
+  int32_t map_next;          // 1; 0: all adapters are w_map's first
   CUtensorMap x_map, w_map;  // (shrink_tiled_kernel)
 };
 
@@ -577,6 +578,7 @@ __global__ void __launch_bounds__(kThreads + 32, RN == 128 ? 1 : BM == 64 && RN 
   if (warp == 8) {
     if (elect_one()) {
       int asked = 0;
+      const int which = t.id * P.map_next;
       for (int c = c0; c < c1; ++c, ++asked) {
         const int stage = asked % S::STAGES;
         const uint32_t bar = full + 8 * stage, at = base + stage * S::STAGE;
@@ -588,12 +590,12 @@ __global__ void __launch_bounds__(kThreads + 32, RN == 128 ? 1 : BM == 64 && RN 
 #pragma unroll
         for (int q = 0; q < S::PANELS; ++q) {
           tma_load_3d(at + q * BM * 128, &P.x_map, c * KC + q * 64, t.row, 0, bar);
-          if (!TRANS) tma_load_3d(at + S::X_BYTES + q * RN * 128, &P.w_map, c * KC + q * 64, 0, t.id, bar);
+          if (!TRANS) tma_load_3d(at + S::X_BYTES + q * RN * 128, &P.w_map, c * KC + q * 64, 0, which, bar);
         }
         if (TRANS)
 #pragma unroll
           for (int q = 0; q < (RN + 63) / 64; ++q)
-            tma_load_3d(at + S::X_BYTES + q * KC * 128, &P.w_map, q * 64, c * KC, t.id, bar);
+            tma_load_3d(at + S::X_BYTES + q * KC * 128, &P.w_map, q * 64, c * KC, which, bar);
       }
       // no copy is under way when the block ends, whether its stages were awaited or not
       for (int i = asked > S::STAGES ? asked - S::STAGES : 0; i < asked; ++i)
