@@ -1317,7 +1317,12 @@ class AdamW:
 
     params, grads: contiguous CUDA tensors (fp32, bf16 or fp16) of the sizes of
     `state`; copies: None or tensors (or None) that receive the new parameters in
-    another type; weight_decay, lr_scale: a number, or one for each tensor."""
+    another type; weight_decay, lr_scale: a number, or one for each tensor.
+
+    The plan keeps the memory that it has laid out alive and goes on with that memory,
+    also where a tensor is given another.  Where grads[i] is params[i].grad, that has
+    to stay (or share) this memory, or step() raises ValueError: gradients are set to zero in place
+    (zero_grad(set_to_none=False)), or a new plan is made, with the same state."""
 
     def __init__(self, params, grads, state, copies=None, weight_decay=0.01, lr_scale=1.0):
         params, grads = list(params), list(grads)
@@ -1330,7 +1335,6 @@ class AdamW:
             raise ValueError("params, grads, copies, weight_decay and lr_scale must be as many as "
                              "the state's tensors")
         self.state, self._groups = state, {}
-        self._kept = (params, grads, copies)
         dev = self._dev = params[0].get_device() if hasattr(params[0], "get_device") else -1
         groups = {}
         for i in range(n):
@@ -1355,6 +1359,9 @@ class AdamW:
                 state.offsets[i], decay[i], rate[i]))
         if state.device_index != dev:
             raise ValueError(f"the state is not on cuda:{dev}, the device of params[0]")
+        # (tensors of its own: what a caller's tensor refers to may change)
+        self._kept = [t.detach() for t in (*params, *grads, *copies) if t is not None]
+        self._own_grads = [(p, g, g.data_ptr()) for p, g in zip(params, grads) if p.is_leaf and p.grad is g]
         self._state_ref = C.byref(state.desc)
         self._groups = [(*k, (AdamwTensor * len(v))(*v), len(v)) for k, v in groups.items()]
 
@@ -1373,6 +1380,10 @@ class AdamW:
         same way every time, and small moments never change); by default the step's number,
         wherever that is."""
         st = _stream_on(self._dev, "the tensors", stream)
+        for p, g, at in self._own_grads:
+            if p.grad is not g and (p.grad is None or p.grad.data_ptr() != at):
+                raise ValueError("a parameter's .grad is no longer what this plan was made with; "
+                                 "zero gradients in place (set_to_none=False) or make a new plan")
         lr_dev = step_dev = scale = 0
         if hasattr(lr, "data_ptr"):
             lr_dev, lr = self._scalar(lr, "lr", T_F32), 0.0

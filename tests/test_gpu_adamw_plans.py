@@ -51,3 +51,53 @@ def test_smallest_eps(polyq_lib, bits):
     p, g = [torch.full((700,), 2.0, device="cuda")], [torch.zeros(700, device="cuda")]
     polyq_lib.AdamW(p, g, polyq_lib.AdamState([700], bits), weight_decay=0.5).step(0.25, 1, eps=2.0 ** -126)
     assert torch.equal(p[0], torch.full_like(p[0], 2.0 * (1 - 0.25 * 0.5)))
+
+
+def test_replaced_gradients_are_refused(polyq_lib):
+    """A plan over parameters' own .grad does not go on with gradients that have been replaced."""
+    ps = [torch.ones(300, device="cuda", requires_grad=True) for _ in range(3)]
+
+    def backward():
+        sum((k + 1) * p.sum() for k, p in enumerate(ps)).backward()
+
+    def plan():
+        return polyq_lib.AdamW(ps, [p.grad for p in ps], state)
+
+    state = polyq_lib.AdamState([300] * 3)
+    opt = torch.optim.SGD(ps)
+    backward()
+    adam = plan()
+    adam.step(1e-3, 1)
+    opt.zero_grad(set_to_none=False)
+    ps[1].grad = ps[1].grad.view(300)  # (the same memory)
+    backward()
+    adam.step(1e-3, 2)
+    before = [p.detach().clone() for p in ps] + [state.m.clone()]
+    opt.zero_grad()  # to None
+    for make in (lambda: None, backward):
+        make()
+        with pytest.raises(ValueError, match="no longer"):
+            adam.step(1e-3, 3)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(before, [p.detach() for p in ps] + [state.m]))
+    plan().step(1e-3, 3)
+    assert all((p.detach() < b).all() for p, b in zip(ps, before))
+    # gradients beside .grad are the caller's own
+    mine = [torch.ones(300, device="cuda") for _ in ps]
+    adam = polyq_lib.AdamW(ps, mine, state)
+    opt.zero_grad()
+    adam.step(1e-3, 4)
+
+
+def test_a_plan_keeps_its_memory(polyq_lib):
+    """Tensors that are given other memory leave the plan with what it has laid out."""
+    n = 1 << 20
+    p, g, c = (torch.ones(n, device="cuda", dtype=t) for t in (torch.float32, torch.float32, torch.bfloat16))
+    old = [t.data_ptr() for t in (p, g, c)]
+    adam = polyq_lib.AdamW([p], [g], polyq_lib.AdamState([n]), copies=[c])
+    for t in (p, g, c):
+        t.data = torch.full_like(t, 5)
+    others = [torch.full((n,), 7, device="cuda", dtype=t) for _ in range(4) for t in (torch.float32, torch.bfloat16)]
+    assert not {t.data_ptr() for t in others} & set(old)
+    adam.step(1e-3, 1)
+    assert all((t == 7).all() for t in others) and all((t == 5).all() for t in (p, g, c))
