@@ -1357,6 +1357,10 @@ class AdamW:
                 params[i].data_ptr(), grads[i].data_ptr(),
                 None if copies[i] is None else copies[i].data_ptr(), state.sizes[i],
                 state.offsets[i], decay[i], rate[i]))
+        written = sorted((t.data_ptr(), t.numel() * t.element_size()) for t in (*params, *copies) if t is not None)
+        if any(at + size > behind for (at, size), (behind, _) in zip(written, written[1:])):
+            raise ValueError("two of params and copies share memory; a tensor that is used twice is one "
+                             "parameter, with the sum of its gradients")
         if state.device_index != dev:
             raise ValueError(f"the state is not on cuda:{dev}, the device of params[0]")
         # (tensors of its own: what a caller's tensor refers to may change)

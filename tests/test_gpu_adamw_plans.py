@@ -101,3 +101,15 @@ def test_a_plan_keeps_its_memory(polyq_lib):
     assert not {t.data_ptr() for t in others} & set(old)
     adam.step(1e-3, 1)
     assert all((t == 7).all() for t in others) and all((t == 5).all() for t in (p, g, c))
+
+
+def test_shared_memory_is_refused(polyq_lib):
+    """Two updates of one element at the same time would give either's result."""
+    buf, g = torch.ones(1000, device="cuda"), [torch.ones(300, device="cuda") for _ in range(2)]
+    state = polyq_lib.AdamState([300] * 2)
+    for ps, cs in (([buf[:300]] * 2, None), ([buf[:300], buf[299:599]], None), ([buf[600:900], buf[:300]], [buf[500:800], None]),
+                   ([buf[:300], buf[300:600]], [buf[600:900], buf[600:900]])):
+        with pytest.raises(ValueError, match="share memory"):
+            polyq_lib.AdamW(ps, g, state, copies=cs)
+    polyq_lib.AdamW([buf[300:600], buf[:300]], g, state, copies=[None, buf[600:900]]).step(1e-3, 1)
+    assert (buf[:900] < 1).all() and (buf[900:] == 1).all()
