@@ -113,3 +113,12 @@ def test_shared_memory_is_refused(polyq_lib):
             polyq_lib.AdamW(ps, g, state, copies=cs)
     polyq_lib.AdamW([buf[300:600], buf[:300]], g, state, copies=[None, buf[600:900]]).step(1e-3, 1)
     assert (buf[:900] < 1).all() and (buf[900:] == 1).all()
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("value", [float("inf"), float("-inf"), float("nan")])
+def test_a_gradient_that_is_not_finite_reaches_its_own_parameter(polyq_lib, bits, value):
+    p, g = [torch.ones(600, device="cuda")], [torch.full((600,), 1e-2, device="cuda")]
+    g[0][300] = value
+    polyq_lib.AdamW(p, g, polyq_lib.AdamState([600], bits)).step(1e-3, 1)
+    assert (~torch.isfinite(p[0])).nonzero().flatten().tolist() == [300]
