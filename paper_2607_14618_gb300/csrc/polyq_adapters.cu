@@ -158,6 +158,24 @@ int expand(const float* v, int64_t T, int64_t N, const polyq_adapters* ad, bool 
                 who);
 }
 
+// Blocks that share the rows of each of `used` adapters (at most), of `columns` tiles.  More of them
+// are worth their exchange where each still has 512 rows of rank 16 or 1024 of a wider one and all of
+// them fit at once; two of 2048 rows, where one has a second round that is nearly empty.  us with one,
+// two, four and eight:
+//   5120 x 5120, rank 64 (80 blocks), 512 rows 28 30 44 84, 2048 rows 84 58 63 90;
+//   1024 x 1024, rank 16 (16), 512 rows 12 11 10 10, 4096 rows 63 39 23 19;
+//   four adapters of it, rank 64 (64), 1024 rows of each 46 38 46 71;
+//   5120 x 5120, rank 128 (160 on 152 SMs), 1024 rows 72 75 94 165, 4096 rows 228 201 207 292;
+//   5120 + 13824 of two adapters, rank 64 (296), 4096 rows 110 124 184 319.
+int gradient_cluster(int64_t T, int64_t used, int64_t columns, int rn, int sms) {
+  const int64_t blocks = used * columns, slots = (int64_t)sms * (rn == 16 ? 3 : rn <= 64 ? 2 : 1);
+  const int64_t each = T / used;
+  if (rn > 16 && blocks > slots && 4 * blocks < 5 * slots && each >= 2048) return 2;
+  int c = 1;
+  while (c < lora::kMaxCluster && each >= (rn == 16 ? 512 : 1024) * c && 2 * c * blocks <= slots) c *= 2;
+  return c;
+}
+
 int check(const polyq_dense* x, int64_t T, const polyq_adapters* ad, const polyq_segments* s, const char* who) {
   if (!ad || !s) return polyq_set_error(POLYQ_EINVAL, "%s: adapters or segments are NULL", who);
   if (T < 1 || T > kMaxSize || ad->K < 1 || ad->K > kMaxSize || ad->N < 1 || ad->N > kMaxSize)
@@ -289,8 +307,7 @@ extern "C" int polyq_adapters_backward(const polyq_dense* x, int64_t T, const po
     G.ranks = adapters->ranks;
     G.seg = seg;
     G.R = adapters->R;
-    G.cluster = 1;
-    while (G.cluster < lora::kMaxCluster && blocks * G.cluster < 2 * sms && T >= 128 * G.cluster) G.cluster *= 2;
+    G.cluster = gradient_cluster(T, std::min(adapters->n, segments->n), G.side[0].tiles + G.side[1].tiles, rn, sms);
     const bool any = (da && !rows_on_16(x)) || (db && !rows_on_16(dy));
     const Kernel k = half ? lora::gradients_of<__half>(rn, any) : lora::gradients_of<__nv_bfloat16>(rn, any);
     rc = launch(k, 256 + (any * 2 + half) * 4 + rank_index(rn), dim3((unsigned)(blocks * G.cluster)), lora::kThreads,
