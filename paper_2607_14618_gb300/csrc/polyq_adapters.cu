@@ -84,7 +84,16 @@ int shrink(const polyq_dense* x, int64_t T, int64_t K, const polyq_adapters* ad,
   const int rn = rank_tile(ad->R);
   const int64_t mean = T / seg.n;
   const bool any = !rows_on_16(x);
-  const int bm = any || !mapped(w, trans ? K : ad->R, ad->n) || mean <= 32 ? 16 : rn >= 64 && mean >= 256 ? 128 : 64;
+  // Rows of a tile, by the segments' mean (us of whole calls with both).
+  // 16 and 64: rank 16, 200 segments of 24 rows of 5120 columns 34 and 24, one of 8 7.7 and 6.7; rank 32, 48
+  // of 13824 columns, of 8 rows 18.8 and 20.1, of 16 21.5 and 20.7, of 31 39 and 32; rank 64, 48 of 5120
+  // columns, of 32 rows 33 and 37, of 48 41 and 36.
+  // 64 and 128, worth it where 64-row tiles in clusters of eight are more than fit at once: rank 64, four of
+  // 13824 columns, of 512 rows 24 and 33, of 1024 46 and 40; rank 128, 5120 columns, 512 rows 14 and 19, 1024
+  // 25 and 21, 16 segments of 512 80 and 66 (but of 256 44 and 56).
+  const bool few = mean <= (rn <= 32 ? 16 : 32);
+  const bool many = rn >= 64 && mean >= 256 && T >= (rn == 64 ? 16 : 6) * (int64_t)sms;
+  const int bm = any || !mapped(w, trans ? K : ad->R, ad->n) || few ? 16 : many ? 128 : 64;
   const bool half = ad->type == POLYQ_F16;
   const Kernel k = half ? lora::shrink_of<__half>(bm, rn, trans, any) : lora::shrink_of<__nv_bfloat16>(bm, rn, trans, any);
   const int64_t tiles = most_tiles(T, seg.n, bm), stages = K / (bm == 128 ? 64 : 128);
@@ -127,6 +136,8 @@ int shrink(const polyq_dense* x, int64_t T, int64_t K, const polyq_adapters* ad,
 int expand(const float* v, int64_t T, int64_t N, const polyq_adapters* ad, bool trans, const lora::Side& w,
            const float* scales, const lora::Segments& seg, const polyq_dense* residual, const polyq_dense* y, int sms,
            void* stream, const char* who) {
+  // (Tiles of 16 against 64 rows, us: rank 64 onto 13824, 32 segments of 32 rows 40 and 42, of 48 50 and 50,
+  // of 64 65 and 56; rank 16 onto 5120, of 32 17 and 20, of 64 26 and 25.)
   const int rn = rank_tile(ad->R), bm = T / seg.n <= 32 ? 16 : 64, bn = rn == 128 && bm == 64 ? 64 : 128;
   const bool half = ad->type == POLYQ_F16, f32 = y->type == POLYQ_F32;
   const Kernel k = half ? lora::expand_of<__half>(bm, rn, trans, f32) : lora::expand_of<__nv_bfloat16>(bm, rn, trans, f32);
@@ -160,18 +171,20 @@ int expand(const float* v, int64_t T, int64_t N, const polyq_adapters* ad, bool 
 
 // Blocks that share the rows of each of `used` adapters (at most), of `columns` tiles.  More of them
 // are worth their exchange where each still has 512 rows of rank 16 or 1024 of a wider one and all of
-// them fit at once; two of 2048 rows, where one has a second round that is nearly empty.  us with one,
-// two, four and eight:
+// them fit at once; two of twice these rows also where they do not quite, as the adapters' rows are
+// uneven, or (of one adapter) where one has a second round that is nearly empty.  us with one, two,
+// four and eight:
 //   5120 x 5120, rank 64 (80 blocks), 512 rows 28 30 44 84, 2048 rows 84 58 63 90;
 //   1024 x 1024, rank 16 (16), 512 rows 12 11 10 10, 4096 rows 63 39 23 19;
 //   four adapters of it, rank 64 (64), 1024 rows of each 46 38 46 71;
 //   5120 x 5120, rank 128 (160 on 152 SMs), 1024 rows 72 75 94 165, 4096 rows 228 201 207 292;
-//   5120 + 13824 of two adapters, rank 64 (296), 4096 rows 110 124 184 319.
+//   5120 + 13824 of two adapters, rank 64 (296), 4096 rows, halves 110 124 184 319, uneven 141 136 196 322,
+//   8192 uneven 232 205 270 412, 2048 83 91 151 280.
 int gradient_cluster(int64_t T, int64_t used, int64_t columns, int rn, int sms) {
   const int64_t blocks = used * columns, slots = (int64_t)sms * (rn == 16 ? 3 : rn <= 64 ? 2 : 1);
   const int64_t each = T / used;
-  if (rn > 16 && blocks > slots && 4 * blocks < 5 * slots && each >= 2048) return 2;
-  int c = 1;
+  const bool two = used > 1 ? 2 * blocks < 5 * sms : blocks > slots && 4 * blocks < 5 * slots;
+  int c = two && each >= (rn <= 32 ? 1024 : 2048) ? 2 : 1;
   while (c < lora::kMaxCluster && each >= (rn == 16 ? 512 : 1024) * c && 2 * c * blocks <= slots) c *= 2;
   return c;
 }
