@@ -34,12 +34,16 @@ namespace {
 using namespace polyq;
 
 constexpr int kMaxCluster = 8;
-// Backward: rows of up to kNarrow columns take eight a thread (8192 x 5120 bf16 80 us, 98 with
-// sixteen), wider ones sixteen in up to kWideThreads; small rows share up to kNarrowThreads.
-constexpr int kNarrow = 5120, kNarrowThreads = 256, kWideThreads = 512;
+// Backward: warps of an SM, whose four parts have 16384 registers each.  Rows that a thread takes
+// together once there are enough.
+constexpr int kBackwardRegs = 96, kBackwardWarps = 4 * (16384 / (32 * kBackwardRegs)), kTogether = 2;
+// Rows that these warps hold with eight columns a thread take eight, wider ones sixteen, in up to
+// kWideThreads, which read hat and dy w twice (with a residual, as wide as 42 M elements of bf16, eight
+// and sixteen: 1024, 2048, 4096 and 4608 columns 69 to 72 and 107 to 110 us, 5120 68 and 102; fp32 97 to 102 and
+// 104 to 108; 21 warps, for 5376 columns, do not launch); small rows share up to kNarrowThreads.
+constexpr int kNarrow = 8 * 32 * kBackwardWarps, kNarrowThreads = 256, kWideThreads = 512;
 constexpr int kReduceCols = 32, kReduceRows = 16;
-// Threads of an SM, as registers allow, and rows that a thread takes together once there are enough.
-constexpr int kBackwardRegs = 96, kBackwardPerSm = 65536 / kBackwardRegs, kTogether = 2;
+constexpr int kBackwardPerSm = 32 * kBackwardWarps;
 constexpr int kMostSmem = 200 << 10;
 constexpr int kSmSmem = 226 << 10, kStaticSmem = 14 << 10;  // of an SM; of a backward block, beside its rows
 
