@@ -393,9 +393,7 @@ struct Shrink {
   static_assert(BM == 16, "tiles of few rows");
   static constexpr int KC = 128;                  // contraction of a stage
   static constexpr int STAGES = RN == 64 ? 3 : 4;  // (three blocks to an SM)
-  // warps along the rows, the rank and the contraction of a stage
-  static constexpr int WM = 1, WN = RN / 16, WK = 8 / WN;
-  static constexpr int MT = 1, NT = 2;
+  static constexpr int WN = RN / 16, WK = 8 / WN;  // warps along the rank (16 each) and the contraction of a stage
   static constexpr int X_BYTES = BM * KC * 2, W_BYTES = RN * KC * 2;
   static constexpr int RED_BYTES = WK * BM * RN * 4;
   static constexpr int SMEM = STAGES * (X_BYTES + W_BYTES) > RED_BYTES ? STAGES * (X_BYTES + W_BYTES) : RED_BYTES;
@@ -471,8 +469,8 @@ __global__ void __launch_bounds__(kThreads) shrink_kernel(const __grid_constant_
     mw.copy(base + stage * (S::X_BYTES + S::W_BYTES) + S::X_BYTES, c * (TRANS ? P.w.stride * KC * 2 : KC * 2),
             TRANS ? left : own);
   };
-  float acc[S::MT][S::NT][4] = {};
-  const int wm = warp % S::WM, wn = warp / S::WM % S::WN, wk = warp / (S::WM * S::WN);
+  float acc[2][4] = {};
+  const int wn = warp % S::WN, wk = warp / S::WN;
   for (int i = 0; i < S::STAGES - 1; ++i) {
     if (c0 + i < c1) copy_w(c0 + i, i);
     cp_commit();  // (the first with all that x has asked for)
@@ -489,41 +487,29 @@ __global__ void __launch_bounds__(kThreads) shrink_kernel(const __grid_constant_
     cp_commit();
     const uint32_t at = base + stage * (S::X_BYTES + S::W_BYTES);
     if (++stage == S::STAGES) stage = 0;
-    float sum[S::MT][S::NT][4] = {};  // of the stage: the tensor cores cut running sums off
+    float sum[2][4] = {};  // of the stage: the tensor cores cut running sums off
 #pragma unroll
     for (int k = wk * 16; k < KC; k += 16 * S::WK) {
-      uint32_t a[S::MT][4];
-#pragma unroll
-      for (int i = 0; i < S::MT; ++i) frag_a<CX, false>(at, (wm * S::MT + i) * 16, k, a[i]);
-#pragma unroll
-      for (int j = 0; j < S::NT; j += 2) {
-        uint32_t b[4];
-        frag_b<CW, TRANS>(at + S::X_BYTES, (wn * S::NT + j) * 8, k, b);
-#pragma unroll
-        for (int i = 0; i < S::MT; ++i) {
-          mma<T>(sum[i][j], a[i], b[0], b[1]);
-          mma<T>(sum[i][j + 1], a[i], b[2], b[3]);
-        }
-      }
+      uint32_t a[4], b[4];
+      frag_a<CX, false>(at, 0, k, a);
+      frag_b<CW, TRANS>(at + S::X_BYTES, wn * 16, k, b);
+      mma<T>(sum[0], a, b[0], b[1]);
+      mma<T>(sum[1], a, b[2], b[3]);
     }
 #pragma unroll
-    for (int i = 0; i < S::MT; ++i)
+    for (int j = 0; j < 2; ++j)
 #pragma unroll
-      for (int j = 0; j < S::NT; ++j)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) acc[i][j][e] += sum[i][j][e];
+      for (int e = 0; e < 4; ++e) acc[j][e] += sum[j][e];
   }
   cp_wait<0>();
   __syncthreads();
   float* red = reinterpret_cast<float*>(smem) + wk * BM * RN;
 #pragma unroll
-  for (int i = 0; i < S::MT; ++i)
-#pragma unroll
-    for (int j = 0; j < S::NT; ++j) {
-      const int row = (wm * S::MT + i) * 16 + lane / 4, col = (wn * S::NT + j) * 8 + lane % 4 * 2;
-      *reinterpret_cast<float2*>(red + row * RN + col) = make_float2(acc[i][j][0], acc[i][j][1]);
-      *reinterpret_cast<float2*>(red + (row + 8) * RN + col) = make_float2(acc[i][j][2], acc[i][j][3]);
-    }
+  for (int j = 0; j < 2; ++j) {
+    const int row = lane / 4, col = wn * 16 + j * 8 + lane % 4 * 2;
+    *reinterpret_cast<float2*>(red + row * RN + col) = make_float2(acc[j][0], acc[j][1]);
+    *reinterpret_cast<float2*>(red + (row + 8) * RN + col) = make_float2(acc[j][2], acc[j][3]);
+  }
   shrink_finish<BM, RN, S::WK>(P, t, base, smem, rank);
 }
 
@@ -578,7 +564,6 @@ __global__ void __launch_bounds__(kThreads + 32, RN == 128 ? 1 : BM == 64 && RN 
   if (warp == 8) {
     if (elect_one()) {
       int asked = 0;
-      const int which = t.id * P.map_next;
       for (int c = c0; c < c1; ++c, ++asked) {
         const int stage = asked % S::STAGES;
         const uint32_t bar = full + 8 * stage, at = base + stage * S::STAGE;
@@ -590,12 +575,12 @@ __global__ void __launch_bounds__(kThreads + 32, RN == 128 ? 1 : BM == 64 && RN 
 #pragma unroll
         for (int q = 0; q < S::PANELS; ++q) {
           tma_load_3d(at + q * BM * 128, &P.x_map, c * KC + q * 64, t.row, 0, bar);
-          if (!TRANS) tma_load_3d(at + S::X_BYTES + q * RN * 128, &P.w_map, c * KC + q * 64, 0, which, bar);
+          if (!TRANS) tma_load_3d(at + S::X_BYTES + q * RN * 128, &P.w_map, c * KC + q * 64, 0, t.id * P.map_next, bar);
         }
         if (TRANS)
 #pragma unroll
           for (int q = 0; q < (RN + 63) / 64; ++q)
-            tma_load_3d(at + S::X_BYTES + q * KC * 128, &P.w_map, q * 64, c * KC, which, bar);
+            tma_load_3d(at + S::X_BYTES + q * KC * 128, &P.w_map, q * 64, c * KC, t.id * P.map_next, bar);
       }
       // no copy is under way when the block ends, whether its stages were awaited or not
       for (int i = asked > S::STAGES ? asked - S::STAGES : 0; i < asked; ++i)

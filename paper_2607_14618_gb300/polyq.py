@@ -1431,15 +1431,13 @@ def _adapters(x, K, ty, a, b, offsets, ids, scales, ranks, dev):
         an, ar, a1 = a.stride()
         bn, br, b1 = b.stride()
         good = (a.dtype == b.dtype == x.dtype and a.get_device() == b.get_device() == dev and nb == n
-                and rb == R and ka == K and (a1 == 1 or K == 1) and (b1 == 1 or R == 1)
+                and rb == R and ka == K and (a1 == 1 or K == 1) and b1 == 1
                 and (ty == T_BF16 or ty == T_F16))
     except (AttributeError, ValueError):
         good = False
     if not good:
         raise ValueError(f"a and b must be tensors [n][R][{K}] and [n][N][R] with contiguous rows of "
                          f"x's type, bf16 or fp16, on cuda:{dev}")
-    if R == 1 and ar < K:
-        ar = K
     if N == 1 and br < R:
         br = R
     if n == 1:  # (one adapter: the stride to the next does not matter)
