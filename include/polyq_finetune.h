@@ -150,7 +150,10 @@ int polyq_adamw_values(const polyq_adamw_state* state, const polyq_dense* m, con
  * elements, a_next and b_next elements from one adapter to the next, all multiples of 8 (many
  * rows are fastest where a_next and b_next are 0 or multiples of the rows' stride that hold a matrix).
  * R is a multiple of 8 (above POLYQ_ADAPTERS_MAX_RANK POLYQ_EUNSUPPORTED); an adapter of a
- * smaller rank has it in `ranks`, and what a and b hold past it does not matter. */
+ * smaller rank has it in `ranks`, and what a and b hold past it does not matter.
+ * Beside a layer of polyq.h, a's columns are in the order of the x that both read (the layer
+ * gathers by itself), and b's rows in that of the y that it emits: the channels' own, or that of
+ * polyq_layer_permute_rows, whose permutation b's rows then take as well. */
 typedef struct {
   const void* a;
   const void* b;

@@ -1458,9 +1458,10 @@ def adapters_forward(x, a, b, offsets, ids, scales=None, ranks=None, residual=No
     the residual) of a [n][R][K] and b [n][N][R].  R is a multiple of 8 up to 128; `ranks`
     holds smaller ranks, `scales` a factor per adapter.  offsets, ids and ranks are int32,
     scales fp32, all on the device and read when the call runs.  residual: the shared
-    projection's result, of y's type (x's or fp32), may be y itself.  Rows of no segment are
-    left as they were: without a `y` they are not set.  `saved` (adapters_saved) receives what
-    adapters_backward needs."""
+    projection's result, of y's type (x's or fp32), may be y itself.  a's columns are in x's
+    order and b's rows in y's: beside a layer whose rows HostLayer.permute_rows has reordered,
+    b's rows take the same permutation.  Rows of no segment are left as they were: without a
+    `y` they are not set.  `saved` (adapters_saved) receives what adapters_backward needs."""
     px, sx, tx, T, K, dev = _rows(x, "x")
     st = _stream_on(dev, "x", stream)
     d, s, _, R, N = _adapters(x, K, tx, a, b, offsets, ids, scales, ranks, dev)
