@@ -11,7 +11,7 @@
  * owns every buffer, entry points check their arguments on the host, never
  * allocate device memory and never synchronise, `stream` is a cudaStream_t.
  * Every entry works on the current device and may be captured in a CUDA graph.
- * Sizes are at least 1: an empty tensor is POLYQ_EINVAL.  Outputs must not
+ * Sizes are at least 1 (an empty tensor is POLYQ_EINVAL), rows and widths at most 2^24.  Outputs must not
  * overlap inputs or each other unless stated otherwise.  A workspace may serve
  * consecutive calls on one stream, but not calls that run at the same time.  Results do not change from run to run.
  */

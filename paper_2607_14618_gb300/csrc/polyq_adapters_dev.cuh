@@ -207,8 +207,8 @@ struct Tile {
 };
 // Tile number `tile` of all segments' in turn (the whole block calls; false: there are
 // fewer).  Offsets outside the tensors' rows are held at their ends.  One warp looks: every
-// block reads the same few lines, and with all warps at it the lines' slice of L2 was
-// what 48 rows of rank 64 waited for (41 us, 30 with fewer requests).
+// block reads the same few lines (48 rows of rank 64 27 us; 29 where every warp looks for itself,
+// and 41 with four neighbouring segments a lane of those).
 __device__ __forceinline__ bool find_tile(const Segments& s, int bm, int tile, Tile& t) {
   __shared__ Tile found;
   const int lane = threadIdx.x & 31;

@@ -14,9 +14,10 @@
 // them (fp32 3551 x 11811, training: 330 us, 508 with element loads).
 //
 // Measured, forward and backward with the residual gradient (by the profiler, operands from
-// HBM): 8192 x 5120 bf16 33 + 64 + 4.5 us, 5.1 and 5.2 TB/s, bound by instructions: 20 for an
-// element forward, 38 backward, in packed fp32 pairs (61% of the issue slots backward).
-// 777 x 5003 fp16: 12.6 + 16.7 + 4.7 us, bound by the latency of three launches.  One row:
+// HBM): RMS norm of 8192 x 5120 bf16 33 + 64 + 4.5 us, 5.1 and 5.2 TB/s, bound by latency at the
+// warps that registers leave room for: 38 instructions for an element backward, in packed fp32
+// pairs, by 20 warps an SM that fill 66% of the issue slots; 17 forward (with mean and bias), by 28
+// warps that fill 57% (shared memory, the row's barrier).  777 x 5003 fp16: 12.6 + 16.7 + 4.7 us, bound by the latency of three launches.  One row:
 // 3.2 us, a launch.
 #include <algorithm>
 #include <atomic>
