@@ -62,7 +62,7 @@ int launch(const Kernel& k, int which, dim3 grid, int threads, int cluster, void
 // Rows of 16-bit elements that start on 16 bytes, as asynchronous copies want them.
 bool rows_on_16(const polyq_dense* d) { return (uintptr_t)d->data % 16 == 0 && d->stride % 8 == 0; }
 
-// Adapters, of `rows` rows each, that one tensor map describes: as the driver documents its strides, an
+// Adapters, of `rows` rows each, that one tensor map describes: as the CUDA API documents its strides, an
 // outer one is the inner one times the rows between, and below 2^40 bytes.  Others, as with one buffer
 // of each adapter's a and b, are copied in the ordinary way in tiles of 16 rows (4096 rows of rank 64
 // forward 97 us, 76 by the map; 6007 of rank 32: 114 and 70).  One matrix of all adapters (a stride of

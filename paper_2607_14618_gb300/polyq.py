@@ -1336,7 +1336,7 @@ class AdamW:
                              "the state's tensors")
         self.state, self._groups = state, {}
         dev = self._dev = params[0].get_device() if hasattr(params[0], "get_device") else -1
-        groups = {}
+        groups, written = {}, []
         for i in range(n):
             types = []
             for name, t in (("params", params[i]), ("grads", grads[i]), ("copies", copies[i])):
@@ -1353,18 +1353,21 @@ class AdamW:
                     raise ValueError(f"{name}[{i}] must be a contiguous fp32, bf16 or fp16 tensor of "
                                      f"{state.sizes[i]} elements on the device of params[0], a CUDA one")
                 types.append(ty)
+            size, pp, pc = state.sizes[i], params[i].data_ptr(), None
+            written.append((pp, pp + size * (4 if types[0] == T_F32 else 2)))
+            if copies[i] is not None:
+                pc = copies[i].data_ptr()
+                written.append((pc, pc + size * (4 if types[2] == T_F32 else 2)))
             groups.setdefault(tuple(types), []).append(AdamwTensor(
-                params[i].data_ptr(), grads[i].data_ptr(),
-                None if copies[i] is None else copies[i].data_ptr(), state.sizes[i],
-                state.offsets[i], decay[i], rate[i]))
-        written = sorted((t.data_ptr(), t.numel() * t.element_size()) for t in (*params, *copies) if t is not None)
-        if any(at + size > behind for (at, size), (behind, _) in zip(written, written[1:])):
+                pp, grads[i].data_ptr(), pc, size, state.offsets[i], decay[i], rate[i]))
+        written.sort()
+        if any(end > at for (_, end), (at, _) in zip(written, written[1:])):
             raise ValueError("two of params and copies share memory; a tensor that is used twice is one "
                              "parameter, with the sum of its gradients")
         if state.device_index != dev:
             raise ValueError(f"the state is not on cuda:{dev}, the device of params[0]")
-        # (tensors of its own: what a caller's tensor refers to may change)
-        self._kept = [t.detach() for t in (*params, *grads, *copies) if t is not None]
+        # (the memory itself: what a caller's tensor refers to may change)
+        self._kept = [t.untyped_storage() for t in (*params, *grads, *copies) if t is not None]
         self._own_grads = [(p, g, g.data_ptr()) for p, g in zip(params, grads) if p.is_leaf and p.grad is g]
         self._state_ref = C.byref(state.desc)
         self._groups = [(*k, (AdamwTensor * len(v))(*v), len(v)) for k, v in groups.items()]
